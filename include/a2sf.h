@@ -344,6 +344,147 @@ int a2sf_ideal_similarity(a2sf_cache *cache, float alpha, int32_t n,
                           void *out, float *cos_out, int32_t *evicted_opt,
                           void *workspace, size_t workspace_bytes, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * Rotary positions.  A pair (x1, x2) of a row at position p is turned by the angle
+ * p * f_k:  y1 = m (x1 cos - x2 sin),  y2 = m (x2 cos + x1 sin), k = 0 .. rotary_dim/2 - 1,
+ * f_k = theta^(-2k / rotary_dim) before scaling.  Pairs are (k, k + rotary_dim/2), or the
+ * neighbours (2k, 2k+1) with `interleaved`.  Elements from rotary_dim on are copied.
+ *
+ * a2sf_rotary_plan_init (host only) turns a configuration into a plan, which the caller keeps:
+ * f_k / 2 pi as a 64-bit fixed-point fraction of a turn, so that  p * f_k  modulo one turn is
+ * exact integer arithmetic on the device however far the position is.
+ *   scaling LINEAR: f / factor.   NTK: theta * factor^(r / (r - 2)) instead of theta.
+ *   BANDS: by wavelength 2 pi / f against the original length L: shorter than L / high is kept,
+ *          longer than L / low is divided by factor, linear in L / wavelength between.
+ *   RAMP : interpolation by parts (YaRN): the dimension at which `high` (beta fast) turns fit
+ *          into L up to the one for `low` (beta slow), linear in the pair index between; the
+ *          default magnitude is 0.1 ln(factor) + 1.
+ *   magnitude: m; 0 selects the default (1 except for RAMP).
+ * Accepted: even 2 <= rotary_dim <= 128 (NTK: >= 4), theta > 1, factor >= 1, and for BANDS and
+ * RAMP original_length >= 1 and 0 < low < high.  INVALID_ARG otherwise.
+ *
+ * a2sf_rotary: x -> y, [B][H][n][d] in `dtype` with element strides of their own, d in {64, 128}
+ * and >= rotary_dim.  y may be x itself (same strides); otherwise they must not overlap.  Row t of
+ * sequence b stands at positions[b][t] (DEVICE [B][n] int32), or at start[b] + t (DEVICE [B]; NULL:
+ * t) when `positions` is NULL.  lens (DEVICE [B] or NULL): rows t >= lens[b] of y are left as they
+ * were.  flags: 0 or A2SF_ROTARY_TRANSPOSE, which applies the transposed matrix: the gradient of
+ * the rotation, and for m = 1 its inverse.  Angles have an absolute error below 2e-7.
+ * ------------------------------------------------------------------------- */
+typedef enum {
+    A2SF_ROTARY_PLAIN = 0, A2SF_ROTARY_LINEAR = 1, A2SF_ROTARY_NTK = 2, A2SF_ROTARY_BANDS = 3, A2SF_ROTARY_RAMP = 4
+} a2sf_rotary_scaling;
+
+typedef struct a2sf_rotary_config {
+    int32_t rotary_dim, interleaved;
+    int32_t scaling;             /* a2sf_rotary_scaling */
+    int32_t original_length;     /* L: the length that the frequencies were made for */
+    double theta, factor, low, high, magnitude;
+} a2sf_rotary_config;
+
+#define A2SF_ROTARY_MAX_PAIRS 64
+typedef struct a2sf_rotary_plan {
+    int32_t rotary_dim, interleaved;
+    float magnitude;
+    int32_t check;               /* written by a2sf_rotary_plan_init; other values are refused */
+    uint64_t turn[A2SF_ROTARY_MAX_PAIRS];
+} a2sf_rotary_plan;
+
+#define A2SF_ROTARY_TRANSPOSE 1
+
+int a2sf_rotary_plan_init(const a2sf_rotary_config *config, a2sf_rotary_plan *plan);
+
+int a2sf_rotary(const a2sf_rotary_plan *plan, int32_t dtype, int32_t B, int32_t H, int32_t n, int32_t d,
+                const void *x, int64_t x_stride_b, int64_t x_stride_h, int64_t x_stride_t,
+                void *y, int64_t y_stride_b, int64_t y_stride_h, int64_t y_stride_t,
+                const int32_t *positions, const int32_t *start, const int32_t *lens, int32_t flags,
+                void *cuda_stream);
+
+/* ---------------------------------------------------------------------------
+ * The cache in pages.  A pool of pages, each holding page_size slots of every K/V head, and a
+ * page table per sequence: slot s of sequence b is slot s % page_size of page
+ * page_table[b][s / page_size].  Prompts of different lengths, prompts that arrive in chunks and
+ * sequences that come and go share one pool.  A sequence uses the same number of slots in every
+ * head, but each head evicts its own tokens: positions and scores are kept per slot and head, and
+ * slot order carries no meaning.  A step of the cache is
+ *     a2sf_paged_append   the chunk's keys and values into slots past .. past + len - 1
+ *     a2sf_paged_attend   its attention over slots 0 .. past + len - 1, and the scores
+ *     a2sf_paged_evict    back to the budget; past and start move on
+ * for chunks of one token (generation) as for whole prompts.  All memory is the caller's; the
+ * struct holds DEVICE pointers and is read during the call only.
+ *   Per call, len[b] = min(lens[b], c), or c when lens is NULL.  A sequence with len 0 takes no
+ *   part: nothing of it is read or written (a2sf_paged_evict still brings it to the budget).
+ *   start[b] = tokens seen before the chunk = position of the chunk's first token (NULL: past).
+ * Lengths and page tables are on the device and cannot be checked on the host: a page number
+ * outside [0, num_pages) or a slot outside the table is never followed -- such slots are not
+ * written, and where they would be read the sequence's results are undefined -- and
+ * a2sf_last_device_status then returns A2SF_ERR_INVALID_ARG.  The first call on a device looks up
+ * that status word and raises kernel limits: make it before a stream capture begins.
+ * Pages must not be shared by two sequences where they are written.  Keys, values and queries of
+ * resident tokens must be finite; slots beyond past + len may hold anything.
+ * ------------------------------------------------------------------------- */
+#define A2SF_PAGED_MAX_SEQUENCES 1024
+typedef struct a2sf_paged {
+    int32_t B;                   /* sequences of the call, <= A2SF_PAGED_MAX_SEQUENCES */
+    int32_t H;                   /* K/V heads */
+    int32_t group;               /* query heads per K/V head, 1 .. A2SF_MAX_GROUP */
+    int32_t d;                   /* 64 or 128 */
+    int32_t dtype;               /* a2sf_dtype of the pages, q, k, v and out */
+    int32_t page_size;           /* 16, 32, 64 or 128 */
+    int32_t num_pages;           /* pages of the pool */
+    int32_t max_pages;           /* entries of a page-table row */
+    float scale;                 /* of the logits; 0 selects 1/sqrt(d) */
+    int32_t reserved;            /* 0 */
+    void *k_pages, *v_pages;     /* [num_pages][H][page_size][d], 16-byte aligned */
+    float *scores;               /* [num_pages][H][page_size] */
+    int32_t *positions;          /* [num_pages][H][page_size] */
+    const int32_t *page_table;   /* [B][max_pages] */
+    const int32_t *past;         /* [B] slots in use before the chunk */
+    const int32_t *start;        /* [B] or NULL */
+} a2sf_paged;
+
+/* k, v [B][H][c][d], q and q_out [B][H*group][c][d], strides of their own (q and k, v have d
+ * contiguous).  Token t of sequence b goes to slot past[b] + t with position start[b] + t and score
+ * 0.  With a plan, keys (and queries, when q is not NULL) are rotated on the way; without one q must
+ * be NULL.  q_out may be q itself with the same strides.  Nothing of past and start changes. */
+int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary_opt, int32_t c, const int32_t *lens,
+                      const void *k, const void *v, int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_t,
+                      const void *q_opt, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
+                      void *q_out, int64_t qo_stride_b, int64_t qo_stride_h, int64_t qo_stride_t,
+                      void *cuda_stream);
+
+/* Attention of the chunk (appended before): row i of query head h*group + g sees slots
+ * 0 .. past[b] + i of K/V head h.
+ *     out = softmax(scale q K^T) V,   lse = log sum exp   ([B][H*group][c] fp32, or NULL)
+ *     score[slot] <- alpha^len * score[slot] + sum_{i,g} alpha^(len-1-i) P_ig,slot
+ * which is Eq. 5 carried over chunks: any split of a prompt into chunks gives the scores of the
+ * whole.  flags: 0, or A2SF_ATTEND_NO_SCORES (scores are neither read nor written).  out has strides
+ * of its own; rows i >= len[b] of out and lse are left as they were.  Rows whose weight alpha^age
+ * is below 2^-150 are left out of the sum (their fp32 contribution is zero).
+ * workspace: DEVICE, 256-byte aligned, a2sf_paged_attend_workspace_bytes (0 = invalid arguments);
+ * contents undefined afterwards; calls that may overlap in time need workspaces of their own. */
+#define A2SF_ATTEND_NO_SCORES 1
+size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c);
+int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha,
+                      const void *q, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
+                      void *out, int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t,
+                      float *lse_opt, int32_t flags, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Ends a step.  Of the n = past + len slots of every head min(n, budget) stay: those at the
+ * `recent` newest positions (position >= start + len - recent) and of the others the best under
+ * (score, position), the order of a2sf_select; equal pairs leave in slot order.  Then
+ * past_out[b] = min(n, budget) and start_out[b] = start[b] + len[b] (may be past and start).
+ *   dst_table NULL: in place.  The free slots below `budget`, in ascending order, take the
+ *   survivors from above, in ascending order; nothing else moves.
+ *   dst_table [B][dst_max_pages]: the survivors are copied, in ascending slot order, into those
+ *   pages (none of them a page of page_table) and the old pages are left as they are -- for pages that
+ *   other sequences share.  dst_max_pages * page_size >= min(budget, capacity) is required.
+ * 0 <= recent <= budget, budget >= 1.  Scores may be any numbers (NaN of either sign sorts beyond
+ * infinity).  workspace: as above, from a2sf_paged_evict_workspace_bytes. */
+size_t a2sf_paged_evict_workspace_bytes(const a2sf_paged *cache, int32_t budget);
+int a2sf_paged_evict(const a2sf_paged *cache, int32_t c, const int32_t *lens, int32_t budget, int32_t recent,
+                     const int32_t *dst_table, int32_t dst_max_pages, int32_t *past_out, int32_t *start_out,
+                     void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 /* Snapshot / restore of the whole cache state into / from caller DEVICE buffers:
  * k, v [B][H][M][d] dtype; scores [B][H][M] fp32; pos [B][H][M] int32; count, len
  * [B][H] int32.  Any pointer may be NULL to skip that part. */
@@ -357,8 +498,9 @@ int a2sf_cache_import(a2sf_cache *cache, const void *k, const void *v, const flo
 /* Number of kernels this library has launched in the calling process so far. */
 int64_t a2sf_kernel_launch_count(void);
 
-/* Synchronises the stream and returns the sticky device-side status (A2SF_OK, or
- * A2SF_ERR_TIMEOUT if a kernel abandoned a bounded wait), then clears it.  While the
+/* Synchronises the stream and returns the sticky device-side status (A2SF_OK,
+ * A2SF_ERR_TIMEOUT if a kernel abandoned a bounded wait, or A2SF_ERR_INVALID_ARG if a paged-cache
+ * kernel met a page number or length outside its bounds), then clears it.  While the
  * status is set the tensor-core prefill kernels return without working, so results
  * of calls made after a timeout and before this call are undefined. */
 int a2sf_last_device_status(void *cuda_stream);

@@ -32,6 +32,26 @@ class a2sf_params(ctypes.Structure):
                 ("score_window", ctypes.c_int32)]
 
 
+class a2sf_rotary_config(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("original_length", ctypes.c_int32), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class a2sf_rotary_plan(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("check", ctypes.c_int32), ("turn", ctypes.c_uint64 * 64)]
+
+
+class a2sf_paged(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("group", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("scores", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("past", ctypes.c_void_p),
+                ("start", ctypes.c_void_p)]
+
+
 class A2SFError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -87,6 +107,15 @@ def _load():
         "a2sf_select": (ctypes.c_int, [ctypes.POINTER(a2sf_params), ctypes.c_int32, vp, vp, vp]),
         "a2sf_selftest_bounded_wait": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, vp, vp]),
         "a2sf_status_string": (ctypes.c_char_p, [ctypes.c_int]),
+        "a2sf_rotary_plan_init": (ctypes.c_int, [ctypes.POINTER(a2sf_rotary_config), ctypes.POINTER(a2sf_rotary_plan)]),
+        "a2sf_rotary": (ctypes.c_int, [vp, i32, i32, i32, i32, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp, vp, vp,
+                                       i32, vp]),
+        "a2sf_paged_append": (ctypes.c_int, [vp, vp, i32, vp, vp, vp, i64, i64, i64, vp, i64, i64, i64,
+                                             vp, i64, i64, i64, vp]),
+        "a2sf_paged_attend_workspace_bytes": (sz, [vp, i32]),
+        "a2sf_paged_attend": (ctypes.c_int, [vp, i32, vp, f32, vp, i64, i64, i64, vp, i64, i64, i64, vp, i32, vp, sz, vp]),
+        "a2sf_paged_evict_workspace_bytes": (sz, [vp, i32]),
+        "a2sf_paged_evict": (ctypes.c_int, [vp, i32, vp, i32, i32, vp, i32, vp, vp, vp, sz, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -415,3 +444,165 @@ class Cache:
         _check(lib.a2sf_cache_import(self.handle, *(_ptr(state.get(k)) for k in
                                                     ("k", "v", "scores", "pos", "count", "len")),
                                      _stream(stream)), "a2sf_cache_import")
+
+
+# ---- rotary positions and the cache in pages -----------------------------------------------------
+A2SF_ROTARY_TRANSPOSE = 1
+A2SF_ATTEND_NO_SCORES = 1
+_ROTARY_SCALING = {"none": 0, "linear": 1, "ntk": 2, "bands": 3, "ramp": 4}
+
+
+def a2sf_rotary_plan_init(rotary_dim: int, theta: float = 10000.0, interleaved: bool = False, scaling: str = "none",
+                          factor: float = 1.0, original_length: int = 0, low: float = 1.0, high: float = 4.0,
+                          magnitude: float = 0.0) -> a2sf_rotary_plan:
+    """The plan of a rotation (host only; keep it and pass it to the calls)."""
+    if scaling not in _ROTARY_SCALING:
+        raise ValueError(f"scaling must be one of {sorted(_ROTARY_SCALING)}, got {scaling!r}")
+    cfg = a2sf_rotary_config(rotary_dim, int(bool(interleaved)), _ROTARY_SCALING[scaling], original_length, theta, factor,
+                             low, high, magnitude)
+    plan = a2sf_rotary_plan()
+    _check(lib.a2sf_rotary_plan_init(ctypes.byref(cfg), ctypes.byref(plan)), "a2sf_rotary_plan_init")
+    return plan
+
+
+def _rows(t: torch.Tensor, shape, dtype, device, name):
+    """Address and strides of a [B,H,n,d] tensor of the call."""
+    if tuple(t.shape) != shape or t.dtype != dtype or t.device != device or t.stride(3) != 1:
+        raise ValueError(f"{name}: expected {shape} {dtype} on {device} with contiguous rows, got {tuple(t.shape)} {t.dtype} "
+                         f"on {t.device}, strides {t.stride()}")
+    return t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)
+
+
+def _ints(t, shape, device, name):
+    """Address of an int32 array of the call (None: NULL)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != shape or t.dtype != torch.int32 or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous int32 {shape} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _call(device, stream, fn, name, *args):
+    """A library call on the tensors' device, on ``stream`` or that device's current stream."""
+    index = device.index
+    handle = (torch.cuda.current_stream(index) if stream is None else stream).cuda_stream
+    if index == torch.cuda.current_device():
+        status = fn(*args, handle)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, handle)
+    if status != A2SF_OK:
+        raise A2SFError(status, name)
+
+
+def a2sf_rotary(plan: a2sf_rotary_plan, x, out=None, positions=None, start=None, lens=None, transpose=False, stream=None):
+    """x [B,H,n,d] rotated by its positions (``positions`` [B,n], or ``start`` [B] + t, or t).  ``out`` may be x."""
+    shape, dtype, device = tuple(x.shape), x.dtype, x.device
+    B, H, n, d = shape
+    if out is None:
+        out = torch.empty_strided(shape, x.stride(), dtype=dtype, device=device)
+    _call(device, stream, lib.a2sf_rotary, "a2sf_rotary", ctypes.byref(plan), _DTYPE_CODE[dtype], B, H, n, d,
+          *_rows(x, shape, dtype, device, "x"), *_rows(out, shape, dtype, device, "out"),
+          _ints(positions, (B, n), device, "positions"), _ints(start, (B,), device, "start"),
+          _ints(lens, (B,), device, "lens"), A2SF_ROTARY_TRANSPOSE if transpose else 0)
+    return out
+
+
+class PagedCache:
+    """A pool of cache pages and the page table and lengths of ``B`` sequences (see ``a2sf_paged``).
+
+    The tensors are attributes: given ones are adopted, the others are made here (pages unset, scores
+    0, positions -1, page table -1, lengths 0).  A step is a2sf_paged_append, a2sf_paged_attend,
+    a2sf_paged_evict.  To replace a tensor, make another PagedCache around it."""
+
+    def __init__(self, B: int, H: int, d: int, dtype: torch.dtype, page_size: int, num_pages: int, max_pages: int, *,
+                 group: int = 1, scale: float = 0.0, device="cuda", k_pages=None, v_pages=None, scores=None,
+                 positions=None, page_table=None, past=None, start=None):
+        if k_pages is not None:
+            device = k_pages.device
+        device = torch.device(device)
+        if device.type == "cuda" and device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        rows = (num_pages, H, page_size)
+
+        def own(t, shape, dt, fill, name):
+            if t is None:
+                return (torch.empty(shape, dtype=dt, device=device) if fill is None
+                        else torch.full(shape, fill, dtype=dt, device=device))
+            if tuple(t.shape) != shape or t.dtype != dt or t.device != device or not t.is_contiguous():
+                raise ValueError(f"{name}: expected contiguous {dt} {shape} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+            return t
+
+        self.k_pages = own(k_pages, rows + (d,), dtype, None, "k_pages")
+        self.v_pages = own(v_pages, rows + (d,), dtype, None, "v_pages")
+        self.scores = own(scores, rows, torch.float32, 0.0, "scores")
+        self.positions = own(positions, rows, torch.int32, -1, "positions")
+        self.page_table = own(page_table, (B, max_pages), torch.int32, -1, "page_table")
+        self.past = own(past, (B,), torch.int32, 0, "past")
+        self.start = own(start, (B,), torch.int32, 0, "start")
+        self.B, self.H, self.group, self.d, self.dtype, self.device = B, H, group, d, dtype, device
+        self.page_size, self.num_pages, self.max_pages = page_size, num_pages, max_pages
+        self.p = a2sf_paged(B, H, group, d, _DTYPE_CODE[dtype], page_size, num_pages, max_pages, scale, 0,
+                            *(t.data_ptr() for t in (self.k_pages, self.v_pages, self.scores, self.positions,
+                                                     self.page_table, self.past, self.start)))
+        self._ref = ctypes.byref(self.p)
+
+    def a2sf_paged_append(self, k, v, lens=None, q=None, q_out=None, rotary=None, stream=None):
+        """k, v [B,H,c,d] (one stride set) into slots past.. of their sequences; with a ``rotary`` plan keys are rotated
+        on the way, and q [B,H*group,c,d] into ``q_out``, which is returned."""
+        c = k.shape[2]
+        kv = (self.B, self.H, c, self.d)
+        kr = _rows(k, kv, self.dtype, self.device, "k")
+        vr = _rows(v, kv, self.dtype, self.device, "v")
+        if kr[1:] != vr[1:]:
+            raise ValueError(f"k and v need the same strides, got {kr[1:]} and {vr[1:]}")
+        qr = qo = (None, 0, 0, 0)
+        if q is not None:
+            shape = (self.B, self.H * self.group, c, self.d)
+            qr = _rows(q, shape, self.dtype, self.device, "q")
+            if q_out is None:
+                q_out = torch.empty_strided(shape, q.stride(), dtype=self.dtype, device=self.device)
+            qo = _rows(q_out, shape, self.dtype, self.device, "q_out")
+        _call(self.device, stream, lib.a2sf_paged_append, "a2sf_paged_append", self._ref,
+              None if rotary is None else ctypes.byref(rotary), c, _ints(lens, (self.B,), self.device, "lens"), kr[0], *vr,
+              *qr, *qo)
+        return q_out
+
+    def a2sf_paged_attend(self, q, alpha=1.0, lens=None, out=None, lse=None, scores=True, workspace=None, stream=None):
+        """Attention of q [B,H*group,c,d] over the cache and the chunk appended before; returns (out, lse).  The cache's
+        scores are decayed and added to unless ``scores`` is False."""
+        c = q.shape[2]
+        shape = (self.B, self.H * self.group, c, self.d)
+        qr = _rows(q, shape, self.dtype, self.device, "q")
+        if out is None:
+            out = torch.empty_strided(shape, q.stride(), dtype=self.dtype, device=self.device)
+        if lse is None:
+            lse = torch.empty(shape[:3], dtype=torch.float32, device=self.device)
+        elif tuple(lse.shape) != shape[:3] or lse.dtype != torch.float32 or lse.device != self.device or not lse.is_contiguous():
+            raise ValueError(f"lse: expected contiguous float32 {shape[:3]} on {self.device}")
+        if workspace is None:
+            workspace = self._workspace(lib.a2sf_paged_attend_workspace_bytes, "a2sf_paged_attend_workspace_bytes", c)
+        _call(self.device, stream, lib.a2sf_paged_attend, "a2sf_paged_attend", self._ref, c,
+              _ints(lens, (self.B,), self.device, "lens"), alpha, *qr, *_rows(out, shape, self.dtype, self.device, "out"),
+              lse.data_ptr(), 0 if scores else A2SF_ATTEND_NO_SCORES, workspace.data_ptr(), workspace.numel())
+        return out, lse
+
+    def a2sf_paged_evict(self, budget: int, recent: int, c: int = 1, lens=None, dst_table=None, past_out=None,
+                         start_out=None, workspace=None, stream=None):
+        """Ends a step whose chunk had ``lens`` (or c) tokens: every head back to ``budget`` slots, in place or into the
+        pages of ``dst_table`` [B, any].  ``past`` and ``start`` move on (or ``past_out`` and ``start_out`` get the values)."""
+        past_out = self.past if past_out is None else past_out
+        start_out = self.start if start_out is None else start_out
+        pages = 0 if dst_table is None else dst_table.shape[1]
+        if workspace is None:
+            workspace = self._workspace(lib.a2sf_paged_evict_workspace_bytes, "a2sf_paged_evict_workspace_bytes", budget)
+        _call(self.device, stream, lib.a2sf_paged_evict, "a2sf_paged_evict", self._ref, c,
+              _ints(lens, (self.B,), self.device, "lens"), budget, recent, _ints(dst_table, (self.B, pages), self.device, "dst_table"),
+              pages, _ints(past_out, (self.B,), self.device, "past_out"), _ints(start_out, (self.B,), self.device, "start_out"),
+              workspace.data_ptr(), workspace.numel())
+
+    def _workspace(self, query, name, arg):
+        nbytes = int(query(self._ref, arg))
+        if nbytes == 0:
+            raise A2SFError(A2SF_ERR_INVALID_ARG, name)
+        return torch.empty((nbytes,), dtype=torch.uint8, device=self.device)

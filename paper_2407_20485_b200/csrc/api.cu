@@ -9,6 +9,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "common.cuh"
+#include "paged.cuh"
 
 namespace a2sf {
 
@@ -768,7 +769,8 @@ int a2sf_last_device_status(void *cuda_stream)
 {
     const int a = read_and_clear_tc_status(static_cast<cudaStream_t>(cuda_stream));
     const int b = read_and_clear_decode_status(static_cast<cudaStream_t>(cuda_stream));
-    return a != A2SF_OK ? a : b;
+    const int c = read_and_clear_paged_status(static_cast<cudaStream_t>(cuda_stream));
+    return a != A2SF_OK ? a : b != A2SF_OK ? b : c;
 }
 
 int a2sf_selftest_bounded_wait(int32_t which, int64_t limit_cycles, int64_t *report, void *cuda_stream)

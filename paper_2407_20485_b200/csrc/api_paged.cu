@@ -1,0 +1,254 @@
+// Host side of the paged-cache and rotary entry points: argument validation, workspaces, dispatch.
+// No data is touched on the host.
+#include <cmath>
+
+#include "paged.cuh"
+
+namespace a2sf {
+namespace {
+
+constexpr int32_t kPlanCheck = 0x52504c4e;
+
+inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+inline int elem_bytes(int dtype) { return dtype == A2SF_F32 ? 4 : 2; }
+
+int check_shape(int dtype, int d)
+{
+    if (dtype != A2SF_F32 && dtype != A2SF_BF16 && dtype != A2SF_F16) return A2SF_ERR_UNSUPPORTED;
+    return d == 64 || d == 128 ? A2SF_OK : A2SF_ERR_UNSUPPORTED;
+}
+
+// a [B][H][n][d] tensor: rows of d elements, 16-byte aligned; axes of extent 1 may have any stride
+int check_tensor(const void *p, int dtype, int d, const int64_t extent[3], const int64_t stride[3])
+{
+    if (!p || !aligned(p, 16)) return A2SF_ERR_INVALID_ARG;
+    const int vec = 16 / elem_bytes(dtype);
+    for (int x = 0; x < 3; ++x) {
+        if (extent[x] <= 1) continue;
+        if (stride[x] < d || stride[x] % vec) return A2SF_ERR_INVALID_ARG;
+    }
+    return A2SF_OK;
+}
+
+int check_plan(const a2sf_rotary_plan *p, int d)
+{
+    if (!p || p->check != kPlanCheck || p->rotary_dim < 2 || p->rotary_dim > 2 * A2SF_ROTARY_MAX_PAIRS || p->rotary_dim % 2)
+        return A2SF_ERR_INVALID_ARG;
+    return p->rotary_dim <= d ? A2SF_OK : A2SF_ERR_INVALID_ARG;
+}
+
+int check_paged(const a2sf_paged *p, int c)
+{
+    if (!p) return A2SF_ERR_INVALID_ARG;
+    const int rc = check_shape(p->dtype, p->d);
+    if (rc != A2SF_OK) return rc;
+    if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128) return A2SF_ERR_UNSUPPORTED;
+    if (p->group < 1 || p->group > A2SF_MAX_GROUP || p->B > A2SF_PAGED_MAX_SEQUENCES) return A2SF_ERR_UNSUPPORTED;
+    if (p->B < 1 || p->H < 1 || p->num_pages < 1 || p->max_pages < 1 || c < 1 || p->reserved != 0) return A2SF_ERR_INVALID_ARG;
+    if (!(p->scale >= 0.f) || std::isinf(p->scale)) return A2SF_ERR_INVALID_ARG;
+    // slots of a sequence, units, folded rows and tiles of a call all stay 32-bit numbers
+    if ((int64_t)p->max_pages * p->page_size > (1 << 28) || (int64_t)c * p->group > (1 << 28) ||
+        (int64_t)p->B * p->H * p->group > (1 << 24) || (int64_t)p->num_pages * p->H * p->page_size >= (1ll << 32))
+        return A2SF_ERR_UNSUPPORTED;
+    if (!p->k_pages || !p->v_pages || !p->scores || !p->positions || !p->page_table || !p->past) return A2SF_ERR_INVALID_ARG;
+    if (!aligned(p->k_pages, 16) || !aligned(p->v_pages, 16) || !aligned(p->scores, 4) || !aligned(p->positions, 4) ||
+        !aligned(p->page_table, 4) || !aligned(p->past, 4) || !aligned(p->start, 4))
+        return A2SF_ERR_INVALID_ARG;
+    return A2SF_OK;
+}
+
+PagedView make_view(const a2sf_paged *p, int c, const int32_t *lens)
+{
+    PagedView v;
+    v.k = static_cast<char *>(p->k_pages); v.v = static_cast<char *>(p->v_pages);
+    v.scores = p->scores; v.positions = p->positions;
+    v.table = p->page_table; v.past = p->past; v.start = p->start; v.lens = lens;
+    v.status = nullptr;
+    v.B = p->B; v.H = p->H; v.G = p->group; v.d = p->d; v.ps = p->page_size;
+    v.ps_shift = p->page_size == 16 ? 4 : p->page_size == 32 ? 5 : p->page_size == 64 ? 6 : 7;
+    v.max_pages = p->max_pages; v.num_pages = p->num_pages; v.c = c;
+    v.sl2 = (p->scale > 0.f ? p->scale : 1.f / std::sqrt((float)p->d)) * kLog2e;
+    return v;
+}
+
+}  // namespace
+}  // namespace a2sf
+
+using namespace a2sf;
+
+extern "C" {
+
+int a2sf_rotary_plan_init(const a2sf_rotary_config *c, a2sf_rotary_plan *plan)
+{
+    if (!c || !plan) return A2SF_ERR_INVALID_ARG;
+    const int r = c->rotary_dim;
+    if (r < 2 || r > 2 * A2SF_ROTARY_MAX_PAIRS || r % 2 || (c->interleaved != 0 && c->interleaved != 1)) return A2SF_ERR_INVALID_ARG;
+    if (c->scaling < A2SF_ROTARY_PLAIN || c->scaling > A2SF_ROTARY_RAMP) return A2SF_ERR_INVALID_ARG;
+    if (!(c->theta > 1.0) || !std::isfinite(c->theta) || !(c->factor >= 1.0) || !std::isfinite(c->factor)) return A2SF_ERR_INVALID_ARG;
+    if (!(c->magnitude >= 0.0) || !std::isfinite(c->magnitude)) return A2SF_ERR_INVALID_ARG;
+    if (c->scaling == A2SF_ROTARY_NTK && r < 4) return A2SF_ERR_INVALID_ARG;
+    const bool by_length = c->scaling == A2SF_ROTARY_BANDS || c->scaling == A2SF_ROTARY_RAMP;
+    if (by_length && (c->original_length < 1 || !(c->low > 0.0) || !(c->high > c->low) || !std::isfinite(c->high))) return A2SF_ERR_INVALID_ARG;
+
+    const double two_pi = 6.283185307179586476925;
+    const double L = c->original_length;
+    const double theta = c->scaling == A2SF_ROTARY_NTK ? c->theta * std::pow(c->factor, r / (r - 2.0)) : c->theta;
+    // RAMP: pair index at which `beta` turns fit into the original length
+    double lo = 0.0, hi = 0.0;
+    if (c->scaling == A2SF_ROTARY_RAMP) {
+        lo = std::floor(r * std::log(L / (c->high * two_pi)) / (2.0 * std::log(c->theta)));
+        hi = std::ceil(r * std::log(L / (c->low * two_pi)) / (2.0 * std::log(c->theta)));
+        lo = lo > 0.0 ? lo : 0.0;
+        hi = hi < r - 1.0 ? hi : r - 1.0;
+    }
+    for (int k = 0; k < A2SF_ROTARY_MAX_PAIRS; ++k) {
+        plan->turn[k] = 0;
+        if (k >= r / 2) continue;
+        double f = std::pow(theta, -2.0 * k / r);
+        double keep = 1.0;                                            // share that is not interpolated
+        if (c->scaling == A2SF_ROTARY_LINEAR) keep = 0.0;
+        if (c->scaling == A2SF_ROTARY_BANDS) keep = (L * f / two_pi - c->low) / (c->high - c->low);
+        if (c->scaling == A2SF_ROTARY_RAMP) keep = 1.0 - (k - lo) / (hi - lo > 0.001 ? hi - lo : 0.001);
+        keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+        f = keep * f + (1.0 - keep) * f / c->factor;
+        // turns per position are below 1/6: 2^64 times that fits, with the double's 53 bits
+        plan->turn[k] = (uint64_t)std::ldexp(f / two_pi, 64);
+    }
+    plan->rotary_dim = r;
+    plan->interleaved = c->interleaved;
+    plan->magnitude = (float)(c->magnitude > 0.0 ? c->magnitude
+                                                 : c->scaling == A2SF_ROTARY_RAMP ? 0.1 * std::log(c->factor) + 1.0 : 1.0);
+    plan->check = kPlanCheck;
+    return A2SF_OK;
+}
+
+int a2sf_rotary(const a2sf_rotary_plan *plan, int32_t dtype, int32_t B, int32_t H, int32_t n, int32_t d, const void *x,
+                int64_t x_stride_b, int64_t x_stride_h, int64_t x_stride_t, void *y, int64_t y_stride_b,
+                int64_t y_stride_h, int64_t y_stride_t, const int32_t *positions, const int32_t *start,
+                const int32_t *lens, int32_t flags, void *cuda_stream)
+{
+    A2SF_TRACE("a2sf_rotary");
+    int rc = check_shape(dtype, d);
+    if (rc != A2SF_OK) return rc;
+    if (B < 1 || H < 1 || n < 1 || (flags & ~A2SF_ROTARY_TRANSPOSE)) return A2SF_ERR_INVALID_ARG;
+    if ((rc = check_plan(plan, d)) != A2SF_OK) return rc;
+    const int64_t extent[3] = {B, H, n};
+    const int64_t xs[3] = {x_stride_b, x_stride_h, x_stride_t}, ys[3] = {y_stride_b, y_stride_h, y_stride_t};
+    if ((rc = check_tensor(x, dtype, d, extent, xs)) != A2SF_OK || (rc = check_tensor(y, dtype, d, extent, ys)) != A2SF_OK) return rc;
+    if (!aligned(positions, 4) || !aligned(start, 4) || !aligned(lens, 4)) return A2SF_ERR_INVALID_ARG;
+    if (x == y)
+        for (int i = 0; i < 3; ++i)
+            if (extent[i] > 1 && xs[i] != ys[i]) return A2SF_ERR_INVALID_ARG;
+    RotaryArgs r = {};
+    r.x = x; r.y = y;
+    r.sx = Strides{x_stride_b, x_stride_h, x_stride_t};
+    r.sy = Strides{y_stride_b, y_stride_h, y_stride_t};
+    r.positions = positions; r.start = start; r.lens = lens;
+    r.B = B; r.n = n; r.d = d; r.Hq = H; r.Hk = 0;
+    r.transpose = flags & A2SF_ROTARY_TRANSPOSE;
+    return launch_rotary(dtype, plan, r, nullptr, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+}
+
+int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary, int32_t c, const int32_t *lens,
+                      const void *k, const void *v, int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_t,
+                      const void *q, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t, void *q_out,
+                      int64_t qo_stride_b, int64_t qo_stride_h, int64_t qo_stride_t, void *cuda_stream)
+{
+    A2SF_TRACE("a2sf_paged_append");
+    int rc = check_paged(cache, c);
+    if (rc != A2SF_OK) return rc;
+    if (rotary && (rc = check_plan(rotary, cache->d)) != A2SF_OK) return rc;
+    if (q && (!rotary || !q_out)) return A2SF_ERR_INVALID_ARG;
+    if (!aligned(lens, 4)) return A2SF_ERR_INVALID_ARG;
+    const int64_t ekv[3] = {cache->B, cache->H, c}, eq[3] = {cache->B, (int64_t)cache->H * cache->group, c};
+    const int64_t skv[3] = {kv_stride_b, kv_stride_h, kv_stride_t};
+    const int64_t sq[3] = {q_stride_b, q_stride_h, q_stride_t}, so[3] = {qo_stride_b, qo_stride_h, qo_stride_t};
+    if ((rc = check_tensor(k, cache->dtype, cache->d, ekv, skv)) != A2SF_OK ||
+        (rc = check_tensor(v, cache->dtype, cache->d, ekv, skv)) != A2SF_OK)
+        return rc;
+    if (q) {
+        if ((rc = check_tensor(q, cache->dtype, cache->d, eq, sq)) != A2SF_OK ||
+            (rc = check_tensor(q_out, cache->dtype, cache->d, eq, so)) != A2SF_OK)
+            return rc;
+        if (q == q_out)
+            for (int i = 0; i < 3; ++i)
+                if (eq[i] > 1 && sq[i] != so[i]) return A2SF_ERR_INVALID_ARG;
+    }
+    PagedView pv = make_view(cache, c, lens);
+    if (!(pv.status = paged_status_word())) return A2SF_ERR_CUDA;
+    RotaryArgs r = {};
+    r.x = q; r.y = q_out; r.k = k; r.v = v;
+    r.sx = Strides{q_stride_b, q_stride_h, q_stride_t};
+    r.sy = Strides{qo_stride_b, qo_stride_h, qo_stride_t};
+    r.skv = Strides{kv_stride_b, kv_stride_h, kv_stride_t};
+    r.start = cache->start; r.lens = lens;
+    r.B = cache->B; r.n = c; r.d = cache->d;
+    r.Hq = q ? cache->H * cache->group : 0;
+    r.Hk = cache->H;
+    return launch_rotary(cache->dtype, rotary, r, &pv, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+}
+
+size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c)
+{
+    if (check_paged(cache, c) != A2SF_OK) return 0;
+    return align_up(attend_simt_ws_bytes(make_view(cache, c, nullptr)));
+}
+
+int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha, const void *q,
+                      int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t, void *out, int64_t out_stride_b,
+                      int64_t out_stride_h, int64_t out_stride_t, float *lse, int32_t flags, void *workspace,
+                      size_t workspace_bytes, void *cuda_stream)
+{
+    A2SF_TRACE("a2sf_paged_attend");
+    int rc = check_paged(cache, c);
+    if (rc != A2SF_OK) return rc;
+    if (!(alpha >= 0.f && alpha <= 1.f) || (flags & ~A2SF_ATTEND_NO_SCORES)) return A2SF_ERR_INVALID_ARG;
+    const int64_t eq[3] = {cache->B, (int64_t)cache->H * cache->group, c};
+    const int64_t sq[3] = {q_stride_b, q_stride_h, q_stride_t}, so[3] = {out_stride_b, out_stride_h, out_stride_t};
+    if ((rc = check_tensor(q, cache->dtype, cache->d, eq, sq)) != A2SF_OK ||
+        (rc = check_tensor(out, cache->dtype, cache->d, eq, so)) != A2SF_OK)
+        return rc;
+    if (!aligned(lens, 4) || !aligned(lse, 4) || !workspace || !aligned(workspace, 256)) return A2SF_ERR_INVALID_ARG;
+    if (workspace_bytes < a2sf_paged_attend_workspace_bytes(cache, c)) return A2SF_ERR_WORKSPACE;
+    AttendArgs a;
+    a.pv = make_view(cache, c, lens);
+    if (!(a.pv.status = paged_status_word())) return A2SF_ERR_CUDA;
+    a.q = q; a.out = out; a.lse = lse;
+    a.sq = Strides{q_stride_b, q_stride_h, q_stride_t};
+    a.so = Strides{out_stride_b, out_stride_h, out_stride_t};
+    a.alpha = alpha; a.nl2a = neg_log2(alpha);
+    a.scores = !(flags & A2SF_ATTEND_NO_SCORES);
+    a.ws = workspace;
+    return launch_attend_simt(cache->dtype, a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+}
+
+size_t a2sf_paged_evict_workspace_bytes(const a2sf_paged *cache, int32_t budget)
+{
+    if (check_paged(cache, 1) != A2SF_OK || budget < 1) return 0;
+    const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
+    return evict_ws_bytes((size_t)cache->B * cache->H, budget < cap ? budget : (int)cap);
+}
+
+int a2sf_paged_evict(const a2sf_paged *cache, int32_t c, const int32_t *lens, int32_t budget, int32_t recent,
+                     const int32_t *dst_table, int32_t dst_max_pages, int32_t *past_out, int32_t *start_out,
+                     void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    A2SF_TRACE("a2sf_paged_evict");
+    const int rc = check_paged(cache, c);
+    if (rc != A2SF_OK) return rc;
+    if (budget < 1 || recent < 0 || recent > budget || !past_out || !start_out) return A2SF_ERR_INVALID_ARG;
+    if (!aligned(lens, 4) || !aligned(dst_table, 4) || !aligned(past_out, 4) || !aligned(start_out, 4) || past_out == start_out)
+        return A2SF_ERR_INVALID_ARG;
+    const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
+    const int M = budget < cap ? budget : (int)cap;           // n never exceeds the capacity
+    if (dst_table && (dst_max_pages < 1 || (int64_t)dst_max_pages * cache->page_size < M)) return A2SF_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256)) return A2SF_ERR_INVALID_ARG;
+    if (workspace_bytes < a2sf_paged_evict_workspace_bytes(cache, budget)) return A2SF_ERR_WORKSPACE;
+    PagedView pv = make_view(cache, c, lens);
+    if (!(pv.status = paged_status_word())) return A2SF_ERR_CUDA;
+    return launch_evict(elem_bytes(cache->dtype), pv, M, recent, dst_table, dst_max_pages, past_out, start_out, workspace,
+                        static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,109 @@
+// The cache in pages: what its kernels share (device view, page lookups, division of work).
+#pragma once
+
+#include "common.cuh"
+
+namespace a2sf {
+
+struct PagedView {
+    char *k, *v;                 // [num_pages][H][ps][d] elements
+    float *scores;               // [num_pages][H][ps]
+    int32_t *positions;
+    const int32_t *table;        // [B][max_pages]
+    const int32_t *past, *start; // [B]; start may be nullptr (past)
+    const int32_t *lens;         // [B] or nullptr (c)
+    int *status;                 // sticky status word of the paged kernels
+    int B, H, G, d, ps, ps_shift, max_pages, num_pages, c;
+    float sl2;                   // scale * log2(e)
+};
+
+struct SeqState {
+    int past, len;               // slots before the chunk, new tokens
+};
+
+// Lengths live on the device: whatever they hold, past + len stays within the page table.
+__device__ __forceinline__ SeqState seq_state(const PagedView &a, int b)
+{
+    SeqState s;
+    const int cap = a.max_pages << a.ps_shift;
+    s.past = a.past[b];
+    s.len = a.lens ? min(a.lens[b], a.c) : a.c;
+    if (s.past < 0 || s.len < 0 || s.past > cap - s.len) {
+        *a.status = A2SF_ERR_INVALID_ARG;
+        s.past = min(max(s.past, 0), cap);
+        s.len = min(max(s.len, 0), cap - s.past);
+    }
+    return s;
+}
+
+// Page of slot `s` of sequence b for reading: a bad entry is reported and page 0 stands in.
+__device__ __forceinline__ int page_for_read(const PagedView &a, const int32_t *row, int s)
+{
+    const int p = row[s >> a.ps_shift];
+    if ((unsigned)p < (unsigned)a.num_pages) return p;
+    *a.status = A2SF_ERR_INVALID_ARG;
+    return 0;
+}
+// ... and for writing: -1, and the write is left out.
+__device__ __forceinline__ int page_for_write(const PagedView &a, const int32_t *row, int s)
+{
+    const int p = row[s >> a.ps_shift];
+    if ((unsigned)p < (unsigned)a.num_pages) return p;
+    *a.status = A2SF_ERR_INVALID_ARG;
+    return -1;
+}
+// Index of a slot's row within the pool (times d: its K and V row; alone: score and position).
+__device__ __forceinline__ int64_t pool_row(const PagedView &a, int page, int h, int s)
+{
+    return (((int64_t)page * a.H + h) << a.ps_shift) + (s & ((1 << a.ps_shift) - 1));
+}
+
+// alpha^age in fp32, with 0^0 = 1 (nl2a = -log2 alpha, +inf for alpha = 0)
+__device__ __forceinline__ float age_exponent(int age, float nl2a) { return age == 0 ? 0.f : (float)age * nl2a; }
+
+__host__ inline float neg_log2(float alpha) { return alpha > 0.f ? -log2f(alpha) : INFINITY; }
+
+// First row (token of the chunk) whose weight alpha^(len-1-i) is not below 2^-150: a probability
+// is at most 1, and 2^-150 rounds to zero in fp32 whatever it is multiplied with.
+__device__ __forceinline__ int first_weighted_token(int len, float nl2a)
+{
+    if (!(nl2a > 0.f)) return 0;
+    const float span = 150.f / nl2a;
+    return span >= (float)len ? 0 : max(0, len - 1 - (int)span);
+}
+
+// ---- launchers -------------------------------------------------------------------------------
+int *paged_status_word();        // device address on the current device (nullptr on failure)
+int read_and_clear_paged_status(cudaStream_t s);
+
+struct RotaryArgs {
+    // heads [0, Hq): x -> y rotated; then (append) Hk keys rotated into pages and Hk values copied
+    const void *x, *k, *v;
+    void *y;
+    Strides sx, sy, skv;
+    const int32_t *positions;    // [B][n] or nullptr
+    const int32_t *start;        // [B] or nullptr (0, or past in append)
+    const int32_t *lens;
+    int B, n, d, Hq, Hk, transpose;
+};
+cudaError_t launch_rotary(int dtype, const a2sf_rotary_plan *plan, const RotaryArgs &r, const PagedView *pages,
+                          cudaStream_t s);
+
+struct AttendArgs {
+    PagedView pv;
+    const void *q;
+    void *out;
+    float *lse;                  // [B][H*G][c] or nullptr
+    Strides sq, so;
+    float alpha, nl2a;           // nl2a = -log2(alpha)
+    bool scores;
+    void *ws;
+};
+size_t attend_simt_ws_bytes(const PagedView &pv);
+cudaError_t launch_attend_simt(int dtype, const AttendArgs &a, cudaStream_t s);
+
+cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int recent, const int32_t *dst_table,
+                         int dst_max_pages, int32_t *past_out, int32_t *start_out, void *ws, cudaStream_t s);
+size_t evict_ws_bytes(size_t units, int budget);
+
+}  // namespace a2sf

@@ -1,0 +1,486 @@
+"""Rotary positions and the cache in pages against plain 64-bit forms on a B200.
+
+Tolerances count roundings.  u = torch.finfo(dtype).eps / 2 is the half step of the storage type, f = 2^-24 that
+of fp32.  A logit is a sum of d products in fp32: off by at most (d + 2) f * sum|q k| * scale =: e.  A probability is
+then off by 2 e + 2^-20 relatively (its own logit, its row's log-sum-exp, the exponential)."""
+import math
+
+import pytest
+import torch
+
+import paged_util as pu
+
+pytestmark = pytest.mark.gpu
+
+F = 2.0 ** -24
+BF, HF, FP = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def a2sf():
+    from paper_2407_20485_b200 import binding
+
+    return binding
+
+
+@pytest.fixture(autouse=True)
+def _clean_status(a2sf):
+    a2sf.a2sf_last_device_status()
+    yield
+    assert a2sf.a2sf_last_device_status() == a2sf.A2SF_OK
+
+
+def close(got, want, tol, what):
+    got, want = got.double().cpu(), want.double()
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), (f"{what}: {int(bad.sum())} of {bad.numel()} off, worst "
+                           f"{float(((got - want).abs() / tol.clamp_min(1e-300)).nan_to_num(math.inf).max()):.3g} of the tolerance")
+
+
+# ---- rotary ---------------------------------------------------------------------------------------------
+
+ROT = [
+    # B, H, n, d, dtype, r, interleaved, scaling, start, transpose, layout
+    (1, 1, 1, 64, BF, 64, False, "none", 0, False, "bhnd"),
+    (2, 5, 7, 128, BF, 128, False, "none", 3, False, "bhnd"),
+    (2, 5, 7, 128, HF, 128, True, "linear", 1000003, False, "bnhd"),
+    (3, 2, 33, 64, FP, 32, True, "ramp", 2000000000, True, "bhnd"),
+    (1, 3, 65, 64, FP, 24, False, "ntk", 130000, False, "bnhd"),
+    (2, 4, 19, 128, HF, 24, False, "bands", 99999, True, "bnhd"),
+    (2, 3, 5, 64, BF, 2, False, "none", 77, False, "bhnd"),
+    (2, 3, 5, 64, BF, 6, True, "none", 77, False, "bhnd"),
+    (1, 40, 130, 128, BF, 36, False, "bands", 50000, False, "bhnd"),
+    (4, 1, 257, 128, FP, 126, False, "none", 12345, False, "bhnd"),
+    (2, 2, 9, 128, FP, 128, True, "ntk", 0, True, "bhnd"),
+]
+
+
+def _scaling(scaling):
+    return dict(scaling=scaling, factor=1.0 if scaling == "none" else 8.0, original_length=4096, low=1.0,
+                high=32.0 if scaling == "ramp" else 4.0)
+
+
+@pytest.mark.parametrize("case", ROT, ids=lambda c: "-".join(str(x).replace("torch.", "") for x in c))
+def test_rotary(a2sf, case):
+    B, H, n, d, dtype, r, il, scaling, start, transpose, layout = case
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn((B, H, n, d) if layout == "bhnd" else (B, n, H, d), generator=g).to(dtype)
+    x = x if layout == "bhnd" else x.transpose(1, 2)
+    kw = _scaling(scaling)
+    plan = a2sf.a2sf_rotary_plan_init(r, interleaved=il, **kw)
+    freqs = pu.inv_freq(r, 10000.0, scaling, kw["factor"], 4096, kw["low"], kw["high"])
+    mag = 0.1 * math.log(8.0) + 1 if scaling == "ramp" else 1.0
+    starts = torch.tensor([start + 11 * b for b in range(B)], dtype=torch.int32)
+    lens = torch.tensor([n if b == 0 else max(0, n - 4 * b) for b in range(B)], dtype=torch.int32)
+    want = torch.stack([pu.rotate(x[b].double(), starts[b].long() + torch.arange(n), freqs, il, mag, transpose) for b in range(B)])
+    xc = x.cuda() if layout == "bhnd" else x.transpose(1, 2).contiguous().cuda().transpose(1, 2)
+    out = torch.full_like(xc, 9.0)
+    got = a2sf.a2sf_rotary(plan, xc, out=out, start=starts.cuda(), lens=lens.cuda(), transpose=transpose)
+    live = (torch.arange(n) < lens[:, None])[:, None, :, None]
+    size = x.double().norm(dim=-1, keepdim=True) * mag            # no pair is longer than its row
+    u = torch.finfo(dtype).eps / 2
+    tol = u * want.abs() + size * (2e-7 + 4 * F)
+    close(torch.where(live.cuda(), got, torch.zeros_like(got)), torch.where(live, want, torch.zeros_like(want)), tol, "rotary")
+    assert bool((got == 9.0)[~live.cuda().expand_as(got)].all()), "rows past the length were written"
+    assert bool((got.cpu()[..., r:] == x[..., r:])[live.expand_as(x)[..., r:]].all()), "elements past rotary_dim are copies"
+    # in place, and by explicit positions: the same bits
+    again = a2sf.a2sf_rotary(plan, xc, out=xc, positions=(starts[:, None] + torch.arange(n, dtype=torch.int32)).cuda(),
+                             lens=lens.cuda(), transpose=transpose)
+    assert again.data_ptr() == xc.data_ptr()
+    assert torch.equal(again[live.cuda().expand_as(again)], got[live.cuda().expand_as(got)])
+
+
+def test_rotary_gradient_by_differences_and_inverse(a2sf):
+    plan = a2sf.a2sf_rotary_plan_init(64)
+    g = torch.Generator().manual_seed(3)
+    x, dy, e = (torch.randn((2, 3, 9, 64), generator=g).cuda() for _ in range(3))
+    dx = a2sf.a2sf_rotary(plan, dy, transpose=True)
+    # y is linear in x: <dy, y(x + h e) - y(x)> / h = <dx, e>, up to the rounding of the two forward passes
+    h = 0.5
+    diff = ((a2sf.a2sf_rotary(plan, x + h * e).double() - a2sf.a2sf_rotary(plan, x).double()) * dy.double()).sum() / h
+    want = (dx.double() * e.double()).sum()
+    tol = 8 * (2e-7 + 4 * F) * float((x.norm() + e.norm()) * dy.norm() / h)
+    assert abs(float(diff - want)) <= tol
+    back = a2sf.a2sf_rotary(plan, a2sf.a2sf_rotary(plan, x), transpose=True)
+    assert float((back - x).abs().max()) <= 2 * (2e-7 + 4 * F) * float(x.norm(dim=-1).max())
+
+
+# ---- append --------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("B,H,G,d,dtype,ps,c,r,il,layout", [
+    (1, 1, 1, 64, FP, 16, 1, 64, False, "bhnd"),
+    (3, 2, 4, 128, BF, 32, 37, 128, False, "bnhd"),
+    (2, 5, 3, 128, HF, 64, 130, 24, True, "bhnd"),
+    (4, 3, 8, 64, HF, 128, 5, 20, False, "bnhd"),
+    (2, 2, 2, 128, BF, 16, 17, 0, False, "bhnd"),
+])
+def test_append(a2sf, B, H, G, d, dtype, ps, c, r, il, layout):
+    past = [(5 * b + 3) % 41 for b in range(B)]
+    cache = pu.make_cache(a2sf, B, H, G, d, dtype, ps, past, c, seed=2)
+    before = {x: getattr(cache, x).cpu().clone() for x in ("k_pages", "v_pages", "scores", "positions")}
+    start = torch.tensor([1000 * b + 7 for b in range(B)], dtype=torch.int32)
+    cache.start.copy_(start)
+    g = torch.Generator().manual_seed(4)
+    lens = torch.tensor([c if b == 0 else (c * (b + 1)) % (c + 1) for b in range(B)], dtype=torch.int32)
+
+    def tensor(h):
+        t = torch.randn((B, h, c, d), generator=g).to(dtype)
+        return t, (t.cuda() if layout == "bhnd" else t.transpose(1, 2).contiguous().cuda().transpose(1, 2))
+
+    (k, kc), (v, vc), (q, qc) = tensor(H), tensor(H), tensor(H * G)
+    plan = a2sf.a2sf_rotary_plan_init(r, interleaved=il) if r else None
+    freqs = pu.inv_freq(r) if r else []
+    q_out = torch.full_like(qc, 5.0)
+    got = cache.a2sf_paged_append(kc, vc, lens=lens.cuda(), q=qc if r else None, q_out=q_out if r else None, rotary=plan)
+    after = {x: getattr(cache, x).cpu() for x in before}
+    want = {x: t.clone().double() if t.is_floating_point() else t.clone() for x, t in before.items()}
+    tol = {"k_pages": torch.zeros_like(want["k_pages"])}
+    u = torch.finfo(dtype).eps / 2
+    table = cache.page_table.cpu()
+    for b in range(B):
+        pos = start[b].long() + torch.arange(c)
+        kr = pu.rotate(k[b].double(), pos, freqs, il)
+        for t in range(int(lens[b])):
+            pg, o = int(table[b, (past[b] + t) // ps]), (past[b] + t) % ps
+            want["k_pages"][pg, :, o] = kr[:, t]
+            tol["k_pages"][pg, :, o] = u * kr[:, t].abs() + k[b, :, t].double().norm(dim=-1, keepdim=True) * (2e-7 + 4 * F) * bool(r)
+            want["v_pages"][pg, :, o] = v[b, :, t].double()
+            want["scores"][pg, :, o] = 0
+            want["positions"][pg, :, o] = int(pos[t])
+        if r:
+            n = int(lens[b])
+            qr = pu.rotate(q[b].double(), pos, freqs, il)
+            close(got[b, :, :n], qr[:, :n], u * qr[:, :n].abs() + q[b, :, :n].double().norm(dim=-1, keepdim=True) * (2e-7 + 4 * F), "q")
+            assert bool((got[b, :, n:] == 5.0).all())
+    garbage = torch.isnan(want["k_pages"])
+    assert torch.equal(torch.isnan(after["k_pages"]), garbage), "slots outside the chunk were touched"
+    close(torch.where(garbage.cuda(), torch.zeros_like(cache.k_pages), cache.k_pages), want["k_pages"].nan_to_num(0.0), tol["k_pages"], "keys")
+    assert torch.equal(after["v_pages"].double().nan_to_num(7.0), want["v_pages"].nan_to_num(7.0))
+    assert torch.equal(after["scores"].double().nan_to_num(7.0), want["scores"].nan_to_num(7.0))
+    assert torch.equal(after["positions"], want["positions"])
+    assert cache.past.tolist() == past
+
+
+# ---- attend ----------------------------------------------------------------------------------------------
+
+ATT = [
+    # B, H, G, d, dtype, ps, past, c, lens, alpha, layout, scale
+    (1, 1, 1, 64, FP, 16, [0], 1, None, 0.5, "bhnd", 0.0),                     # one token, nothing before it
+    (2, 2, 1, 64, FP, 16, [0, 0], 129, None, 0.5, "bhnd", 0.0),
+    (3, 2, 3, 128, FP, 32, [70, 0, 5], 33, [33, 0, 20], 0.9, "bnhd", 0.2),
+    (2, 1, 8, 128, FP, 64, [1000, 33], 1, [1, 0], 1.0, "bhnd", 0.0),
+    (2, 3, 5, 64, FP, 128, [200, 64], 70, [70, 69], 0.0, "bnhd", 0.0),
+    (4, 3, 1, 128, BF, 16, [204, 0, 63, 64], 1, None, 0.3, "bhnd", 0.0),       # few rows
+    (5, 2, 1, 128, BF, 64, [130, 7, 500, 0, 1], 1, [1, 0, 1, 1, 1], 0.5, "bhnd", 0.0),
+    (2, 2, 4, 128, HF, 64, [1999, 17], 4, [4, 3], 0.9, "bnhd", 0.0),
+    (2, 2, 8, 64, HF, 32, [333, 100], 1, None, 1.0, "bhnd", 0.0),
+    (1, 3, 8, 128, BF, 128, [640], 2, None, 0.0, "bhnd", 0.3),
+    (3, 1, 5, 64, BF, 16, [37, 0, 90], 3, [3, 2, 0], 0.7, "bnhd", 0.0),
+    (1, 2, 3, 128, HF, 16, [9000], 5, None, 0.99, "bhnd", 0.0),                # one long sequence
+    (2, 1, 2, 64, BF, 64, [4096, 4095], 1, None, 0.5, "bhnd", 0.0),
+    (1, 1, 1, 128, HF, 16, [0], 17, None, 0.5, "bhnd", 0.0),                   # many rows
+    (2, 2, 1, 128, BF, 64, [0, 0], 128, [128, 127], 0.9, "bhnd", 0.0),
+    (2, 2, 4, 128, HF, 32, [0, 300], 200, [200, 77], 1.0, "bnhd", 0.0),
+    (3, 1, 5, 128, BF, 16, [511, 0, 129], 100, [100, 0, 51], 0.5, "bhnd", 0.0),
+    (1, 2, 8, 64, HF, 128, [1000], 129, None, 0.9, "bhnd", 0.0),
+    (2, 1, 3, 64, BF, 64, [0, 77], 300, [300, 1], 1.0, "bnhd", 0.25),
+    (1, 1, 7, 128, BF, 16, [2500], 41, None, 0.0, "bhnd", 0.0),
+    (2, 3, 1, 128, HF, 128, [640, 1], 513, [513, 512], 0.999, "bhnd", 0.0),
+]
+
+
+def check_attend(a2sf, case, seed=5, garbage=float("nan"), gain=1.0):
+    B, H, G, d, dtype, ps, past, c, lens, alpha, layout, scale = case
+    lens = [c] * B if lens is None else lens
+    cache = pu.make_cache(a2sf, B, H, G, d, dtype, ps, past, c, seed=seed, scale=scale, garbage=garbage)
+    g = torch.Generator().manual_seed(seed + 1)
+
+    def tensor(h, k=1.0):
+        t = (torch.randn((B, h, c, d), generator=g) * k).to(dtype)
+        return t, (t.cuda() if layout == "bhnd" else t.transpose(1, 2).contiguous().cuda().transpose(1, 2))
+
+    (k, kc), (v, vc), (q, qc) = tensor(H), tensor(H), tensor(H * G, gain)
+    L = torch.tensor(lens, dtype=torch.int32).cuda()
+    cache.a2sf_paged_append(kc, vc, lens=L)
+    old = cache.scores.cpu().clone()
+    pool_k, pool_v = cache.k_pages.cpu().double(), cache.v_pages.cpu().double()
+    out, lse = torch.full_like(qc, 3.0), torch.full((B, H * G, c), 3.0, device="cuda")
+    cache.a2sf_paged_attend(qc, alpha, lens=L, out=out, lse=lse)
+    torch.cuda.synchronize()
+    sc = scale or 1 / math.sqrt(d)
+    u = torch.finfo(dtype).eps / 2
+    new, seen = cache.scores.cpu(), torch.zeros_like(old, dtype=torch.bool)
+    for b in range(B):
+        n, Lb = lens[b], past[b] + lens[b]
+        assert bool((out[b, :, n:] == 3.0).all()) and bool((lse[b, :, n:] == 3.0).all()), "rows past the length were written"
+        if n == 0:
+            continue
+        K, V, S, S1 = (pu.slots(cache, x, b, Lb) for x in (pool_k, pool_v, old.double(), new))
+        t, j = cache.page_table.cpu()[b].long(), torch.arange(Lb)
+        seen[t[j // ps], :, j % ps] = True
+        for h in range(H):
+            o, z, s, size, logit = pu.attend_ref(K[h], V[h], q[b, h * G:(h + 1) * G, :n].double(), S[h], past[b], alpha, sc)
+            e = (d + 2) * F * logit
+            rel = 2 * e + 2.0 ** -20
+            # out: its own rounding, a probability's rounding to the storage type (fp16: 2^-25 absolutely below its
+            # normal range, against a row sum of at least 1 at a scale of at most 2^8), the probability's own error
+            under = 0.0 if dtype != HF else 2.0 ** -25 * Lb * float(V[h].abs().max())
+            close(out[b, h * G:(h + 1) * G, :n], o, u * o.abs() + (u + rel + Lb * F) * size + under, f"out {b} {h}")
+            close(lse[b, h * G:(h + 1) * G, :n], z, torch.full_like(z, e + 2.0 ** -20) + 4 * F * z.abs(), f"lse {b} {h}")
+            # scores: a weight's exponent is at most 150 with two roundings; the sums and the decayed old score
+            close(S1[h], s, s * (rel + 150 * 2 * F + (n * G + 4) * F) + 1e-37, f"scores {b} {h}")
+    assert torch.equal(new[~seen].nan_to_num(7.0), old[~seen].nan_to_num(7.0)), "scores outside the sequences were touched"
+    return cache, qc, L, out, lse, old
+
+
+@pytest.mark.parametrize("case", ATT, ids=lambda c: "-".join(str(x).replace("torch.", "").replace(" ", "") for x in c))
+def test_attend(a2sf, case):
+    cache, qc, L, out, lse, old = check_attend(a2sf, case)
+    # the same call again: the same bits; without scores: the same outputs and untouched scores
+    cache.scores.copy_(old.cuda())
+    out2, lse2 = torch.full_like(out, 3.0), torch.full_like(lse, 3.0)
+    cache.a2sf_paged_attend(qc, case[9], lens=L, out=out2, lse=lse2)
+    first = cache.scores.clone()
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+    cache.scores.copy_(old.cuda())
+    cache.a2sf_paged_attend(qc, case[9], lens=L, out=out2, lse=lse2, scores=False)
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+    assert torch.equal(cache.scores.cpu().nan_to_num(7.0), old.nan_to_num(7.0))
+    cache.a2sf_paged_attend(qc, case[9], lens=L, out=out2, lse=lse2)
+    assert torch.equal(cache.scores.nan_to_num(7.0), first.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("dtype,c,past", [(BF, 1, 600), (HF, 1, 600), (FP, 1, 100), (BF, 150, 200), (HF, 150, 200), (HF, 4, 300)])
+def test_attend_large_logits_and_late_maximum(a2sf, dtype, c, past):
+    """Queries 12 times the usual size: logits of +-100, rows that one key takes whole, maxima that come late."""
+    check_attend(a2sf, (1, 2, 2, 128, dtype, 32, [past], c, None, 0.9, "bhnd", 0.0), seed=9, gain=12.0)
+
+
+@pytest.mark.parametrize("dtype,G,c,past", [(BF, 1, 1, 77), (HF, 4, 1, 200), (BF, 4, 40, 33), (FP, 1, 20, 30), (HF, 2, 150, 0)])
+def test_attend_infinities_behind_the_sequence(a2sf, dtype, G, c, past):
+    check_attend(a2sf, (2, 1, G, 128, dtype, 64, [past, 0], c, None, 0.5, "bhnd", 0.0), seed=11, garbage=float("inf"))
+
+
+@pytest.mark.parametrize("dtype,chunks", [(FP, [40, 1, 29]), (BF, [1, 64, 5, 140, 2]), (HF, [200, 10, 1, 1])])
+def test_chunks_of_a_prompt_give_the_scores_of_the_whole(a2sf, dtype, chunks):
+    """append + attend over any split of a prompt equals the dense prefill of the library, scores and outputs."""
+    B, H, d, n, alpha = 2, 3, 128, sum(chunks), 0.9
+    g = torch.Generator().manual_seed(7)
+    q, k, v = (torch.randn((B, H, n, d), generator=g).to(dtype).cuda() for _ in range(3))
+    p = a2sf.make_params(B, H, d, dtype, n, n, alpha)
+    out, scores, _, lse = a2sf.a2sf_prefill(p, q, k, v)
+    cache = a2sf.PagedCache(B, H, d, dtype, 16, 64, 30)
+    cache.page_table.copy_(torch.randperm(64, generator=g)[:60].view(2, 30).to(torch.int32))
+    at = 0
+    for c in chunks:
+        part = slice(at, at + c)
+        cache.a2sf_paged_append(k[:, :, part], v[:, :, part])
+        o, z = cache.a2sf_paged_attend(q[:, :, part], alpha)
+        u = torch.finfo(dtype).eps / 2
+        assert float((o.float() - out[:, :, part].float()).abs().max()) <= 4 * u * float(v.abs().max()) + 1e-5
+        assert float((z - lse[:, :, part]).abs().max()) <= 2e-5
+        cache.a2sf_paged_evict(n, 0, c)
+        at += c
+    assert cache.past.tolist() == [n] * B and cache.start.tolist() == [n] * B
+    got = torch.stack([pu.slots(cache, cache.scores.cpu(), b, n) for b in range(B)])
+    assert torch.allclose(got, scores.cpu(), rtol=1e-4, atol=1e-34)
+    pos = torch.stack([pu.slots(cache, cache.positions.cpu(), b, n) for b in range(B)])
+    assert torch.equal(pos, torch.arange(n, dtype=torch.int32).expand(B, H, n))
+
+
+# ---- evict -----------------------------------------------------------------------------------------------
+
+EVI = [
+    # B, H, d, dtype, ps, past, c, budget, recent, fresh, scores
+    (1, 1, 64, FP, 16, [0], 1, 1, 0, False, "rand"),
+    (2, 3, 128, BF, 32, [100, 20], 5, 40, 16, False, "rand"),
+    (2, 3, 128, BF, 32, [100, 20], 5, 40, 16, True, "rand"),
+    (3, 2, 64, HF, 16, [333, 0, 64], 1, 64, 0, False, "zeros"),
+    (3, 2, 64, HF, 16, [333, 0, 64], 1, 64, 64, True, "zeros"),
+    (1, 2, 128, FP, 64, [1500], 7, 700, 350, False, "ties"),
+    (1, 2, 128, FP, 64, [1500], 7, 1, 1, True, "ties"),
+    (2, 1, 64, BF, 128, [2100, 1000], 1, 2000, 10, False, "signed"),
+    (1, 1, 128, HF, 16, [20000], 3, 5000, 100, False, "rand"),
+    (1, 2, 64, BF, 16, [20000], 1, 600, 599, True, "ties"),
+    (2, 2, 64, BF, 16, [50, 60], 4, 100000, 7, False, "rand"),
+]
+
+
+@pytest.mark.parametrize("case", EVI, ids=lambda c: "-".join(str(x).replace("torch.", "").replace(" ", "") for x in c))
+def test_evict(a2sf, case):
+    B, H, d, dtype, ps, past, c, budget, recent, fresh, kind = case
+    n = [p + c for p in past]
+    cache = pu.make_cache(a2sf, B, H, 1, d, dtype, ps, n, 0, seed=3)         # the chunk is in place already
+    cache.past.copy_(torch.tensor(past, dtype=torch.int32))
+    start = [p + 1000 for p in past]
+    cache.start.copy_(torch.tensor(start, dtype=torch.int32))
+    g = torch.Generator().manual_seed(8)
+    sc = torch.rand(cache.scores.shape, generator=g)
+    if kind == "zeros":
+        sc.zero_()
+    elif kind == "ties":
+        sc = (sc * 4).floor()
+    elif kind == "signed":
+        sc = torch.where(sc < 0.2, torch.full_like(sc, float("inf")), torch.where(sc > 0.9, -0.0 * sc, sc - 0.5))
+        sc[sc.abs() < 0.01] = float("nan")
+    cache.scores.copy_(sc)
+    # positions: in no order, every head its own, up to the newest
+    table = cache.page_table.cpu().long()
+    for b in range(B):
+        for h in range(H):
+            pos = torch.randperm(n[b] + 1000, generator=g)[: n[b]].to(torch.int32)
+            j = torch.arange(n[b])
+            cache.positions[table[b, j // ps], h, j % ps] = pos.cuda()
+    before = {x: getattr(cache, x).cpu().clone() for x in ("k_pages", "v_pages", "scores", "positions")}
+    want = {x: t.clone() for x, t in before.items()}
+    dst = None
+    if fresh:
+        spare = -(-budget // ps)
+        extra = {x: torch.full((B * spare,) + t.shape[1:], 1, dtype=t.dtype) for x, t in want.items()}
+        base = want["scores"].shape[0]
+        want = {x: torch.cat([t, extra[x]]) for x, t in want.items()}
+        dst = (base + torch.randperm(B * spare, generator=g)).to(torch.int32).view(B, spare)
+        cache = a2sf.PagedCache(B, H, d, dtype, ps, base + B * spare, cache.max_pages, page_table=cache.page_table, past=cache.past,
+                                start=cache.start, **{x: t.cuda() for x, t in want.items()})
+        before = {x: t.clone() for x, t in want.items()}
+    for b in range(B):
+        m = min(n[b], budget)
+        for h in range(H):
+            j = torch.arange(n[b])
+            s = before["scores"][table[b, j // ps], h, j % ps].tolist()
+            s = [math.nextafter(math.inf, 0) if x == math.inf else math.inf if x != x else x for x in s]    # NaN beyond infinity
+            pos = before["positions"][table[b, j // ps], h, j % ps].tolist()
+            stay = pu.evict_ref(s, pos, n[b], budget, start[b] + c - recent)
+            if fresh:
+                moves = list(zip(stay, range(m)))
+            else:
+                holes = sorted(set(range(m)) - set(stay))
+                moves = list(zip([x for x in stay if x >= m], holes))
+            to_table = dst[b].long() if fresh else table[b]
+            for x in want:
+                for f, t in moves:
+                    want[x][to_table[t // ps], h, t % ps] = before[x][table[b, f // ps], h, f % ps]
+    cache.a2sf_paged_evict(budget, recent, c, dst_table=None if dst is None else dst.cuda())
+    assert cache.past.tolist() == [min(x, budget) for x in n]
+    assert cache.start.tolist() == [s + c for s in start]
+    for x in want:
+        got = getattr(cache, x).cpu()
+        if got.is_floating_point():
+            assert torch.equal(got.double().nan_to_num(1e9), want[x].double().nan_to_num(1e9)), x
+        else:
+            assert torch.equal(got, want[x]), x
+
+
+def test_evict_with_positions_given_twice_keeps_exactly_the_budget(a2sf):
+    """More recent slots than the budget holds (a position twice): ranked among themselves, lower slots leave first."""
+    cache = pu.make_cache(a2sf, 1, 1, 1, 64, FP, 16, [60], 0, seed=3)
+    cache.scores.fill_(0.5)
+    cache.positions.fill_(59)
+    cache.past.fill_(59)
+    cache.start.fill_(59)
+    cache.a2sf_paged_evict(20, 10, 1)
+    assert cache.past.item() == 20 and cache.start.item() == 60
+
+
+# ---- the whole step -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,G", [(BF, 1), (HF, 4), (FP, 2)])
+def test_generation_steps_equal_the_slot_cache(a2sf, dtype, G):
+    """append + attend + evict of single tokens is the generation step of the slot cache: same outputs, and the same
+    tokens stay (compared while no two scores at the cut are closer than the two paths' rounding)."""
+    B, H, d, n, M, R, T, alpha = 2, 2, 128, 96, 48, 16, 24, 0.9
+    g = torch.Generator().manual_seed(21)
+    q, k, v = (torch.randn((B, h, n + T, d), generator=g).to(dtype).cuda() for h in (H * G, H, H))
+    p = a2sf.make_params(B, H, d, dtype, M, R, alpha)
+    out, scores, kept, _ = a2sf.a2sf_prefill_group(p, G, q[:, :, :n].contiguous(), k[:, :, :n].contiguous(), v[:, :, :n].contiguous())
+    old = a2sf.Cache(p)
+    old.a2sf_cache_load(k[:, :, :n].contiguous(), v[:, :, :n].contiguous(), scores, kept)
+    new = a2sf.PagedCache(B, H, d, dtype, 16, 20, 9, group=G)
+    new.page_table.copy_(torch.randperm(18, generator=g).view(2, 9).to(torch.int32))
+    new.a2sf_paged_append(k[:, :, :n], v[:, :, :n])
+    new.a2sf_paged_attend(q[:, :, :n], alpha)
+    new.a2sf_paged_evict(M, R, n)
+    u = torch.finfo(dtype).eps / 2
+    o1 = torch.empty((B, H * G, d), dtype=dtype, device="cuda")
+    ev = torch.empty((B, H), dtype=torch.int32, device="cuda")
+    for t in range(n, n + T):
+        old.a2sf_decode_step_group(G, alpha, q[:, :, t].contiguous(), k[:, :, t].contiguous(), v[:, :, t].contiguous(), o1, ev)
+        new.a2sf_paged_append(k[:, :, t:t + 1], v[:, :, t:t + 1])
+        o2, _ = new.a2sf_paged_attend(q[:, :, t:t + 1], alpha)
+        new.a2sf_paged_evict(M, R, 1)
+        assert float((o1.float() - o2[:, :, 0].float()).abs().max()) <= 4 * u * float(v.abs().max()) + 1e-5
+    st = old.a2sf_cache_export()
+    pos = torch.stack([pu.slots(new, new.positions.cpu(), b, M) for b in range(B)])
+    assert torch.equal(st["pos"].cpu().sort(-1).values, pos.sort(-1).values)
+    a = torch.gather(st["scores"].cpu(), 2, st["pos"].cpu().argsort(-1))
+    b = torch.gather(torch.stack([pu.slots(new, new.scores.cpu(), x, M) for x in range(B)]), 2, pos.argsort(-1))
+    assert torch.allclose(a, b, rtol=2e-4, atol=1e-30)
+
+
+@pytest.mark.parametrize("dtype,c,past", [(BF, 1, 300), (HF, 150, 40), (FP, 20, 50)])
+def test_graph_replay_and_other_stream(a2sf, dtype, c, past):
+    """A captured step, replayed on new inputs while lengths move on, equals direct calls on another stream."""
+    B, H, G, d, M = 2, 2, 2, 128, past
+    plan = a2sf.a2sf_rotary_plan_init(d)
+    g = torch.Generator().manual_seed(2)
+    ins = [[torch.randn((B, h, c, d), generator=g).to(dtype).cuda() for h in (H * G, H, H)] for _ in range(3)]
+    a, b = (pu.make_cache(a2sf, B, H, G, d, dtype, 32, [past, past // 2], 2 * c, seed=6) for _ in range(2))
+
+    def step(cache, q, k, v, q2, out, lse):
+        cache.a2sf_paged_append(k, v, q=q, q_out=q2, rotary=plan)
+        cache.a2sf_paged_attend(q2, 0.9, out=out, lse=lse)
+        cache.a2sf_paged_evict(M, 8, c)
+
+    q, k, v = (x.clone() for x in ins[0])
+    q2, out, lse = torch.empty_like(q), torch.empty_like(q), torch.empty((B, H * G, c), device="cuda")
+    warm = pu.make_cache(a2sf, B, H, G, d, dtype, 32, [past, past // 2], 2 * c, seed=6)
+    step(warm, q, k, v, q2, out, lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a, q, k, v, q2, out, lse)
+    side = torch.cuda.Stream()
+    for x in ins:
+        for dst, src in zip((q, k, v), x):
+            dst.copy_(src)
+        graph.replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            r2, o2, z2 = torch.empty_like(q), torch.empty_like(q), torch.empty_like(lse)
+            step(b, *x, r2, o2, z2)
+        side.synchronize()
+        assert torch.equal(out, o2) and torch.equal(lse, z2) and torch.equal(q2, r2)
+        for name in ("k_pages", "v_pages", "scores", "positions", "past", "start"):
+            assert torch.equal(getattr(a, name).double().nan_to_num(7.0), getattr(b, name).double().nan_to_num(7.0)), name
+
+
+# ---- what the device finds out ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,c", [(FP, 3), (BF, 1), (HF, 150), (BF, 4)])
+@pytest.mark.parametrize("bad", [-1, -2 ** 31, 2 ** 31 - 1, "pages", "past", "negative", "length"])
+def test_bad_pages_and_lengths_are_reported_and_not_followed(a2sf, dtype, c, bad):
+    cache = pu.make_cache(a2sf, 2, 2, 1, 128, dtype, 16, [40, 30], c, seed=4, garbage=0.0)
+    lens = torch.full((2,), c, dtype=torch.int32, device="cuda")
+    if bad == "past":
+        cache.past[1] = cache.max_pages * 16 + 5
+    elif bad == "negative":
+        cache.past[1] = -3
+    elif bad == "length":
+        lens[1] = -4
+    else:
+        cache.page_table[1, :] = cache.num_pages if bad == "pages" else bad
+    guard = {x: getattr(cache, x).clone() for x in ("v_pages", "positions")}
+    x = torch.randn((2, 2, c, 128), device="cuda").to(dtype)
+    plan = a2sf.a2sf_rotary_plan_init(128)
+    for call in (lambda: cache.a2sf_paged_append(x, x, q=x, rotary=plan, lens=lens), lambda: cache.a2sf_paged_attend(x, 0.5, lens=lens),
+                 lambda: cache.a2sf_paged_evict(20, 4, c, lens=lens, past_out=torch.empty_like(cache.past), start_out=torch.empty_like(cache.past))):
+        call()
+        assert a2sf.a2sf_last_device_status() == a2sf.A2SF_ERR_INVALID_ARG
+        assert a2sf.a2sf_last_device_status() == a2sf.A2SF_OK
+    # the other sequence's pages and the unused ones: only its own chunk was written
+    own = cache.page_table[0].long()
+    others = torch.ones(cache.num_pages, dtype=torch.bool, device="cuda")
+    others[own] = False
+    if bad not in ("past", "negative", "length"):
+        assert torch.equal(cache.v_pages[others], guard["v_pages"][others])
+        assert torch.equal(cache.positions[others], guard["positions"][others])
