@@ -1,6 +1,7 @@
 // Host side of the paged-cache and rotary entry points: argument validation, workspaces, dispatch.
 // No data is touched on the host.
 #include <cmath>
+#include <mutex>
 
 #include "paged.cuh"
 
@@ -49,7 +50,7 @@ int check_paged(const a2sf_paged *p, int c)
     if (!(p->scale >= 0.f) || std::isinf(p->scale)) return A2SF_ERR_INVALID_ARG;
     // slots of a sequence, units, folded rows and tiles of a call all stay 32-bit numbers
     if ((int64_t)p->max_pages * p->page_size > (1 << 28) || (int64_t)c * p->group > (1 << 28) ||
-        (int64_t)p->B * p->H * p->group > (1 << 24) || (int64_t)p->num_pages * p->H * p->page_size >= (1ll << 32))
+        (int64_t)p->B * p->H * p->group > (1 << 24) || (int64_t)p->num_pages * p->H * p->page_size >= (1ll << 31))
         return A2SF_ERR_UNSUPPORTED;
     if (!p->k_pages || !p->v_pages || !p->scores || !p->positions || !p->page_table || !p->past) return A2SF_ERR_INVALID_ARG;
     if (!aligned(p->k_pages, 16) || !aligned(p->v_pages, 16) || !aligned(p->scores, 4) || !aligned(p->positions, 4) ||
@@ -72,7 +73,44 @@ PagedView make_view(const a2sf_paged *p, int c, const int32_t *lens)
     return v;
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn()
+{
+    static EncodeTiledFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    });
+    return fn;
+}
+
+// Few rows go through the split kernel, more rows of any type through the tiled one.
+bool few_rows(const a2sf_paged *p, int c) { return (int64_t)c * p->group <= kFewRows; }
+
 }  // namespace
+
+bool make_pool_map(CUtensorMap *map, int dtype, const void *pool, const PagedView &pv, int box_rows)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const int e = elem_bytes(dtype);
+    const cuuint64_t dims[2] = {(cuuint64_t)pv.d, (cuuint64_t)pv.num_pages * pv.H * pv.ps};
+    const cuuint64_t strides[1] = {(cuuint64_t)pv.d * e};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / e), (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUtensorMapDataType dt = dtype == A2SF_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == A2SF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return fn(map, dt, 2, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace a2sf
 
 using namespace a2sf;
@@ -192,7 +230,8 @@ int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary, i
 size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c)
 {
     if (check_paged(cache, c) != A2SF_OK) return 0;
-    return align_up(attend_simt_ws_bytes(make_view(cache, c, nullptr)));
+    const PagedView pv = make_view(cache, c, nullptr);
+    return align_up(few_rows(cache, c) ? attend_few_ws_bytes(pv) : attend_simt_ws_bytes(pv));
 }
 
 int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha, const void *q,
@@ -220,7 +259,9 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
     a.alpha = alpha; a.nl2a = neg_log2(alpha);
     a.scores = !(flags & A2SF_ATTEND_NO_SCORES);
     a.ws = workspace;
-    return launch_attend_simt(cache->dtype, a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = few_rows(cache, c) ? launch_attend_few(cache->dtype, a, s) : launch_attend_simt(cache->dtype, a, s);
+    return e == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
 }
 
 size_t a2sf_paged_evict_workspace_bytes(const a2sf_paged *cache, int32_t budget)

@@ -1,6 +1,8 @@
 // The cache in pages: what its kernels share (device view, page lookups, division of work).
 #pragma once
 
+#include <cuda.h>
+
 #include "common.cuh"
 
 namespace a2sf {
@@ -99,6 +101,14 @@ struct AttendArgs {
     bool scores;
     void *ws;
 };
+// Tensor map of a pool: rows of d elements, boxes of 128 bytes x box_rows rows, 128-byte swizzle.
+bool make_pool_map(CUtensorMap *map, int dtype, const void *pool, const PagedView &pv, int box_rows);
+
+// few rows (len * G <= kFewRows): the cache is read once, split evenly over the device
+constexpr int kFewRows = 16;
+size_t attend_few_ws_bytes(const PagedView &pv);
+cudaError_t launch_attend_few(int dtype, const AttendArgs &a, cudaStream_t s);
+
 size_t attend_simt_ws_bytes(const PagedView &pv);
 cudaError_t launch_attend_simt(int dtype, const AttendArgs &a, cudaStream_t s);
 

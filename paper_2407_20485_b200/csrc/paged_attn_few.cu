@@ -1,0 +1,691 @@
+// Attention of a few rows (len * G <= 16: generation, drafted tokens) over a paged cache.
+//
+// Every K and V row is read once and used for at most 16 rows: the cache's bytes bound this, and there
+// may be one long sequence or a thousand ragged ones.  So the work is cut without regard to either: the
+// 64-slot tiles of all (sequence, K/V head) units form one list, every CTA takes an equal, contiguous
+// share, and a share that begins or ends inside a unit leaves partial results that the finish kernel joins.
+// The list is built on the device from past and lens (the host knows neither).
+//
+//   main    warp 0 copies tiles (K and V, TMA boxes of up to a page, 128-byte swizzle) into a ring;
+//           warps 1-4 take 16 slots of each tile, keep their own running maximum, sum and output, and
+//           never meet each other.  16-bit storage: S[16 slots x 8 rows] = K Q^T and O^T[d x 8] += V^T P^T
+//           on mma.sync m16n8k16, K and V^T straight from ldmatrix (.trans for V); P changes from
+//           accumulator to operand layout with movmatrix.  The rows fill 8 of the instruction's columns, so
+//           the tensor rate is of no account and tcgen05 (128 rows at least) would compute on padding.
+//           32-bit storage: the same on the CUDA cores.  Logits go to the workspace (4 bytes per slot and
+//           row next to 4 d or 8 d bytes of K and V) so that scores need no second pass over K.
+//   finish  joins the partial outputs; S <- alpha^len S + sum_r alpha^age exp2(x_r - lse_r).
+// P is rounded to the storage type for P V (half a step, as the output itself); the row sum and the
+// scores use the unrounded values.
+#include "paged.cuh"
+#include "tc_sm100.cuh"
+
+namespace a2sf {
+
+A2SF_DEBUG_TRANSLATION_UNIT(paged_attn_few)
+
+namespace {
+
+using namespace tc;
+
+constexpr int kTile = 64;                 // slots per tile
+constexpr int kWarps = 4;                 // consumer warps, 16 slots each
+constexpr int kFewThreads = 32 * (kWarps + 1);
+constexpr int kFinishThreads = 256;
+constexpr int kScoreChunk = 2048;         // slots per score block of the finish kernel
+
+__host__ __device__ constexpr int rows_padded(int rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
+
+template <typename T, int D> struct Ring {
+    static constexpr int kRowBytes = D * (int)sizeof(T);
+    static constexpr int kChunks = kRowBytes / 128;                // 128-byte columns of a tile
+    static constexpr int kTileBytes = kTile * kRowBytes;           // K or V
+    static constexpr int kStages = kRowBytes == 512 ? 2 : kRowBytes == 256 ? 3 : 6;
+    static constexpr size_t kBytes = (size_t)kStages * 2 * kTileBytes + 1024;
+};
+
+struct FewWs {
+    float *logits;        // [U][slots][NP], log2 units
+    float2 *ml;           // [segments][kWarps][NP] running maximum (log2 units), sum
+    float *o;             // [segments][kWarps][NP][D]
+    int32_t *prefix;      // [B + 1] tiles of a head, summed over the sequences before
+    int slots;            // padded slots of a unit
+};
+
+struct Where {            // position in the list of tiles
+    int b, h, t, tiles;
+};
+
+// Tiles of one head of sequence b.
+__device__ __forceinline__ int seq_tiles(const PagedView &pv, int b)
+{
+    const SeqState st = seq_state(pv, b);
+    return st.len > 0 ? (st.past + st.len + kTile - 1) / kTile : 0;
+}
+
+__device__ __forceinline__ Where locate(const int32_t *prefix, int B, int H, long long w)
+{
+    int lo = 0, hi = B - 1;                        // last b with H * prefix[b] <= w
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((long long)H * prefix[mid] <= w) lo = mid;
+        else hi = mid - 1;
+    }
+    Where x;
+    x.b = lo;
+    x.tiles = prefix[lo + 1] - prefix[lo];
+    const long long rest = w - (long long)H * prefix[lo];
+    x.h = (int)(rest / x.tiles);
+    x.t = (int)(rest - (long long)x.h * x.tiles);
+    return x;
+}
+
+__device__ __forceinline__ void next_unit(Where &x, const int32_t *prefix, int B, int H)
+{
+    x.t = 0;
+    if (++x.h < H) return;
+    x.h = 0;
+    do ++x.b; while (x.b < B && prefix[x.b + 1] == prefix[x.b]);
+    x.tiles = x.b < B ? prefix[x.b + 1] - prefix[x.b] : 0;
+}
+
+template <typename T> struct Mma16;
+template <> struct Mma16<__half> {
+    __device__ static void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+    {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    __device__ static uint32_t pack(float lo, float hi)
+    {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+};
+template <> struct Mma16<__nv_bfloat16> {
+    __device__ static void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+    {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    __device__ static uint32_t pack(float lo, float hi)
+    {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+};
+
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Byte offset of 16-byte piece `piece` of row `row` in a tile of 128-byte columns (TMA's 128-byte swizzle).
+__device__ __forceinline__ uint32_t tile_offset(int row, int piece)
+{
+    return (uint32_t)((piece >> 3) * (kTile * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+}
+
+__device__ __forceinline__ const void *query_row(const AttendArgs &a, int b, int h, int r, size_t elem)
+{
+    const int i = r / a.pv.G, g = r - i * a.pv.G;
+    return static_cast<const char *>(a.q) + (b * a.sq.b + (int64_t)(h * a.pv.G + g) * a.sq.h + (int64_t)i * a.sq.t) * elem;
+}
+
+// ---- a consumer warp on 16-bit storage: NC = 8 or 16 row columns ------------------------------------
+template <typename T, int D, int NC> struct Body16 {
+    static constexpr int CG = NC / 8, KS = D / 16;
+    uint32_t q[CG][KS][2];
+    float o[CG][KS][4], m[CG][2], l[CG][2];
+    int vis[CG][2];
+
+    __device__ void begin(const AttendArgs &a, const Where &x, const SeqState &st, float *)
+    {
+        const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3, rows = st.len * a.pv.G;
+#pragma unroll
+        for (int g = 0; g < CG; ++g) {
+            const int row = g * 8 + r;
+            const uint32_t *src = row < rows ? static_cast<const uint32_t *>(query_row(a, x.b, x.h, row, sizeof(T))) : nullptr;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                q[g][k][0] = src ? src[k * 8 + c] : 0u;
+                q[g][k][1] = src ? src[k * 8 + c + 4] : 0u;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[g][k][e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int col = g * 8 + 2 * c + e;
+                vis[g][e] = col < rows ? st.past + col / a.pv.G + 1 : 0;
+                m[g][e] = -INFINITY;
+                l[g][e] = 0.f;
+            }
+        }
+    }
+
+    // 16 slots j0 .. j0+15 (rows `row0` .. of the tile); `used` slots of the sequence hold tokens
+    __device__ void tile(const AttendArgs &a, uint8_t *K, uint8_t *V, int row0, int j0, int used, float *logits, int NP, float *)
+    {
+        const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+        float s[CG][4];
+#pragma unroll
+        for (int g = 0; g < CG; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[g][e] = 0.f;
+        const uint32_t kb = smem_u32(K), vb = smem_u32(V);
+        {
+            const int row = row0 + (lane & 15), piece = lane >> 4;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                uint32_t f[4];
+                ldmatrix4(f, kb + tile_offset(row, 2 * k + piece));
+#pragma unroll
+                for (int g = 0; g < CG; ++g) Mma16<T>::mma(s[g], f, q[g][k][0], q[g][k][1]);
+            }
+        }
+        // what lies behind the sequence may be anything: its keys are masked, its values made zero
+        if (j0 + 16 > used) {
+            for (int x = lane; x < 16 * (D / 8); x += 32) {
+                const int rr = x / (D / 8);
+                if (j0 + rr >= used) *reinterpret_cast<uint4 *>(V + tile_offset(row0 + rr, x % (D / 8))) = make_uint4(0, 0, 0, 0);
+            }
+            fence_async_smem();            // these writes come before the copy that next fills the stage
+            __syncwarp();
+        }
+        uint32_t p0[CG], p1[CG];
+        bool moved = false;
+        float f[CG][2];
+#pragma unroll
+        for (int g = 0; g < CG; ++g) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = j0 + r + (e >> 1) * 8;
+                x[e] = j < vis[g][e & 1] ? s[g][e] * a.pv.sl2 : -INFINITY;
+            }
+            if (logits) {
+                const int col = g * 8 + 2 * c;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float *dst = logits + (size_t)(j0 + r + half * 8) * NP + col;
+                    if (col + 1 < NP) *reinterpret_cast<float2 *>(dst) = make_float2(x[2 * half], x[2 * half + 1]);
+                    else if (col < NP) *dst = x[2 * half];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float mx = fmaxf(x[e], x[e + 2]);
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                const float mn = fmaxf(m[g][e], mx);
+                // all of a row masked so far: any finite reference gives the zeros that are wanted
+                const float ref = mn == -INFINITY ? 0.f : mn;
+                f[g][e] = ex2(m[g][e] - ref);
+                moved |= f[g][e] != 1.f;
+                m[g][e] = mn;
+                x[e] = ex2(x[e] - ref);
+                x[e + 2] = ex2(x[e + 2] - ref);
+                l[g][e] = fmaf(l[g][e], f[g][e], x[e] + x[e + 2]);
+            }
+            p0[g] = movmatrix_trans(Mma16<T>::pack(x[0], x[1]));
+            p1[g] = movmatrix_trans(Mma16<T>::pack(x[2], x[3]));
+        }
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int g = 0; g < CG; ++g)
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[g][k][e] *= f[g][e & 1];
+        }
+        {
+            const int row = row0 + (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                uint32_t v[4];
+                ldmatrix4_trans(v, vb + tile_offset(row, 2 * k + piece));
+#pragma unroll
+                for (int g = 0; g < CG; ++g) Mma16<T>::mma(o[g][k], v, p0[g], p1[g]);
+            }
+        }
+    }
+
+    __device__ void end(float2 *ml, float *op, int NP)
+    {
+        const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+#pragma unroll
+        for (int g = 0; g < CG; ++g)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float sum = l[g][e];
+                sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                const int col = g * 8 + 2 * c + e;
+                if (col >= NP) continue;
+                if (r == 0) ml[col] = make_float2(m[g][e], sum);
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    op[(size_t)col * D + k * 16 + r] = o[g][k][e];
+                    op[(size_t)col * D + k * 16 + 8 + r] = o[g][k][2 + e];
+                }
+            }
+    }
+};
+
+// ---- a consumer warp on 32-bit storage: NC rows, all in use or zero ----------------------------------
+template <int D, int NC> struct Body32 {
+    static constexpr int DV = D / 32;                       // output elements per lane
+    float o[NC][DV], m[NC], l[NC];
+    int rows, G, past;
+
+    // scratch: [NC][D] queries, then [16][NC] probabilities of this warp
+    __device__ void begin(const AttendArgs &a, const Where &x, const SeqState &st, float *scratch)
+    {
+        const int lane = threadIdx.x & 31;
+        rows = st.len * a.pv.G; G = a.pv.G; past = st.past;
+        __syncwarp();
+#pragma unroll 1
+        for (int r = 0; r < NC; ++r)
+            for (int k = lane; k < D; k += 32)
+                scratch[r * D + k] = r < rows ? static_cast<const float *>(query_row(a, x.b, x.h, r, 4))[k] : 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < NC; ++r) {
+            m[r] = -INFINITY; l[r] = 0.f;
+#pragma unroll
+            for (int e = 0; e < DV; ++e) o[r][e] = 0.f;
+        }
+    }
+
+    __device__ void tile(const AttendArgs &a, uint8_t *K, uint8_t *V, int row0, int j0, int used, float *logits, int, float *scratch)
+    {
+        const int lane = threadIdx.x & 31, s = lane & 15, hf = lane >> 4;
+        float *P = scratch + NC * D;
+        float acc[NC];
+#pragma unroll
+        for (int r = 0; r < NC; ++r) acc[r] = 0.f;
+#pragma unroll 4
+        for (int k = hf * (D / 2); k < (hf + 1) * (D / 2); k += 4) {
+            const float4 kk = *reinterpret_cast<const float4 *>(K + tile_offset(row0 + s, k / 4));
+#pragma unroll
+            for (int r = 0; r < NC; ++r) {
+                const float4 qq = *reinterpret_cast<const float4 *>(scratch + r * D + k);
+                acc[r] = fmaf(qq.x, kk.x, acc[r]);
+                acc[r] = fmaf(qq.y, kk.y, acc[r]);
+                acc[r] = fmaf(qq.z, kk.z, acc[r]);
+                acc[r] = fmaf(qq.w, kk.w, acc[r]);
+            }
+        }
+        const int j = j0 + s;
+        __syncwarp();                                       // the previous tile's probabilities have been read
+#pragma unroll
+        for (int r = 0; r < NC; ++r) {
+            const float dot = acc[r] + __shfl_xor_sync(0xffffffffu, acc[r], 16);
+            const bool seen = r < rows && j < past + r / G + 1;
+            const float x = seen ? dot * a.pv.sl2 : -INFINITY;
+            if (logits && hf == 0) logits[(size_t)j * NC + r] = x;
+            float mx = x;
+#pragma unroll
+            for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+            const float mn = fmaxf(m[r], mx);
+            const float ref = mn == -INFINITY ? 0.f : mn;
+            const float f = exp2f(m[r] - ref), p = exp2f(x - ref);
+            m[r] = mn;
+            l[r] = fmaf(l[r], f, p);                        // every half-warp holds the sum over its 16 slots
+            if (hf == 0) P[s * NC + r] = p;
+#pragma unroll
+            for (int e = 0; e < DV; ++e) o[r][e] *= f;
+        }
+        __syncwarp();
+        const int n = min(16, used - j0);                   // values behind the sequence are not touched
+        for (int x = 0; x < n; ++x) {
+            float v[DV];
+            const uint8_t *src = V + tile_offset(row0 + x, lane * DV / 4) + (lane * DV % 4) * 4;
+#pragma unroll
+            for (int e = 0; e < DV; e += 2) *reinterpret_cast<float2 *>(v + e) = *reinterpret_cast<const float2 *>(src + e * 4);
+#pragma unroll
+            for (int r = 0; r < NC; ++r) {
+                const float p = P[x * NC + r];
+#pragma unroll
+                for (int e = 0; e < DV; ++e) o[r][e] = fmaf(p, v[e], o[r][e]);
+            }
+        }
+    }
+
+    __device__ void end(float2 *ml, float *op, int)
+    {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int r = 0; r < NC; ++r) {
+            float sum = l[r];
+#pragma unroll
+            for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+            if (lane == 0) ml[r] = make_float2(m[r], sum);
+#pragma unroll
+            for (int e = 0; e < DV; ++e) op[(size_t)r * D + lane * DV + e] = o[r][e];
+        }
+    }
+};
+
+template <typename T, int D, int NC> struct BodyOf { typedef Body16<T, D, NC> type; static constexpr size_t kScratch = 0; };
+template <int D, int NC> struct BodyOf<float, D, NC> {
+    typedef Body32<D, NC> type;
+    static constexpr size_t kScratch = (size_t)kWarps * (NC * D + 16 * NC) * sizeof(float);
+};
+
+struct FewShared {
+    uint64_t full[6], empty[6];
+    int abort_flag;
+    int32_t prefix[A2SF_PAGED_MAX_SEQUENCES + 1];
+};
+
+template <typename T, int D, int NC>
+__global__ void __launch_bounds__(kFewThreads)
+paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                 const __grid_constant__ AttendArgs a, const __grid_constant__ FewWs ws, int NP)
+{
+    using R = Ring<T, D>;
+    using Body = typename BodyOf<T, D, NC>::type;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ FewShared sh;
+    const PagedView &pv = a.pv;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int *abort_flag = &sh.abort_flag;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            for (int s = 0; s < R::kStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], kWarps); }
+            sh.abort_flag = 0;
+            fence_mbar_init();
+            prefetch_tmap(&map_k);
+            prefetch_tmap(&map_v);
+        }
+        int run = 0;
+        for (int b0 = 0; b0 < pv.B; b0 += 32) {
+            const int b = b0 + lane, t = b < pv.B ? seq_tiles(pv, b) : 0;
+            int incl = t;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += x;
+            }
+            if (b < pv.B) sh.prefix[b + 1] = run + incl;
+            run += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (lane == 0) sh.prefix[0] = 0;
+    }
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b <= pv.B; b += kFewThreads) ws.prefix[b] = sh.prefix[b];
+    const long long total = (long long)pv.H * sh.prefix[pv.B];
+    const long long share = (total + gridDim.x - 1) / gridDim.x;
+    const long long w0 = blockIdx.x * share, w1 = w0 + share < total ? w0 + share : total;
+    if (w0 >= w1) return;
+    Where x = locate(sh.prefix, pv.B, pv.H, w0);
+
+    if (warp == 0) {
+        // ---- producer: lane i copies box i of the tile --------------------------------------------
+        const int box = min(pv.ps, kTile), boxes = kTile / box;
+        int it = 0;
+        for (long long w = w0; w < w1;) {
+            const SeqState st = seq_state(pv, x.b);
+            const int used = st.past + st.len;
+            const int32_t *table = pv.table + (size_t)x.b * pv.max_pages;
+            for (; x.t < x.tiles && w < w1; ++x.t, ++w, ++it) {
+                const int s = it % R::kStages;
+                const int slot = x.t * kTile + lane * box;
+                const int nbox = min(boxes, (used - x.t * kTile + box - 1) / box);
+                int row = 0;
+                if (lane < nbox) row = (int)pool_row(pv, page_for_read(pv, table, slot), x.h, slot);
+                int ok = 1;
+                if (lane == 0) {
+                    if (it >= R::kStages) ok = mbar_wait(&sh.empty[s], ((it / R::kStages) & 1) ^ 1, abort_flag) ? 1 : 0;
+                    if (ok) mbar_arrive_expect_tx(&sh.full[s], (uint32_t)(nbox * box * R::kRowBytes * 2));
+                }
+                if (!__shfl_sync(0xffffffffu, ok, 0)) goto drained;
+                if (lane < nbox) {
+                    uint8_t *dst = ring + (size_t)s * 2 * R::kTileBytes + lane * box * 128;
+#pragma unroll
+                    for (int ch = 0; ch < R::kChunks; ++ch) {
+                        tma_load_2d(dst + ch * (kTile * 128), &map_k, &sh.full[s], ch * (128 / (int)sizeof(T)), row);
+                        tma_load_2d(dst + R::kTileBytes + ch * (kTile * 128), &map_v, &sh.full[s], ch * (128 / (int)sizeof(T)), row);
+                    }
+                }
+                __syncwarp();
+            }
+            if (w < w1) next_unit(x, sh.prefix, pv.B, pv.H);
+        }
+drained:
+        if (lane == 0 && *abort_flag) {
+            // copies still in flight get a bounded chance to land before the CTA exits
+            int dummy = 0;
+            for (int k = max(0, it - R::kStages); k < it; ++k)
+                mbar_wait(&sh.full[k % R::kStages], (k / R::kStages) & 1, &dummy);
+            *pv.status = A2SF_ERR_TIMEOUT;
+        }
+    } else {
+        // ---- consumers ---------------------------------------------------------------------------
+        const int cw = warp - 1;
+        float *scratch = reinterpret_cast<float *>(ring + (size_t)R::kStages * 2 * R::kTileBytes) +
+                         cw * (BodyOf<T, D, NC>::kScratch / kWarps / sizeof(float));
+        Body body;
+        int it = 0;
+        for (long long w = w0; w < w1;) {
+            const SeqState st = seq_state(pv, x.b);
+            const int used = st.past + st.len;
+            const int unit = x.b * pv.H + x.h;
+            float *logits = a.scores ? ws.logits + (size_t)unit * ws.slots * NP : nullptr;
+            body.begin(a, x, st, scratch);
+            for (; x.t < x.tiles && w < w1; ++x.t, ++w, ++it) {
+                const int s = it % R::kStages;
+                if (!*abort_flag && !mbar_wait(&sh.full[s], (it / R::kStages) & 1, abort_flag)) *pv.status = A2SF_ERR_TIMEOUT;
+                const int j0 = x.t * kTile + cw * 16;
+                uint8_t *K = ring + (size_t)s * 2 * R::kTileBytes;
+                if (j0 < used) body.tile(a, K, K + R::kTileBytes, cw * 16, j0, used, logits, NP, scratch);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.empty[s]);
+            }
+            // segment = CTA + unit: both only grow along the list, one of them at every boundary
+            const size_t seg = ((size_t)blockIdx.x + unit) * kWarps + cw;
+            body.end(ws.ml + seg * NP, ws.o + seg * NP * D, NP);
+            if (w < w1) next_unit(x, sh.prefix, pv.B, pv.H);
+        }
+    }
+}
+
+// Blocks 0 .. U*NP-1: one output row each.  The following ones: kScoreChunk slots of a unit each.
+template <typename T, int D>
+__global__ void __launch_bounds__(kFinishThreads)
+paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ FewWs ws, int NP, int ctas, int chunks)
+{
+    __shared__ float red[kFinishThreads], row_c[kFewRows];
+    const PagedView &pv = a.pv;
+    const int U = pv.B * pv.H, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool is_out = (int)blockIdx.x < U * NP;
+    const int id = is_out ? blockIdx.x : blockIdx.x - U * NP;
+    const int u = is_out ? id / NP : id / chunks, b = u / pv.H, h = u - b * pv.H;
+    const SeqState st = seq_state(pv, b);
+    const int rows = st.len * pv.G, used = st.past + st.len;
+    if (rows == 0) return;
+    // the CTAs of the main kernel that had a part of this unit
+    const long long total = (long long)pv.H * ws.prefix[pv.B], share = (total + ctas - 1) / ctas;
+    const int tiles = ws.prefix[b + 1] - ws.prefix[b];
+    const long long u0 = (long long)pv.H * ws.prefix[b] + (long long)h * tiles;
+    const int k0 = (int)(u0 / share), k1 = (int)((u0 + tiles - 1) / share);
+    const size_t seg0 = ((size_t)k0 + u) * kWarps;
+    const int parts = (k1 - k0 + 1) * kWarps;
+    if (is_out) {
+        const int r = id - u * NP;
+        if (r >= rows) return;
+        const float2 *ml = ws.ml + seg0 * NP + r;
+        float mx = -INFINITY;
+        for (int p = tid; p < parts; p += kFinishThreads) mx = fmaxf(mx, ml[(size_t)p * NP].x);
+        mx = warp_max(mx);
+        if (lane == 0) red[warp] = mx;
+        __syncthreads();
+        mx = red[0];
+#pragma unroll
+        for (int w = 1; w < kFinishThreads / 32; ++w) mx = fmaxf(mx, red[w]);
+        __syncthreads();
+        // thread groups take every GR-th partial; joined in a fixed order
+        constexpr int GR = kFinishThreads / D;
+        const int d = tid % D, grp = tid / D;
+        float sum = 0.f, o = 0.f;
+#pragma unroll 4
+        for (int p = grp; p < parts; p += GR) {
+            const float2 x = ml[(size_t)p * NP];
+            const float f = exp2f(x.x - mx);
+            sum = fmaf(f, x.y, sum);
+            o = fmaf(f, ws.o[((seg0 + p) * NP + r) * D + d], o);
+        }
+        red[tid] = o;
+        __shared__ float red_l[GR];
+        if (d == 0) red_l[grp] = sum;
+        __syncthreads();
+        if (grp == 0) {
+            float l = red_l[0];
+#pragma unroll
+            for (int x = 1; x < GR; ++x) { l += red_l[x]; o += red[x * D + d]; }
+            const int i = r / pv.G, g = r - i * pv.G;
+            static_cast<T *>(a.out)[b * a.so.b + (int64_t)(h * pv.G + g) * a.so.h + (int64_t)i * a.so.t + d] = Elem<T>::from_float(o / l);
+            if (d == 0 && a.lse)
+                a.lse[((size_t)u * pv.G + g) * pv.c + i] = (mx + log2f(l)) * 0.6931471805599453f;
+        }
+        return;
+    }
+    const int j0 = (id - u * chunks) * kScoreChunk;
+    if (j0 >= used) return;
+    // a row's constant: log-sum-exp and the weight's exponent (log2 units)
+    for (int r = warp; r < NP; r += kFinishThreads / 32) {
+        const float2 *ml = ws.ml + seg0 * NP + r;
+        float mx = -INFINITY, l = 0.f;
+        for (int p = lane; p < parts; p += 32) mx = fmaxf(mx, ml[(size_t)p * NP].x);
+        mx = warp_max(mx);
+        for (int p = lane; p < parts; p += 32) {
+            const float2 x = ml[(size_t)p * NP];
+            l += x.y > 0.f ? exp2f(x.x - mx) * x.y : 0.f;
+        }
+        l = warp_sum(l);
+        if (lane == 0) row_c[r] = r < rows ? mx + log2f(l) + age_exponent(st.len - 1 - r / pv.G, a.nl2a) : INFINITY;
+    }
+    __syncthreads();
+    const float decay = exp2f(-age_exponent(st.len, a.nl2a));
+    const float *logits = ws.logits + (size_t)u * ws.slots * NP;
+    const int32_t *table = pv.table + (size_t)b * pv.max_pages;
+    const int j1 = min(used, j0 + kScoreChunk);
+    for (int j = j0 + tid; j < j1; j += kFinishThreads) {
+        float gain = 0.f;
+        const float *x = logits + (size_t)j * NP;
+        for (int r = 0; r < rows; ++r) gain += exp2f(x[r] - row_c[r]);      // -inf where the row does not see the slot
+        const int page = page_for_write(pv, table, j);
+        if (page < 0) continue;
+        float *dst = pv.scores + pool_row(pv, page, h, j);
+        *dst = fmaf(*dst, decay, gain);
+    }
+}
+
+size_t pad(size_t x) { return (x + 255) / 256 * 256; }
+int padded_slots(const PagedView &pv) { return ((pv.max_pages << pv.ps_shift) + kTile - 1) / kTile * kTile; }
+
+FewWs carve(const PagedView &pv, void *ws, size_t *bytes)
+{
+    const size_t U = (size_t)pv.B * pv.H, NP = rows_padded(pv.c * pv.G);
+    // the size must not depend on a device: room for any SM count up to 256
+    const size_t segs = (U + 512) * kWarps;
+    FewWs w;
+    size_t off = 0;
+    char *base = static_cast<char *>(ws);
+    w.slots = padded_slots(pv);
+    w.logits = reinterpret_cast<float *>(base + off); off += pad(U * w.slots * NP * 4);
+    w.ml = reinterpret_cast<float2 *>(base + off); off += pad(segs * NP * 8);
+    w.o = reinterpret_cast<float *>(base + off); off += pad(segs * NP * pv.d * 4);
+    w.prefix = reinterpret_cast<int32_t *>(base + off); off += pad(((size_t)pv.B + 1) * 4);
+    if (bytes) *bytes = off;
+    return w;
+}
+
+template <typename T, int D, int NC>
+cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
+{
+    using R = Ring<T, D>;
+    constexpr size_t smem = R::kBytes + BodyOf<T, D, NC>::kScratch;
+    cudaError_t e = allow_dynamic_smem<paged_few_kernel<T, D, NC>>(smem);
+    if (e != cudaSuccess) return e;
+    CUtensorMap mk, mv;
+    const int box = a.pv.ps < kTile ? a.pv.ps : kTile;
+    if (!make_pool_map(&mk, dtype, a.pv.k, a.pv, box) || !make_pool_map(&mv, dtype, a.pv.v, a.pv, box)) return cudaErrorInvalidValue;
+    const FewWs ws = carve(a.pv, a.ws, nullptr);
+    const int NP = rows_padded(a.pv.c * a.pv.G);
+    const int ctas = device_sm_count() * (2 * (smem + sizeof(FewShared) + 1024) <= 228 * 1024 ? 2 : 1);   // what is resident
+    if (ctas < 1 || ctas > 512) return cudaErrorInvalidValue;
+    paged_few_kernel<T, D, NC><<<ctas, kFewThreads, smem, s>>>(mk, mv, a, ws, NP);
+    count_launch();
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    const int cap = a.pv.max_pages << a.pv.ps_shift, chunks = a.scores ? (cap + kScoreChunk - 1) / kScoreChunk : 0;
+    const long long grid = (long long)a.pv.B * a.pv.H * (NP + chunks);
+    if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
+    paged_few_finish_kernel<T, D><<<(unsigned)grid, kFinishThreads, 0, s>>>(a, ws, NP, ctas, chunks);
+    count_launch();
+    return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t launch_d(int dtype, const AttendArgs &a, cudaStream_t s)
+{
+    const int rows = a.pv.c * a.pv.G;
+    if constexpr (sizeof(T) == 4) {
+        switch (rows_padded(rows)) {
+        case 1: return launch_nc<T, D, 1>(dtype, a, s);
+        case 2: return launch_nc<T, D, 2>(dtype, a, s);
+        case 4: return launch_nc<T, D, 4>(dtype, a, s);
+        case 8: return launch_nc<T, D, 8>(dtype, a, s);
+        default: return launch_nc<T, D, 16>(dtype, a, s);
+        }
+    } else {
+        return rows <= 8 ? launch_nc<T, D, 8>(dtype, a, s) : launch_nc<T, D, 16>(dtype, a, s);
+    }
+}
+
+}  // namespace
+
+size_t attend_few_ws_bytes(const PagedView &pv)
+{
+    size_t bytes = 0;
+    carve(pv, nullptr, &bytes);
+    return bytes;
+}
+
+cudaError_t launch_attend_few(int dtype, const AttendArgs &a, cudaStream_t s)
+{
+    const bool wide = a.pv.d == 128;
+    switch (dtype) {
+    case A2SF_F32: return wide ? launch_d<float, 128>(dtype, a, s) : launch_d<float, 64>(dtype, a, s);
+    case A2SF_BF16: return wide ? launch_d<__nv_bfloat16, 128>(dtype, a, s) : launch_d<__nv_bfloat16, 64>(dtype, a, s);
+    default: return wide ? launch_d<__half, 128>(dtype, a, s) : launch_d<__half, 64>(dtype, a, s);
+    }
+}
+
+}  // namespace a2sf
