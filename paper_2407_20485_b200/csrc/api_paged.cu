@@ -91,8 +91,14 @@ EncodeTiledFn encode_fn()
     return fn;
 }
 
-// Few rows go through the split kernel, more rows of any type through the tiled one.
-bool few_rows(const a2sf_paged *p, int c) { return (int64_t)c * p->group <= kFewRows; }
+// Which attention: few rows are bound by the cache's bytes whatever the type; more rows of 16-bit storage
+// by the matrix products (tensor cores), of 32-bit storage by fp32 multiply-adds.
+enum Path { kFew, kTc, kSimt };
+Path path_of(const a2sf_paged *p, int c)
+{
+    if ((int64_t)c * p->group <= kFewRows) return kFew;
+    return p->dtype == A2SF_F32 ? kSimt : kTc;
+}
 
 }  // namespace
 
@@ -108,6 +114,24 @@ bool make_pool_map(CUtensorMap *map, int dtype, const void *pool, const PagedVie
     const CUtensorMapDataType dt = dtype == A2SF_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                    : dtype == A2SF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     return fn(map, dt, 2, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Query rows in tiles of 128: box of 64 elements x group heads x 128/group tokens, so that row
+// r = token * group + head of a tile stands at row r of shared memory.
+bool make_query_map(CUtensorMap *map, int dtype, const void *q, const PagedView &pv, const Strides &st)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)pv.d, (cuuint64_t)pv.H * pv.G, (cuuint64_t)pv.c, (cuuint64_t)pv.B};
+    // an axis of extent 1 may come with any stride: one that the map accepts takes its place
+    const cuuint64_t row = (cuuint64_t)pv.d * 2;
+    const cuuint64_t strides[3] = {dims[1] > 1 ? (cuuint64_t)st.h * 2 : row, dims[2] > 1 ? (cuuint64_t)st.t * 2 : row,
+                                   dims[3] > 1 ? (cuuint64_t)st.b * 2 : row};
+    const cuuint32_t box[4] = {64, (cuuint32_t)pv.G, (cuuint32_t)(128 / pv.G), 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    const CUtensorMapDataType dt = dtype == A2SF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return fn(map, dt, 4, const_cast<void *>(q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -231,7 +255,8 @@ size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c)
 {
     if (check_paged(cache, c) != A2SF_OK) return 0;
     const PagedView pv = make_view(cache, c, nullptr);
-    return align_up(few_rows(cache, c) ? attend_few_ws_bytes(pv) : attend_simt_ws_bytes(pv));
+    const Path path = path_of(cache, c);
+    return align_up(path == kFew ? attend_few_ws_bytes(pv) : path == kTc ? attend_tc_ws_bytes(pv) : attend_simt_ws_bytes(pv));
 }
 
 int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha, const void *q,
@@ -260,7 +285,9 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
     a.scores = !(flags & A2SF_ATTEND_NO_SCORES);
     a.ws = workspace;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    const cudaError_t e = few_rows(cache, c) ? launch_attend_few(cache->dtype, a, s) : launch_attend_simt(cache->dtype, a, s);
+    const Path path = path_of(cache, c);
+    const cudaError_t e = path == kFew ? launch_attend_few(cache->dtype, a, s)
+                          : path == kTc ? launch_attend_tc(cache->dtype, a, s) : launch_attend_simt(cache->dtype, a, s);
     return e == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
 }
 

@@ -74,6 +74,63 @@ __device__ __forceinline__ int first_weighted_token(int len, float nl2a)
     return span >= (float)len ? 0 : max(0, len - 1 - (int)span);
 }
 
+// ---- the tiles of all (sequence, K/V head) units as one list ---------------------------------------
+struct Where {            // position in the list: unit (b, h), tile t of its `tiles`
+    int b, h, t, tiles;
+};
+
+// Tiles of one head of sequence b; none where it takes no part in the call.
+template <int Tile> __device__ __forceinline__ int seq_tiles(const PagedView &pv, int b)
+{
+    const SeqState st = seq_state(pv, b);
+    return st.len > 0 ? (st.past + st.len + Tile - 1) / Tile : 0;
+}
+
+// prefix[0 .. B] of the sequences' tiles, by one warp
+template <int Tile> __device__ __forceinline__ void tile_prefix(int32_t *prefix, const PagedView &pv)
+{
+    const int lane = threadIdx.x & 31;
+    int run = 0;
+    for (int b0 = 0; b0 < pv.B; b0 += 32) {
+        const int b = b0 + lane;
+        int incl = b < pv.B ? seq_tiles<Tile>(pv, b) : 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        if (b < pv.B) prefix[b + 1] = run + incl;
+        run += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) prefix[0] = 0;
+}
+
+__device__ __forceinline__ Where locate(const int32_t *prefix, int B, int H, long long w)
+{
+    int lo = 0, hi = B - 1;                        // last b with H * prefix[b] <= w
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((long long)H * prefix[mid] <= w) lo = mid;
+        else hi = mid - 1;
+    }
+    Where x;
+    x.b = lo;
+    x.tiles = prefix[lo + 1] - prefix[lo];
+    const long long rest = w - (long long)H * prefix[lo];
+    x.h = (int)(rest / x.tiles);
+    x.t = (int)(rest - (long long)x.h * x.tiles);
+    return x;
+}
+
+__device__ __forceinline__ void next_unit(Where &x, const int32_t *prefix, int B, int H)
+{
+    x.t = 0;
+    if (++x.h < H) return;
+    x.h = 0;
+    do ++x.b; while (x.b < B && prefix[x.b + 1] == prefix[x.b]);
+    x.tiles = x.b < B ? prefix[x.b + 1] - prefix[x.b] : 0;
+}
+
 // ---- launchers -------------------------------------------------------------------------------
 int *paged_status_word();        // device address on the current device (nullptr on failure)
 int read_and_clear_paged_status(cudaStream_t s);
@@ -108,6 +165,11 @@ bool make_pool_map(CUtensorMap *map, int dtype, const void *pool, const PagedVie
 constexpr int kFewRows = 16;
 size_t attend_few_ws_bytes(const PagedView &pv);
 cudaError_t launch_attend_few(int dtype, const AttendArgs &a, cudaStream_t s);
+
+// many rows, 16-bit storage: tcgen05
+bool make_query_map(CUtensorMap *map, int dtype, const void *q, const PagedView &pv, const Strides &st);
+size_t attend_tc_ws_bytes(const PagedView &pv);
+cudaError_t launch_attend_tc(int dtype, const AttendArgs &a, cudaStream_t s);
 
 size_t attend_simt_ws_bytes(const PagedView &pv);
 cudaError_t launch_attend_simt(int dtype, const AttendArgs &a, cudaStream_t s);

@@ -52,43 +52,6 @@ struct FewWs {
     int slots;            // padded slots of a unit
 };
 
-struct Where {            // position in the list of tiles
-    int b, h, t, tiles;
-};
-
-// Tiles of one head of sequence b.
-__device__ __forceinline__ int seq_tiles(const PagedView &pv, int b)
-{
-    const SeqState st = seq_state(pv, b);
-    return st.len > 0 ? (st.past + st.len + kTile - 1) / kTile : 0;
-}
-
-__device__ __forceinline__ Where locate(const int32_t *prefix, int B, int H, long long w)
-{
-    int lo = 0, hi = B - 1;                        // last b with H * prefix[b] <= w
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if ((long long)H * prefix[mid] <= w) lo = mid;
-        else hi = mid - 1;
-    }
-    Where x;
-    x.b = lo;
-    x.tiles = prefix[lo + 1] - prefix[lo];
-    const long long rest = w - (long long)H * prefix[lo];
-    x.h = (int)(rest / x.tiles);
-    x.t = (int)(rest - (long long)x.h * x.tiles);
-    return x;
-}
-
-__device__ __forceinline__ void next_unit(Where &x, const int32_t *prefix, int B, int H)
-{
-    x.t = 0;
-    if (++x.h < H) return;
-    x.h = 0;
-    do ++x.b; while (x.b < B && prefix[x.b + 1] == prefix[x.b]);
-    x.tiles = x.b < B ? prefix[x.b + 1] - prefix[x.b] : 0;
-}
-
 template <typename T> struct Mma16;
 template <> struct Mma16<__half> {
     __device__ static void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -423,19 +386,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             prefetch_tmap(&map_k);
             prefetch_tmap(&map_v);
         }
-        int run = 0;
-        for (int b0 = 0; b0 < pv.B; b0 += 32) {
-            const int b = b0 + lane, t = b < pv.B ? seq_tiles(pv, b) : 0;
-            int incl = t;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int x = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += x;
-            }
-            if (b < pv.B) sh.prefix[b + 1] = run + incl;
-            run += __shfl_sync(0xffffffffu, incl, 31);
-        }
-        if (lane == 0) sh.prefix[0] = 0;
+        tile_prefix<kTile>(sh.prefix, pv);
     }
     __syncthreads();
     if (blockIdx.x == 0)

@@ -1,0 +1,964 @@
+// Attention of a chunk over a paged cache for 16-bit storage (TMA + tcgen05 + TMEM).
+//
+// The G query heads of a K/V head and the chunk's tokens are folded into rows: a row tile is
+// 128/G tokens x G heads (128 rows, or a few less when G does not divide 128), so K and V are read once
+// for the whole group and the mask is a bound on the slot that grows with the row.
+//
+//   plan    one CTA, from the lengths on the device: an item is a pair of row tiles of one (sequence, K/V
+//           head) and the key tiles it sees.  When there are too few items for the device's SMs (a short
+//           chunk behind a long cache) items are cut along the keys.  Sorted, longest first.
+//   attn    persistent CTAs take items in that order.  Two row tiles ("streams") share every K/V tile and
+//           take turns: while one's rows are in the softmax warps, the other's products run.
+//             S = Q K^T -> TMEM;  P, rounded to the storage type, replaces its logits in TMEM and is the A
+//             operand of O += P V;  V is read MN-major from its TMA tile.
+//           A row's reference (what is subtracted before the exponential) stays where it is unless a
+//           row sum shows that a probability may have left fp16's range: then the tile is done again
+//           against the row's maximum and the accumulator rescaled.
+//   merge   joins the items that were cut.
+//   score   S_j <- alpha^len S_j + sum_r exp2(s_rj - c_r), c_r = lse_r + age * (-log2 alpha): K tile x Q
+//           tiles transposed, so a slot is a TMEM lane and its sum is made by two threads in row order.
+//           Rows whose weight is zero in fp32 are not visited (alpha = 0.9: all but the last 990 tokens).
+//
+// Bound by the special-function unit: one exponential per logit in attn and one in score, 16 a clock and
+// SM, against 128 x 128 x d x 4 operations of a tile at 8192 a clock: 1024 clocks each for d = 128.
+// P as one term of the storage type: half a step per probability, as much as the output's own rounding.
+#include <type_traits>
+
+#include "paged.cuh"
+#include "tc_sm100.cuh"
+
+namespace a2sf {
+
+A2SF_DEBUG_TRANSLATION_UNIT(paged_attn_tc)
+
+namespace {
+
+using namespace tc;
+
+constexpr int kBlk = 128;                    // rows per tile = TMEM lanes; key slots per tile
+constexpr int kSms = 148;
+constexpr int kSplitBelow = 4 * kSms;        // items of a call from which none is cut
+constexpr int kPieces = 4 * kSms;            // pieces that cutting aims at
+constexpr int kMinPiece = 4;                 // key tiles of a piece at least
+constexpr int kMaxParts = kSplitBelow + kPieces;   // sum of ceil(T / piece) <= total / piece + items
+constexpr int kPlanThreads = 1024;
+constexpr int kLenBuckets = 512;
+
+struct Item {                                // of one head; all heads have the same
+    int b, pair, t0, t1;                     // key tiles t0 .. t1-1
+    int part;                                // -1: whole; else index of its partial result
+    int pad[3];
+};
+struct Merge {
+    int b, pair, n, part;                    // partial results part .. part + n - 1
+};
+struct PlanHead { int items, merges; };
+
+struct TcWs {
+    float *lse2;          // [B*H][c*G] log-sum-exp, log2 units
+    PlanHead *head;
+    Item *items;          // [max_items]
+    Merge *merges;        // [B * pairs]
+    float2 *part_ml;      // [kMaxParts][part_rows]
+    float *part_o;        // [kMaxParts][part_rows][d]
+    int max_items, part_rows, pairs, pair_tokens;
+};
+
+__device__ __forceinline__ int pair_key_tiles(const SeqState &st, int pair, int pair_tokens)
+{
+    return (st.past + min((pair + 1) * pair_tokens, st.len) + kBlk - 1) / kBlk;
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ TcWs ws)
+{
+    __shared__ int hist[kLenBuckets], n_parts, n_merges, n_items;
+    __shared__ unsigned long long tiles;
+    const int tid = threadIdx.x;
+    for (int x = tid; x < kLenBuckets; x += kPlanThreads) hist[x] = 0;
+    if (tid == 0) { n_parts = 0; n_merges = 0; n_items = 0; tiles = 0; }
+    __syncthreads();
+    const int all = pv.B * ws.pairs;
+    auto item_tiles = [&](int x) -> int {
+        const int b = x / ws.pairs, p = x - b * ws.pairs;
+        const SeqState st = seq_state(pv, b);
+        return p * ws.pair_tokens < st.len ? pair_key_tiles(st, p, ws.pair_tokens) : 0;
+    };
+    unsigned long long sum = 0;
+    int mine = 0;
+    for (int x = tid; x < all; x += kPlanThreads) {
+        const int t = item_tiles(x);
+        sum += t;
+        mine += t > 0;
+    }
+    if (mine) { atomicAdd(&tiles, sum); atomicAdd(&n_items, mine); }
+    __syncthreads();
+    const long long work = (long long)tiles * pv.H, units = (long long)n_items * pv.H;
+    long long piece = 0x7fffffff;
+    if (units < kSplitBelow) piece = max((long long)kMinPiece, (work + kPieces - 1) / kPieces);
+    auto pieces = [&](int t) { return (int)((t + piece - 1) / piece); };
+    for (int x = tid; x < all; x += kPlanThreads) {
+        const int t = item_tiles(x);
+        if (!t) continue;
+        const int n = pieces(t), len = (t + n - 1) / n;
+        atomicAdd(&hist[kLenBuckets - 1 - min(len, kLenBuckets - 1)], n);
+    }
+    __syncthreads();
+    if (tid < 32) {                                          // exclusive scan: longest first
+        int run = 0;
+        for (int x0 = 0; x0 < kLenBuckets; x0 += 32) {
+            const int v = hist[x0 + tid];
+            int incl = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, incl, o);
+                if (tid >= o) incl += y;
+            }
+            hist[x0 + tid] = run + incl - v;
+            run += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (tid == 0) ws.head->items = min(run, ws.max_items);
+    }
+    __syncthreads();
+    // the order of equal lengths may differ from run to run; no result depends on it
+    for (int x = tid; x < all; x += kPlanThreads) {
+        const int t = item_tiles(x);
+        if (!t) continue;
+        const int n = pieces(t), len = (t + n - 1) / n, b = x / ws.pairs, p = x - b * ws.pairs;
+        int at = atomicAdd(&hist[kLenBuckets - 1 - min(len, kLenBuckets - 1)], n);
+        int part = -1;
+        if (n > 1) {
+            part = atomicAdd(&n_parts, n);
+            ws.merges[atomicAdd(&n_merges, 1)] = Merge{b, p, n, part};
+        }
+        for (int s = 0; s < n; ++s, ++at)
+            if (at < ws.max_items)
+                ws.items[at] = Item{b, p, (int)((long long)t * s / n), (int)((long long)t * (s + 1) / n), n > 1 ? part + s : -1, {0, 0, 0}};
+    }
+    __syncthreads();
+    if (tid == 0) ws.head->merges = n_merges;
+}
+
+__device__ __forceinline__ float ex2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Two fp32 operations per instruction (packed arithmetic on register pairs).
+__device__ __forceinline__ uint64_t pack_f32x2(uint32_t lo, uint32_t hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float &lo, float &hi)
+{
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b)
+{
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+template <int D> struct Tile {
+    static constexpr int kHalves = D / 64;                  // 64-element swizzled columns
+    static constexpr int kHalfBytes = kBlk * 128;
+    static constexpr int kBytes = kHalves * kHalfBytes;
+};
+
+__device__ __forceinline__ uint64_t kmajor_desc(uint32_t smem_addr) { return make_sdesc_sw128(smem_addr, 16, 1024); }
+
+// S = A B^T over D elements: step k starts (k / 4) halves + (k % 4) * 32 bytes into the tiles
+template <int D>
+__device__ __forceinline__ void issue_qk(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc)
+{
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        const uint64_t off = (uint64_t)(((k >> 2) * Tile<D>::kHalfBytes + (k & 3) * 32) >> 4);
+        umma_ss(d_tmem, a_desc + off, b_desc + off, idesc, k > 0);
+    }
+}
+
+// Boxes of key tile t that hold tokens, and one lane's share of the copy (lane i: box i).
+struct PageTile {
+    int box, boxes;
+};
+__device__ __forceinline__ PageTile page_tile(const PagedView &pv, int t, int used)
+{
+    PageTile p;
+    p.box = min(pv.ps, kBlk);
+    p.boxes = min(kBlk / p.box, (used - t * kBlk + p.box - 1) / p.box);
+    return p;
+}
+template <int D>
+__device__ __forceinline__ void copy_page_tile(uint8_t *dst, const CUtensorMap *map, uint64_t *bar, const PageTile &p, int row)
+{
+    const int lane = threadIdx.x & 31;
+    if (lane < p.boxes)
+#pragma unroll
+        for (int x = 0; x < Tile<D>::kHalves; ++x) tma_load_2d(dst + x * Tile<D>::kHalfBytes + lane * p.box * 128, map, bar, x * 64, row);
+}
+template <int D>
+__device__ __forceinline__ void copy_query_tile(uint8_t *dst, const CUtensorMap *map, uint64_t *bar, int head, int token, int b)
+{
+#pragma unroll
+    for (int x = 0; x < Tile<D>::kHalves; ++x) tma_load_4d(dst + x * Tile<D>::kHalfBytes, map, bar, x * 64, head, token, b);
+}
+
+// ============================================================================================
+// attn
+// ============================================================================================
+constexpr int kAttnThreads = 320;            // producer warp, MMA warp, 8 softmax warps
+constexpr int kKStages = 3, kVStages = 2;
+constexpr float kRescaleThreshold = 8.0f;    // log2 units
+constexpr float kOptimisticLimit = 32768.f;  // a row sum below this keeps every probability < 2^15
+
+struct AttnShared {
+    uint64_t q_full, q_empty, k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
+    uint64_t s_full[2], p_full[2], o_done[2], o_free[2];    // per stream
+    uint32_t tmem_base;
+    int abort_flag;
+    float xch[2][2][kBlk];                                  // [stream][column half][row]
+};
+
+template <int D> constexpr size_t attn_smem() { return (size_t)Tile<D>::kBytes * (2 + kKStages + kVStages) + sizeof(AttnShared); }
+static_assert(attn_smem<128>() <= 227 * 1024, "attention shared memory");
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendArgs a, const __grid_constant__ TcWs ws)
+{
+    constexpr int kTileBytes = Tile<D>::kBytes;
+    constexpr int kFmt = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+    constexpr int OW = D / 2;                               // output columns per thread
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t *Qs = smem, *Ks = Qs + 2 * kTileBytes, *Vs = Ks + kKStages * kTileBytes;
+    AttnShared *sh = reinterpret_cast<AttnShared *>(Vs + kVStages * kTileBytes);
+    const PagedView &pv = a.pv;
+    const int G = pv.G, tile_tokens = kBlk / G, tile_rows = tile_tokens * G;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int *abort_flag = &sh->abort_flag;
+
+    if (threadIdx.x == 0) {
+        mbar_init(&sh->q_full, 1);
+        mbar_init(&sh->q_empty, 1);
+        for (int s = 0; s < kKStages; ++s) { mbar_init(&sh->k_full[s], 1); mbar_init(&sh->k_empty[s], 1); }
+        for (int s = 0; s < kVStages; ++s) { mbar_init(&sh->v_full[s], 1); mbar_init(&sh->v_empty[s], 1); }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&sh->s_full[x], 1);
+            mbar_init(&sh->p_full[x], 2 * kBlk);
+            mbar_init(&sh->o_done[x], 1);
+            mbar_init(&sh->o_free[x], 2 * kBlk);
+        }
+        sh->abort_flag = smem_u32(smem) & 1023u ? 1 : 0;    // the swizzled tiles need this alignment
+        fence_mbar_init();
+        prefetch_tmap(&map_q); prefetch_tmap(&map_k); prefetch_tmap(&map_v);
+    }
+    if (warp == 1) {
+        tmem_alloc(&sh->tmem_base, 512);
+        tmem_relinquish();
+    }
+    // rows that no query copy fills (G does not divide 128) stay zero, so that their logits stay finite
+    for (int x = threadIdx.x; x < 2 * Tile<D>::kHalves * (kBlk - tile_rows) * 8; x += kAttnThreads) {
+        const int piece = x & 7, row = tile_rows + (x >> 3) % (kBlk - tile_rows), half = (x >> 3) / (kBlk - tile_rows);
+        *reinterpret_cast<uint4 *>(Qs + half * Tile<D>::kHalfBytes + row * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
+    }
+    fence_async_smem();
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = sh->tmem_base;
+
+    // A failed wait poisons the CTA: later waits return at once, loops keep their shape.
+    auto wait = [&](uint64_t *bar, uint32_t parity) -> bool {
+        if (*abort_flag) return false;
+        return mbar_wait(bar, parity, abort_flag);
+    };
+    const int n_units = ws.head->items * pv.H;
+    // what an item means to every role
+    struct Job {
+        int b, h, i0, tokens, t0, nt, ntA, ntB, past, used, part;
+    };
+    auto job = [&](int unit) -> Job {
+        const Item it = ws.items[unit / pv.H];
+        Job j;
+        j.b = it.b; j.h = unit % pv.H;
+        const SeqState st = seq_state(pv, it.b);
+        j.past = st.past; j.used = st.past + st.len;
+        j.i0 = it.pair * ws.pair_tokens;
+        j.tokens = min(ws.pair_tokens, st.len - j.i0);
+        j.t0 = it.t0;
+        // stream A sees no slot beyond its own last token's
+        const int endA = (st.past + min(j.i0 + tile_tokens, st.len) + kBlk - 1) / kBlk;
+        j.ntB = j.tokens > tile_tokens ? it.t1 - it.t0 : 0;
+        j.ntA = max(0, min(it.t1, endA) - it.t0);
+        j.nt = max(j.ntA, j.ntB);
+        j.part = it.part < 0 ? -1 : it.part * pv.H + j.h;
+        return j;
+    };
+
+    if (warp == 0) {
+        // ---- TMA producer: lane i copies page box i ------------------------------------------
+        int kt = 0, n = 0;                                  // tiles and items so far
+        for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x, ++n) {
+            const Job j = job(unit);
+            const int32_t *table = pv.table + (size_t)j.b * pv.max_pages;
+            int ok = 1;
+            if (lane == 0) {
+                ok = n == 0 || wait(&sh->q_empty, (n - 1) & 1) ? 1 : 0;
+                if (ok) {
+                    const uint32_t bytes = (uint32_t)(tile_rows * 128 * Tile<D>::kHalves);
+                    mbar_arrive_expect_tx(&sh->q_full, j.ntB ? 2 * bytes : bytes);
+                    copy_query_tile<D>(Qs, &map_q, &sh->q_full, j.h * G, j.i0, j.b);
+                    if (j.ntB) copy_query_tile<D>(Qs + kTileBytes, &map_q, &sh->q_full, j.h * G, j.i0 + tile_tokens, j.b);
+                }
+            }
+            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+            for (int t = 0; t < j.nt; ++t, ++kt) {
+                const int tile = j.t0 + t, ks = kt % kKStages, vs = kt % kVStages;
+                const PageTile p = page_tile(pv, tile, j.used);
+                const int slot = tile * kBlk + lane * p.box;
+                int row = 0;
+                if (lane < p.boxes) row = (int)pool_row(pv, page_for_read(pv, table, slot), j.h, slot);
+                const uint32_t bytes = (uint32_t)(p.boxes * p.box * 128 * Tile<D>::kHalves);
+                ok = 1;
+                if (lane == 0) {
+                    if (kt >= kKStages) ok = wait(&sh->k_empty[ks], ((kt / kKStages) & 1) ^ 1) ? 1 : 0;
+                    if (ok) mbar_arrive_expect_tx(&sh->k_full[ks], bytes);
+                }
+                if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+                copy_page_tile<D>(Ks + ks * kTileBytes, &map_k, &sh->k_full[ks], p, row);
+                if (lane == 0) {
+                    if (kt >= kVStages) ok = wait(&sh->v_empty[vs], ((kt / kVStages) & 1) ^ 1) ? 1 : 0;
+                    if (ok) mbar_arrive_expect_tx(&sh->v_full[vs], bytes);
+                }
+                if (!__shfl_sync(0xffffffffu, ok, 0)) { ++kt; break; }   // K of this tile is on its way
+                copy_page_tile<D>(Vs + vs * kTileBytes, &map_v, &sh->v_full[vs], p, row);
+            }
+        }
+        if (lane == 0 && *abort_flag) {
+            // copies still in flight get a bounded chance to land before the CTA exits
+            int dummy = 0;
+            for (int k = max(0, kt - kKStages); k < kt; ++k) mbar_wait(&sh->k_full[k % kKStages], (k / kKStages) & 1, &dummy);
+            for (int k = max(0, kt - kVStages); k < kt; ++k) mbar_wait(&sh->v_full[k % kVStages], (k / kVStages) & 1, &dummy);
+            if (n > 0) mbar_wait(&sh->q_full, (n - 1) & 1, &dummy);
+        }
+    } else if (warp == 1) {
+        // ---- MMA issuer (lane 0; the warp stays together to clear values behind a sequence) -----------
+        const uint32_t idesc_qk = make_idesc(kFmt, kBlk, kBlk, 0, 0);
+        const uint32_t idesc_pv = make_idesc(kFmt, kBlk, D, 0, 1);        // V is MN-major
+        // descriptors of the first buffers; the others lie whole tiles behind (16-byte units)
+        const uint64_t step = kTileBytes >> 4;
+        const uint64_t q_desc = kmajor_desc(smem_u32(Qs)), k_desc = kmajor_desc(smem_u32(Ks));
+        // V as an MN-major operand: 64-wide halves 16 KB apart, 8-key groups 1024 bytes apart
+        const uint64_t v_desc = make_sdesc_sw128(smem_u32(Vs), Tile<D>::kHalfBytes, 1024);
+        auto issue_s = [&](int X, int kt) {
+            issue_qk<D>(tmem_base + X * 2 * kBlk, q_desc + X * step, k_desc + kt % kKStages * step, idesc_qk);
+            umma_commit(&sh->s_full[X]);
+        };
+        auto issue_pv = [&](int X, int kt, bool first) {
+            const uint64_t vd = v_desc + kt % kVStages * step;
+            const uint32_t sp = tmem_base + X * 2 * kBlk, o = sp + kBlk;
+            // 16 keys per step: 8 columns of packed P, two 8-key groups of V.  Keys 64h .. 64h+63 have
+            // their P at columns 64h .. 64h+31: a softmax thread writes over logits it has read itself.
+#pragma unroll
+            for (int k = 0; k < kBlk / 16; ++k)
+                umma_ts(o, sp + 64 * (k >> 2) + 8 * (k & 3), vd + (uint64_t)(k * 2048 >> 4), idesc_pv, !first || k > 0);
+            umma_commit(&sh->o_done[X]);
+        };
+        int kt = 0, n = 0, cnt[2] = {0, 0}, used_before[2] = {0, 0};      // tiles per stream; items per stream
+        for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x, ++n) {
+            if (__any_sync(0xffffffffu, *abort_flag)) break;
+            const Job j = job(unit);
+            const int ntX[2] = {j.ntA, j.ntB};
+            wait(&sh->q_full, n & 1);
+            wait(&sh->k_full[kt % kKStages], (kt / kKStages) & 1);
+            tc_fence_after_sync();
+            if (lane == 0) {
+                if (j.ntA) issue_s(0, kt);
+                if (j.ntB) issue_s(1, kt);
+                umma_commit(&sh->k_empty[kt % kKStages]);
+                if (j.nt == 1) umma_commit(&sh->q_empty);
+            }
+            for (int t = 0; t < j.nt; ++t, ++kt) {
+                const int vs = kt % kVStages;
+                wait(&sh->v_full[vs], (kt / kVStages) & 1);
+                const bool more = t + 1 < j.nt;
+                if (more) wait(&sh->k_full[(kt + 1) % kKStages], ((kt + 1) / kKStages) & 1);
+                // slots behind the sequence may hold anything, NaN included: 0 * NaN must not reach O
+                const int valid = j.used - (j.t0 + t) * kBlk;
+                if (valid < kBlk) {
+                    uint8_t *V = Vs + vs * kTileBytes;
+                    for (int x = lane; x < Tile<D>::kHalves * (kBlk - valid) * 8; x += 32) {
+                        const int piece = x & 7, row = valid + (x >> 3) % (kBlk - valid), half = (x >> 3) / (kBlk - valid);
+                        *reinterpret_cast<uint4 *>(V + half * Tile<D>::kHalfBytes + row * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int X = 0; X < 2; ++X) {
+                    if (t >= ntX[X]) continue;
+                    if (t == 0 && used_before[X]) wait(&sh->o_free[X], (used_before[X] - 1) & 1);
+                    wait(&sh->p_full[X], cnt[X] & 1);
+                    ++cnt[X];
+                    tc_fence_after_sync();
+                    if (lane == 0) {
+                        issue_pv(X, kt, t == 0);
+                        if (t + 1 < ntX[X]) issue_s(X, kt + 1);
+                    }
+                }
+                if (lane == 0) {
+                    umma_commit(&sh->v_empty[vs]);
+                    if (more) umma_commit(&sh->k_empty[(kt + 1) % kKStages]);
+                    if (t + 2 == j.nt) umma_commit(&sh->q_empty);          // the last logits have been asked for
+                }
+                __syncwarp();
+            }
+            for (int X = 0; X < 2; ++X) used_before[X] += ntX[X] > 0;
+        }
+    } else {
+        // ---- softmax + epilogue: two threads per row, the streams taken in turn ----------------------
+        const int quarter = warp & 3;                      // TMEM lanes this warp may touch
+        const int half = (warp - 2) >> 2;                  // logits 64*half .. 64*half+63
+        const int r = quarter * 32 + lane;                 // row in the tile = TMEM lane
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        int cnt[2] = {0, 0};
+        float m_used[2], l[2];
+        // no early exit here: the two warps of a quarter meet at named barriers, and after a failed wait
+        // all that follows runs through without waiting
+        for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x) {
+            const Job j = job(unit);
+            auto do_tile = [&](auto Xc, int t) {
+                constexpr int X = decltype(Xc)::value;
+                const uint32_t sp = tmem_base + X * 2 * kBlk + lane_base + half * 64;
+                const uint32_t to = tmem_base + X * 2 * kBlk + kBlk + lane_base + half * OW;
+                const int first_token = j.i0 + X * tile_tokens;
+                wait(&sh->s_full[X], cnt[X] & 1);
+                tc_fence_after_sync();
+                uint32_t v[2][32];
+                tmem_ld32(sp, v[0]);
+                tmem_ld32(sp + 32, v[1]);
+                tmem_wait_ld();
+                const int tile0 = (j.t0 + t) * kBlk;
+                if (tile0 + kBlk > j.past + first_token + 1) {
+                    // some row of the tile does not see all of it: a masked logit becomes -inf
+                    const int vis = min(j.past + first_token + r / G + 1, j.used) - tile0 - half * 64;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int x = 0; x < 32; ++x)
+                            if (c * 32 + x >= vis) v[c][x] = 0xff800000u;
+                }
+                auto write_p = [&](float neg_m) -> float {
+                    const uint64_t sl2x2 = pack_f32x2(__float_as_uint(pv.sl2), __float_as_uint(pv.sl2));
+                    const uint64_t nmx2 = pack_f32x2(__float_as_uint(neg_m), __float_as_uint(neg_m));
+                    uint64_t rs2[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            float x0, x1;
+                            unpack_f32x2(fma_f32x2(pack_f32x2(v[c][2 * e], v[c][2 * e + 1]), sl2x2, nmx2), x0, x1);
+                            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+                            rs2[e & 3] = add_f32x2(rs2[e & 3], pack_f32x2(__float_as_uint(p0), __float_as_uint(p1)));
+                            p[e] = pack2<T>(p0, p1);
+                        }
+                        tmem_st16(sp + c * 16, p);
+                    }
+                    float rs[8];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) unpack_f32x2(rs2[x], rs[2 * x], rs[2 * x + 1]);
+                    return ((rs[0] + rs[1]) + (rs[2] + rs[3])) + ((rs[4] + rs[5]) + (rs[6] + rs[7]));
+                };
+                float factor = 1.f, rowsum = 0.f;
+                bool exact = (t == 0);
+                if (!exact) {
+                    rowsum = write_p(-m_used[X]);
+                    const bool bad = !(rowsum <= kOptimisticLimit);          // also NaN
+                    sh->xch[X][half][r] = bad ? 1.f : 0.f;
+                    named_barrier(1 + quarter, 64);                // this quarter's two warps
+                    const bool pair_bad = bad || sh->xch[X][half ^ 1][r] != 0.f;
+                    exact = __any_sync(0xffffffffu, pair_bad);
+                    if (exact) named_barrier(1 + quarter, 64);     // flags read before the buffer is reused
+                }
+                if (exact) {
+                    float own = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) own = fmaxf(own, __uint_as_float(v[c][x]));
+                    sh->xch[X][half][r] = own;
+                    named_barrier(1 + quarter, 64);
+                    const float smax = fmaxf(own, sh->xch[X][half ^ 1][r]);
+                    if (t == 0) {
+                        // a piece of the keys may hold none that this row sees (then none of the following
+                        // tiles does either): any finite reference gives the zeros that are wanted
+                        m_used[X] = smax == -INFINITY ? 0.f : smax * pv.sl2;
+                        l[X] = 0.f;
+                    } else {
+                        const float xmax = fmaf(smax, pv.sl2, -m_used[X]);
+                        const bool grow = xmax > kRescaleThreshold;
+                        if (grow) {
+                            m_used[X] += xmax;
+                            factor = ex2_approx(-xmax);
+                        }
+                        if (__any_sync(0xffffffffu, grow)) {
+                            wait(&sh->o_done[X], (cnt[X] - 1) & 1);          // O holds the tiles before
+                            tc_fence_after_sync();
+#pragma unroll 1
+                            for (int c = 0; c < OW / 32; ++c) {
+                                uint32_t o[32];
+                                tmem_ld32(to + c * 32, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * factor);
+                                tmem_st32(to + c * 32, o);
+                            }
+                            tmem_wait_st();
+                        }
+                    }
+                    rowsum = write_p(-m_used[X]);
+                }
+                tmem_wait_st();
+                l[X] = fmaf(l[X], factor, rowsum);
+                tc_fence_before_sync();
+                mbar_arrive(&sh->p_full[X]);
+                ++cnt[X];
+            };
+            for (int t = 0; t < j.nt; ++t) {
+                if (t < j.ntA) do_tile(std::integral_constant<int, 0>{}, t);
+                if (t < j.ntB) do_tile(std::integral_constant<int, 1>{}, t);
+            }
+            // ---- epilogue: each thread normalises (or hands on) and stores its half of the columns
+            auto finish = [&](auto Xc, int ntX) {
+                constexpr int X = decltype(Xc)::value;
+                const int tok = X * tile_tokens + r / G, g = r - r / G * G;
+                const bool live = r < tile_rows && tok < j.tokens;
+                if (ntX == 0) {
+                    // a cut item whose piece lies behind everything stream A sees: an empty partial result
+                    if (j.part >= 0 && X == 0 && half == 0) ws.part_ml[(size_t)j.part * ws.part_rows + r] = make_float2(-INFINITY, 0.f);
+                    return;
+                }
+                const uint32_t to = tmem_base + X * 2 * kBlk + kBlk + lane_base + half * OW;
+                named_barrier(1 + quarter, 64);                // the partner has read the last exchange
+                sh->xch[X][half][r] = l[X];
+                named_barrier(1 + quarter, 64);
+                const float lsum = l[X] + sh->xch[X][half ^ 1][r];
+                named_barrier(1 + quarter, 64);                // read before the next item writes
+                const bool done = wait(&sh->o_done[X], (cnt[X] - 1) & 1);
+                tc_fence_after_sync();
+                const float inv = j.part < 0 ? 1.f / lsum : 1.f;
+                const int i = j.i0 + tok;
+                T *orow = static_cast<T *>(a.out) + (int64_t)j.b * a.so.b + (int64_t)(j.h * G + g) * a.so.h + (int64_t)i * a.so.t + half * OW;
+                const size_t prow = (size_t)(j.part < 0 ? 0 : j.part) * ws.part_rows + X * kBlk + r;
+                float *po = ws.part_o + prow * D + half * OW;
+#pragma unroll 1
+                for (int c = 0; c < OW / 32; ++c) {
+                    uint32_t o[32];
+                    tmem_ld32(to + c * 32, o);
+                    tmem_wait_ld();
+                    if (!live || !done) continue;
+                    if (j.part < 0) {
+#pragma unroll
+                        for (int q4 = 0; q4 < 4; ++q4) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                w[e] = pack2<T>(__uint_as_float(o[q4 * 8 + 2 * e]) * inv, __uint_as_float(o[q4 * 8 + 2 * e + 1]) * inv);
+                            *reinterpret_cast<uint4 *>(orow + c * 32 + q4 * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int q8 = 0; q8 < 8; ++q8)
+                            *reinterpret_cast<uint4 *>(po + c * 32 + q8 * 4) = make_uint4(o[q8 * 4], o[q8 * 4 + 1], o[q8 * 4 + 2], o[q8 * 4 + 3]);
+                    }
+                }
+                tc_fence_before_sync();
+                mbar_arrive(&sh->o_free[X]);
+                if (half == 0 && live && done) {
+                    if (j.part < 0) {
+                        const float z = m_used[X] + log2f(lsum);
+                        ws.lse2[((size_t)j.b * pv.H + j.h) * pv.c * G + (size_t)i * G + g] = z;
+                        if (a.lse) a.lse[(((size_t)j.b * pv.H + j.h) * G + g) * pv.c + i] = z * 0.6931471805599453f;
+                    } else {
+                        ws.part_ml[prow] = make_float2(lsum > 0.f ? m_used[X] : -INFINITY, lsum);
+                    }
+                }
+            };
+            finish(std::integral_constant<int, 0>{}, j.ntA);
+            finish(std::integral_constant<int, 1>{}, j.ntB);
+        }
+    }
+
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, 512);
+    }
+    if (threadIdx.x == 0 && sh->abort_flag) *pv.status = A2SF_ERR_TIMEOUT;
+}
+
+// ============================================================================================
+// merge: a warp per row of a cut item
+// ============================================================================================
+constexpr int kMergeThreads = 256;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kMergeThreads)
+paged_merge_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ TcWs ws)
+{
+    const PagedView &pv = a.pv;
+    const int G = pv.G, tile_tokens = kBlk / G, lane = threadIdx.x & 31;
+    const long long rows = (long long)ws.head->merges * pv.H * ws.part_rows;
+    const int wpg = gridDim.x * (kMergeThreads / 32);
+    for (long long x = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5); x < rows; x += wpg) {
+        const int pr = (int)(x % ws.part_rows);
+        const long long y = x / ws.part_rows;
+        const int h = (int)(y % pv.H);
+        const Merge mg = ws.merges[y / pv.H];
+        const SeqState st = seq_state(pv, mg.b);
+        const int X = pr / kBlk, r = pr - X * kBlk;
+        const int tok = X * tile_tokens + r / G, g = r - r / G * G, i = mg.pair * ws.pair_tokens + tok;
+        if (r >= tile_tokens * G || tok >= ws.pair_tokens || i >= st.len) continue;
+        const size_t step = (size_t)pv.H * ws.part_rows, base = ((size_t)mg.part * pv.H + h) * ws.part_rows + pr;
+        float mx = -INFINITY;
+        for (int s = lane; s < mg.n; s += 32) mx = fmaxf(mx, ws.part_ml[base + s * step].x);
+        mx = warp_max(mx);
+        float l = 0.f, o[D / 32];
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
+        for (int s = 0; s < mg.n; ++s) {
+            const float2 ml = ws.part_ml[base + s * step];
+            if (!(ml.y > 0.f)) continue;                     // the piece holds nothing that the row sees
+            const float f = exp2f(ml.x - mx);
+            l = fmaf(f, ml.y, l);
+            const float *src = ws.part_o + (base + s * step) * D + lane * (D / 32);
+#pragma unroll
+            for (int e = 0; e < D / 32; e += 2) {
+                const float2 v = *reinterpret_cast<const float2 *>(src + e);
+                o[e] = fmaf(f, v.x, o[e]);
+                o[e + 1] = fmaf(f, v.y, o[e + 1]);
+            }
+        }
+        const float inv = 1.f / l;
+        T *dst = static_cast<T *>(a.out) + (int64_t)mg.b * a.so.b + (int64_t)(h * G + g) * a.so.h + (int64_t)i * a.so.t + lane * (D / 32);
+#pragma unroll
+        for (int e = 0; e < D / 32; e += 2) *reinterpret_cast<uint32_t *>(dst + e) = pack2<T>(o[e] * inv, o[e + 1] * inv);
+        if (lane == 0) {
+            const float z = mx + log2f(l);
+            ws.lse2[((size_t)mg.b * pv.H + h) * pv.c * G + (size_t)i * G + g] = z;
+            if (a.lse) a.lse[(((size_t)mg.b * pv.H + h) * G + g) * pv.c + i] = z * 0.6931471805599453f;
+        }
+    }
+}
+
+// ============================================================================================
+// score
+// ============================================================================================
+constexpr int kScoreThreads = 320;           // producer warp, MMA warp, 8 epilogue warps
+constexpr int kScoreStages = 2;
+// Ring of row-constant vectors.  Slot x % ring is rewritten for tile x after the products of tile x-2 have
+// retired; those needed the accumulator of tile x-4, i.e. every thread had finished tile x-5.
+constexpr int kScoreRing = 8;
+
+struct ScoreShared {
+    uint64_t k_full, k_empty, q_full[kScoreStages], q_empty[kScoreStages], acc_full[2], acc_empty[2], c_ready[kScoreRing];
+    uint32_t tmem_base;
+    int abort_flag;
+    alignas(16) float cbuf[kScoreRing][kBlk];
+    float part[kBlk];
+    int32_t prefix[A2SF_PAGED_MAX_SEQUENCES + 1];
+};
+template <int D> constexpr size_t score_smem() { return 1024 + (size_t)Tile<D>::kBytes * (1 + kScoreStages) + sizeof(ScoreShared); }
+
+// Sum of exp2(s * sl2 - c) over this thread's 64 rows; Masked: only rows lo .. hi-1 of them.
+template <bool Masked>
+__device__ __forceinline__ float strip_sum(const uint32_t (&r)[2][32], const float *cb, float sl2, int lo, int hi)
+{
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int x = 0; x < 32; x += 4) {
+            const float4 c4 = *reinterpret_cast<const float4 *>(cb + c * 32 + x);
+            const float cc[4] = {c4.x, c4.y, c4.z, c4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float pw = ex2_approx(fmaf(__uint_as_float(r[c][x + e]), sl2, -cc[e]));
+                if (Masked) pw = c * 32 + x + e >= lo && c * 32 + x + e < hi ? pw : 0.f;
+                part[e] += pw;
+            }
+        }
+    }
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kScoreThreads, 2)
+paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                      const __grid_constant__ AttendArgs a, const __grid_constant__ TcWs ws, int ab_fmt)
+{
+    constexpr int kTileBytes = Tile<D>::kBytes;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *Ks = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *Qs = Ks + kTileBytes;
+    ScoreShared *sh = reinterpret_cast<ScoreShared *>(Qs + kScoreStages * kTileBytes);
+    const PagedView &pv = a.pv;
+    const int G = pv.G, tile_tokens = kBlk / G, tile_rows = tile_tokens * G;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int *abort_flag = &sh->abort_flag;
+
+    if (threadIdx.x == 0) {
+        mbar_init(&sh->k_full, 1);
+        mbar_init(&sh->k_empty, 1);
+        for (int s = 0; s < kScoreStages; ++s) { mbar_init(&sh->q_full[s], 1); mbar_init(&sh->q_empty[s], 1); }
+        for (int x = 0; x < 2; ++x) { mbar_init(&sh->acc_full[x], 1); mbar_init(&sh->acc_empty[x], 256); }
+        for (int x = 0; x < kScoreRing; ++x) mbar_init(&sh->c_ready[x], 1);
+        sh->abort_flag = 0;
+        fence_mbar_init();
+        prefetch_tmap(&map_q);
+        prefetch_tmap(&map_k);
+    }
+    if (warp == 1) {
+        tmem_alloc(&sh->tmem_base, 256);
+        tmem_relinquish();
+    }
+    if (warp == 2) tile_prefix<kBlk>(sh->prefix, pv);
+    // rows that no query copy fills stay zero, so that their logits stay finite
+    for (int x = threadIdx.x; x < kScoreStages * Tile<D>::kHalves * (kBlk - tile_rows) * 8; x += kScoreThreads) {
+        const int piece = x & 7, row = tile_rows + (x >> 3) % (kBlk - tile_rows), half = (x >> 3) / (kBlk - tile_rows);
+        *reinterpret_cast<uint4 *>(Qs + half * Tile<D>::kHalfBytes + row * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
+    }
+    fence_async_smem();
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = sh->tmem_base;
+    const long long total = (long long)pv.H * sh->prefix[pv.B];
+
+    struct Job {
+        int b, h, j0, past, len, used, q0, nq;             // query tiles q0 .. q0 + nq - 1
+    };
+    auto job = [&](long long w) -> Job {
+        const Where x = locate(sh->prefix, pv.B, pv.H, w);
+        const SeqState st = seq_state(pv, x.b);
+        Job j;
+        j.b = x.b; j.h = x.h; j.j0 = x.t * kBlk;
+        j.past = st.past; j.len = st.len; j.used = st.past + st.len;
+        const int first = max(max(first_weighted_token(st.len, a.nl2a), j.j0 - st.past), 0);
+        j.q0 = first / tile_tokens;
+        j.nq = (st.len + tile_tokens - 1) / tile_tokens - j.q0;
+        return j;
+    };
+    auto wait = [&](uint64_t *bar, uint32_t parity) -> bool {
+        if (*abort_flag) return false;
+        return mbar_wait(bar, parity, abort_flag);
+    };
+
+    if (warp == 0) {
+        int qt = 0, n = 0;
+        for (long long w = blockIdx.x; w < total; w += gridDim.x, ++n) {
+            const Job j = job(w);
+            const PageTile p = page_tile(pv, j.j0 / kBlk, j.used);
+            const int slot = j.j0 + lane * p.box;
+            int row = 0, ok = 1;
+            if (lane < p.boxes) row = (int)pool_row(pv, page_for_read(pv, pv.table + (size_t)j.b * pv.max_pages, slot), j.h, slot);
+            if (lane == 0) {
+                ok = n == 0 || wait(&sh->k_empty, (n - 1) & 1) ? 1 : 0;
+                if (ok) mbar_arrive_expect_tx(&sh->k_full, (uint32_t)(p.boxes * p.box * 128 * Tile<D>::kHalves));
+            }
+            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+            copy_page_tile<D>(Ks, &map_k, &sh->k_full, p, row);
+            const float *lse2 = ws.lse2 + ((size_t)j.b * pv.H + j.h) * pv.c * G;
+            for (int t = 0; t < j.nq; ++t, ++qt) {
+                const int s = qt % kScoreStages, i0 = (j.q0 + t) * tile_tokens;
+                float c4[4];                                // in flight while lane 0 waits for the stage
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = lane * 4 + e, i = i0 + r / G;
+                    c4[e] = r < tile_rows && i < j.len ? lse2[(size_t)i0 * G + r] + age_exponent(j.len - 1 - i, a.nl2a) : INFINITY;
+                }
+                ok = 1;
+                if (lane == 0) {
+                    if (qt >= kScoreStages) ok = wait(&sh->q_empty[s], ((qt / kScoreStages) & 1) ^ 1) ? 1 : 0;
+                    if (ok) {
+                        mbar_arrive_expect_tx(&sh->q_full[s], (uint32_t)(tile_rows * 128 * Tile<D>::kHalves));
+                        copy_query_tile<D>(Qs + s * kTileBytes, &map_q, &sh->q_full[s], j.h * G, i0, j.b);
+                    }
+                }
+                if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+                *reinterpret_cast<float4 *>(&sh->cbuf[qt % kScoreRing][lane * 4]) = make_float4(c4[0], c4[1], c4[2], c4[3]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh->c_ready[qt % kScoreRing]);
+            }
+        }
+        if (lane == 0 && *abort_flag) {
+            int dummy = 0;
+            for (int k = max(0, qt - kScoreStages); k < qt; ++k) mbar_wait(&sh->q_full[k % kScoreStages], (k / kScoreStages) & 1, &dummy);
+            if (n > 0) mbar_wait(&sh->k_full, (n - 1) & 1, &dummy);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = make_idesc(ab_fmt, kBlk, kBlk, 0, 0);
+            const uint64_t k_desc = kmajor_desc(smem_u32(Ks));
+            const uint64_t q_desc = kmajor_desc(smem_u32(Qs));
+            int qt = 0, n = 0;
+            for (long long w = blockIdx.x; w < total && !*abort_flag; w += gridDim.x, ++n) {
+                const Job j = job(w);
+                wait(&sh->k_full, n & 1);
+                for (int t = 0; t < j.nq; ++t, ++qt) {
+                    const int s = qt % kScoreStages, acc = qt & 1;
+                    wait(&sh->q_full[s], (qt / kScoreStages) & 1);
+                    wait(&sh->acc_empty[acc], ((qt >> 1) & 1) ^ 1);
+                    tc_fence_after_sync();
+                    issue_qk<D>(tmem_base + acc * kBlk, k_desc, q_desc + s * (uint64_t)(kTileBytes >> 4), idesc);
+                    umma_commit(&sh->q_empty[s]);
+                    umma_commit(&sh->acc_full[acc]);
+                }
+                umma_commit(&sh->k_empty);
+            }
+        }
+    } else {
+        const int quarter = warp & 3, hsel = (warp - 2) >> 2;
+        const int key = quarter * 32 + lane;
+        int qt = 0;
+        const float decay_unit = a.nl2a;
+        for (long long w = blockIdx.x; w < total; w += gridDim.x) {
+            const Job j = job(w);
+            const int slot = j.j0 + key;
+            float *dst = nullptr, old = 0.f;
+            if (hsel == 0 && slot < j.used) {
+                const int page = page_for_write(pv, pv.table + (size_t)j.b * pv.max_pages, slot);
+                if (page >= 0) {
+                    dst = pv.scores + pool_row(pv, page, j.h, slot);
+                    old = *dst;
+                }
+            }
+            float sum = 0.f;
+            for (int t = 0; t < j.nq; ++t, ++qt) {
+                const int acc = qt & 1, i0 = (j.q0 + t) * tile_tokens;
+                wait(&sh->c_ready[qt % kScoreRing], (qt / kScoreRing) & 1);
+                wait(&sh->acc_full[acc], (qt >> 1) & 1);
+                tc_fence_after_sync();
+                const float *cb = sh->cbuf[qt % kScoreRing] + hsel * 64;
+                uint32_t r[2][32];
+                const uint32_t addr = tmem_base + acc * kBlk + hsel * 64 + ((uint32_t)(quarter * 32) << 16);
+                tmem_ld32(addr, r[0]);
+                tmem_ld32(addr + 32, r[1]);
+                tmem_wait_ld();
+                tc_fence_before_sync();
+                mbar_arrive(&sh->acc_empty[acc]);
+                // tiles with rows that do not see the slot, or with rows past the chunk (whose queries may
+                // hold anything), take the test; the others run the bare multiply-add / exponential / add
+                if (j.j0 + kBlk > j.past + i0 + 1 || i0 + tile_tokens > j.len)
+                    sum += strip_sum<true>(r, cb, pv.sl2, max(0, slot - j.past - i0) * G - hsel * 64,
+                                           min(tile_rows, (j.len - i0) * G) - hsel * 64);
+                else
+                    sum += strip_sum<false>(r, cb, pv.sl2, 0, 0);
+            }
+            if (hsel == 1) sh->part[key] = sum;
+            named_barrier(1, 256);
+            if (dst && !*abort_flag) *dst = fmaf(old, ex2_approx(-age_exponent(j.len, decay_unit)), sum + sh->part[key]);
+            named_barrier(1, 256);                          // read before the next item writes
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, 256);
+    }
+    if (threadIdx.x == 0 && sh->abort_flag) *pv.status = A2SF_ERR_TIMEOUT;
+}
+
+size_t pad(size_t x) { return (x + 255) / 256 * 256; }
+
+TcWs carve(const PagedView &pv, void *mem, size_t *bytes)
+{
+    TcWs w;
+    const int tile_tokens = kBlk / pv.G;
+    // a chunk of one row tile needs no second stream
+    w.pair_tokens = 2 * tile_tokens;
+    w.pairs = (pv.c + w.pair_tokens - 1) / w.pair_tokens;
+    w.part_rows = pv.c <= tile_tokens ? kBlk : 2 * kBlk;
+    const size_t U = (size_t)pv.B * pv.H, items = (size_t)pv.B * w.pairs;
+    const size_t cap_tiles = (((size_t)pv.max_pages << pv.ps_shift) + kBlk - 1) / kBlk;
+    w.max_items = (int)(items + kMaxParts);
+    size_t parts = cap_tiles <= kMinPiece ? 0 : items * pv.H * ((cap_tiles + kMinPiece - 1) / kMinPiece);
+    if (parts > kMaxParts) parts = kMaxParts;
+    char *base = static_cast<char *>(mem);
+    size_t off = 0;
+    w.lse2 = reinterpret_cast<float *>(base + off); off += pad(U * pv.c * pv.G * 4);
+    w.head = reinterpret_cast<PlanHead *>(base + off); off += 256;
+    w.items = reinterpret_cast<Item *>(base + off); off += pad(w.max_items * sizeof(Item));
+    w.merges = reinterpret_cast<Merge *>(base + off); off += pad(items * sizeof(Merge));
+    w.part_ml = reinterpret_cast<float2 *>(base + off); off += pad(parts * w.part_rows * 8);
+    w.part_o = reinterpret_cast<float *>(base + off); off += pad(parts * w.part_rows * pv.d * 4);
+    if (bytes) *bytes = off;
+    return w;
+}
+
+template <typename T, int D>
+cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
+{
+    cudaError_t e = allow_dynamic_smem<paged_attn_tc_kernel<T, D>>(attn_smem<D>());
+    if (e == cudaSuccess) e = allow_dynamic_smem<paged_score_tc_kernel<D>>(score_smem<D>());
+    if (e != cudaSuccess) return e;
+    CUtensorMap mq, mk, mv;
+    const int box = a.pv.ps;
+    if (!make_query_map(&mq, dtype, a.q, a.pv, a.sq) || !make_pool_map(&mk, dtype, a.pv.k, a.pv, box) ||
+        !make_pool_map(&mv, dtype, a.pv.v, a.pv, box))
+        return cudaErrorInvalidValue;
+    const TcWs ws = carve(a.pv, a.ws, nullptr);
+    if ((long long)ws.max_items * a.pv.H > 0x7fffffffll) return cudaErrorInvalidValue;
+    paged_plan_kernel<<<1, kPlanThreads, 0, s>>>(a.pv, ws);
+    paged_attn_tc_kernel<T, D><<<kSms, kAttnThreads, attn_smem<D>(), s>>>(mq, mk, mv, a, ws);
+    paged_merge_kernel<T, D><<<2 * kSms, kMergeThreads, 0, s>>>(a, ws);
+    count_launch(3);
+    if ((e = cudaGetLastError()) != cudaSuccess || !a.scores) return e;
+    paged_score_tc_kernel<D><<<2 * kSms, kScoreThreads, score_smem<D>(), s>>>(mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
+    count_launch();
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t attend_tc_ws_bytes(const PagedView &pv)
+{
+    size_t bytes = 0;
+    carve(pv, nullptr, &bytes);
+    return bytes;
+}
+
+cudaError_t launch_attend_tc(int dtype, const AttendArgs &a, cudaStream_t s)
+{
+    const bool wide = a.pv.d == 128;
+    if (dtype == A2SF_BF16) return wide ? launch<__nv_bfloat16, 128>(dtype, a, s) : launch<__nv_bfloat16, 64>(dtype, a, s);
+    return wide ? launch<__half, 128>(dtype, a, s) : launch<__half, 64>(dtype, a, s);
+}
+
+}  // namespace a2sf
