@@ -459,7 +459,7 @@ int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary_op
  * which is Eq. 5 carried over chunks: any split of a prompt into chunks gives the scores of the
  * whole.  flags: 0, or A2SF_ATTEND_NO_SCORES (scores are neither read nor written).  out has strides
  * of its own; rows i >= len[b] of out and lse are left as they were.  Rows whose weight alpha^age
- * is below 2^-150 are left out of the sum (their fp32 contribution is zero).
+ * is below 2^-126 (the smallest normal fp32 number) are left out of the sum.
  * workspace: DEVICE, 256-byte aligned, a2sf_paged_attend_workspace_bytes (0 = invalid arguments);
  * contents undefined afterwards; calls that may overlap in time need workspaces of their own. */
 #define A2SF_ATTEND_NO_SCORES 1

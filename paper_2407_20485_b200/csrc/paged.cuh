@@ -65,12 +65,12 @@ __device__ __forceinline__ float age_exponent(int age, float nl2a) { return age 
 
 __host__ inline float neg_log2(float alpha) { return alpha > 0.f ? -log2f(alpha) : INFINITY; }
 
-// First row (token of the chunk) whose weight alpha^(len-1-i) is not below 2^-150: a probability
-// is at most 1, and 2^-150 rounds to zero in fp32 whatever it is multiplied with.
+// First row (token of the chunk) whose weight alpha^(len-1-i) is not below 2^-126, the smallest normal
+// fp32 number: a probability is at most 1, and the exponential of what lies below is flushed to zero.
 __device__ __forceinline__ int first_weighted_token(int len, float nl2a)
 {
     if (!(nl2a > 0.f)) return 0;
-    const float span = 150.f / nl2a;
+    const float span = 126.f / nl2a;
     return span >= (float)len ? 0 : max(0, len - 1 - (int)span);
 }
 
@@ -129,6 +129,29 @@ __device__ __forceinline__ void next_unit(Where &x, const int32_t *prefix, int B
     x.h = 0;
     do ++x.b; while (x.b < B && prefix[x.b + 1] == prefix[x.b]);
     x.tiles = x.b < B ? prefix[x.b + 1] - prefix[x.b] : 0;
+}
+
+// ---- kernels of one call follow each other by programmatic launch ----------------------------------
+// A follower is resident, its barriers and descriptors set up, while its predecessor drains; it waits
+// with dependency_wait() before it touches anything that any earlier kernel wrote.  Every kernel of such a
+// chain waits, so a kernel that runs has all its predecessors behind it, not only the last one.
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... Params, typename... Args>
+cudaError_t launch_follower(void (*kernel)(Params...), unsigned grid, unsigned threads, size_t smem, cudaStream_t s, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
 }
 
 // ---- launchers -------------------------------------------------------------------------------

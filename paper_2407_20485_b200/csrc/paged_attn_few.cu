@@ -32,7 +32,6 @@ constexpr int kTile = 64;                 // slots per tile
 constexpr int kWarps = 4;                 // consumer warps, 16 slots each
 constexpr int kFewThreads = 32 * (kWarps + 1);
 constexpr int kFinishThreads = 256;
-constexpr int kScoreChunk = 2048;         // slots per score block of the finish kernel
 
 __host__ __device__ constexpr int rows_padded(int rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
 
@@ -391,6 +390,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     __syncthreads();
     if (blockIdx.x == 0)
         for (int b = threadIdx.x; b <= pv.B; b += kFewThreads) ws.prefix[b] = sh.prefix[b];
+    dependents_may_start();
     const long long total = (long long)pv.H * sh.prefix[pv.B];
     const long long share = (total + gridDim.x - 1) / gridDim.x;
     const long long w0 = blockIdx.x * share, w1 = w0 + share < total ? w0 + share : total;
@@ -467,20 +467,25 @@ drained:
     }
 }
 
-// Blocks 0 .. U*NP-1: one output row each.  The following ones: kScoreChunk slots of a unit each.
-template <typename T, int D>
+// The finish kernel: `blocks` blocks per unit.  Block y joins the output rows y, y + blocks, .. and brings the
+// scores of slots y * chunk .. up to date.  Each is a chain of dependent loads, so several slots of a thread are
+// in flight at a time and there are several blocks for every SM.
+constexpr int kScoreSlots = 4;            // slots per thread in flight
+
+template <typename T, int D, int NP>
 __global__ void __launch_bounds__(kFinishThreads)
-paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ FewWs ws, int NP, int ctas, int chunks)
+paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ FewWs ws, int ctas, int blocks, int chunk)
 {
-    __shared__ float red[kFinishThreads], row_c[kFewRows];
+    constexpr int GR = kFinishThreads / D;
+    __shared__ float red[kFinishThreads], red_l[GR], row_m[kFewRows], row_c[kFewRows];
     const PagedView &pv = a.pv;
-    const int U = pv.B * pv.H, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const bool is_out = (int)blockIdx.x < U * NP;
-    const int id = is_out ? blockIdx.x : blockIdx.x - U * NP;
-    const int u = is_out ? id / NP : id / chunks, b = u / pv.H, h = u - b * pv.H;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int u = blockIdx.x / blocks, y = blockIdx.x - u * blocks, b = u / pv.H, h = u - b * pv.H;
     const SeqState st = seq_state(pv, b);
     const int rows = st.len * pv.G, used = st.past + st.len;
-    if (rows == 0) return;
+    dependency_wait();
+    const int j0 = y * chunk;
+    if (rows == 0 || (y >= rows && j0 >= used)) return;
     // the CTAs of the main kernel that had a part of this unit
     const long long total = (long long)pv.H * ws.prefix[pv.B], share = (total + ctas - 1) / ctas;
     const int tiles = ws.prefix[b + 1] - ws.prefix[b];
@@ -488,32 +493,39 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
     const int k0 = (int)(u0 / share), k1 = (int)((u0 + tiles - 1) / share);
     const size_t seg0 = ((size_t)k0 + u) * kWarps;
     const int parts = (k1 - k0 + 1) * kWarps;
-    if (is_out) {
-        const int r = id - u * NP;
-        if (r >= rows) return;
+    // a row's maximum and its constant: log-sum-exp and the weight's exponent (log2 units)
+    for (int r = warp; r < NP; r += kFinishThreads / 32) {
         const float2 *ml = ws.ml + seg0 * NP + r;
-        float mx = -INFINITY;
-        for (int p = tid; p < parts; p += kFinishThreads) mx = fmaxf(mx, ml[(size_t)p * NP].x);
+        float mx = -INFINITY, l = 0.f;
+        for (int p = lane; p < parts; p += 32) mx = fmaxf(mx, ml[(size_t)p * NP].x);
         mx = warp_max(mx);
-        if (lane == 0) red[warp] = mx;
-        __syncthreads();
-        mx = red[0];
-#pragma unroll
-        for (int w = 1; w < kFinishThreads / 32; ++w) mx = fmaxf(mx, red[w]);
-        __syncthreads();
-        // thread groups take every GR-th partial; joined in a fixed order
-        constexpr int GR = kFinishThreads / D;
+        for (int p = lane; p < parts; p += 32) {
+            const float2 x = ml[(size_t)p * NP];
+            l += x.y > 0.f ? exp2f(x.x - mx) * x.y : 0.f;
+        }
+        l = warp_sum(l);
+        if (lane == 0) {
+            row_m[r] = mx;
+            row_c[r] = r < rows ? mx + log2f(l) + age_exponent(st.len - 1 - r / pv.G, a.nl2a) : INFINITY;
+        }
+    }
+    __syncthreads();
+    for (int r = y; r < rows; r += blocks) {
+        // thread groups take every GR-th partial result; joined in a fixed order
+        const float2 *ml = ws.ml + seg0 * NP + r;
+        const float *op = ws.o + (seg0 * NP + r) * D;
         const int d = tid % D, grp = tid / D;
+        const float mx = row_m[r];
         float sum = 0.f, o = 0.f;
-#pragma unroll 4
+#pragma unroll 8
         for (int p = grp; p < parts; p += GR) {
             const float2 x = ml[(size_t)p * NP];
-            const float f = exp2f(x.x - mx);
+            const float f = exp2f(x.x - mx), v = op[(size_t)p * NP * D + d];
             sum = fmaf(f, x.y, sum);
-            o = fmaf(f, ws.o[((seg0 + p) * NP + r) * D + d], o);
+            o = fmaf(f, v, o);
         }
+        __syncthreads();
         red[tid] = o;
-        __shared__ float red_l[GR];
         if (d == 0) red_l[grp] = sum;
         __syncthreads();
         if (grp == 0) {
@@ -525,36 +537,44 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
             if (d == 0 && a.lse)
                 a.lse[((size_t)u * pv.G + g) * pv.c + i] = (mx + log2f(l)) * 0.6931471805599453f;
         }
-        return;
     }
-    const int j0 = (id - u * chunks) * kScoreChunk;
-    if (j0 >= used) return;
-    // a row's constant: log-sum-exp and the weight's exponent (log2 units)
-    for (int r = warp; r < NP; r += kFinishThreads / 32) {
-        const float2 *ml = ws.ml + seg0 * NP + r;
-        float mx = -INFINITY, l = 0.f;
-        for (int p = lane; p < parts; p += 32) mx = fmaxf(mx, ml[(size_t)p * NP].x);
-        mx = warp_max(mx);
-        for (int p = lane; p < parts; p += 32) {
-            const float2 x = ml[(size_t)p * NP];
-            l += x.y > 0.f ? exp2f(x.x - mx) * x.y : 0.f;
-        }
-        l = warp_sum(l);
-        if (lane == 0) row_c[r] = r < rows ? mx + log2f(l) + age_exponent(st.len - 1 - r / pv.G, a.nl2a) : INFINITY;
-    }
-    __syncthreads();
+    if (!a.scores) return;
     const float decay = exp2f(-age_exponent(st.len, a.nl2a));
     const float *logits = ws.logits + (size_t)u * ws.slots * NP;
     const int32_t *table = pv.table + (size_t)b * pv.max_pages;
-    const int j1 = min(used, j0 + kScoreChunk);
-    for (int j = j0 + tid; j < j1; j += kFinishThreads) {
-        float gain = 0.f;
-        const float *x = logits + (size_t)j * NP;
-        for (int r = 0; r < rows; ++r) gain += exp2f(x[r] - row_c[r]);      // -inf where the row does not see the slot
-        const int page = page_for_write(pv, table, j);
-        if (page < 0) continue;
-        float *dst = pv.scores + pool_row(pv, page, h, j);
-        *dst = fmaf(*dst, decay, gain);
+    const int j1 = min(used, j0 + chunk);
+    for (int jb = j0 + tid; jb < j1; jb += kScoreSlots * kFinishThreads) {
+        int page[kScoreSlots];
+        float gain[kScoreSlots], old[kScoreSlots];
+        float *dst[kScoreSlots];
+#pragma unroll
+        for (int x = 0; x < kScoreSlots; ++x) {
+            const int j = jb + x * kFinishThreads;
+            page[x] = j < j1 ? page_for_write(pv, table, j) : -1;
+        }
+#pragma unroll
+        for (int x = 0; x < kScoreSlots; ++x) {
+            const int j = jb + x * kFinishThreads;
+            dst[x] = page[x] >= 0 ? pv.scores + pool_row(pv, page[x], h, j) : nullptr;
+            old[x] = dst[x] ? *dst[x] : 0.f;
+            gain[x] = 0.f;
+            if (j < j1) {
+                // rows that do not see the slot, or are none, have -inf there
+                alignas(16) float v[NP];
+                const float *src = logits + (size_t)j * NP;
+                if constexpr (NP == 1) v[0] = src[0];
+                else if constexpr (NP == 2) *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(src);
+                else {
+#pragma unroll
+                    for (int r = 0; r < NP; r += 4) *reinterpret_cast<float4 *>(v + r) = *reinterpret_cast<const float4 *>(src + r);
+                }
+#pragma unroll
+                for (int r = 0; r < NP; ++r) gain[x] += exp2f(v[r] - row_c[r]);
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < kScoreSlots; ++x)
+            if (dst[x]) *dst[x] = fmaf(old[x], decay, gain[x]);
     }
 }
 
@@ -595,12 +615,26 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     paged_few_kernel<T, D, NC><<<ctas, kFewThreads, smem, s>>>(mk, mv, a, ws, NP);
     count_launch();
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    const int cap = a.pv.max_pages << a.pv.ps_shift, chunks = a.scores ? (cap + kScoreChunk - 1) / kScoreChunk : 0;
-    const long long grid = (long long)a.pv.B * a.pv.H * (NP + chunks);
+    // blocks per unit: enough for the rows and the slots, as far as that fills the device
+    const int cap = a.pv.max_pages << a.pv.ps_shift;
+    const long long units = (long long)a.pv.B * a.pv.H;
+    const int least = kScoreSlots * kFinishThreads, want = (int)((8ll * device_sm_count() + units - 1) / units);
+    int blocks = (cap + least - 1) / least;
+    if (blocks < a.pv.c * a.pv.G) blocks = a.pv.c * a.pv.G;
+    if (blocks > want) blocks = want;
+    const int chunk = ((cap + blocks - 1) / blocks + least - 1) / least * least;
+    const long long grid = units * blocks;
     if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
-    paged_few_finish_kernel<T, D><<<(unsigned)grid, kFinishThreads, 0, s>>>(a, ws, NP, ctas, chunks);
-    count_launch();
-    return cudaGetLastError();
+    auto finish = [&](auto kernel) { return launch_follower(kernel, (unsigned)grid, kFinishThreads, 0, s, a, ws, ctas, blocks, chunk); };
+    switch (NP) {
+    case 1: e = finish(paged_few_finish_kernel<T, D, 1>); break;
+    case 2: e = finish(paged_few_finish_kernel<T, D, 2>); break;
+    case 4: e = finish(paged_few_finish_kernel<T, D, 4>); break;
+    case 8: e = finish(paged_few_finish_kernel<T, D, 8>); break;
+    default: e = finish(paged_few_finish_kernel<T, D, 16>); break;
+    }
+    if (e == cudaSuccess) count_launch();
+    return e;
 }
 
 template <typename T, int D>

@@ -38,11 +38,14 @@ using namespace tc;
 constexpr int kBlk = 128;                    // rows per tile = TMEM lanes; key slots per tile
 constexpr int kSms = 148;
 constexpr int kSplitBelow = 4 * kSms;        // items of a call from which none is cut
-constexpr int kPieces = 4 * kSms;            // pieces that cutting aims at
+constexpr int kPieces = 4 * kSms;            // pieces that cutting makes at most, next to one per item
 constexpr int kMinPiece = 4;                 // key tiles of a piece at least
 constexpr int kMaxParts = kSplitBelow + kPieces;   // sum of ceil(T / piece) <= total / piece + items
 constexpr int kPlanThreads = 1024;
-constexpr int kLenBuckets = 512;
+constexpr int kPlanCache = 4096;             // items whose length fits in the plan's shared memory
+constexpr int kLevels = 8;                   // the list is sorted by length in this many steps
+constexpr int kItemCost = 3;                 // what an item costs beside its tiles (set-up, epilogue), in tiles
+constexpr int kScoreParts = 4 * 2 * kSms;    // below this many score jobs, they are cut along the rows
 
 struct Item {                                // of one head; all heads have the same
     int b, pair, t0, t1;                     // key tiles t0 .. t1-1
@@ -52,7 +55,10 @@ struct Item {                                // of one head; all heads have the 
 struct Merge {
     int b, pair, n, part;                    // partial results part .. part + n - 1
 };
-struct PlanHead { int items, merges; };
+struct PlanHead {
+    int level[kLevels + 1];                  // first item of each step, longest first
+    int merges;
+};
 
 struct TcWs {
     float *lse2;          // [B*H][c*G] log-sum-exp, log2 units
@@ -61,6 +67,7 @@ struct TcWs {
     Merge *merges;        // [B * pairs]
     float2 *part_ml;      // [kMaxParts][part_rows]
     float *part_o;        // [kMaxParts][part_rows][d]
+    float *score_parts;   // [2 * kScoreParts][kBlk]
     int max_items, part_rows, pairs, pair_tokens;
 };
 
@@ -69,63 +76,97 @@ __device__ __forceinline__ int pair_key_tiles(const SeqState &st, int pair, int 
     return (st.past + min((pair + 1) * pair_tokens, st.len) + kBlk - 1) / kBlk;
 }
 
+// The item list.  Cutting items into pieces of p tiles makes sum(ceil(T / p)) of them; CTAs take them in
+// rounds, so a call takes about  max(ceil(pieces / SMs) * (mean length + kItemCost), longest + kItemCost):  32
+// warps try 32 lengths between a quarter and one and a half of an SM's even share, and no cut at all.
 __global__ void __launch_bounds__(kPlanThreads)
 paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ TcWs ws)
 {
-    __shared__ int hist[kLenBuckets], n_parts, n_merges, n_items;
-    __shared__ unsigned long long tiles;
-    const int tid = threadIdx.x;
-    for (int x = tid; x < kLenBuckets; x += kPlanThreads) hist[x] = 0;
-    if (tid == 0) { n_parts = 0; n_merges = 0; n_items = 0; tiles = 0; }
-    __syncthreads();
+    __shared__ int tiles[kPlanCache], level[kLevels], warp_cnt[32], warp_max_[32], cand_piece[32], n_parts, n_merges;
+    __shared__ float cand_cost[32], warp_work[32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    dependents_may_start();
+    if (tid < kLevels) level[tid] = 0;
+    if (tid == 0) { n_parts = 0; n_merges = 0; }
     const int all = pv.B * ws.pairs;
-    auto item_tiles = [&](int x) -> int {
+    auto measure = [&](int x) -> int {
         const int b = x / ws.pairs, p = x - b * ws.pairs;
         const SeqState st = seq_state(pv, b);
         return p * ws.pair_tokens < st.len ? pair_key_tiles(st, p, ws.pair_tokens) : 0;
     };
-    unsigned long long sum = 0;
-    int mine = 0;
+    auto item_tiles = [&](int x) -> int { return x < kPlanCache ? tiles[x] : measure(x); };
+    float sum = 0.f;                                         // of tiles: only the choice below uses it
+    int cnt = 0, mx = 0;
     for (int x = tid; x < all; x += kPlanThreads) {
-        const int t = item_tiles(x);
+        const int t = measure(x);
+        if (x < kPlanCache) tiles[x] = t;
         sum += t;
-        mine += t > 0;
+        cnt += t > 0;
+        mx = max(mx, t);
     }
-    if (mine) { atomicAdd(&tiles, sum); atomicAdd(&n_items, mine); }
+    sum = warp_sum(sum);
+    const int wcnt = __reduce_add_sync(0xffffffffu, cnt), wmax = __reduce_max_sync(0xffffffffu, mx);
+    if (lane == 0) { warp_work[warp] = sum; warp_cnt[warp] = wcnt; warp_max_[warp] = wmax; }
     __syncthreads();
-    const long long work = (long long)tiles * pv.H, units = (long long)n_items * pv.H;
-    long long piece = 0x7fffffff;
-    if (units < kSplitBelow) piece = max((long long)kMinPiece, (work + kPieces - 1) / kPieces);
-    auto pieces = [&](int t) { return (int)((t + piece - 1) / piece); };
+    const float work = (float)pv.H * warp_sum(warp_work[lane]);
+    const int items = __reduce_add_sync(0xffffffffu, warp_cnt[lane]);
+    const int longest = __reduce_max_sync(0xffffffffu, warp_max_[lane]);
+    int piece = 0x7fffffff;
+    if ((long long)items * pv.H < kSplitBelow && longest > kMinPiece) {
+        // warp w tries one length; the last one no cut
+        const float share = work / kSms;
+        const int p = warp == 31 ? 0x7fffffff : max(kMinPiece, (int)ceilf(share * 0.25f * exp2f(warp * (2.585f / 30.f))));
+        int n = 0, most = 0;
+        for (int x = lane; x < all; x += 32) {
+            const int t = item_tiles(x);
+            const int k = t > 0 ? (t - 1) / p + 1 : 0;
+            n += k;
+            most = max(most, k ? (t + k - 1) / k : 0);
+        }
+        n = __reduce_add_sync(0xffffffffu, n) * pv.H;
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) {
+            const float rounds = (float)((n + kSms - 1) / kSms);
+            cand_cost[warp] = fmaxf(rounds * (work / (float)max(n, 1) + kItemCost), (float)(most + kItemCost));
+            cand_piece[warp] = p;
+        }
+        __syncthreads();
+        float best = cand_cost[lane];
+        int at = lane;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const float c = __shfl_xor_sync(0xffffffffu, best, o);
+            const int i = __shfl_xor_sync(0xffffffffu, at, o);
+            if (c < best || (c == best && i > at)) { best = c; at = i; }     // of equals the longer piece
+        }
+        piece = cand_piece[at];
+    }
+    const int longest_piece = min(longest, piece);
+    auto level_of = [&](int len) { return kLevels - 1 - min(kLevels - 1, (int)((long long)len * kLevels / (longest_piece + 1))); };
     for (int x = tid; x < all; x += kPlanThreads) {
         const int t = item_tiles(x);
         if (!t) continue;
-        const int n = pieces(t), len = (t + n - 1) / n;
-        atomicAdd(&hist[kLenBuckets - 1 - min(len, kLenBuckets - 1)], n);
+        const int n = (t - 1) / piece + 1;
+        atomicAdd(&level[level_of((t + n - 1) / n)], n);
     }
     __syncthreads();
-    if (tid < 32) {                                          // exclusive scan: longest first
+    if (tid == 0) {
         int run = 0;
-        for (int x0 = 0; x0 < kLenBuckets; x0 += 32) {
-            const int v = hist[x0 + tid];
-            int incl = v;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, incl, o);
-                if (tid >= o) incl += y;
-            }
-            hist[x0 + tid] = run + incl - v;
-            run += __shfl_sync(0xffffffffu, incl, 31);
+        for (int l = 0; l < kLevels; ++l) {
+            const int v = level[l];
+            ws.head->level[l] = min(run, ws.max_items);
+            level[l] = run;
+            run += v;
         }
-        if (tid == 0) ws.head->items = min(run, ws.max_items);
+        ws.head->level[kLevels] = min(run, ws.max_items);
     }
     __syncthreads();
     // the order of equal lengths may differ from run to run; no result depends on it
     for (int x = tid; x < all; x += kPlanThreads) {
         const int t = item_tiles(x);
         if (!t) continue;
-        const int n = pieces(t), len = (t + n - 1) / n, b = x / ws.pairs, p = x - b * ws.pairs;
-        int at = atomicAdd(&hist[kLenBuckets - 1 - min(len, kLenBuckets - 1)], n);
+        const int n = (t - 1) / piece + 1, b = x / ws.pairs, p = x - b * ws.pairs;
+        int at = atomicAdd(&level[level_of((t + n - 1) / n)], n);
         int part = -1;
         if (n > 1) {
             part = atomicAdd(&n_parts, n);
@@ -238,6 +279,7 @@ struct AttnShared {
     uint64_t s_full[2], p_full[2], o_done[2], o_free[2];    // per stream
     uint32_t tmem_base;
     int abort_flag;
+    int level[kLevels + 1];
     float xch[2][2][kBlk];                                  // [stream][column half][row]
 };
 
@@ -285,9 +327,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         *reinterpret_cast<uint4 *>(Qs + half * Tile<D>::kHalfBytes + row * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
     }
     fence_async_smem();
+    dependency_wait();
+    if (threadIdx.x <= kLevels) sh->level[threadIdx.x] = ws.head->level[threadIdx.x];
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    dependents_may_start();
     const uint32_t tmem_base = sh->tmem_base;
 
     // A failed wait poisons the CTA: later waits return at once, loops keep their shape.
@@ -295,15 +340,21 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         if (*abort_flag) return false;
         return mbar_wait(bar, parity, abort_flag);
     };
-    const int n_units = ws.head->items * pv.H;
+    // Jobs: by step of length, then by head (the items of a head run together and share its K and V
+    // through L2), dealt in rounds of alternating direction.
+    const int n_units = sh->level[kLevels] * pv.H;
+    auto dealt = [&](int round) { return round * (int)gridDim.x + (round & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
     // what an item means to every role
     struct Job {
         int b, h, i0, tokens, t0, nt, ntA, ntB, past, used, part;
     };
     auto job = [&](int unit) -> Job {
-        const Item it = ws.items[unit / pv.H];
+        int l = 0;
+        while (l < kLevels - 1 && unit >= sh->level[l + 1] * pv.H) ++l;
+        const int first = sh->level[l], n_items = sh->level[l + 1] - first, rest = unit - first * pv.H;
+        const Item it = ws.items[first + rest % n_items];
         Job j;
-        j.b = it.b; j.h = unit % pv.H;
+        j.b = it.b; j.h = rest / n_items;
         const SeqState st = seq_state(pv, it.b);
         j.past = st.past; j.used = st.past + st.len;
         j.i0 = it.pair * ws.pair_tokens;
@@ -321,7 +372,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     if (warp == 0) {
         // ---- TMA producer: lane i copies page box i ------------------------------------------
         int kt = 0, n = 0;                                  // tiles and items so far
-        for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x, ++n) {
+        for (int unit; (unit = dealt(n)) < n_units; ++n) {
             const Job j = job(unit);
             const int32_t *table = pv.table + (size_t)j.b * pv.max_pages;
             int ok = 1;
@@ -388,7 +439,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             umma_commit(&sh->o_done[X]);
         };
         int kt = 0, n = 0, cnt[2] = {0, 0}, used_before[2] = {0, 0};      // tiles per stream; items per stream
-        for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x, ++n) {
+        for (int unit; (unit = dealt(n)) < n_units; ++n) {
             if (__any_sync(0xffffffffu, *abort_flag)) break;
             const Job j = job(unit);
             const int ntX[2] = {j.ntA, j.ntB};
@@ -448,7 +499,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         float m_used[2], l[2];
         // no early exit here: the two warps of a quarter meet at named barriers, and after a failed wait
         // all that follows runs through without waiting
-        for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x) {
+        for (int n = 0, unit; (unit = dealt(n)) < n_units; ++n) {
             const Job j = job(unit);
             auto do_tile = [&](auto Xc, int t) {
                 constexpr int X = decltype(Xc)::value;
@@ -631,8 +682,11 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kMergeThreads)
 paged_merge_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ TcWs ws)
 {
+    constexpr int V = D / 32;                                // elements per lane
     const PagedView &pv = a.pv;
     const int G = pv.G, tile_tokens = kBlk / G, lane = threadIdx.x & 31;
+    dependency_wait();
+    dependents_may_start();
     const long long rows = (long long)ws.head->merges * pv.H * ws.part_rows;
     const int wpg = gridDim.x * (kMergeThreads / 32);
     for (long long x = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5); x < rows; x += wpg) {
@@ -645,29 +699,37 @@ paged_merge_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__
         const int tok = X * tile_tokens + r / G, g = r - r / G * G, i = mg.pair * ws.pair_tokens + tok;
         if (r >= tile_tokens * G || tok >= ws.pair_tokens || i >= st.len) continue;
         const size_t step = (size_t)pv.H * ws.part_rows, base = ((size_t)mg.part * pv.H + h) * ws.part_rows + pr;
-        float mx = -INFINITY;
-        for (int s = lane; s < mg.n; s += 32) mx = fmaxf(mx, ws.part_ml[base + s * step].x);
-        mx = warp_max(mx);
-        float l = 0.f, o[D / 32];
+        // lane s holds piece s0 + s; pieces that hold nothing the row sees have weight 0 and are not read
+        float mx = -INFINITY, l = 0.f, o[V];
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-        for (int s = 0; s < mg.n; ++s) {
-            const float2 ml = ws.part_ml[base + s * step];
-            if (!(ml.y > 0.f)) continue;                     // the piece holds nothing that the row sees
-            const float f = exp2f(ml.x - mx);
-            l = fmaf(f, ml.y, l);
-            const float *src = ws.part_o + (base + s * step) * D + lane * (D / 32);
+        for (int e = 0; e < V; ++e) o[e] = 0.f;
+        for (int s0 = 0; s0 < mg.n; s0 += 32) {
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (s0 + lane < mg.n) ml = ws.part_ml[base + (s0 + lane) * step];
+            const float mn = fmaxf(mx, warp_max(ml.y > 0.f ? ml.x : -INFINITY));
+            if (mn == -INFINITY) continue;
+            const float old = exp2f(mx - mn), f = ml.y > 0.f ? exp2f(ml.x - mn) : 0.f;
+            mx = mn;
+            l = fmaf(l, old, warp_sum(f * ml.y));
 #pragma unroll
-            for (int e = 0; e < D / 32; e += 2) {
-                const float2 v = *reinterpret_cast<const float2 *>(src + e);
-                o[e] = fmaf(f, v.x, o[e]);
-                o[e + 1] = fmaf(f, v.y, o[e + 1]);
+            for (int e = 0; e < V; ++e) o[e] *= old;
+            const int n = min(32, mg.n - s0);
+#pragma unroll 4
+            for (int s = 0; s < n; ++s) {
+                const float w = __shfl_sync(0xffffffffu, f, s);
+                if (w == 0.f) continue;
+                const float *src = ws.part_o + (base + (s0 + s) * step) * D + lane * V;
+                alignas(16) float v[V];
+                if constexpr (V == 4) *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(src);
+                else                  *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(src);
+#pragma unroll
+                for (int e = 0; e < V; ++e) o[e] = fmaf(w, v[e], o[e]);
             }
         }
         const float inv = 1.f / l;
-        T *dst = static_cast<T *>(a.out) + (int64_t)mg.b * a.so.b + (int64_t)(h * G + g) * a.so.h + (int64_t)i * a.so.t + lane * (D / 32);
+        T *dst = static_cast<T *>(a.out) + (int64_t)mg.b * a.so.b + (int64_t)(h * G + g) * a.so.h + (int64_t)i * a.so.t + lane * V;
 #pragma unroll
-        for (int e = 0; e < D / 32; e += 2) *reinterpret_cast<uint32_t *>(dst + e) = pack2<T>(o[e] * inv, o[e + 1] * inv);
+        for (int e = 0; e < V; e += 2) *reinterpret_cast<uint32_t *>(dst + e) = pack2<T>(o[e] * inv, o[e + 1] * inv);
         if (lane == 0) {
             const float z = mx + log2f(l);
             ws.lse2[((size_t)mg.b * pv.H + h) * pv.c * G + (size_t)i * G + g] = z;
@@ -717,6 +779,14 @@ __device__ __forceinline__ float strip_sum(const uint32_t (&r)[2][32], const flo
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+// Few key tiles (a prompt of its own, not behind a long cache) leave SMs without a job: then every job is cut
+// along the rows into this many, whose sums score_join adds in order.
+__device__ __forceinline__ int score_cuts(const int32_t *prefix, const PagedView &pv)
+{
+    const long long jobs = (long long)pv.H * prefix[pv.B];
+    return jobs == 0 || jobs >= kScoreParts ? 1 : (int)min(16ll, (kScoreParts + jobs - 1) / jobs);
+}
+
 template <int D>
 __global__ void __launch_bounds__(kScoreThreads, 2)
 paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -747,7 +817,7 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         tmem_alloc(&sh->tmem_base, 256);
         tmem_relinquish();
     }
-    if (warp == 2) tile_prefix<kBlk>(sh->prefix, pv);
+    if (warp == 2) tile_prefix<kBlk>(sh->prefix, pv);       // lengths: no kernel of the call writes them
     // rows that no query copy fills stay zero, so that their logits stay finite
     for (int x = threadIdx.x; x < kScoreStages * Tile<D>::kHalves * (kBlk - tile_rows) * 8; x += kScoreThreads) {
         const int piece = x & 7, row = tile_rows + (x >> 3) % (kBlk - tile_rows), half = (x >> 3) / (kBlk - tile_rows);
@@ -758,20 +828,25 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = sh->tmem_base;
-    const long long total = (long long)pv.H * sh->prefix[pv.B];
+    const int cuts = score_cuts(sh->prefix, pv);
+    const long long total = (long long)pv.H * sh->prefix[pv.B] * cuts;
+    dependency_wait();
+    dependents_may_start();
 
     struct Job {
         int b, h, j0, past, len, used, q0, nq;             // query tiles q0 .. q0 + nq - 1
     };
     auto job = [&](long long w) -> Job {
-        const Where x = locate(sh->prefix, pv.B, pv.H, w);
+        const int cut = (int)(w % cuts);
+        const Where x = locate(sh->prefix, pv.B, pv.H, w / cuts);
         const SeqState st = seq_state(pv, x.b);
         Job j;
         j.b = x.b; j.h = x.h; j.j0 = x.t * kBlk;
         j.past = st.past; j.len = st.len; j.used = st.past + st.len;
-        const int first = max(max(first_weighted_token(st.len, a.nl2a), j.j0 - st.past), 0);
-        j.q0 = first / tile_tokens;
-        j.nq = (st.len + tile_tokens - 1) / tile_tokens - j.q0;
+        const int first = max(max(first_weighted_token(st.len, a.nl2a), j.j0 - st.past), 0) / tile_tokens;
+        const int n = (st.len + tile_tokens - 1) / tile_tokens - first;
+        j.q0 = first + n * cut / cuts;
+        j.nq = first + n * (cut + 1) / cuts - j.q0;
         return j;
     };
     auto wait = [&](uint64_t *bar, uint32_t parity) -> bool {
@@ -846,12 +921,11 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         const int quarter = warp & 3, hsel = (warp - 2) >> 2;
         const int key = quarter * 32 + lane;
         int qt = 0;
-        const float decay_unit = a.nl2a;
         for (long long w = blockIdx.x; w < total; w += gridDim.x) {
             const Job j = job(w);
             const int slot = j.j0 + key;
             float *dst = nullptr, old = 0.f;
-            if (hsel == 0 && slot < j.used) {
+            if (cuts == 1 && hsel == 0 && slot < j.used) {
                 const int page = page_for_write(pv, pv.table + (size_t)j.b * pv.max_pages, slot);
                 if (page >= 0) {
                     dst = pv.scores + pool_row(pv, page, j.h, slot);
@@ -882,7 +956,8 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             }
             if (hsel == 1) sh->part[key] = sum;
             named_barrier(1, 256);
-            if (dst && !*abort_flag) *dst = fmaf(old, ex2_approx(-age_exponent(j.len, decay_unit)), sum + sh->part[key]);
+            if (dst && !*abort_flag) *dst = fmaf(old, ex2_approx(-age_exponent(j.len, a.nl2a)), sum + sh->part[key]);
+            if (cuts > 1 && hsel == 0) ws.score_parts[w * kBlk + key] = sum + sh->part[key];
             named_barrier(1, 256);                          // read before the next item writes
         }
     }
@@ -893,6 +968,32 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         tmem_dealloc(tmem_base, 256);
     }
     if (threadIdx.x == 0 && sh->abort_flag) *pv.status = A2SF_ERR_TIMEOUT;
+}
+
+// Adds the sums of jobs that were cut: a block per key tile.
+__global__ void __launch_bounds__(kBlk)
+paged_score_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ TcWs ws)
+{
+    __shared__ int32_t prefix[A2SF_PAGED_MAX_SEQUENCES + 1];
+    const PagedView &pv = a.pv;
+    if (threadIdx.x < 32) tile_prefix<kBlk>(prefix, pv);
+    __syncthreads();
+    const int cuts = score_cuts(prefix, pv);
+    dependency_wait();
+    if (cuts == 1) return;
+    const long long jobs = (long long)pv.H * prefix[pv.B];
+    for (long long w = blockIdx.x; w < jobs; w += gridDim.x) {
+        const Where x = locate(prefix, pv.B, pv.H, w);
+        const SeqState st = seq_state(pv, x.b);
+        const int slot = x.t * kBlk + threadIdx.x;
+        if (slot >= st.past + st.len) continue;
+        const int page = page_for_write(pv, pv.table + (size_t)x.b * pv.max_pages, slot);
+        if (page < 0) continue;
+        float sum = 0.f;
+        for (int c = 0; c < cuts; ++c) sum += ws.score_parts[(w * cuts + c) * kBlk + threadIdx.x];
+        float *dst = pv.scores + pool_row(pv, page, x.h, slot);
+        *dst = fmaf(*dst, ex2_approx(-age_exponent(st.len, a.nl2a)), sum);
+    }
 }
 
 size_t pad(size_t x) { return (x + 255) / 256 * 256; }
@@ -918,6 +1019,7 @@ TcWs carve(const PagedView &pv, void *mem, size_t *bytes)
     w.merges = reinterpret_cast<Merge *>(base + off); off += pad(items * sizeof(Merge));
     w.part_ml = reinterpret_cast<float2 *>(base + off); off += pad(parts * w.part_rows * 8);
     w.part_o = reinterpret_cast<float *>(base + off); off += pad(parts * w.part_rows * pv.d * 4);
+    w.score_parts = reinterpret_cast<float *>(base + off); off += pad((size_t)2 * kScoreParts * kBlk * 4);
     if (bytes) *bytes = off;
     return w;
 }
@@ -936,13 +1038,20 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
     const TcWs ws = carve(a.pv, a.ws, nullptr);
     if ((long long)ws.max_items * a.pv.H > 0x7fffffffll) return cudaErrorInvalidValue;
     paged_plan_kernel<<<1, kPlanThreads, 0, s>>>(a.pv, ws);
-    paged_attn_tc_kernel<T, D><<<kSms, kAttnThreads, attn_smem<D>(), s>>>(mq, mk, mv, a, ws);
-    paged_merge_kernel<T, D><<<2 * kSms, kMergeThreads, 0, s>>>(a, ws);
-    count_launch(3);
-    if ((e = cudaGetLastError()) != cudaSuccess || !a.scores) return e;
-    paged_score_tc_kernel<D><<<2 * kSms, kScoreThreads, score_smem<D>(), s>>>(mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
     count_launch();
-    return cudaGetLastError();
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    e = launch_follower(paged_attn_tc_kernel<T, D>, kSms, kAttnThreads, attn_smem<D>(), s, mq, mk, mv, a, ws);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    if ((e = launch_follower(paged_merge_kernel<T, D>, 8 * kSms, kMergeThreads, 0, s, a, ws)) != cudaSuccess) return e;
+    count_launch();
+    if (!a.scores) return cudaSuccess;
+    e = launch_follower(paged_score_tc_kernel<D>, 2 * kSms, kScoreThreads, score_smem<D>(), s, mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    if ((e = launch_follower(paged_score_join_kernel, 4 * kSms, kBlk, 0, s, a, ws)) != cudaSuccess) return e;
+    count_launch();
+    return cudaSuccess;
 }
 
 }  // namespace

@@ -17,7 +17,8 @@ A2SF_DEBUG_TRANSLATION_UNIT(paged_evict)
 
 namespace {
 
-constexpr int kSelThreads = 1024;
+constexpr int kSelThreads = 512;
+constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kCached = 16384;       // slots whose (score key, position) fit in shared memory
 
 struct EvictArgs {
@@ -29,6 +30,7 @@ struct EvictArgs {
     int32_t *from, *to;              // [U][M] slot lists (to: in place only)
     int32_t *moves;                  // [U]
     int32_t *ends;                   // [B][2] new past, new start
+    int blocks;                      // of the move kernel, per unit
 };
 
 // Order-preserving key of a score; every NaN sorts last, -0 like +0.
@@ -41,40 +43,41 @@ __device__ __forceinline__ unsigned score_key(float s)
 
 struct SelShared {
     int hist[256];
-    int warp_tot[3][33];
+    int warp_tot[3][kSelWarps + 1];
     unsigned prefix;
     int rank, equal, ncand;
 };
 
-// Exclusive scan of one int per warp (lane 0 holds it) over the CTA's 32 warps, for `which`.
+// Exclusive scan of one int per warp (lane 0 holds it) over the CTA's warps, for `which`.
 __device__ __forceinline__ int warps_excl_scan(SelShared &sh, int which, int v, int &total)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (lane == 0) sh.warp_tot[which][warp] = v;
     __syncthreads();
     if (warp == which) {
-        const int t = sh.warp_tot[which][lane];
+        const int t = lane < kSelWarps ? sh.warp_tot[which][lane] : 0;
         int ti = t;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, ti, o);
             if (lane >= o) ti += x;
         }
-        sh.warp_tot[which][lane] = ti - t;
-        if (lane == 31) sh.warp_tot[which][32] = ti;
+        if (lane < kSelWarps) sh.warp_tot[which][lane] = ti - t;
+        if (lane == 31) sh.warp_tot[which][kSelWarps] = ti;
     }
     __syncthreads();
-    total = sh.warp_tot[which][32];
+    total = sh.warp_tot[which][kSelWarps];
     return sh.warp_tot[which][warp];
 }
 
-__global__ void __launch_bounds__(kSelThreads)
+__global__ void __launch_bounds__(kSelThreads, 4)
 paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
 {
     extern __shared__ __align__(8) uint2 cache[];       // [cached] (key, position)
     __shared__ SelShared sh;
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = u / a.pv.H, h = u - b * a.pv.H;
+    dependents_may_start();
     const SeqState st = seq_state(a.pv, b);
     const int n = st.past + st.len, M = a.M;
     const int start = a.pv.start ? a.pv.start[b] : st.past;
@@ -97,6 +100,7 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
         const int64_t row = pool_row(a.pv, page_for_read(a.pv, table, j), h, j);
         return make_uint2(score_key(a.pv.scores[row]), (unsigned)a.pv.positions[row]);
     };
+#pragma unroll 4
     for (int j = tid; j < min(n, cached); j += kSelThreads) cache[j] = fetch(j);
     auto item = [&](int j) -> uint2 { return j < cached ? cache[j] : fetch(j); };
     auto recent = [&](const uint2 &x) { return (long long)(int)x.y >= newest; };
@@ -168,7 +172,7 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
     };
     auto drops = [&](const uint2 &x) { return below(x) || (from_recent && !recent(x)); };
     // every warp takes a contiguous range of slots, 32 at a time: count, scan over the warps, list
-    const int per = ((n + 31) / 32 + 31) / 32 * 32;
+    const int per = ((n + kSelWarps - 1) / kSelWarps + 31) / 32 * 32;
     const int w0 = min(n, warp * per), w1 = min(n, w0 + per);
     int eq_cnt = 0, total;
     for (int j0 = w0; j0 < w1; j0 += 32) {
@@ -227,6 +231,7 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
 }
 
 constexpr int kMoveThreads = 256;
+constexpr int kRows = 4;             // rows of a lane group in flight
 
 // A group of ROW_BYTES / 16 lanes copies one row of K and of V.
 template <int ROW_BYTES>
@@ -234,8 +239,9 @@ __global__ void __launch_bounds__(kMoveThreads)
 paged_move_kernel(const __grid_constant__ EvictArgs a)
 {
     constexpr int LPR = ROW_BYTES / 16, RPB = kMoveThreads / LPR;
-    const int u = blockIdx.x, b = u / a.pv.H, h = u - b * a.pv.H;
-    if (h == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+    const int u = blockIdx.x / a.blocks, by = blockIdx.x - u * a.blocks, b = u / a.pv.H, h = u - b * a.pv.H;
+    dependency_wait();
+    if (h == 0 && by == 0 && threadIdx.x == 0) {
         a.past_out[b] = a.ends[2 * b];
         a.start_out[b] = a.ends[2 * b + 1];
     }
@@ -243,19 +249,35 @@ paged_move_kernel(const __grid_constant__ EvictArgs a)
     const bool fresh = a.dst_table != nullptr;
     const int32_t *from_row = a.pv.table + (size_t)b * a.pv.max_pages;
     const int32_t *to_row = fresh ? a.dst_table + (size_t)b * a.dst_max_pages : from_row;
-    for (int k = blockIdx.y * RPB + threadIdx.x / LPR; k < moves; k += gridDim.y * RPB) {
-        const int src = a.from[(size_t)u * a.M + k], dst = fresh ? k : a.to[(size_t)u * a.M + k];
-        const int to_page = page_for_write(a.pv, to_row, dst);
-        if (to_page < 0) continue;
-        const int64_t s = pool_row(a.pv, page_for_read(a.pv, from_row, src), h, src);
-        const int64_t t = pool_row(a.pv, to_page, h, dst);
-        const uint4 kv = *reinterpret_cast<const uint4 *>(a.pv.k + s * ROW_BYTES + part * 16);
-        const uint4 vv = *reinterpret_cast<const uint4 *>(a.pv.v + s * ROW_BYTES + part * 16);
-        *reinterpret_cast<uint4 *>(a.pv.k + t * ROW_BYTES + part * 16) = kv;
-        *reinterpret_cast<uint4 *>(a.pv.v + t * ROW_BYTES + part * 16) = vv;
-        if (part == 0) {
-            a.pv.scores[t] = a.pv.scores[s];
-            a.pv.positions[t] = a.pv.positions[s];
+    // kRows rows of a lane group in flight: a move is a chain of three loads (list, page, row)
+    for (int k0 = by * RPB * kRows + threadIdx.x / LPR; k0 < moves; k0 += a.blocks * RPB * kRows) {
+        int64_t s[kRows], t[kRows];
+        uint4 kv[kRows], vv[kRows];
+        float sc[kRows];
+        int32_t ps[kRows];
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            const int k = k0 + x * RPB;
+            t[x] = -1;
+            if (k >= moves) continue;
+            const int src = a.from[(size_t)u * a.M + k], dst = fresh ? k : a.to[(size_t)u * a.M + k];
+            const int to_page = page_for_write(a.pv, to_row, dst);
+            s[x] = pool_row(a.pv, page_for_read(a.pv, from_row, src), h, src);
+            if (to_page >= 0) t[x] = pool_row(a.pv, to_page, h, dst);
+        }
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            if (t[x] < 0) continue;
+            kv[x] = ld_stream16_rw(a.pv.k + s[x] * ROW_BYTES + part * 16);
+            vv[x] = ld_stream16_rw(a.pv.v + s[x] * ROW_BYTES + part * 16);
+            if (part == 0) { sc[x] = a.pv.scores[s[x]]; ps[x] = a.pv.positions[s[x]]; }
+        }
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            if (t[x] < 0) continue;
+            *reinterpret_cast<uint4 *>(a.pv.k + t[x] * ROW_BYTES + part * 16) = kv[x];
+            *reinterpret_cast<uint4 *>(a.pv.v + t[x] * ROW_BYTES + part * 16) = vv[x];
+            if (part == 0) { a.pv.scores[t[x]] = sc[x]; a.pv.positions[t[x]] = ps[x]; }
         }
     }
 }
@@ -277,6 +299,7 @@ cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int re
     a.pv = pv; a.M = budget; a.R = recent;
     a.dst_table = dst_table; a.dst_max_pages = dst_max_pages;
     a.past_out = past_out; a.start_out = start_out;
+    a.blocks = 1;
     char *w = static_cast<char *>(ws);
     a.from = reinterpret_cast<int32_t *>(w); w += pad(units * (size_t)budget * 4);
     a.to = reinterpret_cast<int32_t *>(w); w += pad(units * (size_t)budget * 4);
@@ -291,17 +314,18 @@ cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int re
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     const int row_bytes = pv.d * elem_bytes, rpb = kMoveThreads / (row_bytes / 16);
     const int most = budget < cap ? budget : cap;
-    long long gy = (most + rpb - 1) / rpb;
+    long long blocks = (most + rpb * kRows - 1) / (rpb * kRows);
     const long long want = (16ll * device_sm_count() + (long long)units - 1) / (long long)units;
-    if (gy > want) gy = want;
-    const dim3 grid((unsigned)units, (unsigned)gy);
+    if (blocks > want) blocks = want;
+    a.blocks = (int)blocks;
+    const unsigned grid = (unsigned)(units * blocks);
     switch (row_bytes) {
-    case 128: paged_move_kernel<128><<<grid, kMoveThreads, 0, s>>>(a); break;
-    case 256: paged_move_kernel<256><<<grid, kMoveThreads, 0, s>>>(a); break;
-    default: paged_move_kernel<512><<<grid, kMoveThreads, 0, s>>>(a); break;
+    case 128: e = launch_follower(paged_move_kernel<128>, grid, kMoveThreads, 0, s, a); break;
+    case 256: e = launch_follower(paged_move_kernel<256>, grid, kMoveThreads, 0, s, a); break;
+    default: e = launch_follower(paged_move_kernel<512>, grid, kMoveThreads, 0, s, a); break;
     }
-    count_launch();
-    return cudaGetLastError();
+    if (e == cudaSuccess) count_launch();
+    return e;
 }
 
 }  // namespace a2sf

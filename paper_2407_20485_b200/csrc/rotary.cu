@@ -150,12 +150,11 @@ cudaError_t launch_w(const a2sf_rotary_plan *plan, const RotaryArgs &r, const Pa
     const long long threads = (long long)r.B * r.n * items;
     const long long gx = (threads + kRotThreads - 1) / kRotThreads;
     if (gx > 0x7fffffffll) return cudaErrorInvalidValue;
-    // the heads are split over blocks only as far as it takes to fill the device
+    // the heads are split over blocks only as far as it takes to fill the device, a batch of kHeads at least
     const int total = r.Hq + (Append ? 2 * r.Hk : 0);
-    const long long want = 8ll * device_sm_count();
-    long long gy = (want + gx - 1) / gx;
-    if (gy > total) gy = total;
-    const int hpb = (int)((total + gy - 1) / gy);
+    const long long want = 32ll * device_sm_count();
+    const long long gy = (want + gx - 1) / gx;
+    const int hpb = (int)(((total + gy - 1) / gy + kHeads - 1) / kHeads) * kHeads;
     const dim3 grid((unsigned)gx, (unsigned)((total + hpb - 1) / hpb));
     rotary_kernel<T, W, Interleaved, Append><<<grid, kRotThreads, 0, s>>>(
         pa, r, pv, r_dim, plan ? plan->magnitude : 1.f, rot_items, items, hpb);
