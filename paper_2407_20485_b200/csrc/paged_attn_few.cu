@@ -400,6 +400,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (warp == 0) {
         // ---- producer: lane i copies box i of the tile --------------------------------------------
         const int box = min(pv.ps, kTile), boxes = kTile / box;
+        const uint64_t policy = policy_evict_first();     // read once: the logits are to stay in L2 instead
         int it = 0;
         for (long long w = w0; w < w1;) {
             const SeqState st = seq_state(pv, x.b);
@@ -421,8 +422,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                     uint8_t *dst = ring + (size_t)s * 2 * R::kTileBytes + lane * box * 128;
 #pragma unroll
                     for (int ch = 0; ch < R::kChunks; ++ch) {
-                        tma_load_2d(dst + ch * (kTile * 128), &map_k, &sh.full[s], ch * (128 / (int)sizeof(T)), row);
-                        tma_load_2d(dst + R::kTileBytes + ch * (kTile * 128), &map_v, &sh.full[s], ch * (128 / (int)sizeof(T)), row);
+                        tma_load_2d(dst + ch * (kTile * 128), &map_k, &sh.full[s], ch * (128 / (int)sizeof(T)), row, policy);
+                        tma_load_2d(dst + R::kTileBytes + ch * (kTile * 128), &map_v, &sh.full[s], ch * (128 / (int)sizeof(T)), row, policy);
                     }
                 }
                 __syncwarp();
@@ -468,24 +469,86 @@ drained:
 }
 
 // The finish kernel: `blocks` blocks per unit.  Block y joins the output rows y, y + blocks, .. and brings the
-// scores of slots y * chunk .. up to date.  Each is a chain of dependent loads, so several slots of a thread are
-// in flight at a time and there are several blocks for every SM.
-constexpr int kScoreSlots = 4;            // slots per thread in flight
+// scores of slots y * chunk .. up to date.  All of it is latency: dependent loads around a few bytes.  So the page
+// numbers and old scores of the first slots are read while the main kernel still drains, the logits and the
+// partial maxima and sums are requested together, and a thread has several slots in flight.
+
+constexpr int finish_ctas(int NP) { return NP <= 2 ? 5 : 4; }     // of an SM: one round of blocks covers a call, where it can
+constexpr int kMlCache = 2048;            // partial (maximum, sum) pairs that fit in shared memory
+
+template <int NP> struct SlotBatch {
+    static constexpr int kScoreSlots = NP >= 8 ? 2 : 4;
+    float *dst[kScoreSlots];
+    float old[kScoreSlots], x[kScoreSlots][NP];
+
+    __device__ void addresses(const PagedView &pv, const int32_t *table, int h, int jb, int j1)
+    {
+        int page[kScoreSlots];
+#pragma unroll
+        for (int e = 0; e < kScoreSlots; ++e) {
+            const int j = jb + e * kFinishThreads;
+            page[e] = j < j1 ? page_for_write(pv, table, j) : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < kScoreSlots; ++e) {
+            dst[e] = page[e] >= 0 ? pv.scores + pool_row(pv, page[e], h, jb + e * kFinishThreads) : nullptr;
+            old[e] = dst[e] ? *dst[e] : 0.f;
+        }
+    }
+    __device__ void logits(const float *src, int jb)
+    {
+#pragma unroll
+        for (int e = 0; e < kScoreSlots; ++e) {
+            if (!dst[e]) continue;
+            const float *s = src + (size_t)(jb + e * kFinishThreads) * NP;
+            if constexpr (NP == 1) x[e][0] = s[0];
+            else if constexpr (NP == 2) {
+                const float2 v = *reinterpret_cast<const float2 *>(s);
+                x[e][0] = v.x; x[e][1] = v.y;
+            } else {
+#pragma unroll
+                for (int r = 0; r < NP; r += 4) {
+                    const float4 v = *reinterpret_cast<const float4 *>(s + r);
+                    x[e][r] = v.x; x[e][r + 1] = v.y; x[e][r + 2] = v.z; x[e][r + 3] = v.w;
+                }
+            }
+        }
+    }
+    __device__ void store(const float *row_c, float decay)
+    {
+#pragma unroll
+        for (int e = 0; e < kScoreSlots; ++e) {
+            if (!dst[e]) continue;
+            float gain = 0.f;              // rows that do not see the slot, or are none, have -inf there
+#pragma unroll
+            for (int r = 0; r < NP; ++r) gain += ex2(x[e][r] - row_c[r]);
+            *dst[e] = fmaf(old[e], decay, gain);
+        }
+    }
+};
 
 template <typename T, int D, int NP>
-__global__ void __launch_bounds__(kFinishThreads)
+__global__ void __launch_bounds__(kFinishThreads, NP <= 2 ? 5 : 4)
 paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ FewWs ws, int ctas, int blocks, int chunk)
 {
-    constexpr int GR = kFinishThreads / D;
-    __shared__ float red[kFinishThreads], red_l[GR], row_m[kFewRows], row_c[kFewRows];
+    constexpr int GR = kFinishThreads / (D / 4);             // thread groups of an output row, 4 elements a thread
+    __shared__ float4 red[kFinishThreads];
+    __shared__ float row_m[kFewRows], row_l[kFewRows], row_c[kFewRows];
+    __shared__ float2 ml_cache[kMlCache];
     const PagedView &pv = a.pv;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x;
     const int u = blockIdx.x / blocks, y = blockIdx.x - u * blocks, b = u / pv.H, h = u - b * pv.H;
     const SeqState st = seq_state(pv, b);
     const int rows = st.len * pv.G, used = st.past + st.len;
+    const int j0 = y * chunk, j1 = a.scores ? min(used, j0 + chunk) : 0;
+    const int32_t *table = pv.table + (size_t)b * pv.max_pages;
+    SlotBatch<NP> batch;
+    const bool working = rows > 0 && (y < rows || j0 < j1);
+    if (working) batch.addresses(pv, table, h, j0 + tid, j1);
     dependency_wait();
-    const int j0 = y * chunk;
-    if (rows == 0 || (y >= rows && j0 >= used)) return;
+    if (!working) return;
+    const float *logits = ws.logits + (size_t)u * ws.slots * NP;
+    batch.logits(logits, j0 + tid);
     // the CTAs of the main kernel that had a part of this unit
     const long long total = (long long)pv.H * ws.prefix[pv.B], share = (total + ctas - 1) / ctas;
     const int tiles = ws.prefix[b + 1] - ws.prefix[b];
@@ -493,88 +556,76 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
     const int k0 = (int)(u0 / share), k1 = (int)((u0 + tiles - 1) / share);
     const size_t seg0 = ((size_t)k0 + u) * kWarps;
     const int parts = (k1 - k0 + 1) * kWarps;
-    // a row's maximum and its constant: log-sum-exp and the weight's exponent (log2 units)
-    for (int r = warp; r < NP; r += kFinishThreads / 32) {
-        const float2 *ml = ws.ml + seg0 * NP + r;
+    // (maximum, sum) of part p and row r at ml[r * row_step + p * part_step]
+    const float2 *ml = ws.ml + seg0 * NP;
+    int row_step = 1, part_step = NP;
+    if (parts * NP <= kMlCache) {
+        for (int x = tid; x < parts * NP; x += kFinishThreads) ml_cache[x % NP * parts + x / NP] = ml[x];
+        ml = ml_cache;
+        row_step = parts; part_step = 1;
+        __syncthreads();
+    }
+    // a row's maximum, sum, and its constant for the scores: log-sum-exp and the weight's exponent (log2 units)
+    constexpr int LR = NP <= 8 ? 32 : 16;                    // lanes per row: all rows at once
+    if (tid < NP * LR) {
+        const int r = tid / LR, l0 = tid % LR;
+        const float2 *row = ml + r * row_step;
         float mx = -INFINITY, l = 0.f;
-        for (int p = lane; p < parts; p += 32) mx = fmaxf(mx, ml[(size_t)p * NP].x);
-        mx = warp_max(mx);
-        for (int p = lane; p < parts; p += 32) {
-            const float2 x = ml[(size_t)p * NP];
-            l += x.y > 0.f ? exp2f(x.x - mx) * x.y : 0.f;
+        for (int p = l0; p < parts; p += LR) mx = fmaxf(mx, row[p * part_step].x);
+#pragma unroll
+        for (int o = LR / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        for (int p = l0; p < parts; p += LR) {
+            const float2 x = row[p * part_step];
+            l += x.y > 0.f ? ex2(x.x - mx) * x.y : 0.f;
         }
-        l = warp_sum(l);
-        if (lane == 0) {
+#pragma unroll
+        for (int o = LR / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (l0 == 0) {
             row_m[r] = mx;
+            row_l[r] = l;
             row_c[r] = r < rows ? mx + log2f(l) + age_exponent(st.len - 1 - r / pv.G, a.nl2a) : INFINITY;
         }
     }
     __syncthreads();
+    const float decay = exp2f(-age_exponent(st.len, a.nl2a));
+    batch.store(row_c, decay);
+    for (int jb = j0 + SlotBatch<NP>::kScoreSlots * kFinishThreads; jb < j1; jb += SlotBatch<NP>::kScoreSlots * kFinishThreads) {
+        batch.addresses(pv, table, h, jb + tid, j1);
+        batch.logits(logits, jb + tid);
+        batch.store(row_c, decay);
+    }
     for (int r = y; r < rows; r += blocks) {
         // thread groups take every GR-th partial result; joined in a fixed order
-        const float2 *ml = ws.ml + seg0 * NP + r;
-        const float *op = ws.o + (seg0 * NP + r) * D;
-        const int d = tid % D, grp = tid / D;
+        const int d4 = tid % (D / 4), grp = tid / (D / 4);
+        const float4 *op = reinterpret_cast<const float4 *>(ws.o + (seg0 * NP + r) * D) + d4;
+        const float2 *row = ml + r * row_step;
         const float mx = row_m[r];
-        float sum = 0.f, o = 0.f;
-#pragma unroll 8
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
         for (int p = grp; p < parts; p += GR) {
-            const float2 x = ml[(size_t)p * NP];
-            const float f = exp2f(x.x - mx), v = op[(size_t)p * NP * D + d];
-            sum = fmaf(f, x.y, sum);
-            o = fmaf(f, v, o);
+            const float4 v = op[(size_t)p * (NP * D / 4)];
+            const float f = ex2(row[p * part_step].x - mx);
+            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
         }
         __syncthreads();
         red[tid] = o;
-        if (d == 0) red_l[grp] = sum;
         __syncthreads();
         if (grp == 0) {
-            float l = red_l[0];
 #pragma unroll
-            for (int x = 1; x < GR; ++x) { l += red_l[x]; o += red[x * D + d]; }
+            for (int x = 1; x < GR; ++x) {
+                const float4 v = red[x * (D / 4) + d4];
+                o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+            }
             const int i = r / pv.G, g = r - i * pv.G;
-            static_cast<T *>(a.out)[b * a.so.b + (int64_t)(h * pv.G + g) * a.so.h + (int64_t)i * a.so.t + d] = Elem<T>::from_float(o / l);
-            if (d == 0 && a.lse)
+            const float l = row_l[r], inv = 1.f / l;
+            T *dst = static_cast<T *>(a.out) + b * a.so.b + (int64_t)(h * pv.G + g) * a.so.h + (int64_t)i * a.so.t + d4 * 4;
+            dst[0] = Elem<T>::from_float(o.x * inv);
+            dst[1] = Elem<T>::from_float(o.y * inv);
+            dst[2] = Elem<T>::from_float(o.z * inv);
+            dst[3] = Elem<T>::from_float(o.w * inv);
+            if (d4 == 0 && a.lse)
                 a.lse[((size_t)u * pv.G + g) * pv.c + i] = (mx + log2f(l)) * 0.6931471805599453f;
         }
-    }
-    if (!a.scores) return;
-    const float decay = exp2f(-age_exponent(st.len, a.nl2a));
-    const float *logits = ws.logits + (size_t)u * ws.slots * NP;
-    const int32_t *table = pv.table + (size_t)b * pv.max_pages;
-    const int j1 = min(used, j0 + chunk);
-    for (int jb = j0 + tid; jb < j1; jb += kScoreSlots * kFinishThreads) {
-        int page[kScoreSlots];
-        float gain[kScoreSlots], old[kScoreSlots];
-        float *dst[kScoreSlots];
-#pragma unroll
-        for (int x = 0; x < kScoreSlots; ++x) {
-            const int j = jb + x * kFinishThreads;
-            page[x] = j < j1 ? page_for_write(pv, table, j) : -1;
-        }
-#pragma unroll
-        for (int x = 0; x < kScoreSlots; ++x) {
-            const int j = jb + x * kFinishThreads;
-            dst[x] = page[x] >= 0 ? pv.scores + pool_row(pv, page[x], h, j) : nullptr;
-            old[x] = dst[x] ? *dst[x] : 0.f;
-            gain[x] = 0.f;
-            if (j < j1) {
-                // rows that do not see the slot, or are none, have -inf there
-                alignas(16) float v[NP];
-                const float *src = logits + (size_t)j * NP;
-                if constexpr (NP == 1) v[0] = src[0];
-                else if constexpr (NP == 2) *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(src);
-                else {
-#pragma unroll
-                    for (int r = 0; r < NP; r += 4) *reinterpret_cast<float4 *>(v + r) = *reinterpret_cast<const float4 *>(src + r);
-                }
-#pragma unroll
-                for (int r = 0; r < NP; ++r) gain[x] += exp2f(v[r] - row_c[r]);
-            }
-        }
-#pragma unroll
-        for (int x = 0; x < kScoreSlots; ++x)
-            if (dst[x]) *dst[x] = fmaf(old[x], decay, gain[x]);
     }
 }
 
@@ -618,11 +669,11 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     // blocks per unit: enough for the rows and the slots, as far as that fills the device
     const int cap = a.pv.max_pages << a.pv.ps_shift;
     const long long units = (long long)a.pv.B * a.pv.H;
-    const int least = kScoreSlots * kFinishThreads, want = (int)((8ll * device_sm_count() + units - 1) / units);
-    int blocks = (cap + least - 1) / least;
+    const long long want = (long long)finish_ctas(NP) * device_sm_count() / units;
+    int blocks = (cap + kFinishThreads - 1) / kFinishThreads;
     if (blocks < a.pv.c * a.pv.G) blocks = a.pv.c * a.pv.G;
-    if (blocks > want) blocks = want;
-    const int chunk = ((cap + blocks - 1) / blocks + least - 1) / least * least;
+    if (blocks > want) blocks = want > 0 ? (int)want : 1;
+    const int chunk = ((cap + blocks - 1) / blocks + 31) / 32 * 32;
     const long long grid = units * blocks;
     if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
     auto finish = [&](auto kernel) { return launch_follower(kernel, (unsigned)grid, kFinishThreads, 0, s, a, ws, ctas, blocks, chunk); };

@@ -22,10 +22,16 @@ static __device__ int g_paged_status = 0;
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kHeads = 4;        // heads in flight per thread
+constexpr int kHeads = 2;        // heads in flight per thread: with four blocks an SM, 128 KB on the way
 
 // W consecutive elements of 16- or 32-bit storage, moved as one access of up to 16 bytes
 template <typename T, int W> struct alignas(sizeof(T) * W) Pack { T e[W]; };
+
+template <typename P> __device__ __forceinline__ void store_pack(void *dst, const P &v)
+{
+    if constexpr (sizeof(P) == 16) __stcs(reinterpret_cast<uint4 *>(dst), *reinterpret_cast<const uint4 *>(&v));
+    else                           *reinterpret_cast<P *>(dst) = v;
+}
 
 struct PlanArg {
     unsigned long long turn[A2SF_ROTARY_MAX_PAIRS];
@@ -34,7 +40,7 @@ struct PlanArg {
 // One thread item of a row: W elements at `a`, and in the split layout W more at `b`.
 // Items 0 .. rot_items-1 rotate, the following ones copy W elements each.
 template <typename T, int W, bool Interleaved, bool Append>
-__global__ void __launch_bounds__(kRotThreads)
+__global__ void __launch_bounds__(kRotThreads, 4)
 rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ RotaryArgs r,
               const __grid_constant__ PagedView pv, int r_dim, float magnitude, int rot_items, int items,
               int heads_per_block)
@@ -130,8 +136,8 @@ rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ Rota
                     else             { va[x].e[e] = y1; vb[x].e[e] = y2; }
                 }
             }
-            *reinterpret_cast<P *>(dst[x] + a_off) = va[x];
-            if (!Interleaved && rotates) *reinterpret_cast<P *>(dst[x] + b_off) = vb[x];
+            store_pack(dst[x] + a_off, va[x]);
+            if (!Interleaved && rotates) store_pack(dst[x] + b_off, vb[x]);
         }
     }
 }
@@ -152,7 +158,7 @@ cudaError_t launch_w(const a2sf_rotary_plan *plan, const RotaryArgs &r, const Pa
     if (gx > 0x7fffffffll) return cudaErrorInvalidValue;
     // the heads are split over blocks only as far as it takes to fill the device, a batch of kHeads at least
     const int total = r.Hq + (Append ? 2 * r.Hk : 0);
-    const long long want = 32ll * device_sm_count();
+    const long long want = 16ll * device_sm_count();
     const long long gy = (want + gx - 1) / gx;
     const int hpb = (int)(((total + gy - 1) / gy + kHeads - 1) / kHeads) * kHeads;
     const dim3 grid((unsigned)gx, (unsigned)((total + hpb - 1) / hpb));
