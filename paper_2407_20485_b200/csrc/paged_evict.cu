@@ -1,14 +1,16 @@
 // Back to the budget: which slots of a head stay, and the rows that have to move for it.
 //
-//   select  one CTA per (sequence, K/V head).  Of n slots, n - M leave: those with the smallest
-//           (score, position) among the slots outside the recent window.  A radix select over the 32
-//           ordered score bits (8 at a time) finds the score at which the cut falls, a second one over
-//           the positions decides among slots of exactly that score -- there are many when alpha = 0
-//           or a chunk was just appended -- and a scan in slot order lists the moves.  Integer work:
-//           exact, and the same on every run.
-//   move    grid-wide copies of the listed rows (K, V, score, position).
-// In place only the survivors above M move, into the holes below M: at most min(M, n - M) rows.
-// Bound by memory: 8 bytes per slot for the decision, two rows read and written per move.
+// One CTA per (sequence, K/V head).  Of n slots, n - M leave: the smallest under (score, position, slot) among
+// those outside the recent window.  A radix search narrows the score at which the cut falls, 8 bits at a
+// time, and then the position -- many scores are equal when alpha = 0 or a chunk was just appended -- until at
+// most kShort slots are left to decide about; those are ranked directly.  Usually two digits do.  The survivors
+// become a bit mask, and a scan over it in slot order lists the moves: integer work, exact, the same on
+// every run.  In place only the survivors above M move, into the holes below M: at most min(M, n - M) rows.
+//
+// Bound by memory -- 8 bytes per slot for the decision, two rows read and written per move -- where there are many
+// heads: then a CTA moves its own rows, and one CTA's search hides behind the others' copies.  Where there are
+// few, long moves are left to a kernel that spreads them over the whole device.  past and start change in the
+// last kernel only: past_out may be past, which every CTA reads.
 #include "paged.cuh"
 
 namespace a2sf {
@@ -17,9 +19,13 @@ A2SF_DEBUG_TRANSLATION_UNIT(paged_evict)
 
 namespace {
 
-constexpr int kSelThreads = 512;
+constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kCached = 16384;       // slots whose (score key, position) fit in shared memory
+constexpr int kMaskWords = 1024;     // survivors' mask: 32768 slots; beyond, it is worked out again where it is needed
+constexpr int kShort = 64;           // slots that are ranked directly
+constexpr int kInline = 64;          // moves that the searching CTA makes itself in any case
+constexpr int kRows = 4;             // rows of a lane group in flight
 
 struct EvictArgs {
     PagedView pv;
@@ -30,7 +36,7 @@ struct EvictArgs {
     int32_t *from, *to;              // [U][M] slot lists (to: in place only)
     int32_t *moves;                  // [U]
     int32_t *ends;                   // [B][2] new past, new start
-    int blocks;                      // of the move kernel, per unit
+    int blocks;                      // of the move kernel, per unit; 0: every CTA moves its own rows
 };
 
 // Order-preserving key of a score; every NaN sorts last, -0 like +0.
@@ -43,9 +49,14 @@ __device__ __forceinline__ unsigned score_key(float s)
 
 struct SelShared {
     int hist[256];
-    int warp_tot[3][kSelWarps + 1];
+    int warp_tot[2][kSelWarps + 1];
     unsigned prefix;
-    int rank, equal, ncand;
+    int rank, equal, total, count;
+    unsigned list_key[kShort], list_pos[kShort];
+    int list_slot[kShort];
+    unsigned thr_key, thr_pos;
+    int thr_slot;
+    unsigned mask[kMaskWords];
 };
 
 // Exclusive scan of one int per warp (lane 0 holds it) over the CTA's warps, for `which`.
@@ -54,22 +65,60 @@ __device__ __forceinline__ int warps_excl_scan(SelShared &sh, int which, int v, 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (lane == 0) sh.warp_tot[which][warp] = v;
     __syncthreads();
-    if (warp == which) {
-        const int t = lane < kSelWarps ? sh.warp_tot[which][lane] : 0;
-        int ti = t;
+    int before = 0;
+    total = 0;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, ti, o);
-            if (lane >= o) ti += x;
-        }
-        if (lane < kSelWarps) sh.warp_tot[which][lane] = ti - t;
-        if (lane == 31) sh.warp_tot[which][kSelWarps] = ti;
+    for (int w = 0; w < kSelWarps; ++w) {
+        const int t = sh.warp_tot[which][w];
+        before += w < warp ? t : 0;
+        total += t;
     }
-    __syncthreads();
-    total = sh.warp_tot[which][kSelWarps];
-    return sh.warp_tot[which][warp];
+    return before;
 }
 
+// Rows k0, k0 + step, .. of a unit's list; a group of ROW_BYTES / 16 lanes copies one row of K and of V.
+template <int ROW_BYTES>
+__device__ __forceinline__ void move_rows(const EvictArgs &a, int u, int b, int h, int moves, int group, int groups)
+{
+    constexpr int LPR = ROW_BYTES / 16;
+    const int part = threadIdx.x % LPR;
+    const bool fresh = a.dst_table != nullptr;
+    const int32_t *from_row = a.pv.table + (size_t)b * a.pv.max_pages;
+    const int32_t *to_row = fresh ? a.dst_table + (size_t)b * a.dst_max_pages : from_row;
+    // kRows rows in flight: a move is a chain of three loads (list, page, row)
+    for (int k0 = group; k0 < moves; k0 += groups * kRows) {
+        int64_t s[kRows], t[kRows];
+        uint4 kv[kRows], vv[kRows];
+        float sc[kRows];
+        int32_t ps[kRows];
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            const int k = k0 + x * groups;
+            t[x] = -1;
+            if (k >= moves) continue;
+            const int src = a.from[(size_t)u * a.M + k], dst = fresh ? k : a.to[(size_t)u * a.M + k];
+            const int to_page = page_for_write(a.pv, to_row, dst);
+            s[x] = pool_row(a.pv, page_for_read(a.pv, from_row, src), h, src);
+            if (to_page >= 0) t[x] = pool_row(a.pv, to_page, h, dst);
+        }
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            if (t[x] < 0) continue;
+            kv[x] = ld_stream16_rw(a.pv.k + s[x] * ROW_BYTES + part * 16);
+            vv[x] = ld_stream16_rw(a.pv.v + s[x] * ROW_BYTES + part * 16);
+            if (part == 0) { sc[x] = a.pv.scores[s[x]]; ps[x] = a.pv.positions[s[x]]; }
+        }
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            if (t[x] < 0) continue;
+            __stcs(reinterpret_cast<uint4 *>(a.pv.k + t[x] * ROW_BYTES + part * 16), kv[x]);
+            __stcs(reinterpret_cast<uint4 *>(a.pv.v + t[x] * ROW_BYTES + part * 16), vv[x]);
+            if (part == 0) { a.pv.scores[t[x]] = sc[x]; a.pv.positions[t[x]] = ps[x]; }
+        }
+    }
+}
+
+template <int ROW_BYTES>
 __global__ void __launch_bounds__(kSelThreads, 4)
 paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
 {
@@ -90,196 +139,176 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
     const bool fresh = a.dst_table != nullptr;
     const int drop = n - M;
     int32_t *from = a.from + (size_t)u * M, *to = a.to + (size_t)u * M;
-    if (drop <= 0) {
-        if (fresh)
-            for (int j = tid; j < n; j += kSelThreads) from[j] = j;
-        if (tid == 0) a.moves[u] = fresh ? n : 0;
-        return;
-    }
-    auto fetch = [&](int j) -> uint2 {
-        const int64_t row = pool_row(a.pv, page_for_read(a.pv, table, j), h, j);
-        return make_uint2(score_key(a.pv.scores[row]), (unsigned)a.pv.positions[row]);
-    };
+    int moves = fresh ? min(n, M) : 0;
+    if (drop > 0) {
+        auto fetch = [&](int j) -> uint2 {
+            const int64_t row = pool_row(a.pv, page_for_read(a.pv, table, j), h, j);
+            return make_uint2(score_key(a.pv.scores[row]), (unsigned)a.pv.positions[row]);
+        };
 #pragma unroll 4
-    for (int j = tid; j < min(n, cached); j += kSelThreads) cache[j] = fetch(j);
-    auto item = [&](int j) -> uint2 { return j < cached ? cache[j] : fetch(j); };
-    auto recent = [&](const uint2 &x) { return (long long)(int)x.y >= newest; };
-    if (tid == 0) sh.ncand = 0;
-    __syncthreads();
-    int mine = 0;
-    for (int j = tid; j < n; j += kSelThreads) mine += recent(item(j)) ? 0 : 1;
-    mine = __reduce_add_sync(0xffffffffu, mine);
-    if (lane == 0) atomicAdd(&sh.ncand, mine);
-    __syncthreads();
-    // Slots leave from among those outside the window.  Positions given twice can make the window
-    // hold more than the budget; then all others leave and the window is ranked itself.
-    const bool from_recent = sh.ncand < drop;
-    auto candidate = [&](const uint2 &x) { return recent(x) == from_recent; };
-    int rank = from_recent ? drop - sh.ncand : drop;    // 1-based rank of the last one to leave
-    // digits 0-3: the score; 4-7: the position, among slots of the threshold score
-    unsigned thr_key = 0, thr_pos = 0;
-    bool pos_needed = true;
-    for (int digit = 0; digit < 8 && pos_needed; ++digit) {
-        const int shift = 24 - 8 * (digit & 3);
-        const unsigned above = (digit & 3) == 0 ? 0u : 0xffffffffu << (shift + 8);
-        if (tid < 256) sh.hist[tid] = 0;
-        __syncthreads();
+        for (int j = tid; j < min(n, cached); j += kSelThreads) cache[j] = fetch(j);
+        auto item = [&](int j) -> uint2 { return j < cached ? cache[j] : fetch(j); };
+        auto recent = [&](const uint2 &x) { return (long long)(int)x.y >= newest; };
+        // Slots leave from among those outside the window.  Positions given twice can make the window
+        // hold more than the budget; then all others leave and the window is ranked itself.
+        bool from_recent = false;
+        auto candidate = [&](const uint2 &x) { return recent(x) == from_recent; };
+        // digit 0-3: score, 4-7: position (signed), 8-11: slot
+        auto word = [&](int digit, const uint2 &x, int j) -> unsigned { return digit < 4 ? x.x : digit < 8 ? x.y ^ 0x80000000u : (unsigned)j; };
+        unsigned thr[3] = {0u, 0u, 0u};
+        // whether x agrees with the threshold in all digits before `digit`
+        auto agrees = [&](int digit, const uint2 &x, int j) {
+            const int part = digit & 3;
+            const unsigned above = part == 0 ? 0u : 0xffffffffu << (32 - 8 * part);
+            if (digit >= 4 && x.x != thr[0]) return false;
+            if (digit >= 8 && (x.y ^ 0x80000000u) != thr[1]) return false;
+            return ((word(digit, x, j) ^ (digit < 4 ? thr[0] : digit < 8 ? thr[1] : thr[2])) & above) == 0u;
+        };
+        int rank = drop, digit = 0;                      // 1-based rank of the last one to leave
+        for (;;) {
+            const int shift = 24 - 8 * (digit & 3);
+            sh.hist[tid] = 0;
+            if (tid == 0) sh.count = 0;
+            __syncthreads();
+            for (int j = tid; j < n; j += kSelThreads) {
+                const uint2 x = item(j);
+                if (candidate(x) && agrees(digit, x, j)) atomicAdd(&sh.hist[(word(digit, x, j) >> shift) & 255u], 1);
+            }
+            __syncthreads();
+            if (warp == 0) {                             // 8 bins a lane, then the lane that holds the rank
+                int c[8], sum = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { c[e] = sh.hist[lane * 8 + e]; sum += c[e]; }
+                int incl = sum;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int x = __shfl_up_sync(0xffffffffu, incl, o);
+                    if (lane >= o) incl += x;
+                }
+                int before = incl - sum;
+                if (before < rank && rank <= incl) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (before < rank && rank <= before + c[e]) {
+                            sh.prefix = (unsigned)(lane * 8 + e) << shift;
+                            sh.rank = rank - before;
+                            sh.equal = c[e];
+                        }
+                        before += c[e];
+                    }
+                }
+                if (lane == 31) sh.total = incl;
+            }
+            __syncthreads();
+            if (digit == 0 && !from_recent && sh.total < drop) {
+                from_recent = true;
+                rank = drop - sh.total;
+                continue;                                // the histogram is cleared before anyone adds: two barriers away
+            }
+            thr[digit >> 2] |= sh.prefix;
+            rank = sh.rank;
+            ++digit;
+            if (sh.equal <= kShort) break;               // digits 0-11 tell all slots apart
+            __syncthreads();
+        }
+        // the slots that agree so far, ranked by (score, position, slot)
+        const int m = sh.equal;
+        auto agrees_all = [&](const uint2 &x, int j) {   // `digit` digits are decided; 12 of them: everything
+            return digit < 12 ? agrees(digit, x, j) : x.x == thr[0] && (x.y ^ 0x80000000u) == thr[1] && (unsigned)j == thr[2];
+        };
         for (int j = tid; j < n; j += kSelThreads) {
             const uint2 x = item(j);
-            if (!candidate(x)) continue;
-            const unsigned v = digit < 4 ? x.x : x.y ^ 0x80000000u;      // positions are signed
-            const unsigned thr = digit < 4 ? thr_key : thr_pos;
-            if (digit >= 4 && x.x != thr_key) continue;
-            if ((v & above) == (thr & above)) atomicAdd(&sh.hist[(v >> shift) & 255u], 1);
-        }
-        __syncthreads();
-        if (warp == 0) {                                 // 8 bins a lane, then the lane that holds the rank
-            int c[8], sum = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { c[e] = sh.hist[lane * 8 + e]; sum += c[e]; }
-            int incl = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int x = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += x;
-            }
-            int before = incl - sum;
-            if (before < rank && rank <= incl) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (before < rank && rank <= before + c[e]) {
-                        sh.prefix = (unsigned)(lane * 8 + e) << shift;
-                        sh.rank = rank - before;
-                        sh.equal = c[e];
-                        break;
-                    }
-                    before += c[e];
-                }
+            if (candidate(x) && agrees_all(x, j)) {
+                const int k = atomicAdd(&sh.count, 1);
+                if (k < kShort) { sh.list_key[k] = x.x; sh.list_pos[k] = x.y ^ 0x80000000u; sh.list_slot[k] = j; }
             }
         }
         __syncthreads();
-        if (digit < 4) thr_key |= sh.prefix;
-        else           thr_pos |= sh.prefix;
-        rank = sh.rank;
-        if (digit == 3) pos_needed = sh.equal != rank;   // all slots of that score leave: no second key
-    }
-    // leaves: candidates below (thr_key, thr_pos), and the first `rank` of those equal to it
-    auto below = [&](const uint2 &x) {
-        return candidate(x) && (x.x < thr_key || (pos_needed && x.x == thr_key && (x.y ^ 0x80000000u) < thr_pos));
-    };
-    auto equal = [&](const uint2 &x) {
-        return candidate(x) && x.x == thr_key && (!pos_needed || (x.y ^ 0x80000000u) == thr_pos);
-    };
-    auto drops = [&](const uint2 &x) { return below(x) || (from_recent && !recent(x)); };
-    // every warp takes a contiguous range of slots, 32 at a time: count, scan over the warps, list
-    const int per = ((n + kSelWarps - 1) / kSelWarps + 31) / 32 * 32;
-    const int w0 = min(n, warp * per), w1 = min(n, w0 + per);
-    int eq_cnt = 0, total;
-    for (int j0 = w0; j0 < w1; j0 += 32) {
-        const int j = j0 + lane;
-        eq_cnt += __popc(__ballot_sync(0xffffffffu, j < w1 && equal(item(j))));
-    }
-    const int eq0 = warps_excl_scan(sh, 0, eq_cnt, total);
-    int eq = eq0, stay_lo = 0, stay_hi = 0;              // survivors below / from slot M on
-    const unsigned lt = (1u << lane) - 1u;
-    auto stays = [&](int j, int &eq_run) {
-        bool in = j < w1, is_eq = false, s = false;
-        if (in) {
+        if (tid < m) {
+            const unsigned k = sh.list_key[tid], p = sh.list_pos[tid];
+            const int s = sh.list_slot[tid];
+            int less = 0;
+            for (int x = 0; x < m; ++x) {
+                const unsigned k2 = sh.list_key[x], p2 = sh.list_pos[x];
+                less += k2 < k || (k2 == k && (p2 < p || (p2 == p && sh.list_slot[x] < s)));
+            }
+            if (less == rank - 1) { sh.thr_key = k; sh.thr_pos = p; sh.thr_slot = s; }
+        }
+        __syncthreads();
+        const unsigned tk = sh.thr_key, tp = sh.thr_pos;
+        const int ts = sh.thr_slot;
+        auto stays = [&](int j) {
             const uint2 x = item(j);
-            is_eq = equal(x);
-            s = !drops(x);
-        }
-        const unsigned eqs = __ballot_sync(0xffffffffu, is_eq);
-        if (is_eq) s = eq_run + __popc(eqs & lt) >= rank;
-        eq_run += __popc(eqs);
-        return __ballot_sync(0xffffffffu, s);
-    };
-    for (int j0 = w0; j0 < w1; j0 += 32) {
-        const unsigned s = stays(j0 + lane, eq);
-        const unsigned lo = j0 + 32 <= M ? 0xffffffffu : j0 >= M ? 0u : (1u << (M - j0)) - 1u;
-        stay_lo += __popc(s & lo);
-        stay_hi += __popc(s & ~lo);
-    }
-    int total_hi;
-    const int lo0 = warps_excl_scan(sh, 1, stay_lo, total);
-    const int hi0 = warps_excl_scan(sh, 2, stay_hi, total_hi);
-    eq = eq0;
-    if (fresh) {
-        int at = lo0 + hi0;
+            if (!candidate(x)) return !from_recent;
+            const unsigned p = x.y ^ 0x80000000u;
+            return !(x.x < tk || (x.x == tk && (p < tp || (p == tp && j <= ts))));
+        };
+        // every warp takes a contiguous range of slots, 32 at a time: mask and counts, scan over the warps, list
+        const int per = ((n + kSelWarps - 1) / kSelWarps + 31) / 32 * 32;
+        const int w0 = min(n, warp * per), w1 = min(n, w0 + per);
+        auto low = [&](int j0) { return j0 + 32 <= M ? 0xffffffffu : j0 >= M ? 0u : (1u << (M - j0)) - 1u; };
+        int stay_lo = 0, stay_hi = 0;                    // survivors below / from slot M on
         for (int j0 = w0; j0 < w1; j0 += 32) {
-            const unsigned s = stays(j0 + lane, eq);
-            const int k = at + __popc(s & lt);
-            if ((s >> lane & 1) && k < M) from[k] = j0 + lane;
-            at += __popc(s);
+            const unsigned s = __ballot_sync(0xffffffffu, j0 + lane < w1 && stays(j0 + lane));
+            if (lane == 0 && j0 / 32 < kMaskWords) sh.mask[j0 / 32] = s;
+            stay_lo += __popc(s & low(j0));
+            stay_hi += __popc(s & ~low(j0));
         }
-        if (tid == 0) a.moves[u] = M;
-    } else {
-        int hole = min(w0, M) - lo0, src = hi0;          // holes and survivors before this warp's range
-        for (int j0 = w0; j0 < w1; j0 += 32) {
-            const unsigned s = stays(j0 + lane, eq);
-            const unsigned in = j0 + 32 <= w1 ? 0xffffffffu : (1u << (w1 - j0)) - 1u;
-            const unsigned lo = j0 + 32 <= M ? 0xffffffffu : j0 >= M ? 0u : (1u << (M - j0)) - 1u;
-            const unsigned holes = in & lo & ~s, ups = s & ~lo;
-            const int kh = hole + __popc(holes & lt), ks = src + __popc(ups & lt);
-            if ((holes >> lane & 1) && kh < M) to[kh] = j0 + lane;
-            if ((ups >> lane & 1) && ks < M) from[ks] = j0 + lane;
-            hole += __popc(holes);
-            src += __popc(ups);
+        int total_lo, total_hi;
+        const int lo0 = warps_excl_scan(sh, 0, stay_lo, total_lo), hi0 = warps_excl_scan(sh, 1, stay_hi, total_hi);
+        auto mask_of = [&](int j0) -> unsigned {
+            return j0 / 32 < kMaskWords ? sh.mask[j0 / 32] : __ballot_sync(0xffffffffu, j0 + lane < w1 && stays(j0 + lane));
+        };
+        const unsigned lt = (1u << lane) - 1u;
+        if (fresh) {
+            int at = lo0 + hi0;
+            for (int j0 = w0; j0 < w1; j0 += 32) {
+                const unsigned s = mask_of(j0);
+                const int k = at + __popc(s & lt);
+                if ((s >> lane & 1) && k < M) from[k] = j0 + lane;
+                at += __popc(s);
+            }
+        } else {
+            int hole = min(w0, M) - lo0, src = hi0;      // holes and survivors before this warp's range
+            for (int j0 = w0; j0 < w1; j0 += 32) {
+                const unsigned s = mask_of(j0);
+                const unsigned in = j0 + 32 <= w1 ? 0xffffffffu : (1u << (w1 - j0)) - 1u;
+                const unsigned lo = low(j0), holes = in & lo & ~s, ups = s & ~lo;
+                const int kh = hole + __popc(holes & lt), ks = src + __popc(ups & lt);
+                if ((holes >> lane & 1) && kh < M) to[kh] = j0 + lane;
+                if ((ups >> lane & 1) && ks < M) from[ks] = j0 + lane;
+                hole += __popc(holes);
+                src += __popc(ups);
+            }
+            moves = total_hi;
         }
-        if (tid == 0) a.moves[u] = total_hi;
+    } else if (fresh) {
+        for (int j = tid; j < n; j += kSelThreads) from[j] = j;
     }
+    const bool here = a.blocks == 0 || moves <= kInline;
+    if (tid == 0) a.moves[u] = here ? 0 : moves;
+    if (!here) return;
+    __syncthreads();                                     // the lists, written by this CTA
+    constexpr int LPR = ROW_BYTES / 16;
+    move_rows<ROW_BYTES>(a, u, b, h, moves, tid / LPR, kSelThreads / LPR);
 }
 
 constexpr int kMoveThreads = 256;
-constexpr int kRows = 4;             // rows of a lane group in flight
 
-// A group of ROW_BYTES / 16 lanes copies one row of K and of V.
+// Long moves of few heads, and the new lengths.
 template <int ROW_BYTES>
 __global__ void __launch_bounds__(kMoveThreads)
 paged_move_kernel(const __grid_constant__ EvictArgs a)
 {
-    constexpr int LPR = ROW_BYTES / 16, RPB = kMoveThreads / LPR;
-    const int u = blockIdx.x / a.blocks, by = blockIdx.x - u * a.blocks, b = u / a.pv.H, h = u - b * a.pv.H;
     dependency_wait();
-    if (h == 0 && by == 0 && threadIdx.x == 0) {
+    for (int b = blockIdx.x * kMoveThreads + threadIdx.x; b < a.pv.B; b += gridDim.x * kMoveThreads) {
         a.past_out[b] = a.ends[2 * b];
         a.start_out[b] = a.ends[2 * b + 1];
     }
-    const int moves = a.moves[u], part = threadIdx.x % LPR;
-    const bool fresh = a.dst_table != nullptr;
-    const int32_t *from_row = a.pv.table + (size_t)b * a.pv.max_pages;
-    const int32_t *to_row = fresh ? a.dst_table + (size_t)b * a.dst_max_pages : from_row;
-    // kRows rows of a lane group in flight: a move is a chain of three loads (list, page, row)
-    for (int k0 = by * RPB * kRows + threadIdx.x / LPR; k0 < moves; k0 += a.blocks * RPB * kRows) {
-        int64_t s[kRows], t[kRows];
-        uint4 kv[kRows], vv[kRows];
-        float sc[kRows];
-        int32_t ps[kRows];
-#pragma unroll
-        for (int x = 0; x < kRows; ++x) {
-            const int k = k0 + x * RPB;
-            t[x] = -1;
-            if (k >= moves) continue;
-            const int src = a.from[(size_t)u * a.M + k], dst = fresh ? k : a.to[(size_t)u * a.M + k];
-            const int to_page = page_for_write(a.pv, to_row, dst);
-            s[x] = pool_row(a.pv, page_for_read(a.pv, from_row, src), h, src);
-            if (to_page >= 0) t[x] = pool_row(a.pv, to_page, h, dst);
-        }
-#pragma unroll
-        for (int x = 0; x < kRows; ++x) {
-            if (t[x] < 0) continue;
-            kv[x] = ld_stream16_rw(a.pv.k + s[x] * ROW_BYTES + part * 16);
-            vv[x] = ld_stream16_rw(a.pv.v + s[x] * ROW_BYTES + part * 16);
-            if (part == 0) { sc[x] = a.pv.scores[s[x]]; ps[x] = a.pv.positions[s[x]]; }
-        }
-#pragma unroll
-        for (int x = 0; x < kRows; ++x) {
-            if (t[x] < 0) continue;
-            *reinterpret_cast<uint4 *>(a.pv.k + t[x] * ROW_BYTES + part * 16) = kv[x];
-            *reinterpret_cast<uint4 *>(a.pv.v + t[x] * ROW_BYTES + part * 16) = vv[x];
-            if (part == 0) { a.pv.scores[t[x]] = sc[x]; a.pv.positions[t[x]] = ps[x]; }
-        }
-    }
+    if (a.blocks == 0) return;
+    constexpr int LPR = ROW_BYTES / 16, RPB = kMoveThreads / LPR;
+    const int u = blockIdx.x / a.blocks, y = blockIdx.x - u * a.blocks, b = u / a.pv.H, h = u - b * a.pv.H;
+    move_rows<ROW_BYTES>(a, u, b, h, a.moves[u], y * RPB + threadIdx.x / LPR, a.blocks * RPB);
 }
 
 size_t pad(size_t x) { return (x + 255) / 256 * 256; }
@@ -299,7 +328,6 @@ cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int re
     a.pv = pv; a.M = budget; a.R = recent;
     a.dst_table = dst_table; a.dst_max_pages = dst_max_pages;
     a.past_out = past_out; a.start_out = start_out;
-    a.blocks = 1;
     char *w = static_cast<char *>(ws);
     a.from = reinterpret_cast<int32_t *>(w); w += pad(units * (size_t)budget * 4);
     a.to = reinterpret_cast<int32_t *>(w); w += pad(units * (size_t)budget * 4);
@@ -307,25 +335,37 @@ cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int re
     a.ends = reinterpret_cast<int32_t *>(w);
     const int cap = pv.max_pages << pv.ps_shift;
     const int cached = cap < kCached ? cap : kCached;
-    cudaError_t e = allow_dynamic_smem<paged_select_kernel>((size_t)cached * 8);
-    if (e != cudaSuccess) return e;
-    paged_select_kernel<<<(unsigned)units, kSelThreads, (size_t)cached * 8, s>>>(a, cached);
-    count_launch();
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    const size_t smem = (size_t)cached * 8;
     const int row_bytes = pv.d * elem_bytes, rpb = kMoveThreads / (row_bytes / 16);
-    const int most = budget < cap ? budget : cap;
-    long long blocks = (most + rpb * kRows - 1) / (rpb * kRows);
-    const long long want = (16ll * device_sm_count() + (long long)units - 1) / (long long)units;
-    if (blocks > want) blocks = want;
-    a.blocks = (int)blocks;
-    const unsigned grid = (unsigned)(units * blocks);
-    switch (row_bytes) {
-    case 128: e = launch_follower(paged_move_kernel<128>, grid, kMoveThreads, 0, s, a); break;
-    case 256: e = launch_follower(paged_move_kernel<256>, grid, kMoveThreads, 0, s, a); break;
-    default: e = launch_follower(paged_move_kernel<512>, grid, kMoveThreads, 0, s, a); break;
+    // from two CTAs per SM on the heads fill the device with their own copies
+    long long blocks = 0;
+    if (units < 2 * (size_t)device_sm_count()) {
+        blocks = ((budget < cap ? budget : cap) + rpb * kRows - 1) / (rpb * kRows);
+        const long long want = (16ll * device_sm_count() + (long long)units - 1) / (long long)units;
+        if (blocks > want) blocks = want;
     }
-    if (e == cudaSuccess) count_launch();
-    return e;
+    a.blocks = (int)blocks;
+    const unsigned grid = blocks ? (unsigned)(units * blocks) : 1u;
+    auto run = [&](auto select, auto move) -> cudaError_t {
+        select<<<(unsigned)units, kSelThreads, smem, s>>>(a, cached);
+        count_launch();
+        cudaError_t e = cudaGetLastError();
+        if (e == cudaSuccess) e = launch_follower(move, grid, kMoveThreads, 0, s, a);
+        if (e == cudaSuccess) count_launch();
+        return e;
+    };
+    cudaError_t e;
+    switch (row_bytes) {
+    case 128:
+        if ((e = allow_dynamic_smem<paged_select_kernel<128>>(smem)) != cudaSuccess) return e;
+        return run(paged_select_kernel<128>, paged_move_kernel<128>);
+    case 256:
+        if ((e = allow_dynamic_smem<paged_select_kernel<256>>(smem)) != cudaSuccess) return e;
+        return run(paged_select_kernel<256>, paged_move_kernel<256>);
+    default:
+        if ((e = allow_dynamic_smem<paged_select_kernel<512>>(smem)) != cudaSuccess) return e;
+        return run(paged_select_kernel<512>, paged_move_kernel<512>);
+    }
 }
 
 }  // namespace a2sf
