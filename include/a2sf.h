@@ -435,8 +435,8 @@ typedef struct a2sf_paged {
     float scale;                 /* of the logits; 0 selects 1/sqrt(d) */
     int32_t reserved;            /* 0 */
     void *k_pages, *v_pages;     /* [num_pages][H][page_size][d], 16-byte aligned */
-    float *scores;               /* [num_pages][H][page_size] */
-    int32_t *positions;          /* [num_pages][H][page_size] */
+    float *scores;               /* [num_pages][H][page_size], 16-byte aligned */
+    int32_t *positions;          /* [num_pages][H][page_size], 16-byte aligned */
     const int32_t *page_table;   /* [B][max_pages] */
     const int32_t *past;         /* [B] slots in use before the chunk */
     const int32_t *start;        /* [B] or NULL */

@@ -53,7 +53,7 @@ int check_paged(const a2sf_paged *p, int c)
         (int64_t)p->B * p->H * p->group > (1 << 24) || (int64_t)p->num_pages * p->H * p->page_size >= (1ll << 31))
         return A2SF_ERR_UNSUPPORTED;
     if (!p->k_pages || !p->v_pages || !p->scores || !p->positions || !p->page_table || !p->past) return A2SF_ERR_INVALID_ARG;
-    if (!aligned(p->k_pages, 16) || !aligned(p->v_pages, 16) || !aligned(p->scores, 4) || !aligned(p->positions, 4) ||
+    if (!aligned(p->k_pages, 16) || !aligned(p->v_pages, 16) || !aligned(p->scores, 16) || !aligned(p->positions, 16) ||
         !aligned(p->page_table, 4) || !aligned(p->past, 4) || !aligned(p->start, 4))
         return A2SF_ERR_INVALID_ARG;
     return A2SF_OK;

@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
-constexpr int kCached = 16384;       // slots whose (score key, position) fit in shared memory
+constexpr int kCached = 16384;       // slots whose score key and position fit in shared memory
 constexpr int kMaskWords = 1024;     // survivors' mask: 32768 slots; beyond, it is worked out again where it is needed
 constexpr int kShort = 64;           // slots that are ranked directly
 constexpr int kInline = 64;          // moves that the searching CTA makes itself in any case
@@ -39,12 +39,14 @@ struct EvictArgs {
     int blocks;                      // of the move kernel, per unit; 0: every CTA moves its own rows
 };
 
-// Order-preserving key of a score; every NaN sorts last, -0 like +0.
+// Order-preserving key of a score, -0 like +0, every NaN behind infinity; kNoKey stands for a slot that is no
+// candidate (inside the recent window, or behind the last one).
+constexpr unsigned kNoKey = 0xffffffffu;
 __device__ __forceinline__ unsigned score_key(float s)
 {
-    if (s != s) return 0xffffffffu;
     const unsigned bits = __float_as_uint(s + 0.f);
-    return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+    const unsigned key = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+    return s != s ? 0xfffffffeu : key;
 }
 
 struct SelShared {
@@ -119,10 +121,10 @@ __device__ __forceinline__ void move_rows(const EvictArgs &a, int u, int b, int 
 }
 
 template <int ROW_BYTES>
-__global__ void __launch_bounds__(kSelThreads, 4)
+__global__ void __launch_bounds__(kSelThreads, 3)
 paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
 {
-    extern __shared__ __align__(8) uint2 cache[];       // [cached] (key, position)
+    extern __shared__ __align__(16) unsigned cache[];   // [cached] keys, [cached] positions
     __shared__ SelShared sh;
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = u / a.pv.H, h = u - b * a.pv.H;
@@ -141,28 +143,54 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
     int32_t *from = a.from + (size_t)u * M, *to = a.to + (size_t)u * M;
     int moves = fresh ? min(n, M) : 0;
     if (drop > 0) {
-        auto fetch = [&](int j) -> uint2 {
-            const int64_t row = pool_row(a.pv, page_for_read(a.pv, table, j), h, j);
-            return make_uint2(score_key(a.pv.scores[row]), (unsigned)a.pv.positions[row]);
-        };
-#pragma unroll 4
-        for (int j = tid; j < min(n, cached); j += kSelThreads) cache[j] = fetch(j);
-        auto item = [&](int j) -> uint2 { return j < cached ? cache[j] : fetch(j); };
-        auto recent = [&](const uint2 &x) { return (long long)(int)x.y >= newest; };
+        unsigned *keys = cache;
+        int32_t *poss = reinterpret_cast<int32_t *>(cache + cached);
         // Slots leave from among those outside the window.  Positions given twice can make the window
         // hold more than the budget; then all others leave and the window is ranked itself.
         bool from_recent = false;
-        auto candidate = [&](const uint2 &x) { return recent(x) == from_recent; };
-        // digit 0-3: score, 4-7: position (signed), 8-11: slot
-        auto word = [&](int digit, const uint2 &x, int j) -> unsigned { return digit < 4 ? x.x : digit < 8 ? x.y ^ 0x80000000u : (unsigned)j; };
+        // four slots j .. j+3 (j a multiple of 4: they share a page)
+        auto fetch = [&](int j, uint4 &k, int4 &p) {
+            const int64_t row = pool_row(a.pv, page_for_read(a.pv, table, j), h, j);
+            const float4 sc = *reinterpret_cast<const float4 *>(a.pv.scores + row);
+            p = *reinterpret_cast<const int4 *>(a.pv.positions + row);
+            auto key = [&](float s, int pos, int x) { return x < n && ((long long)pos >= newest) == from_recent ? score_key(s) : kNoKey; };
+            k = make_uint4(key(sc.x, p.x, j), key(sc.y, p.y, j + 1), key(sc.z, p.z, j + 2), key(sc.w, p.w, j + 3));
+        };
+        auto fill = [&] {
+#pragma unroll 2
+            for (int j = 4 * tid; j < n && j < cached; j += 4 * kSelThreads) {
+                uint4 k;
+                int4 p;
+                fetch(j, k, p);
+                *reinterpret_cast<uint4 *>(keys + j) = k;
+                *reinterpret_cast<int4 *>(poss + j) = p;
+            }
+        };
+        auto keys4 = [&](int j, unsigned (&k)[4]) {
+            uint4 v;
+            int4 p;
+            if (j < cached) v = *reinterpret_cast<const uint4 *>(keys + j);
+            else fetch(j, v, p);
+            k[0] = v.x; k[1] = v.y; k[2] = v.z; k[3] = v.w;
+        };
+        auto key_at = [&](int j) -> unsigned {
+            if (j < cached) return keys[j];
+            unsigned k[4];
+            keys4(j & ~3, k);
+            return j & 2 ? (j & 1 ? k[3] : k[2]) : (j & 1 ? k[1] : k[0]);
+        };
+        auto pos_at = [&](int j) -> unsigned {           // signed positions in unsigned order
+            const int32_t p = j < cached ? poss[j] : a.pv.positions[pool_row(a.pv, page_for_read(a.pv, table, j), h, j)];
+            return (unsigned)p ^ 0x80000000u;
+        };
+        fill();
+        // digit 0-3: score, 4-7: position, 8-11: slot.  A candidate is still in question when it agrees with the
+        // threshold in all digits found so far.
         unsigned thr[3] = {0u, 0u, 0u};
-        // whether x agrees with the threshold in all digits before `digit`
-        auto agrees = [&](int digit, const uint2 &x, int j) {
-            const int part = digit & 3;
-            const unsigned above = part == 0 ? 0u : 0xffffffffu << (32 - 8 * part);
-            if (digit >= 4 && x.x != thr[0]) return false;
-            if (digit >= 8 && (x.y ^ 0x80000000u) != thr[1]) return false;
-            return ((word(digit, x, j) ^ (digit < 4 ? thr[0] : digit < 8 ? thr[1] : thr[2])) & above) == 0u;
+        auto prefix_mask = [](int digits) { return digits <= 0 ? 0u : digits >= 4 ? 0xffffffffu : 0xffffffffu << (32 - 8 * digits); };
+        auto agrees_beyond_score = [&](int digits, int j) {
+            const unsigned p = pos_at(j);
+            return ((p ^ thr[1]) & prefix_mask(digits - 4)) == 0u && (((unsigned)j ^ thr[2]) & prefix_mask(digits - 8)) == 0u;
         };
         int rank = drop, digit = 0;                      // 1-based rank of the last one to leave
         for (;;) {
@@ -170,9 +198,17 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
             sh.hist[tid] = 0;
             if (tid == 0) sh.count = 0;
             __syncthreads();
-            for (int j = tid; j < n; j += kSelThreads) {
-                const uint2 x = item(j);
-                if (candidate(x) && agrees(digit, x, j)) atomicAdd(&sh.hist[(word(digit, x, j) >> shift) & 255u], 1);
+            const unsigned above = prefix_mask(digit);
+            for (int j = 4 * tid; j < n; j += 4 * kSelThreads) {
+                unsigned k[4];
+                keys4(j, k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (k[e] == kNoKey || ((k[e] ^ thr[0]) & above) != 0u) continue;
+                    if (digit < 4) atomicAdd(&sh.hist[(k[e] >> shift) & 255u], 1);
+                    else if (agrees_beyond_score(digit, j + e))
+                        atomicAdd(&sh.hist[((digit < 8 ? pos_at(j + e) : (unsigned)(j + e)) >> shift) & 255u], 1);
+                }
             }
             __syncthreads();
             if (warp == 0) {                             // 8 bins a lane, then the lane that holds the rank
@@ -203,24 +239,27 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
             if (digit == 0 && !from_recent && sh.total < drop) {
                 from_recent = true;
                 rank = drop - sh.total;
-                continue;                                // the histogram is cleared before anyone adds: two barriers away
+                fill();
+                __syncthreads();
+                continue;
             }
             thr[digit >> 2] |= sh.prefix;
             rank = sh.rank;
             ++digit;
-            if (sh.equal <= kShort) break;               // digits 0-11 tell all slots apart
+            if (sh.equal <= kShort) break;               // twelve digits tell all slots apart
             __syncthreads();
         }
         // the slots that agree so far, ranked by (score, position, slot)
         const int m = sh.equal;
-        auto agrees_all = [&](const uint2 &x, int j) {   // `digit` digits are decided; 12 of them: everything
-            return digit < 12 ? agrees(digit, x, j) : x.x == thr[0] && (x.y ^ 0x80000000u) == thr[1] && (unsigned)j == thr[2];
-        };
-        for (int j = tid; j < n; j += kSelThreads) {
-            const uint2 x = item(j);
-            if (candidate(x) && agrees_all(x, j)) {
-                const int k = atomicAdd(&sh.count, 1);
-                if (k < kShort) { sh.list_key[k] = x.x; sh.list_pos[k] = x.y ^ 0x80000000u; sh.list_slot[k] = j; }
+        const unsigned above = prefix_mask(digit);
+        for (int j = 4 * tid; j < n; j += 4 * kSelThreads) {
+            unsigned k[4];
+            keys4(j, k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (k[e] == kNoKey || ((k[e] ^ thr[0]) & above) != 0u || (digit > 4 && !agrees_beyond_score(digit, j + e))) continue;
+                const int x = atomicAdd(&sh.count, 1);
+                if (x < kShort) { sh.list_key[x] = k[e]; sh.list_pos[x] = pos_at(j + e); sh.list_slot[x] = j + e; }
             }
         }
         __syncthreads();
@@ -238,10 +277,11 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
         const unsigned tk = sh.thr_key, tp = sh.thr_pos;
         const int ts = sh.thr_slot;
         auto stays = [&](int j) {
-            const uint2 x = item(j);
-            if (!candidate(x)) return !from_recent;
-            const unsigned p = x.y ^ 0x80000000u;
-            return !(x.x < tk || (x.x == tk && (p < tp || (p == tp && j <= ts))));
+            const unsigned k = key_at(j);
+            if (k == kNoKey) return !from_recent;
+            if (k != tk) return k > tk;
+            const unsigned p = pos_at(j);
+            return p != tp ? p > tp : j > ts;
         };
         // every warp takes a contiguous range of slots, 32 at a time: mask and counts, scan over the warps, list
         const int per = ((n + kSelWarps - 1) / kSelWarps + 31) / 32 * 32;
