@@ -66,7 +66,7 @@ struct TcWs {
     Item *items;          // [max_items]
     Merge *merges;        // [B * pairs]
     float2 *part_ml;      // [kMaxParts][part_rows]
-    float *part_o;        // [kMaxParts][part_rows][d]
+    float *part_o;        // [kMaxParts][d/4][part_rows][4]: a warp stores 32 rows' four columns as 512 bytes
     float *score_parts;   // [2 * kScoreParts][kBlk]
     int max_items, part_rows, pairs, pair_tokens;
 };
@@ -219,6 +219,29 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b)
 {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// Four lanes hold four 16-byte pieces of a row each; afterwards lane i holds piece i of all four rows, so that a
+// store instruction covers 64 consecutive bytes of 8 rows and not 16 bytes of 32.
+__device__ __forceinline__ void transpose4(uint4 (&p)[4])
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int step = 1; step <= 2; step <<= 1) {
+        const bool up = lane & step;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            if (x & step) continue;
+            const int y = x | step;                         // keep x (lower lane) or y (upper lane), exchange the other
+            uint4 send = up ? p[x] : p[y], got;
+            got.x = __shfl_xor_sync(0xffffffffu, send.x, step);
+            got.y = __shfl_xor_sync(0xffffffffu, send.y, step);
+            got.z = __shfl_xor_sync(0xffffffffu, send.z, step);
+            got.w = __shfl_xor_sync(0xffffffffu, send.w, step);
+            if (up) p[x] = got;
+            else    p[y] = got;
+        }
+    }
 }
 
 template <int D> struct Tile {
@@ -621,30 +644,40 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 named_barrier(1 + quarter, 64);                // read before the next item writes
                 const bool done = wait(&sh->o_done[X], (cnt[X] - 1) & 1);
                 tc_fence_after_sync();
-                const float inv = j.part < 0 ? 1.f / lsum : 1.f;
+                const float inv = 1.f / lsum;
                 const int i = j.i0 + tok;
-                T *orow = static_cast<T *>(a.out) + (int64_t)j.b * a.so.b + (int64_t)(j.h * G + g) * a.so.h + (int64_t)i * a.so.t + half * OW;
-                const size_t prow = (size_t)(j.part < 0 ? 0 : j.part) * ws.part_rows + X * kBlk + r;
-                float *po = ws.part_o + prow * D + half * OW;
+                const size_t prow = (size_t)(j.part < 0 ? 0 : j.part) * ws.part_rows * (D / 4) + X * kBlk + r;
+                float4 *po = reinterpret_cast<float4 *>(ws.part_o) + prow + (size_t)(half * OW / 4) * ws.part_rows;
+                // this lane stores piece lane & 3 of rows r0 .. r0 + 3
+                const int r0 = r & ~3;
+                T *orow = static_cast<T *>(a.out) + (int64_t)j.b * a.so.b + half * OW + (lane & 3) * 8;
 #pragma unroll 1
                 for (int c = 0; c < OW / 32; ++c) {
                     uint32_t o[32];
                     tmem_ld32(to + c * 32, o);
                     tmem_wait_ld();
-                    if (!live || !done) continue;
                     if (j.part < 0) {
+                        uint4 w[4];
 #pragma unroll
                         for (int q4 = 0; q4 < 4; ++q4) {
-                            uint32_t w[4];
+                            uint32_t x[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                w[e] = pack2<T>(__uint_as_float(o[q4 * 8 + 2 * e]) * inv, __uint_as_float(o[q4 * 8 + 2 * e + 1]) * inv);
-                            *reinterpret_cast<uint4 *>(orow + c * 32 + q4 * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+                                x[e] = pack2<T>(__uint_as_float(o[q4 * 8 + 2 * e]) * inv, __uint_as_float(o[q4 * 8 + 2 * e + 1]) * inv);
+                            w[q4] = make_uint4(x[0], x[1], x[2], x[3]);
                         }
-                    } else {
+                        transpose4(w);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int rk = r0 + k, tk = X * tile_tokens + rk / G, gk = rk - rk / G * G;
+                            if (done && rk < tile_rows && tk < j.tokens)
+                                *reinterpret_cast<uint4 *>(orow + (int64_t)(j.h * G + gk) * a.so.h + (int64_t)(j.i0 + tk) * a.so.t + c * 32) = w[k];
+                        }
+                    } else if (live && done) {
 #pragma unroll
                         for (int q8 = 0; q8 < 8; ++q8)
-                            *reinterpret_cast<uint4 *>(po + c * 32 + q8 * 4) = make_uint4(o[q8 * 4], o[q8 * 4 + 1], o[q8 * 4 + 2], o[q8 * 4 + 3]);
+                            po[(size_t)(c * 8 + q8) * ws.part_rows] = make_float4(__uint_as_float(o[q8 * 4]), __uint_as_float(o[q8 * 4 + 1]),
+                                                                                  __uint_as_float(o[q8 * 4 + 2]), __uint_as_float(o[q8 * 4 + 3]));
                     }
                 }
                 tc_fence_before_sync();
@@ -655,7 +688,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         ws.lse2[((size_t)j.b * pv.H + j.h) * pv.c * G + (size_t)i * G + g] = z;
                         if (a.lse) a.lse[(((size_t)j.b * pv.H + j.h) * G + g) * pv.c + i] = z * 0.6931471805599453f;
                     } else {
-                        ws.part_ml[prow] = make_float2(lsum > 0.f ? m_used[X] : -INFINITY, lsum);
+                        ws.part_ml[(size_t)j.part * ws.part_rows + X * kBlk + r] = make_float2(lsum > 0.f ? m_used[X] : -INFINITY, lsum);
                     }
                 }
             };
@@ -674,7 +707,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 }
 
 // ============================================================================================
-// merge: a warp per row of a cut item
+// merge: a block per 32 rows of a cut item; lane = row, a warp takes every eighth group of four columns
 // ============================================================================================
 constexpr int kMergeThreads = 256;
 
@@ -682,58 +715,67 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kMergeThreads)
 paged_merge_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ TcWs ws)
 {
-    constexpr int V = D / 32;                                // elements per lane
+    constexpr int NG = D / 4 / 8;                            // column groups of a warp
+    constexpr int LD = D + 8;                                // halfwords of a staged row
+    __shared__ __align__(16) T stage[32][LD];
     const PagedView &pv = a.pv;
-    const int G = pv.G, tile_tokens = kBlk / G, lane = threadIdx.x & 31;
+    const int G = pv.G, tile_tokens = kBlk / G, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     dependency_wait();
     dependents_may_start();
-    const long long rows = (long long)ws.head->merges * pv.H * ws.part_rows;
-    const int wpg = gridDim.x * (kMergeThreads / 32);
-    for (long long x = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5); x < rows; x += wpg) {
-        const int pr = (int)(x % ws.part_rows);
-        const long long y = x / ws.part_rows;
+    const int row_blocks = ws.part_rows / 32;
+    const long long jobs = (long long)ws.head->merges * pv.H * row_blocks;
+    for (long long x = blockIdx.x; x < jobs; x += gridDim.x) {
+        const int pr0 = (int)(x % row_blocks) * 32, pr = pr0 + lane;
+        const long long y = x / row_blocks;
         const int h = (int)(y % pv.H);
         const Merge mg = ws.merges[y / pv.H];
         const SeqState st = seq_state(pv, mg.b);
-        const int X = pr / kBlk, r = pr - X * kBlk;
-        const int tok = X * tile_tokens + r / G, g = r - r / G * G, i = mg.pair * ws.pair_tokens + tok;
-        if (r >= tile_tokens * G || tok >= ws.pair_tokens || i >= st.len) continue;
-        const size_t step = (size_t)pv.H * ws.part_rows, base = ((size_t)mg.part * pv.H + h) * ws.part_rows + pr;
-        // lane s holds piece s0 + s; pieces that hold nothing the row sees have weight 0 and are not read
-        float mx = -INFINITY, l = 0.f, o[V];
+        auto token = [&](int row) {                          // of the chunk, or -1 for a row that is none
+            const int X = row / kBlk, r = row - X * kBlk, tok = X * tile_tokens + r / G;
+            const int i = mg.pair * ws.pair_tokens + tok;
+            return r < tile_tokens * G && tok < ws.pair_tokens && i < st.len ? i : -1;
+        };
+        const size_t base = ((size_t)mg.part * pv.H + h) * ws.part_rows, step = (size_t)pv.H * ws.part_rows;
+        const int i = token(pr);
+        // pieces that hold nothing the row sees have weight 0; what lies there is not used
+        float mx = -INFINITY, l = 0.f;
+        for (int s = 0; s < mg.n; ++s) {
+            const float2 ml = i >= 0 ? ws.part_ml[base + s * step + pr] : make_float2(0.f, 0.f);
+            mx = fmaxf(mx, ml.y > 0.f ? ml.x : -INFINITY);
+        }
+        float4 o[NG];
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = 0.f;
-        for (int s0 = 0; s0 < mg.n; s0 += 32) {
-            float2 ml = make_float2(-INFINITY, 0.f);
-            if (s0 + lane < mg.n) ml = ws.part_ml[base + (s0 + lane) * step];
-            const float mn = fmaxf(mx, warp_max(ml.y > 0.f ? ml.x : -INFINITY));
-            if (mn == -INFINITY) continue;
-            const float old = exp2f(mx - mn), f = ml.y > 0.f ? exp2f(ml.x - mn) : 0.f;
-            mx = mn;
-            l = fmaf(l, old, warp_sum(f * ml.y));
+        for (int e = 0; e < NG; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int s = 0; s < mg.n; ++s) {
+            const float2 ml = i >= 0 ? ws.part_ml[base + s * step + pr] : make_float2(0.f, 0.f);
+            const float f = ml.y > 0.f ? exp2f(ml.x - mx) : 0.f;
+            l = fmaf(f, ml.y, l);
+            const float4 *src = reinterpret_cast<const float4 *>(ws.part_o) + (base + s * step) * (D / 4) + pr;
 #pragma unroll
-            for (int e = 0; e < V; ++e) o[e] *= old;
-            const int n = min(32, mg.n - s0);
-#pragma unroll 4
-            for (int s = 0; s < n; ++s) {
-                const float w = __shfl_sync(0xffffffffu, f, s);
-                if (w == 0.f) continue;
-                const float *src = ws.part_o + (base + (s0 + s) * step) * D + lane * V;
-                alignas(16) float v[V];
-                if constexpr (V == 4) *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(src);
-                else                  *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(src);
-#pragma unroll
-                for (int e = 0; e < V; ++e) o[e] = fmaf(w, v[e], o[e]);
+            for (int e = 0; e < NG; ++e) {
+                const float4 v = f > 0.f ? src[(size_t)(warp + 8 * e) * ws.part_rows] : make_float4(0.f, 0.f, 0.f, 0.f);
+                o[e].x = fmaf(f, v.x, o[e].x); o[e].y = fmaf(f, v.y, o[e].y);
+                o[e].z = fmaf(f, v.z, o[e].z); o[e].w = fmaf(f, v.w, o[e].w);
             }
         }
         const float inv = 1.f / l;
-        T *dst = static_cast<T *>(a.out) + (int64_t)mg.b * a.so.b + (int64_t)(h * G + g) * a.so.h + (int64_t)i * a.so.t + lane * V;
+        __syncthreads();                                     // the stage has been read
 #pragma unroll
-        for (int e = 0; e < V; e += 2) *reinterpret_cast<uint32_t *>(dst + e) = pack2<T>(o[e] * inv, o[e + 1] * inv);
-        if (lane == 0) {
+        for (int e = 0; e < NG; ++e)
+            *reinterpret_cast<uint2 *>(&stage[lane][(warp + 8 * e) * 4]) = make_uint2(pack2<T>(o[e].x * inv, o[e].y * inv), pack2<T>(o[e].z * inv, o[e].w * inv));
+        if (warp == 0 && i >= 0) {
+            const int g = (pr % kBlk) % G;
             const float z = mx + log2f(l);
             ws.lse2[((size_t)mg.b * pv.H + h) * pv.c * G + (size_t)i * G + g] = z;
             if (a.lse) a.lse[(((size_t)mg.b * pv.H + h) * G + g) * pv.c + i] = z * 0.6931471805599453f;
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < 32 * (D / 8); e += kMergeThreads) {
+            const int row = e / (D / 8), ch = e % (D / 8), ir = token(pr0 + row), g = ((pr0 + row) % kBlk) % G;
+            if (ir >= 0)
+                *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + (int64_t)mg.b * a.so.b + (int64_t)(h * G + g) * a.so.h +
+                                           (int64_t)ir * a.so.t + ch * 8) = *reinterpret_cast<const uint4 *>(&stage[row][ch * 8]);
         }
     }
 }
