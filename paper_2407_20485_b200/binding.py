@@ -478,7 +478,7 @@ def _ints(t, shape, index, name):
     """Address of an int32 array of the call (None: NULL)."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype is not torch.int32 or t.get_device() != index or not t.is_contiguous():
+    if t.dtype is not _I32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name}: expected contiguous int32 {shape} on CUDA device {index}, got {t.dtype} {tuple(t.shape)} "
                          f"on {t.device}")
     return t.data_ptr()
@@ -486,6 +486,8 @@ def _ints(t, shape, index, name):
 
 # address of a device's current stream without the Stream object around it (1.2 us less per call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
 
 
 def _call(index, stream, fn, name, *args):
@@ -493,7 +495,7 @@ def _call(index, stream, fn, name, *args):
     if index < 0:
         raise ValueError(f"{name}: tensors must be on a CUDA device")
     handle = _raw_stream(index) if stream is None else stream.cuda_stream
-    if index == torch.cuda.current_device():
+    if index == _current_device():
         status = fn(*args, handle)
     else:
         with torch.cuda.device(index):
@@ -554,6 +556,8 @@ class PagedCache:
                             *(t.data_ptr() for t in (self.k_pages, self.v_pages, self.scores, self.positions,
                                                      self.page_table, self.past, self.start)))
         self._ref = ctypes.byref(self.p)
+        self._kv_heads, self._q_heads = H, H * group
+        self._nbytes = {}                                   # workspace sizes by call and argument
 
     def a2sf_paged_append(self, k, v, lens=None, q=None, q_out=None, rotary=None, stream=None):
         """k, v [B,H,c,d] (one stride set) into slots past.. of their sequences; with a ``rotary`` plan keys are rotated
@@ -610,7 +614,10 @@ class PagedCache:
               workspace.data_ptr(), workspace.numel())
 
     def _workspace(self, query, name, arg):
-        nbytes = int(query(self._ref, arg))
-        if nbytes == 0:
-            raise A2SFError(A2SF_ERR_INVALID_ARG, name)
-        return torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
+        nbytes = self._nbytes.get((name, arg))
+        if nbytes is None:
+            nbytes = int(query(self._ref, arg))
+            if nbytes == 0:
+                raise A2SFError(A2SF_ERR_INVALID_ARG, name)
+            self._nbytes[name, arg] = nbytes
+        return torch.empty((nbytes,), dtype=_U8, device=self.device)

@@ -287,7 +287,7 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const Path path = path_of(cache, c);
     const cudaError_t e = path == kFew ? launch_attend_few(cache->dtype, a, s)
-                          : path == kTc ? launch_attend_tc(cache->dtype, a, s) : launch_attend_simt(cache->dtype, a, s);
+                          : path == kTc ? launch_attend_tc(cache->dtype, a, s) : launch_attend_simt(a, s);
     return e == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
 }
 
