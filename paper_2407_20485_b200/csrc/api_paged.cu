@@ -50,7 +50,8 @@ int check_paged(const a2sf_paged *p, int c)
     if (!(p->scale >= 0.f) || std::isinf(p->scale)) return A2SF_ERR_INVALID_ARG;
     // slots of a sequence, units, folded rows and tiles of a call all stay 32-bit numbers
     if ((int64_t)p->max_pages * p->page_size > (1 << 28) || (int64_t)c * p->group > (1 << 28) ||
-        (int64_t)p->B * p->H * p->group > (1 << 24) || (int64_t)p->num_pages * p->H * p->page_size >= (1ll << 31))
+        (int64_t)p->B * p->H * p->group > (1 << 24) || (int64_t)p->num_pages * p->H * p->page_size >= (1ll << 31) ||
+        ((int64_t)p->max_pages * p->page_size / 128 + 1) * ((int64_t)c * p->group / 64 + 1) >= (1ll << 31))
         return A2SF_ERR_UNSUPPORTED;
     if (!p->k_pages || !p->v_pages || !p->scores || !p->positions || !p->page_table || !p->past) return A2SF_ERR_INVALID_ARG;
     if (!aligned(p->k_pages, 16) || !aligned(p->v_pages, 16) || !aligned(p->scores, 16) || !aligned(p->positions, 16) ||

@@ -17,7 +17,9 @@
 //   merge   joins the items that were cut.
 //   score   S_j <- alpha^len S_j + sum_r exp2(s_rj - c_r), c_r = lse_r + age * (-log2 alpha): K tile x Q
 //           tiles transposed, so a slot is a TMEM lane and its sum is made by two threads in row order.
-//           Rows whose weight is zero in fp32 are not visited (alpha = 0.9: all but the last 990 tokens).
+//           Rows whose weight is below fp32's normal numbers are not visited (alpha = 0.9: all but the last
+//           830 tokens).  The (key tile, row tile) pairs of the call are one list, cut into equal shares; a
+//           key tile that a cut goes through is summed in parts, which the join kernel adds in order.
 //
 // Bound by the special-function unit: one exponential per logit in attn and one in score, 16 a clock and
 // SM, against 128 x 128 x d x 4 operations of a tile at 8192 a clock: 1024 clocks each for d = 128.
@@ -45,12 +47,12 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanCache = 4096;             // items whose length fits in the plan's shared memory
 constexpr int kLevels = 8;                   // the list is sorted by length in this many steps
 constexpr int kItemCost = 3;                 // what an item costs beside its tiles (set-up, epilogue), in tiles
-constexpr int kScoreParts = 4 * 2 * kSms;    // below this many score jobs, they are cut along the rows
+constexpr int kScoreCtas = 2 * kSms;
 
 struct Item {                                // of one head; all heads have the same
     int b, pair, t0, t1;                     // key tiles t0 .. t1-1
     int part;                                // -1: whole; else index of its partial result
-    int pad[3];
+    int past, len, pad;                      // of its sequence
 };
 struct Merge {
     int b, pair, n, part;                    // partial results part .. part + n - 1
@@ -67,7 +69,7 @@ struct TcWs {
     Merge *merges;        // [B * pairs]
     float2 *part_ml;      // [kMaxParts][part_rows]
     float *part_o;        // [kMaxParts][d/4][part_rows][4]: a warp stores 32 rows' four columns as 512 bytes
-    float *score_parts;   // [2 * kScoreParts][kBlk]
+    float *score_parts;   // [2 * kScoreCtas][kBlk] sums of key tiles that two CTAs or more share
     int max_items, part_rows, pairs, pair_tokens;
 };
 
@@ -166,6 +168,7 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
         const int t = item_tiles(x);
         if (!t) continue;
         const int n = (t - 1) / piece + 1, b = x / ws.pairs, p = x - b * ws.pairs;
+        const SeqState st = seq_state(pv, b);
         int at = atomicAdd(&level[level_of((t + n - 1) / n)], n);
         int part = -1;
         if (n > 1) {
@@ -174,7 +177,7 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
         }
         for (int s = 0; s < n; ++s, ++at)
             if (at < ws.max_items)
-                ws.items[at] = Item{b, p, (int)((long long)t * s / n), (int)((long long)t * (s + 1) / n), n > 1 ? part + s : -1, {0, 0, 0}};
+                ws.items[at] = Item{b, p, (int)((long long)t * s / n), (int)((long long)t * (s + 1) / n), n > 1 ? part + s : -1, st.past, st.len, 0};
     }
     __syncthreads();
     if (tid == 0) ws.head->merges = n_merges;
@@ -378,13 +381,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const Item it = ws.items[first + rest % n_items];
         Job j;
         j.b = it.b; j.h = rest / n_items;
-        const SeqState st = seq_state(pv, it.b);
-        j.past = st.past; j.used = st.past + st.len;
+        j.past = it.past; j.used = it.past + it.len;
         j.i0 = it.pair * ws.pair_tokens;
-        j.tokens = min(ws.pair_tokens, st.len - j.i0);
+        j.tokens = min(ws.pair_tokens, it.len - j.i0);
         j.t0 = it.t0;
         // stream A sees no slot beyond its own last token's
-        const int endA = (st.past + min(j.i0 + tile_tokens, st.len) + kBlk - 1) / kBlk;
+        const int endA = (it.past + min(j.i0 + tile_tokens, it.len) + kBlk - 1) / kBlk;
         j.ntB = j.tokens > tile_tokens ? it.t1 - it.t0 : 0;
         j.ntA = max(0, min(it.t1, endA) - it.t0);
         j.nt = max(j.ntA, j.ntB);
@@ -795,7 +797,7 @@ struct ScoreShared {
     int abort_flag;
     alignas(16) float cbuf[kScoreRing][kBlk];
     float part[kBlk];
-    int32_t prefix[A2SF_PAGED_MAX_SEQUENCES + 1];
+    long long prefix[A2SF_PAGED_MAX_SEQUENCES + 1];
 };
 template <int D> constexpr size_t score_smem() { return 1024 + (size_t)Tile<D>::kBytes * (1 + kScoreStages) + sizeof(ScoreShared); }
 
@@ -821,12 +823,106 @@ __device__ __forceinline__ float strip_sum(const uint32_t (&r)[2][32], const flo
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// Few key tiles (a prompt of its own, not behind a long cache) leave SMs without a job: then every job is cut
-// along the rows into this many, whose sums score_join adds in order.
-__device__ __forceinline__ int score_cuts(const int32_t *prefix, const PagedView &pv)
+// A sequence's key tiles: the row tiles that see tile kt are the last rows_of(kt) of N.
+struct SeqRows {
+    int past, len, tiles, N, tile_tokens, first0;           // first0: first row tile with a weight
+    __device__ __forceinline__ int first(int kt) const { return max(first0, (kt * kBlk - past) / tile_tokens); }
+    __device__ __forceinline__ int rows_of(int kt) const { return N - first(kt); }
+    // tiles 0 .. flat()-1 are seen by the same rows
+    __device__ __forceinline__ int flat() const { return min(tiles, (past + first0 * tile_tokens) / kBlk + 1); }
+};
+__device__ __forceinline__ SeqRows seq_rows(const PagedView &pv, float nl2a, int b)
 {
-    const long long jobs = (long long)pv.H * prefix[pv.B];
-    return jobs == 0 || jobs >= kScoreParts ? 1 : (int)min(16ll, (kScoreParts + jobs - 1) / jobs);
+    const SeqState st = seq_state(pv, b);
+    SeqRows s;
+    s.tile_tokens = kBlk / pv.G;
+    s.past = st.past; s.len = st.len;
+    s.tiles = st.len > 0 ? (st.past + st.len + kBlk - 1) / kBlk : 0;
+    s.N = (st.len + s.tile_tokens - 1) / s.tile_tokens;
+    s.first0 = first_weighted_token(st.len, nl2a) / s.tile_tokens;
+    return s;
+}
+// Pairs of one head, by a warp.
+__device__ __forceinline__ int seq_pairs(const SeqRows &s)
+{
+    const int lane = threadIdx.x & 31, flat = s.flat();
+    int sum = 0;
+    for (int kt = flat + lane; kt < s.tiles; kt += 32) sum += s.rows_of(kt);
+    return __reduce_add_sync(0xffffffffu, sum) + (s.tiles ? flat * s.rows_of(0) : 0);
+}
+
+struct ScorePos {             // a place in the list: key tile kt of (b, h), its row tile q, where the tile begins
+    int b, h, kt, q;
+    long long begins;
+};
+// The place of pair w, by a warp; prefix: pairs of one head, summed over the sequences before.
+__device__ __forceinline__ ScorePos score_pos(const PagedView &pv, float nl2a, const long long *prefix, long long w)
+{
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = pv.B - 1;                              // last b with H * prefix[b] <= w
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (pv.H * prefix[mid] <= w) lo = mid;
+        else hi = mid - 1;
+    }
+    const SeqRows s = seq_rows(pv, nl2a, lo);
+    const long long rest = w - pv.H * prefix[lo], per_head = prefix[lo + 1] - prefix[lo];
+    ScorePos p;
+    p.b = lo;
+    p.h = (int)(rest / per_head);
+    int r = (int)(rest - p.h * per_head);
+    const int flat = s.flat(), n0 = s.rows_of(0);
+    if (r < flat * n0) {
+        p.kt = r / n0;
+        p.q = r - p.kt * n0;
+    } else {
+        r -= flat * n0;
+        int kt0 = flat;
+        for (;; kt0 += 32) {                                // the tile whose running sum goes beyond r
+            const int n = kt0 + lane < s.tiles ? s.rows_of(kt0 + lane) : 0;
+            int incl = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += y;
+            }
+            const unsigned beyond = __ballot_sync(0xffffffffu, incl > r);
+            if (beyond || kt0 + 32 >= s.tiles) {
+                const int at = beyond ? __ffs(beyond) - 1 : 31;
+                p.kt = kt0 + at;
+                p.q = r - __shfl_sync(0xffffffffu, incl - n, at);
+                break;
+            }
+            r -= __shfl_sync(0xffffffffu, incl, 31);
+        }
+    }
+    p.begins = w - p.q;
+    return p;
+}
+// prefix[0 .. B] of the sequences' pairs, by all warps of a block of `warps`
+__device__ __forceinline__ void score_prefix(long long *prefix, const PagedView &pv, float nl2a, int warps)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int b = warp; b < pv.B; b += warps) {
+        const int n = seq_pairs(seq_rows(pv, nl2a, b));
+        if (lane == 0) prefix[b + 1] = n;
+    }
+    if (threadIdx.x == 0) prefix[0] = 0;
+    __syncthreads();
+    if (warp == 0) {
+        long long run = 0;
+        for (int b0 = 0; b0 < pv.B; b0 += 32) {
+            long long incl = b0 + lane < pv.B ? prefix[b0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += y;
+            }
+            if (b0 + lane < pv.B) prefix[b0 + lane + 1] = run + incl;
+            run += __shfl_sync(0xffffffffu, incl, 31);
+        }
+    }
+    __syncthreads();
 }
 
 template <int D>
@@ -859,7 +955,7 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         tmem_alloc(&sh->tmem_base, 256);
         tmem_relinquish();
     }
-    if (warp == 2) tile_prefix<kBlk>(sh->prefix, pv);       // lengths: no kernel of the call writes them
+    score_prefix(sh->prefix, pv, a.nl2a, kScoreThreads / 32);     // from the lengths: no kernel of the call writes them
     // rows that no query copy fills stay zero, so that their logits stay finite
     for (int x = threadIdx.x; x < kScoreStages * Tile<D>::kHalves * (kBlk - tile_rows) * 8; x += kScoreThreads) {
         const int piece = x & 7, row = tile_rows + (x >> 3) % (kBlk - tile_rows), half = (x >> 3) / (kBlk - tile_rows);
@@ -870,25 +966,40 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = sh->tmem_base;
-    const int cuts = score_cuts(sh->prefix, pv);
-    const long long total = (long long)pv.H * sh->prefix[pv.B] * cuts;
+    const long long total = pv.H * sh->prefix[pv.B], share = (total + gridDim.x - 1) / gridDim.x;
+    const long long w0 = blockIdx.x * share, w1 = w0 + share < total ? w0 + share : total;
+    ScorePos at = {};
+    SeqRows seq = {};
+    if (w0 < w1) {
+        at = score_pos(pv, a.nl2a, sh->prefix, w0);
+        seq = seq_rows(pv, a.nl2a, at.b);
+    }
     dependency_wait();
     dependents_may_start();
 
     struct Job {
         int b, h, j0, past, len, used, q0, nq;             // query tiles q0 .. q0 + nq - 1
+        int part;                                          // -1: all of the key tile's; else where its sums go
     };
-    auto job = [&](long long w) -> Job {
-        const int cut = (int)(w % cuts);
-        const Where x = locate(sh->prefix, pv.B, pv.H, w / cuts);
-        const SeqState st = seq_state(pv, x.b);
+    // the part of this CTA's share that lies in the current key tile; then on to the next tile
+    auto next_job = [&](long long &w) -> Job {
         Job j;
-        j.b = x.b; j.h = x.h; j.j0 = x.t * kBlk;
-        j.past = st.past; j.len = st.len; j.used = st.past + st.len;
-        const int first = max(max(first_weighted_token(st.len, a.nl2a), j.j0 - st.past), 0) / tile_tokens;
-        const int n = (st.len + tile_tokens - 1) / tile_tokens - first;
-        j.q0 = first + n * cut / cuts;
-        j.nq = first + n * (cut + 1) / cuts - j.q0;
+        j.b = at.b; j.h = at.h; j.j0 = at.kt * kBlk;
+        j.past = seq.past; j.len = seq.len; j.used = seq.past + seq.len;
+        const int n = seq.rows_of(at.kt);
+        j.nq = (int)min((long long)(n - at.q), w1 - w);
+        j.q0 = seq.first(at.kt) + at.q;
+        // a tile begun by another CTA is this one's first, a tile that the next one goes on with its last
+        j.part = at.q > 0 ? 2 * blockIdx.x : j.nq < n ? 2 * blockIdx.x + 1 : -1;
+        w += j.nq;
+        at.q = 0;
+        if (w < w1 && ++at.kt == seq.tiles) {
+            at.kt = 0;
+            if (++at.h == pv.H) {
+                at.h = 0;
+                do seq = seq_rows(pv, a.nl2a, ++at.b); while (seq.tiles == 0);      // there is one: w < w1
+            }
+        }
         return j;
     };
     auto wait = [&](uint64_t *bar, uint32_t parity) -> bool {
@@ -898,8 +1009,8 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 
     if (warp == 0) {
         int qt = 0, n = 0;
-        for (long long w = blockIdx.x; w < total; w += gridDim.x, ++n) {
-            const Job j = job(w);
+        for (long long w = w0; w < w1; ++n) {
+            const Job j = next_job(w);
             const PageTile p = page_tile(pv, j.j0 / kBlk, j.used);
             const int slot = j.j0 + lane * p.box;
             int row = 0, ok = 1;
@@ -944,8 +1055,8 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             const uint64_t k_desc = kmajor_desc(smem_u32(Ks));
             const uint64_t q_desc = kmajor_desc(smem_u32(Qs));
             int qt = 0, n = 0;
-            for (long long w = blockIdx.x; w < total && !*abort_flag; w += gridDim.x, ++n) {
-                const Job j = job(w);
+            for (long long w = w0; w < w1 && !*abort_flag; ++n) {
+                const Job j = next_job(w);
                 wait(&sh->k_full, n & 1);
                 for (int t = 0; t < j.nq; ++t, ++qt) {
                     const int s = qt % kScoreStages, acc = qt & 1;
@@ -963,11 +1074,11 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         const int quarter = warp & 3, hsel = (warp - 2) >> 2;
         const int key = quarter * 32 + lane;
         int qt = 0;
-        for (long long w = blockIdx.x; w < total; w += gridDim.x) {
-            const Job j = job(w);
+        for (long long w = w0; w < w1;) {
+            const Job j = next_job(w);
             const int slot = j.j0 + key;
             float *dst = nullptr, old = 0.f;
-            if (cuts == 1 && hsel == 0 && slot < j.used) {
+            if (j.part < 0 && hsel == 0 && slot < j.used) {
                 const int page = page_for_write(pv, pv.table + (size_t)j.b * pv.max_pages, slot);
                 if (page >= 0) {
                     dst = pv.scores + pool_row(pv, page, j.h, slot);
@@ -999,7 +1110,7 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             if (hsel == 1) sh->part[key] = sum;
             named_barrier(1, 256);
             if (dst && !*abort_flag) *dst = fmaf(old, ex2_approx(-age_exponent(j.len, a.nl2a)), sum + sh->part[key]);
-            if (cuts > 1 && hsel == 0) ws.score_parts[w * kBlk + key] = sum + sh->part[key];
+            if (j.part >= 0 && hsel == 0) ws.score_parts[(size_t)j.part * kBlk + key] = sum + sh->part[key];
             named_barrier(1, 256);                          // read before the next item writes
         }
     }
@@ -1012,30 +1123,39 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     if (threadIdx.x == 0 && sh->abort_flag) *pv.status = A2SF_ERR_TIMEOUT;
 }
 
-// Adds the sums of jobs that were cut: a block per key tile.
+// Block k: the key tile that the cut before CTA k's share goes through, if it is the tile's first cut.
 __global__ void __launch_bounds__(kBlk)
 paged_score_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ TcWs ws)
 {
-    __shared__ int32_t prefix[A2SF_PAGED_MAX_SEQUENCES + 1];
+    __shared__ long long prefix[A2SF_PAGED_MAX_SEQUENCES + 1];
     const PagedView &pv = a.pv;
-    if (threadIdx.x < 32) tile_prefix<kBlk>(prefix, pv);
-    __syncthreads();
-    const int cuts = score_cuts(prefix, pv);
-    dependency_wait();
-    if (cuts == 1) return;
-    const long long jobs = (long long)pv.H * prefix[pv.B];
-    for (long long w = blockIdx.x; w < jobs; w += gridDim.x) {
-        const Where x = locate(prefix, pv.B, pv.H, w);
-        const SeqState st = seq_state(pv, x.b);
-        const int slot = x.t * kBlk + threadIdx.x;
-        if (slot >= st.past + st.len) continue;
-        const int page = page_for_write(pv, pv.table + (size_t)x.b * pv.max_pages, slot);
-        if (page < 0) continue;
-        float sum = 0.f;
-        for (int c = 0; c < cuts; ++c) sum += ws.score_parts[(w * cuts + c) * kBlk + threadIdx.x];
-        float *dst = pv.scores + pool_row(pv, page, x.h, slot);
-        *dst = fmaf(*dst, ex2_approx(-age_exponent(st.len, a.nl2a)), sum);
+    score_prefix(prefix, pv, a.nl2a, kBlk / 32);
+    const long long total = pv.H * prefix[pv.B], share = (total + kScoreCtas - 1) / kScoreCtas;
+    const int k = blockIdx.x + 1;
+    const long long w = k * share;
+    ScorePos at = {};
+    SeqRows seq = {};
+    bool mine = w < total;
+    if (mine) {
+        at = score_pos(pv, a.nl2a, prefix, w);
+        seq = seq_rows(pv, a.nl2a, at.b);
+        mine = at.begins < w && at.begins >= w - share;
     }
+    const int slot = at.kt * kBlk + threadIdx.x;
+    float *dst = nullptr, old = 0.f;
+    if (mine && slot < seq.past + seq.len) {
+        const int page = page_for_write(pv, pv.table + (size_t)at.b * pv.max_pages, slot);
+        if (page >= 0) {
+            dst = pv.scores + pool_row(pv, page, at.h, slot);
+            old = *dst;
+        }
+    }
+    dependency_wait();
+    if (!dst) return;
+    const int last = (int)((at.begins + seq.rows_of(at.kt) - 1) / share);
+    float sum = ws.score_parts[(size_t)(2 * (k - 1) + 1) * kBlk + threadIdx.x];
+    for (int c = k; c <= last; ++c) sum += ws.score_parts[(size_t)(2 * c) * kBlk + threadIdx.x];
+    *dst = fmaf(old, ex2_approx(-age_exponent(seq.len, a.nl2a)), sum);
 }
 
 size_t pad(size_t x) { return (x + 255) / 256 * 256; }
@@ -1061,7 +1181,7 @@ TcWs carve(const PagedView &pv, void *mem, size_t *bytes)
     w.merges = reinterpret_cast<Merge *>(base + off); off += pad(items * sizeof(Merge));
     w.part_ml = reinterpret_cast<float2 *>(base + off); off += pad(parts * w.part_rows * 8);
     w.part_o = reinterpret_cast<float *>(base + off); off += pad(parts * w.part_rows * pv.d * 4);
-    w.score_parts = reinterpret_cast<float *>(base + off); off += pad((size_t)2 * kScoreParts * kBlk * 4);
+    w.score_parts = reinterpret_cast<float *>(base + off); off += pad((size_t)2 * kScoreCtas * kBlk * 4);
     if (bytes) *bytes = off;
     return w;
 }
@@ -1085,13 +1205,13 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
     e = launch_follower(paged_attn_tc_kernel<T, D>, kSms, kAttnThreads, attn_smem<D>(), s, mq, mk, mv, a, ws);
     if (e != cudaSuccess) return e;
     count_launch();
-    if ((e = launch_follower(paged_merge_kernel<T, D>, 8 * kSms, kMergeThreads, 0, s, a, ws)) != cudaSuccess) return e;
+    if ((e = launch_follower(paged_merge_kernel<T, D>, 4 * kSms, kMergeThreads, 0, s, a, ws)) != cudaSuccess) return e;
     count_launch();
     if (!a.scores) return cudaSuccess;
-    e = launch_follower(paged_score_tc_kernel<D>, 2 * kSms, kScoreThreads, score_smem<D>(), s, mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
+    e = launch_follower(paged_score_tc_kernel<D>, kScoreCtas, kScoreThreads, score_smem<D>(), s, mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
     if (e != cudaSuccess) return e;
     count_launch();
-    if ((e = launch_follower(paged_score_join_kernel, 4 * kSms, kBlk, 0, s, a, ws)) != cudaSuccess) return e;
+    if ((e = launch_follower(paged_score_join_kernel, kScoreCtas - 1, kBlk, 0, s, a, ws)) != cudaSuccess) return e;
     count_launch();
     return cudaSuccess;
 }
