@@ -44,6 +44,8 @@ constexpr int kPieces = 4 * kSms;            // pieces that cutting makes at mos
 constexpr int kMinPiece = 4;                 // key tiles of a piece at least
 constexpr int kMaxParts = kSplitBelow + kPieces;   // sum of ceil(T / piece) <= total / piece + items
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanWarps = kPlanThreads / 32;
+constexpr int kCandidates = 32;
 constexpr int kPlanCache = 4096;             // items whose length fits in the plan's shared memory
 constexpr int kLevels = 8;                   // the list is sorted by length in this many steps
 constexpr int kItemCost = 3;                 // what an item costs beside its tiles (set-up, epilogue), in tiles
@@ -79,21 +81,24 @@ __device__ __forceinline__ int pair_key_tiles(const SeqState &st, int pair, int 
 }
 
 // The item list.  Cutting items into pieces of p tiles makes sum(ceil(T / p)) of them; CTAs take them in
-// rounds, so a call takes about  max(ceil(pieces / SMs) * (mean length + kItemCost), longest + kItemCost):  32
-// warps try 32 lengths between a quarter and one and a half of an SM's even share, and no cut at all.
+// rounds, so a call takes about  max(ceil(pieces / SMs) * (mean length + kItemCost), longest + kItemCost):
+// lengths between a quarter and one and a half of an SM's even share are tried, and no cut at all.
 __global__ void __launch_bounds__(kPlanThreads)
 paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ TcWs ws)
 {
-    __shared__ int tiles[kPlanCache], level[kLevels], warp_cnt[32], warp_max_[32], cand_piece[32], n_parts, n_merges;
-    __shared__ float cand_cost[32], warp_work[32];
+    __shared__ int tiles[kPlanCache], level[kLevels], warp_cnt[kPlanWarps], warp_max_[kPlanWarps], cand_piece[kCandidates], n_parts, n_merges;
+    __shared__ float cand_cost[kCandidates], warp_work[kPlanWarps];
+    __shared__ SeqState seqs[A2SF_PAGED_MAX_SEQUENCES];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     dependents_may_start();
     if (tid < kLevels) level[tid] = 0;
     if (tid == 0) { n_parts = 0; n_merges = 0; }
     const int all = pv.B * ws.pairs;
+    for (int b = tid; b < pv.B; b += kPlanThreads) seqs[b] = seq_state(pv, b);
+    __syncthreads();
     auto measure = [&](int x) -> int {
         const int b = x / ws.pairs, p = x - b * ws.pairs;
-        const SeqState st = seq_state(pv, b);
+        const SeqState st = seqs[b];
         return p * ws.pair_tokens < st.len ? pair_key_tiles(st, p, ws.pair_tokens) : 0;
     };
     auto item_tiles = [&](int x) -> int { return x < kPlanCache ? tiles[x] : measure(x); };
@@ -110,27 +115,30 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
     const int wcnt = __reduce_add_sync(0xffffffffu, cnt), wmax = __reduce_max_sync(0xffffffffu, mx);
     if (lane == 0) { warp_work[warp] = sum; warp_cnt[warp] = wcnt; warp_max_[warp] = wmax; }
     __syncthreads();
-    const float work = (float)pv.H * warp_sum(warp_work[lane]);
-    const int items = __reduce_add_sync(0xffffffffu, warp_cnt[lane]);
-    const int longest = __reduce_max_sync(0xffffffffu, warp_max_[lane]);
+    const bool in = lane < kPlanWarps;
+    const float work = (float)pv.H * warp_sum(in ? warp_work[lane] : 0.f);
+    const int items = __reduce_add_sync(0xffffffffu, in ? warp_cnt[lane] : 0);
+    const int longest = __reduce_max_sync(0xffffffffu, in ? warp_max_[lane] : 0);
     int piece = 0x7fffffff;
     if ((long long)items * pv.H < kSplitBelow && longest > kMinPiece) {
-        // warp w tries one length; the last one no cut
+        // the last candidate is no cut
         const float share = work / kSms;
-        const int p = warp == 31 ? 0x7fffffff : max(kMinPiece, (int)ceilf(share * 0.25f * exp2f(warp * (2.585f / 30.f))));
-        int n = 0, most = 0;
-        for (int x = lane; x < all; x += 32) {
-            const int t = item_tiles(x);
-            const int k = t > 0 ? (t - 1) / p + 1 : 0;
-            n += k;
-            most = max(most, k ? (t + k - 1) / k : 0);
-        }
-        n = __reduce_add_sync(0xffffffffu, n) * pv.H;
-        most = __reduce_max_sync(0xffffffffu, most);
-        if (lane == 0) {
-            const float rounds = (float)((n + kSms - 1) / kSms);
-            cand_cost[warp] = fmaxf(rounds * (work / (float)max(n, 1) + kItemCost), (float)(most + kItemCost));
-            cand_piece[warp] = p;
+        for (int w = warp; w < kCandidates; w += kPlanWarps) {
+            const int p = w == kCandidates - 1 ? 0x7fffffff : max(kMinPiece, (int)ceilf(share * 0.25f * exp2f(w * (2.585f / 30.f))));
+            const float per = 1.f / (float)p;                // an estimate: no exact division needed
+            float n = 0.f, most = 0.f;
+            for (int x = lane; x < all; x += 32) {
+                const float t = (float)item_tiles(x), k = ceilf(t * per);
+                n += k;
+                most = fmaxf(most, t > 0.f ? __fdividef(t, k) : 0.f);
+            }
+            n = warp_sum(n) * pv.H;
+            most = warp_max(most);
+            if (lane == 0) {
+                const float rounds = ceilf(n / kSms);
+                cand_cost[w] = fmaxf(rounds * (work / fmaxf(n, 1.f) + kItemCost), most + kItemCost);
+                cand_piece[w] = p;
+            }
         }
         __syncthreads();
         float best = cand_cost[lane];
@@ -168,7 +176,7 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
         const int t = item_tiles(x);
         if (!t) continue;
         const int n = (t - 1) / piece + 1, b = x / ws.pairs, p = x - b * ws.pairs;
-        const SeqState st = seq_state(pv, b);
+        const SeqState st = seqs[b];
         int at = atomicAdd(&level[level_of((t + n - 1) / n)], n);
         int part = -1;
         if (n > 1) {
@@ -974,7 +982,6 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         at = score_pos(pv, a.nl2a, sh->prefix, w0);
         seq = seq_rows(pv, a.nl2a, at.b);
     }
-    dependency_wait();
     dependents_may_start();
 
     struct Job {
@@ -1008,7 +1015,10 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     };
 
     if (warp == 0) {
+        // Only the row constants come from the kernels before: the first K and Q tiles are requested, and the
+        // first products made, without waiting for them.
         int qt = 0, n = 0;
+        bool waited = false;
         for (long long w = w0; w < w1; ++n) {
             const Job j = next_job(w);
             const PageTile p = page_tile(pv, j.j0 / kBlk, j.used);
@@ -1024,12 +1034,6 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             const float *lse2 = ws.lse2 + ((size_t)j.b * pv.H + j.h) * pv.c * G;
             for (int t = 0; t < j.nq; ++t, ++qt) {
                 const int s = qt % kScoreStages, i0 = (j.q0 + t) * tile_tokens;
-                float c4[4];                                // in flight while lane 0 waits for the stage
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = lane * 4 + e, i = i0 + r / G;
-                    c4[e] = r < tile_rows && i < j.len ? lse2[(size_t)i0 * G + r] + age_exponent(j.len - 1 - i, a.nl2a) : INFINITY;
-                }
                 ok = 1;
                 if (lane == 0) {
                     if (qt >= kScoreStages) ok = wait(&sh->q_empty[s], ((qt / kScoreStages) & 1) ^ 1) ? 1 : 0;
@@ -1038,12 +1042,21 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         copy_query_tile<D>(Qs + s * kTileBytes, &map_q, &sh->q_full[s], j.h * G, i0, j.b);
                     }
                 }
+                if (!waited) dependency_wait();
+                waited = true;
+                float c4[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = lane * 4 + e, i = i0 + r / G;
+                    c4[e] = r < tile_rows && i < j.len ? lse2[(size_t)i0 * G + r] + age_exponent(j.len - 1 - i, a.nl2a) : INFINITY;
+                }
                 if (!__shfl_sync(0xffffffffu, ok, 0)) break;
                 *reinterpret_cast<float4 *>(&sh->cbuf[qt % kScoreRing][lane * 4]) = make_float4(c4[0], c4[1], c4[2], c4[3]);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh->c_ready[qt % kScoreRing]);
             }
         }
+        if (!waited) dependency_wait();
         if (lane == 0 && *abort_flag) {
             int dummy = 0;
             for (int k = max(0, qt - kScoreStages); k < qt; ++k) mbar_wait(&sh->q_full[k % kScoreStages], (k / kScoreStages) & 1, &dummy);
