@@ -419,8 +419,10 @@ int a2sf_rotary(const a2sf_rotary_plan *plan, int32_t dtype, int32_t B, int32_t 
  * written, and where they would be read the sequence's results are undefined -- and
  * a2sf_last_device_status then returns A2SF_ERR_INVALID_ARG.  The first call on a device looks up
  * that status word and raises kernel limits: make it before a stream capture begins.
- * Pages must not be shared by two sequences where they are written.  Keys, values and queries of
- * resident tokens must be finite; slots beyond past + len may hold anything.
+ * A page that two sequences share must not be written: by a2sf_paged_append, by a2sf_paged_evict in
+ * place, nor by a2sf_paged_attend, which updates scores unless told not to.  Keys, values and
+ * queries of resident tokens must be finite; slots beyond past + len may hold anything.  Calls on
+ * the same sequences must be ordered (same stream, or events between streams).
  * ------------------------------------------------------------------------- */
 #define A2SF_PAGED_MAX_SEQUENCES 1024
 typedef struct a2sf_paged {
@@ -458,7 +460,7 @@ int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary_op
  *     score[slot] <- alpha^len * score[slot] + sum_{i,g} alpha^(len-1-i) P_ig,slot
  * which is Eq. 5 carried over chunks: any split of a prompt into chunks gives the scores of the
  * whole.  flags: 0, or A2SF_ATTEND_NO_SCORES (scores are neither read nor written).  out has strides
- * of its own; rows i >= len[b] of out and lse are left as they were.  Rows whose weight alpha^age
+ * of its own and must not overlap q; rows i >= len[b] of out and lse are left as they were.  Rows whose weight alpha^age
  * is below 2^-126 (the smallest normal fp32 number) are left out of the sum.
  * workspace: DEVICE, 256-byte aligned, a2sf_paged_attend_workspace_bytes (0 = invalid arguments);
  * contents undefined afterwards; calls that may overlap in time need workspaces of their own. */

@@ -275,6 +275,7 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
         (rc = check_tensor(out, cache->dtype, cache->d, eq, so)) != A2SF_OK)
         return rc;
     if (!aligned(lens, 4) || !aligned(lse, 4) || !workspace || !aligned(workspace, 256)) return A2SF_ERR_INVALID_ARG;
+    if (q == out) return A2SF_ERR_INVALID_ARG;               // the scores read the queries after the outputs are written
     if (workspace_bytes < a2sf_paged_attend_workspace_bytes(cache, c)) return A2SF_ERR_WORKSPACE;
     AttendArgs a;
     a.pv = make_view(cache, c, lens);

@@ -115,7 +115,8 @@ __device__ __forceinline__ unsigned long long warp_min_u64(unsigned long long v)
 enum DebugKernelId {
     kDbgSelect = 1, kDbgCacheLoad, kDbgDecodeStream, kDbgDecodeSplit, kDbgGroupMma, kDbgGroupSimt,
     kDbgGroupSum, kDbgPrefillSimt1, kDbgPrefillSimt2, kDbgAttnTc, kDbgScoreTc, kDbgVToHalf,
-    kDbgIdealStats, kDbgSimilarityRow
+    kDbgIdealStats, kDbgSimilarityRow,
+    kDbgPagedRow, kDbgPagedFew, kDbgPagedTc, kDbgPagedSimt, kDbgPagedEvict, kDbgRotary
 };
 #ifdef A2SF_DEBUG
 // one record per translation unit (no relocatable device code): {violations, kernel << 32 | line,

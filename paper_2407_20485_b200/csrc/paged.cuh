@@ -41,6 +41,7 @@ __device__ __forceinline__ SeqState seq_state(const PagedView &a, int b)
 // Page of slot `s` of sequence b for reading: a bad entry is reported and page 0 stands in.
 __device__ __forceinline__ int page_for_read(const PagedView &a, const int32_t *row, int s)
 {
+    if (!A2SF_IN_RANGE(s >> a.ps_shift, a.max_pages, kDbgPagedRow)) return 0;
     const int p = row[s >> a.ps_shift];
     if ((unsigned)p < (unsigned)a.num_pages) return p;
     *a.status = A2SF_ERR_INVALID_ARG;
@@ -49,6 +50,7 @@ __device__ __forceinline__ int page_for_read(const PagedView &a, const int32_t *
 // ... and for writing: -1, and the write is left out.
 __device__ __forceinline__ int page_for_write(const PagedView &a, const int32_t *row, int s)
 {
+    if (!A2SF_IN_RANGE(s >> a.ps_shift, a.max_pages, kDbgPagedRow)) return -1;
     const int p = row[s >> a.ps_shift];
     if ((unsigned)p < (unsigned)a.num_pages) return p;
     *a.status = A2SF_ERR_INVALID_ARG;
@@ -57,7 +59,8 @@ __device__ __forceinline__ int page_for_write(const PagedView &a, const int32_t 
 // Index of a slot's row within the pool (times d: its K and V row; alone: score and position).
 __device__ __forceinline__ int64_t pool_row(const PagedView &a, int page, int h, int s)
 {
-    return (((int64_t)page * a.H + h) << a.ps_shift) + (s & ((1 << a.ps_shift) - 1));
+    const int64_t row = (((int64_t)page * a.H + h) << a.ps_shift) + (s & ((1 << a.ps_shift) - 1));
+    return A2SF_IN_RANGE(row, ((int64_t)a.num_pages * a.H) << a.ps_shift, kDbgPagedRow) && A2SF_IN_RANGE(h, a.H, kDbgPagedRow) ? row : 0;
 }
 
 // alpha^age in fp32, with 0^0 = 1 (nl2a = -log2 alpha, +inf for alpha = 0)

@@ -49,6 +49,7 @@ struct FewWs {
     float *o;             // [segments][kWarps][NP][D]
     int32_t *prefix;      // [B + 1] tiles of a head, summed over the sequences before
     int slots;            // padded slots of a unit
+    int segs;             // segments that there is room for, times kWarps
 };
 
 template <typename T> struct Mma16;
@@ -456,13 +457,13 @@ drained:
                 if (!*abort_flag && !mbar_wait(&sh.full[s], (it / R::kStages) & 1, abort_flag)) *pv.status = A2SF_ERR_TIMEOUT;
                 const int j0 = x.t * kTile + cw * 16;
                 uint8_t *K = ring + (size_t)s * 2 * R::kTileBytes;
-                if (j0 < used) body.tile(a, K, K + R::kTileBytes, cw * 16, j0, used, logits, NP, scratch);
+                if (j0 < used && A2SF_IN_RANGE(j0 + 15, ws.slots, kDbgPagedFew)) body.tile(a, K, K + R::kTileBytes, cw * 16, j0, used, logits, NP, scratch);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.empty[s]);
             }
             // segment = CTA + unit: both only grow along the list, one of them at every boundary
             const size_t seg = ((size_t)blockIdx.x + unit) * kWarps + cw;
-            body.end(ws.ml + seg * NP, ws.o + seg * NP * D, NP);
+            if (A2SF_IN_RANGE(seg, ws.segs, kDbgPagedFew)) body.end(ws.ml + seg * NP, ws.o + seg * NP * D, NP);
             if (w < w1) next_unit(x, sh.prefix, pv.B, pv.H);
         }
     }
@@ -546,7 +547,7 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
     const bool working = rows > 0 && (y < rows || j0 < j1);
     if (working) batch.addresses(pv, table, h, j0 + tid, j1);
     dependency_wait();
-    if (!working) return;
+    if (!working || !A2SF_IN_RANGE(u, pv.B * pv.H, kDbgPagedFew)) return;
     const float *logits = ws.logits + (size_t)u * ws.slots * NP;
     batch.logits(logits, j0 + tid);
     // the CTAs of the main kernel that had a part of this unit
@@ -556,6 +557,7 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
     const int k0 = (int)(u0 / share), k1 = (int)((u0 + tiles - 1) / share);
     const size_t seg0 = ((size_t)k0 + u) * kWarps;
     const int parts = (k1 - k0 + 1) * kWarps;
+    if (!A2SF_IN_RANGE(seg0 + parts - 1, ws.segs, kDbgPagedFew)) return;
     // (maximum, sum) of part p and row r at ml[r * row_step + p * part_step]
     const float2 *ml = ws.ml + seg0 * NP;
     int row_step = 1, part_step = NP;
@@ -641,6 +643,7 @@ FewWs carve(const PagedView &pv, void *ws, size_t *bytes)
     size_t off = 0;
     char *base = static_cast<char *>(ws);
     w.slots = padded_slots(pv);
+    w.segs = (int)segs;
     w.logits = reinterpret_cast<float *>(base + off); off += pad(U * w.slots * NP * 4);
     w.ml = reinterpret_cast<float2 *>(base + off); off += pad(segs * NP * 8);
     w.o = reinterpret_cast<float *>(base + off); off += pad(segs * NP * pv.d * 4);

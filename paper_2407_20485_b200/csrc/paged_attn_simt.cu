@@ -63,7 +63,7 @@ __device__ __forceinline__ void copy_queries(float *dst, const AttendArgs &a, co
     constexpr int CH = D / 4;
     for (int x = threadIdx.x; x < n * CH; x += kThreads) {
         const int row = x / CH, ch = x % CH, r = r0 + row;
-        const bool live = r < u.rows;
+        const bool live = r < u.rows && A2SF_IN_RANGE(r, a.pv.c * a.pv.G, kDbgPagedSimt);
         const int i = live ? r / a.pv.G : 0, g = live ? r - i * a.pv.G : 0;
         const float *p = static_cast<const float *>(a.q) + u.b * a.sq.b + (int64_t)(u.h * a.pv.G + g) * a.sq.h + (int64_t)i * a.sq.t;
         copy16(dst + row * Lay<D>::LD + ch * 4, p + ch * 4, live);
@@ -211,7 +211,7 @@ paged_attn_simt_kernel(const __grid_constant__ AttendArgs a, int row_tiles)
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         const int r = r0 + ty * RT + i;
-        if (r > last_row) continue;
+        if (r > last_row || !A2SF_IN_RANGE(r, a.pv.c * G, kDbgPagedSimt)) continue;
         const int tok = r / G, g = r - tok * G;
         const float inv = 1.f / l[i];
         float *dst = static_cast<float *>(a.out) + u.b * a.so.b + (int64_t)(u.h * G + g) * a.so.h + (int64_t)tok * a.so.t;

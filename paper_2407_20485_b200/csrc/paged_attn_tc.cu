@@ -72,7 +72,7 @@ struct TcWs {
     float2 *part_ml;      // [kMaxParts][part_rows]
     float *part_o;        // [kMaxParts][d/4][part_rows][4]: a warp stores 32 rows' four columns as 512 bytes
     float *score_parts;   // [2 * kScoreCtas][kBlk] sums of key tiles that two CTAs or more share
-    int max_items, part_rows, pairs, pair_tokens;
+    int max_items, part_rows, pairs, pair_tokens, parts;
 };
 
 __device__ __forceinline__ int pair_key_tiles(const SeqState &st, int pair, int pair_tokens)
@@ -181,10 +181,11 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
         int part = -1;
         if (n > 1) {
             part = atomicAdd(&n_parts, n);
+            (void)A2SF_IN_RANGE((long long)(part + n) * pv.H - 1, ws.parts, kDbgPagedTc);
             ws.merges[atomicAdd(&n_merges, 1)] = Merge{b, p, n, part};
         }
         for (int s = 0; s < n; ++s, ++at)
-            if (at < ws.max_items)
+            if (A2SF_IN_RANGE(at, ws.max_items, kDbgPagedTc) && at < ws.max_items)
                 ws.items[at] = Item{b, p, (int)((long long)t * s / n), (int)((long long)t * (s + 1) / n), n > 1 ? part + s : -1, st.past, st.len, 0};
     }
     __syncthreads();
@@ -399,6 +400,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         j.ntA = max(0, min(it.t1, endA) - it.t0);
         j.nt = max(j.ntA, j.ntB);
         j.part = it.part < 0 ? -1 : it.part * pv.H + j.h;
+        if (j.part >= 0 && !A2SF_IN_RANGE(j.part, ws.parts, kDbgPagedTc)) j.part = 0;
         return j;
     };
 
@@ -640,7 +642,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             auto finish = [&](auto Xc, int ntX) {
                 constexpr int X = decltype(Xc)::value;
                 const int tok = X * tile_tokens + r / G, g = r - r / G * G;
-                const bool live = r < tile_rows && tok < j.tokens;
+                const bool live = r < tile_rows && tok < j.tokens && A2SF_IN_RANGE(j.i0 + tok, pv.c, kDbgPagedTc);
                 if (ntX == 0) {
                     // a cut item whose piece lies behind everything stream A sees: an empty partial result
                     if (j.part >= 0 && X == 0 && half == 0) ws.part_ml[(size_t)j.part * ws.part_rows + r] = make_float2(-INFINITY, 0.f);
@@ -1123,7 +1125,7 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             if (hsel == 1) sh->part[key] = sum;
             named_barrier(1, 256);
             if (dst && !*abort_flag) *dst = fmaf(old, ex2_approx(-age_exponent(j.len, a.nl2a)), sum + sh->part[key]);
-            if (j.part >= 0 && hsel == 0) ws.score_parts[(size_t)j.part * kBlk + key] = sum + sh->part[key];
+            if (j.part >= 0 && hsel == 0 && A2SF_IN_RANGE(j.part, 2 * kScoreCtas, kDbgPagedTc)) ws.score_parts[(size_t)j.part * kBlk + key] = sum + sh->part[key];
             named_barrier(1, 256);                          // read before the next item writes
         }
     }
@@ -1186,6 +1188,7 @@ TcWs carve(const PagedView &pv, void *mem, size_t *bytes)
     w.max_items = (int)(items + kMaxParts);
     size_t parts = cap_tiles <= kMinPiece ? 0 : items * pv.H * ((cap_tiles + kMinPiece - 1) / kMinPiece);
     if (parts > kMaxParts) parts = kMaxParts;
+    w.parts = (int)parts;
     char *base = static_cast<char *>(mem);
     size_t off = 0;
     w.lse2 = reinterpret_cast<float *>(base + off); off += pad(U * pv.c * pv.G * 4);

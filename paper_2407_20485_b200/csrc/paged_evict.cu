@@ -97,7 +97,7 @@ __device__ __forceinline__ void move_rows(const EvictArgs &a, int u, int b, int 
         for (int x = 0; x < kRows; ++x) {
             const int k = k0 + x * groups;
             t[x] = -1;
-            if (k >= moves) continue;
+            if (k >= moves || !A2SF_IN_RANGE(k, a.M, kDbgPagedEvict)) continue;
             const int src = a.from[(size_t)u * a.M + k], dst = fresh ? k : a.to[(size_t)u * a.M + k];
             const int to_page = page_for_write(a.pv, to_row, dst);
             s[x] = pool_row(a.pv, page_for_read(a.pv, from_row, src), h, src);
@@ -259,7 +259,7 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
             for (int e = 0; e < 4; ++e) {
                 if (k[e] == kNoKey || ((k[e] ^ thr[0]) & above) != 0u || (digit > 4 && !agrees_beyond_score(digit, j + e))) continue;
                 const int x = atomicAdd(&sh.count, 1);
-                if (x < kShort) { sh.list_key[x] = k[e]; sh.list_pos[x] = pos_at(j + e); sh.list_slot[x] = j + e; }
+                if (A2SF_IN_RANGE(x, kShort, kDbgPagedEvict) && x < kShort) { sh.list_key[x] = k[e]; sh.list_pos[x] = pos_at(j + e); sh.list_slot[x] = j + e; }
             }
         }
         __syncthreads();
@@ -305,7 +305,7 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
             for (int j0 = w0; j0 < w1; j0 += 32) {
                 const unsigned s = mask_of(j0);
                 const int k = at + __popc(s & lt);
-                if ((s >> lane & 1) && k < M) from[k] = j0 + lane;
+                if ((s >> lane & 1) && A2SF_IN_RANGE(k, M, kDbgPagedEvict) && k < M) from[k] = j0 + lane;
                 at += __popc(s);
             }
         } else {
@@ -315,8 +315,8 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
                 const unsigned in = j0 + 32 <= w1 ? 0xffffffffu : (1u << (w1 - j0)) - 1u;
                 const unsigned lo = low(j0), holes = in & lo & ~s, ups = s & ~lo;
                 const int kh = hole + __popc(holes & lt), ks = src + __popc(ups & lt);
-                if ((holes >> lane & 1) && kh < M) to[kh] = j0 + lane;
-                if ((ups >> lane & 1) && ks < M) from[ks] = j0 + lane;
+                if ((holes >> lane & 1) && A2SF_IN_RANGE(kh, M, kDbgPagedEvict) && kh < M) to[kh] = j0 + lane;
+                if ((ups >> lane & 1) && A2SF_IN_RANGE(ks, M, kDbgPagedEvict) && ks < M) from[ks] = j0 + lane;
                 hole += __popc(holes);
                 src += __popc(ups);
             }

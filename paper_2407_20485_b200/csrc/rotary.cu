@@ -69,11 +69,13 @@ rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ Rota
     const bool rotates = item < rot_items;
     const int a_off = rotates ? item * W : r_dim + (item - rot_items) * W;
     const int b_off = item * W + r_dim / 2;                 // split layout only
+    if (!A2SF_IN_RANGE(a_off + W - 1, r.d, kDbgRotary) || (!Interleaved && rotates && !A2SF_IN_RANGE(b_off + W - 1, r.d, kDbgRotary))) return;
     float cs[NP], sn[NP];
     if (rotates) {
 #pragma unroll
         for (int e = 0; e < NP; ++e) {
             const int k = Interleaved ? item * NP + e : item * W + e;
+            if (!A2SF_IN_RANGE(k, A2SF_ROTARY_MAX_PAIRS, kDbgRotary)) return;
             const unsigned long long turn = plan.turn[k] * (unsigned long long)(long long)pos;
             const float x = (float)(int)(turn >> 32) * (1.f / 2147483648.f);       // half turns in [-1, 1]
             sincospif(x, &sn[e], &cs[e]);

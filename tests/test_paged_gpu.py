@@ -4,6 +4,7 @@ Tolerances count roundings.  u = torch.finfo(dtype).eps / 2 is the half step of 
 of fp32.  A logit is a sum of d products in fp32: off by at most (d + 2) f * sum|q k| * scale =: e.  A probability is
 then off by 2 e + 2^-20 relatively (its own logit, its row's log-sum-exp, the exponential)."""
 import math
+import random
 
 import pytest
 import torch
@@ -250,6 +251,20 @@ def test_attend(a2sf, case):
     assert torch.equal(cache.scores.nan_to_num(7.0), first.nan_to_num(7.0))
 
 
+@pytest.mark.parametrize("seed", range(40))
+def test_attend_random_cases(a2sf, seed):
+    check_attend(a2sf, random_attend(random.Random(seed)), seed=seed + 100)
+
+
+def random_attend(r):
+    B, H, G = r.choice([1, 1, 2, 3, 6]), r.choice([1, 2, 3]), r.choice([1, 1, 2, 3, 4, 5, 6, 7, 8])
+    c = r.choice([1, 1, 2, 16 // G, 16 // G + 1, int(2 ** r.uniform(1, 9)), 128 // G, 256 // G + 1])
+    past = [int(2 ** r.uniform(0, 10)) - 1 if r.random() < 0.9 else 0 for _ in range(B)]
+    lens = [r.choice([c, c, c, 0, r.randint(0, c)]) for _ in range(B)]
+    return (B, H, G, r.choice([64, 128]), r.choice([FP, BF, BF, HF]), r.choice([16, 32, 64, 128]), past, max(1, c), lens,
+            r.choice([0.0, 0.3, 0.5, 0.9, 0.99, 1.0]), r.choice(["bhnd", "bnhd"]), r.choice([0.0, 0.0, 0.2]))
+
+
 @pytest.mark.parametrize("dtype,c,past", [(BF, 1, 600), (HF, 1, 600), (FP, 1, 100), (BF, 150, 200), (HF, 150, 200), (HF, 4, 300)])
 def test_attend_large_logits_and_late_maximum(a2sf, dtype, c, past):
     """Queries 12 times the usual size: logits of +-100, rows that one key takes whole, maxima that come late."""
@@ -306,15 +321,14 @@ EVI = [
 ]
 
 
-@pytest.mark.parametrize("case", EVI, ids=lambda c: "-".join(str(x).replace("torch.", "").replace(" ", "") for x in c))
-def test_evict(a2sf, case):
+def check_evict(a2sf, case, seed=3):
     B, H, d, dtype, ps, past, c, budget, recent, fresh, kind = case
     n = [p + c for p in past]
-    cache = pu.make_cache(a2sf, B, H, 1, d, dtype, ps, n, 0, seed=3)         # the chunk is in place already
+    cache = pu.make_cache(a2sf, B, H, 1, d, dtype, ps, n, 0, seed=seed)      # the chunk is in place already
     cache.past.copy_(torch.tensor(past, dtype=torch.int32))
     start = [p + 1000 for p in past]
     cache.start.copy_(torch.tensor(start, dtype=torch.int32))
-    g = torch.Generator().manual_seed(8)
+    g = torch.Generator().manual_seed(seed + 5)
     sc = torch.rand(cache.scores.shape, generator=g)
     if kind == "zeros":
         sc.zero_()
@@ -369,6 +383,30 @@ def test_evict(a2sf, case):
             assert torch.equal(got.double().nan_to_num(1e9), want[x].double().nan_to_num(1e9)), x
         else:
             assert torch.equal(got, want[x]), x
+
+
+@pytest.mark.parametrize("case", EVI, ids=lambda c: "-".join(str(x).replace("torch.", "").replace(" ", "") for x in c))
+def test_evict(a2sf, case):
+    check_evict(a2sf, case)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_evict_random_cases(a2sf, seed):
+    check_evict(a2sf, random_evict(random.Random(seed)), seed=seed + 50)
+
+
+def random_evict(r):
+    B, H, c = r.choice([1, 2, 3, 5]), r.choice([1, 2, 3]), r.choice([1, 2, 7, 40])
+    past = [int(2 ** r.uniform(0, 10.5)) - 1 for _ in range(B)]
+    budget = max(1, int((max(past) + c) * r.uniform(0.05, 1.1)))
+    return (B, H, r.choice([64, 128]), r.choice([FP, BF, HF]), r.choice([16, 32, 64, 128]), past, c, budget, r.choice([0, budget // 2, budget]),
+            r.random() < 0.5, r.choice(["rand", "zeros", "ties", "signed"]))
+
+
+def test_evict_of_many_heads_moves_rows_in_the_searching_blocks(a2sf):
+    """More heads than the device has SMs twice over: the other form of the kernel, in place and into fresh pages."""
+    for fresh in (False, True):
+        check_evict(a2sf, (7, 47, 64, BF, 16, [40, 3, 0, 25, 90, 64, 33], 3, 30, 10, fresh, "ties"), seed=17)
 
 
 def test_evict_with_positions_given_twice_keeps_exactly_the_budget(a2sf):
@@ -484,3 +522,93 @@ def test_bad_pages_and_lengths_are_reported_and_not_followed(a2sf, dtype, c, bad
     if bad not in ("past", "negative", "length"):
         assert torch.equal(cache.v_pages[others], guard["v_pages"][others])
         assert torch.equal(cache.positions[others], guard["positions"][others])
+
+
+# ---- large and together ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,c", [(BF, 1), (HF, 130), (FP, 1)])
+def test_rows_beyond_32_bit_offsets(a2sf, dtype, c):
+    """Pages at the end of a pool of more than 2^31 elements give what the same pages give in a small pool."""
+    H, d, ps, past = 8, 128, 128, 300
+    pages = (2 ** 31) // (H * ps * d) + 40
+    rows = torch.arange(past + c)
+    far = (pages - 1 - torch.arange(4)).to(torch.int32).view(1, 4).cuda()
+    near = torch.tensor([[2, 0, 3, 1]], dtype=torch.int32).cuda()
+    g = torch.Generator().manual_seed(5)
+    k, v, q = (torch.randn((1, H, past, d), generator=g).to(dtype).cuda(), torch.randn((1, H, past, d), generator=g).to(dtype).cuda(),
+               torch.randn((1, H, past, d), generator=g).to(dtype).cuda())
+    plan = a2sf.a2sf_rotary_plan_init(d)
+    results = []
+    for n_pages, table in ((pages, far), (4, near)):
+        cache = a2sf.PagedCache(1, H, d, dtype, ps, n_pages, 4, page_table=table)
+        cache.a2sf_paged_append(k, v)
+        cache.a2sf_paged_evict(past, 0, past)
+        part = slice(0, c)
+        q2 = cache.a2sf_paged_append(k[:, :, part], v[:, :, part], q=q[:, :, part], rotary=plan)
+        out, lse = cache.a2sf_paged_attend(q2, 0.9)
+        scores = pu.slots(cache, cache.scores.cpu(), 0, past + c)
+        cache.a2sf_paged_evict(200, 50, c)
+        t = cache.page_table[0].long()
+        pool = [x[t].cpu() for x in (cache.k_pages, cache.v_pages, cache.positions)]
+        results.append([out.cpu(), lse.cpu(), scores] + [x.transpose(1, 2).reshape(4 * ps, H, -1)[:200] for x in pool])
+        del cache
+    assert len(rows) == past + c
+    for x, y in zip(*results):
+        assert torch.equal(x, y)
+
+
+def test_calls_on_two_streams_at_once(a2sf):
+    """Chunks and tokens of two caches, issued alternately on two streams with no order between them."""
+    B, H, G, d = 2, 4, 2, 128
+    g = torch.Generator().manual_seed(31)
+    data = [[torch.randn((B, h, c, d), generator=g).to(BF).cuda() for h in (H * G, H, H)] for c in (300, 1, 40, 1, 200, 3)]
+
+    def run(cache, streams, results):
+        for q, k, v in data:
+            with torch.cuda.stream(streams):
+                cache.a2sf_paged_append(k, v)
+                results.append(cache.a2sf_paged_attend(q, 0.9))
+                cache.a2sf_paged_evict(250, 30, q.shape[2])
+            yield
+
+    caches = [pu.make_cache(a2sf, B, H, G, d, BF, 32, [100, 7], 600, seed=6) for _ in range(3)]
+    torch.cuda.synchronize()
+    alone, one, two = [], [], []
+    for _ in run(caches[0], torch.cuda.current_stream(), alone):
+        pass
+    torch.cuda.synchronize()
+    for _ in zip(run(caches[1], torch.cuda.Stream(), one), run(caches[2], torch.cuda.Stream(), two)):
+        pass
+    torch.cuda.synchronize()
+    for a, b, c in zip(alone, one, two):
+        for x, y, z in zip(a, b, c):
+            assert torch.equal(x, y) and torch.equal(x, z)
+
+
+def test_a_stream_given_and_inputs_from_another(a2sf):
+    """The stream argument: work is queued there, behind what that stream waits for."""
+    x = torch.zeros((1, 2, 5, 64), device="cuda")
+    plan = a2sf.a2sf_rotary_plan_init(64)
+    side, main = torch.cuda.Stream(), torch.cuda.current_stream()
+    big = torch.randn((4096, 4096), device="cuda")
+    for _ in range(20):
+        big = big @ big * 1e-4                      # keeps the current stream busy
+    x.copy_(torch.ones_like(x))
+    side.wait_stream(main)
+    out = torch.zeros_like(x)
+    side.wait_stream(main)
+    a2sf.a2sf_rotary(plan, x, out=out, stream=side)
+    main.wait_stream(side)
+    want = pu.rotate(torch.ones((1, 2, 5, 64), dtype=torch.float64), torch.arange(5), pu.inv_freq(64))
+    close(out, want, torch.full_like(want, 8 * (2e-7 + 4 * F)), "rotary on a side stream")
+
+
+def test_the_largest_batch_with_mostly_empty_sequences(a2sf):
+    B = 1024
+    past = [0] * B
+    lens = [0] * B
+    for b, (p, n) in {0: (5, 1), 17: (100, 1), 500: (0, 1), 1023: (33, 1)}.items():
+        past[b], lens[b] = p, n
+    check_attend(a2sf, (B, 1, 1, 64, BF, 16, past, 1, lens, 0.5, "bhnd", 0.0))
+    lens = [20 * n for n in lens]
+    check_attend(a2sf, (B, 1, 1, 64, HF, 16, past, 20, lens, 0.5, "bhnd", 0.0))

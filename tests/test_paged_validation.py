@@ -38,7 +38,7 @@ def _append(a2sf, p, plan=None, c=5, k=OK, v=OK, skv=SKV, q=None, q_out=None, sq
                                       k, v, *skv, q, *sq, q_out, *so, None)
 
 
-def _attend(a2sf, p, c=5, alpha=0.5, q=OK, sq=S, out=OK, so=S, lse=None, flags=0, ws=OK, nbytes=1 << 40, lens=None):
+def _attend(a2sf, p, c=5, alpha=0.5, q=OK, sq=S, out=OK + 4096, so=S, lse=None, flags=0, ws=OK, nbytes=1 << 40, lens=None):
     return a2sf.lib.a2sf_paged_attend(ctypes.byref(p) if p is not None else None, c, lens, alpha, q, *sq, out, *so, lse, flags, ws, nbytes, None)
 
 
@@ -73,7 +73,7 @@ def test_bad_arguments_of_the_calls(a2sf):
         assert _append(a2sf, p, **bad) == INVALID, bad
     assert _append(a2sf, _paged(a2sf, d=64), plan=plan) == INVALID                                        # rotary_dim > d
     for bad in (dict(c=0), dict(alpha=-0.1), dict(alpha=1.1), dict(alpha=float("nan")), dict(q=None), dict(out=None), dict(q=ODD),
-                dict(sq=(S[0], S[1], 64)), dict(so=(S[0], 1, 128)), dict(flags=2), dict(lse=OK + 2), dict(ws=None), dict(ws=OK + 128)):
+                dict(out=OK), dict(sq=(S[0], S[1], 64)), dict(so=(S[0], 1, 128)), dict(flags=2), dict(lse=OK + 2), dict(ws=None), dict(ws=OK + 128)):
         assert _attend(a2sf, p, **bad) == INVALID, bad
     assert _attend(a2sf, p, nbytes=16) == WORKSPACE
     for bad in (dict(budget=0), dict(recent=-1), dict(recent=101), dict(past=None), dict(start=None), dict(past=OK, start=OK),
