@@ -465,55 +465,33 @@ def a2sf_rotary_plan_init(rotary_dim: int, theta: float = 10000.0, interleaved: 
     return plan
 
 
-def _rows(t, shape, dtype, index, name):
-    """Address and strides of a [B,H,n,d] tensor of the call, on CUDA device ``index``."""
-    st = t.stride()
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or st[3] != 1:
-        raise ValueError(f"{name}: expected {tuple(shape)} {dtype} on CUDA device {index} with contiguous rows, got "
-                         f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {st}")
-    return t.data_ptr(), st[0], st[1], st[2]
+def _load_calls():
+    """The extension that marshals torch tensors for the calls below (see csrc/torch_calls.cpp)."""
+    import importlib.util
+
+    path = Path(__file__).resolve().parent / "_torch_calls.so"
+    if not path.exists():
+        raise ImportError(f"{path} is missing: build it with `python -m paper_2407_20485_b200.build`")
+    spec = importlib.util.spec_from_file_location("_torch_calls", path)
+    calls = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(calls)
+    calls.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+        "a2sf_rotary", "a2sf_paged_append", "a2sf_paged_attend", "a2sf_paged_attend_workspace_bytes", "a2sf_paged_evict",
+        "a2sf_paged_evict_workspace_bytes")})
+    return calls
 
 
-def _ints(t, shape, index, name):
-    """Address of an int32 array of the call (None: NULL)."""
-    if t is None:
-        return None
-    if t.dtype is not _I32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
-        raise ValueError(f"{name}: expected contiguous int32 {shape} on CUDA device {index}, got {t.dtype} {tuple(t.shape)} "
-                         f"on {t.device}")
-    return t.data_ptr()
-
-
-# address of a device's current stream without the Stream object around it (1.2 us less per call)
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-_I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
-
-
-def _call(index, stream, fn, name, *args):
-    """A library call on CUDA device ``index``, on ``stream`` or that device's current stream."""
-    if index < 0:
-        raise ValueError(f"{name}: tensors must be on a CUDA device")
-    handle = _raw_stream(index) if stream is None else stream.cuda_stream
-    if index == _current_device():
-        status = fn(*args, handle)
-    else:
-        with torch.cuda.device(index):
-            status = fn(*args, handle)
-    if status != A2SF_OK:
-        raise A2SFError(status, name)
+_calls = _load_calls()
+_addressof = ctypes.addressof
 
 
 def a2sf_rotary(plan: a2sf_rotary_plan, x, out=None, positions=None, start=None, lens=None, transpose=False, stream=None):
     """x [B,H,n,d] rotated by its positions (``positions`` [B,n], or ``start`` [B] + t, or t).  ``out`` may be x."""
-    shape, dtype, index = x.shape, x.dtype, x.get_device()
-    B, H, n, d = shape
     if out is None:
-        out = torch.empty_strided(shape, x.stride(), dtype=dtype, device=x.device)
-    _call(index, stream, lib.a2sf_rotary, "a2sf_rotary", ctypes.byref(plan), _DTYPE_CODE[dtype], B, H, n, d,
-          *_rows(x, shape, dtype, index, "x"), *_rows(out, shape, dtype, index, "out"),
-          _ints(positions, (B, n), index, "positions"), _ints(start, (B,), index, "start"),
-          _ints(lens, (B,), index, "lens"), A2SF_ROTARY_TRANSPOSE if transpose else 0)
+        out = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+    status = _calls.rotary(_addressof(plan), x, out, positions, start, lens, transpose, -1 if stream is None else stream.cuda_stream)
+    if status != A2SF_OK:
+        raise A2SFError(status, "a2sf_rotary")
     return out
 
 
@@ -550,74 +528,42 @@ class PagedCache:
         self.past = own(past, (B,), torch.int32, 0, "past")
         self.start = own(start, (B,), torch.int32, 0, "start")
         self.B, self.H, self.group, self.d, self.dtype, self.device = B, H, group, d, dtype, device
-        self._index = self.k_pages.get_device()             # -1: not on a CUDA device, calls are refused
         self.page_size, self.num_pages, self.max_pages = page_size, num_pages, max_pages
         self.p = a2sf_paged(B, H, group, d, _DTYPE_CODE[dtype], page_size, num_pages, max_pages, scale, 0,
                             *(t.data_ptr() for t in (self.k_pages, self.v_pages, self.scores, self.positions,
                                                      self.page_table, self.past, self.start)))
-        self._ref = ctypes.byref(self.p)
-        self._kv_heads, self._q_heads = H, H * group
-        self._nbytes = {}                                   # workspace sizes by call and argument
+        self._calls = _calls.Calls(_addressof(self.p), self.k_pages.get_device())   # -1: no CUDA device, calls are refused
 
     def a2sf_paged_append(self, k, v, lens=None, q=None, q_out=None, rotary=None, stream=None):
         """k, v [B,H,c,d] (one stride set) into slots past.. of their sequences; with a ``rotary`` plan keys are rotated
         on the way, and q [B,H*group,c,d] into ``q_out``, which is returned."""
-        c = k.shape[2]
-        kv = (self.B, self.H, c, self.d)
-        kr = _rows(k, kv, self.dtype, self._index, "k")
-        vr = _rows(v, kv, self.dtype, self._index, "v")
-        if kr[1:] != vr[1:]:
-            raise ValueError(f"k and v need the same strides, got {kr[1:]} and {vr[1:]}")
-        qr = qo = (None, 0, 0, 0)
-        if q is not None:
-            shape = (self.B, self.H * self.group, c, self.d)
-            qr = _rows(q, shape, self.dtype, self._index, "q")
-            if q_out is None:
-                q_out = torch.empty_strided(shape, q.stride(), dtype=self.dtype, device=self.device)
-            qo = _rows(q_out, shape, self.dtype, self._index, "q_out")
-        _call(self._index, stream, lib.a2sf_paged_append, "a2sf_paged_append", self._ref,
-              None if rotary is None else ctypes.byref(rotary), c, _ints(lens, (self.B,), self._index, "lens"), kr[0], *vr,
-              *qr, *qo)
+        status, q_out = self._calls.append(k, v, lens, q, q_out, 0 if rotary is None else _addressof(rotary),
+                                           -1 if stream is None else stream.cuda_stream)
+        if status != A2SF_OK:
+            raise A2SFError(status, "a2sf_paged_append")
         return q_out
 
     def a2sf_paged_attend(self, q, alpha=1.0, lens=None, out=None, lse=None, scores=True, workspace=None, stream=None):
         """Attention of q [B,H*group,c,d] over the cache and the chunk appended before; returns (out, lse).  The cache's
         scores are decayed and added to unless ``scores`` is False."""
-        c = q.shape[2]
-        shape = (self.B, self.H * self.group, c, self.d)
-        qr = _rows(q, shape, self.dtype, self._index, "q")
-        if out is None:
-            out = torch.empty_strided(shape, q.stride(), dtype=self.dtype, device=self.device)
-        if lse is None:
-            lse = torch.empty(shape[:3], dtype=torch.float32, device=self.device)
-        elif lse.shape != shape[:3] or lse.dtype is not torch.float32 or lse.get_device() != self._index or not lse.is_contiguous():
-            raise ValueError(f"lse: expected contiguous float32 {shape[:3]} on {self.device}")
-        if workspace is None:
-            workspace = self._workspace(lib.a2sf_paged_attend_workspace_bytes, "a2sf_paged_attend_workspace_bytes", c)
-        _call(self._index, stream, lib.a2sf_paged_attend, "a2sf_paged_attend", self._ref, c,
-              _ints(lens, (self.B,), self._index, "lens"), alpha, *qr, *_rows(out, shape, self.dtype, self._index, "out"),
-              lse.data_ptr(), 0 if scores else A2SF_ATTEND_NO_SCORES, workspace.data_ptr(), workspace.numel())
+        status, out, lse = self._calls.attend(q, alpha, lens, out, lse, scores, workspace, -1 if stream is None else stream.cuda_stream)
+        if status != A2SF_OK:
+            raise A2SFError(status, "a2sf_paged_attend")
         return out, lse
 
     def a2sf_paged_evict(self, budget: int, recent: int, c: int = 1, lens=None, dst_table=None, past_out=None,
                          start_out=None, workspace=None, stream=None):
         """Ends a step whose chunk had ``lens`` (or c) tokens: every head back to ``budget`` slots, in place or into the
         pages of ``dst_table`` [B, any].  ``past`` and ``start`` move on (or ``past_out`` and ``start_out`` get the values)."""
-        past_out = self.past if past_out is None else past_out
-        start_out = self.start if start_out is None else start_out
-        pages = 0 if dst_table is None else dst_table.shape[1]
-        if workspace is None:
-            workspace = self._workspace(lib.a2sf_paged_evict_workspace_bytes, "a2sf_paged_evict_workspace_bytes", budget)
-        _call(self._index, stream, lib.a2sf_paged_evict, "a2sf_paged_evict", self._ref, c,
-              _ints(lens, (self.B,), self._index, "lens"), budget, recent, _ints(dst_table, (self.B, pages), self._index, "dst_table"),
-              pages, _ints(past_out, (self.B,), self._index, "past_out"), _ints(start_out, (self.B,), self._index, "start_out"),
-              workspace.data_ptr(), workspace.numel())
+        status = self._calls.evict(budget, recent, c, lens, dst_table, self.past if past_out is None else past_out,
+                                   self.start if start_out is None else start_out, workspace,
+                                   -1 if stream is None else stream.cuda_stream)
+        if status != A2SF_OK:
+            raise A2SFError(status, "a2sf_paged_evict")
 
-    def _workspace(self, query, name, arg):
-        nbytes = self._nbytes.get((name, arg))
-        if nbytes is None:
-            nbytes = int(query(self._ref, arg))
-            if nbytes == 0:
-                raise A2SFError(A2SF_ERR_INVALID_ARG, name)
-            self._nbytes[name, arg] = nbytes
-        return torch.empty((nbytes,), dtype=_U8, device=self.device)
+    def attend_workspace_bytes(self, c: int) -> int:
+        """Size of a workspace for chunks of c tokens (0: invalid arguments)."""
+        return int(lib.a2sf_paged_attend_workspace_bytes(ctypes.byref(self.p), c))
+
+    def evict_workspace_bytes(self, budget: int) -> int:
+        return int(lib.a2sf_paged_evict_workspace_bytes(ctypes.byref(self.p), budget))

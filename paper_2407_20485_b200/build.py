@@ -19,6 +19,8 @@ CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 OBJ_DIR = PKG / "_build"
 LIB_PATH = PKG / "liba2sf.so"
+CALLS_SRC = CSRC / "torch_calls.cpp"
+CALLS_PATH = PKG / "_torch_calls.so"
 DEBUG_OBJ_DIR = PKG / "_build_debug"
 DEBUG_LIB_PATH = PKG / "liba2sf_debug.so"
 
@@ -44,12 +46,36 @@ def _deps_mtime() -> float:
     return max(f.stat().st_mtime for f in files)
 
 
+def build_calls(force: bool = False) -> Path:
+    """Compile ``_torch_calls.so``, the Python extension that marshals torch tensors (host code only)."""
+    newest = max(CALLS_SRC.stat().st_mtime, *(f.stat().st_mtime for f in INCLUDE.glob("*.h")))
+    if not force and CALLS_PATH.exists() and CALLS_PATH.stat().st_mtime >= newest:
+        return CALLS_PATH
+    import sysconfig
+
+    import torch
+
+    root = Path(torch.__file__).resolve().parent
+    cuda = Path(_nvcc()).resolve().parent.parent / "include"
+    tmp = CALLS_PATH.with_suffix(f".tmp{os.getpid()}.so")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-o", str(tmp), str(CALLS_SRC),
+           *(f"-I{p}" for p in (root / "include", root / "include/torch/csrc/api/include", cuda, sysconfig.get_paths()["include"])),
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f"-L{root / 'lib'}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, CALLS_PATH)
+    return CALLS_PATH
+
+
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> Path:
     """Compile every ``csrc/*.cu`` and link the shared library (the bounds-checked one with
     ``debug``).  Returns its path."""
     obj_dir, lib_path = (DEBUG_OBJ_DIR, DEBUG_LIB_PATH) if debug else (OBJ_DIR, LIB_PATH)
     extra = ["-DA2SF_DEBUG"] if debug else []
     obj_dir.mkdir(exist_ok=True)
+    build_calls(force)
     nvcc = _nvcc()
     hdr_m = _deps_mtime()
     jobs = []

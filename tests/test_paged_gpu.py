@@ -206,7 +206,9 @@ def check_attend(a2sf, case, seed=5, garbage=float("nan"), gain=1.0):
     old = cache.scores.cpu().clone()
     pool_k, pool_v = cache.k_pages.cpu().double(), cache.v_pages.cpu().double()
     out, lse = torch.full_like(qc, 3.0), torch.full((B, H * G, c), 3.0, device="cuda")
-    cache.a2sf_paged_attend(qc, alpha, lens=L, out=out, lse=lse)
+    # the binding's torch: in the debug sweep it puts guard words around the workspace
+    cache.a2sf_paged_attend(qc, alpha, lens=L, out=out, lse=lse, workspace=a2sf.torch.empty(
+        (cache.attend_workspace_bytes(c),), dtype=torch.uint8, device="cuda"))
     torch.cuda.synchronize()
     sc = scale or 1 / math.sqrt(d)
     u = torch.finfo(dtype).eps / 2
@@ -374,7 +376,8 @@ def check_evict(a2sf, case, seed=3):
             for x in want:
                 for f, t in moves:
                     want[x][to_table[t // ps], h, t % ps] = before[x][table[b, f // ps], h, f % ps]
-    cache.a2sf_paged_evict(budget, recent, c, dst_table=None if dst is None else dst.cuda())
+    cache.a2sf_paged_evict(budget, recent, c, dst_table=None if dst is None else dst.cuda(), workspace=a2sf.torch.empty(
+        (cache.evict_workspace_bytes(budget),), dtype=torch.uint8, device="cuda"))
     assert cache.past.tolist() == [min(x, budget) for x in n]
     assert cache.start.tolist() == [s + c for s in start]
     for x in want:
