@@ -135,14 +135,16 @@ __device__ __forceinline__ void next_unit(Where &x, const int32_t *prefix, int B
 }
 
 // ---- kernels of one call follow each other by programmatic launch ----------------------------------
-// A follower is resident, its barriers and descriptors set up, while its predecessor drains; it waits
-// with dependency_wait() before it touches anything that any earlier kernel wrote.  Every kernel of such a
-// chain waits, so a kernel that runs has all its predecessors behind it, not only the last one.
+// A kernel is resident, its barriers and descriptors set up, while its predecessor drains; it waits
+// with dependency_wait() before it touches anything that any earlier kernel wrote.  Every kernel waits, and
+// lets its followers start only after that, so behind a kernel that has waited lie all its predecessors, not
+// only the last one.  The first kernel of a call waits before it reads anything (what runs before it in the
+// stream may be anybody's); the following ones may read what no kernel of the call writes without waiting.
 __device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 template <typename... Params, typename... Args>
-cudaError_t launch_follower(void (*kernel)(Params...), unsigned grid, unsigned threads, size_t smem, cudaStream_t s, Args... args)
+cudaError_t launch_chained(void (*kernel)(Params...), unsigned grid, unsigned threads, size_t smem, cudaStream_t s, Args... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);

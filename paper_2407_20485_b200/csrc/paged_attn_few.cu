@@ -386,8 +386,10 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             prefetch_tmap(&map_k);
             prefetch_tmap(&map_v);
         }
+        dependency_wait();
         tile_prefix<kTile>(sh.prefix, pv);
     }
+    if (warp != 0) dependency_wait();
     __syncthreads();
     if (blockIdx.x == 0)
         for (int b = threadIdx.x; b <= pv.B; b += kFewThreads) ws.prefix[b] = sh.prefix[b];
@@ -666,9 +668,8 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     const int NP = rows_padded(a.pv.c * a.pv.G);
     const int ctas = device_sm_count() * (2 * (smem + sizeof(FewShared) + 1024) <= 228 * 1024 ? 2 : 1);   // what is resident
     if (ctas < 1 || ctas > 512) return cudaErrorInvalidValue;
-    paged_few_kernel<T, D, NC><<<ctas, kFewThreads, smem, s>>>(mk, mv, a, ws, NP);
+    if ((e = launch_chained(paged_few_kernel<T, D, NC>, ctas, kFewThreads, smem, s, mk, mv, a, ws, NP)) != cudaSuccess) return e;
     count_launch();
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
     // blocks per unit: enough for the rows and the slots, as far as that fills the device
     const int cap = a.pv.max_pages << a.pv.ps_shift;
     const long long units = (long long)a.pv.B * a.pv.H;
@@ -679,7 +680,7 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     const int chunk = ((cap + blocks - 1) / blocks + 31) / 32 * 32;
     const long long grid = units * blocks;
     if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
-    auto finish = [&](auto kernel) { return launch_follower(kernel, (unsigned)grid, kFinishThreads, 0, s, a, ws, ctas, blocks, chunk); };
+    auto finish = [&](auto kernel) { return launch_chained(kernel, (unsigned)grid, kFinishThreads, 0, s, a, ws, ctas, blocks, chunk); };
     switch (NP) {
     case 1: e = finish(paged_few_finish_kernel<T, D, 1>); break;
     case 2: e = finish(paged_few_finish_kernel<T, D, 2>); break;

@@ -119,6 +119,7 @@ paged_attn_simt_kernel(const __grid_constant__ AttendArgs a, int row_tiles)
     extern __shared__ __align__(16) float sm[];
     float *Q = sm, *K = Q + kR * LD, *V = K + 2 * Lay<D>::kTileFloats, *P = V + 2 * Lay<D>::kTileFloats;
     const int G = a.pv.G;
+    dependency_wait();
     dependents_may_start();
     const Unit u = make_unit(a.pv, blockIdx.x / row_tiles);
     // the tiles that see most slots first
@@ -303,10 +304,10 @@ cudaError_t launch(const AttendArgs &a, cudaStream_t s)
     const long long row_tiles = ((long long)a.pv.c * a.pv.G + 16 * T - 1) / (16 * T);
     const long long slot_tiles = (((long long)a.pv.max_pages << a.pv.ps_shift) + 16 * T - 1) / (16 * T);
     if (units * row_tiles > 0x7fffffffll || units * slot_tiles > 0x7fffffffll) return cudaErrorInvalidValue;
-    paged_attn_simt_kernel<D, T><<<(unsigned)(units * row_tiles), kThreads, attn, s>>>(a, (int)row_tiles);
+    if ((e = launch_chained(paged_attn_simt_kernel<D, T>, (unsigned)(units * row_tiles), kThreads, attn, s, a, (int)row_tiles)) != cudaSuccess) return e;
     count_launch();
-    if ((e = cudaGetLastError()) != cudaSuccess || !a.scores) return e;
-    e = launch_follower(paged_score_simt_kernel<D, T>, (unsigned)(units * slot_tiles), kThreads, score, s, a, (int)slot_tiles);
+    if (!a.scores) return cudaSuccess;
+    e = launch_chained(paged_score_simt_kernel<D, T>, (unsigned)(units * slot_tiles), kThreads, score, s, a, (int)slot_tiles);
     if (e == cudaSuccess) count_launch();
     return e;
 }

@@ -90,6 +90,7 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
     __shared__ float cand_cost[kCandidates], warp_work[kPlanWarps];
     __shared__ SeqState seqs[A2SF_PAGED_MAX_SEQUENCES];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    dependency_wait();
     dependents_may_start();
     if (tid < kLevels) level[tid] = 0;
     if (tid == 0) { n_parts = 0; n_merges = 0; }
@@ -1215,19 +1216,18 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
         return cudaErrorInvalidValue;
     const TcWs ws = carve(a.pv, a.ws, nullptr);
     if ((long long)ws.max_items * a.pv.H > 0x7fffffffll) return cudaErrorInvalidValue;
-    paged_plan_kernel<<<1, kPlanThreads, 0, s>>>(a.pv, ws);
+    if ((e = launch_chained(paged_plan_kernel, 1, kPlanThreads, 0, s, a.pv, ws)) != cudaSuccess) return e;
     count_launch();
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    e = launch_follower(paged_attn_tc_kernel<T, D>, kSms, kAttnThreads, attn_smem<D>(), s, mq, mk, mv, a, ws);
+    e = launch_chained(paged_attn_tc_kernel<T, D>, kSms, kAttnThreads, attn_smem<D>(), s, mq, mk, mv, a, ws);
     if (e != cudaSuccess) return e;
     count_launch();
-    if ((e = launch_follower(paged_merge_kernel<T, D>, 4 * kSms, kMergeThreads, 0, s, a, ws)) != cudaSuccess) return e;
+    if ((e = launch_chained(paged_merge_kernel<T, D>, 4 * kSms, kMergeThreads, 0, s, a, ws)) != cudaSuccess) return e;
     count_launch();
     if (!a.scores) return cudaSuccess;
-    e = launch_follower(paged_score_tc_kernel<D>, kScoreCtas, kScoreThreads, score_smem<D>(), s, mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
+    e = launch_chained(paged_score_tc_kernel<D>, kScoreCtas, kScoreThreads, score_smem<D>(), s, mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
     if (e != cudaSuccess) return e;
     count_launch();
-    if ((e = launch_follower(paged_score_join_kernel, kScoreCtas - 1, kBlk, 0, s, a, ws)) != cudaSuccess) return e;
+    if ((e = launch_chained(paged_score_join_kernel, kScoreCtas - 1, kBlk, 0, s, a, ws)) != cudaSuccess) return e;
     count_launch();
     return cudaSuccess;
 }

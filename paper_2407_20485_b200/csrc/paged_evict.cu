@@ -128,6 +128,7 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
     __shared__ SelShared sh;
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = u / a.pv.H, h = u - b * a.pv.H;
+    dependency_wait();
     dependents_may_start();
     const SeqState st = seq_state(a.pv, b);
     const int n = st.past + st.len, M = a.M;
@@ -387,10 +388,10 @@ cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int re
     a.blocks = (int)blocks;
     const unsigned grid = blocks ? (unsigned)(units * blocks) : 1u;
     auto run = [&](auto select, auto move) -> cudaError_t {
-        select<<<(unsigned)units, kSelThreads, smem, s>>>(a, cached);
+        cudaError_t e = launch_chained(select, (unsigned)units, kSelThreads, smem, s, a, cached);
+        if (e != cudaSuccess) return e;
         count_launch();
-        cudaError_t e = cudaGetLastError();
-        if (e == cudaSuccess) e = launch_follower(move, grid, kMoveThreads, 0, s, a);
+        e = launch_chained(move, grid, kMoveThreads, 0, s, a);
         if (e == cudaSuccess) count_launch();
         return e;
     };

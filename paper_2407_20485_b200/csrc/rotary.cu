@@ -43,11 +43,14 @@ template <typename T, int W, bool Interleaved, bool Append>
 __global__ void __launch_bounds__(kRotThreads, 4)
 rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ RotaryArgs r,
               const __grid_constant__ PagedView pv, int r_dim, float magnitude, int rot_items, int items,
-              int heads_per_block)
+              int heads_per_block, int splits)
 {
     constexpr int NP = Interleaved ? (W + 1) / 2 : W;        // pairs of an item
     using P = Pack<T, W>;
-    const long long idx = (long long)blockIdx.x * kRotThreads + threadIdx.x;
+    dependency_wait();
+    dependents_may_start();
+    const int split = blockIdx.x % splits;
+    const long long idx = (long long)(blockIdx.x / splits) * kRotThreads + threadIdx.x;
     const long long tok = idx / items;
     const int item = (int)(idx - tok * items);
     if (tok >= (long long)r.B * r.n) return;
@@ -90,7 +93,7 @@ rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ Rota
         if (page >= 0) page_row = pool_row(pv, page, 0, slot);
     }
     const int total = r.Hq + (Append ? 2 * r.Hk : 0);
-    const int h0 = blockIdx.y * heads_per_block, h1 = min(total, h0 + heads_per_block);
+    const int h0 = split * heads_per_block, h1 = min(total, h0 + heads_per_block);
 
     for (int hb = h0; hb < h1; hb += kHeads) {
         const T *src[kHeads];
@@ -163,11 +166,12 @@ cudaError_t launch_w(const a2sf_rotary_plan *plan, const RotaryArgs &r, const Pa
     const long long want = 16ll * device_sm_count();
     const long long gy = (want + gx - 1) / gx;
     const int hpb = (int)(((total + gy - 1) / gy + kHeads - 1) / kHeads) * kHeads;
-    const dim3 grid((unsigned)gx, (unsigned)((total + hpb - 1) / hpb));
-    rotary_kernel<T, W, Interleaved, Append><<<grid, kRotThreads, 0, s>>>(
-        pa, r, pv, r_dim, plan ? plan->magnitude : 1.f, rot_items, items, hpb);
-    count_launch();
-    return cudaGetLastError();
+    const int splits = (total + hpb - 1) / hpb;
+    if (gx * splits > 0x7fffffffll) return cudaErrorInvalidValue;
+    const cudaError_t e = launch_chained(rotary_kernel<T, W, Interleaved, Append>, (unsigned)(gx * splits), kRotThreads, 0, s, pa, r, pv, r_dim,
+                                         plan ? plan->magnitude : 1.f, rot_items, items, hpb, splits);
+    if (e == cudaSuccess) count_launch();
+    return e;
 }
 
 template <typename T, bool Append>

@@ -468,9 +468,13 @@ def test_graph_replay_and_other_stream(a2sf, dtype, c, past):
     a, b = (pu.make_cache(a2sf, B, H, G, d, dtype, 32, [past, past // 2], 2 * c, seed=6) for _ in range(2))
 
     def step(cache, q, k, v, q2, out, lse):
-        cache.a2sf_paged_append(k, v, q=q, q_out=q2, rotary=plan)
+        # other kernels before, between and after the library's
+        cache.a2sf_paged_append(k * 0.5, v.clone(), q=q, q_out=q2, rotary=plan)
+        q2.mul_(2.0)
         cache.a2sf_paged_attend(q2, 0.9, out=out, lse=lse)
+        cache.scores.mul_(0.75)
         cache.a2sf_paged_evict(M, 8, c)
+        cache.start.add_(1)
 
     q, k, v = (x.clone() for x in ins[0])
     q2, out, lse = torch.empty_like(q), torch.empty_like(q), torch.empty((B, H * G, c), device="cuda")
