@@ -24,6 +24,7 @@ constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kCached = 16384;       // slots whose score key and position fit in shared memory
 constexpr int kMaskWords = 1024;     // survivors' mask: 32768 slots; beyond, it is worked out again where it is needed
 constexpr int kShort = 64;           // slots that are ranked directly
+constexpr int kFewDrops = 8;         // as many slots leave one minimum after the other
 constexpr int kInline = 64;          // moves that the searching CTA makes itself in any case
 constexpr int kRows = 4;             // rows of a lane group in flight
 
@@ -58,6 +59,8 @@ struct SelShared {
     int list_slot[kShort];
     unsigned thr_key, thr_pos;
     int thr_slot;
+    unsigned long long low_key[2][kSelWarps];
+    int low_slot[2][kSelWarps], leaving[kFewDrops];
     unsigned mask[kMaskWords];
 };
 
@@ -185,143 +188,212 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
             return (unsigned)p ^ 0x80000000u;
         };
         fill();
-        // digit 0-3: score, 4-7: position, 8-11: slot.  A candidate is still in question when it agrees with the
-        // threshold in all digits found so far.
-        unsigned thr[3] = {0u, 0u, 0u};
-        auto prefix_mask = [](int digits) { return digits <= 0 ? 0u : digits >= 4 ? 0xffffffffu : 0xffffffffu << (32 - 8 * digits); };
-        auto agrees_beyond_score = [&](int digits, int j) {
-            const unsigned p = pos_at(j);
-            return ((p ^ thr[1]) & prefix_mask(digits - 4)) == 0u && (((unsigned)j ^ thr[2]) & prefix_mask(digits - 8)) == 0u;
-        };
-        int rank = drop, digit = 0;                      // 1-based rank of the last one to leave
-        for (;;) {
-            const int shift = 24 - 8 * (digit & 3);
-            sh.hist[tid] = 0;
-            if (tid == 0) sh.count = 0;
+        // A generation step lets a few slots leave: the minimum under (score, position, slot), as often as needed.
+        bool found = drop <= kFewDrops && n <= cached;
+        if (found) {
+            __syncthreads();                             // keys and positions are in place
+            unsigned long long gone = 0, low;            // the last one that left, this thread's lowest behind it
+            int gone_slot = -1, low_slot;
+            auto lowest = [&] {
+                low = ~0ull;
+                low_slot = 0x7fffffff;
+                for (int j = 4 * tid; j < n; j += 4 * kSelThreads) {
+                    const uint4 k = *reinterpret_cast<const uint4 *>(keys + j);
+                    const int4 q = *reinterpret_cast<const int4 *>(poss + j);
+                    auto take = [&](unsigned key, int pos, int slot) {
+                        const unsigned long long x = (unsigned long long)key << 32 | ((unsigned)pos ^ 0x80000000u);
+                        if (key != kNoKey && (x > gone || (x == gone && slot > gone_slot)) && x < low) { low = x; low_slot = slot; }
+                    };
+                    take(k.x, q.x, j); take(k.y, q.y, j + 1); take(k.z, q.z, j + 2); take(k.w, q.w, j + 3);
+                }
+            };
+            lowest();
+            for (int r = 0; r < drop && found; ++r) {
+                unsigned long long x = low;
+                int slot = low_slot;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    const unsigned long long y = __shfl_xor_sync(0xffffffffu, x, o);
+                    const int z = __shfl_xor_sync(0xffffffffu, slot, o);
+                    if (y < x || (y == x && z < slot)) { x = y; slot = z; }
+                }
+                if (lane == 0) { sh.low_key[r & 1][warp] = x; sh.low_slot[r & 1][warp] = slot; }
+                __syncthreads();
+                x = sh.low_key[r & 1][0];
+                slot = sh.low_slot[r & 1][0];
+#pragma unroll
+                for (int w = 1; w < kSelWarps; ++w) {
+                    const unsigned long long y = sh.low_key[r & 1][w];
+                    const int z = sh.low_slot[r & 1][w];
+                    if (y < x || (y == x && z < slot)) { x = y; slot = z; }
+                }
+                found = x != ~0ull;                      // else too few candidates: the general search sorts that out
+                gone = x;
+                gone_slot = slot;
+                if (tid == 0) sh.leaving[r] = slot;
+                if (slot == low_slot && r + 1 < drop) lowest();
+            }
+            if (tid == 0) { sh.thr_key = (unsigned)(gone >> 32); sh.thr_pos = (unsigned)gone; sh.thr_slot = gone_slot; }
             __syncthreads();
+        }
+        const bool listed = found && !fresh;
+        if (listed) {
+            // in place, holes and survivors from M on follow from the few that leave
+            int rank_of = 0, others = 0;
+            bool leaves = false;
+            if (tid < drop) {
+                const int hole = sh.leaving[tid], up = M + tid;
+                for (int r = 0; r < drop; ++r) {
+                    rank_of += sh.leaving[r] < hole;
+                    others += sh.leaving[r] >= M && sh.leaving[r] < up;
+                    leaves |= sh.leaving[r] == up;
+                }
+                if (hole < M && A2SF_IN_RANGE(rank_of, M, kDbgPagedEvict)) to[rank_of] = hole;
+                if (!leaves && A2SF_IN_RANGE(tid - others, M, kDbgPagedEvict)) from[tid - others] = up;
+            }
+            for (int r = 0; r < drop; ++r) moves += sh.leaving[r] < M;
+        }
+        if (!found) {
+            // digit 0-3: score, 4-7: position, 8-11: slot.  A candidate is still in question when it agrees with the
+            // threshold in all digits found so far.
+            unsigned thr[3] = {0u, 0u, 0u};
+            auto prefix_mask = [](int digits) { return digits <= 0 ? 0u : digits >= 4 ? 0xffffffffu : 0xffffffffu << (32 - 8 * digits); };
+            auto agrees_beyond_score = [&](int digits, int j) {
+                const unsigned p = pos_at(j);
+                return ((p ^ thr[1]) & prefix_mask(digits - 4)) == 0u && (((unsigned)j ^ thr[2]) & prefix_mask(digits - 8)) == 0u;
+            };
+            int rank = drop, digit = 0;                      // 1-based rank of the last one to leave
+            for (;;) {
+                const int shift = 24 - 8 * (digit & 3);
+                sh.hist[tid] = 0;
+                if (tid == 0) sh.count = 0;
+                __syncthreads();
+                const unsigned above = prefix_mask(digit);
+                for (int j = 4 * tid; j < n; j += 4 * kSelThreads) {
+                    unsigned k[4];
+                    keys4(j, k);
+    #pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (k[e] == kNoKey || ((k[e] ^ thr[0]) & above) != 0u) continue;
+                        if (digit < 4) atomicAdd(&sh.hist[(k[e] >> shift) & 255u], 1);
+                        else if (agrees_beyond_score(digit, j + e))
+                            atomicAdd(&sh.hist[((digit < 8 ? pos_at(j + e) : (unsigned)(j + e)) >> shift) & 255u], 1);
+                    }
+                }
+                __syncthreads();
+                if (warp == 0) {                             // 8 bins a lane, then the lane that holds the rank
+                    int c[8], sum = 0;
+    #pragma unroll
+                    for (int e = 0; e < 8; ++e) { c[e] = sh.hist[lane * 8 + e]; sum += c[e]; }
+                    int incl = sum;
+    #pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int x = __shfl_up_sync(0xffffffffu, incl, o);
+                        if (lane >= o) incl += x;
+                    }
+                    int before = incl - sum;
+                    if (before < rank && rank <= incl) {
+    #pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (before < rank && rank <= before + c[e]) {
+                                sh.prefix = (unsigned)(lane * 8 + e) << shift;
+                                sh.rank = rank - before;
+                                sh.equal = c[e];
+                            }
+                            before += c[e];
+                        }
+                    }
+                    if (lane == 31) sh.total = incl;
+                }
+                __syncthreads();
+                if (digit == 0 && !from_recent && sh.total < drop) {
+                    from_recent = true;
+                    rank = drop - sh.total;
+                    fill();
+                    __syncthreads();
+                    continue;
+                }
+                thr[digit >> 2] |= sh.prefix;
+                rank = sh.rank;
+                ++digit;
+                if (sh.equal <= kShort) break;               // twelve digits tell all slots apart
+                __syncthreads();
+            }
+            // the slots that agree so far, ranked by (score, position, slot)
+            const int m = sh.equal;
             const unsigned above = prefix_mask(digit);
             for (int j = 4 * tid; j < n; j += 4 * kSelThreads) {
                 unsigned k[4];
                 keys4(j, k);
-#pragma unroll
+    #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (k[e] == kNoKey || ((k[e] ^ thr[0]) & above) != 0u) continue;
-                    if (digit < 4) atomicAdd(&sh.hist[(k[e] >> shift) & 255u], 1);
-                    else if (agrees_beyond_score(digit, j + e))
-                        atomicAdd(&sh.hist[((digit < 8 ? pos_at(j + e) : (unsigned)(j + e)) >> shift) & 255u], 1);
+                    if (k[e] == kNoKey || ((k[e] ^ thr[0]) & above) != 0u || (digit > 4 && !agrees_beyond_score(digit, j + e))) continue;
+                    const int x = atomicAdd(&sh.count, 1);
+                    if (A2SF_IN_RANGE(x, kShort, kDbgPagedEvict) && x < kShort) { sh.list_key[x] = k[e]; sh.list_pos[x] = pos_at(j + e); sh.list_slot[x] = j + e; }
                 }
             }
             __syncthreads();
-            if (warp == 0) {                             // 8 bins a lane, then the lane that holds the rank
-                int c[8], sum = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) { c[e] = sh.hist[lane * 8 + e]; sum += c[e]; }
-                int incl = sum;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int x = __shfl_up_sync(0xffffffffu, incl, o);
-                    if (lane >= o) incl += x;
+            if (tid < m) {
+                const unsigned k = sh.list_key[tid], p = sh.list_pos[tid];
+                const int s = sh.list_slot[tid];
+                int less = 0;
+                for (int x = 0; x < m; ++x) {
+                    const unsigned k2 = sh.list_key[x], p2 = sh.list_pos[x];
+                    less += k2 < k || (k2 == k && (p2 < p || (p2 == p && sh.list_slot[x] < s)));
                 }
-                int before = incl - sum;
-                if (before < rank && rank <= incl) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (before < rank && rank <= before + c[e]) {
-                            sh.prefix = (unsigned)(lane * 8 + e) << shift;
-                            sh.rank = rank - before;
-                            sh.equal = c[e];
-                        }
-                        before += c[e];
-                    }
-                }
-                if (lane == 31) sh.total = incl;
+                if (less == rank - 1) { sh.thr_key = k; sh.thr_pos = p; sh.thr_slot = s; }
             }
             __syncthreads();
-            if (digit == 0 && !from_recent && sh.total < drop) {
-                from_recent = true;
-                rank = drop - sh.total;
-                fill();
-                __syncthreads();
-                continue;
-            }
-            thr[digit >> 2] |= sh.prefix;
-            rank = sh.rank;
-            ++digit;
-            if (sh.equal <= kShort) break;               // twelve digits tell all slots apart
-            __syncthreads();
         }
-        // the slots that agree so far, ranked by (score, position, slot)
-        const int m = sh.equal;
-        const unsigned above = prefix_mask(digit);
-        for (int j = 4 * tid; j < n; j += 4 * kSelThreads) {
-            unsigned k[4];
-            keys4(j, k);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (k[e] == kNoKey || ((k[e] ^ thr[0]) & above) != 0u || (digit > 4 && !agrees_beyond_score(digit, j + e))) continue;
-                const int x = atomicAdd(&sh.count, 1);
-                if (A2SF_IN_RANGE(x, kShort, kDbgPagedEvict) && x < kShort) { sh.list_key[x] = k[e]; sh.list_pos[x] = pos_at(j + e); sh.list_slot[x] = j + e; }
-            }
-        }
-        __syncthreads();
-        if (tid < m) {
-            const unsigned k = sh.list_key[tid], p = sh.list_pos[tid];
-            const int s = sh.list_slot[tid];
-            int less = 0;
-            for (int x = 0; x < m; ++x) {
-                const unsigned k2 = sh.list_key[x], p2 = sh.list_pos[x];
-                less += k2 < k || (k2 == k && (p2 < p || (p2 == p && sh.list_slot[x] < s)));
-            }
-            if (less == rank - 1) { sh.thr_key = k; sh.thr_pos = p; sh.thr_slot = s; }
-        }
-        __syncthreads();
-        const unsigned tk = sh.thr_key, tp = sh.thr_pos;
-        const int ts = sh.thr_slot;
-        auto stays = [&](int j) {
-            const unsigned k = key_at(j);
-            if (k == kNoKey) return !from_recent;
-            if (k != tk) return k > tk;
-            const unsigned p = pos_at(j);
-            return p != tp ? p > tp : j > ts;
-        };
-        // every warp takes a contiguous range of slots, 32 at a time: mask and counts, scan over the warps, list
-        const int per = ((n + kSelWarps - 1) / kSelWarps + 31) / 32 * 32;
-        const int w0 = min(n, warp * per), w1 = min(n, w0 + per);
-        auto low = [&](int j0) { return j0 + 32 <= M ? 0xffffffffu : j0 >= M ? 0u : (1u << (M - j0)) - 1u; };
-        int stay_lo = 0, stay_hi = 0;                    // survivors below / from slot M on
-        for (int j0 = w0; j0 < w1; j0 += 32) {
-            const unsigned s = __ballot_sync(0xffffffffu, j0 + lane < w1 && stays(j0 + lane));
-            if (lane == 0 && j0 / 32 < kMaskWords) sh.mask[j0 / 32] = s;
-            stay_lo += __popc(s & low(j0));
-            stay_hi += __popc(s & ~low(j0));
-        }
-        int total_lo, total_hi;
-        const int lo0 = warps_excl_scan(sh, 0, stay_lo, total_lo), hi0 = warps_excl_scan(sh, 1, stay_hi, total_hi);
-        auto mask_of = [&](int j0) -> unsigned {
-            return j0 / 32 < kMaskWords ? sh.mask[j0 / 32] : __ballot_sync(0xffffffffu, j0 + lane < w1 && stays(j0 + lane));
-        };
-        const unsigned lt = (1u << lane) - 1u;
-        if (fresh) {
-            int at = lo0 + hi0;
+        if (!listed) {
+            const unsigned tk = sh.thr_key, tp = sh.thr_pos;
+            const int ts = sh.thr_slot;
+            auto stays = [&](int j) {
+                const unsigned k = key_at(j);
+                if (k == kNoKey) return !from_recent;
+                if (k != tk) return k > tk;
+                const unsigned p = pos_at(j);
+                return p != tp ? p > tp : j > ts;
+            };
+            // every warp takes a contiguous range of slots, 32 at a time: mask and counts, scan over the warps, list
+            const int per = ((n + kSelWarps - 1) / kSelWarps + 31) / 32 * 32;
+            const int w0 = min(n, warp * per), w1 = min(n, w0 + per);
+            auto low = [&](int j0) { return j0 + 32 <= M ? 0xffffffffu : j0 >= M ? 0u : (1u << (M - j0)) - 1u; };
+            int stay_lo = 0, stay_hi = 0;                    // survivors below / from slot M on
             for (int j0 = w0; j0 < w1; j0 += 32) {
-                const unsigned s = mask_of(j0);
-                const int k = at + __popc(s & lt);
-                if ((s >> lane & 1) && A2SF_IN_RANGE(k, M, kDbgPagedEvict) && k < M) from[k] = j0 + lane;
-                at += __popc(s);
+                const unsigned s = __ballot_sync(0xffffffffu, j0 + lane < w1 && stays(j0 + lane));
+                if (lane == 0 && j0 / 32 < kMaskWords) sh.mask[j0 / 32] = s;
+                stay_lo += __popc(s & low(j0));
+                stay_hi += __popc(s & ~low(j0));
             }
-        } else {
-            int hole = min(w0, M) - lo0, src = hi0;      // holes and survivors before this warp's range
-            for (int j0 = w0; j0 < w1; j0 += 32) {
-                const unsigned s = mask_of(j0);
-                const unsigned in = j0 + 32 <= w1 ? 0xffffffffu : (1u << (w1 - j0)) - 1u;
-                const unsigned lo = low(j0), holes = in & lo & ~s, ups = s & ~lo;
-                const int kh = hole + __popc(holes & lt), ks = src + __popc(ups & lt);
-                if ((holes >> lane & 1) && A2SF_IN_RANGE(kh, M, kDbgPagedEvict) && kh < M) to[kh] = j0 + lane;
-                if ((ups >> lane & 1) && A2SF_IN_RANGE(ks, M, kDbgPagedEvict) && ks < M) from[ks] = j0 + lane;
-                hole += __popc(holes);
-                src += __popc(ups);
+            int total_lo, total_hi;
+            const int lo0 = warps_excl_scan(sh, 0, stay_lo, total_lo), hi0 = warps_excl_scan(sh, 1, stay_hi, total_hi);
+            auto mask_of = [&](int j0) -> unsigned {
+                return j0 / 32 < kMaskWords ? sh.mask[j0 / 32] : __ballot_sync(0xffffffffu, j0 + lane < w1 && stays(j0 + lane));
+            };
+            const unsigned lt = (1u << lane) - 1u;
+            if (fresh) {
+                int at = lo0 + hi0;
+                for (int j0 = w0; j0 < w1; j0 += 32) {
+                    const unsigned s = mask_of(j0);
+                    const int k = at + __popc(s & lt);
+                    if ((s >> lane & 1) && A2SF_IN_RANGE(k, M, kDbgPagedEvict) && k < M) from[k] = j0 + lane;
+                    at += __popc(s);
+                }
+            } else {
+                int hole = min(w0, M) - lo0, src = hi0;      // holes and survivors before this warp's range
+                for (int j0 = w0; j0 < w1; j0 += 32) {
+                    const unsigned s = mask_of(j0);
+                    const unsigned in = j0 + 32 <= w1 ? 0xffffffffu : (1u << (w1 - j0)) - 1u;
+                    const unsigned lo = low(j0), holes = in & lo & ~s, ups = s & ~lo;
+                    const int kh = hole + __popc(holes & lt), ks = src + __popc(ups & lt);
+                    if ((holes >> lane & 1) && A2SF_IN_RANGE(kh, M, kDbgPagedEvict) && kh < M) to[kh] = j0 + lane;
+                    if ((ups >> lane & 1) && A2SF_IN_RANGE(ks, M, kDbgPagedEvict) && ks < M) from[ks] = j0 + lane;
+                    hole += __popc(holes);
+                    src += __popc(ups);
+                }
+                moves = total_hi;
             }
-            moves = total_hi;
         }
     } else if (fresh) {
         for (int j = tid; j < n; j += kSelThreads) from[j] = j;

@@ -399,9 +399,9 @@ def test_evict_random_cases(a2sf, seed):
 
 
 def random_evict(r):
-    B, H, c = r.choice([1, 2, 3, 5]), r.choice([1, 2, 3]), r.choice([1, 2, 7, 40])
+    B, H, c = r.choice([1, 2, 3, 5]), r.choice([1, 2, 3]), r.choice([1, 2, 7, 8, 9, 40])
     past = [int(2 ** r.uniform(0, 10.5)) - 1 for _ in range(B)]
-    budget = max(1, int((max(past) + c) * r.uniform(0.05, 1.1)))
+    budget = max(1, r.choice([int((max(past) + c) * r.uniform(0.05, 1.1)), past[0]]))
     return (B, H, r.choice([64, 128]), r.choice([FP, BF, HF]), r.choice([16, 32, 64, 128]), past, c, budget, r.choice([0, budget // 2, budget]),
             r.random() < 0.5, r.choice(["rand", "zeros", "ties", "signed"]))
 
@@ -414,13 +414,23 @@ def test_evict_of_many_heads_moves_rows_in_the_searching_blocks(a2sf):
 
 def test_evict_with_positions_given_twice_keeps_exactly_the_budget(a2sf):
     """More recent slots than the budget holds (a position twice): ranked among themselves, lower slots leave first."""
-    cache = pu.make_cache(a2sf, 1, 1, 1, 64, FP, 16, [60], 0, seed=3)
-    cache.scores.fill_(0.5)
-    cache.positions.fill_(59)
-    cache.past.fill_(59)
-    cache.start.fill_(59)
-    cache.a2sf_paged_evict(20, 10, 1)
-    assert cache.past.item() == 20 and cache.start.item() == 60
+    for n, budget, recent in ((60, 20, 10), (60, 57, 10), (60, 52, 52)):
+        cache = pu.make_cache(a2sf, 1, 1, 1, 64, FP, 16, [n], 0, seed=3)
+        cache.scores.fill_(0.5)
+        cache.positions.fill_(n - 1)
+        cache.past.fill_(n - 1)
+        cache.start.fill_(n - 1)
+        first = pu.slots(cache, cache.k_pages.cpu(), 0, n)[0]
+        cache.a2sf_paged_evict(budget, recent, 1)
+        assert cache.past.item() == budget and cache.start.item() == n
+        # slots 0 .. n - budget - 1 leave, the last ones take their places in order
+        got = pu.slots(cache, cache.k_pages.cpu(), 0, budget)[0]
+        stay = list(range(n - budget, n))
+        holes = [j for j in range(budget) if j not in stay]
+        want = first[:budget].clone()
+        for hole, src in zip(holes, [j for j in stay if j >= budget]):
+            want[hole] = first[src]
+        assert torch.equal(got, want)
 
 
 # ---- the whole step -------------------------------------------------------------------------------------
