@@ -257,7 +257,7 @@ size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c)
     if (check_paged(cache, c) != A2SF_OK) return 0;
     const PagedView pv = make_view(cache, c, nullptr);
     const Path path = path_of(cache, c);
-    return align_up(path == kFew ? attend_few_ws_bytes(pv) : path == kTc ? attend_tc_ws_bytes(pv) : attend_simt_ws_bytes(pv));
+    return align_up(path == kFew ? attend_few_ws_bytes(cache->dtype, pv) : path == kTc ? attend_tc_ws_bytes(pv) : attend_simt_ws_bytes(pv));
 }
 
 int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha, const void *q,

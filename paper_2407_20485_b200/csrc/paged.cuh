@@ -191,7 +191,7 @@ bool make_pool_map(CUtensorMap *map, int dtype, const void *pool, const PagedVie
 
 // few rows (len * G <= kFewRows): the cache is read once, split evenly over the device
 constexpr int kFewRows = 16;
-size_t attend_few_ws_bytes(const PagedView &pv);
+size_t attend_few_ws_bytes(int dtype, const PagedView &pv);
 cudaError_t launch_attend_few(int dtype, const AttendArgs &a, cudaStream_t s);
 
 // many rows, 16-bit storage: tcgen05

@@ -7,16 +7,18 @@
 // The list is built on the device from past and lens (the host knows neither).
 //
 //   main    warp 0 copies tiles (K and V, TMA boxes of up to a page, 128-byte swizzle) into a ring;
-//           warps 1-4 take 16 slots of each tile, keep their own running maximum, sum and output, and
-//           never meet each other.  16-bit storage: S[16 slots x 8 rows] = K Q^T and O^T[d x 8] += V^T P^T
+//           consumer warps take 16 slots (8 in 32-bit storage) of each tile and keep their own running
+//           maximum, sum and output.  16-bit storage: S[16 slots x 8 rows] = K Q^T and O^T[d x 8] += V^T P^T
 //           on mma.sync m16n8k16, K and V^T straight from ldmatrix (.trans for V); P changes from
 //           accumulator to operand layout with movmatrix.  The rows fill 8 of the instruction's columns, so
 //           the tensor rate is of no account and tcgen05 (128 rows at least) would compute on padding.
-//           32-bit storage: the same on the CUDA cores.  Logits go to the workspace (4 bytes per slot and
+//           32-bit storage: the same on the CUDA cores, a lane working on a quarter of a key.  Logits go to the workspace (4 bytes per slot and
 //           row next to 4 d or 8 d bytes of K and V) so that scores need no second pass over K.
 //   finish  joins the partial outputs; S <- alpha^len S + sum_r alpha^age exp2(x_r - lse_r).
 // P is rounded to the storage type for P V (half a step, as the output itself); the row sum and the
 // scores use the unrounded values.
+#include <type_traits>
+
 #include "paged.cuh"
 #include "tc_sm100.cuh"
 
@@ -29,8 +31,9 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = 64;                 // slots per tile
-constexpr int kWarps = 4;                 // consumer warps, 16 slots each
-constexpr int kFewThreads = 32 * (kWarps + 1);
+// Consumer warps of a CTA.  32-bit storage spends 8 times the instructions on a slot and runs one CTA per SM
+// (d = 128), so twice as many warps share a tile there to hide each other's latencies.
+template <typename T> constexpr int warps_of = sizeof(T) == 4 ? 8 : 4;
 constexpr int kFinishThreads = 256;
 
 __host__ __device__ constexpr int rows_padded(int rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
@@ -45,11 +48,11 @@ template <typename T, int D> struct Ring {
 
 struct FewWs {
     float *logits;        // [U][slots][NP], log2 units
-    float2 *ml;           // [segments][kWarps][NP] running maximum (log2 units), sum
-    float *o;             // [segments][kWarps][NP][D]
+    float2 *ml;           // [segments][warps][NP] running maximum (log2 units), sum
+    float *o;             // [segments][warps][NP][D]
     int32_t *prefix;      // [B + 1] tiles of a head, summed over the sequences before
     int slots;            // padded slots of a unit
-    int segs;             // segments that there is room for, times kWarps
+    int segs;             // segments that there is room for, times warps
 };
 
 template <typename T> struct Mma16;
@@ -118,6 +121,7 @@ __device__ __forceinline__ const void *query_row(const AttendArgs &a, int b, int
 // ---- a consumer warp on 16-bit storage: NC = 8 or 16 row columns ------------------------------------
 template <typename T, int D, int NC> struct Body16 {
     static constexpr int CG = NC / 8, KS = D / 16;
+    static constexpr float kSlack = std::is_same<T, __half>::value ? 14.f : 60.f;    // fp16 ends at 2^16
     uint32_t q[CG][KS][2];
     float o[CG][KS][4], m[CG][2], l[CG][2];
     int vis[CG][2];
@@ -175,52 +179,62 @@ template <typename T, int D, int NC> struct Body16 {
             fence_async_smem();            // these writes come before the copy that next fills the stage
             __syncwarp();
         }
-        uint32_t p0[CG], p1[CG];
-        bool moved = false;
-        float f[CG][2];
+        // The reference of a column (what is subtracted before the exponential) moves only when a logit exceeds it by
+        // more than kSlack: probabilities up to 2^kSlack are as exact, and no maximum is looked for in between.
+        float x[CG][4];
+        bool beyond = false;
 #pragma unroll
         for (int g = 0; g < CG; ++g) {
-            float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = j0 + r + (e >> 1) * 8;
-                x[e] = j < vis[g][e & 1] ? s[g][e] * a.pv.sl2 : -INFINITY;
+                x[g][e] = j < vis[g][e & 1] ? s[g][e] * a.pv.sl2 : -INFINITY;
+                beyond |= x[g][e] > m[g][e & 1] + kSlack;          // also where m is still -inf
             }
             if (logits) {
                 const int col = g * 8 + 2 * c;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     float *dst = logits + (size_t)(j0 + r + half * 8) * NP + col;
-                    if (col + 1 < NP) *reinterpret_cast<float2 *>(dst) = make_float2(x[2 * half], x[2 * half + 1]);
-                    else if (col < NP) *dst = x[2 * half];
+                    if (col + 1 < NP) *reinterpret_cast<float2 *>(dst) = make_float2(x[g][2 * half], x[g][2 * half + 1]);
+                    else if (col < NP) *dst = x[g][2 * half];
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float mx = fmaxf(x[e], x[e + 2]);
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                const float mn = fmaxf(m[g][e], mx);
-                // all of a row masked so far: any finite reference gives the zeros that are wanted
-                const float ref = mn == -INFINITY ? 0.f : mn;
-                f[g][e] = ex2(m[g][e] - ref);
-                moved |= f[g][e] != 1.f;
-                m[g][e] = mn;
-                x[e] = ex2(x[e] - ref);
-                x[e + 2] = ex2(x[e + 2] - ref);
-                l[g][e] = fmaf(l[g][e], f[g][e], x[e] + x[e + 2]);
-            }
-            p0[g] = movmatrix_trans(Mma16<T>::pack(x[0], x[1]));
-            p1[g] = movmatrix_trans(Mma16<T>::pack(x[2], x[3]));
         }
-        if (__any_sync(0xffffffffu, moved)) {
+        if (__any_sync(0xffffffffu, beyond)) {
 #pragma unroll
-            for (int g = 0; g < CG; ++g)
+            for (int g = 0; g < CG; ++g) {
+                float f[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float mx = fmaxf(x[g][e], x[g][e + 2]);
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                    const float mn = fmaxf(m[g][e], mx);
+                    f[e] = mn == -INFINITY ? 1.f : ex2(m[g][e] - mn);
+                    m[g][e] = mn;
+                    l[g][e] *= f[e];
+                }
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[g][k][e] *= f[g][e & 1];
+                    for (int e = 0; e < 4; ++e) o[g][k][e] *= f[e & 1];
+            }
+        }
+        uint32_t p0[CG], p1[CG];
+#pragma unroll
+        for (int g = 0; g < CG; ++g) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                // nothing seen so far: any finite reference gives the zeros that are wanted
+                const float ref = m[g][e] == -INFINITY ? 0.f : m[g][e];
+                x[g][e] = ex2(x[g][e] - ref);
+                x[g][e + 2] = ex2(x[g][e + 2] - ref);
+                l[g][e] += x[g][e] + x[g][e + 2];
+            }
+            p0[g] = movmatrix_trans(Mma16<T>::pack(x[g][0], x[g][1]));
+            p1[g] = movmatrix_trans(Mma16<T>::pack(x[g][2], x[g][3]));
         }
         {
             const int row = row0 + (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
@@ -260,20 +274,30 @@ template <typename T, int D, int NC> struct Body16 {
 // ---- a consumer warp on 32-bit storage: NC rows, all in use or zero ----------------------------------
 template <int D, int NC> struct Body32 {
     static constexpr int DV = D / 32;                       // output elements per lane
+    static constexpr int QP = D / 4, QS = QP + 4;           // a quarter of a query, and its distance in shared memory
     float o[NC][DV], m[NC], l[NC];
     int rows, G, past;
+    unsigned long long tokens;                              // token of row r in bits 4r .. 4r+3
 
-    // scratch: [NC][D] queries, then [16][NC] probabilities of this warp
+    __device__ int seen_by(int r) const { return r < rows ? (int)(tokens >> (4 * r) & 15) + 1 : -(1 << 30); }
+
+    // scratch: [NC][4][QS] queries, shared by the consumer warps, then [8][NC] probabilities of each warp
     __device__ void begin(const AttendArgs &a, const Where &x, const SeqState &st, float *scratch)
     {
-        const int lane = threadIdx.x & 31;
+        constexpr int kThreads = 32 * warps_of<float>;
+        const int tid = threadIdx.x - 32;
         rows = st.len * a.pv.G; G = a.pv.G; past = st.past;
-        __syncwarp();
-#pragma unroll 1
-        for (int r = 0; r < NC; ++r)
-            for (int k = lane; k < D; k += 32)
-                scratch[r * D + k] = r < rows ? static_cast<const float *>(query_row(a, x.b, x.h, r, 4))[k] : 0.f;
-        __syncwarp();
+        tokens = 0;
+        for (int r = 0; r < rows; ++r) tokens |= (unsigned long long)(r / G) << (4 * r);
+        named_barrier(1, kThreads);                         // the unit before has been worked off
+#pragma unroll
+        for (int e = tid; e < NC * (D / 4); e += kThreads) {
+            const int r = e / (D / 4), k = e % (D / 4) * 4;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r < rows) v = *reinterpret_cast<const float4 *>(static_cast<const float *>(query_row(a, x.b, x.h, r, 4)) + k);
+            *reinterpret_cast<float4 *>(scratch + (r * 4 + k / QP) * QS + k % QP) = v;
+        }
+        named_barrier(1, kThreads);
 #pragma unroll
         for (int r = 0; r < NC; ++r) {
             m[r] = -INFINITY; l[r] = 0.f;
@@ -282,58 +306,73 @@ template <int D, int NC> struct Body32 {
         }
     }
 
+    // 8 slots j0 .. j0+7, rows `row0` .. of the tile
     __device__ void tile(const AttendArgs &a, uint8_t *K, uint8_t *V, int row0, int j0, int used, float *logits, int, float *scratch)
     {
-        const int lane = threadIdx.x & 31, s = lane & 15, hf = lane >> 4;
-        float *P = scratch + NC * D;
+        const int lane = threadIdx.x & 31, s = lane & 7, part = lane >> 3;
+        float *P = scratch + NC * 4 * QS + ((threadIdx.x >> 5) - 1) * 8 * NC;
         float acc[NC];
 #pragma unroll
         for (int r = 0; r < NC; ++r) acc[r] = 0.f;
+        const float *qq = scratch + part * QS;
 #pragma unroll 4
-        for (int k = hf * (D / 2); k < (hf + 1) * (D / 2); k += 4) {
-            const float4 kk = *reinterpret_cast<const float4 *>(K + tile_offset(row0 + s, k / 4));
+        for (int k = 0; k < QP; k += 4) {
+            const float4 kk = *reinterpret_cast<const float4 *>(K + tile_offset(row0 + s, (part * QP + k) / 4));
 #pragma unroll
             for (int r = 0; r < NC; ++r) {
-                const float4 qq = *reinterpret_cast<const float4 *>(scratch + r * D + k);
-                acc[r] = fmaf(qq.x, kk.x, acc[r]);
-                acc[r] = fmaf(qq.y, kk.y, acc[r]);
-                acc[r] = fmaf(qq.z, kk.z, acc[r]);
-                acc[r] = fmaf(qq.w, kk.w, acc[r]);
+                const float4 q = *reinterpret_cast<const float4 *>(qq + r * 4 * QS + k);
+                acc[r] = fmaf(q.x, kk.x, acc[r]);
+                acc[r] = fmaf(q.y, kk.y, acc[r]);
+                acc[r] = fmaf(q.z, kk.z, acc[r]);
+                acc[r] = fmaf(q.w, kk.w, acc[r]);
             }
         }
         const int j = j0 + s;
         __syncwarp();                                       // the previous tile's probabilities have been read
+        // references move as in Body16
+        bool beyond = false;
 #pragma unroll
         for (int r = 0; r < NC; ++r) {
-            const float dot = acc[r] + __shfl_xor_sync(0xffffffffu, acc[r], 16);
-            const bool seen = r < rows && j < past + r / G + 1;
-            const float x = seen ? dot * a.pv.sl2 : -INFINITY;
-            if (logits && hf == 0) logits[(size_t)j * NC + r] = x;
-            float mx = x;
+            acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], 8);
+            acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], 16);
+            const bool seen = j < past + seen_by(r);
+            acc[r] = seen ? acc[r] * a.pv.sl2 : -INFINITY;
+            if (logits && part == r % 4) logits[(size_t)j * NC + r] = acc[r];
+            beyond |= acc[r] > m[r] + 60.f;
+        }
+        if (__any_sync(0xffffffffu, beyond)) {
 #pragma unroll
-            for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-            const float mn = fmaxf(m[r], mx);
-            const float ref = mn == -INFINITY ? 0.f : mn;
-            const float f = exp2f(m[r] - ref), p = exp2f(x - ref);
-            m[r] = mn;
-            l[r] = fmaf(l[r], f, p);                        // every half-warp holds the sum over its 16 slots
-            if (hf == 0) P[s * NC + r] = p;
+            for (int r = 0; r < NC; ++r) {
+                float mx = acc[r];
 #pragma unroll
-            for (int e = 0; e < DV; ++e) o[r][e] *= f;
+                for (int w = 4; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                const float mn = fmaxf(m[r], mx), f = mn == -INFINITY ? 1.f : exp2f(m[r] - mn);
+                m[r] = mn;
+                l[r] *= f;
+#pragma unroll
+                for (int e = 0; e < DV; ++e) o[r][e] *= f;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < NC; ++r) {
+            const float p = exp2f(acc[r] - (m[r] == -INFINITY ? 0.f : m[r]));
+            l[r] += p;                                      // every quarter-warp holds the sum over its 8 slots
+            if (part == r % 4) P[s * NC + r] = p;
         }
         __syncwarp();
-        const int n = min(16, used - j0);                   // values behind the sequence are not touched
+        const int n = min(8, used - j0);                    // values behind the sequence are not touched
+#pragma unroll 4
         for (int x = 0; x < n; ++x) {
-            float v[DV];
+            float v[DV], p[NC];
             const uint8_t *src = V + tile_offset(row0 + x, lane * DV / 4) + (lane * DV % 4) * 4;
 #pragma unroll
             for (int e = 0; e < DV; e += 2) *reinterpret_cast<float2 *>(v + e) = *reinterpret_cast<const float2 *>(src + e * 4);
 #pragma unroll
-            for (int r = 0; r < NC; ++r) {
-                const float p = P[x * NC + r];
+            for (int r = 0; r < NC; ++r) p[r] = P[x * NC + r];
 #pragma unroll
-                for (int e = 0; e < DV; ++e) o[r][e] = fmaf(p, v[e], o[r][e]);
-            }
+            for (int r = 0; r < NC; ++r)
+#pragma unroll
+                for (int e = 0; e < DV; ++e) o[r][e] = fmaf(p[r], v[e], o[r][e]);
         }
     }
 
@@ -344,10 +383,10 @@ template <int D, int NC> struct Body32 {
         for (int r = 0; r < NC; ++r) {
             float sum = l[r];
 #pragma unroll
-            for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+            for (int w = 4; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
             if (lane == 0) ml[r] = make_float2(m[r], sum);
 #pragma unroll
-            for (int e = 0; e < DV; ++e) op[(size_t)r * D + lane * DV + e] = o[r][e];
+            for (int e = 0; e < DV; e += 2) *reinterpret_cast<float2 *>(op + (size_t)r * D + lane * DV + e) = make_float2(o[r][e], o[r][e + 1]);
         }
     }
 };
@@ -355,7 +394,7 @@ template <int D, int NC> struct Body32 {
 template <typename T, int D, int NC> struct BodyOf { typedef Body16<T, D, NC> type; static constexpr size_t kScratch = 0; };
 template <int D, int NC> struct BodyOf<float, D, NC> {
     typedef Body32<D, NC> type;
-    static constexpr size_t kScratch = (size_t)kWarps * (NC * D + 16 * NC) * sizeof(float);
+    static constexpr size_t kScratch = (size_t)(NC * 4 * (D / 4 + 4) + warps_of<float> * 8 * NC) * sizeof(float);
 };
 
 struct FewShared {
@@ -365,12 +404,13 @@ struct FewShared {
 };
 
 template <typename T, int D, int NC>
-__global__ void __launch_bounds__(kFewThreads)
+__global__ void __launch_bounds__(32 * (warps_of<T> + 1))
 paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ AttendArgs a, const __grid_constant__ FewWs ws, int NP)
 {
     using R = Ring<T, D>;
     using Body = typename BodyOf<T, D, NC>::type;
+    constexpr int kWarps = warps_of<T>, kSlots = kTile / kWarps;     // slots per warp and tile
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ FewShared sh;
@@ -392,7 +432,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     if (warp != 0) dependency_wait();
     __syncthreads();
     if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= pv.B; b += kFewThreads) ws.prefix[b] = sh.prefix[b];
+        for (int b = threadIdx.x; b <= pv.B; b += 32 * (kWarps + 1)) ws.prefix[b] = sh.prefix[b];
     dependents_may_start();
     const long long total = (long long)pv.H * sh.prefix[pv.B];
     const long long share = (total + gridDim.x - 1) / gridDim.x;
@@ -444,8 +484,7 @@ drained:
     } else {
         // ---- consumers ---------------------------------------------------------------------------
         const int cw = warp - 1;
-        float *scratch = reinterpret_cast<float *>(ring + (size_t)R::kStages * 2 * R::kTileBytes) +
-                         cw * (BodyOf<T, D, NC>::kScratch / kWarps / sizeof(float));
+        float *scratch = reinterpret_cast<float *>(ring + (size_t)R::kStages * 2 * R::kTileBytes);
         Body body;
         int it = 0;
         for (long long w = w0; w < w1;) {
@@ -457,9 +496,9 @@ drained:
             for (; x.t < x.tiles && w < w1; ++x.t, ++w, ++it) {
                 const int s = it % R::kStages;
                 if (!*abort_flag && !mbar_wait(&sh.full[s], (it / R::kStages) & 1, abort_flag)) *pv.status = A2SF_ERR_TIMEOUT;
-                const int j0 = x.t * kTile + cw * 16;
+                const int j0 = x.t * kTile + cw * kSlots;
                 uint8_t *K = ring + (size_t)s * 2 * R::kTileBytes;
-                if (j0 < used && A2SF_IN_RANGE(j0 + 15, ws.slots, kDbgPagedFew)) body.tile(a, K, K + R::kTileBytes, cw * 16, j0, used, logits, NP, scratch);
+                if (j0 < used && A2SF_IN_RANGE(j0 + kSlots - 1, ws.slots, kDbgPagedFew)) body.tile(a, K, K + R::kTileBytes, cw * kSlots, j0, used, logits, NP, scratch);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.empty[s]);
             }
@@ -534,6 +573,7 @@ template <typename T, int D, int NP>
 __global__ void __launch_bounds__(kFinishThreads, NP <= 2 ? 5 : 4)
 paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ FewWs ws, int ctas, int blocks, int chunk)
 {
+    constexpr int kWarps = warps_of<T>;
     constexpr int GR = kFinishThreads / (D / 4);             // thread groups of an output row, 4 elements a thread
     __shared__ float4 red[kFinishThreads];
     __shared__ float row_m[kFewRows], row_l[kFewRows], row_c[kFewRows];
@@ -636,11 +676,11 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
 size_t pad(size_t x) { return (x + 255) / 256 * 256; }
 int padded_slots(const PagedView &pv) { return ((pv.max_pages << pv.ps_shift) + kTile - 1) / kTile * kTile; }
 
-FewWs carve(const PagedView &pv, void *ws, size_t *bytes)
+FewWs carve(int dtype, const PagedView &pv, void *ws, size_t *bytes)
 {
     const size_t U = (size_t)pv.B * pv.H, NP = rows_padded(pv.c * pv.G);
     // the size must not depend on a device: room for any SM count up to 256
-    const size_t segs = (U + 512) * kWarps;
+    const size_t segs = (U + 512) * (dtype == A2SF_F32 ? warps_of<float> : warps_of<__half>);
     FewWs w;
     size_t off = 0;
     char *base = static_cast<char *>(ws);
@@ -664,11 +704,11 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     CUtensorMap mk, mv;
     const int box = a.pv.ps < kTile ? a.pv.ps : kTile;
     if (!make_pool_map(&mk, dtype, a.pv.k, a.pv, box) || !make_pool_map(&mv, dtype, a.pv.v, a.pv, box)) return cudaErrorInvalidValue;
-    const FewWs ws = carve(a.pv, a.ws, nullptr);
+    const FewWs ws = carve(dtype, a.pv, a.ws, nullptr);
     const int NP = rows_padded(a.pv.c * a.pv.G);
     const int ctas = device_sm_count() * (2 * (smem + sizeof(FewShared) + 1024) <= 228 * 1024 ? 2 : 1);   // what is resident
     if (ctas < 1 || ctas > 512) return cudaErrorInvalidValue;
-    if ((e = launch_chained(paged_few_kernel<T, D, NC>, ctas, kFewThreads, smem, s, mk, mv, a, ws, NP)) != cudaSuccess) return e;
+    if ((e = launch_chained(paged_few_kernel<T, D, NC>, ctas, 32 * (warps_of<T> + 1), smem, s, mk, mv, a, ws, NP)) != cudaSuccess) return e;
     count_launch();
     // blocks per unit: enough for the rows and the slots, as far as that fills the device
     const int cap = a.pv.max_pages << a.pv.ps_shift;
@@ -711,10 +751,10 @@ cudaError_t launch_d(int dtype, const AttendArgs &a, cudaStream_t s)
 
 }  // namespace
 
-size_t attend_few_ws_bytes(const PagedView &pv)
+size_t attend_few_ws_bytes(int dtype, const PagedView &pv)
 {
     size_t bytes = 0;
-    carve(pv, nullptr, &bytes);
+    carve(dtype, pv, nullptr, &bytes);
     return bytes;
 }
 
