@@ -42,6 +42,11 @@ constexpr int kSms = 148;
 constexpr int kSplitBelow = 4 * kSms;        // items of a call from which none is cut
 constexpr int kPieces = 4 * kSms;            // pieces that cutting makes at most, next to one per item
 constexpr int kMinPiece = 4;                 // key tiles of a piece at least
+// Sequences of at most so many key tiles need no plan: no item is long, so none is cut and their order is of no
+// account.  Such a call is attn and score alone (12 heads, 244 tokens: 27 us with plan, merge and join, 16 us without).
+constexpr int kDirectTiles = 8;
+// Up to so many row tiles a key tile's sum is left whole: at most 5 us for one CTA, what the join kernel costs.
+constexpr int kWholeRows = 4;
 constexpr int kMaxParts = kSplitBelow + kPieces;   // sum of ceil(T / piece) <= total / piece + items
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
@@ -73,6 +78,7 @@ struct TcWs {
     float *part_o;        // [kMaxParts][d/4][part_rows][4]: a warp stores 32 rows' four columns as 512 bytes
     float *score_parts;   // [2 * kScoreCtas][kBlk] sums of key tiles that two CTAs or more share
     int max_items, part_rows, pairs, pair_tokens, parts;
+    bool direct, whole_scores;
 };
 
 __device__ __forceinline__ int pair_key_tiles(const SeqState &st, int pair, int pair_tokens)
@@ -364,7 +370,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     }
     fence_async_smem();
     dependency_wait();
-    if (threadIdx.x <= kLevels) sh->level[threadIdx.x] = ws.head->level[threadIdx.x];
+    if (!ws.direct && threadIdx.x <= kLevels) sh->level[threadIdx.x] = ws.head->level[threadIdx.x];
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -378,19 +384,33 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     };
     // Jobs: by step of length, then by head (the items of a head run together and share its K and V
     // through L2), dealt in rounds of alternating direction.
-    const int n_units = sh->level[kLevels] * pv.H;
+    const int n_units = ws.direct ? pv.B * ws.pairs * pv.H : sh->level[kLevels] * pv.H;
     auto dealt = [&](int round) { return round * (int)gridDim.x + (round & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
     // what an item means to every role
     struct Job {
         int b, h, i0, tokens, t0, nt, ntA, ntB, past, used, part;
     };
     auto job = [&](int unit) -> Job {
-        int l = 0;
-        while (l < kLevels - 1 && unit >= sh->level[l + 1] * pv.H) ++l;
-        const int first = sh->level[l], n_items = sh->level[l + 1] - first, rest = unit - first * pv.H;
-        const Item it = ws.items[first + rest % n_items];
         Job j;
-        j.b = it.b; j.h = rest / n_items;
+        Item it;
+        if (ws.direct) {
+            // the pairs of a (sequence, head) next to each other, the longest first; pairs behind the chunk are empty
+            const int unit_of = unit / ws.pairs;
+            it.b = unit_of / pv.H;
+            j.h = unit_of - it.b * pv.H;
+            it.pair = ws.pairs - 1 - (unit - unit_of * ws.pairs);
+            const SeqState st = seq_state(pv, it.b);
+            it.past = st.past; it.len = st.len; it.part = -1;
+            it.t0 = 0;
+            it.t1 = it.pair * ws.pair_tokens < st.len ? pair_key_tiles(st, it.pair, ws.pair_tokens) : 0;
+        } else {
+            int l = 0;
+            while (l < kLevels - 1 && unit >= sh->level[l + 1] * pv.H) ++l;
+            const int first = sh->level[l], n_items = sh->level[l + 1] - first, rest = unit - first * pv.H;
+            it = ws.items[first + rest % n_items];
+            j.h = rest / n_items;
+        }
+        j.b = it.b;
         j.past = it.past; j.used = it.past + it.len;
         j.i0 = it.pair * ws.pair_tokens;
         j.tokens = min(ws.pair_tokens, it.len - j.i0);
@@ -408,8 +428,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     if (warp == 0) {
         // ---- TMA producer: lane i copies page box i ------------------------------------------
         int kt = 0, n = 0;                                  // tiles and items so far
-        for (int unit; (unit = dealt(n)) < n_units; ++n) {
+        for (int round = 0, unit; (unit = dealt(round)) < n_units; ++round) {
             const Job j = job(unit);
+            if (j.nt == 0) continue;
             const int32_t *table = pv.table + (size_t)j.b * pv.max_pages;
             int ok = 1;
             if (lane == 0) {
@@ -422,6 +443,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 }
             }
             if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+            ++n;
             for (int t = 0; t < j.nt; ++t, ++kt) {
                 const int tile = j.t0 + t, ks = kt % kKStages, vs = kt % kVStages;
                 const PageTile p = page_tile(pv, tile, j.used);
@@ -475,11 +497,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             umma_commit(&sh->o_done[X]);
         };
         int kt = 0, n = 0, cnt[2] = {0, 0}, used_before[2] = {0, 0};      // tiles per stream; items per stream
-        for (int unit; (unit = dealt(n)) < n_units; ++n) {
+        for (int round = 0, unit; (unit = dealt(round)) < n_units; ++round) {
             if (__any_sync(0xffffffffu, *abort_flag)) break;
             const Job j = job(unit);
+            if (j.nt == 0) continue;
             const int ntX[2] = {j.ntA, j.ntB};
-            wait(&sh->q_full, n & 1);
+            wait(&sh->q_full, n++ & 1);
             wait(&sh->k_full[kt % kKStages], (kt / kKStages) & 1);
             tc_fence_after_sync();
             if (lane == 0) {
@@ -535,8 +558,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         float m_used[2], l[2];
         // no early exit here: the two warps of a quarter meet at named barriers, and after a failed wait
         // all that follows runs through without waiting
-        for (int n = 0, unit; (unit = dealt(n)) < n_units; ++n) {
+        for (int round = 0, unit; (unit = dealt(round)) < n_units; ++round) {
             const Job j = job(unit);
+            if (j.nt == 0) continue;
             auto do_tile = [&](auto Xc, int t) {
                 constexpr int X = decltype(Xc)::value;
                 const uint32_t sp = tmem_base + X * 2 * kBlk + lane_base + half * 64;
@@ -978,12 +1002,28 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     tc_fence_after_sync();
     const uint32_t tmem_base = sh->tmem_base;
     const long long total = pv.H * sh->prefix[pv.B], share = (total + gridDim.x - 1) / gridDim.x;
-    const long long w0 = blockIdx.x * share, w1 = w0 + share < total ? w0 + share : total;
+    long long w0 = blockIdx.x * share;
+    const long long w1 = w0 + share < total ? w0 + share : total;
     ScorePos at = {};
     SeqRows seq = {};
     if (w0 < w1) {
         at = score_pos(pv, a.nl2a, sh->prefix, w0);
         seq = seq_rows(pv, a.nl2a, at.b);
+    }
+    // the pair behind `at`'s key tile
+    auto next_tile = [&](long long w) {
+        at.q = 0;
+        if (w < w1 && ++at.kt == seq.tiles) {
+            at.kt = 0;
+            if (++at.h == pv.H) {
+                at.h = 0;
+                do seq = seq_rows(pv, a.nl2a, ++at.b); while (seq.tiles == 0);      // there is one: w < w1
+            }
+        }
+    };
+    if (ws.whole_scores && at.q > 0) {                     // that tile is another CTA's
+        w0 += seq.rows_of(at.kt) - at.q;
+        next_tile(w0);
     }
     dependents_may_start();
 
@@ -997,19 +1037,12 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         j.b = at.b; j.h = at.h; j.j0 = at.kt * kBlk;
         j.past = seq.past; j.len = seq.len; j.used = seq.past + seq.len;
         const int n = seq.rows_of(at.kt);
-        j.nq = (int)min((long long)(n - at.q), w1 - w);
+        j.nq = ws.whole_scores ? n : (int)min((long long)(n - at.q), w1 - w);
         j.q0 = seq.first(at.kt) + at.q;
         // a tile begun by another CTA is this one's first, a tile that the next one goes on with its last
         j.part = at.q > 0 ? 2 * blockIdx.x : j.nq < n ? 2 * blockIdx.x + 1 : -1;
         w += j.nq;
-        at.q = 0;
-        if (w < w1 && ++at.kt == seq.tiles) {
-            at.kt = 0;
-            if (++at.h == pv.H) {
-                at.h = 0;
-                do seq = seq_rows(pv, a.nl2a, ++at.b); while (seq.tiles == 0);      // there is one: w < w1
-            }
-        }
+        next_tile(w);
         return j;
     };
     auto wait = [&](uint64_t *bar, uint32_t parity) -> bool {
@@ -1187,7 +1220,9 @@ TcWs carve(const PagedView &pv, void *mem, size_t *bytes)
     const size_t U = (size_t)pv.B * pv.H, items = (size_t)pv.B * w.pairs;
     const size_t cap_tiles = (((size_t)pv.max_pages << pv.ps_shift) + kBlk - 1) / kBlk;
     w.max_items = (int)(items + kMaxParts);
-    size_t parts = cap_tiles <= kMinPiece ? 0 : items * pv.H * ((cap_tiles + kMinPiece - 1) / kMinPiece);
+    w.direct = cap_tiles <= kDirectTiles && items * pv.H < 0x7fffffff;
+    w.whole_scores = (pv.c + tile_tokens - 1) / tile_tokens <= kWholeRows;
+    size_t parts = w.direct ? 0 : items * pv.H * ((cap_tiles + kMinPiece - 1) / kMinPiece);
     if (parts > kMaxParts) parts = kMaxParts;
     w.parts = (int)parts;
     char *base = static_cast<char *>(mem);
@@ -1216,17 +1251,22 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
         return cudaErrorInvalidValue;
     const TcWs ws = carve(a.pv, a.ws, nullptr);
     if ((long long)ws.max_items * a.pv.H > 0x7fffffffll) return cudaErrorInvalidValue;
-    if ((e = launch_chained(paged_plan_kernel, 1, kPlanThreads, 0, s, a.pv, ws)) != cudaSuccess) return e;
-    count_launch();
+    if (!ws.direct) {
+        if ((e = launch_chained(paged_plan_kernel, 1, kPlanThreads, 0, s, a.pv, ws)) != cudaSuccess) return e;
+        count_launch();
+    }
     e = launch_chained(paged_attn_tc_kernel<T, D>, kSms, kAttnThreads, attn_smem<D>(), s, mq, mk, mv, a, ws);
     if (e != cudaSuccess) return e;
     count_launch();
-    if ((e = launch_chained(paged_merge_kernel<T, D>, 4 * kSms, kMergeThreads, 0, s, a, ws)) != cudaSuccess) return e;
-    count_launch();
+    if (!ws.direct) {
+        if ((e = launch_chained(paged_merge_kernel<T, D>, 4 * kSms, kMergeThreads, 0, s, a, ws)) != cudaSuccess) return e;
+        count_launch();
+    }
     if (!a.scores) return cudaSuccess;
     e = launch_chained(paged_score_tc_kernel<D>, kScoreCtas, kScoreThreads, score_smem<D>(), s, mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
     if (e != cudaSuccess) return e;
     count_launch();
+    if (ws.whole_scores) return cudaSuccess;
     if ((e = launch_chained(paged_score_join_kernel, kScoreCtas - 1, kBlk, 0, s, a, ws)) != cudaSuccess) return e;
     count_launch();
     return cudaSuccess;
