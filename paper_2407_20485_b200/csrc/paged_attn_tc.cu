@@ -561,12 +561,13 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         for (int round = 0, unit; (unit = dealt(round)) < n_units; ++round) {
             const Job j = job(unit);
             if (j.nt == 0) continue;
-            auto do_tile = [&](auto Xc, int t) {
-                constexpr int X = decltype(Xc)::value;
+            // The stream is a run-time number and each body stands in the code once: a CTA's first pass through
+            // it waits for its instructions (1 to 2 us for every copy of a body).
+            auto do_tile = [&](int X, int t, float &m_x, float &l_x, int cnt_x) {
                 const uint32_t sp = tmem_base + X * 2 * kBlk + lane_base + half * 64;
                 const uint32_t to = tmem_base + X * 2 * kBlk + kBlk + lane_base + half * OW;
                 const int first_token = j.i0 + X * tile_tokens;
-                wait(&sh->s_full[X], cnt[X] & 1);
+                wait(&sh->s_full[X], cnt_x & 1);
                 tc_fence_after_sync();
                 uint32_t v[2][32];
                 tmem_ld32(sp, v[0]);
@@ -607,7 +608,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 float factor = 1.f, rowsum = 0.f;
                 bool exact = (t == 0);
                 if (!exact) {
-                    rowsum = write_p(-m_used[X]);
+                    rowsum = write_p(-m_x);
                     const bool bad = !(rowsum <= kOptimisticLimit);          // also NaN
                     sh->xch[X][half][r] = bad ? 1.f : 0.f;
                     named_barrier(1 + quarter, 64);                // this quarter's two warps
@@ -627,17 +628,17 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (t == 0) {
                         // a piece of the keys may hold none that this row sees (then none of the following
                         // tiles does either): any finite reference gives the zeros that are wanted
-                        m_used[X] = smax == -INFINITY ? 0.f : smax * pv.sl2;
-                        l[X] = 0.f;
+                        m_x = smax == -INFINITY ? 0.f : smax * pv.sl2;
+                        l_x = 0.f;
                     } else {
-                        const float xmax = fmaf(smax, pv.sl2, -m_used[X]);
+                        const float xmax = fmaf(smax, pv.sl2, -m_x);
                         const bool grow = xmax > kRescaleThreshold;
                         if (grow) {
-                            m_used[X] += xmax;
+                            m_x += xmax;
                             factor = ex2_approx(-xmax);
                         }
                         if (__any_sync(0xffffffffu, grow)) {
-                            wait(&sh->o_done[X], (cnt[X] - 1) & 1);          // O holds the tiles before
+                            wait(&sh->o_done[X], (cnt_x - 1) & 1);          // O holds the tiles before
                             tc_fence_after_sync();
 #pragma unroll 1
                             for (int c = 0; c < OW / 32; ++c) {
@@ -651,21 +652,24 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                             tmem_wait_st();
                         }
                     }
-                    rowsum = write_p(-m_used[X]);
+                    rowsum = write_p(-m_x);
                 }
                 tmem_wait_st();
-                l[X] = fmaf(l[X], factor, rowsum);
+                l_x = fmaf(l_x, factor, rowsum);
                 tc_fence_before_sync();
                 mbar_arrive(&sh->p_full[X]);
-                ++cnt[X];
             };
-            for (int t = 0; t < j.nt; ++t) {
-                if (t < j.ntA) do_tile(std::integral_constant<int, 0>{}, t);
-                if (t < j.ntB) do_tile(std::integral_constant<int, 1>{}, t);
+#pragma unroll 1
+            for (int step = 0; step < 2 * j.nt; ++step) {
+                const int X = step & 1, t = step >> 1;
+                if (t >= (X ? j.ntB : j.ntA)) continue;
+                float m_x = X ? m_used[1] : m_used[0], l_x = X ? l[1] : l[0];
+                do_tile(X, t, m_x, l_x, X ? cnt[1] : cnt[0]);
+                if (X) { m_used[1] = m_x; l[1] = l_x; ++cnt[1]; }
+                else   { m_used[0] = m_x; l[0] = l_x; ++cnt[0]; }
             }
             // ---- epilogue: each thread normalises (or hands on) and stores its half of the columns
-            auto finish = [&](auto Xc, int ntX) {
-                constexpr int X = decltype(Xc)::value;
+            auto finish = [&](int X, int ntX, float m_x, float l_x, int cnt_x) {
                 const int tok = X * tile_tokens + r / G, g = r - r / G * G;
                 const bool live = r < tile_rows && tok < j.tokens && A2SF_IN_RANGE(j.i0 + tok, pv.c, kDbgPagedTc);
                 if (ntX == 0) {
@@ -675,24 +679,39 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 }
                 const uint32_t to = tmem_base + X * 2 * kBlk + kBlk + lane_base + half * OW;
                 named_barrier(1 + quarter, 64);                // the partner has read the last exchange
-                sh->xch[X][half][r] = l[X];
+                sh->xch[X][half][r] = l_x;
                 named_barrier(1 + quarter, 64);
-                const float lsum = l[X] + sh->xch[X][half ^ 1][r];
+                const float lsum = l_x + sh->xch[X][half ^ 1][r];
                 named_barrier(1 + quarter, 64);                // read before the next item writes
-                const bool done = wait(&sh->o_done[X], (cnt[X] - 1) & 1);
-                tc_fence_after_sync();
                 const float inv = 1.f / lsum;
                 const int i = j.i0 + tok;
-                const size_t prow = (size_t)(j.part < 0 ? 0 : j.part) * ws.part_rows * (D / 4) + X * kBlk + r;
-                float4 *po = reinterpret_cast<float4 *>(ws.part_o) + prow + (size_t)(half * OW / 4) * ws.part_rows;
-                // this lane stores piece lane & 3 of rows r0 .. r0 + 3
-                const int r0 = r & ~3;
-                T *orow = static_cast<T *>(a.out) + (int64_t)j.b * a.so.b + half * OW + (lane & 3) * 8;
-#pragma unroll 1
+                // addresses first: the last product is still under way.  This lane stores piece lane & 3 of rows
+                // r0 .. r0 + 3, or its own row's partial columns
+                T *orow[4];
+                float4 *po = nullptr;
+                if (j.part < 0) {
+                    const int r0 = r & ~3;
+                    int tk = X * tile_tokens + r0 / G, gk = r0 - r0 / G * G;
+                    T *base = static_cast<T *>(a.out) + (int64_t)j.b * a.so.b + half * OW + (lane & 3) * 8;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const bool in = r0 + k < tile_rows && tk < j.tokens && A2SF_IN_RANGE(j.i0 + tk, pv.c, kDbgPagedTc);
+                        orow[k] = in ? base + (int64_t)(j.h * G + gk) * a.so.h + (int64_t)(j.i0 + tk) * a.so.t : nullptr;
+                        if (++gk == G) { gk = 0; ++tk; }
+                    }
+                } else if (live) {
+                    po = reinterpret_cast<float4 *>(ws.part_o) + ((size_t)j.part * (D / 4) + half * (OW / 4)) * ws.part_rows + X * kBlk + r;
+                }
+                const bool done = wait(&sh->o_done[X], (cnt_x - 1) & 1);
+                tc_fence_after_sync();
+                uint32_t o[OW / 32][32];
+#pragma unroll
+                for (int c = 0; c < OW / 32; ++c) tmem_ld32(to + c * 32, o[c]);
+                tmem_wait_ld();
+                tc_fence_before_sync();
+                mbar_arrive(&sh->o_free[X]);                   // the accumulator is in registers
+#pragma unroll
                 for (int c = 0; c < OW / 32; ++c) {
-                    uint32_t o[32];
-                    tmem_ld32(to + c * 32, o);
-                    tmem_wait_ld();
                     if (j.part < 0) {
                         uint4 w[4];
 #pragma unroll
@@ -700,37 +719,35 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                             uint32_t x[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                x[e] = pack2<T>(__uint_as_float(o[q4 * 8 + 2 * e]) * inv, __uint_as_float(o[q4 * 8 + 2 * e + 1]) * inv);
+                                x[e] = pack2<T>(__uint_as_float(o[c][q4 * 8 + 2 * e]) * inv, __uint_as_float(o[c][q4 * 8 + 2 * e + 1]) * inv);
                             w[q4] = make_uint4(x[0], x[1], x[2], x[3]);
                         }
                         transpose4(w);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int rk = r0 + k, tk = X * tile_tokens + rk / G, gk = rk - rk / G * G;
-                            if (done && rk < tile_rows && tk < j.tokens)
-                                *reinterpret_cast<uint4 *>(orow + (int64_t)(j.h * G + gk) * a.so.h + (int64_t)(j.i0 + tk) * a.so.t + c * 32) = w[k];
-                        }
-                    } else if (live && done) {
+                        for (int k = 0; k < 4; ++k)
+                            if (orow[k] && done) *reinterpret_cast<uint4 *>(orow[k] + c * 32) = w[k];
+                    } else if (po && done) {
 #pragma unroll
-                        for (int q8 = 0; q8 < 8; ++q8)
-                            po[(size_t)(c * 8 + q8) * ws.part_rows] = make_float4(__uint_as_float(o[q8 * 4]), __uint_as_float(o[q8 * 4 + 1]),
-                                                                                  __uint_as_float(o[q8 * 4 + 2]), __uint_as_float(o[q8 * 4 + 3]));
+                        for (int q8 = 0; q8 < 8; ++q8) {
+                            *po = make_float4(__uint_as_float(o[c][q8 * 4]), __uint_as_float(o[c][q8 * 4 + 1]), __uint_as_float(o[c][q8 * 4 + 2]),
+                                              __uint_as_float(o[c][q8 * 4 + 3]));
+                            po += ws.part_rows;
+                        }
                     }
                 }
-                tc_fence_before_sync();
-                mbar_arrive(&sh->o_free[X]);
                 if (half == 0 && live && done) {
                     if (j.part < 0) {
-                        const float z = m_used[X] + log2f(lsum);
+                        const float z = m_x + log2f(lsum);
                         ws.lse2[((size_t)j.b * pv.H + j.h) * pv.c * G + (size_t)i * G + g] = z;
                         if (a.lse) a.lse[(((size_t)j.b * pv.H + j.h) * G + g) * pv.c + i] = z * 0.6931471805599453f;
                     } else {
-                        ws.part_ml[(size_t)j.part * ws.part_rows + X * kBlk + r] = make_float2(lsum > 0.f ? m_used[X] : -INFINITY, lsum);
+                        ws.part_ml[(size_t)j.part * ws.part_rows + X * kBlk + r] = make_float2(lsum > 0.f ? m_x : -INFINITY, lsum);
                     }
                 }
             };
-            finish(std::integral_constant<int, 0>{}, j.ntA);
-            finish(std::integral_constant<int, 1>{}, j.ntB);
+#pragma unroll 1
+            for (int X = 0; X < 2; ++X)
+                finish(X, X ? j.ntB : j.ntA, X ? m_used[1] : m_used[0], X ? l[1] : l[0], X ? cnt[1] : cnt[0]);
         }
     }
 
