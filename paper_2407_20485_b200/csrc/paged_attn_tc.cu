@@ -554,6 +554,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         const int half = (warp - 2) >> 2;                  // logits 64*half .. 64*half+63
         const int r = quarter * 32 + lane;                 // row in the tile = TMEM lane
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const int r_tok = r / G, r_head = r - r_tok * G;   // token and head of the row in its tile,
+        const int r0_tok = (r & ~3) / G, r0_head = (r & ~3) - r0_tok * G;     // and of the first of four rows
         int cnt[2] = {0, 0};
         float m_used[2], l[2];
         // no early exit here: the two warps of a quarter meet at named barriers, and after a failed wait
@@ -576,7 +578,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const int tile0 = (j.t0 + t) * kBlk;
                 if (tile0 + kBlk > j.past + first_token + 1) {
                     // some row of the tile does not see all of it: a masked logit becomes -inf
-                    const int vis = min(j.past + first_token + r / G + 1, j.used) - tile0 - half * 64;
+                    const int vis = min(j.past + first_token + r_tok + 1, j.used) - tile0 - half * 64;
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -669,8 +671,16 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 else   { m_used[0] = m_x; l[0] = l_x; ++cnt[0]; }
             }
             // ---- epilogue: each thread normalises (or hands on) and stores its half of the columns
-            auto finish = [&](int X, int ntX, float m_x, float l_x, int cnt_x) {
-                const int tok = X * tile_tokens + r / G, g = r - r / G * G;
+            // the halves of the row sums, of both streams at once
+            named_barrier(1 + quarter, 64);                    // the partner has read the last exchange
+            sh->xch[0][half][r] = l[0];
+            sh->xch[1][half][r] = l[1];
+            named_barrier(1 + quarter, 64);
+            l[0] += sh->xch[0][half ^ 1][r];
+            l[1] += sh->xch[1][half ^ 1][r];
+            named_barrier(1 + quarter, 64);                    // read before the next item writes
+            auto finish = [&](int X, int ntX, float m_x, float lsum, int cnt_x) {
+                const int tok = X * tile_tokens + r_tok, g = r_head;
                 const bool live = r < tile_rows && tok < j.tokens && A2SF_IN_RANGE(j.i0 + tok, pv.c, kDbgPagedTc);
                 if (ntX == 0) {
                     // a cut item whose piece lies behind everything stream A sees: an empty partial result
@@ -678,11 +688,6 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     return;
                 }
                 const uint32_t to = tmem_base + X * 2 * kBlk + kBlk + lane_base + half * OW;
-                named_barrier(1 + quarter, 64);                // the partner has read the last exchange
-                sh->xch[X][half][r] = l_x;
-                named_barrier(1 + quarter, 64);
-                const float lsum = l_x + sh->xch[X][half ^ 1][r];
-                named_barrier(1 + quarter, 64);                // read before the next item writes
                 const float inv = 1.f / lsum;
                 const int i = j.i0 + tok;
                 // addresses first: the last product is still under way.  This lane stores piece lane & 3 of rows
@@ -691,7 +696,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 float4 *po = nullptr;
                 if (j.part < 0) {
                     const int r0 = r & ~3;
-                    int tk = X * tile_tokens + r0 / G, gk = r0 - r0 / G * G;
+                    int tk = X * tile_tokens + r0_tok, gk = r0_head;
                     T *base = static_cast<T *>(a.out) + (int64_t)j.b * a.so.b + half * OW + (lane & 3) * 8;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
