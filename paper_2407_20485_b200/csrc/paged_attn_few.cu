@@ -262,6 +262,7 @@ template <typename T, int D, int NC> struct Body16 {
                 const int col = g * 8 + 2 * c + e;
                 if (col >= NP) continue;
                 if (r == 0) ml[col] = make_float2(m[g][e], sum);
+                if (m[g][e] == -INFINITY) continue;         // the row saw nothing here: no output is read either
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     op[(size_t)col * D + k * 16 + r] = o[g][k][e];
@@ -385,6 +386,7 @@ template <int D, int NC> struct Body32 {
 #pragma unroll
             for (int w = 4; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
             if (lane == 0) ml[r] = make_float2(m[r], sum);
+            if (m[r] == -INFINITY) continue;
 #pragma unroll
             for (int e = 0; e < DV; e += 2) *reinterpret_cast<float2 *>(op + (size_t)r * D + lane * DV + e) = make_float2(o[r][e], o[r][e + 1]);
         }
@@ -647,8 +649,8 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int p = grp; p < parts; p += GR) {
-            const float4 v = op[(size_t)p * (NP * D / 4)];
             const float f = ex2(row[p * part_step].x - mx);
+            const float4 v = f > 0.f ? op[(size_t)p * (NP * D / 4)] : make_float4(0.f, 0.f, 0.f, 0.f);
             o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
         }
         __syncthreads();

@@ -42,8 +42,7 @@ constexpr int kSms = 148;
 constexpr int kSplitBelow = 4 * kSms;        // items of a call from which none is cut
 constexpr int kPieces = 4 * kSms;            // pieces that cutting makes at most, next to one per item
 constexpr int kMinPiece = 4;                 // key tiles of a piece at least
-// Sequences of at most so many key tiles need no plan: no item is long, so none is cut and their order is of no
-// account.  Such a call is attn and score alone (12 heads, 244 tokens: 27 us with plan, merge and join, 16 us without).
+// Sequences of at most so many key tiles need no plan: no item is long, so none is cut.  Such a call is attn and score alone (12 heads, 244 tokens: 27 us with plan, merge and join, 16 us without).
 constexpr int kDirectTiles = 8;
 // Up to so many row tiles a key tile's sum is left whole: at most 5 us for one CTA, what the join kernel costs.
 constexpr int kWholeRows = 4;
@@ -394,11 +393,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         Job j;
         Item it;
         if (ws.direct) {
-            // the pairs of a (sequence, head) next to each other, the longest first; pairs behind the chunk are empty
-            const int unit_of = unit / ws.pairs;
-            it.b = unit_of / pv.H;
-            j.h = unit_of - it.b * pv.H;
-            it.pair = ws.pairs - 1 - (unit - unit_of * ws.pairs);
+            // the longest pairs of all sequences and heads first, so that a round of jobs is of about one length; pairs
+            // behind the chunk are empty
+            const int units = pv.B * pv.H, back = unit / units, rest = unit - back * units;
+            it.b = rest / pv.H;
+            j.h = rest - it.b * pv.H;
+            it.pair = ws.pairs - 1 - back;
             const SeqState st = seq_state(pv, it.b);
             it.past = st.past; it.len = st.len; it.part = -1;
             it.t0 = 0;
