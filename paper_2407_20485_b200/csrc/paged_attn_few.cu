@@ -7,7 +7,7 @@
 // The list is built on the device from past and lens (the host knows neither).
 //
 //   main    warp 0 copies tiles (K and V, TMA boxes of up to a page, 128-byte swizzle) into a ring;
-//           consumer warps take 16 slots (8 in 32-bit storage) of each tile and keep their own running
+//           consumer warps take 16 slots (32 for d = 64, 8 in 32-bit storage) of each tile and keep their own running
 //           maximum, sum and output.  16-bit storage: S[16 slots x 8 rows] = K Q^T and O^T[d x 8] += V^T P^T
 //           on mma.sync m16n8k16, K and V^T straight from ldmatrix (.trans for V); P changes from
 //           accumulator to operand layout with movmatrix.  The rows fill 8 of the instruction's columns, so
@@ -30,7 +30,8 @@ namespace {
 
 using namespace tc;
 
-constexpr int kTile = 64;                 // slots per tile
+// Slots of a tile: 16 KB of K and of V for 16-bit rows of either size.
+template <typename T, int D> constexpr int tile_slots = D * sizeof(T) == 128 ? 128 : 64;
 // Consumer warps of a CTA.  32-bit storage spends 8 times the instructions on a slot and runs one CTA per SM
 // (d = 128), so twice as many warps share a tile there to hide each other's latencies.
 template <typename T> constexpr int warps_of = sizeof(T) == 4 ? 8 : 4;
@@ -39,10 +40,11 @@ constexpr int kFinishThreads = 256;
 __host__ __device__ constexpr int rows_padded(int rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
 
 template <typename T, int D> struct Ring {
+    static constexpr int kTile = tile_slots<T, D>;
     static constexpr int kRowBytes = D * (int)sizeof(T);
     static constexpr int kChunks = kRowBytes / 128;                // 128-byte columns of a tile
     static constexpr int kTileBytes = kTile * kRowBytes;           // K or V
-    static constexpr int kStages = kRowBytes == 512 ? 2 : kRowBytes == 256 ? 3 : 6;
+    static constexpr int kStages = kRowBytes == 512 ? 2 : 3;
     static constexpr size_t kBytes = (size_t)kStages * 2 * kTileBytes + 1024;
 };
 
@@ -107,9 +109,9 @@ __device__ __forceinline__ float ex2(float x)
 }
 
 // Byte offset of 16-byte piece `piece` of row `row` in a tile of 128-byte columns (TMA's 128-byte swizzle).
-__device__ __forceinline__ uint32_t tile_offset(int row, int piece)
+template <int Tile> __device__ __forceinline__ uint32_t tile_offset(int row, int piece)
 {
-    return (uint32_t)((piece >> 3) * (kTile * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
+    return (uint32_t)((piece >> 3) * (Tile * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
 }
 
 __device__ __forceinline__ const void *query_row(const AttendArgs &a, int b, int h, int r, size_t elem)
@@ -120,7 +122,7 @@ __device__ __forceinline__ const void *query_row(const AttendArgs &a, int b, int
 
 // ---- a consumer warp on 16-bit storage: NC = 8 or 16 row columns ------------------------------------
 template <typename T, int D, int NC> struct Body16 {
-    static constexpr int CG = NC / 8, KS = D / 16;
+    static constexpr int CG = NC / 8, KS = D / 16, kTile = tile_slots<T, D>, kSub = kTile / warps_of<T> / 16;
     static constexpr float kSlack = std::is_same<T, __half>::value ? 14.f : 60.f;    // fp16 ends at 2^16
     uint32_t q[CG][KS][2];
     float o[CG][KS][4], m[CG][2], l[CG][2];
@@ -150,64 +152,68 @@ template <typename T, int D, int NC> struct Body16 {
         }
     }
 
-    // 16 slots j0 .. j0+15 (rows `row0` .. of the tile); `used` slots of the sequence hold tokens
+    // kSub x 16 slots from j0 on (rows `row0` .. of the tile); `used` slots of the sequence hold tokens
     __device__ void tile(const AttendArgs &a, uint8_t *K, uint8_t *V, int row0, int j0, int used, float *logits, int NP, float *)
     {
         const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-        float s[CG][4];
-#pragma unroll
-        for (int g = 0; g < CG; ++g)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[g][e] = 0.f;
+        float x[kSub][CG][4];
         const uint32_t kb = smem_u32(K), vb = smem_u32(V);
-        {
-            const int row = row0 + (lane & 15), piece = lane >> 4;
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) {
+#pragma unroll
+            for (int g = 0; g < CG; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[u][g][e] = 0.f;
+            const int row = row0 + u * 16 + (lane & 15), piece = lane >> 4;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 uint32_t f[4];
-                ldmatrix4(f, kb + tile_offset(row, 2 * k + piece));
+                ldmatrix4(f, kb + tile_offset<kTile>(row, 2 * k + piece));
 #pragma unroll
-                for (int g = 0; g < CG; ++g) Mma16<T>::mma(s[g], f, q[g][k][0], q[g][k][1]);
+                for (int g = 0; g < CG; ++g) Mma16<T>::mma(x[u][g], f, q[g][k][0], q[g][k][1]);
             }
         }
         // what lies behind the sequence may be anything: its keys are masked, its values made zero
-        if (j0 + 16 > used) {
-            for (int x = lane; x < 16 * (D / 8); x += 32) {
-                const int rr = x / (D / 8);
-                if (j0 + rr >= used) *reinterpret_cast<uint4 *>(V + tile_offset(row0 + rr, x % (D / 8))) = make_uint4(0, 0, 0, 0);
+        if (j0 + kSub * 16 > used) {
+            for (int e = lane; e < kSub * 16 * (D / 8); e += 32) {
+                const int rr = e / (D / 8);
+                if (j0 + rr >= used) *reinterpret_cast<uint4 *>(V + tile_offset<kTile>(row0 + rr, e % (D / 8))) = make_uint4(0, 0, 0, 0);
             }
             fence_async_smem();            // these writes come before the copy that next fills the stage
             __syncwarp();
         }
         // The reference of a column (what is subtracted before the exponential) moves only when a logit exceeds it by
         // more than kSlack: probabilities up to 2^kSlack are as exact, and no maximum is looked for in between.
-        float x[CG][4];
         bool beyond = false;
 #pragma unroll
-        for (int g = 0; g < CG; ++g) {
+        for (int u = 0; u < kSub; ++u)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = j0 + r + (e >> 1) * 8;
-                x[g][e] = j < vis[g][e & 1] ? s[g][e] * a.pv.sl2 : -INFINITY;
-                beyond |= x[g][e] > m[g][e & 1] + kSlack;          // also where m is still -inf
-            }
-            if (logits) {
-                const int col = g * 8 + 2 * c;
+            for (int g = 0; g < CG; ++g) {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float *dst = logits + (size_t)(j0 + r + half * 8) * NP + col;
-                    if (col + 1 < NP) *reinterpret_cast<float2 *>(dst) = make_float2(x[g][2 * half], x[g][2 * half + 1]);
-                    else if (col < NP) *dst = x[g][2 * half];
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j0 + u * 16 + r + (e >> 1) * 8;
+                    x[u][g][e] = j < vis[g][e & 1] ? x[u][g][e] * a.pv.sl2 : -INFINITY;
+                    beyond |= x[u][g][e] > m[g][e & 1] + kSlack;       // also where m is still -inf
+                }
+                if (logits) {
+                    const int col = g * 8 + 2 * c;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float *dst = logits + (size_t)(j0 + u * 16 + r + half * 8) * NP + col;
+                        if (col + 1 < NP) *reinterpret_cast<float2 *>(dst) = make_float2(x[u][g][2 * half], x[u][g][2 * half + 1]);
+                        else if (col < NP) *dst = x[u][g][2 * half];
+                    }
                 }
             }
-        }
         if (__any_sync(0xffffffffu, beyond)) {
 #pragma unroll
             for (int g = 0; g < CG; ++g) {
                 float f[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = fmaxf(x[g][e], x[g][e + 2]);
+                    float mx = fmaxf(x[0][g][e], x[0][g][e + 2]);
+#pragma unroll
+                    for (int u = 1; u < kSub; ++u) mx = fmaxf(mx, fmaxf(x[u][g][e], x[u][g][e + 2]));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -222,28 +228,30 @@ template <typename T, int D, int NC> struct Body16 {
                     for (int e = 0; e < 4; ++e) o[g][k][e] *= f[e & 1];
             }
         }
-        uint32_t p0[CG], p1[CG];
+        uint32_t p[kSub][CG][2];
 #pragma unroll
-        for (int g = 0; g < CG; ++g) {
+        for (int u = 0; u < kSub; ++u)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                // nothing seen so far: any finite reference gives the zeros that are wanted
-                const float ref = m[g][e] == -INFINITY ? 0.f : m[g][e];
-                x[g][e] = ex2(x[g][e] - ref);
-                x[g][e + 2] = ex2(x[g][e + 2] - ref);
-                l[g][e] += x[g][e] + x[g][e + 2];
+            for (int g = 0; g < CG; ++g) {
+                float w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    // nothing seen so far: any finite reference gives the zeros that are wanted
+                    w[e] = ex2(x[u][g][e] - (m[g][e & 1] == -INFINITY ? 0.f : m[g][e & 1]));
+                    l[g][e & 1] += w[e];
+                }
+                p[u][g][0] = movmatrix_trans(Mma16<T>::pack(w[0], w[1]));
+                p[u][g][1] = movmatrix_trans(Mma16<T>::pack(w[2], w[3]));
             }
-            p0[g] = movmatrix_trans(Mma16<T>::pack(x[g][0], x[g][1]));
-            p1[g] = movmatrix_trans(Mma16<T>::pack(x[g][2], x[g][3]));
-        }
-        {
-            const int row = row0 + (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) {
+            const int row = row0 + u * 16 + (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 uint32_t v[4];
-                ldmatrix4_trans(v, vb + tile_offset(row, 2 * k + piece));
+                ldmatrix4_trans(v, vb + tile_offset<kTile>(row, 2 * k + piece));
 #pragma unroll
-                for (int g = 0; g < CG; ++g) Mma16<T>::mma(o[g][k], v, p0[g], p1[g]);
+                for (int g = 0; g < CG; ++g) Mma16<T>::mma(o[g][k], v, p[u][g][0], p[u][g][1]);
             }
         }
     }
@@ -318,7 +326,7 @@ template <int D, int NC> struct Body32 {
         const float *qq = scratch + part * QS;
 #pragma unroll 4
         for (int k = 0; k < QP; k += 4) {
-            const float4 kk = *reinterpret_cast<const float4 *>(K + tile_offset(row0 + s, (part * QP + k) / 4));
+            const float4 kk = *reinterpret_cast<const float4 *>(K + tile_offset<tile_slots<float, D>>(row0 + s, (part * QP + k) / 4));
 #pragma unroll
             for (int r = 0; r < NC; ++r) {
                 const float4 q = *reinterpret_cast<const float4 *>(qq + r * 4 * QS + k);
@@ -365,7 +373,7 @@ template <int D, int NC> struct Body32 {
 #pragma unroll 4
         for (int x = 0; x < n; ++x) {
             float v[DV], p[NC];
-            const uint8_t *src = V + tile_offset(row0 + x, lane * DV / 4) + (lane * DV % 4) * 4;
+            const uint8_t *src = V + tile_offset<tile_slots<float, D>>(row0 + x, lane * DV / 4) + (lane * DV % 4) * 4;
 #pragma unroll
             for (int e = 0; e < DV; e += 2) *reinterpret_cast<float2 *>(v + e) = *reinterpret_cast<const float2 *>(src + e * 4);
 #pragma unroll
@@ -412,7 +420,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 {
     using R = Ring<T, D>;
     using Body = typename BodyOf<T, D, NC>::type;
-    constexpr int kWarps = warps_of<T>, kSlots = kTile / kWarps;     // slots per warp and tile
+    constexpr int kTile = R::kTile, kWarps = warps_of<T>, kSlots = kTile / kWarps;     // slots per warp and tile
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ FewShared sh;
@@ -676,7 +684,7 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
 }
 
 size_t pad(size_t x) { return (x + 255) / 256 * 256; }
-int padded_slots(const PagedView &pv) { return ((pv.max_pages << pv.ps_shift) + kTile - 1) / kTile * kTile; }
+int padded_slots(const PagedView &pv) { return ((pv.max_pages << pv.ps_shift) + 127) / 128 * 128; }       // of either tile
 
 FewWs carve(int dtype, const PagedView &pv, void *ws, size_t *bytes)
 {
@@ -704,7 +712,7 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     cudaError_t e = allow_dynamic_smem<paged_few_kernel<T, D, NC>>(smem);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
-    const int box = a.pv.ps < kTile ? a.pv.ps : kTile;
+    const int box = a.pv.ps < R::kTile ? a.pv.ps : R::kTile;
     if (!make_pool_map(&mk, dtype, a.pv.k, a.pv, box) || !make_pool_map(&mv, dtype, a.pv.v, a.pv, box)) return cudaErrorInvalidValue;
     const FewWs ws = carve(dtype, a.pv, a.ws, nullptr);
     const int NP = rows_padded(a.pv.c * a.pv.G);
