@@ -530,28 +530,28 @@ constexpr int kMlCache = 2048;            // partial (maximum, sum) pairs that f
 
 template <int NP> struct SlotBatch {
     static constexpr int kScoreSlots = NP >= 8 ? 2 : 4;
-    float *dst[kScoreSlots];
+    int32_t row[kScoreSlots];                 // of the pool, or -1
     float old[kScoreSlots], x[kScoreSlots][NP];
 
     __device__ void addresses(const PagedView &pv, const int32_t *table, int h, int jb, int j1)
     {
-        int page[kScoreSlots];
 #pragma unroll
         for (int e = 0; e < kScoreSlots; ++e) {
             const int j = jb + e * kFinishThreads;
-            page[e] = j < j1 ? page_for_write(pv, table, j) : -1;
+            row[e] = j < j1 ? page_for_write(pv, table, j) : -1;
         }
 #pragma unroll
         for (int e = 0; e < kScoreSlots; ++e) {
-            dst[e] = page[e] >= 0 ? pv.scores + pool_row(pv, page[e], h, jb + e * kFinishThreads) : nullptr;
-            old[e] = dst[e] ? *dst[e] : 0.f;
+            if (row[e] < 0) continue;
+            row[e] = (int32_t)pool_row(pv, row[e], h, jb + e * kFinishThreads);
+            old[e] = pv.scores[row[e]];
         }
     }
     __device__ void logits(const float *src, int jb)
     {
 #pragma unroll
         for (int e = 0; e < kScoreSlots; ++e) {
-            if (!dst[e]) continue;
+            if (row[e] < 0) continue;
             const float *s = src + (size_t)(jb + e * kFinishThreads) * NP;
             if constexpr (NP == 1) x[e][0] = s[0];
             else if constexpr (NP == 2) {
@@ -566,15 +566,15 @@ template <int NP> struct SlotBatch {
             }
         }
     }
-    __device__ void store(const float *row_c, float decay)
+    __device__ void store(float *scores, const float *row_c, float decay)
     {
 #pragma unroll
         for (int e = 0; e < kScoreSlots; ++e) {
-            if (!dst[e]) continue;
+            if (row[e] < 0) continue;
             float gain = 0.f;              // rows that do not see the slot, or are none, have -inf there
 #pragma unroll
             for (int r = 0; r < NP; ++r) gain += ex2(x[e][r] - row_c[r]);
-            *dst[e] = fmaf(old[e], decay, gain);
+            scores[row[e]] = fmaf(old[e], decay, gain);
         }
     }
 };
@@ -642,11 +642,11 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
     }
     __syncthreads();
     const float decay = exp2f(-age_exponent(st.len, a.nl2a));
-    batch.store(row_c, decay);
+    batch.store(pv.scores, row_c, decay);
     for (int jb = j0 + SlotBatch<NP>::kScoreSlots * kFinishThreads; jb < j1; jb += SlotBatch<NP>::kScoreSlots * kFinishThreads) {
         batch.addresses(pv, table, h, jb + tid, j1);
         batch.logits(logits, jb + tid);
-        batch.store(row_c, decay);
+        batch.store(pv.scores, row_c, decay);
     }
     for (int r = y; r < rows; r += blocks) {
         // thread groups take every GR-th partial result; joined in a fixed order
