@@ -487,9 +487,7 @@ _addressof = ctypes.addressof
 
 def a2sf_rotary(plan: a2sf_rotary_plan, x, out=None, positions=None, start=None, lens=None, transpose=False, stream=None):
     """x [B,H,n,d] rotated by its positions (``positions`` [B,n], or ``start`` [B] + t, or t).  ``out`` may be x."""
-    if out is None:
-        out = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
-    status = _calls.rotary(_addressof(plan), x, out, positions, start, lens, transpose, -1 if stream is None else stream.cuda_stream)
+    status, out = _calls.rotary(_addressof(plan), x, out, positions, start, lens, transpose, -1 if stream is None else stream.cuda_stream)
     if status != A2SF_OK:
         raise A2SFError(status, "a2sf_rotary")
     return out

@@ -65,31 +65,43 @@ template <typename T> T *array(const OptTensor &x, at::IntArrayRef shape, int de
     return static_cast<T *>(x->data_ptr());
 }
 
-// the device made current for the call, and the stream: an address, or -1 for the device's current one
+// The device and the stream made current for the call: a stream's address, or -1 for the device's current one.  What
+// the call allocates then belongs to the stream that it runs on.
 struct Place {
-    c10::cuda::OptionalCUDAGuard guard;
+    c10::cuda::OptionalCUDAGuard device_guard;
+    c10::cuda::OptionalCUDAStreamGuard stream_guard;
     void *stream;
     Place(int device, int64_t given, const char *name)
     {
         if (device < 0) throw pybind11::value_error(std::string(name) + ": tensors must be on a CUDA device");
-        guard.set_index((c10::DeviceIndex)device);
-        stream = given == -1 ? (void *)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream() : (void *)given;
+        const auto index = (c10::DeviceIndex)device;
+        if (given == -1) {
+            device_guard.set_index(index);
+            stream = (void *)c10::cuda::getCurrentCUDAStream(index).stream();
+        } else {
+            stream_guard.reset_stream(c10::cuda::getStreamFromExternal(reinterpret_cast<cudaStream_t>(given), index));
+            stream = (void *)given;
+        }
     }
 };
 
-int rotary(int64_t plan, const Tensor &x, const Tensor &out, const OptTensor &positions, const OptTensor &start, const OptTensor &lens,
-           bool transpose, int64_t stream)
+std::pair<int, Tensor> rotary(int64_t plan, const Tensor &x, const OptTensor &out_opt, const OptTensor &positions, const OptTensor &start,
+                              const OptTensor &lens, bool transpose, int64_t stream)
 {
     if (x.dim() != 4) throw pybind11::value_error("x: expected a [B,H,n,d] tensor");
     const int device = x.get_device();
     const auto shape = x.sizes();
-    const Rows xr(x, shape, x.scalar_type(), device, "x"), yr(out, shape, x.scalar_type(), device, "out");
+    const Rows xr(x, shape, x.scalar_type(), device, "x");
+    Place at(device, stream, "a2sf_rotary");
+    const Tensor out = out_opt ? *out_opt : at::empty_strided(shape, x.strides(), x.options());
+    const Rows yr(out, shape, x.scalar_type(), device, "out");
     const int64_t B = shape[0], n = shape[2];
     const int32_t *pos = array<int32_t>(positions, {B, n}, device, "positions"), *st = array<int32_t>(start, {B}, device, "start"),
                   *ln = array<int32_t>(lens, {B}, device, "lens");
-    Place at(device, stream, "a2sf_rotary");
-    return fn.rotary(reinterpret_cast<const a2sf_rotary_plan *>(plan), dtype_code(x.scalar_type()), (int32_t)B, (int32_t)shape[1], (int32_t)n,
-                     (int32_t)shape[3], xr.p, xr.b, xr.h, xr.t, yr.p, yr.b, yr.h, yr.t, pos, st, ln, transpose ? A2SF_ROTARY_TRANSPOSE : 0, at.stream);
+    const int rc = fn.rotary(reinterpret_cast<const a2sf_rotary_plan *>(plan), dtype_code(x.scalar_type()), (int32_t)B, (int32_t)shape[1], (int32_t)n,
+                             (int32_t)shape[3], xr.p, xr.b, xr.h, xr.t, yr.p, yr.b, yr.h, yr.t, pos, st, ln, transpose ? A2SF_ROTARY_TRANSPOSE : 0,
+                             at.stream);
+    return {rc, out};
 }
 
 class Calls {
@@ -104,6 +116,7 @@ public:
         const int64_t c = chunk(k, "k"), kv[4] = {p_.B, p_.H, c, p_.d}, qs[4] = {p_.B, (int64_t)p_.H * p_.group, c, p_.d};
         const Rows kr(k, kv, type_, device_, "k"), vr(v, kv, type_, device_, "v");
         if (!kr.same_strides(vr)) throw pybind11::value_error("k and v need the same strides");
+        Place at(device_, stream, "a2sf_paged_append");
         Rows qr, yr;
         if (q) {
             qr = Rows(*q, qs, type_, device_, "q");
@@ -111,7 +124,6 @@ public:
             yr = Rows(*q_out, qs, type_, device_, "q_out");
         }
         const int32_t *ln = array<int32_t>(lens, {p_.B}, device_, "lens");
-        Place at(device_, stream, "a2sf_paged_append");
         const int rc = fn.append(&p_, reinterpret_cast<const a2sf_rotary_plan *>(plan), (int32_t)c, ln, kr.p, vr.p, kr.b, kr.h, kr.t, qr.p, qr.b, qr.h, qr.t,
                                  yr.p, yr.b, yr.h, yr.t, at.stream);
         return {rc, q ? q_out : OptTensor()};

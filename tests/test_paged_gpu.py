@@ -320,6 +320,8 @@ EVI = [
     (1, 1, 128, HF, 16, [20000], 3, 5000, 100, False, "rand"),
     (1, 2, 64, BF, 16, [20000], 1, 600, 599, True, "ties"),
     (2, 2, 64, BF, 16, [50, 60], 4, 100000, 7, False, "rand"),
+    (1, 1, 64, BF, 128, [40000], 1, 30000, 100, False, "ties"),
+    (1, 1, 64, HF, 128, [40000], 9, 9000, 1000, True, "rand"),
 ]
 
 
@@ -629,3 +631,45 @@ def test_the_largest_batch_with_mostly_empty_sequences(a2sf):
     check_attend(a2sf, (B, 1, 1, 64, BF, 16, past, 1, lens, 0.5, "bhnd", 0.0))
     lens = [20 * n for n in lens]
     check_attend(a2sf, (B, 1, 1, 64, HF, 16, past, 20, lens, 0.5, "bhnd", 0.0))
+
+
+def test_append_queries_in_place_and_a_cache_without_start(a2sf):
+    """q_out = q; start = NULL: positions and the recent window follow from past."""
+    import ctypes
+
+    B, H, G, d, c = 2, 3, 2, 64, 5
+    plan = a2sf.a2sf_rotary_plan_init(d)
+    g = torch.Generator().manual_seed(12)
+    q, k, v = (torch.randn((B, h, c, d), generator=g).to(HF).cuda() for h in (H * G, H, H))
+    a, b = (pu.make_cache(a2sf, B, H, G, d, HF, 16, [20, 3], c, seed=6) for _ in range(2))
+    b.p.start = None
+    b._calls = a2sf._calls.Calls(ctypes.addressof(b.p), 0)
+    want = a.a2sf_paged_append(k, v, q=q, rotary=plan)
+    mine = q.clone()
+    got = b.a2sf_paged_append(k, v, q=mine, q_out=mine, rotary=plan)
+    assert got.data_ptr() == mine.data_ptr() and torch.equal(got, want)
+    for x in (a, b):
+        x.a2sf_paged_attend(want, 0.5)
+        x.a2sf_paged_evict(8, 4, c)
+    for name in ("k_pages", "v_pages", "scores", "positions", "past"):
+        assert torch.equal(getattr(a, name).double().nan_to_num(7.0), getattr(b, name).double().nan_to_num(7.0)), name
+    assert a.start.tolist() == b.start.tolist() == [20 + c, 3 + c]
+
+
+def test_a_call_on_a_given_stream_allocates_there(a2sf):
+    """Workspaces and outputs of a call on a given stream come from that stream's memory: work queued on the
+    current stream afterwards may not get it while the call is still running."""
+    B, H, d, c = 2, 8, 128, 64
+    g = torch.Generator().manual_seed(13)
+    q, k, v = (torch.randn((B, H, c, d), generator=g).to(BF).cuda() for _ in range(3))
+    cache, ref = (pu.make_cache(a2sf, B, H, 1, d, BF, 64, [3000, 2000], c, seed=6) for _ in range(2))
+    for x in (cache, ref):
+        x.a2sf_paged_append(k, v)
+    want = ref.a2sf_paged_attend(q, 0.9)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    out, lse = cache.a2sf_paged_attend(q, 0.9, stream=side)
+    for _ in range(20):                                 # would land in the workspace, were it the current stream's
+        torch.full((cache.attend_workspace_bytes(c) // 4,), float("nan"), device="cuda")
+    torch.cuda.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1]) and torch.equal(cache.scores.nan_to_num(7.0), ref.scores.nan_to_num(7.0))
