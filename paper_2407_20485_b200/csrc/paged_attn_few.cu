@@ -36,6 +36,9 @@ template <typename T, int D> constexpr int tile_slots = D * sizeof(T) == 128 ? 1
 // (d = 128), so twice as many warps share a tile there to hide each other's latencies.
 template <typename T> constexpr int warps_of = sizeof(T) == 4 ? 8 : 4;
 constexpr int kFinishThreads = 256;
+// How far a logit may lie above its column's reference (log2 units): 2^14 is a probability that fp16 holds, and
+// sums of it and of values up to 2^113 / slots stay finite.
+constexpr float kSlack = 14.f;
 
 __host__ __device__ constexpr int rows_padded(int rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
 
@@ -123,7 +126,6 @@ __device__ __forceinline__ const void *query_row(const AttendArgs &a, int b, int
 // ---- a consumer warp on 16-bit storage: NC = 8 or 16 row columns ------------------------------------
 template <typename T, int D, int NC> struct Body16 {
     static constexpr int CG = NC / 8, KS = D / 16, kTile = tile_slots<T, D>, kSub = kTile / warps_of<T> / 16;
-    static constexpr float kSlack = std::is_same<T, __half>::value ? 14.f : 60.f;    // fp16 ends at 2^16
     uint32_t q[CG][KS][2];
     float o[CG][KS][4], m[CG][2], l[CG][2];
     int vis[CG][2];
@@ -347,7 +349,7 @@ template <int D, int NC> struct Body32 {
             const bool seen = j < past + seen_by(r);
             acc[r] = seen ? acc[r] * a.pv.sl2 : -INFINITY;
             if (logits && part == r % 4) logits[(size_t)j * NC + r] = acc[r];
-            beyond |= acc[r] > m[r] + 60.f;
+            beyond |= acc[r] > m[r] + kSlack;
         }
         if (__any_sync(0xffffffffu, beyond)) {
 #pragma unroll

@@ -1132,6 +1132,9 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 for (int t = 0; t < j.nq; ++t, ++qt) {
                     const int s = qt % kScoreStages, acc = qt & 1;
                     wait(&sh->q_full[s], (qt / kScoreStages) & 1);
+                    // from the third product on the epilogue is waited for, which waits for the attention: a time
+                    // that no limit of a wait may hold
+                    if (qt == 2) dependency_wait();
                     wait(&sh->acc_empty[acc], ((qt >> 1) & 1) ^ 1);
                     tc_fence_after_sync();
                     issue_qk<D>(tmem_base + acc * kBlk, k_desc, q_desc + s * (uint64_t)(kTileBytes >> 4), idesc);
@@ -1156,6 +1159,7 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     old = *dst;
                 }
             }
+            if (qt == 0) dependency_wait();                 // as the producer does: not a wait with a limit
             float sum = 0.f;
             for (int t = 0; t < j.nq; ++t, ++qt) {
                 const int acc = qt & 1, i0 = (j.q0 + t) * tile_tokens;

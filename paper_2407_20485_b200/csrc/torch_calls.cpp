@@ -65,6 +65,12 @@ template <typename T> T *array(const OptTensor &x, at::IntArrayRef shape, int de
     return static_cast<T *>(x->data_ptr());
 }
 
+// A new output for x: of its layout, or contiguous where rows of x overlap or lie apart.
+Tensor like(const Tensor &x)
+{
+    return x.is_non_overlapping_and_dense() ? at::empty_strided(x.sizes(), x.strides(), x.options()) : at::empty(x.sizes(), x.options());
+}
+
 // The device and the stream made current for the call: a stream's address, or -1 for the device's current one.  What
 // the call allocates then belongs to the stream that it runs on.
 struct Place {
@@ -93,7 +99,7 @@ std::pair<int, Tensor> rotary(int64_t plan, const Tensor &x, const OptTensor &ou
     const auto shape = x.sizes();
     const Rows xr(x, shape, x.scalar_type(), device, "x");
     Place at(device, stream, "a2sf_rotary");
-    const Tensor out = out_opt ? *out_opt : at::empty_strided(shape, x.strides(), x.options());
+    const Tensor out = out_opt ? *out_opt : like(x);
     const Rows yr(out, shape, x.scalar_type(), device, "out");
     const int64_t B = shape[0], n = shape[2];
     const int32_t *pos = array<int32_t>(positions, {B, n}, device, "positions"), *st = array<int32_t>(start, {B}, device, "start"),
@@ -120,7 +126,7 @@ public:
         Rows qr, yr;
         if (q) {
             qr = Rows(*q, qs, type_, device_, "q");
-            if (!q_out) q_out = at::empty_strided(q->sizes(), q->strides(), q->options());
+            if (!q_out) q_out = like(*q);
             yr = Rows(*q_out, qs, type_, device_, "q_out");
         }
         const int32_t *ln = array<int32_t>(lens, {p_.B}, device_, "lens");
@@ -135,7 +141,7 @@ public:
         const int64_t c = chunk(q, "q"), qs[4] = {p_.B, (int64_t)p_.H * p_.group, c, p_.d};
         const Rows qr(q, qs, type_, device_, "q");
         Place at(device_, stream, "a2sf_paged_attend");
-        const Tensor out = out_opt ? *out_opt : at::empty_strided(q.sizes(), q.strides(), q.options());
+        const Tensor out = out_opt ? *out_opt : like(q);
         const Tensor lse = lse_opt ? *lse_opt : at::empty({qs[0], qs[1], c}, q.options().dtype(at::kFloat));
         const Rows yr(out, qs, type_, device_, "out");
         float *z = array<float>(lse, {qs[0], qs[1], c}, device_, "lse");
@@ -149,6 +155,8 @@ public:
     int evict(int64_t budget, int64_t recent, int64_t c, const OptTensor &lens, const OptTensor &dst, const Tensor &past_out, const Tensor &start_out,
               const OptTensor &workspace, int64_t stream)
     {
+        for (const int64_t x : {budget, recent, c})
+            if (x != (int32_t)x) throw pybind11::value_error("budget, recent and c are 32-bit numbers");
         if (dst && dst->dim() != 2) throw pybind11::value_error("dst_table: expected [B, pages]");
         const int64_t pages = dst ? dst->size(1) : 0;
         const int32_t *ln = array<int32_t>(lens, {p_.B}, device_, "lens"), *dt = array<int32_t>(dst, {p_.B, pages}, device_, "dst_table");

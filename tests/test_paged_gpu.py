@@ -673,3 +673,40 @@ def test_a_call_on_a_given_stream_allocates_there(a2sf):
         torch.full((cache.attend_workspace_bytes(c) // 4,), float("nan"), device="cuda")
     torch.cuda.synchronize()
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1]) and torch.equal(cache.scores.nan_to_num(7.0), ref.scores.nan_to_num(7.0))
+
+
+def test_inputs_whose_rows_overlap_or_lie_apart_get_outputs_of_their_own(a2sf):
+    """x[b,h,t] = row h + t of one matrix (strides of d allow it); and every third row of a larger tensor."""
+    g = torch.Generator().manual_seed(14)
+    H, n, d = 4, 20, 64
+    base = torch.randn((H + n, d), generator=g).to(BF).cuda()
+    plan = a2sf.a2sf_rotary_plan_init(d)
+    for x in (base.as_strided((1, H, n, d), (0, d, d, 1)), torch.randn((1, n, 3 * H, d), generator=g).to(BF).cuda().transpose(1, 2)[:, ::3]):
+        flat = x.contiguous()
+        assert torch.equal(a2sf.a2sf_rotary(plan, x), a2sf.a2sf_rotary(plan, flat))
+        a, b = (pu.make_cache(a2sf, 1, H, 1, d, BF, 16, [40], n, seed=6) for _ in range(2))
+        assert torch.equal(a.a2sf_paged_append(flat, flat, q=x, rotary=plan), b.a2sf_paged_append(flat, flat, q=flat, rotary=plan))
+        for got, want in zip(a.a2sf_paged_attend(x), b.a2sf_paged_attend(flat)):
+            assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_large_values_under_logits_that_rise_by_tiles(a2sf, dtype):
+    """Logits 0, 10, .. 40 in turn every 64 slots, values of 1e30: no sum before the division may overflow."""
+    d, ps, L = 128, 128, 76800
+    g = torch.Generator().manual_seed(15)
+    cache = a2sf.PagedCache(1, 1, d, dtype, ps, L // ps, L // ps, scale=1.0)
+    logit = (torch.arange(L) // 64 % 5 * 10).to(dtype)
+    k, v = torch.zeros((L, d), dtype=dtype), (torch.randn((L, d), generator=g) * 1e30).to(dtype)
+    k[:, 0] = logit
+    cache.k_pages.copy_(k.view(-1, 1, ps, d))
+    cache.v_pages.copy_(v.view(-1, 1, ps, d))
+    cache.page_table.copy_(torch.arange(L // ps).view(1, -1))
+    cache.past.fill_(L - 1)
+    q = torch.zeros((1, 1, 1, d), dtype=dtype, device="cuda")
+    q[..., 0] = 1
+    out, lse = cache.a2sf_paged_attend(q, 0.5)
+    o, z, s, size, _ = pu.attend_ref(k.double(), v.double(), q[0].cpu().double(), torch.zeros(L, dtype=torch.float64), L - 1, 0.5, 1.0)
+    u, e = torch.finfo(dtype).eps / 2, (d + 2) * F * 40
+    close(out[0], o, u * o.abs() + (u + 2 * e + 2.0 ** -20 + L * F) * size, "out")
+    close(lse[0], z, torch.full_like(z, e + 2.0 ** -20) + 4 * F * z.abs(), "lse")

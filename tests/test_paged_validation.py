@@ -141,3 +141,10 @@ def test_the_binding_refuses_tensors_of_other_shapes_types_and_places(a2sf):
                  lambda: a2sf.PagedCache(2, 3, 64, torch.bfloat16, 16, 10, 4, k_pages=torch.zeros(1))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_the_binding_refuses_numbers_of_more_than_32_bits(a2sf):
+    cache = a2sf.PagedCache(2, 3, 64, torch.bfloat16, 16, 10, 4, device="cpu")
+    for bad in (dict(budget=2 ** 32 + 5, recent=1), dict(budget=5, recent=2 ** 32 + 1), dict(budget=5, recent=1, c=2 ** 32 + 1)):
+        with pytest.raises(ValueError, match="32-bit"):
+            cache.a2sf_paged_evict(**bad)
