@@ -467,16 +467,18 @@ cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int re
         if (e == cudaSuccess) count_launch();
         return e;
     };
+    // static shared memory counts towards the 48 KB that need no permission: it is asked for the most, whatever this call takes
+    constexpr size_t most = (size_t)kCached * 8;
     cudaError_t e;
     switch (row_bytes) {
     case 128:
-        if ((e = allow_dynamic_smem<paged_select_kernel<128>>(smem)) != cudaSuccess) return e;
+        if ((e = allow_dynamic_smem<paged_select_kernel<128>>(most)) != cudaSuccess) return e;
         return run(paged_select_kernel<128>, paged_move_kernel<128>);
     case 256:
-        if ((e = allow_dynamic_smem<paged_select_kernel<256>>(smem)) != cudaSuccess) return e;
+        if ((e = allow_dynamic_smem<paged_select_kernel<256>>(most)) != cudaSuccess) return e;
         return run(paged_select_kernel<256>, paged_move_kernel<256>);
     default:
-        if ((e = allow_dynamic_smem<paged_select_kernel<512>>(smem)) != cudaSuccess) return e;
+        if ((e = allow_dynamic_smem<paged_select_kernel<512>>(most)) != cudaSuccess) return e;
         return run(paged_select_kernel<512>, paged_move_kernel<512>);
     }
 }

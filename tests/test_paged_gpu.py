@@ -710,3 +710,29 @@ def test_large_values_under_logits_that_rise_by_tiles(a2sf, dtype):
     u, e = torch.finfo(dtype).eps / 2, (d + 2) * F * 40
     close(out[0], o, u * o.abs() + (u + 2 * e + 2.0 ** -20 + L * F) * size, "out")
     close(lse[0], z, torch.full_like(z, e + 2.0 ** -20) + 4 * F * z.abs(), "lse")
+
+
+def test_the_first_eviction_of_a_process_at_any_capacity():
+    """What a kernel may take of shared memory is asked for once: the first call decides, so it is a process of its own."""
+    import subprocess
+    import sys
+    from pathlib import Path
+
+    code = """
+import torch
+from paper_2407_20485_b200 import binding as a2sf
+for d, dtype in ((64, torch.bfloat16), (128, torch.bfloat16), (128, torch.float32)):
+    for slots in (5120, 5632, 6016, 6144, 6272):
+        cache = a2sf.PagedCache(1, 1, d, dtype, 128, slots // 128, slots // 128)
+        cache.page_table.copy_(torch.arange(slots // 128).view(1, -1))
+        cache.k_pages.zero_(), cache.v_pages.zero_()
+        cache.scores.copy_(torch.arange(slots).view(-1, 1, 128))
+        cache.positions.copy_(torch.arange(slots).view(-1, 1, 128))
+        cache.past.fill_(slots - 1), cache.start.fill_(slots - 1)
+        cache.a2sf_paged_evict(100, 0)
+        assert cache.past.tolist() == [100] and sorted(cache.scores[0, 0, :100].tolist()) == list(range(slots - 100, slots)), slots
+assert a2sf.a2sf_last_device_status() == 0
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300,
+                       cwd=Path(__file__).resolve().parent.parent)
+    assert r.returncode == 0, r.stderr[-2000:]
