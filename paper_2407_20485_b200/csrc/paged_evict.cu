@@ -3,14 +3,17 @@
 // One CTA per (sequence, K/V head).  Of n slots, n - M leave: the smallest under (score, position, slot) among
 // those outside the recent window.  A radix search narrows the score at which the cut falls, 8 bits at a
 // time, and then the position -- many scores are equal when alpha = 0 or a chunk was just appended -- until at
-// most kShort slots are left to decide about; those are ranked directly.  Usually two digits do.  The survivors
+// most kShort slots are left to decide about; those are ranked directly.  Usually two digits do; bits that all
+// candidates share are passed over (a cut among 950 equal scores: 35 us digit by digit, 28 so).  The survivors
 // become a bit mask, and a scan over it in slot order lists the moves: integer work, exact, the same on
 // every run.  In place only the survivors above M move, into the holes below M: at most min(M, n - M) rows.
 //
 // Bound by memory -- 8 bytes per slot for the decision, two rows read and written per move -- where there are many
 // heads: then a CTA moves its own rows, and one CTA's search hides behind the others' copies.  Where there are
-// few, long moves are left to a kernel that spreads them over the whole device.  past and start change in the
-// last kernel only: past_out may be past, which every CTA reads.
+// few, long moves are left to a kernel that spreads them over the whole device.  Every CTA reads past and start, so
+// where past_out or start_out is one of them they change in a kernel behind.
+#include <type_traits>
+
 #include "paged.cuh"
 
 namespace a2sf {
@@ -19,13 +22,13 @@ A2SF_DEBUG_TRANSLATION_UNIT(paged_evict)
 
 namespace {
 
-constexpr int kSelThreads = 256;
-constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kCached = 16384;       // slots whose score key and position fit in shared memory
 constexpr int kMaskWords = 1024;     // survivors' mask: 32768 slots; beyond, it is worked out again where it is needed
 constexpr int kShort = 64;           // slots that are ranked directly
 constexpr int kFewDrops = 8;         // as many slots leave one minimum after the other
 constexpr int kInline = 64;          // moves that the searching CTA makes itself in any case
+constexpr int kDirect = 256;         // ... and all that a call can have, where nothing else asks for a second kernel
+constexpr int kWide = 512;           // threads of a searching CTA where heads are few
 constexpr int kRows = 4;             // rows of a lane group in flight
 
 struct EvictArgs {
@@ -38,6 +41,7 @@ struct EvictArgs {
     int32_t *moves;                  // [U]
     int32_t *ends;                   // [B][2] new past, new start
     int blocks;                      // of the move kernel, per unit; 0: every CTA moves its own rows
+    bool direct;                     // there is no move kernel: the lengths change here
 };
 
 // Order-preserving key of a score, -0 like +0, every NaN behind infinity; kNoKey stands for a slot that is no
@@ -50,10 +54,11 @@ __device__ __forceinline__ unsigned score_key(float s)
     return s != s ? 0xfffffffeu : key;
 }
 
-struct SelShared {
+template <int NT> struct SelShared {
+    static constexpr int kSelWarps = NT / 32;
     int hist[256];
     int warp_tot[2][kSelWarps + 1];
-    unsigned prefix;
+    unsigned prefix, all_or, all_and;
     int rank, equal, total, count;
     unsigned list_key[kShort], list_pos[kShort];
     int list_slot[kShort];
@@ -65,8 +70,9 @@ struct SelShared {
 };
 
 // Exclusive scan of one int per warp (lane 0 holds it) over the CTA's warps, for `which`.
-__device__ __forceinline__ int warps_excl_scan(SelShared &sh, int which, int v, int &total)
+template <int NT> __device__ __forceinline__ int warps_excl_scan(SelShared<NT> &sh, int which, int v, int &total)
 {
+    constexpr int kSelWarps = NT / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (lane == 0) sh.warp_tot[which][warp] = v;
     __syncthreads();
@@ -123,12 +129,13 @@ __device__ __forceinline__ void move_rows(const EvictArgs &a, int u, int b, int 
     }
 }
 
-template <int ROW_BYTES>
-__global__ void __launch_bounds__(kSelThreads, 3)
+template <int ROW_BYTES, int kSelThreads>
+__global__ void __launch_bounds__(kSelThreads, kSelThreads == 256 ? 3 : 1)
 paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
 {
+    constexpr int kSelWarps = kSelThreads / 32;
     extern __shared__ __align__(16) unsigned cache[];   // [cached] keys, [cached] positions
-    __shared__ SelShared sh;
+    __shared__ SelShared<kSelThreads> sh;
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = u / a.pv.H, h = u - b * a.pv.H;
     dependency_wait();
@@ -139,8 +146,8 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
     const long long newest = (long long)start + st.len - a.R;       // positions from here on are recent
     const int32_t *table = a.pv.table + (size_t)b * a.pv.max_pages;
     if (h == 0 && tid == 0) {
-        a.ends[2 * b] = min(n, M);
-        a.ends[2 * b + 1] = start + st.len;
+        (a.direct ? a.past_out[b] : a.ends[2 * b]) = min(n, M);
+        (a.direct ? a.start_out[b] : a.ends[2 * b + 1]) = start + st.len;
     }
     const bool fresh = a.dst_table != nullptr;
     const int drop = n - M;
@@ -254,46 +261,42 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
             for (int r = 0; r < drop; ++r) moves += sh.leaving[r] < M;
         }
         if (!found) {
-            // digit 0-3: score, 4-7: position, 8-11: slot.  A candidate is still in question when it agrees with the
-            // threshold in all digits found so far.
-            unsigned thr[3] = {0u, 0u, 0u};
-            auto prefix_mask = [](int digits) { return digits <= 0 ? 0u : digits >= 4 ? 0xffffffffu : 0xffffffffu << (32 - 8 * digits); };
-            auto agrees_beyond_score = [&](int digits, int j) {
-                const unsigned p = pos_at(j);
-                return ((p ^ thr[1]) & prefix_mask(digits - 4)) == 0u && (((unsigned)j ^ thr[2]) & prefix_mask(digits - 8)) == 0u;
+            // The threshold's score is found from the top, eight bits at a time, then its position and its slot (part 0, 1, 2).  A
+            // candidate is in question while it agrees with all that is known; `open` are the bits of the part that are not.
+            unsigned thr[3] = {0u, 0u, 0u}, open = 0xffffffffu;
+            int part = 0, shift = 24;
+            auto value = [&](unsigned k, int j) { return part == 0 ? k : part == 1 ? pos_at(j) : (unsigned)j; };
+            auto agrees = [&](unsigned k, int j) {
+                if (k == kNoKey || ((k ^ thr[0]) & (part == 0 ? ~open : 0xffffffffu)) != 0u) return false;
+                if (part == 0) return true;
+                return ((pos_at(j) ^ thr[1]) & (part == 1 ? ~open : 0xffffffffu)) == 0u && (part < 2 || (((unsigned)j ^ thr[2]) & ~open) == 0u);
             };
-            int rank = drop, digit = 0;                      // 1-based rank of the last one to leave
+            int rank = drop, total = n;                      // 1-based rank of the last one to leave
             for (;;) {
-                const int shift = 24 - 8 * (digit & 3);
-                sh.hist[tid] = 0;
-                if (tid == 0) sh.count = 0;
+                if (tid < 256) sh.hist[tid] = 0;
+                if (tid == 0) { sh.count = 0; sh.all_or = 0u; sh.all_and = 0xffffffffu; }
                 __syncthreads();
-                const unsigned above = prefix_mask(digit);
                 for (int j = 4 * tid; j < n; j += 4 * kSelThreads) {
                     unsigned k[4];
                     keys4(j, k);
-    #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (k[e] == kNoKey || ((k[e] ^ thr[0]) & above) != 0u) continue;
-                        if (digit < 4) atomicAdd(&sh.hist[(k[e] >> shift) & 255u], 1);
-                        else if (agrees_beyond_score(digit, j + e))
-                            atomicAdd(&sh.hist[((digit < 8 ? pos_at(j + e) : (unsigned)(j + e)) >> shift) & 255u], 1);
-                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (agrees(k[e], j + e)) atomicAdd(&sh.hist[(value(k[e], j + e) >> shift) & 255u], 1);
                 }
                 __syncthreads();
                 if (warp == 0) {                             // 8 bins a lane, then the lane that holds the rank
                     int c[8], sum = 0;
-    #pragma unroll
+#pragma unroll
                     for (int e = 0; e < 8; ++e) { c[e] = sh.hist[lane * 8 + e]; sum += c[e]; }
                     int incl = sum;
-    #pragma unroll
+#pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
                         const int x = __shfl_up_sync(0xffffffffu, incl, o);
                         if (lane >= o) incl += x;
                     }
                     int before = incl - sum;
                     if (before < rank && rank <= incl) {
-    #pragma unroll
+#pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             if (before < rank && rank <= before + c[e]) {
                                 sh.prefix = (unsigned)(lane * 8 + e) << shift;
@@ -306,28 +309,58 @@ paged_select_kernel(const __grid_constant__ EvictArgs a, int cached)
                     if (lane == 31) sh.total = incl;
                 }
                 __syncthreads();
-                if (digit == 0 && !from_recent && sh.total < drop) {
+                if (part == 0 && shift == 24 && !from_recent && sh.total < drop) {
                     from_recent = true;
                     rank = drop - sh.total;
                     fill();
                     __syncthreads();
                     continue;
                 }
-                thr[digit >> 2] |= sh.prefix;
+                thr[part] |= sh.prefix;
+                open = (1u << shift) - 1u;
                 rank = sh.rank;
-                ++digit;
-                if (sh.equal <= kShort) break;               // twelve digits tell all slots apart
-                __syncthreads();
+                const int equal = sh.equal;
+                if (equal <= kShort || (part == 2 && open == 0u)) break;     // all bits of the slot tell all of them apart
+                // Eight bits that told little (a quarter or more still agrees: equal scores, most of all) say that the next eight
+                // may not either: then a look at which bits differ at all, one pass without atomics, finds the ones that do.
+                bool look = 4 * equal >= total;
+                total = equal;
+                shift = shift > 8 ? shift - 8 : 0;
+                for (;;) {
+                    if (open == 0u && part < 2) { ++part; open = 0xffffffffu; look = true; }
+                    if (!look) break;
+                    unsigned any = 0u, all = 0xffffffffu;
+                    for (int j = 4 * tid; j < n; j += 4 * kSelThreads) {
+                        unsigned k[4];
+                        keys4(j, k);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (agrees(k[e], j + e)) { const unsigned v = value(k[e], j + e); any |= v; all &= v; }
+                    }
+                    any = __reduce_or_sync(0xffffffffu, any);
+                    all = __reduce_and_sync(0xffffffffu, all);
+                    if (lane == 0) { atomicOr(&sh.all_or, any); atomicAnd(&sh.all_and, all); }
+                    __syncthreads();
+                    any = sh.all_or;
+                    const unsigned differ = (any ^ sh.all_and) & open;
+                    const int top = 32 - __clz((int)differ); // bits from here on are the same
+                    open = top == 32 ? 0xffffffffu : (1u << top) - 1u;
+                    thr[part] = any & ~open;
+                    shift = top > 8 ? top - 8 : 0;
+                    look = false;
+                    __syncthreads();
+                    if (open == 0u && tid == 0) { sh.all_or = 0u; sh.all_and = 0xffffffffu; }
+                    if (open == 0u) __syncthreads();
+                }
             }
             // the slots that agree so far, ranked by (score, position, slot)
-            const int m = sh.equal;
-            const unsigned above = prefix_mask(digit);
+            const int m = min(sh.equal, kShort);
             for (int j = 4 * tid; j < n; j += 4 * kSelThreads) {
                 unsigned k[4];
                 keys4(j, k);
-    #pragma unroll
+#pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (k[e] == kNoKey || ((k[e] ^ thr[0]) & above) != 0u || (digit > 4 && !agrees_beyond_score(digit, j + e))) continue;
+                    if (!agrees(k[e], j + e)) continue;
                     const int x = atomicAdd(&sh.count, 1);
                     if (A2SF_IN_RANGE(x, kShort, kDbgPagedEvict) && x < kShort) { sh.list_key[x] = k[e]; sh.list_pos[x] = pos_at(j + e); sh.list_slot[x] = j + e; }
                 }
@@ -457,29 +490,39 @@ cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int re
         const long long want = (16ll * device_sm_count() + (long long)units - 1) / (long long)units;
         if (blocks > want) blocks = want;
     }
+    // New lengths that do not lie where the old ones are read need no second kernel for their own sake; and so many moves
+    // at most are no more than it costs (1 us: 3 heads from 304 slots to 40, 12.1 us with it, 10.9 without).
+    const int bound = dst_table ? (budget < cap ? budget : cap) : (cap - budget < budget ? cap - budget : budget);
+    auto apart = [&](const int32_t *out, const int32_t *in) { return !in || out + pv.B <= in || in + pv.B <= out; };
+    a.direct = (blocks == 0 || bound <= kDirect) && apart(past_out, pv.past) && apart(past_out, pv.start) && apart(past_out, pv.lens) &&
+               apart(start_out, pv.past) && apart(start_out, pv.start) && apart(start_out, pv.lens);
+    if (a.direct) blocks = 0;
     a.blocks = (int)blocks;
     const unsigned grid = blocks ? (unsigned)(units * blocks) : 1u;
-    auto run = [&](auto select, auto move) -> cudaError_t {
-        cudaError_t e = launch_chained(select, (unsigned)units, kSelThreads, smem, s, a, cached);
+    auto run = [&](auto select, int threads, auto move) -> cudaError_t {
+        cudaError_t e = launch_chained(select, (unsigned)units, threads, smem, s, a, cached);
         if (e != cudaSuccess) return e;
         count_launch();
+        if (a.direct) return cudaSuccess;
         e = launch_chained(move, grid, kMoveThreads, 0, s, a);
         if (e == cudaSuccess) count_launch();
         return e;
     };
     // static shared memory counts towards the 48 KB that need no permission: it is asked for the most, whatever this call takes
     constexpr size_t most = (size_t)kCached * 8;
-    cudaError_t e;
+    // Twice the threads where every head has an SM to itself (21 heads, 17 of 3,237 slots leave: 28 us with 256 threads, 21 with
+    // 512, 20 with 1024, which lose elsewhere; 69 heads, 3 of 4,330: 14.9 and 15.1).
+    const bool wide = units <= (size_t)device_sm_count();
+    auto pick = [&](auto rows) -> cudaError_t {
+        constexpr int RB = decltype(rows)::value;
+        cudaError_t e = wide ? allow_dynamic_smem<paged_select_kernel<RB, kWide>>(most) : allow_dynamic_smem<paged_select_kernel<RB, 256>>(most);
+        if (e != cudaSuccess) return e;
+        return wide ? run(paged_select_kernel<RB, kWide>, kWide, paged_move_kernel<RB>) : run(paged_select_kernel<RB, 256>, 256, paged_move_kernel<RB>);
+    };
     switch (row_bytes) {
-    case 128:
-        if ((e = allow_dynamic_smem<paged_select_kernel<128>>(most)) != cudaSuccess) return e;
-        return run(paged_select_kernel<128>, paged_move_kernel<128>);
-    case 256:
-        if ((e = allow_dynamic_smem<paged_select_kernel<256>>(most)) != cudaSuccess) return e;
-        return run(paged_select_kernel<256>, paged_move_kernel<256>);
-    default:
-        if ((e = allow_dynamic_smem<paged_select_kernel<512>>(most)) != cudaSuccess) return e;
-        return run(paged_select_kernel<512>, paged_move_kernel<512>);
+    case 128: return pick(std::integral_constant<int, 128>{});
+    case 256: return pick(std::integral_constant<int, 256>{});
+    default: return pick(std::integral_constant<int, 512>{});
     }
 }
 
