@@ -736,3 +736,72 @@ assert a2sf.a2sf_last_device_status() == 0
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300,
                        cwd=Path(__file__).resolve().parent.parent)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("B,H,past,c,budget,fresh", [
+    (3, 2, [90, 300, 17], 3, 250, True), (3, 2, [90, 300, 17], 3, 280, False), (5, 70, [40, 3, 0, 25, 60], 3, 30, True),
+    (2, 2, [700, 100], 1, 600, True), (2, 1, [900, 850], 20, 400, False)])
+def test_new_lengths_apart_from_the_old_ones(a2sf, B, H, past, c, budget, fresh):
+    """past_out and start_out in arrays of their own, overlapping past by all but one entry, or past and start themselves."""
+    n, ps, d = [p + c for p in past], 16, 64
+    spare = -(-budget // ps)
+    g = torch.Generator().manual_seed(16)
+    results = []
+    for how in ("same", "apart", "shifted"):
+        cache = pu.make_cache(a2sf, B, H, 1, d, BF, ps, n, spare * ps, seed=4)
+        cache.scores.copy_(torch.rand(cache.scores.shape, generator=torch.Generator().manual_seed(5)).mul(6).floor())
+        lengths, start = torch.zeros(2 * B + 2, dtype=torch.int32), torch.tensor([p + 9 for p in past], dtype=torch.int32)
+        lengths[:B] = torch.tensor(past)
+        lengths, start = lengths.cuda(), start.cuda()
+        pages = cache.k_pages.shape[0]
+        pool = {x: torch.cat([getattr(cache, x), torch.zeros((B * spare,) + getattr(cache, x).shape[1:], device="cuda", dtype=getattr(cache, x).dtype)])
+                for x in ("k_pages", "v_pages", "scores", "positions")}
+        cache = a2sf.PagedCache(B, H, d, BF, ps, pages + B * spare, cache.max_pages, page_table=cache.page_table, past=lengths[:B], start=start, **pool)
+        dst = (pages + torch.arange(B * spare, dtype=torch.int32)).view(B, spare).cuda() if fresh else None
+        at = {"same": 0, "apart": B + 1, "shifted": 1}[how]
+        past_out, start_out = lengths[at:at + B], start if how == "same" else torch.zeros_like(start)
+        cache.a2sf_paged_evict(budget, 10, c, dst_table=dst, past_out=past_out, start_out=start_out)
+        assert past_out.tolist() == [min(x, budget) for x in n] and start_out.tolist() == [p + 9 + c for p in past], how
+        if how == "apart":
+            assert lengths[:B].tolist() == past and start.tolist() == [p + 9 for p in past]
+        results.append([getattr(cache, x).double().nan_to_num(7.0) for x in pool])
+    assert all(torch.equal(x, y) for r in results[1:] for x, y in zip(results[0], r))
+
+
+@pytest.mark.parametrize("kind", ["last bits", "equal scores", "equal pairs", "wide positions"])
+@pytest.mark.parametrize("heads,n,drop", [(1, 500, 100), (200, 300, 60)])
+def test_evict_where_most_bits_are_shared(a2sf, kind, heads, n, drop):
+    """Scores that differ in their last bits only, scores or (score, position) pairs that are all equal, positions of all sizes."""
+    ps = 16
+    cache = pu.make_cache(a2sf, 1, heads, 1, 64, BF, ps, [n], 0, seed=3)
+    g = torch.Generator().manual_seed(18)
+    table, j = cache.page_table.cpu()[0].long(), torch.arange(n)
+    bits = torch.full((heads, n), 0x3f800000, dtype=torch.int32)
+    if kind == "last bits":
+        bits += torch.randint(0, 200, (heads, n), generator=g).to(torch.int32)
+    score = bits.view(torch.float32)
+    pos = torch.full((heads, n), 77, dtype=torch.int32)
+    if kind == "wide positions":
+        pos = torch.randint(-2 ** 31, 2 ** 31 - 1, (heads, n), generator=g).to(torch.int32)
+    elif kind != "equal pairs":
+        pos = torch.stack([torch.randperm(n, generator=g) for _ in range(heads)]).to(torch.int32)
+    cpu = {x: getattr(cache, x).cpu() for x in ("scores", "positions", "k_pages")}
+    cpu["scores"][table[j // ps], :, j % ps] = score.T
+    cpu["positions"][table[j // ps], :, j % ps] = pos.T
+    cache.scores.copy_(cpu["scores"])
+    cache.positions.copy_(cpu["positions"])
+    cache.past.fill_(n - 1)
+    cache.start.fill_(2 ** 31 - 2)                              # nothing is recent
+    M = n - drop
+    cache.a2sf_paged_evict(M, 0)
+    got = {x: getattr(cache, x).cpu()[table[j[:M] // ps], :, j[:M] % ps] for x in cpu}
+    for h in range(heads):
+        order = sorted(range(n), key=lambda s: (float(score[h, s]), int(pos[h, s]), s))
+        stay = set(order[drop:])
+        holes, ups = [s for s in range(M) if s not in stay], [s for s in range(M, n) if s in stay]
+        src = list(range(M))
+        for hole, up in zip(holes, ups):
+            src[hole] = up
+        src = torch.tensor(src)
+        for x in cpu:
+            assert torch.equal(got[x][:, h], cpu[x][table[src // ps], h, src % ps]), (kind, h, x)
