@@ -15,6 +15,8 @@
 //           32-bit storage: the same on the CUDA cores, a lane working on a quarter of a key.  Logits go to the workspace (4 bytes per slot and
 //           row next to 4 d or 8 d bytes of K and V) so that scores need no second pass over K.
 //   finish  joins the partial outputs; S <- alpha^len S + sum_r alpha^age exp2(x_r - lse_r).
+//   whole   instead of both where no sequence can have more than a few tiles: a CTA takes whole units, keeps
+//           logits and partial results in shared memory and ends each unit itself.
 // P is rounded to the storage type for P V (half a step, as the output itself); the row sum and the
 // scores use the unrounded values.
 #include <type_traits>
@@ -36,6 +38,7 @@ template <typename T, int D> constexpr int tile_slots = D * sizeof(T) == 128 ? 1
 // (d = 128), so twice as many warps share a tile there to hide each other's latencies.
 template <typename T> constexpr int warps_of = sizeof(T) == 4 ? 8 : 4;
 constexpr int kFinishThreads = 256;
+constexpr int kSms = 148;
 // How far a logit may lie above its column's reference (log2 units): 2^14 is a probability that fp16 holds, and
 // sums of it and of values up to 2^113 / slots stay finite.
 constexpr float kSlack = 14.f;
@@ -522,6 +525,185 @@ drained:
     }
 }
 
+// ---- short caches: whole units ---------------------------------------------------------------------
+// Sequences of at most so many tiles: the second kernel of the split costs more (us, split and whole: 32 heads x 205 slots,
+// d 128, 8.6 and 7.3; 12 x 4, d 64, 7.8 and 4.5) than a share of fewer tiles saves (8 heads x 496: 8.2 and 11.3).  Where
+// there are units for every SM, twice as many (256 heads x 496: 19.1 and 15.7; 400 x 1001, again twice: 40 and 51).
+constexpr int kWholeTiles = 4, kWholeTilesMany = 8;
+
+// Shared memory behind the ring and the scratch: (maximum, sum) and output of every warp, logits of all slots.
+__host__ __device__ constexpr size_t whole_bytes(int warps, int D, int NP, int slots) { return (size_t)NP * (warps * (8 + D * 4) + slots * 4); }
+
+struct WholeShared {
+    uint64_t full[3], empty[3];
+    int abort_flag;
+    float row_m[kFewRows], row_inv[kFewRows], row_c[kFewRows];
+};
+
+template <typename T, int D, int NC>
+__global__ void __launch_bounds__(32 * (warps_of<T> + 1))
+paged_few_whole_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                       const __grid_constant__ AttendArgs a, int NP, int slots)
+{
+    using R = Ring<T, D>;
+    using Body = typename BodyOf<T, D, NC>::type;
+    constexpr int kTile = R::kTile, kWarps = warps_of<T>, kSlots = kTile / kWarps, kConsumers = 32 * kWarps;
+    constexpr int kPer = kWholeTiles * kTile / kConsumers;          // slots of a thread whose old scores are asked for early
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ WholeShared sh;
+    const PagedView &pv = a.pv;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, units = pv.B * pv.H;
+    volatile int *abort_flag = &sh.abort_flag;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < R::kStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], kWarps); }
+        sh.abort_flag = 0;
+        fence_mbar_init();
+        prefetch_tmap(&map_k);
+        prefetch_tmap(&map_v);
+    }
+    dependency_wait();
+    __syncthreads();
+    dependents_may_start();
+
+    if (warp == 0) {
+        const int box = min(pv.ps, kTile), boxes = kTile / box;
+        int it = 0;
+        for (int u = blockIdx.x; u < units; u += gridDim.x) {
+            const int b = u / pv.H, h = u - b * pv.H;
+            const SeqState st = seq_state(pv, b);
+            const int used = st.len > 0 ? st.past + st.len : 0;
+            const int32_t *table = pv.table + (size_t)b * pv.max_pages;
+            for (int t = 0; t * kTile < used; ++t, ++it) {
+                const int s = it % R::kStages;
+                const int slot = t * kTile + lane * box;
+                const int nbox = min(boxes, (used - t * kTile + box - 1) / box);
+                int row = 0;
+                if (lane < nbox) row = (int)pool_row(pv, page_for_read(pv, table, slot), h, slot);
+                int ok = 1;
+                if (lane == 0) {
+                    if (it >= R::kStages) ok = mbar_wait(&sh.empty[s], ((it / R::kStages) & 1) ^ 1, abort_flag) ? 1 : 0;
+                    if (ok) mbar_arrive_expect_tx(&sh.full[s], (uint32_t)(nbox * box * R::kRowBytes * 2));
+                }
+                if (!__shfl_sync(0xffffffffu, ok, 0)) goto drained;
+                if (lane < nbox) {
+                    uint8_t *dst = ring + (size_t)s * 2 * R::kTileBytes + lane * box * 128;
+#pragma unroll
+                    for (int ch = 0; ch < R::kChunks; ++ch) {
+                        tma_load_2d(dst + ch * (kTile * 128), &map_k, &sh.full[s], ch * (128 / (int)sizeof(T)), row);
+                        tma_load_2d(dst + R::kTileBytes + ch * (kTile * 128), &map_v, &sh.full[s], ch * (128 / (int)sizeof(T)), row);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+drained:
+        if (lane == 0 && *abort_flag) {
+            int dummy = 0;                                   // copies still in flight get a bounded chance to land
+            for (int k = max(0, it - R::kStages); k < it; ++k)
+                mbar_wait(&sh.full[k % R::kStages], (k / R::kStages) & 1, &dummy);
+            *pv.status = A2SF_ERR_TIMEOUT;
+        }
+        return;
+    }
+    const int cw = warp - 1, ct = threadIdx.x - 32;
+    float *scratch = reinterpret_cast<float *>(ring + (size_t)R::kStages * 2 * R::kTileBytes);
+    float2 *ml = reinterpret_cast<float2 *>(reinterpret_cast<uint8_t *>(scratch) + BodyOf<T, D, NC>::kScratch);
+    float *o = reinterpret_cast<float *>(ml + kWarps * NP);
+    float *logits = a.scores ? o + (size_t)kWarps * NP * D : nullptr;
+    Body body;
+    int it = 0;
+    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+        Where x = {};
+        x.b = u / pv.H;
+        x.h = u - x.b * pv.H;
+        const SeqState st = seq_state(pv, x.b);
+        if (st.len <= 0) continue;
+        const int used = st.past + st.len, rows = st.len * pv.G;
+        const int32_t *table = pv.table + (size_t)x.b * pv.max_pages;
+        // old scores are asked for here and used at the unit's end
+        int row[kPer];
+        float old[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const int j = ct + e * kConsumers;
+            row[e] = a.scores && j < used ? page_for_write(pv, table, j) : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (row[e] >= 0) {
+                row[e] = (int)pool_row(pv, row[e], x.h, ct + e * kConsumers);
+                old[e] = pv.scores[row[e]];
+            }
+        body.begin(a, x, st, scratch);
+        for (int t = 0; t * kTile < used; ++t, ++it) {
+            const int s = it % R::kStages;
+            if (!*abort_flag && !mbar_wait(&sh.full[s], (it / R::kStages) & 1, abort_flag)) *pv.status = A2SF_ERR_TIMEOUT;
+            const int j0 = t * kTile + cw * kSlots;
+            uint8_t *K = ring + (size_t)s * 2 * R::kTileBytes;
+            if (j0 < used && A2SF_IN_RANGE(j0 + kSlots - 1, slots, kDbgPagedFew)) body.tile(a, K, K + R::kTileBytes, cw * kSlots, j0, used, logits, NP, scratch);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.empty[s]);
+        }
+        body.end(ml + cw * NP, o + (size_t)cw * NP * D, NP);
+        named_barrier(1, kConsumers);
+        if (ct < NP) {
+            float mx = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[w * NP + ct].x);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float2 y = ml[w * NP + ct];
+                l += y.y > 0.f ? ex2(y.x - mx) * y.y : 0.f;
+            }
+            const float z = mx + log2f(l);
+            const int i = ct / pv.G, g = ct - i * pv.G;
+            sh.row_m[ct] = mx;
+            sh.row_inv[ct] = 1.f / l;
+            sh.row_c[ct] = ct < rows ? z + age_exponent(st.len - 1 - i, a.nl2a) : INFINITY;
+            if (ct < rows && a.lse) a.lse[((size_t)u * pv.G + g) * pv.c + i] = z * 0.6931471805599453f;
+        }
+        named_barrier(1, kConsumers);
+        const float decay = exp2f(-age_exponent(st.len, a.nl2a));
+        auto gain = [&](int j) {                             // rows that do not see the slot, or are none, have -inf there
+            const float *z = logits + j * NP;
+            float sum = 0.f;
+            for (int r = 0; r < NP; ++r) sum += ex2(z[r] - sh.row_c[r]);
+            return sum;
+        };
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (row[e] >= 0) pv.scores[row[e]] = fmaf(old[e], decay, gain(ct + e * kConsumers));
+        if (a.scores)
+            for (int j = ct + kPer * kConsumers; j < used; j += kConsumers) {
+                const int page = page_for_write(pv, table, j);
+                if (page < 0) continue;
+                float *dst = pv.scores + pool_row(pv, page, x.h, j);
+                *dst = fmaf(*dst, decay, gain(j));
+            }
+        for (int e = ct; e < rows * (D / 4); e += kConsumers) {
+            const int r = e / (D / 4), d4 = e - r * (D / 4);
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = ex2(ml[w * NP + r].x - sh.row_m[r]);
+                if (!(f > 0.f)) continue;                    // a warp that saw nothing wrote no output
+                const float4 v = reinterpret_cast<const float4 *>(o + (size_t)(w * NP + r) * D)[d4];
+                sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y);
+                sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+            }
+            const int i = r / pv.G, g = r - i * pv.G;
+            const float inv = sh.row_inv[r];
+            T *dst = static_cast<T *>(a.out) + x.b * a.so.b + (int64_t)(x.h * pv.G + g) * a.so.h + (int64_t)i * a.so.t + d4 * 4;
+            dst[0] = Elem<T>::from_float(sum.x * inv);
+            dst[1] = Elem<T>::from_float(sum.y * inv);
+            dst[2] = Elem<T>::from_float(sum.z * inv);
+            dst[3] = Elem<T>::from_float(sum.w * inv);
+        }
+        named_barrier(1, kConsumers);                        // all has been read
+    }
+}
+
 // The finish kernel: `blocks` blocks per unit.  Block y joins the output rows y, y + blocks, .. and brings the
 // scores of slots y * chunk .. up to date.  All of it is latency: dependent loads around a few bytes.  So the page
 // numbers and old scores of the first slots are read while the main kernel still drains, the logits and the
@@ -706,6 +888,16 @@ FewWs carve(int dtype, const PagedView &pv, void *ws, size_t *bytes)
     return w;
 }
 
+// Shared memory of the whole-unit kernel, or 0 where it does not serve: longer caches, or more rows than fit.
+template <typename T, int D, int NC> size_t whole_smem(const PagedView &pv)
+{
+    using R = Ring<T, D>;
+    const int slots = ((pv.max_pages << pv.ps_shift) + R::kTile - 1) / R::kTile * R::kTile;
+    const size_t smem = R::kBytes + BodyOf<T, D, NC>::kScratch + whole_bytes(warps_of<T>, D, rows_padded(pv.c * pv.G), slots);
+    const int most = pv.B * pv.H >= kSms ? kWholeTilesMany : kWholeTiles;
+    return slots <= most * R::kTile && smem + sizeof(WholeShared) <= 227 * 1024 ? smem : 0;
+}
+
 template <typename T, int D, int NC>
 cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
 {
@@ -716,8 +908,16 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     CUtensorMap mk, mv;
     const int box = a.pv.ps < R::kTile ? a.pv.ps : R::kTile;
     if (!make_pool_map(&mk, dtype, a.pv.k, a.pv, box) || !make_pool_map(&mv, dtype, a.pv.v, a.pv, box)) return cudaErrorInvalidValue;
-    const FewWs ws = carve(dtype, a.pv, a.ws, nullptr);
     const int NP = rows_padded(a.pv.c * a.pv.G);
+    if (const size_t whole = whole_smem<T, D, NC>(a.pv)) {
+        if ((e = allow_dynamic_smem<paged_few_whole_kernel<T, D, NC>>(whole)) != cudaSuccess) return e;
+        const long long resident = device_sm_count() * (2 * (whole + sizeof(WholeShared) + 1024) <= 228 * 1024 ? 2 : 1), units = (long long)a.pv.B * a.pv.H;
+        const int slots = ((a.pv.max_pages << a.pv.ps_shift) + R::kTile - 1) / R::kTile * R::kTile;
+        e = launch_chained(paged_few_whole_kernel<T, D, NC>, (unsigned)(units < resident ? units : resident), 32 * (warps_of<T> + 1), whole, s, mk, mv, a, NP, slots);
+        if (e == cudaSuccess) count_launch();
+        return e;
+    }
+    const FewWs ws = carve(dtype, a.pv, a.ws, nullptr);
     const int ctas = device_sm_count() * (2 * (smem + sizeof(FewShared) + 1024) <= 228 * 1024 ? 2 : 1);   // what is resident
     if (ctas < 1 || ctas > 512) return cudaErrorInvalidValue;
     if ((e = launch_chained(paged_few_kernel<T, D, NC>, ctas, 32 * (warps_of<T> + 1), smem, s, mk, mv, a, ws, NP)) != cudaSuccess) return e;
