@@ -93,12 +93,12 @@ EncodeTiledFn encode_fn()
 }
 
 // Which attention: few rows are bound by the cache's bytes whatever the type; more rows of 16-bit storage
-// by the matrix products (tensor cores), of 32-bit storage by fp32 multiply-adds.
-enum Path { kFew, kTc, kSimt };
+// by the matrix products (tcgen05), of 32-bit storage by products of split operands.
+enum Path { kFew, kTc, kFp32 };
 Path path_of(const a2sf_paged *p, int c)
 {
     if ((int64_t)c * p->group <= kFewRows) return kFew;
-    return p->dtype == A2SF_F32 ? kSimt : kTc;
+    return p->dtype == A2SF_F32 ? kFp32 : kTc;
 }
 
 }  // namespace
@@ -257,7 +257,7 @@ size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c)
     if (check_paged(cache, c) != A2SF_OK) return 0;
     const PagedView pv = make_view(cache, c, nullptr);
     const Path path = path_of(cache, c);
-    return align_up(path == kFew ? attend_few_ws_bytes(cache->dtype, pv) : path == kTc ? attend_tc_ws_bytes(pv) : attend_simt_ws_bytes(pv));
+    return align_up(path == kFew ? attend_few_ws_bytes(cache->dtype, pv) : path == kTc ? attend_tc_ws_bytes(pv) : attend_fp32_ws_bytes(pv));
 }
 
 int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha, const void *q,
@@ -289,7 +289,7 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const Path path = path_of(cache, c);
     const cudaError_t e = path == kFew ? launch_attend_few(cache->dtype, a, s)
-                          : path == kTc ? launch_attend_tc(cache->dtype, a, s) : launch_attend_simt(a, s);
+                          : path == kTc ? launch_attend_tc(cache->dtype, a, s) : launch_attend_fp32(a, s);
     return e == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
 }
 
