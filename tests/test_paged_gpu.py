@@ -805,3 +805,12 @@ def test_evict_where_most_bits_are_shared(a2sf, kind, heads, n, drop):
         src = torch.tensor(src)
         for x in cpu:
             assert torch.equal(got[x][:, h], cpu[x][table[src // ps], h, src % ps]), (kind, h, x)
+
+
+@pytest.mark.parametrize("case", [
+    (20, 3, 1, 64, FP, 16, [600 - 7 * b for b in range(20)], 200, [200 - 9 * b for b in range(20)], 0.9, "bhnd", 0.0),
+    (20, 2, 3, 128, FP, 64, [3 * b for b in range(20)], 173, None, 1.0, "bnhd", 0.0),
+    (1, 2, 1, 128, FP, 32, [5000], 33, [31], 0.5, "bhnd", 0.0),
+    (2, 1, 4, 64, FP, 128, [2999, 0], 50, [50, 17], 0.99, "bnhd", 0.0)], ids=["many-pieces", "many", "few-long", "few-group"])
+def test_attend_in_32_bits_in_large_tiles_and_in_pieces(a2sf, case):
+    check_attend(a2sf, case, seed=21)
