@@ -92,13 +92,19 @@ EncodeTiledFn encode_fn()
     return fn;
 }
 
-// Which attention: few rows are bound by the cache's bytes whatever the type; more rows of 16-bit storage
-// by the matrix products (tcgen05), of 32-bit storage by products of split operands.
-enum Path { kFew, kTc, kFp32 };
+// Which attention: few rows are bound by the cache's bytes whatever the type; more rows of 32-bit storage by products of
+// split operands, of 16-bit storage by tcgen05 -- whose plan, 128-row tiles and one CTA per SM cost more than a small call
+// takes.  Small goes by the multiply-adds of Q K^T at the cache's capacity (us, tcgen05 and mma.sync): 12 heads, 244 tokens,
+// 5e7: 14.8 and 10.8; 36 heads, 302 tokens, 2e8: 26.7 and 18.9; 8 heads, 928 tokens, 5e8: 31.8 and 31.2; 32 heads, 100 behind
+// 2,000, 9e8: 42 and 67.  One tile of 64 rows: 640 heads, 64 behind 100, 1e9: 73 and 51; 64 x 64 behind 4,000, 2e9: 85 and 86.
+enum Path { kFew, kTc, kMma };
 Path path_of(const a2sf_paged *p, int c)
 {
-    if ((int64_t)c * p->group <= kFewRows) return kFew;
-    return p->dtype == A2SF_F32 ? kFp32 : kTc;
+    const int64_t rows = (int64_t)c * p->group;
+    if (rows <= kFewRows) return kFew;
+    if (p->dtype == A2SF_F32) return kMma;
+    const double work = (double)p->B * p->H * rows * p->max_pages * p->page_size * p->d;
+    return work < (rows <= 64 ? 1.2e9 : 3e8) ? kMma : kTc;
 }
 
 }  // namespace
@@ -257,7 +263,7 @@ size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c)
     if (check_paged(cache, c) != A2SF_OK) return 0;
     const PagedView pv = make_view(cache, c, nullptr);
     const Path path = path_of(cache, c);
-    return align_up(path == kFew ? attend_few_ws_bytes(cache->dtype, pv) : path == kTc ? attend_tc_ws_bytes(pv) : attend_fp32_ws_bytes(pv));
+    return align_up(path == kFew ? attend_few_ws_bytes(cache->dtype, pv) : path == kTc ? attend_tc_ws_bytes(pv) : attend_mma_ws_bytes(cache->dtype, pv));
 }
 
 int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha, const void *q,
@@ -289,7 +295,7 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const Path path = path_of(cache, c);
     const cudaError_t e = path == kFew ? launch_attend_few(cache->dtype, a, s)
-                          : path == kTc ? launch_attend_tc(cache->dtype, a, s) : launch_attend_fp32(a, s);
+                          : path == kTc ? launch_attend_tc(cache->dtype, a, s) : launch_attend_mma(cache->dtype, a, s);
     return e == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
 }
 

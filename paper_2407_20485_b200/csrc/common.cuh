@@ -116,7 +116,7 @@ enum DebugKernelId {
     kDbgSelect = 1, kDbgCacheLoad, kDbgDecodeStream, kDbgDecodeSplit, kDbgGroupMma, kDbgGroupSimt,
     kDbgGroupSum, kDbgPrefillSimt1, kDbgPrefillSimt2, kDbgAttnTc, kDbgScoreTc, kDbgVToHalf,
     kDbgIdealStats, kDbgSimilarityRow,
-    kDbgPagedRow, kDbgPagedFew, kDbgPagedTc, kDbgPagedFp32, kDbgPagedEvict, kDbgRotary
+    kDbgPagedRow, kDbgPagedFew, kDbgPagedTc, kDbgPagedMma, kDbgPagedEvict, kDbgRotary
 };
 #ifdef A2SF_DEBUG
 // one record per translation unit (no relocatable device code): {violations, kernel << 32 | line,

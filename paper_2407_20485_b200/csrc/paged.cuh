@@ -199,8 +199,9 @@ bool make_query_map(CUtensorMap *map, int dtype, const void *q, const PagedView 
 size_t attend_tc_ws_bytes(const PagedView &pv);
 cudaError_t launch_attend_tc(int dtype, const AttendArgs &a, cudaStream_t s);
 
-size_t attend_fp32_ws_bytes(const PagedView &pv);
-cudaError_t launch_attend_fp32(const AttendArgs &a, cudaStream_t s);     // 32-bit storage
+// 32-bit storage, and small calls of 16-bit storage
+size_t attend_mma_ws_bytes(int dtype, const PagedView &pv);
+cudaError_t launch_attend_mma(int dtype, const AttendArgs &a, cudaStream_t s);
 
 cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int recent, const int32_t *dst_table,
                          int dst_max_pages, int32_t *past_out, int32_t *start_out, void *ws, cudaStream_t s);
