@@ -190,10 +190,10 @@ ATT = [
 ]
 
 
-def check_attend(a2sf, case, seed=5, garbage=float("nan"), gain=1.0):
+def check_attend(a2sf, case, seed=5, garbage=float("nan"), gain=1.0, room=0):
     B, H, G, d, dtype, ps, past, c, lens, alpha, layout, scale = case
     lens = [c] * B if lens is None else lens
-    cache = pu.make_cache(a2sf, B, H, G, d, dtype, ps, past, c, seed=seed, scale=scale, garbage=garbage)
+    cache = pu.make_cache(a2sf, B, H, G, d, dtype, ps, past, max(c, room), seed=seed, scale=scale, garbage=garbage)
     g = torch.Generator().manual_seed(seed + 1)
 
     def tensor(h, k=1.0):
@@ -814,3 +814,107 @@ def test_evict_where_most_bits_are_shared(a2sf, kind, heads, n, drop):
     (2, 1, 4, 64, FP, 128, [2999, 0], 50, [50, 17], 0.99, "bnhd", 0.0)], ids=["many-pieces", "many", "few-long", "few-group"])
 def test_attend_in_32_bits_in_large_tiles_and_in_pieces(a2sf, case):
     check_attend(a2sf, case, seed=21)
+
+
+# ---- many rows in 16-bit storage on tcgen05: calls that are large by the capacity of their page tables ------------
+
+def room_for_large(case):
+    """Slots behind `past` that make the call large: 3e8 multiply-adds of Q K^T at capacity, 1.2e9 for up to 64 rows."""
+    B, H, G, d, _, _, _, c = case[:8]
+    return int((1.3e9 if c * G <= 64 else 3.3e8) / (B * H * G * c * d))
+
+
+LARGE = [c for c in ATT if c[4] != FP and c[2] * c[7] > 16] + [
+    (6, 4, 1, 128, BF, 64, [500, 0, 63, 64, 65, 1300], 40, [40, 40, 0, 1, 39, 40], 0.9, "bhnd", 0.0),
+    (2, 2, 4, 128, HF, 32, [0, 600], 200, [200, 150], 1.0, "bnhd", 0.0),           # a capacity of 800 slots: no plan
+    (3, 4, 2, 64, BF, 16, [0, 300, 128], 290, [290, 0, 129], 0.5, "bhnd", 0.0)]
+
+
+@pytest.mark.parametrize("case", LARGE, ids=lambda c: "-".join(str(x).replace("torch.", "").replace(" ", "") for x in c))
+def test_attend_of_large_calls(a2sf, case):
+    if case[7] * case[2] == 17:
+        case = (3, 5) + case[2:6] + ([0, 70, 129],) + case[7:]
+    check_attend(a2sf, case, room=room_for_large(case), seed=31)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_attend_random_large_calls(a2sf, seed):
+    r = random.Random(1000 + seed)
+    while True:
+        case = random_attend(r)
+        if case[4] != FP and case[2] * case[7] > 64:
+            break
+    check_attend(a2sf, case, seed=seed + 300, room=room_for_large(case))
+
+
+@pytest.mark.parametrize("dtype,G,c,past,gain,garbage", [
+    (BF, 2, 150, 200, 12.0, math.nan), (HF, 2, 150, 200, 12.0, math.nan), (BF, 4, 40, 33, 1.0, math.inf), (HF, 2, 150, 0, 1.0, math.inf)])
+def test_large_logits_and_infinities_in_large_calls(a2sf, dtype, G, c, past, gain, garbage):
+    case = (2, 2, G, 128, dtype, 32, [past, 1], c, [c, c - 3], 0.9, "bhnd", 0.0)
+    check_attend(a2sf, case, seed=9, gain=gain, garbage=garbage, room=room_for_large(case))
+
+
+@pytest.mark.parametrize("bad", [-1, 2 ** 31 - 1, "pages", "past", "length"])
+def test_bad_pages_and_lengths_in_large_calls(a2sf, bad):
+    c = 150
+    cache = pu.make_cache(a2sf, 2, 2, 1, 128, HF, 16, [40, 30], 8000, seed=4, garbage=0.0)
+    lens = torch.full((2,), c, dtype=torch.int32, device="cuda")
+    if bad == "past":
+        cache.past[1] = cache.max_pages * 16 + 5
+    elif bad == "length":
+        lens[1] = -4
+    else:
+        cache.page_table[1, :] = cache.num_pages if bad == "pages" else bad
+    x = torch.randn((2, 2, c, 128), device="cuda").to(HF)
+    cache.a2sf_paged_attend(x, 0.5, lens=lens)
+    assert a2sf.a2sf_last_device_status() == a2sf.A2SF_ERR_INVALID_ARG
+    assert a2sf.a2sf_last_device_status() == a2sf.A2SF_OK
+
+
+def test_a_large_call_captured_and_replayed(a2sf):
+    B, H, G, d, c = 2, 2, 2, 128, 200
+    g = torch.Generator().manual_seed(33)
+    ins = [[torch.randn((B, h, c, d), generator=g).to(BF).cuda() for h in (H * G, H, H)] for _ in range(3)]
+    a, b = (pu.make_cache(a2sf, B, H, G, d, BF, 32, [300, 5], 8000, seed=6) for _ in range(2))
+    q, k, v = (x.clone() for x in ins[0])
+    out, lse = torch.empty_like(q), torch.empty((B, H * G, c), device="cuda")
+
+    def step(cache, q, k, v, out, lse):
+        cache.a2sf_paged_append(k, v)
+        cache.a2sf_paged_attend(q, 0.9, out=out, lse=lse)
+        cache.a2sf_paged_evict(1000, 8, c)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a, q, k, v, out, lse)
+    for x in ins:
+        for dst, src in zip((q, k, v), x):
+            dst.copy_(src)
+        graph.replay()
+        o2, z2 = torch.empty_like(q), torch.empty_like(lse)
+        step(b, *x, o2, z2)
+        torch.cuda.synchronize()
+        assert torch.equal(out, o2) and torch.equal(lse, z2)
+        for name in ("k_pages", "scores", "positions", "past", "start"):
+            assert torch.equal(getattr(a, name).double().nan_to_num(7.0), getattr(b, name).double().nan_to_num(7.0)), name
+
+
+def test_a_large_call_far_inside_a_large_pool(a2sf):
+    """Pages beyond 2^31 elements, read through a table of 40 entries, give what the same pages give in a small pool."""
+    H, d, ps, past, c = 8, 128, 128, 300, 130
+    pages = (2 ** 31) // (H * ps * d) + 40
+    far = torch.zeros((1, 40), dtype=torch.int32)
+    near = far.clone()
+    far[0, :4], near[0, :4] = pages - 1 - torch.arange(4), torch.tensor([2, 0, 3, 1])
+    g = torch.Generator().manual_seed(5)
+    k, v, q = (torch.randn((1, H, past + c, d), generator=g).to(HF).cuda() for _ in range(3))
+    results = []
+    for n_pages, table in ((pages, far), (4, near)):
+        cache = a2sf.PagedCache(1, H, d, HF, ps, n_pages, 40, page_table=table.cuda())
+        cache.a2sf_paged_append(k, v)
+        cache.past.fill_(past)
+        out, lse = cache.a2sf_paged_attend(q[:, :, past:], 0.9)
+        results.append((out.cpu(), lse.cpu(), pu.slots(cache, cache.scores.cpu(), 0, past + c)))
+        del cache
+    for x, y in zip(*results):
+        assert torch.equal(x, y)
