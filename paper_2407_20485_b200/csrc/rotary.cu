@@ -161,10 +161,13 @@ cudaError_t launch_w(const a2sf_rotary_plan *plan, const RotaryArgs &r, const Pa
     const long long threads = (long long)r.B * r.n * items;
     const long long gx = (threads + kRotThreads - 1) / kRotThreads;
     if (gx > 0x7fffffffll) return cudaErrorInvalidValue;
-    // the heads are split over blocks only as far as it takes to fill the device, a batch of kHeads at least
+    // The heads are split over blocks as far as it takes to fill the device twice (8 ragged prompts of up to 2047 tokens: 22.2 us,
+    // once 26.7, four times 22.7), but where once is enough for four heads a block, no further: a second, partial round costs more
+    // than longer blocks do (4 x 300 tokens, 48 heads: 8.6 against 10.0 us).
     const int total = r.Hq + (Append ? 2 * r.Hk : 0);
-    const long long want = 16ll * device_sm_count();
-    const long long gy = (want + gx - 1) / gx;
+    const long long once = 4ll * device_sm_count();
+    long long gy = once / gx;
+    if (gy * 4 < total) gy = (2 * once + gx - 1) / gx;
     const int hpb = (int)(((total + gy - 1) / gy + kHeads - 1) / kHeads) * kHeads;
     const int splits = (total + hpb - 1) / hpb;
     if (gx * splits > 0x7fffffffll) return cudaErrorInvalidValue;
