@@ -421,8 +421,9 @@ int a2sf_rotary(const a2sf_rotary_plan *plan, int32_t dtype, int32_t B, int32_t 
  * that status word and raises kernel limits: make it before a stream capture begins.
  * A page that two sequences share must not be written: by a2sf_paged_append, by a2sf_paged_evict in
  * place, nor by a2sf_paged_attend, which updates scores unless told not to.  Keys, values and
- * queries of resident tokens must be finite; slots beyond past + len may hold anything.  Calls on
- * the same sequences must be ordered (same stream, or events between streams).
+ * queries of resident tokens must be finite (32-bit storage: below 2^127 in magnitude); slots beyond
+ * past + len may hold anything.  Calls on the same sequences must be ordered (same stream, or events
+ * between streams).
  * ------------------------------------------------------------------------- */
 #define A2SF_PAGED_MAX_SEQUENCES 1024
 typedef struct a2sf_paged {
