@@ -1062,7 +1062,7 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         j.nq = ws.whole_scores ? n : (int)min((long long)(n - at.q), w1 - w);
         j.q0 = seq.first(at.kt) + at.q;
         // a tile begun by another CTA is this one's first, a tile that the next one goes on with its last
-        j.part = at.q > 0 ? 2 * blockIdx.x : j.nq < n ? 2 * blockIdx.x + 1 : -1;
+        j.part = at.q > 0 ? 2 * (int)blockIdx.x : j.nq < n ? 2 * (int)blockIdx.x + 1 : -1;
         w += j.nq;
         next_tile(w);
         return j;
