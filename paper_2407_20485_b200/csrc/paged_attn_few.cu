@@ -17,8 +17,10 @@
 //   finish  joins the partial outputs; S <- alpha^len S + sum_r alpha^age exp2(x_r - lse_r).
 //   whole   instead of both where no sequence can have more than a few tiles: a CTA takes whole units, keeps
 //           logits and partial results in shared memory and ends each unit itself.
-// P is rounded to the storage type for P V (half a step, as the output itself); the row sum and the
-// scores use the unrounded values.
+// P goes into P V as two terms of the storage type (off by the square of half a step; one term would be off by half a
+// step of every product, which shows where products cancel), as in the steps of the slot cache.  The memory time hides it: one
+// token over 32 x 40 caches of up to 4096 slots 244.5 us with one term, 245.3 with two; four tokens, G = 4, over 2 x 8 x 32,700
+// slots 61.4 and 61.7.  The row sum and the scores use the unrounded values.
 #include <type_traits>
 
 #include "paged.cuh"
@@ -76,6 +78,11 @@ template <> struct Mma16<__half> {
         const __half2 h = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t *>(&h);
     }
+    __device__ static void subtract(float (&x)[2], uint32_t packed)
+    {
+        const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&packed));
+        x[0] -= y.x; x[1] -= y.y;
+    }
 };
 template <> struct Mma16<__nv_bfloat16> {
     __device__ static void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -88,6 +95,11 @@ template <> struct Mma16<__nv_bfloat16> {
     {
         const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    __device__ static void subtract(float (&x)[2], uint32_t packed)      // a bf16 is the upper half of an fp32
+    {
+        x[0] -= __uint_as_float(packed << 16);
+        x[1] -= __uint_as_float(packed & 0xffff0000u);
     }
 };
 
@@ -226,6 +238,7 @@ template <typename T, int D, int NC> struct Body16 {
                     f[e] = mn == -INFINITY ? 1.f : ex2(m[g][e] - mn);
                     m[g][e] = mn;
                     l[g][e] *= f[e];
+                    if (CG == 1 && NP <= 4) f[e] = __shfl_sync(0xffffffffu, f[e], lane & ~2);      // lo's columns as hi's
                 }
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
@@ -233,7 +246,10 @@ template <typename T, int D, int NC> struct Body16 {
                     for (int e = 0; e < 4; ++e) o[g][k][e] *= f[e & 1];
             }
         }
-        uint32_t p[kSub][CG][2];
+        // A probability is the sum of two terms of the storage type: hi, and lo, what rounding to hi left.  Up to four rows use
+        // half of the instruction's columns: there lo goes into the other half, column + 4, and end() adds the two.
+        const bool beside = CG == 1 && NP <= 4;
+        uint32_t p[kSub][CG][2], rest[kSub][CG][2];
 #pragma unroll
         for (int u = 0; u < kSub; ++u)
 #pragma unroll
@@ -245,8 +261,20 @@ template <typename T, int D, int NC> struct Body16 {
                     w[e] = ex2(x[u][g][e] - (m[g][e & 1] == -INFINITY ? 0.f : m[g][e & 1]));
                     l[g][e & 1] += w[e];
                 }
-                p[u][g][0] = movmatrix_trans(Mma16<T>::pack(w[0], w[1]));
-                p[u][g][1] = movmatrix_trans(Mma16<T>::pack(w[2], w[3]));
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t hi = Mma16<T>::pack(w[2 * half], w[2 * half + 1]);
+                    float left[2] = {w[2 * half], w[2 * half + 1]};
+                    Mma16<T>::subtract(left, hi);
+                    const uint32_t lo = Mma16<T>::pack(left[0], left[1]);
+                    if (beside) {
+                        const uint32_t other = __shfl_xor_sync(0xffffffffu, lo, 2);
+                        if (c >= 2) hi = other;
+                    } else {
+                        rest[u][g][half] = movmatrix_trans(lo);
+                    }
+                    p[u][g][half] = movmatrix_trans(hi);
+                }
             }
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
@@ -256,7 +284,10 @@ template <typename T, int D, int NC> struct Body16 {
                 uint32_t v[4];
                 ldmatrix4_trans(v, vb + tile_offset<kTile>(row, 2 * k + piece));
 #pragma unroll
-                for (int g = 0; g < CG; ++g) Mma16<T>::mma(o[g][k], v, p[u][g][0], p[u][g][1]);
+                for (int g = 0; g < CG; ++g) {
+                    if (!beside) Mma16<T>::mma(o[g][k], v, rest[u][g][0], rest[u][g][1]);
+                    Mma16<T>::mma(o[g][k], v, p[u][g][0], p[u][g][1]);
+                }
             }
         }
     }
@@ -264,6 +295,12 @@ template <typename T, int D, int NC> struct Body16 {
     __device__ void end(float2 *ml, float *op, int NP)
     {
         const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+        if (CG == 1 && NP <= 4) {
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[0][k][e] += __shfl_xor_sync(0xffffffffu, o[0][k][e], 2);
+        }
 #pragma unroll
         for (int g = 0; g < CG; ++g)
 #pragma unroll

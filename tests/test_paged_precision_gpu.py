@@ -1,0 +1,78 @@
+"""How exact the attention over the paged cache is, on inputs where a rounding of the probabilities would show.
+
+Keys are made for given logits (log2 units): q = (1, 2^-9, 0, ..), k = (hi, lo, 0, ..), scale = ln 2; the reference takes what
+is stored.  u = torch.finfo(dtype).eps / 2 is the half step of the storage type, F = 2^-24 that of fp32."""
+import math
+
+import pytest
+import torch
+
+import paged_util as pu
+
+pytestmark = pytest.mark.gpu
+
+F = 2.0 ** -24
+BF, HF, FP = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def a2sf():
+    from paper_2407_20485_b200 import binding
+
+    return binding
+
+
+def run(a2sf, B, H, G, d, dtype, c, logits, values, room=0, ps=64):
+    """Attention of the last c tokens of sequences that all hold these logits and values [L] -> out, lse of every head and
+    the 64-bit out, lse, sum P|V| of one."""
+    L = logits.numel()
+    hi = logits.to(dtype)
+    k, v = torch.zeros((L, d), dtype=dtype), values.to(dtype)[:, None].expand(L, d).contiguous()
+    k[:, 0], k[:, 1] = hi, ((logits - hi.double()) * 512).to(dtype)
+    pages = -(-L // ps)
+    cache = a2sf.PagedCache(B, H, d, dtype, ps, B * pages, max(pages, -(-(L + room) // ps)), group=G, scale=math.log(2))
+    pad = torch.zeros((pages * ps, d), dtype=dtype)
+    for pool, x in ((cache.k_pages, k), (cache.v_pages, v)):
+        pad[:L] = x
+        pool.copy_(pad.view(1, pages, 1, ps, d).expand(B, pages, H, ps, d).reshape(B * pages, H, ps, d))
+    cache.page_table[:, :pages] = torch.arange(B * pages, dtype=torch.int32).view(B, pages)
+    cache.past.fill_(L - c)
+    q = torch.zeros((B, H * G, c, d), dtype=dtype, device="cuda")
+    q[..., 0], q[..., 1] = 1.0, 2.0 ** -9
+    out, lse = cache.a2sf_paged_attend(q, 0.9)
+    assert a2sf.a2sf_last_device_status() == a2sf.A2SF_OK
+    want = pu.attend_ref(k.double(), v.double(), q[0, :1].cpu().double(), torch.zeros(L, dtype=torch.float64), L - c, 0.9,
+                         float(torch.tensor(math.log(2), dtype=FP)))
+    return out.cpu().double(), lse.cpu().double(), want[0], want[1], want[3]
+
+
+def compare(out, o, tol, what):
+    worst = float(((out - o).abs() / tol).max())
+    assert worst <= 1, f"{what}: {worst:.3g} of the tolerance"
+
+
+PATHS = {
+    # B, H, G, d, c, L
+    "whole units": (1, 2, 1, 128, 1, 200), "whole units, 64": (2, 2, 2, 64, 2, 300), "whole units, 8 rows": (1, 2, 8, 128, 1, 150),
+    "split": (2, 2, 1, 128, 1, 4000), "split, 64": (1, 3, 3, 64, 1, 5000), "split, 8 rows": (2, 1, 4, 128, 2, 3000),
+    "split, 16 rows": (2, 2, 4, 64, 4, 3000), "small tiles": (1, 3, 1, 128, 40, 333), "small tiles, pieces": (1, 1, 2, 64, 30, 3000),
+    "large tiles": (60, 10, 1, 64, 64, 128)}
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("path", PATHS)
+def test_probabilities_keep_two_terms_of_the_storage_type(a2sf, path, dtype):
+    """Half of the keys have a probability just below the middle of two neighbours of the storage type, half just above, and
+    values 1 and -1: what is left of their sum is a tenth of what rounding to one term would add.  Two terms are off by u^2."""
+    B, H, G, d, c, L = PATHS[path]
+    u = torch.finfo(dtype).eps / 2
+    j = torch.arange(L)
+    kind = torch.where(j % 8 == 0, torch.zeros_like(j), 1 + j % 2)              # every eighth key: logit 0 and value 0
+    step = u                                                                   # between neighbours from 1/2 on
+    p = torch.tensor([1.0, 0.5 + 0.45 * step, 0.5 + 0.55 * step], dtype=torch.float64)[kind]
+    values = torch.tensor([0.0, 1.0, -1.0], dtype=torch.float64)[kind]
+    out, lse, o, z, size = run(a2sf, B, H, G, d, dtype, c, torch.log2(p), values)
+    e = (d + 2) * F * 2                                                        # logits of -1 and 0, from products of 1 at most
+    under = 0.0 if dtype != HF else 2.0 ** -25 * L                             # fp16 below its normal range
+    compare(out, o, u * o.abs() + (u * u + 2 * e + 2.0 ** -20 + L * F) * size + under, path)
+    compare(lse, z, torch.full_like(z, e + 2.0 ** -20) + 4 * F * z.abs(), path)
