@@ -41,9 +41,12 @@ template <typename T, int D> constexpr int tile_slots = D * sizeof(T) == 128 ? 1
 template <typename T> constexpr int warps_of = sizeof(T) == 4 ? 8 : 4;
 constexpr int kFinishThreads = 256;
 constexpr int kSms = 148;
-// How far a logit may lie above its column's reference (log2 units): 2^14 is a probability that fp16 holds, and
-// sums of it and of values up to 2^113 / slots stay finite.
-constexpr float kSlack = 14.f;
+// A column's reference is what is subtracted before the exponential (log2 units).  It is set kBelow under the maximum and stays
+// until a logit lies more than kSlack above it.  bf16 and fp32 have the range for any: sums of 2^14 and of values up to
+// 2^113 / slots stay finite.  fp16 has not: what falls under 2^-24 packs to 0 while the row sum still counts it, and from 2^-14
+// down there are fewer bits.  So its probabilities use the range up to 2^15, and that begins 2^-37 and 2^-27 under the maximum.
+template <typename T> constexpr float kBelow = std::is_same<T, __half>::value ? 13.f : 0.f;
+template <typename T> constexpr float kSlack = std::is_same<T, __half>::value ? 15.f : 14.f;
 
 __host__ __device__ constexpr int rows_padded(int rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
 
@@ -58,7 +61,7 @@ template <typename T, int D> struct Ring {
 
 struct FewWs {
     float *logits;        // [U][slots][NP], log2 units
-    float2 *ml;           // [segments][warps][NP] running maximum (log2 units), sum
+    float2 *ml;           // [segments][warps][NP] reference (log2 units), sum
     float *o;             // [segments][warps][NP][D]
     int32_t *prefix;      // [B + 1] tiles of a head, summed over the sequences before
     int slots;            // padded slots of a unit
@@ -199,8 +202,8 @@ template <typename T, int D, int NC> struct Body16 {
             fence_async_smem();            // these writes come before the copy that next fills the stage
             __syncwarp();
         }
-        // The reference of a column (what is subtracted before the exponential) moves only when a logit exceeds it by
-        // more than kSlack: probabilities up to 2^kSlack are as exact, and no maximum is looked for in between.
+        // The reference of a column moves only when a logit exceeds it by more than kSlack: probabilities up to 2^kSlack
+        // are as exact, and no maximum is looked for in between.
         bool beyond = false;
 #pragma unroll
         for (int u = 0; u < kSub; ++u)
@@ -210,7 +213,7 @@ template <typename T, int D, int NC> struct Body16 {
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + u * 16 + r + (e >> 1) * 8;
                     x[u][g][e] = j < vis[g][e & 1] ? x[u][g][e] * a.pv.sl2 : -INFINITY;
-                    beyond |= x[u][g][e] > m[g][e & 1] + kSlack;       // also where m is still -inf
+                    beyond |= x[u][g][e] > m[g][e & 1] + kSlack<T>;       // also where m is still -inf
                 }
                 if (logits) {
                     const int col = g * 8 + 2 * c;
@@ -234,7 +237,7 @@ template <typename T, int D, int NC> struct Body16 {
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                    const float mn = fmaxf(m[g][e], mx);
+                    const float mn = fmaxf(m[g][e], mx - kBelow<T>);
                     f[e] = mn == -INFINITY ? 1.f : ex2(m[g][e] - mn);
                     m[g][e] = mn;
                     l[g][e] *= f[e];
@@ -389,7 +392,7 @@ template <int D, int NC> struct Body32 {
             const bool seen = j < past + seen_by(r);
             acc[r] = seen ? acc[r] * a.pv.sl2 : -INFINITY;
             if (logits && part == r % 4) logits[(size_t)j * NC + r] = acc[r];
-            beyond |= acc[r] > m[r] + kSlack;
+            beyond |= acc[r] > m[r] + kSlack<float>;
         }
         if (__any_sync(0xffffffffu, beyond)) {
 #pragma unroll

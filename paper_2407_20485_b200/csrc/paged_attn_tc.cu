@@ -13,7 +13,7 @@
 //             operand of O += P V;  V is read MN-major from its TMA tile.
 //           A row's reference (what is subtracted before the exponential) stays where it is unless a
 //           row sum shows that a probability may have left fp16's range: then the tile is done again
-//           against the row's maximum and the accumulator rescaled.
+//           against the row's maximum and the accumulator rescaled.  (fp16: against 2^8 less, see kBelow.)
 //   merge   joins the items that were cut.
 //   score   S_j <- alpha^len S_j + sum_r exp2(s_rj - c_r), c_r = lse_r + age * (-log2 alpha): K tile x Q
 //           tiles transposed, so a slot is a TMEM lane and its sum is made by two threads in row order.
@@ -315,8 +315,12 @@ __device__ __forceinline__ void copy_query_tile(uint8_t *dst, const CUtensorMap 
 // ============================================================================================
 constexpr int kAttnThreads = 320;            // producer warp, MMA warp, 8 softmax warps
 constexpr int kKStages = 3, kVStages = 2;
-constexpr float kRescaleThreshold = 8.0f;    // log2 units
 constexpr float kOptimisticLimit = 32768.f;  // a row sum below this keeps every probability < 2^15
+constexpr float kRescaleThreshold = 8.0f;    // log2 units above the reference; beyond that limit one of 64 is 9 above
+// A new reference lies so far below the row's maximum (log2 units).  fp16 holds all bits of a probability down to 2^-14 and none
+// below 2^-24, while the row sum counts it: with 8 that is 2^-22 and 2^-32 of the maximum, and a tile of which all logits equal
+// it still has half of the limit.
+template <typename T> constexpr float kBelow = std::is_same<T, __half>::value ? 8.f : 0.f;
 
 struct AttnShared {
     uint64_t q_full, q_empty, k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
@@ -633,14 +637,14 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (t == 0) {
                         // a piece of the keys may hold none that this row sees (then none of the following
                         // tiles does either): any finite reference gives the zeros that are wanted
-                        m_x = smax == -INFINITY ? 0.f : smax * pv.sl2;
+                        m_x = smax == -INFINITY ? 0.f : fmaf(smax, pv.sl2, -kBelow<T>);
                         l_x = 0.f;
                     } else {
                         const float xmax = fmaf(smax, pv.sl2, -m_x);
                         const bool grow = xmax > kRescaleThreshold;
                         if (grow) {
-                            m_x += xmax;
-                            factor = ex2_approx(-xmax);
+                            m_x += xmax - kBelow<T>;
+                            factor = ex2_approx(kBelow<T> - xmax);
                         }
                         if (__any_sync(0xffffffffu, grow)) {
                             wait(&sh->o_done[X], (cnt_x - 1) & 1);          // O holds the tiles before

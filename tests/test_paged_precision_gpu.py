@@ -76,3 +76,31 @@ def test_probabilities_keep_two_terms_of_the_storage_type(a2sf, path, dtype):
     under = 0.0 if dtype != HF else 2.0 ** -25 * L                             # fp16 below its normal range
     compare(out, o, u * o.abs() + (u * u + 2 * e + 2.0 ** -20 + L * F) * size + under, path)
     compare(lse, z, torch.full_like(z, e + 2.0 ** -20) + 4 * F * z.abs(), path)
+
+
+# tcgen05: large by the capacity of the page table (`room` slots behind the sequence), with a plan and pieces; direct; two row tiles of a group
+LARGE = {"tcgen05": (1, 2, 1, 128, 130, 3000, 8000), "tcgen05, direct": (8, 8, 1, 128, 200, 700, 0), "tcgen05, group": (2, 1, 3, 64, 100, 2000, 20000)}
+BELOW = {"whole": 13, "split": 13, "small": 15, "large": 15, "tcgen05": 8}       # of the reference under the maximum, log2 units
+
+
+@pytest.mark.parametrize("sink", ["every", "first", "last"])
+@pytest.mark.parametrize("path", [*PATHS, *LARGE])
+def test_small_probabilities_in_fp16(a2sf, path, sink):
+    """Keys of equal, small probability beside one (or every sixteenth) that draws nearly everything and has value 0: the output is
+    the others' share.  fp16 holds a probability to half a step down to 2^-14 and to 2^-25 absolutely below, against a reference
+    2^BELOW under the maximum."""
+    B, H, G, d, c, L, room = (PATHS.get(path) or LARGE[path])[:6] + (LARGE.get(path, (0,) * 7)[6],)
+    u = 2.0 ** -11
+    j = torch.arange(L)
+    at = j % 16 == 0 if sink == "every" else j == (0 if sink == "first" else L - c)
+    values = torch.where(at, 0.0, 1000.0).double()
+    terms = u if path in LARGE else u * u
+    least = 2.0 ** -25 / 2.0 ** BELOW[path.split(",")[0].split(" ")[0]]
+    for small in (25.01, 24.45, 22.3, 17.6, 13.7, 30.0):
+        out, lse, o, z, size = run(a2sf, B, H, G, d, HF, c, torch.where(at, 0.0, -small).double(), values, room)
+        e = 6 * F * small                                                      # two products that are not zero, the sum, the scale
+        seen = L - c + 1 + torch.arange(c, dtype=torch.float64)[None, :, None]
+        weight = torch.floor((seen + 15) / 16) if sink == "every" else 1.0     # of the row, in units of the largest
+        under = least * seen * 1000 / weight
+        compare(out, o, u * o.abs() + 2.0 ** -25 + (terms + 2 * e + 2.0 ** -20 + L * F) * size + under, f"{path}, 2^-{small}")
+        compare(lse, z, torch.full_like(z, e + 2.0 ** -20) + 4 * F * z.abs() + L * F, path)
