@@ -1,5 +1,6 @@
 // Host side of the paged-cache and rotary entry points: argument validation, workspaces, dispatch.
 // No data is touched on the host.
+#include <cfloat>
 #include <cmath>
 #include <mutex>
 
@@ -160,28 +161,31 @@ int a2sf_rotary_plan_init(const a2sf_rotary_config *c, a2sf_rotary_plan *plan)
     const bool by_length = c->scaling == A2SF_ROTARY_BANDS || c->scaling == A2SF_ROTARY_RAMP;
     if (by_length && (c->original_length < 1 || !(c->low > 0.0) || !(c->high > c->low) || !std::isfinite(c->high))) return A2SF_ERR_INVALID_ARG;
 
-    const double two_pi = 6.283185307179586476925;
-    const double L = c->original_length;
-    const double theta = c->scaling == A2SF_ROTARY_NTK ? c->theta * std::pow(c->factor, r / (r - 2.0)) : c->theta;
+    // A position times a frequency keeps the error of the frequency 2^31 times: 53 bits leave 3e-7 of an angle, 64 bits 1e-10.
+    typedef long double wide;
+    static_assert(LDBL_MANT_DIG >= 64, "frequencies need 64 bits");
+    const wide two_pi = 6.283185307179586476925286766559006L;
+    const wide L = c->original_length, factor = c->factor;
+    const wide theta = c->scaling == A2SF_ROTARY_NTK ? c->theta * std::pow(factor, r / (r - 2.0L)) : (wide)c->theta;
     // RAMP: pair index at which `beta` turns fit into the original length
-    double lo = 0.0, hi = 0.0;
+    wide lo = 0.0L, hi = 0.0L;
     if (c->scaling == A2SF_ROTARY_RAMP) {
-        lo = std::floor(r * std::log(L / (c->high * two_pi)) / (2.0 * std::log(c->theta)));
-        hi = std::ceil(r * std::log(L / (c->low * two_pi)) / (2.0 * std::log(c->theta)));
-        lo = lo > 0.0 ? lo : 0.0;
-        hi = hi < r - 1.0 ? hi : r - 1.0;
+        lo = std::floor(r * std::log(L / (c->high * two_pi)) / (2.0L * std::log((wide)c->theta)));
+        hi = std::ceil(r * std::log(L / (c->low * two_pi)) / (2.0L * std::log((wide)c->theta)));
+        lo = lo > 0.0L ? lo : 0.0L;
+        hi = hi < r - 1.0L ? hi : r - 1.0L;
     }
     for (int k = 0; k < A2SF_ROTARY_MAX_PAIRS; ++k) {
         plan->turn[k] = 0;
         if (k >= r / 2) continue;
-        double f = std::pow(theta, -2.0 * k / r);
-        double keep = 1.0;                                            // share that is not interpolated
-        if (c->scaling == A2SF_ROTARY_LINEAR) keep = 0.0;
-        if (c->scaling == A2SF_ROTARY_BANDS) keep = (L * f / two_pi - c->low) / (c->high - c->low);
-        if (c->scaling == A2SF_ROTARY_RAMP) keep = 1.0 - (k - lo) / (hi - lo > 0.001 ? hi - lo : 0.001);
-        keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
-        f = keep * f + (1.0 - keep) * f / c->factor;
-        // turns per position are below 1/6: 2^64 times that fits, with the double's 53 bits
+        wide f = std::pow(theta, -2.0L * k / r);
+        wide keep = 1.0L;                                             // share that is not interpolated
+        if (c->scaling == A2SF_ROTARY_LINEAR) keep = 0.0L;
+        if (c->scaling == A2SF_ROTARY_BANDS) keep = (L * f / two_pi - c->low) / ((wide)c->high - c->low);
+        if (c->scaling == A2SF_ROTARY_RAMP) keep = 1.0L - (k - lo) / (hi - lo > 0.001L ? hi - lo : 0.001L);
+        keep = keep < 0.0L ? 0.0L : keep > 1.0L ? 1.0L : keep;
+        f = keep * f + (1.0L - keep) * f / factor;
+        // turns per position are below 1/6: 2^64 times that fits
         plan->turn[k] = (uint64_t)std::ldexp(f / two_pi, 64);
     }
     plan->rotary_dim = r;
