@@ -3,8 +3,9 @@
 //   y1 = m (x1 cos - x2 sin),  y2 = m (x2 cos + x1 sin),  angle = position * f_k
 //
 // The angle is held in turns as a 64-bit fixed-point fraction: position * turn[k] modulo 2^64 drops
-// whole turns exactly, so a far position costs no accuracy and no reduction.  Its top 32 bits are
-// rounded to fp32 (absolute error below 2^-26 turns) and go to sincospif.
+// whole turns exactly, so a far position costs no accuracy and no reduction.  Of its top 32 bits the
+// quarter turns are taken off; an eighth of a turn at most is rounded to fp32 (off by 2^-28 turns, 2.4e-8
+// of an angle) and goes to sincospif.
 //
 // Bound by memory: every element is read and written once.  A thread owns W neighbouring elements
 // (two groups of W, in the split layout) of one token and walks over the heads, so the sines and
@@ -80,10 +81,15 @@ rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ Rota
             const int k = Interleaved ? item * NP + e : item * W + e;
             if (!A2SF_IN_RANGE(k, A2SF_ROTARY_MAX_PAIRS, kDbgRotary)) return;
             const unsigned long long turn = plan.turn[k] * (unsigned long long)(long long)pos;
-            const float x = (float)(int)(turn >> 32) * (1.f / 2147483648.f);       // half turns in [-1, 1]
-            sincospif(x, &sn[e], &cs[e]);
-            sn[e] *= r.transpose ? -magnitude : magnitude;
-            cs[e] *= magnitude;
+            // quarter turns q, and an eighth of a turn either way (in half turns: [-1/4, 1/4])
+            const unsigned top = (unsigned)(turn >> 32), q = (top + 0x20000000u) >> 30;
+            const float x = (float)(int)(top - (q << 30)) * (1.f / 2147483648.f);
+            float s0, c0;
+            sincospif(x, &s0, &c0);
+            sn[e] = q & 1 ? c0 : s0;
+            cs[e] = q & 1 ? s0 : c0;
+            sn[e] *= (q & 2) != 0 != (r.transpose != 0) ? -magnitude : magnitude;
+            cs[e] *= ((q + 1) & 2) != 0 ? -magnitude : magnitude;
         }
     }
 
