@@ -104,3 +104,19 @@ def test_small_probabilities_in_fp16(a2sf, path, sink):
         under = least * seen * 1000 / weight
         compare(out, o, u * o.abs() + 2.0 ** -25 + (terms + 2 * e + 2.0 ** -20 + L * F) * size + under, f"{path}, 2^-{small}")
         compare(lse, z, torch.full_like(z, e + 2.0 ** -20) + 4 * F * z.abs() + L * F, path)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("path", [*PATHS, *LARGE])
+def test_values_up_to_the_stated_bound(a2sf, path, dtype):
+    """Values of nearly 2^113 / slots, all of one sign, under logits that rise and fall by tiles within what a reference may be
+    exceeded by: no sum before the division overflows."""
+    B, H, G, d, c, L, room = (PATHS.get(path) or LARGE[path])[:6] + (LARGE.get(path, (0,) * 7)[6],)
+    u = torch.finfo(dtype).eps / 2
+    j = torch.arange(L)
+    logits = (j // 64 % 4 * 4.5 + (j % 64 == 9) * 0.25).double()
+    values = torch.full((L,), 0.99 * 2.0 ** 113 / L, dtype=torch.float64)
+    out, lse, o, z, size = run(a2sf, B, H, G, d, dtype, c, logits, values, room)
+    e = 6 * F * 14
+    compare(out, o, u * o.abs() + (u + 2 * e + 2.0 ** -20 + L * F) * size, path)
+    compare(lse, z, torch.full_like(z, e + 2.0 ** -20) + 4 * F * z.abs() + L * F, path)
