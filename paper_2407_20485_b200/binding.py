@@ -465,23 +465,31 @@ def a2sf_rotary_plan_init(rotary_dim: int, theta: float = 10000.0, interleaved: 
     return plan
 
 
-def _load_calls():
-    """The extension that marshals torch tensors for the calls below (see csrc/torch_calls.cpp)."""
-    import importlib.util
+class _TorchCalls:
+    """The extension that marshals torch tensors for the calls below (see csrc/torch_calls.cpp), loaded when one of
+    them is made first: the rest of this module does without it."""
 
-    path = Path(__file__).resolve().parent / "_torch_calls.so"
-    if not path.exists():
-        raise ImportError(f"{path} is missing: build it with `python -m paper_2407_20485_b200.build`")
-    spec = importlib.util.spec_from_file_location("_torch_calls", path)
-    calls = importlib.util.module_from_spec(spec)
-    spec.loader.exec_module(calls)
-    calls.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
-        "a2sf_rotary", "a2sf_paged_append", "a2sf_paged_attend", "a2sf_paged_attend_workspace_bytes", "a2sf_paged_evict",
-        "a2sf_paged_evict_workspace_bytes")})
-    return calls
+    def __getattr__(self, name):
+        if name not in ("rotary", "Calls"):
+            raise AttributeError(name)
+        import importlib.util
+
+        from .build import calls_path
+
+        path = calls_path()
+        if not path.exists():
+            raise ImportError(f"{path} is missing: build it for this torch with `python -m paper_2407_20485_b200.build`")
+        spec = importlib.util.spec_from_file_location("_torch_calls", path)
+        calls = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(calls)
+        calls.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+            "a2sf_rotary", "a2sf_paged_append", "a2sf_paged_attend", "a2sf_paged_attend_workspace_bytes", "a2sf_paged_evict",
+            "a2sf_paged_evict_workspace_bytes")})
+        self.rotary, self.Calls = calls.rotary, calls.Calls
+        return self.__dict__[name]
 
 
-_calls = _load_calls()
+_calls = _TorchCalls()
 _addressof = ctypes.addressof
 
 

@@ -20,7 +20,6 @@ INCLUDE = PKG.parent / "include"
 OBJ_DIR = PKG / "_build"
 LIB_PATH = PKG / "liba2sf.so"
 CALLS_SRC = CSRC / "torch_calls.cpp"
-CALLS_PATH = PKG / "_torch_calls.so"
 DEBUG_OBJ_DIR = PKG / "_build_debug"
 DEBUG_LIB_PATH = PKG / "liba2sf_debug.so"
 
@@ -46,18 +45,40 @@ def _deps_mtime() -> float:
     return max(f.stat().st_mtime for f in files)
 
 
+def calls_path() -> Path:
+    """The Python extension that marshals torch tensors: made for one interpreter and one torch, and named after them."""
+    import torch
+
+    return PKG / f"_torch_calls.{sys.implementation.cache_tag}.torch-{torch.__version__}.so"
+
+
+def missing_for_calls() -> str | None:
+    """What this machine lacks to build the extension (the library itself needs nvcc alone), or None."""
+    import sysconfig
+
+    try:
+        import torch
+    except ImportError:
+        return "torch"
+    for header in (Path(torch.__file__).resolve().parent / "include/ATen/ATen.h", Path(sysconfig.get_paths()["include"]) / "Python.h"):
+        if not header.exists():
+            return str(header)
+    return None
+
+
 def build_calls(force: bool = False) -> Path:
-    """Compile ``_torch_calls.so``, the Python extension that marshals torch tensors (host code only)."""
+    """Compile the extension of ``calls_path()`` (host code only)."""
+    path = calls_path()
     newest = max(CALLS_SRC.stat().st_mtime, *(f.stat().st_mtime for f in INCLUDE.glob("*.h")))
-    if not force and CALLS_PATH.exists() and CALLS_PATH.stat().st_mtime >= newest:
-        return CALLS_PATH
+    if not force and path.exists() and path.stat().st_mtime >= newest:
+        return path
     import sysconfig
 
     import torch
 
     root = Path(torch.__file__).resolve().parent
     cuda = Path(_nvcc()).resolve().parent.parent / "include"
-    tmp = CALLS_PATH.with_suffix(f".tmp{os.getpid()}.so")
+    tmp = path.with_suffix(f".tmp{os.getpid()}.so")
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-o", str(tmp), str(CALLS_SRC),
            *(f"-I{p}" for p in (root / "include", root / "include/torch/csrc/api/include", cuda, sysconfig.get_paths()["include"])),
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
@@ -65,17 +86,16 @@ def build_calls(force: bool = False) -> Path:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, CALLS_PATH)
-    return CALLS_PATH
+    os.replace(tmp, path)
+    return path
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> Path:
     """Compile every ``csrc/*.cu`` and link the shared library (the bounds-checked one with
-    ``debug``).  Returns its path."""
+    ``debug``), and the extension for torch tensors where there is a torch.  Returns the library's path."""
     obj_dir, lib_path = (DEBUG_OBJ_DIR, DEBUG_LIB_PATH) if debug else (OBJ_DIR, LIB_PATH)
     extra = ["-DA2SF_DEBUG"] if debug else []
     obj_dir.mkdir(exist_ok=True)
-    build_calls(force)
     nvcc = _nvcc()
     hdr_m = _deps_mtime()
     jobs = []
@@ -104,6 +124,11 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> Pa
                "-o", str(tmp), *map(str, objs), "-cudart", "static"]
         run(cmd)
         os.replace(tmp, lib_path)
+    missing = missing_for_calls()
+    if missing is None:
+        build_calls(force)
+    else:
+        print(f"{missing} is missing: built {lib_path.name} without the extension for torch tensors", file=sys.stderr)
     return lib_path
 
 
