@@ -1054,7 +1054,6 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         w0 += seq.rows_of(at.kt) - at.q;
         next_tile(w0);
     }
-    dependents_may_start();
 
     struct Job {
         int b, h, j0, past, len, used, q0, nq;             // query tiles q0 .. q0 + nq - 1
@@ -1107,7 +1106,10 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                         copy_query_tile<D>(Qs + s * kTileBytes, &map_q, &sh->q_full[s], j.h * G, i0, j.b);
                     }
                 }
-                if (!waited) dependency_wait();
+                if (!waited) {
+                    dependency_wait();
+                    dependents_may_start();                 // the CTA's part: behind a wait, as everywhere
+                }
                 waited = true;
                 float c4[4];
 #pragma unroll
@@ -1121,7 +1123,10 @@ paged_score_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 if (lane == 0) mbar_arrive(&sh->c_ready[qt % kScoreRing]);
             }
         }
-        if (!waited) dependency_wait();
+        if (!waited) {
+            dependency_wait();
+            dependents_may_start();
+        }
         if (lane == 0 && *abort_flag) {
             int dummy = 0;
             for (int k = max(0, qt - kScoreStages); k < qt; ++k) mbar_wait(&sh->q_full[k % kScoreStages], (k / kScoreStages) & 1, &dummy);
