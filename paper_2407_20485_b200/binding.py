@@ -506,7 +506,20 @@ class PagedCache:
 
     The tensors are attributes: given ones are adopted, the others are made here (pages unset, scores
     0, positions -1, page table -1, lengths 0).  A step is a2sf_paged_append, a2sf_paged_attend,
-    a2sf_paged_evict.  To replace a tensor, make another PagedCache around it."""
+    a2sf_paged_evict.  Tensors change in place only, since the kernels have their addresses: to replace one, make
+    another PagedCache around it."""
+
+    _TENSORS = ("k_pages", "v_pages", "scores", "positions", "page_table", "past", "start")
+
+    def __setattr__(self, name, value):
+        if name in self._TENSORS and self.__dict__.get(name, value) is not value:
+            raise AttributeError(f"{name} cannot be replaced: the kernels have its address (make another PagedCache around the new one)")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        if name in self._TENSORS:
+            raise AttributeError(f"{name} cannot be deleted: the kernels have its address")
+        object.__delattr__(self, name)
 
     def __init__(self, B: int, H: int, d: int, dtype: torch.dtype, page_size: int, num_pages: int, max_pages: int, *,
                  group: int = 1, scale: float = 0.0, device="cuda", k_pages=None, v_pages=None, scores=None,

@@ -14,7 +14,7 @@ def kernels():
             yield pytest.param(text[m.end():text.index("\n}\n", m.end())], id=f"{path.stem}-{m.group(1)}")
 
 
-@pytest.mark.parametrize("body", kernels())
+@pytest.mark.parametrize("body", list(kernels()))
 def test_followers_may_start_only_behind_a_wait(body):
     """Every kernel waits for its predecessors; the followers' start is allowed, where it is allowed early, after a wait."""
     assert "dependency_wait();" in body
