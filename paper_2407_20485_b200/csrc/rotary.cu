@@ -81,15 +81,13 @@ rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ Rota
             const int k = Interleaved ? item * NP + e : item * W + e;
             if (!A2SF_IN_RANGE(k, A2SF_ROTARY_MAX_PAIRS, kDbgRotary)) return;
             const unsigned long long turn = plan.turn[k] * (unsigned long long)(long long)pos;
-            // quarter turns q, and an eighth of a turn either way (in half turns: [-1/4, 1/4])
-            const unsigned top = (unsigned)(turn >> 32), q = (top + 0x20000000u) >> 30;
-            const float x = (float)(int)(top - (q << 30)) * (1.f / 2147483648.f);
+            // the nearest quarter turn is in the top two bits of `near`; an eighth of a turn is left either way (half turns: [-1/4, 1/4])
+            const unsigned top = (unsigned)(turn >> 32), near = top + 0x20000000u;
             float s0, c0;
-            sincospif(x, &s0, &c0);
-            sn[e] = q & 1 ? c0 : s0;
-            cs[e] = q & 1 ? s0 : c0;
-            sn[e] *= (q & 2) != 0 != (r.transpose != 0) ? -magnitude : magnitude;
-            cs[e] *= ((q + 1) & 2) != 0 ? -magnitude : magnitude;
+            sincospif((float)(int)(top - (near & 0xc0000000u)) * (1.f / 2147483648.f), &s0, &c0);
+            const bool odd = near & 0x40000000u;
+            sn[e] = __uint_as_float(__float_as_uint(odd ? c0 : s0) ^ (near & 0x80000000u)) * (r.transpose ? -magnitude : magnitude);
+            cs[e] = __uint_as_float(__float_as_uint(odd ? s0 : c0) ^ ((near + 0x40000000u) & 0x80000000u)) * magnitude;
         }
     }
 
