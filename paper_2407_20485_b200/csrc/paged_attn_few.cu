@@ -19,8 +19,8 @@
 //           logits and partial results in shared memory and ends each unit itself.
 // P goes into P V as two terms of the storage type (off by the square of half a step; one term would be off by half a
 // step of every product, which shows where products cancel), as in the steps of the slot cache.  The memory time hides it: one
-// token over 32 x 40 caches of up to 4096 slots 244.5 us with one term, 245.3 with two; four tokens, G = 4, over 2 x 8 x 32,700
-// slots 61.4 and 61.7.  The row sum and the scores use the unrounded values.
+// token over 32 x 40 caches of up to 4096 slots 241 us with one term, 242 with two; four tokens, G = 4, over 2 x 8 x 32,700
+// slots 61.4 and 62.0.  The row sum and the scores use the unrounded values.
 #include <type_traits>
 
 #include "paged.cuh"
@@ -141,9 +141,13 @@ __device__ __forceinline__ const void *query_row(const AttendArgs &a, int b, int
     return static_cast<const char *>(a.q) + (b * a.sq.b + (int64_t)(h * a.pv.G + g) * a.sq.h + (int64_t)i * a.sq.t) * elem;
 }
 
-// ---- a consumer warp on 16-bit storage: NC = 8 or 16 row columns ------------------------------------
+// ---- a consumer warp on 16-bit storage: NC = 4, 8 or 16 rows ----------------------------------------
+// A probability is the sum of two terms of the storage type: hi, and lo, what rounding to hi left.  Up to four rows (kBeside) use
+// half of the instruction's columns: the other half gets the same rows, lo is what they bring into P V, and end() adds the
+// two.  It is a kernel of its own: with both forms in one, one token over 32 x 40 caches takes 247 us and not 242.
 template <typename T, int D, int NC> struct Body16 {
-    static constexpr int CG = NC / 8, KS = D / 16, kTile = tile_slots<T, D>, kSub = kTile / warps_of<T> / 16;
+    static constexpr bool kBeside = NC == 4;
+    static constexpr int CG = kBeside ? 1 : NC / 8, KS = D / 16, kTile = tile_slots<T, D>, kSub = kTile / warps_of<T> / 16;
     uint32_t q[CG][KS][2];
     float o[CG][KS][4], m[CG][2], l[CG][2];
     int vis[CG][2];
@@ -153,7 +157,7 @@ template <typename T, int D, int NC> struct Body16 {
         const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3, rows = st.len * a.pv.G;
 #pragma unroll
         for (int g = 0; g < CG; ++g) {
-            const int row = g * 8 + r;
+            const int row = (g * 8 + r) % NC;
             const uint32_t *src = row < rows ? static_cast<const uint32_t *>(query_row(a, x.b, x.h, row, sizeof(T))) : nullptr;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
@@ -164,7 +168,7 @@ template <typename T, int D, int NC> struct Body16 {
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int col = g * 8 + 2 * c + e;
+                const int col = (g * 8 + 2 * c + e) % NC;
                 vis[g][e] = col < rows ? st.past + col / a.pv.G + 1 : 0;
                 m[g][e] = -INFINITY;
                 l[g][e] = 0.f;
@@ -241,7 +245,6 @@ template <typename T, int D, int NC> struct Body16 {
                     f[e] = mn == -INFINITY ? 1.f : ex2(m[g][e] - mn);
                     m[g][e] = mn;
                     l[g][e] *= f[e];
-                    if (CG == 1 && NP <= 4) f[e] = __shfl_sync(0xffffffffu, f[e], lane & ~2);      // lo's columns as hi's
                 }
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
@@ -249,9 +252,6 @@ template <typename T, int D, int NC> struct Body16 {
                     for (int e = 0; e < 4; ++e) o[g][k][e] *= f[e & 1];
             }
         }
-        // A probability is the sum of two terms of the storage type: hi, and lo, what rounding to hi left.  Up to four rows use
-        // half of the instruction's columns: there lo goes into the other half, column + 4, and end() adds the two.
-        const bool beside = CG == 1 && NP <= 4;
         uint32_t p[kSub][CG][2], rest[kSub][CG][2];
 #pragma unroll
         for (int u = 0; u < kSub; ++u)
@@ -266,17 +266,12 @@ template <typename T, int D, int NC> struct Body16 {
                 }
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    uint32_t hi = Mma16<T>::pack(w[2 * half], w[2 * half + 1]);
+                    const uint32_t hi = Mma16<T>::pack(w[2 * half], w[2 * half + 1]);
                     float left[2] = {w[2 * half], w[2 * half + 1]};
                     Mma16<T>::subtract(left, hi);
                     const uint32_t lo = Mma16<T>::pack(left[0], left[1]);
-                    if (beside) {
-                        const uint32_t other = __shfl_xor_sync(0xffffffffu, lo, 2);
-                        if (c >= 2) hi = other;
-                    } else {
-                        rest[u][g][half] = movmatrix_trans(lo);
-                    }
-                    p[u][g][half] = movmatrix_trans(hi);
+                    if (!kBeside) rest[u][g][half] = movmatrix_trans(lo);
+                    p[u][g][half] = movmatrix_trans(kBeside && c >= 2 ? lo : hi);
                 }
             }
 #pragma unroll
@@ -287,10 +282,10 @@ template <typename T, int D, int NC> struct Body16 {
                 uint32_t v[4];
                 ldmatrix4_trans(v, vb + tile_offset<kTile>(row, 2 * k + piece));
 #pragma unroll
-                for (int g = 0; g < CG; ++g) {
-                    if (!beside) Mma16<T>::mma(o[g][k], v, rest[u][g][0], rest[u][g][1]);
-                    Mma16<T>::mma(o[g][k], v, p[u][g][0], p[u][g][1]);
-                }
+                for (int g = 0; g < CG; ++g)
+                    if (!kBeside) Mma16<T>::mma(o[g][k], v, rest[u][g][0], rest[u][g][1]);
+#pragma unroll
+                for (int g = 0; g < CG; ++g) Mma16<T>::mma(o[g][k], v, p[u][g][0], p[u][g][1]);
             }
         }
     }
@@ -298,7 +293,7 @@ template <typename T, int D, int NC> struct Body16 {
     __device__ void end(float2 *ml, float *op, int NP)
     {
         const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-        if (CG == 1 && NP <= 4) {
+        if (kBeside) {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -997,7 +992,7 @@ cudaError_t launch_d(int dtype, const AttendArgs &a, cudaStream_t s)
         default: return launch_nc<T, D, 16>(dtype, a, s);
         }
     } else {
-        return rows <= 8 ? launch_nc<T, D, 8>(dtype, a, s) : launch_nc<T, D, 16>(dtype, a, s);
+        return rows <= 4 ? launch_nc<T, D, 4>(dtype, a, s) : rows <= 8 ? launch_nc<T, D, 8>(dtype, a, s) : launch_nc<T, D, 16>(dtype, a, s);
     }
 }
 
