@@ -466,7 +466,9 @@ int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary_op
  * of its own and must not overlap q; rows i >= len[b] of out and lse are left as they were.  Rows whose weight alpha^age
  * is below 2^-126 (the smallest normal fp32 number) are left out of the sum.
  * workspace: DEVICE, 256-byte aligned, a2sf_paged_attend_workspace_bytes (0 = invalid arguments);
- * contents undefined afterwards; calls that may overlap in time need workspaces of their own. */
+ * contents undefined afterwards; calls that may overlap in time need workspaces of their own.  Its size follows
+ * the capacity of the page table, not what is cached: for c * group <= 16 it is mostly the logits, 4 bytes for
+ * every sequence, head, slot of capacity and row (rows rounded up to a power of two), with scores or without. */
 #define A2SF_ATTEND_NO_SCORES 1
 size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c);
 int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha,

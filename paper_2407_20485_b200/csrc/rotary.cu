@@ -23,7 +23,7 @@ static __device__ int g_paged_status = 0;
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kHeads = 2;        // heads in flight per thread: with four blocks an SM, 128 KB on the way
+constexpr int kHeads = 2;        // heads in flight per thread: with four blocks an SM, 64 KB on the way (neighbouring pairs: 32)
 
 // W consecutive elements of 16- or 32-bit storage, moved as one access of up to 16 bytes
 template <typename T, int W> struct alignas(sizeof(T) * W) Pack { T e[W]; };
