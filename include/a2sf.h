@@ -421,7 +421,8 @@ int a2sf_rotary(const a2sf_rotary_plan *plan, int32_t dtype, int32_t B, int32_t 
  * that status word and raises kernel limits: make it before a stream capture begins.
  * A page that two sequences share must not be written: by a2sf_paged_append, by a2sf_paged_evict in
  * place, nor by a2sf_paged_attend, which updates scores unless told not to.  Keys, values and
- * queries of resident tokens must be finite, and so must their logits in fp32; values must be below
+ * queries of resident tokens must be finite, their logits below 2^27 in magnitude (from 2^20 on the last place
+ * of an fp32 logit is no longer small against a probability's exponent); values must be below
  * 2^113 / (past + len) in magnitude (fp16 always is), since up to 2^14 times their sum is held before
  * the division by the row sum, and keys and queries of 32-bit storage below 2^127.  Slots beyond
  * past + len may hold anything.  Calls on the same sequences must be ordered (same stream, or events

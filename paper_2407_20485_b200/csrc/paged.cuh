@@ -68,6 +68,15 @@ __device__ __forceinline__ float age_exponent(int age, float nl2a) { return age 
 
 __host__ inline float neg_log2(float alpha) { return alpha > 0.f ? -log2f(alpha) : INFINITY; }
 
+// The reference (what is subtracted before the exponential, log2 units) of a row whose largest logit is `mx`: kBelow under it, but
+// nowhere by more than 15 -- large logits round the difference -- so that fp16 holds the largest probability.
+template <int kBelow> __device__ __forceinline__ float reference(float mx)
+{
+    if (kBelow == 0) return mx;
+    const float m = mx - (float)kBelow;
+    return mx - m <= 15.f ? m : mx;                      // -inf stays -inf
+}
+
 // First row (token of the chunk) whose weight alpha^(len-1-i) is not below 2^-126, the smallest normal
 // fp32 number: a probability is at most 1, and the exponential of what lies below is flushed to zero.
 __device__ __forceinline__ int first_weighted_token(int len, float nl2a)

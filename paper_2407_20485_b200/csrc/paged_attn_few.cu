@@ -45,7 +45,7 @@ constexpr int kSms = 148;
 // until a logit lies more than kSlack above it.  bf16 and fp32 have the range for any: sums of 2^14 and of values up to
 // 2^113 / slots stay finite.  fp16 has not: what falls under 2^-24 packs to 0 while the row sum still counts it, and from 2^-14
 // down there are fewer bits.  So its probabilities use the range up to 2^15, and that begins 2^-37 and 2^-27 under the maximum.
-template <typename T> constexpr float kBelow = std::is_same<T, __half>::value ? 13.f : 0.f;
+template <typename T> constexpr int kBelow = std::is_same<T, __half>::value ? 13 : 0;
 template <typename T> constexpr float kSlack = std::is_same<T, __half>::value ? 15.f : 14.f;
 
 __host__ __device__ constexpr int rows_padded(int rows) { return rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
@@ -217,7 +217,7 @@ template <typename T, int D, int NC> struct Body16 {
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + u * 16 + r + (e >> 1) * 8;
                     x[u][g][e] = j < vis[g][e & 1] ? x[u][g][e] * a.pv.sl2 : -INFINITY;
-                    beyond |= x[u][g][e] > m[g][e & 1] + kSlack<T>;       // also where m is still -inf
+                    beyond |= x[u][g][e] - m[g][e & 1] > kSlack<T>;       // also where m is still -inf; the difference is exact
                 }
                 if (logits) {
                     const int col = g * 8 + 2 * c;
@@ -241,7 +241,7 @@ template <typename T, int D, int NC> struct Body16 {
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                    const float mn = fmaxf(m[g][e], mx - kBelow<T>);
+                    const float mn = fmaxf(m[g][e], reference<kBelow<T>>(mx));
                     f[e] = mn == -INFINITY ? 1.f : ex2(m[g][e] - mn);
                     m[g][e] = mn;
                     l[g][e] *= f[e];
@@ -387,7 +387,7 @@ template <int D, int NC> struct Body32 {
             const bool seen = j < past + seen_by(r);
             acc[r] = seen ? acc[r] * a.pv.sl2 : -INFINITY;
             if (logits && part == r % 4) logits[(size_t)j * NC + r] = acc[r];
-            beyond |= acc[r] > m[r] + kSlack<float>;
+            beyond |= acc[r] - m[r] > kSlack<float>;
         }
         if (__any_sync(0xffffffffu, beyond)) {
 #pragma unroll

@@ -38,7 +38,7 @@ constexpr int kTile = 64;        // keys (attn) or rows (score) of a walked tile
 constexpr int kSms = 148;
 // The reference (what is subtracted before the exponential, log2 units) lies so far below the maximum: fp16 then holds all bits of a
 // probability down to 2^-29 of the largest, and some down to 2^-39; what is below packs to 0 while the row sum counts it.
-template <typename T> constexpr float kBelow = std::is_same<T, __half>::value ? 15.f : 0.f;
+template <typename T> constexpr int kBelow = std::is_same<T, __half>::value ? 15 : 0;
 
 // Row distances in shared memory, in elements.  32 bits: 8 lanes reading 64 bytes of 2 rows (Q, K), or 16 bytes of every second
 // of 8 rows (V), meet 32 different banks; 16 bits: 8 rows of an 8 x 8 matrix do.
@@ -419,7 +419,7 @@ paged_attn_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
                     v = j0 + wk + n * 8 + 2 * c + e < vis[x] ? v * a.pv.sl2 : -INFINITY;
                     mx = fmaxf(mx, v);
                 }
-            const float mn = fmaxf(m[x], quad_max(mx) - kBelow<T>);
+            const float mn = fmaxf(m[x], reference<kBelow<T>>(quad_max(mx)));
             const float ref = mn == -INFINITY ? 0.f : mn; // nothing seen so far: any finite reference gives zeros
             const float factor = exp2f(m[x] - ref);
             m[x] = mn;

@@ -321,7 +321,7 @@ constexpr float kOptimisticLimit = 32768.f;  // a row sum below this keeps every
 constexpr float kRescaleThreshold = 8.0f;    // log2 units above the reference; beyond that limit one of 64 is 9 above
 // A new reference lies so far below the row's maximum (log2 units).  fp16 holds all bits of a probability down to 2^-14 and none
 // below 2^-24, while the row sum counts it: with 8 that is 2^-22 and 2^-32 of the maximum, and a tile of which all logits equal
-// it still has half of the limit.
+// it still has half of the limit.  Rounded up, where logits are large: no exponent is above kBelow then.
 template <typename T> constexpr float kBelow = std::is_same<T, __half>::value ? 8.f : 0.f;
 
 struct AttnShared {
@@ -639,14 +639,15 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (t == 0) {
                         // a piece of the keys may hold none that this row sees (then none of the following
                         // tiles does either): any finite reference gives the zeros that are wanted
-                        m_x = smax == -INFINITY ? 0.f : fmaf(smax, pv.sl2, -kBelow<T>);
+                        m_x = smax == -INFINITY ? 0.f : __fmaf_ru(smax, pv.sl2, -kBelow<T>);
                         l_x = 0.f;
                     } else {
                         const float xmax = fmaf(smax, pv.sl2, -m_x);
                         const bool grow = xmax > kRescaleThreshold;
                         if (grow) {
-                            m_x += xmax - kBelow<T>;
-                            factor = ex2_approx(kBelow<T> - xmax);
+                            const float before = m_x;
+                            m_x = __fmaf_ru(smax, pv.sl2, -kBelow<T>);
+                            factor = ex2_approx(before - m_x);
                         }
                         if (__any_sync(0xffffffffu, grow)) {
                             wait(&sh->o_done[X], (cnt_x - 1) & 1);          // O holds the tiles before

@@ -120,3 +120,33 @@ def test_values_up_to_the_stated_bound(a2sf, path, dtype):
     e = 6 * F * 14
     compare(out, o, u * o.abs() + (u + 2 * e + 2.0 ** -20 + L * F) * size, path)
     compare(lse, z, torch.full_like(z, e + 2.0 ** -20) + 4 * F * z.abs() + L * F, path)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("place", [2, 8, 16])
+@pytest.mark.parametrize("path", [*PATHS, *LARGE])
+def test_logits_whose_last_place_is_a_power_of_the_probability(a2sf, path, place, dtype):
+    """Logits of 1.5e7 last places that rise and fall by up to 30 of them: a last place of 2 (log2 units) or more rounds what is
+    subtracted before the exponential.  With values of 1 the output is 1 whatever the probabilities; none may leave the type's
+    range."""
+    B, H, G, d, c, L, room = (PATHS.get(path) or LARGE[path])[:6] + (LARGE.get(path, (0,) * 7)[6],)
+    u, ps = torch.finfo(dtype).eps / 2, 64
+    pages = -(-L // ps)
+    j = torch.arange(pages * ps)
+    k = torch.zeros((pages * ps, d), dtype=dtype)
+    k[:, 0], k[:, 1] = 59904.0, (j // 64 % 4 * 20 + j % 16).div(2).floor().mul(2).to(dtype)
+    cache = a2sf.PagedCache(B, H, d, dtype, ps, B * pages, max(pages, -(-(L + room) // ps)), group=G, scale=256 * place * math.log(2))
+    cache.k_pages.copy_(k.view(1, pages, 1, ps, d).expand(B, pages, H, ps, d).reshape(B * pages, H, ps, d))
+    cache.v_pages.fill_(1.0)
+    cache.page_table[:, :pages] = torch.arange(B * pages, dtype=torch.int32).view(B, pages)
+    cache.past.fill_(L - c)
+    q = torch.zeros((B, H * G, c, d), dtype=dtype, device="cuda")
+    q[..., 0], q[..., 1] = 1.0, 2.0 ** -9
+    out, lse = cache.a2sf_paged_attend(q, 0.9)
+    assert a2sf.a2sf_last_device_status() == a2sf.A2SF_OK
+    terms = u if path in LARGE else u * u
+    compare(out.cpu().double(), torch.ones(()), torch.tensor(u + terms + 2.0 ** -20 + L * F), path)
+    # the largest logit is one that the row sees; the sum adds ln L at most
+    seen = (59904 + k[:L, 1].double() / 512).cummax(0).values[L - c:] * float(torch.tensor(256 * place * math.log(2), dtype=FP))
+    worst = float((lse.cpu().double() - seen).abs().max())
+    assert worst <= math.log(L) + 4 * place * math.log(2), worst
