@@ -95,9 +95,9 @@ EncodeTiledFn encode_fn()
 
 // Which attention: few rows are bound by the cache's bytes whatever the type; more rows of 32-bit storage by products of
 // split operands, of 16-bit storage by tcgen05 -- whose plan, 128-row tiles and one CTA per SM cost more than a small call
-// takes.  Small goes by the multiply-adds of Q K^T at the cache's capacity (us, tcgen05 and mma.sync): 12 heads, 244 tokens,
-// 5e7: 14.8 and 10.8; 36 heads, 302 tokens, 2e8: 26.7 and 18.9; 8 heads, 928 tokens, 5e8: 31.8 and 31.2; 32 heads, 100 behind
-// 2,000, 9e8: 42 and 67.  One tile of 64 rows: 640 heads, 64 behind 100, 1e9: 73 and 51; 64 x 64 behind 4,000, 2e9: 85 and 86.
+// takes.  Small goes by the multiply-adds of Q K^T at the cache's capacity (us, tcgen05 and mma.sync, bf16): 12 heads, 244 tokens,
+// 5e7: 14.9 and 12.4; 36 heads, 302 tokens, 2e8: 21.2 and 18.5; 8 heads, 928 tokens, 5e8: 32.1 and 31.7; 32 heads, 100 behind
+// 2,000, 9e8: 42 and 70.  One tile of 64 rows: 640 heads, 64 behind 100, 1e9: 71 and 52; 64 x 64 behind 4,000, 2e9: 83 and 96.
 enum Path { kFew, kTc, kMma };
 Path path_of(const a2sf_paged *p, int c)
 {
