@@ -400,6 +400,41 @@ int a2sf_rotary(const a2sf_rotary_plan *plan, int32_t dtype, int32_t B, int32_t 
                 void *cuda_stream);
 
 /* ---------------------------------------------------------------------------
+ * Rotary positions with several axes (time, height and width of images and video, say): every token has a position
+ * on each axis, and pair k of a row turns by the position on ITS axis times f_k.  Everything else is as above.
+ *
+ * a2sf_rotary_axes_plan_init (host only): `axes` axes, pairs[a] pairs of axis a, rotary_dim = 2 * their sum.
+ *   order BLOCKS: the first pairs[0] pairs are axis 0's, the next pairs[1] axis 1's, and so on.
+ *         CYCLE : pairs are dealt to the axes in turn; an axis that has all of its own is passed over.
+ *   n_plans 1   : pair k has the frequency f_k of plans[0], whose rotary_dim must be that of the whole.
+ *           axes: the j-th pair of axis a has the frequency f_j of plans[a], whose rotary_dim must be 2 * pairs[a];
+ *                 the plans must agree in `interleaved` and magnitude.
+ * Accepted: 1 <= axes <= A2SF_ROTARY_MAX_AXES, pairs[a] >= 1, at most A2SF_ROTARY_MAX_PAIRS pairs.  INVALID_ARG otherwise.
+ *
+ * a2sf_rotary_axes: as a2sf_rotary; positions (DEVICE [axes][B][n] int32, contiguous, any values) must be given and are
+ * not read for rows t >= lens[b].
+ * ------------------------------------------------------------------------- */
+typedef enum { A2SF_ROTARY_BLOCKS = 0, A2SF_ROTARY_CYCLE = 1 } a2sf_rotary_order;
+
+#define A2SF_ROTARY_MAX_AXES 4
+typedef struct a2sf_rotary_axes_plan {
+    int32_t rotary_dim, interleaved;
+    float magnitude;
+    int32_t check;               /* written by a2sf_rotary_axes_plan_init; other values are refused */
+    int32_t axes, reserved;
+    uint64_t turn[A2SF_ROTARY_MAX_PAIRS];
+    uint8_t axis[A2SF_ROTARY_MAX_PAIRS];
+} a2sf_rotary_axes_plan;
+
+int a2sf_rotary_axes_plan_init(int32_t axes, const int32_t *pairs, int32_t order, const a2sf_rotary_plan *plans, int32_t n_plans,
+                               a2sf_rotary_axes_plan *plan);
+
+int a2sf_rotary_axes(const a2sf_rotary_axes_plan *plan, int32_t dtype, int32_t B, int32_t H, int32_t n, int32_t d,
+                     const void *x, int64_t x_stride_b, int64_t x_stride_h, int64_t x_stride_t,
+                     void *y, int64_t y_stride_b, int64_t y_stride_h, int64_t y_stride_t,
+                     const int32_t *positions, const int32_t *lens, int32_t flags, void *cuda_stream);
+
+/* ---------------------------------------------------------------------------
  * The cache in pages.  A pool of pages, each holding page_size slots of every K/V head, and a
  * page table per sequence: slot s of sequence b is slot s % page_size of page
  * page_table[b][s / page_size].  Prompts of different lengths, prompts that arrive in chunks and
@@ -409,7 +444,7 @@ int a2sf_rotary(const a2sf_rotary_plan *plan, int32_t dtype, int32_t B, int32_t 
  *     a2sf_paged_append   the chunk's keys and values into slots past .. past + len - 1
  *     a2sf_paged_attend   its attention over slots 0 .. past + len - 1, and the scores
  *     a2sf_paged_evict    back to the budget; past and start move on
- * for chunks of one token (generation) as for whole prompts.  All memory is the caller's; the
+ * (for layers of bounded reach a2sf_paged_attend_window and a2sf_paged_slide) for chunks of one token (generation) as for whole prompts.  All memory is the caller's; the
  * struct holds DEVICE pointers and is read during the call only.
  *   Per call, len[b] = min(lens[b], c), or c when lens is NULL.  A sequence with len 0 takes no
  *   part: nothing of it is read or written (a2sf_paged_evict still brings it to the budget).
@@ -458,6 +493,16 @@ int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary_op
                       void *q_out, int64_t qo_stride_b, int64_t qo_stride_h, int64_t qo_stride_t,
                       void *cuda_stream);
 
+/* a2sf_paged_append with a rotation of several axes: keys (and queries, when q is not NULL) turn by `positions`, DEVICE
+ * [axes][B][c] int32, which is read for tokens t < len[b].  The positions that the cache keeps, by which a2sf_paged_evict tells
+ * new tokens from old ones, are start[b] + t as there.  The plan must be given. */
+int a2sf_paged_append_axes(const a2sf_paged *cache, const a2sf_rotary_axes_plan *plan, const int32_t *positions, int32_t c,
+                           const int32_t *lens,
+                           const void *k, const void *v, int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_t,
+                           const void *q_opt, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
+                           void *q_out, int64_t qo_stride_b, int64_t qo_stride_h, int64_t qo_stride_t,
+                           void *cuda_stream);
+
 /* Attention of the chunk (appended before): row i of query head h*group + g sees slots
  * 0 .. past[b] + i of K/V head h.
  *     out = softmax(scale q K^T) V,   lse = log sum exp   ([B][H*group][c] fp32, or NULL)
@@ -476,6 +521,35 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
                       const void *q, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
                       void *out, int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t,
                       float *lse_opt, int32_t flags, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Attention of the chunk (appended before) through a sliding window, with a few first slots that stay visible (sinks): row i,
+ * at slot p = past[b] + i, of query head h*group + g sees of K/V head h
+ *     slots j < sinks with j <= p,   and   slots j with p - window < j <= p      (itself and the window - 1 before it)
+ *     out = softmax(scale q K^T) V,   lse = log sum exp   ([B][H*group][c] fp32, or NULL).
+ * window >= 1; sinks >= 0.  Slots must be in the order of their tokens, as a2sf_paged_append leaves them and a2sf_paged_evict with
+ * a dst_table (the window then counts the tokens that are left); eviction in place does not keep it.
+ * Scores are neither read nor written: what a token outside the window gets is zero from then on, so that age alone decides what
+ * stays (a2sf_paged_slide).  Page-table entries whose page holds no slot that a row of the call sees are not read, and slots of
+ * other pages that no row sees may hold anything.  out has strides of its own and must not overlap q; rows i >= len[b] of out
+ * and lse are left as they were.  workspace: as for a2sf_paged_attend, from a2sf_paged_attend_window_workspace_bytes (0 = invalid
+ * arguments); its size follows min(sinks + window + c, the capacity of the page table). */
+size_t a2sf_paged_attend_window_workspace_bytes(const a2sf_paged *cache, int32_t c, int32_t window, int32_t sinks);
+int a2sf_paged_attend_window(const a2sf_paged *cache, int32_t c, const int32_t *lens, int32_t window, int32_t sinks,
+                             const void *q, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,
+                             void *out, int64_t out_stride_b, int64_t out_stride_h, int64_t out_stride_t,
+                             float *lse_opt, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Ends a step of sequences whose attention is windowed: with n = past + len, past_out[b] = n and start_out[b] = start[b] + len[b],
+ * and the pages that no later row sees leave the page table: those of entries e with sinks <= e * page_size
+ * and (e + 1) * page_size <= n - window + 1.  A sequence with len 0 takes part (n = past).
+ *   table_out [B][max_pages]: the table with -1 in their place.
+ *   freed [B][max_pages] or NULL: their page numbers, in the order of the entries; freed_count [B] or NULL: how many there are.
+ *     What follows them in freed is left as it was.  Entries below 0 have left before and are not listed.
+ * table_out, past_out and start_out may be page_table, past and start; otherwise no output overlaps an input or another output.
+ * Slots keep their numbers: the capacity of the page table bounds a sequence's whole length.  A page that several sequences share
+ * is listed for each that it leaves.  Keys, values, scores and positions are not touched (k_pages and the like are not read). */
+int a2sf_paged_slide(const a2sf_paged *cache, int32_t c, const int32_t *lens, int32_t window, int32_t sinks, int32_t *table_out,
+                     int32_t *freed, int32_t *freed_count, int32_t *past_out, int32_t *start_out, void *cuda_stream);
 
 /* Ends a step.  Of the n = past + len slots of every head min(n, budget) stay: those at the
  * `recent` newest positions (position >= start + len - recent) and of the others the best under

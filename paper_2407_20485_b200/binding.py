@@ -43,6 +43,12 @@ class a2sf_rotary_plan(ctypes.Structure):
                 ("check", ctypes.c_int32), ("turn", ctypes.c_uint64 * 64)]
 
 
+class a2sf_rotary_axes_plan(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("check", ctypes.c_int32), ("axes", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("turn", ctypes.c_uint64 * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
 class a2sf_paged(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("group", ctypes.c_int32), ("d", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32),
@@ -110,6 +116,14 @@ def _load():
         "a2sf_rotary_plan_init": (ctypes.c_int, [ctypes.POINTER(a2sf_rotary_config), ctypes.POINTER(a2sf_rotary_plan)]),
         "a2sf_rotary": (ctypes.c_int, [vp, i32, i32, i32, i32, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp, vp, vp,
                                        i32, vp]),
+        "a2sf_rotary_axes_plan_init": (ctypes.c_int, [i32, ctypes.POINTER(i32), i32, ctypes.POINTER(a2sf_rotary_plan), i32,
+                                                      ctypes.POINTER(a2sf_rotary_axes_plan)]),
+        "a2sf_rotary_axes": (ctypes.c_int, [vp, i32, i32, i32, i32, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp, vp, i32, vp]),
+        "a2sf_paged_append_axes": (ctypes.c_int, [vp, vp, vp, i32, vp, vp, vp, i64, i64, i64, vp, i64, i64, i64,
+                                                  vp, i64, i64, i64, vp]),
+        "a2sf_paged_attend_window_workspace_bytes": (sz, [vp, i32, i32, i32]),
+        "a2sf_paged_attend_window": (ctypes.c_int, [vp, i32, vp, i32, i32, vp, i64, i64, i64, vp, i64, i64, i64, vp, vp, sz, vp]),
+        "a2sf_paged_slide": (ctypes.c_int, [vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp]),
         "a2sf_paged_append": (ctypes.c_int, [vp, vp, i32, vp, vp, vp, i64, i64, i64, vp, i64, i64, i64,
                                              vp, i64, i64, i64, vp]),
         "a2sf_paged_attend_workspace_bytes": (sz, [vp, i32]),
@@ -470,7 +484,7 @@ class _TorchCalls:
     them is made first: the rest of this module does without it."""
 
     def __getattr__(self, name):
-        if name not in ("rotary", "Calls"):
+        if name not in ("rotary", "rotary_axes", "Calls"):
             raise AttributeError(name)
         import importlib.util
 
@@ -484,8 +498,9 @@ class _TorchCalls:
         spec.loader.exec_module(calls)
         calls.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
             "a2sf_rotary", "a2sf_paged_append", "a2sf_paged_attend", "a2sf_paged_attend_workspace_bytes", "a2sf_paged_evict",
-            "a2sf_paged_evict_workspace_bytes")})
-        self.rotary, self.Calls = calls.rotary, calls.Calls
+            "a2sf_paged_evict_workspace_bytes", "a2sf_rotary_axes", "a2sf_paged_append_axes", "a2sf_paged_attend_window",
+            "a2sf_paged_attend_window_workspace_bytes", "a2sf_paged_slide")})
+        self.rotary, self.rotary_axes, self.Calls = calls.rotary, calls.rotary_axes, calls.Calls
         return self.__dict__[name]
 
 
@@ -501,12 +516,39 @@ def a2sf_rotary(plan: a2sf_rotary_plan, x, out=None, positions=None, start=None,
     return out
 
 
+def a2sf_rotary_axes_plan_init(pairs, plans, cycle: bool = False) -> a2sf_rotary_axes_plan:
+    """The plan of a rotation with several axes (host only): ``pairs`` of each axis, in blocks or dealt to the axes in turn
+    (``cycle``).  ``plans``: one plan for the frequencies of all pairs, or a list of one plan for each axis."""
+    plans = [plans] if isinstance(plans, a2sf_rotary_plan) else list(plans)
+    pairs = [int(n) for n in pairs]
+    if not pairs or not all(0 < n <= 64 for n in pairs) or not all(isinstance(p, a2sf_rotary_plan) for p in plans):
+        raise ValueError(f"pairs: expected 1 to 64 for each axis, and plans of a2sf_rotary_plan_init, got {pairs} and {plans}")
+    plan = a2sf_rotary_axes_plan()
+    _check(lib.a2sf_rotary_axes_plan_init(len(pairs), (ctypes.c_int32 * len(pairs))(*pairs), int(bool(cycle)),
+                                          (a2sf_rotary_plan * len(plans))(*plans), len(plans), ctypes.byref(plan)), "a2sf_rotary_axes_plan_init")
+    return plan
+
+
+def _axes_plan(plan) -> int:
+    if not isinstance(plan, a2sf_rotary_axes_plan):
+        raise ValueError(f"expected a plan of a2sf_rotary_axes_plan_init, got {type(plan).__name__}")
+    return _addressof(plan)
+
+
+def a2sf_rotary_axes(plan: a2sf_rotary_axes_plan, x, positions, out=None, lens=None, transpose=False, stream=None):
+    """x [B,H,n,d] rotated by its ``positions`` [axes,B,n] (int32), every pair by that on its own axis.  ``out`` may be x."""
+    status, out = _calls.rotary_axes(_axes_plan(plan), x, positions, out, lens, transpose, -1 if stream is None else stream.cuda_stream)
+    if status != A2SF_OK:
+        raise A2SFError(status, "a2sf_rotary_axes")
+    return out
+
+
 class PagedCache:
     """A pool of cache pages and the page table and lengths of ``B`` sequences (see ``a2sf_paged``).
 
     The tensors are attributes: given ones are adopted, the others are made here (pages unset, scores
     0, positions -1, page table -1, lengths 0).  A step is a2sf_paged_append, a2sf_paged_attend,
-    a2sf_paged_evict.  Tensors change in place only, since the kernels have their addresses: to replace one, make
+    a2sf_paged_evict (or, for layers of bounded reach, a2sf_paged_attend_window and a2sf_paged_slide).  Tensors change in place only, since the kernels have their addresses: to replace one, make
     another PagedCache around it."""
 
     _TENSORS = ("k_pages", "v_pages", "scores", "positions", "page_table", "past", "start")
@@ -562,6 +604,13 @@ class PagedCache:
             raise A2SFError(status, "a2sf_paged_append")
         return q_out
 
+    def a2sf_paged_append_axes(self, k, v, positions, rotary, lens=None, q=None, q_out=None, stream=None):
+        """a2sf_paged_append with a ``rotary`` plan of several axes: keys and queries turn by ``positions`` [axes,B,c] (int32)."""
+        status, q_out = self._calls.append_axes(k, v, positions, _axes_plan(rotary), lens, q, q_out, -1 if stream is None else stream.cuda_stream)
+        if status != A2SF_OK:
+            raise A2SFError(status, "a2sf_paged_append_axes")
+        return q_out
+
     def a2sf_paged_attend(self, q, alpha=1.0, lens=None, out=None, lse=None, scores=True, workspace=None, stream=None):
         """Attention of q [B,H*group,c,d] over the cache and the chunk appended before; returns (out, lse).  The cache's
         scores are decayed and added to unless ``scores`` is False."""
@@ -569,6 +618,25 @@ class PagedCache:
         if status != A2SF_OK:
             raise A2SFError(status, "a2sf_paged_attend")
         return out, lse
+
+    def a2sf_paged_attend_window(self, q, window: int, sinks: int = 0, lens=None, out=None, lse=None, workspace=None, stream=None):
+        """Attention of q [B,H*group,c,d] where the row at slot p sees the first ``sinks`` slots and the ``window`` up to p;
+        returns (out, lse).  Scores are neither read nor written."""
+        status, out, lse = self._calls.attend_window(q, window, sinks, lens, out, lse, workspace, -1 if stream is None else stream.cuda_stream)
+        if status != A2SF_OK:
+            raise A2SFError(status, "a2sf_paged_attend_window")
+        return out, lse
+
+    def a2sf_paged_slide(self, window: int, sinks: int = 0, c: int = 1, lens=None, table_out=None, freed=None, freed_count=None,
+                         past_out=None, start_out=None, stream=None):
+        """Ends a step of windowed attention whose chunk had ``lens`` (or c) tokens: ``past`` and ``start`` move on (or
+        ``past_out`` and ``start_out`` get the values), and pages that no later row sees leave the page table (or ``table_out``
+        gets it).  Their numbers go to ``freed`` [B, max_pages], how many there are to ``freed_count`` [B], where given."""
+        status = self._calls.slide(window, sinks, c, lens, self.page_table if table_out is None else table_out, freed, freed_count,
+                                   self.past if past_out is None else past_out, self.start if start_out is None else start_out,
+                                   -1 if stream is None else stream.cuda_stream)
+        if status != A2SF_OK:
+            raise A2SFError(status, "a2sf_paged_slide")
 
     def a2sf_paged_evict(self, budget: int, recent: int, c: int = 1, lens=None, dst_table=None, past_out=None,
                          start_out=None, workspace=None, stream=None):
@@ -583,6 +651,9 @@ class PagedCache:
     def attend_workspace_bytes(self, c: int) -> int:
         """Size of a workspace for chunks of c tokens (0: invalid arguments)."""
         return int(lib.a2sf_paged_attend_workspace_bytes(ctypes.byref(self.p), c))
+
+    def attend_window_workspace_bytes(self, c: int, window: int, sinks: int = 0) -> int:
+        return int(lib.a2sf_paged_attend_window_workspace_bytes(ctypes.byref(self.p), c, window, sinks))
 
     def evict_workspace_bytes(self, budget: int) -> int:
         return int(lib.a2sf_paged_evict_workspace_bytes(ctypes.byref(self.p), budget))

@@ -9,7 +9,7 @@
 namespace a2sf {
 namespace {
 
-constexpr int32_t kPlanCheck = 0x52504c4e;
+constexpr int32_t kPlanCheck = 0x52504c4e, kAxesPlanCheck = 0x52415850;
 
 inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -38,6 +38,27 @@ int check_plan(const a2sf_rotary_plan *p, int d)
     if (!p || p->check != kPlanCheck || p->rotary_dim < 2 || p->rotary_dim > 2 * A2SF_ROTARY_MAX_PAIRS || p->rotary_dim % 2)
         return A2SF_ERR_INVALID_ARG;
     return p->rotary_dim <= d ? A2SF_OK : A2SF_ERR_INVALID_ARG;
+}
+
+int check_axes_plan(const a2sf_rotary_axes_plan *p, int d)
+{
+    if (!p || p->check != kAxesPlanCheck || p->rotary_dim < 2 || p->rotary_dim > 2 * A2SF_ROTARY_MAX_PAIRS || p->rotary_dim % 2 ||
+        p->axes < 1 || p->axes > A2SF_ROTARY_MAX_AXES)
+        return A2SF_ERR_INVALID_ARG;
+    for (int k = 0; k < p->rotary_dim / 2; ++k)
+        if (p->axis[k] >= p->axes) return A2SF_ERR_INVALID_ARG;
+    return p->rotary_dim <= d ? A2SF_OK : A2SF_ERR_INVALID_ARG;
+}
+
+// x and y of a rotation: valid tensors, and in place only with the same strides
+int check_rotation(int dtype, int d, const int64_t extent[3], const void *x, const int64_t xs[3], const void *y, const int64_t ys[3])
+{
+    int rc;
+    if ((rc = check_tensor(x, dtype, d, extent, xs)) != A2SF_OK || (rc = check_tensor(y, dtype, d, extent, ys)) != A2SF_OK) return rc;
+    if (x == y)
+        for (int i = 0; i < 3; ++i)
+            if (extent[i] > 1 && xs[i] != ys[i]) return A2SF_ERR_INVALID_ARG;
+    return A2SF_OK;
 }
 
 int check_paged(const a2sf_paged *p, int c)
@@ -72,6 +93,21 @@ PagedView make_view(const a2sf_paged *p, int c, const int32_t *lens)
     v.ps_shift = p->page_size == 16 ? 4 : p->page_size == 32 ? 5 : p->page_size == 64 ? 6 : 7;
     v.max_pages = p->max_pages; v.num_pages = p->num_pages; v.c = c;
     v.sl2 = (p->scale > 0.f ? p->scale : 1.f / std::sqrt((float)p->d)) * kLog2e;
+    v.window = v.sinks = v.sink_end = v.grain = 0;
+    return v;
+}
+
+// Slots that lie together in the list of what a windowed call sees, and in one box of a copy.
+constexpr int kGrain = 16;
+
+PagedView make_window_view(const a2sf_paged *p, int c, const int32_t *lens, int window, int sinks)
+{
+    PagedView v = make_view(p, c, lens);
+    const int cap = p->max_pages * p->page_size;              // nothing is beyond it
+    v.grain = kGrain < p->page_size ? kGrain : p->page_size;
+    v.window = window < cap ? window : cap;
+    v.sinks = sinks < cap ? sinks : cap;
+    v.sink_end = (v.sinks + v.grain - 1) / v.grain * v.grain;
     return v;
 }
 
@@ -99,13 +135,28 @@ EncodeTiledFn encode_fn()
 // 5e7: 14.9 and 12.4; 36 heads, 302 tokens, 2e8: 21.2 and 18.5; 8 heads, 928 tokens, 5e8: 32.1 and 31.7; 32 heads, 100 behind
 // 2,000, 9e8: 42 and 70.  One tile of 64 rows: 640 heads, 64 behind 100, 1e9: 71 and 52; 64 x 64 behind 4,000, 2e9: 83 and 96.
 enum Path { kFew, kTc, kMma };
-Path path_of(const a2sf_paged *p, int c)
+// Windowed, a row tile of tcgen05 (256 rows) sees the near capacity of its tokens and that is what counts.
+Path path_of(const PagedView &v, int dtype)
 {
-    const int64_t rows = (int64_t)c * p->group;
+    const int64_t rows = (int64_t)v.c * v.G;
     if (rows <= kFewRows) return kFew;
-    if (p->dtype == A2SF_F32) return kMma;
-    const double work = (double)p->B * p->H * rows * p->max_pages * p->page_size * p->d;
+    if (dtype == A2SF_F32) return kMma;
+    const int tokens = 256 / v.G < v.c ? 256 / v.G : v.c;
+    const double work = (double)v.B * v.H * rows * near_capacity(v, tokens) * v.d;
     return work < (rows <= 64 ? 1.2e9 : 3e8) ? kMma : kTc;
+}
+
+size_t attend_ws_bytes(const PagedView &v, int dtype)
+{
+    const Path path = path_of(v, dtype);
+    const size_t bytes = align_up(path == kFew ? attend_few_ws_bytes(dtype, v) : path == kTc ? attend_tc_ws_bytes(v) : attend_mma_ws_bytes(dtype, v));
+    return bytes ? bytes : 256;                               // 0 says that arguments are invalid
+}
+
+cudaError_t launch_attend(int dtype, const AttendArgs &a, cudaStream_t s)
+{
+    const Path path = path_of(a.pv, dtype);
+    return path == kFew ? launch_attend_few(dtype, a, s) : path == kTc ? launch_attend_tc(dtype, a, s) : launch_attend_mma(dtype, a, s);
 }
 
 }  // namespace
@@ -223,6 +274,96 @@ int a2sf_rotary(const a2sf_rotary_plan *plan, int32_t dtype, int32_t B, int32_t 
     return launch_rotary(dtype, plan, r, nullptr, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
 }
 
+int a2sf_rotary_axes_plan_init(int32_t axes, const int32_t *pairs, int32_t order, const a2sf_rotary_plan *plans, int32_t n_plans,
+                               a2sf_rotary_axes_plan *plan)
+{
+    if (axes < 1 || axes > A2SF_ROTARY_MAX_AXES || !pairs || !plans || !plan || (n_plans != 1 && n_plans != axes)) return A2SF_ERR_INVALID_ARG;
+    if (order != A2SF_ROTARY_BLOCKS && order != A2SF_ROTARY_CYCLE) return A2SF_ERR_INVALID_ARG;
+    int total = 0;
+    for (int a = 0; a < axes; ++a) {
+        if (pairs[a] < 1 || pairs[a] > A2SF_ROTARY_MAX_PAIRS) return A2SF_ERR_INVALID_ARG;
+        total += pairs[a];
+    }
+    if (total > A2SF_ROTARY_MAX_PAIRS) return A2SF_ERR_INVALID_ARG;
+    for (int p = 0; p < n_plans; ++p) {
+        if (check_plan(&plans[p], 2 * A2SF_ROTARY_MAX_PAIRS) != A2SF_OK || plans[p].rotary_dim != 2 * (n_plans == 1 ? total : pairs[p]) ||
+            plans[p].interleaved != plans[0].interleaved || plans[p].magnitude != plans[0].magnitude)
+            return A2SF_ERR_INVALID_ARG;
+    }
+    int taken[A2SF_ROTARY_MAX_AXES] = {};
+    int turn = 0;                                             // whose it is
+    for (int k = 0; k < A2SF_ROTARY_MAX_PAIRS; ++k) {
+        plan->turn[k] = 0;
+        plan->axis[k] = 0;
+        if (k >= total) continue;
+        while (taken[turn] == pairs[turn]) turn = (turn + 1) % axes;
+        plan->axis[k] = (uint8_t)turn;
+        plan->turn[k] = n_plans == 1 ? plans[0].turn[k] : plans[turn].turn[taken[turn]];
+        ++taken[turn];
+        if (order == A2SF_ROTARY_CYCLE) turn = (turn + 1) % axes;
+    }
+    plan->rotary_dim = 2 * total;
+    plan->interleaved = plans[0].interleaved;
+    plan->magnitude = plans[0].magnitude;
+    plan->axes = axes;
+    plan->reserved = 0;
+    plan->check = kAxesPlanCheck;
+    return A2SF_OK;
+}
+
+int a2sf_rotary_axes(const a2sf_rotary_axes_plan *plan, int32_t dtype, int32_t B, int32_t H, int32_t n, int32_t d, const void *x,
+                     int64_t x_stride_b, int64_t x_stride_h, int64_t x_stride_t, void *y, int64_t y_stride_b, int64_t y_stride_h,
+                     int64_t y_stride_t, const int32_t *positions, const int32_t *lens, int32_t flags, void *cuda_stream)
+{
+    A2SF_TRACE("a2sf_rotary_axes");
+    int rc = check_shape(dtype, d);
+    if (rc != A2SF_OK) return rc;
+    if (B < 1 || H < 1 || n < 1 || (flags & ~A2SF_ROTARY_TRANSPOSE)) return A2SF_ERR_INVALID_ARG;
+    if ((rc = check_axes_plan(plan, d)) != A2SF_OK) return rc;
+    const int64_t extent[3] = {B, H, n};
+    const int64_t xs[3] = {x_stride_b, x_stride_h, x_stride_t}, ys[3] = {y_stride_b, y_stride_h, y_stride_t};
+    if ((rc = check_rotation(dtype, d, extent, x, xs, y, ys)) != A2SF_OK) return rc;
+    if (!positions || !aligned(positions, 4) || !aligned(lens, 4)) return A2SF_ERR_INVALID_ARG;
+    RotaryArgs r = {};
+    r.x = x; r.y = y;
+    r.sx = Strides{x_stride_b, x_stride_h, x_stride_t};
+    r.sy = Strides{y_stride_b, y_stride_h, y_stride_t};
+    r.positions = positions; r.lens = lens;
+    r.B = B; r.n = n; r.d = d; r.Hq = H; r.Hk = 0;
+    r.transpose = flags & A2SF_ROTARY_TRANSPOSE;
+    return launch_rotary_axes(dtype, plan, r, nullptr, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+}
+
+int a2sf_paged_append_axes(const a2sf_paged *cache, const a2sf_rotary_axes_plan *plan, const int32_t *positions, int32_t c, const int32_t *lens,
+                           const void *k, const void *v, int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_t,
+                           const void *q, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t, void *q_out,
+                           int64_t qo_stride_b, int64_t qo_stride_h, int64_t qo_stride_t, void *cuda_stream)
+{
+    A2SF_TRACE("a2sf_paged_append_axes");
+    int rc = check_paged(cache, c);
+    if (rc != A2SF_OK) return rc;
+    if ((rc = check_axes_plan(plan, cache->d)) != A2SF_OK) return rc;
+    if (!positions || !aligned(positions, 4) || !aligned(lens, 4)) return A2SF_ERR_INVALID_ARG;
+    const int64_t ekv[3] = {cache->B, cache->H, c}, eq[3] = {cache->B, (int64_t)cache->H * cache->group, c};
+    const int64_t skv[3] = {kv_stride_b, kv_stride_h, kv_stride_t};
+    const int64_t sq[3] = {q_stride_b, q_stride_h, q_stride_t}, so[3] = {qo_stride_b, qo_stride_h, qo_stride_t};
+    if ((rc = check_tensor(k, cache->dtype, cache->d, ekv, skv)) != A2SF_OK || (rc = check_tensor(v, cache->dtype, cache->d, ekv, skv)) != A2SF_OK)
+        return rc;
+    if (q && (rc = check_rotation(cache->dtype, cache->d, eq, q, sq, q_out, so)) != A2SF_OK) return rc;
+    PagedView pv = make_view(cache, c, lens);
+    if (!(pv.status = paged_status_word())) return A2SF_ERR_CUDA;
+    RotaryArgs r = {};
+    r.x = q; r.y = q_out; r.k = k; r.v = v;
+    r.sx = Strides{q_stride_b, q_stride_h, q_stride_t};
+    r.sy = Strides{qo_stride_b, qo_stride_h, qo_stride_t};
+    r.skv = Strides{kv_stride_b, kv_stride_h, kv_stride_t};
+    r.positions = positions; r.start = cache->start; r.lens = lens;
+    r.B = cache->B; r.n = c; r.d = cache->d;
+    r.Hq = q ? cache->H * cache->group : 0;
+    r.Hk = cache->H;
+    return launch_rotary_axes(cache->dtype, plan, r, &pv, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+}
+
 int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary, int32_t c, const int32_t *lens,
                       const void *k, const void *v, int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_t,
                       const void *q, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t, void *q_out,
@@ -265,9 +406,7 @@ int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary, i
 size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c)
 {
     if (check_paged(cache, c) != A2SF_OK) return 0;
-    const PagedView pv = make_view(cache, c, nullptr);
-    const Path path = path_of(cache, c);
-    return align_up(path == kFew ? attend_few_ws_bytes(cache->dtype, pv) : path == kTc ? attend_tc_ws_bytes(pv) : attend_mma_ws_bytes(cache->dtype, pv));
+    return attend_ws_bytes(make_view(cache, c, nullptr), cache->dtype);
 }
 
 int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha, const void *q,
@@ -296,11 +435,74 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
     a.alpha = alpha; a.nl2a = neg_log2(alpha);
     a.scores = !(flags & A2SF_ATTEND_NO_SCORES);
     a.ws = workspace;
-    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    const Path path = path_of(cache, c);
-    const cudaError_t e = path == kFew ? launch_attend_few(cache->dtype, a, s)
-                          : path == kTc ? launch_attend_tc(cache->dtype, a, s) : launch_attend_mma(cache->dtype, a, s);
-    return e == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+    return launch_attend(cache->dtype, a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+}
+
+size_t a2sf_paged_attend_window_workspace_bytes(const a2sf_paged *cache, int32_t c, int32_t window, int32_t sinks)
+{
+    if (check_paged(cache, c) != A2SF_OK || window < 1 || sinks < 0) return 0;
+    return attend_ws_bytes(make_window_view(cache, c, nullptr, window, sinks), cache->dtype);
+}
+
+int a2sf_paged_attend_window(const a2sf_paged *cache, int32_t c, const int32_t *lens, int32_t window, int32_t sinks, const void *q,
+                             int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t, void *out, int64_t out_stride_b,
+                             int64_t out_stride_h, int64_t out_stride_t, float *lse, void *workspace, size_t workspace_bytes,
+                             void *cuda_stream)
+{
+    A2SF_TRACE("a2sf_paged_attend_window");
+    int rc = check_paged(cache, c);
+    if (rc != A2SF_OK) return rc;
+    if (window < 1 || sinks < 0) return A2SF_ERR_INVALID_ARG;
+    const int64_t eq[3] = {cache->B, (int64_t)cache->H * cache->group, c};
+    const int64_t sq[3] = {q_stride_b, q_stride_h, q_stride_t}, so[3] = {out_stride_b, out_stride_h, out_stride_t};
+    if ((rc = check_tensor(q, cache->dtype, cache->d, eq, sq)) != A2SF_OK ||
+        (rc = check_tensor(out, cache->dtype, cache->d, eq, so)) != A2SF_OK)
+        return rc;
+    if (!aligned(lens, 4) || !aligned(lse, 4) || !workspace || !aligned(workspace, 256)) return A2SF_ERR_INVALID_ARG;
+    if (q == out) return A2SF_ERR_INVALID_ARG;
+    AttendArgs a;
+    a.pv = make_window_view(cache, c, lens, window, sinks);
+    if (workspace_bytes < attend_ws_bytes(a.pv, cache->dtype)) return A2SF_ERR_WORKSPACE;
+    if (!(a.pv.status = paged_status_word())) return A2SF_ERR_CUDA;
+    a.q = q; a.out = out; a.lse = lse;
+    a.sq = Strides{q_stride_b, q_stride_h, q_stride_t};
+    a.so = Strides{out_stride_b, out_stride_h, out_stride_t};
+    a.alpha = 1.f; a.nl2a = 0.f;
+    a.scores = false;
+    a.ws = workspace;
+    return launch_attend(cache->dtype, a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
+}
+
+int a2sf_paged_slide(const a2sf_paged *cache, int32_t c, const int32_t *lens, int32_t window, int32_t sinks, int32_t *table_out,
+                     int32_t *freed, int32_t *freed_count, int32_t *past_out, int32_t *start_out, void *cuda_stream)
+{
+    A2SF_TRACE("a2sf_paged_slide");
+    const int rc = check_paged(cache, c);
+    if (rc != A2SF_OK) return rc;
+    if (window < 1 || sinks < 0 || !table_out || !past_out || !start_out) return A2SF_ERR_INVALID_ARG;
+    // a block reads one sequence's entries and writes its outputs: an output may be the array it comes from, and else touches
+    // no input and no other output
+    const size_t B = cache->B, pages = B * cache->max_pages;
+    const struct { const int32_t *p, *from; size_t n; } outs[] = {{table_out, cache->page_table, pages}, {past_out, cache->past, B},
+                                                                  {start_out, cache->start, B}, {freed, nullptr, pages}, {freed_count, nullptr, B}};
+    const struct { const int32_t *p; size_t n; } ins[] = {{cache->page_table, pages}, {cache->past, B}, {cache->start, B}, {lens, B}};
+    auto meet = [](const int32_t *a, size_t na, const int32_t *b, size_t nb) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+        return a && b && x < y + nb * 4 && y < x + na * 4;
+    };
+    for (int x = 0; x < 5; ++x) {
+        if (!aligned(outs[x].p, 4)) return A2SF_ERR_INVALID_ARG;
+        for (int y = 0; y < x; ++y)
+            if (meet(outs[x].p, outs[x].n, outs[y].p, outs[y].n)) return A2SF_ERR_INVALID_ARG;
+        for (const auto &in : ins)
+            if (meet(outs[x].p, outs[x].n, in.p, in.n) && !(outs[x].p == outs[x].from && in.p == outs[x].from)) return A2SF_ERR_INVALID_ARG;
+    }
+    if (!aligned(lens, 4)) return A2SF_ERR_INVALID_ARG;
+    PagedView pv = make_view(cache, c, lens);
+    if (!(pv.status = paged_status_word())) return A2SF_ERR_CUDA;
+    const int cap = cache->max_pages * cache->page_size;       // nothing is beyond it
+    const SlideArgs a = {table_out, freed, freed_count, past_out, start_out, window < cap ? window : cap, sinks < cap ? sinks : cap};
+    return launch_slide(pv, a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
 }
 
 size_t a2sf_paged_evict_workspace_bytes(const a2sf_paged *cache, int32_t budget)

@@ -17,6 +17,7 @@ struct PagedView {
     int *status;                 // sticky status word of the paged kernels
     int B, H, G, d, ps, ps_shift, max_pages, num_pages, c;
     float sl2;                   // scale * log2(e)
+    int window, sinks, sink_end, grain;   // windowed attention (else 0), see Near: sink_end is sinks in whole grains
 };
 
 struct SeqState {
@@ -63,6 +64,53 @@ __device__ __forceinline__ int64_t pool_row(const PagedView &a, int page, int h,
     return A2SF_IN_RANGE(row, ((int64_t)a.num_pages * a.H) << a.ps_shift, kDbgPagedRow) && A2SF_IN_RANGE(h, a.H, kDbgPagedRow) ? row : 0;
 }
 
+// ---- windowed attention (template parameter Win): what is seen, as a list without a gap ----------------
+// The row at slot p sees slots j < sinks and p - window < j <= p.  Of the rows from token i0 of the chunk on none sees a slot
+// between the sinks and  lo = past + i0 + 1 - window.  So their slots are numbered along a list: the grains (16 slots or more, of one
+// page) that hold the sinks, then those from lo's on; `skip` slots, whole grains, lie between and are neither read nor looked up.
+// In these numbers a row's place is past - skip + i, and the rule above holds as it stands: a slot of the sinks' grains is
+// below every window if anything is skipped.  Without a window nothing is skipped, and near numbers are slots.
+struct Near {
+    int past, skip;              // near slots before the chunk; slots left out
+    int dead;                    // near slots sinks .. dead-1 are seen by none of the rows: they may hold anything
+};
+
+template <bool Win> __device__ __forceinline__ Near near_slots(const PagedView &a, int past, int i0)
+{
+    Near n = {past, 0, 0};
+    if (Win) {
+        const int lo = max(0, past + i0 + 1 - a.window);
+        n.skip = max(0, (lo & -a.grain) - a.sink_end);
+        n.past = past - n.skip;
+        n.dead = lo - n.skip;
+    }
+    return n;
+}
+template <bool Win> __device__ __forceinline__ int real_slot(const PagedView &a, const Near &n, int s)
+{
+    return Win && s >= a.sink_end ? s + n.skip : s;
+}
+// Rows of one TMA box: what lies together in a page and in the list.
+template <bool Win> __device__ __forceinline__ int box_rows(const PagedView &a, int tile) { return min(Win ? a.grain : a.ps, tile); }
+
+// Lengths of sequence b with past in near numbers, for all rows of the chunk.
+template <bool Win> __device__ __forceinline__ SeqState near_state(const PagedView &a, int b, Near &n)
+{
+    SeqState s = seq_state(a, b);
+    n = near_slots<Win>(a, s.past, 0);
+    s.past = n.past;
+    return s;
+}
+
+// Near slots that `rows` consecutive tokens can see at most (host): the capacity without a window.
+__host__ inline int near_capacity(const PagedView &a, int rows)
+{
+    const long long cap = (long long)a.max_pages << a.ps_shift;
+    if (!a.window) return (int)cap;
+    const long long most = (long long)a.sink_end + a.window - 1 + rows + a.grain - 1;
+    return (int)(most < cap ? most : cap);
+}
+
 // alpha^age in fp32, with 0^0 = 1 (nl2a = -log2 alpha, +inf for alpha = 0)
 __device__ __forceinline__ float age_exponent(int age, float nl2a) { return age == 0 ? 0.f : (float)age * nl2a; }
 
@@ -92,20 +140,21 @@ struct Where {            // position in the list: unit (b, h), tile t of its `t
 };
 
 // Tiles of one head of sequence b; none where it takes no part in the call.
-template <int Tile> __device__ __forceinline__ int seq_tiles(const PagedView &pv, int b)
+template <int Tile, bool Win = false> __device__ __forceinline__ int seq_tiles(const PagedView &pv, int b)
 {
-    const SeqState st = seq_state(pv, b);
+    Near near;
+    const SeqState st = near_state<Win>(pv, b, near);
     return st.len > 0 ? (st.past + st.len + Tile - 1) / Tile : 0;
 }
 
 // prefix[0 .. B] of the sequences' tiles, by one warp
-template <int Tile> __device__ __forceinline__ void tile_prefix(int32_t *prefix, const PagedView &pv)
+template <int Tile, bool Win = false> __device__ __forceinline__ void tile_prefix(int32_t *prefix, const PagedView &pv)
 {
     const int lane = threadIdx.x & 31;
     int run = 0;
     for (int b0 = 0; b0 < pv.B; b0 += 32) {
         const int b = b0 + lane;
-        int incl = b < pv.B ? seq_tiles<Tile>(pv, b) : 0;
+        int incl = b < pv.B ? seq_tiles<Tile, Win>(pv, b) : 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, incl, o);
@@ -177,13 +226,16 @@ struct RotaryArgs {
     const void *x, *k, *v;
     void *y;
     Strides sx, sy, skv;
-    const int32_t *positions;    // [B][n] or nullptr
+    const int32_t *positions;    // [B][n] or nullptr; with several axes [axes][B][n]
     const int32_t *start;        // [B] or nullptr (0, or past in append)
     const int32_t *lens;
     int B, n, d, Hq, Hk, transpose;
 };
 cudaError_t launch_rotary(int dtype, const a2sf_rotary_plan *plan, const RotaryArgs &r, const PagedView *pages,
                           cudaStream_t s);
+
+cudaError_t launch_rotary_axes(int dtype, const a2sf_rotary_axes_plan *plan, const RotaryArgs &r, const PagedView *pages,
+                               cudaStream_t s);
 
 struct AttendArgs {
     PagedView pv;
@@ -215,5 +267,11 @@ cudaError_t launch_attend_mma(int dtype, const AttendArgs &a, cudaStream_t s);
 cudaError_t launch_evict(int elem_bytes, const PagedView &pv, int budget, int recent, const int32_t *dst_table,
                          int dst_max_pages, int32_t *past_out, int32_t *start_out, void *ws, cudaStream_t s);
 size_t evict_ws_bytes(size_t units, int budget);
+
+struct SlideArgs {
+    int32_t *table_out, *freed, *freed_count, *past_out, *start_out;      // freed, freed_count may be nullptr
+    int window, sinks;
+};
+cudaError_t launch_slide(const PagedView &pv, const SlideArgs &a, cudaStream_t s);
 
 }  // namespace a2sf

@@ -17,6 +17,8 @@
 //   finish  joins the partial outputs; S <- alpha^len S + sum_r alpha^age exp2(x_r - lse_r).
 //   whole   instead of both where no sequence can have more than a few tiles: a CTA takes whole units, keeps
 //           logits and partial results in shared memory and ends each unit itself.
+// Windowed (Win): the same over the near slots of a sequence (see Near), which is all that it sees; no logits are kept, and the
+// finish kernel joins outputs alone.
 // P goes into P V as two terms of the storage type (off by the square of half a step; one term would be off by half a
 // step of every product, which shows where products cancel), as in the steps of the slot cache.  The memory time hides it: one
 // token over 32 x 40 caches of up to 4096 slots 241 us with one term, 242 with two; four tokens, G = 4, over 2 x 8 x 32,700
@@ -145,15 +147,16 @@ __device__ __forceinline__ const void *query_row(const AttendArgs &a, int b, int
 // A probability is the sum of two terms of the storage type: hi, and lo, what rounding to hi left.  Up to four rows (kBeside) use
 // half of the instruction's columns: the other half gets the same rows, lo is what they bring into P V, and end() adds the
 // two.  It is a kernel of its own: with both forms in one, one token over 32 x 40 caches takes 247 us and not 242.
-template <typename T, int D, int NC> struct Body16 {
+template <typename T, int D, int NC, bool Win> struct Body16 {
     static constexpr bool kBeside = NC == 4;
     static constexpr int CG = kBeside ? 1 : NC / 8, KS = D / 16, kTile = tile_slots<T, D>, kSub = kTile / warps_of<T> / 16;
     uint32_t q[CG][KS][2];
     float o[CG][KS][4], m[CG][2], l[CG][2];
-    int vis[CG][2];
+    int vis[CG][2], dead;
 
-    __device__ void begin(const AttendArgs &a, const Where &x, const SeqState &st, float *)
+    __device__ void begin(const AttendArgs &a, const Where &x, const SeqState &st, const Near &near, float *)
     {
+        dead = near.dead;
         const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3, rows = st.len * a.pv.G;
 #pragma unroll
         for (int g = 0; g < CG; ++g) {
@@ -198,10 +201,10 @@ template <typename T, int D, int NC> struct Body16 {
             }
         }
         // what lies behind the sequence may be anything: its keys are masked, its values made zero
-        if (j0 + kSub * 16 > used) {
+        if (j0 + kSub * 16 > used || (Win && j0 < dead && j0 + kSub * 16 > a.pv.sinks)) {
             for (int e = lane; e < kSub * 16 * (D / 8); e += 32) {
                 const int rr = e / (D / 8);
-                if (j0 + rr >= used) *reinterpret_cast<uint4 *>(V + tile_offset<kTile>(row0 + rr, e % (D / 8))) = make_uint4(0, 0, 0, 0);
+                if (j0 + rr >= used || (Win && j0 + rr < dead && j0 + rr >= a.pv.sinks)) *reinterpret_cast<uint4 *>(V + tile_offset<kTile>(row0 + rr, e % (D / 8))) = make_uint4(0, 0, 0, 0);
             }
             fence_async_smem();            // these writes come before the copy that next fills the stage
             __syncwarp();
@@ -216,7 +219,8 @@ template <typename T, int D, int NC> struct Body16 {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + u * 16 + r + (e >> 1) * 8;
-                    x[u][g][e] = j < vis[g][e & 1] ? x[u][g][e] * a.pv.sl2 : -INFINITY;
+                    const bool seen = j < vis[g][e & 1] && (!Win || j >= vis[g][e & 1] - a.pv.window || j < a.pv.sinks);
+                    x[u][g][e] = seen ? x[u][g][e] * a.pv.sl2 : -INFINITY;
                     beyond |= x[u][g][e] - m[g][e & 1] > kSlack<T>;       // also where m is still -inf; the difference is exact
                 }
                 if (logits) {
@@ -321,21 +325,21 @@ template <typename T, int D, int NC> struct Body16 {
 };
 
 // ---- a consumer warp on 32-bit storage: NC rows, all in use or zero ----------------------------------
-template <int D, int NC> struct Body32 {
+template <int D, int NC, bool Win> struct Body32 {
     static constexpr int DV = D / 32;                       // output elements per lane
     static constexpr int QP = D / 4, QS = QP + 4;           // a quarter of a query, and its distance in shared memory
     float o[NC][DV], m[NC], l[NC];
-    int rows, G, past;
+    int rows, G, past, dead;
     unsigned long long tokens;                              // token of row r in bits 4r .. 4r+3
 
     __device__ int seen_by(int r) const { return r < rows ? (int)(tokens >> (4 * r) & 15) + 1 : -(1 << 30); }
 
     // scratch: [NC][4][QS] queries, shared by the consumer warps, then [8][NC] probabilities of each warp
-    __device__ void begin(const AttendArgs &a, const Where &x, const SeqState &st, float *scratch)
+    __device__ void begin(const AttendArgs &a, const Where &x, const SeqState &st, const Near &near, float *scratch)
     {
         constexpr int kThreads = 32 * warps_of<float>;
         const int tid = threadIdx.x - 32;
-        rows = st.len * a.pv.G; G = a.pv.G; past = st.past;
+        rows = st.len * a.pv.G; G = a.pv.G; past = st.past; dead = near.dead;
         tokens = 0;
         for (int r = 0; r < rows; ++r) tokens |= (unsigned long long)(r / G) << (4 * r);
         named_barrier(1, kThreads);                         // the unit before has been worked off
@@ -384,7 +388,8 @@ template <int D, int NC> struct Body32 {
         for (int r = 0; r < NC; ++r) {
             acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], 8);
             acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], 16);
-            const bool seen = j < past + seen_by(r);
+            const int top = past + seen_by(r);
+            const bool seen = j < top && (!Win || j >= top - a.pv.window || j < a.pv.sinks);
             acc[r] = seen ? acc[r] * a.pv.sl2 : -INFINITY;
             if (logits && part == r % 4) logits[(size_t)j * NC + r] = acc[r];
             beyond |= acc[r] - m[r] > kSlack<float>;
@@ -412,6 +417,7 @@ template <int D, int NC> struct Body32 {
         const int n = min(8, used - j0);                    // values behind the sequence are not touched
 #pragma unroll 4
         for (int x = 0; x < n; ++x) {
+            if (Win && j0 + x < dead && j0 + x >= a.pv.sinks) continue;
             float v[DV], p[NC];
             const uint8_t *src = V + tile_offset<tile_slots<float, D>>(row0 + x, lane * DV / 4) + (lane * DV % 4) * 4;
 #pragma unroll
@@ -441,9 +447,9 @@ template <int D, int NC> struct Body32 {
     }
 };
 
-template <typename T, int D, int NC> struct BodyOf { typedef Body16<T, D, NC> type; static constexpr size_t kScratch = 0; };
-template <int D, int NC> struct BodyOf<float, D, NC> {
-    typedef Body32<D, NC> type;
+template <typename T, int D, int NC, bool Win> struct BodyOf { typedef Body16<T, D, NC, Win> type; static constexpr size_t kScratch = 0; };
+template <int D, int NC, bool Win> struct BodyOf<float, D, NC, Win> {
+    typedef Body32<D, NC, Win> type;
     static constexpr size_t kScratch = (size_t)(NC * 4 * (D / 4 + 4) + warps_of<float> * 8 * NC) * sizeof(float);
 };
 
@@ -453,13 +459,13 @@ struct FewShared {
     int32_t prefix[A2SF_PAGED_MAX_SEQUENCES + 1];
 };
 
-template <typename T, int D, int NC>
+template <typename T, int D, int NC, bool Win>
 __global__ void __launch_bounds__(32 * (warps_of<T> + 1))
 paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ AttendArgs a, const __grid_constant__ FewWs ws, int NP)
 {
     using R = Ring<T, D>;
-    using Body = typename BodyOf<T, D, NC>::type;
+    using Body = typename BodyOf<T, D, NC, Win>::type;
     constexpr int kTile = R::kTile, kWarps = warps_of<T>, kSlots = kTile / kWarps;     // slots per warp and tile
     extern __shared__ uint8_t smem_raw[];
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -477,7 +483,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             prefetch_tmap(&map_v);
         }
         dependency_wait();
-        tile_prefix<kTile>(sh.prefix, pv);
+        tile_prefix<kTile, Win>(sh.prefix, pv);
     }
     if (warp != 0) dependency_wait();
     __syncthreads();
@@ -492,11 +498,12 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 
     if (warp == 0) {
         // ---- producer: lane i copies box i of the tile --------------------------------------------
-        const int box = min(pv.ps, kTile), boxes = kTile / box;
+        const int box = box_rows<Win>(pv, kTile), boxes = kTile / box;
         const uint64_t policy = policy_evict_first();     // read once: the logits are to stay in L2 instead
         int it = 0;
         for (long long w = w0; w < w1;) {
-            const SeqState st = seq_state(pv, x.b);
+            Near near;
+            const SeqState st = near_state<Win>(pv, x.b, near);
             const int used = st.past + st.len;
             const int32_t *table = pv.table + (size_t)x.b * pv.max_pages;
             for (; x.t < x.tiles && w < w1; ++x.t, ++w, ++it) {
@@ -504,7 +511,10 @@ paged_few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 const int slot = x.t * kTile + lane * box;
                 const int nbox = min(boxes, (used - x.t * kTile + box - 1) / box);
                 int row = 0;
-                if (lane < nbox) row = (int)pool_row(pv, page_for_read(pv, table, slot), x.h, slot);
+                if (lane < nbox) {
+                    const int real = real_slot<Win>(pv, near, slot);
+                    row = (int)pool_row(pv, page_for_read(pv, table, real), x.h, real);
+                }
                 int ok = 1;
                 if (lane == 0) {
                     if (it >= R::kStages) ok = mbar_wait(&sh.empty[s], ((it / R::kStages) & 1) ^ 1, abort_flag) ? 1 : 0;
@@ -538,11 +548,12 @@ drained:
         Body body;
         int it = 0;
         for (long long w = w0; w < w1;) {
-            const SeqState st = seq_state(pv, x.b);
+            Near near;
+            const SeqState st = near_state<Win>(pv, x.b, near);
             const int used = st.past + st.len;
             const int unit = x.b * pv.H + x.h;
-            float *logits = a.scores ? ws.logits + (size_t)unit * ws.slots * NP : nullptr;
-            body.begin(a, x, st, scratch);
+            float *logits = !Win && a.scores ? ws.logits + (size_t)unit * ws.slots * NP : nullptr;
+            body.begin(a, x, st, near, scratch);
             for (; x.t < x.tiles && w < w1; ++x.t, ++w, ++it) {
                 const int s = it % R::kStages;
                 if (!*abort_flag && !mbar_wait(&sh.full[s], (it / R::kStages) & 1, abort_flag)) *pv.status = A2SF_ERR_TIMEOUT;
@@ -575,13 +586,13 @@ struct WholeShared {
     float row_m[kFewRows], row_inv[kFewRows], row_c[kFewRows];
 };
 
-template <typename T, int D, int NC>
+template <typename T, int D, int NC, bool Win>
 __global__ void __launch_bounds__(32 * (warps_of<T> + 1))
 paged_few_whole_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                        const __grid_constant__ AttendArgs a, int NP, int slots)
 {
     using R = Ring<T, D>;
-    using Body = typename BodyOf<T, D, NC>::type;
+    using Body = typename BodyOf<T, D, NC, Win>::type;
     constexpr int kTile = R::kTile, kWarps = warps_of<T>, kSlots = kTile / kWarps, kConsumers = 32 * kWarps;
     constexpr int kPer = kWholeTiles * kTile / kConsumers;          // slots of a thread whose old scores are asked for early
     extern __shared__ uint8_t smem_raw[];
@@ -602,11 +613,12 @@ paged_few_whole_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     dependents_may_start();
 
     if (warp == 0) {
-        const int box = min(pv.ps, kTile), boxes = kTile / box;
+        const int box = box_rows<Win>(pv, kTile), boxes = kTile / box;
         int it = 0;
         for (int u = blockIdx.x; u < units; u += gridDim.x) {
             const int b = u / pv.H, h = u - b * pv.H;
-            const SeqState st = seq_state(pv, b);
+            Near near;
+            const SeqState st = near_state<Win>(pv, b, near);
             const int used = st.len > 0 ? st.past + st.len : 0;
             const int32_t *table = pv.table + (size_t)b * pv.max_pages;
             for (int t = 0; t * kTile < used; ++t, ++it) {
@@ -614,7 +626,10 @@ paged_few_whole_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 const int slot = t * kTile + lane * box;
                 const int nbox = min(boxes, (used - t * kTile + box - 1) / box);
                 int row = 0;
-                if (lane < nbox) row = (int)pool_row(pv, page_for_read(pv, table, slot), h, slot);
+                if (lane < nbox) {
+                    const int real = real_slot<Win>(pv, near, slot);
+                    row = (int)pool_row(pv, page_for_read(pv, table, real), h, real);
+                }
                 int ok = 1;
                 if (lane == 0) {
                     if (it >= R::kStages) ok = mbar_wait(&sh.empty[s], ((it / R::kStages) & 1) ^ 1, abort_flag) ? 1 : 0;
@@ -643,16 +658,18 @@ drained:
     }
     const int cw = warp - 1, ct = threadIdx.x - 32;
     float *scratch = reinterpret_cast<float *>(ring + (size_t)R::kStages * 2 * R::kTileBytes);
-    float2 *ml = reinterpret_cast<float2 *>(reinterpret_cast<uint8_t *>(scratch) + BodyOf<T, D, NC>::kScratch);
+    const bool scores = !Win && a.scores;
+    float2 *ml = reinterpret_cast<float2 *>(reinterpret_cast<uint8_t *>(scratch) + BodyOf<T, D, NC, Win>::kScratch);
     float *o = reinterpret_cast<float *>(ml + kWarps * NP);
-    float *logits = a.scores ? o + (size_t)kWarps * NP * D : nullptr;
+    float *logits = scores ? o + (size_t)kWarps * NP * D : nullptr;
     Body body;
     int it = 0;
     for (int u = blockIdx.x; u < units; u += gridDim.x) {
         Where x = {};
         x.b = u / pv.H;
         x.h = u - x.b * pv.H;
-        const SeqState st = seq_state(pv, x.b);
+        Near near;
+        const SeqState st = near_state<Win>(pv, x.b, near);
         if (st.len <= 0) continue;
         const int used = st.past + st.len, rows = st.len * pv.G;
         const int32_t *table = pv.table + (size_t)x.b * pv.max_pages;
@@ -662,7 +679,7 @@ drained:
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             const int j = ct + e * kConsumers;
-            row[e] = a.scores && j < used ? page_for_write(pv, table, j) : -1;
+            row[e] = scores && j < used ? page_for_write(pv, table, j) : -1;
         }
 #pragma unroll
         for (int e = 0; e < kPer; ++e)
@@ -670,7 +687,7 @@ drained:
                 row[e] = (int)pool_row(pv, row[e], x.h, ct + e * kConsumers);
                 old[e] = pv.scores[row[e]];
             }
-        body.begin(a, x, st, scratch);
+        body.begin(a, x, st, near, scratch);
         for (int t = 0; t * kTile < used; ++t, ++it) {
             const int s = it % R::kStages;
             if (!*abort_flag && !mbar_wait(&sh.full[s], (it / R::kStages) & 1, abort_flag)) *pv.status = A2SF_ERR_TIMEOUT;
@@ -709,7 +726,7 @@ drained:
 #pragma unroll
         for (int e = 0; e < kPer; ++e)
             if (row[e] >= 0) pv.scores[row[e]] = fmaf(old[e], decay, gain(ct + e * kConsumers));
-        if (a.scores)
+        if (scores)
             for (int j = ct + kPer * kConsumers; j < used; j += kConsumers) {
                 const int page = page_for_write(pv, table, j);
                 if (page < 0) continue;
@@ -903,7 +920,7 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
 }
 
 size_t pad(size_t x) { return (x + 255) / 256 * 256; }
-int padded_slots(const PagedView &pv) { return ((pv.max_pages << pv.ps_shift) + 127) / 128 * 128; }       // of either tile
+int padded_slots(const PagedView &pv) { return (near_capacity(pv, pv.c) + 127) / 128 * 128; }       // of either tile
 
 FewWs carve(int dtype, const PagedView &pv, void *ws, size_t *bytes)
 {
@@ -915,7 +932,7 @@ FewWs carve(int dtype, const PagedView &pv, void *ws, size_t *bytes)
     char *base = static_cast<char *>(ws);
     w.slots = padded_slots(pv);
     w.segs = (int)segs;
-    w.logits = reinterpret_cast<float *>(base + off); off += pad(U * w.slots * NP * 4);
+    w.logits = reinterpret_cast<float *>(base + off); off += pv.window ? 0 : pad(U * w.slots * NP * 4);
     w.ml = reinterpret_cast<float2 *>(base + off); off += pad(segs * NP * 8);
     w.o = reinterpret_cast<float *>(base + off); off += pad(segs * NP * pv.d * 4);
     w.prefix = reinterpret_cast<int32_t *>(base + off); off += pad(((size_t)pv.B + 1) * 4);
@@ -924,41 +941,41 @@ FewWs carve(int dtype, const PagedView &pv, void *ws, size_t *bytes)
 }
 
 // Shared memory of the whole-unit kernel, or 0 where it does not serve: longer caches, or more rows than fit.
-template <typename T, int D, int NC> size_t whole_smem(const PagedView &pv)
+template <typename T, int D, int NC, bool Win> size_t whole_smem(const PagedView &pv)
 {
     using R = Ring<T, D>;
-    const int slots = ((pv.max_pages << pv.ps_shift) + R::kTile - 1) / R::kTile * R::kTile;
-    const size_t smem = R::kBytes + BodyOf<T, D, NC>::kScratch + whole_bytes(warps_of<T>, D, rows_padded(pv.c * pv.G), slots);
+    const int slots = (near_capacity(pv, pv.c) + R::kTile - 1) / R::kTile * R::kTile;
+    const size_t smem = R::kBytes + BodyOf<T, D, NC, Win>::kScratch + whole_bytes(warps_of<T>, D, rows_padded(pv.c * pv.G), Win ? 0 : slots);
     const int most = pv.B * pv.H >= kSms ? kWholeTilesMany : kWholeTiles;
     return slots <= most * R::kTile && smem + sizeof(WholeShared) <= 227 * 1024 ? smem : 0;
 }
 
-template <typename T, int D, int NC>
+template <typename T, int D, int NC, bool Win>
 cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
 {
     using R = Ring<T, D>;
-    constexpr size_t smem = R::kBytes + BodyOf<T, D, NC>::kScratch;
-    cudaError_t e = allow_dynamic_smem<paged_few_kernel<T, D, NC>>(smem);
+    constexpr size_t smem = R::kBytes + BodyOf<T, D, NC, Win>::kScratch;
+    cudaError_t e = allow_dynamic_smem<paged_few_kernel<T, D, NC, Win>>(smem);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
-    const int box = a.pv.ps < R::kTile ? a.pv.ps : R::kTile;
+    const int row = Win ? a.pv.grain : a.pv.ps, box = row < R::kTile ? row : R::kTile;
     if (!make_pool_map(&mk, dtype, a.pv.k, a.pv, box) || !make_pool_map(&mv, dtype, a.pv.v, a.pv, box)) return cudaErrorInvalidValue;
     const int NP = rows_padded(a.pv.c * a.pv.G);
-    if (const size_t whole = whole_smem<T, D, NC>(a.pv)) {
-        if ((e = allow_dynamic_smem<paged_few_whole_kernel<T, D, NC>>(whole)) != cudaSuccess) return e;
+    if (const size_t whole = whole_smem<T, D, NC, Win>(a.pv)) {
+        if ((e = allow_dynamic_smem<paged_few_whole_kernel<T, D, NC, Win>>(whole)) != cudaSuccess) return e;
         const long long resident = device_sm_count() * (2 * (whole + sizeof(WholeShared) + 1024) <= 228 * 1024 ? 2 : 1), units = (long long)a.pv.B * a.pv.H;
-        const int slots = ((a.pv.max_pages << a.pv.ps_shift) + R::kTile - 1) / R::kTile * R::kTile;
-        e = launch_chained(paged_few_whole_kernel<T, D, NC>, (unsigned)(units < resident ? units : resident), 32 * (warps_of<T> + 1), whole, s, mk, mv, a, NP, slots);
+        const int slots = (near_capacity(a.pv, a.pv.c) + R::kTile - 1) / R::kTile * R::kTile;
+        e = launch_chained(paged_few_whole_kernel<T, D, NC, Win>, (unsigned)(units < resident ? units : resident), 32 * (warps_of<T> + 1), whole, s, mk, mv, a, NP, slots);
         if (e == cudaSuccess) count_launch();
         return e;
     }
     const FewWs ws = carve(dtype, a.pv, a.ws, nullptr);
     const int ctas = device_sm_count() * (2 * (smem + sizeof(FewShared) + 1024) <= 228 * 1024 ? 2 : 1);   // what is resident
     if (ctas < 1 || ctas > 512) return cudaErrorInvalidValue;
-    if ((e = launch_chained(paged_few_kernel<T, D, NC>, ctas, 32 * (warps_of<T> + 1), smem, s, mk, mv, a, ws, NP)) != cudaSuccess) return e;
+    if ((e = launch_chained(paged_few_kernel<T, D, NC, Win>, ctas, 32 * (warps_of<T> + 1), smem, s, mk, mv, a, ws, NP)) != cudaSuccess) return e;
     count_launch();
     // blocks per unit: enough for the rows and the slots, as far as that fills the device
-    const int cap = a.pv.max_pages << a.pv.ps_shift;
+    const int cap = Win ? 1 : a.pv.max_pages << a.pv.ps_shift;
     const long long units = (long long)a.pv.B * a.pv.H;
     const long long want = (long long)finish_ctas(NP) * device_sm_count() / units;
     int blocks = (cap + kFinishThreads - 1) / kFinishThreads;
@@ -979,20 +996,31 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     return e;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool Win>
 cudaError_t launch_d(int dtype, const AttendArgs &a, cudaStream_t s)
 {
     const int rows = a.pv.c * a.pv.G;
     if constexpr (sizeof(T) == 4) {
         switch (rows_padded(rows)) {
-        case 1: return launch_nc<T, D, 1>(dtype, a, s);
-        case 2: return launch_nc<T, D, 2>(dtype, a, s);
-        case 4: return launch_nc<T, D, 4>(dtype, a, s);
-        case 8: return launch_nc<T, D, 8>(dtype, a, s);
-        default: return launch_nc<T, D, 16>(dtype, a, s);
+        case 1: return launch_nc<T, D, 1, Win>(dtype, a, s);
+        case 2: return launch_nc<T, D, 2, Win>(dtype, a, s);
+        case 4: return launch_nc<T, D, 4, Win>(dtype, a, s);
+        case 8: return launch_nc<T, D, 8, Win>(dtype, a, s);
+        default: return launch_nc<T, D, 16, Win>(dtype, a, s);
         }
     } else {
-        return rows <= 4 ? launch_nc<T, D, 4>(dtype, a, s) : rows <= 8 ? launch_nc<T, D, 8>(dtype, a, s) : launch_nc<T, D, 16>(dtype, a, s);
+        return rows <= 4 ? launch_nc<T, D, 4, Win>(dtype, a, s) : rows <= 8 ? launch_nc<T, D, 8, Win>(dtype, a, s) : launch_nc<T, D, 16, Win>(dtype, a, s);
+    }
+}
+
+template <bool Win>
+cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
+{
+    const bool wide = a.pv.d == 128;
+    switch (dtype) {
+    case A2SF_F32: return wide ? launch_d<float, 128, Win>(dtype, a, s) : launch_d<float, 64, Win>(dtype, a, s);
+    case A2SF_BF16: return wide ? launch_d<__nv_bfloat16, 128, Win>(dtype, a, s) : launch_d<__nv_bfloat16, 64, Win>(dtype, a, s);
+    default: return wide ? launch_d<__half, 128, Win>(dtype, a, s) : launch_d<__half, 64, Win>(dtype, a, s);
     }
 }
 
@@ -1007,12 +1035,7 @@ size_t attend_few_ws_bytes(int dtype, const PagedView &pv)
 
 cudaError_t launch_attend_few(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    const bool wide = a.pv.d == 128;
-    switch (dtype) {
-    case A2SF_F32: return wide ? launch_d<float, 128>(dtype, a, s) : launch_d<float, 64>(dtype, a, s);
-    case A2SF_BF16: return wide ? launch_d<__nv_bfloat16, 128>(dtype, a, s) : launch_d<__nv_bfloat16, 64>(dtype, a, s);
-    default: return wide ? launch_d<__half, 128>(dtype, a, s) : launch_d<__half, 64>(dtype, a, s);
-    }
+    return a.pv.window ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
 }
 
 }  // namespace a2sf

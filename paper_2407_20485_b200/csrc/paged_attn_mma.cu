@@ -19,6 +19,8 @@
 // 16 bits: products on mma.sync m16n8k16, operands by ldmatrix; P is the sum of two terms of the storage type, off by the square
 // of half a step (36 heads, 302 tokens, d = 64: 18.0 us with one term, 18.6 with two).
 //
+// Windowed (Win): a row tile walks over the near slots of its rows (see Near); attn and merge alone.
+//
 // The next tile's keys are on their way (16-byte asynchronous copies) while the tile before is finished, values while
 // logits are made (16 bits: a whole tile ahead, with two buffers); a warp looks up the pages of its rows all at once (one after the other: 262 us where it takes 164).
 // Bound by the instructions around the products -- four to split an operand -- and, in small calls, by the latency of a
@@ -59,8 +61,9 @@ struct MmaWs {
 };
 
 struct Unit {
-    int b, h, past, len, rows;   // rows = len * G
+    int b, h, past, len, rows;   // rows = len * G; past in near slots
     const int32_t *table;
+    Near near;
 };
 
 __device__ __forceinline__ Unit make_unit(const PagedView &pv, int u)
@@ -71,6 +74,7 @@ __device__ __forceinline__ Unit make_unit(const PagedView &pv, int u)
     const SeqState st = seq_state(pv, x.b);
     x.past = st.past; x.len = st.len; x.rows = st.len * pv.G;
     x.table = pv.table + (size_t)x.b * pv.max_pages;
+    x.near = near_slots<false>(pv, st.past, 0);
     return x;
 }
 
@@ -101,16 +105,16 @@ __device__ __forceinline__ void copy_queries(T *dst, const AttendArgs &a, const 
     }
 }
 
-// slots j0 .. j0+N-1 of the unit's keys or values; slots from `limit` on become zero and are not read.  A warp's lanes look
-// up the rows that it copies, all at once.
-template <typename T, int D, int N>
+// slots j0 .. j0+N-1 of the unit's keys or values; slots from `limit` on, and those that no row sees, become zero and are not
+// read.  A warp's lanes look up the rows that it copies, all at once.
+template <typename T, int D, int N, bool Win = false>
 __device__ __forceinline__ void copy_slots(T *dst, int ld, const PagedView &pv, const Unit &u, const char *pool, int j0, int limit)
 {
     constexpr int VEC = 16 / sizeof(T), CH = D / VEC, kAt = 32 / CH, kPer = N / (kThreads / 32);      // rows of a warp's copy, rows of a warp
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ch = lane % CH, sub = lane / CH;
     const int mine = j0 + warp * kPer + lane;
-    const bool live = lane < kPer && mine < limit;
-    const int row = live ? (int)pool_row(pv, page_for_read(pv, u.table, mine), u.h, mine) : -1;
+    const bool live = lane < kPer && mine < limit && !(Win && mine < u.near.dead && mine >= pv.sinks);
+    const int real = real_slot<Win>(pv, u.near, mine), row = live ? (int)pool_row(pv, page_for_read(pv, u.table, real), u.h, real) : -1;
 #pragma unroll
     for (int x = 0; x < kPer; x += kAt) {
         const int from = __shfl_sync(0xffffffffu, row, x + sub);
@@ -350,11 +354,11 @@ __device__ __forceinline__ void store_lse(const AttendArgs &a, const MmaWs &ws, 
 {
     const int tok = r / a.pv.G, g = r - tok * a.pv.G;
     const size_t unit = (size_t)u.b * a.pv.H + u.h;
-    ws.lse2[unit * a.pv.c * a.pv.G + r] = z;
+    if (ws.lse2) ws.lse2[unit * a.pv.c * a.pv.G + r] = z;
     if (a.lse) a.lse[(unit * a.pv.G + g) * a.pv.c + tok] = z * 0.6931471805599453f;
 }
 
-template <typename T, int D, int R>
+template <typename T, int D, int R, bool Win>
 __global__ void __launch_bounds__(kThreads)
 paged_attn_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ MmaWs ws, int row_tiles)
 {
@@ -367,18 +371,22 @@ paged_attn_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
     const int piece = blockIdx.x % ws.pieces, work = blockIdx.x / ws.pieces;
     // the tiles that see most slots first, of all units
     const int units = a.pv.B * a.pv.H, tile = work / units;
-    const Unit u = make_unit(a.pv, work - tile * units);
+    Unit u = make_unit(a.pv, work - tile * units);
     const int r0 = (row_tiles - 1 - tile) * kRows;
     if (r0 >= u.rows) return;
+    if (Win) {
+        u.near = near_slots<Win>(a.pv, u.past, r0 / G);
+        u.past = u.near.past;
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int last_row = min(r0 + kRows, u.rows) - 1;
     const int limit = u.past + last_row / G + 1;         // slots that the last row sees
     const int tiles = (limit + kTile - 1) / kTile;
     const int t0 = (int)((long long)tiles * piece / ws.pieces), t1 = (int)((long long)tiles * (piece + 1) / ws.pieces);
     copy_queries<T, D, kRows>(Q, a, u, r0);
-    if (t0 < t1) copy_slots<T, D, kTile>(K, LD, a.pv, u, a.pv.k, t0 * kTile, limit);
+    if (t0 < t1) copy_slots<T, D, kTile, Win>(K, LD, a.pv, u, a.pv.k, t0 * kTile, limit);
     copies_commit();
-    if (t0 < t1) copy_slots<T, D, kTile>(V, LV, a.pv, u, a.pv.v, t0 * kTile, limit);
+    if (t0 < t1) copy_slots<T, D, kTile, Win>(V, LV, a.pv, u, a.pv.v, t0 * kTile, limit);
     copies_commit();
 
     const int wr = R == 4 ? 16 * warp : 0, wk = R == 4 ? 0 : 16 * warp;      // the warp's rows and keys of a tile
@@ -397,11 +405,11 @@ paged_attn_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
         __syncthreads();
         const int buf = kBufs == 2 ? (t - t0) & 1 : 0, next = kBufs == 2 ? buf ^ 1 : 0;
         auto next_keys = [&] {
-            if (t + 1 < t1) copy_slots<T, D, kTile>(K + next * kTile * LD, LD, a.pv, u, a.pv.k, j0 + kTile, limit);
+            if (t + 1 < t1) copy_slots<T, D, kTile, Win>(K + next * kTile * LD, LD, a.pv, u, a.pv.k, j0 + kTile, limit);
             copies_commit();
         };
         auto next_values = [&] {
-            if (t + 1 < t1) copy_slots<T, D, kTile>(V + next * kTile * LV, LV, a.pv, u, a.pv.v, j0 + kTile, limit);
+            if (t + 1 < t1) copy_slots<T, D, kTile, Win>(V + next * kTile * LV, LV, a.pv, u, a.pv.v, j0 + kTile, limit);
             copies_commit();
         };
         if (kBufs == 2) next_keys();
@@ -416,7 +424,8 @@ paged_attn_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     float &v = s[n][2 * x + e];
-                    v = j0 + wk + n * 8 + 2 * c + e < vis[x] ? v * a.pv.sl2 : -INFINITY;
+                    const int j = j0 + wk + n * 8 + 2 * c + e;
+                    v = j < vis[x] && (!Win || j >= vis[x] - a.pv.window || j < a.pv.sinks) ? v * a.pv.sl2 : -INFINITY;
                     mx = fmaxf(mx, v);
                 }
             const float mn = fmaxf(m[x], reference<kBelow<T>>(quad_max(mx)));
@@ -636,7 +645,7 @@ struct Shape {
 Shape shape_of(int dtype, const PagedView &pv)
 {
     Shape s;
-    const long long units = (long long)pv.B * pv.H, rows = (long long)pv.c * pv.G, cap = (long long)pv.max_pages << pv.ps_shift;
+    const long long units = (long long)pv.B * pv.H, rows = (long long)pv.c * pv.G, cap = near_capacity(pv, std::min(pv.c, 64));      // of a row tile
     const long long most = std::max(1ll, (cap + kTile - 1) / kTile / (dtype == A2SF_F32 ? 2 : 4)), tiles = units * ((rows + 63) / 64);
     s.large = tiles * most >= 4 * kSms;
     s.row_tiles = s.large ? (rows + 63) / 64 : (rows + 15) / 16;
@@ -654,21 +663,21 @@ MmaWs carve(int dtype, const PagedView &pv, void *mem, size_t *bytes)
     char *base = static_cast<char *>(mem);
     size_t off = 0;
     const size_t parts = w.pieces > 1 ? rows * w.pieces : 0;
-    w.lse2 = reinterpret_cast<float *>(base + off); off += pad(rows * 4);
+    w.lse2 = pv.window ? nullptr : reinterpret_cast<float *>(base + off); off += pv.window ? 0 : pad(rows * 4);     // for the scores
     w.ml = reinterpret_cast<float2 *>(base + off); off += pad(parts * 8);
     w.o = reinterpret_cast<float *>(base + off); off += pad(parts * pv.d * 4);
     if (bytes) *bytes = off;
     return w;
 }
 
-template <typename T, int D, int R>
+template <typename T, int D, int R, bool Win>
 cudaError_t launch_attn(const AttendArgs &a, const MmaWs &ws, long long row_tiles, cudaStream_t s)
 {
     const long long grid = (long long)a.pv.B * a.pv.H * row_tiles * ws.pieces;
     if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
     constexpr size_t smem = Lay<T, D>::attn(16 * R);
-    cudaError_t e = allow_dynamic_smem<paged_attn_mma_kernel<T, D, R>>(smem);
-    if (e == cudaSuccess) e = launch_chained(paged_attn_mma_kernel<T, D, R>, (unsigned)grid, kThreads, smem, s, a, ws, (int)row_tiles);
+    cudaError_t e = allow_dynamic_smem<paged_attn_mma_kernel<T, D, R, Win>>(smem);
+    if (e == cudaSuccess) e = launch_chained(paged_attn_mma_kernel<T, D, R, Win>, (unsigned)grid, kThreads, smem, s, a, ws, (int)row_tiles);
     if (e == cudaSuccess) count_launch();
     return e;
 }
@@ -684,12 +693,12 @@ cudaError_t launch_score(const AttendArgs &a, const MmaWs &ws, long long slot_ti
     return e;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool Win>
 cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
 {
     const Shape sh = shape_of(dtype, a.pv);
     const MmaWs ws = carve(dtype, a.pv, a.ws, nullptr);
-    cudaError_t e = sh.large ? launch_attn<T, D, 4>(a, ws, sh.row_tiles, s) : launch_attn<T, D, 1>(a, ws, sh.row_tiles, s);
+    cudaError_t e = sh.large ? launch_attn<T, D, 4, Win>(a, ws, sh.row_tiles, s) : launch_attn<T, D, 1, Win>(a, ws, sh.row_tiles, s);
     if (e != cudaSuccess) return e;
     if (ws.pieces > 1) {
         const long long rows = (long long)a.pv.B * a.pv.H * a.pv.c * a.pv.G, grid = (rows + 3) / 4;
@@ -697,8 +706,19 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
         if (e != cudaSuccess) return e;
         count_launch();
     }
-    if (!a.scores) return cudaSuccess;
+    if (Win || !a.scores) return cudaSuccess;
     return sh.large_score ? launch_score<T, D, 4>(a, ws, sh.slot_tiles, s) : launch_score<T, D, 1>(a, ws, sh.slot_tiles, s);
+}
+
+template <bool Win>
+cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
+{
+    const bool wide = a.pv.d == 128;
+    switch (dtype) {
+    case A2SF_F32: return wide ? launch<float, 128, Win>(dtype, a, s) : launch<float, 64, Win>(dtype, a, s);
+    case A2SF_BF16: return wide ? launch<__nv_bfloat16, 128, Win>(dtype, a, s) : launch<__nv_bfloat16, 64, Win>(dtype, a, s);
+    default: return wide ? launch<__half, 128, Win>(dtype, a, s) : launch<__half, 64, Win>(dtype, a, s);
+    }
 }
 
 }  // namespace
@@ -712,12 +732,7 @@ size_t attend_mma_ws_bytes(int dtype, const PagedView &pv)
 
 cudaError_t launch_attend_mma(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    const bool wide = a.pv.d == 128;
-    switch (dtype) {
-    case A2SF_F32: return wide ? launch<float, 128>(dtype, a, s) : launch<float, 64>(dtype, a, s);
-    case A2SF_BF16: return wide ? launch<__nv_bfloat16, 128>(dtype, a, s) : launch<__nv_bfloat16, 64>(dtype, a, s);
-    default: return wide ? launch<__half, 128>(dtype, a, s) : launch<__half, 64>(dtype, a, s);
-    }
+    return a.pv.window ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
 }
 
 }  // namespace a2sf

@@ -21,6 +21,10 @@
 //           830 tokens).  The (key tile, row tile) pairs of the call are one list, cut into equal shares; a
 //           key tile that a cut goes through is summed in parts, which the join kernel adds in order.
 //
+// Windowed (Win): an item walks over the near slots of its pair's rows (see Near): the sinks, and from the window of its first row
+// on; attn and merge alone.  All items of a call then are about as long as the window, so a plan is made only where they are to
+// be cut.  A row may see nothing of its item's first tiles; its reference is unset, +inf, until it does.
+//
 // What binds: one exponential per logit in attn and one in score, 16 a clock and SM, and 128 x 128 x d x 4
 // operations of a tile at 8192 a clock, 1024 clocks each for d = 128.  They overlap in part: the special-function unit runs at
 // 45 % of its rate in attn and at 53 % in score, the tensor pipe at 41 % and 21 %, and neither is full (a chunk of 2048 tokens
@@ -63,7 +67,7 @@ constexpr int kScoreCtas = 2 * kSms;
 struct Item {                                // of one head; all heads have the same
     int b, pair, t0, t1;                     // key tiles t0 .. t1-1
     int part;                                // -1: whole; else index of its partial result
-    int past, len, pad;                      // of its sequence
+    int past, len, skip;                     // of its sequence, in near slots of the pair, and what they leave out
 };
 struct Merge {
     int b, pair, n, part;                    // partial results part .. part + n - 1
@@ -90,9 +94,19 @@ __device__ __forceinline__ int pair_key_tiles(const SeqState &st, int pair, int 
     return (st.past + min((pair + 1) * pair_tokens, st.len) + kBlk - 1) / kBlk;
 }
 
+// past of the pair's rows in near slots
+template <bool Win> __device__ __forceinline__ SeqState pair_state(const PagedView &pv, SeqState st, int pair, int pair_tokens, int &skip)
+{
+    const Near near = near_slots<Win>(pv, st.past, pair * pair_tokens);
+    st.past = near.past;
+    skip = near.skip;
+    return st;
+}
+
 // The item list.  Cutting items into pieces of p tiles makes sum(ceil(T / p)) of them; CTAs take them in
 // rounds, so a call takes about  max(ceil(pieces / SMs) * (mean length + kItemCost), longest + kItemCost):
 // lengths between a quarter and one and a half of an SM's even share are tried, and no cut at all.
+template <bool Win>
 __global__ void __launch_bounds__(kPlanThreads)
 paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ TcWs ws)
 {
@@ -109,7 +123,8 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
     __syncthreads();
     auto measure = [&](int x) -> int {
         const int b = x / ws.pairs, p = x - b * ws.pairs;
-        const SeqState st = seqs[b];
+        int skip;
+        const SeqState st = pair_state<Win>(pv, seqs[b], p, ws.pair_tokens, skip);
         return p * ws.pair_tokens < st.len ? pair_key_tiles(st, p, ws.pair_tokens) : 0;
     };
     auto item_tiles = [&](int x) -> int { return x < kPlanCache ? tiles[x] : measure(x); };
@@ -187,7 +202,8 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
         const int t = item_tiles(x);
         if (!t) continue;
         const int n = (t - 1) / piece + 1, b = x / ws.pairs, p = x - b * ws.pairs;
-        const SeqState st = seqs[b];
+        int skip;
+        const SeqState st = pair_state<Win>(pv, seqs[b], p, ws.pair_tokens, skip);
         int at = atomicAdd(&level[level_of((t + n - 1) / n)], n);
         int part = -1;
         if (n > 1) {
@@ -197,7 +213,7 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
         }
         for (int s = 0; s < n; ++s, ++at)
             if (A2SF_IN_RANGE(at, ws.max_items, kDbgPagedTc) && at < ws.max_items)
-                ws.items[at] = Item{b, p, (int)((long long)t * s / n), (int)((long long)t * (s + 1) / n), n > 1 ? part + s : -1, st.past, st.len, 0};
+                ws.items[at] = Item{b, p, (int)((long long)t * s / n), (int)((long long)t * (s + 1) / n), n > 1 ? part + s : -1, st.past, st.len, skip};
     }
     __syncthreads();
     if (tid == 0) ws.head->merges = n_merges;
@@ -290,10 +306,10 @@ __device__ __forceinline__ void issue_qk(uint32_t d_tmem, uint64_t a_desc, uint6
 struct PageTile {
     int box, boxes;
 };
-__device__ __forceinline__ PageTile page_tile(const PagedView &pv, int t, int used)
+template <bool Win = false> __device__ __forceinline__ PageTile page_tile(const PagedView &pv, int t, int used)
 {
     PageTile p;
-    p.box = min(pv.ps, kBlk);
+    p.box = box_rows<Win>(pv, kBlk);
     p.boxes = min(kBlk / p.box, (used - t * kBlk + p.box - 1) / p.box);
     return p;
 }
@@ -336,7 +352,7 @@ struct AttnShared {
 template <int D> constexpr size_t attn_smem() { return (size_t)Tile<D>::kBytes * (2 + kKStages + kVStages) + sizeof(AttnShared); }
 static_assert(attn_smem<128>() <= 227 * 1024, "attention shared memory");
 
-template <typename T, int D>
+template <typename T, int D, bool Win>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendArgs a, const __grid_constant__ TcWs ws)
@@ -396,7 +412,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     auto dealt = [&](int round) { return round * (int)gridDim.x + (round & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
     // what an item means to every role
     struct Job {
-        int b, h, i0, tokens, t0, nt, ntA, ntB, past, used, part;
+        int b, h, i0, tokens, t0, nt, ntA, ntB, past, used, part, skip;
     };
     auto job = [&](int unit) -> Job {
         Job j;
@@ -408,7 +424,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             it.b = rest / pv.H;
             j.h = rest - it.b * pv.H;
             it.pair = ws.pairs - 1 - back;
-            const SeqState st = seq_state(pv, it.b);
+            const SeqState st = pair_state<Win>(pv, seq_state(pv, it.b), it.pair, ws.pair_tokens, it.skip);
             it.past = st.past; it.len = st.len; it.part = -1;
             it.t0 = 0;
             it.t1 = it.pair * ws.pair_tokens < st.len ? pair_key_tiles(st, it.pair, ws.pair_tokens) : 0;
@@ -420,7 +436,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             j.h = rest / n_items;
         }
         j.b = it.b;
-        j.past = it.past; j.used = it.past + it.len;
+        j.past = it.past; j.used = it.past + it.len; j.skip = it.skip;
         j.i0 = it.pair * ws.pair_tokens;
         j.tokens = min(ws.pair_tokens, it.len - j.i0);
         j.t0 = it.t0;
@@ -455,10 +471,13 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             ++n;
             for (int t = 0; t < j.nt; ++t, ++kt) {
                 const int tile = j.t0 + t, ks = kt % kKStages, vs = kt % kVStages;
-                const PageTile p = page_tile(pv, tile, j.used);
+                const PageTile p = page_tile<Win>(pv, tile, j.used);
                 const int slot = tile * kBlk + lane * p.box;
                 int row = 0;
-                if (lane < p.boxes) row = (int)pool_row(pv, page_for_read(pv, table, slot), j.h, slot);
+                if (lane < p.boxes) {
+                    const int real = real_slot<Win>(pv, Near{0, j.skip, 0}, slot);
+                    row = (int)pool_row(pv, page_for_read(pv, table, real), j.h, real);
+                }
                 const uint32_t bytes = (uint32_t)(p.boxes * p.box * 128 * Tile<D>::kHalves);
                 ok = 1;
                 if (lane == 0) {
@@ -536,6 +555,19 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     fence_async_smem();
                     __syncwarp();
                 }
+                if constexpr (Win) {
+                    // nor what lies between the sinks and the window of the pair's first row
+                    const int tile0 = (j.t0 + t) * kBlk, from = max(pv.sinks - tile0, 0), to = min(max(j.past + j.i0 + 1 - pv.window, 0) - tile0, kBlk);
+                    if (from < to) {
+                        uint8_t *V = Vs + vs * kTileBytes;
+                        for (int x = lane; x < Tile<D>::kHalves * (to - from) * 8; x += 32) {
+                            const int piece = x & 7, row = from + (x >> 3) % (to - from), half = (x >> 3) / (to - from);
+                            *reinterpret_cast<uint4 *>(V + half * Tile<D>::kHalfBytes + row * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                    }
+                }
 #pragma unroll
                 for (int X = 0; X < 2; ++X) {
                     if (t >= ntX[X]) continue;
@@ -585,7 +617,19 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 tmem_ld32(sp + 32, v[1]);
                 tmem_wait_ld();
                 const int tile0 = (j.t0 + t) * kBlk;
-                if (tile0 + kBlk > j.past + first_token + 1) {
+                if constexpr (Win) {
+                    // the window of the stream's last row begins behind the tile's first slot, or some row ends before its last
+                    const int first_top = j.past + first_token + 1, last_top = min(first_top + tile_tokens - 1, j.used);
+                    if (tile0 + kBlk > first_top || tile0 < last_top - pv.window) {
+                        const int top = min(first_top + r_tok, j.used) - tile0 - half * 64;
+                        const int low = top - pv.window, sinks = min(top, pv.sinks - tile0 - half * 64);
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                if (c * 32 + x >= sinks && (c * 32 + x >= top || c * 32 + x < low)) v[c][x] = 0xff800000u;
+                    }
+                } else if (tile0 + kBlk > j.past + first_token + 1) {
                     // some row of the tile does not see all of it: a masked logit becomes -inf
                     const int vis = min(j.past + first_token + r_tok + 1, j.used) - tile0 - half * 64;
 #pragma unroll
@@ -620,7 +664,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 bool exact = (t == 0);
                 if (!exact) {
                     rowsum = write_p(-m_x);
-                    const bool bad = !(rowsum <= kOptimisticLimit);          // also NaN
+                    bool bad = !(rowsum <= kOptimisticLimit);                // also NaN
+                    // rows behind the chunk hold anything: they must not decide when the others' references move
+                    if constexpr (Win) bad = (bad || m_x == INFINITY) && X * tile_tokens + r_tok < j.tokens;
                     sh->xch[X][half][r] = bad ? 1.f : 0.f;
                     named_barrier(1 + quarter, 64);                // this quarter's two warps
                     const bool pair_bad = bad || sh->xch[X][half ^ 1][r] != 0.f;
@@ -639,11 +685,13 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (t == 0) {
                         // a piece of the keys may hold none that this row sees (then none of the following
                         // tiles does either): any finite reference gives the zeros that are wanted
-                        m_x = smax == -INFINITY ? 0.f : __fmaf_ru(smax, pv.sl2, -kBelow<T>);
+                        m_x = smax == -INFINITY ? (Win ? INFINITY : 0.f) : __fmaf_ru(smax, pv.sl2, -kBelow<T>);
                         l_x = 0.f;
                     } else {
+                        const bool unset = Win && m_x == INFINITY;
                         const float xmax = fmaf(smax, pv.sl2, -m_x);
-                        const bool grow = xmax > kRescaleThreshold;
+                        const bool grow = !unset && xmax > kRescaleThreshold;
+                        if (unset && smax != -INFINITY) m_x = __fmaf_ru(smax, pv.sl2, -kBelow<T>);       // what it has summed are zeros
                         if (grow) {
                             const float before = m_x;
                             m_x = __fmaf_ru(smax, pv.sl2, -kBelow<T>);
@@ -753,7 +801,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (half == 0 && live && done) {
                     if (j.part < 0) {
                         const float z = m_x + log2f(lsum);
-                        ws.lse2[((size_t)j.b * pv.H + j.h) * pv.c * G + (size_t)i * G + g] = z;
+                        if (!Win) ws.lse2[((size_t)j.b * pv.H + j.h) * pv.c * G + (size_t)i * G + g] = z;
                         if (a.lse) a.lse[(((size_t)j.b * pv.H + j.h) * G + g) * pv.c + i] = z * 0.6931471805599453f;
                     } else {
                         ws.part_ml[(size_t)j.part * ws.part_rows + X * kBlk + r] = make_float2(lsum > 0.f ? m_x : -INFINITY, lsum);
@@ -836,7 +884,7 @@ paged_merge_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__
         if (warp == 0 && i >= 0) {
             const int g = (pr % kBlk) % G;
             const float z = mx + log2f(l);
-            ws.lse2[((size_t)mg.b * pv.H + h) * pv.c * G + (size_t)i * G + g] = z;
+            if (ws.lse2) ws.lse2[((size_t)mg.b * pv.H + h) * pv.c * G + (size_t)i * G + g] = z;
             if (a.lse) a.lse[(((size_t)mg.b * pv.H + h) * G + g) * pv.c + i] = z * 0.6931471805599453f;
         }
         __syncthreads();
@@ -1259,51 +1307,52 @@ TcWs carve(const PagedView &pv, void *mem, size_t *bytes)
     w.pairs = (pv.c + w.pair_tokens - 1) / w.pair_tokens;
     w.part_rows = pv.c <= tile_tokens ? kBlk : 2 * kBlk;
     const size_t U = (size_t)pv.B * pv.H, items = (size_t)pv.B * w.pairs;
-    const size_t cap_tiles = (((size_t)pv.max_pages << pv.ps_shift) + kBlk - 1) / kBlk;
+    const size_t cap_tiles = ((size_t)near_capacity(pv, w.pair_tokens) + kBlk - 1) / kBlk;
     w.max_items = (int)(items + kMaxParts);
-    w.direct = cap_tiles <= kDirectTiles && items * pv.H < 0x7fffffff;
+    // windowed, items are of one length: a plan is for cutting them
+    w.direct = (cap_tiles <= kDirectTiles || (pv.window && items * pv.H >= kSplitBelow)) && items * pv.H < 0x7fffffff;
     w.whole_scores = (pv.c + tile_tokens - 1) / tile_tokens <= kWholeRows;
     size_t parts = w.direct ? 0 : items * pv.H * ((cap_tiles + kMinPiece - 1) / kMinPiece);
     if (parts > kMaxParts) parts = kMaxParts;
     w.parts = (int)parts;
     char *base = static_cast<char *>(mem);
     size_t off = 0;
-    w.lse2 = reinterpret_cast<float *>(base + off); off += pad(U * pv.c * pv.G * 4);
+    w.lse2 = pv.window ? nullptr : reinterpret_cast<float *>(base + off); off += pv.window ? 0 : pad(U * pv.c * pv.G * 4);      // for the scores
     w.head = reinterpret_cast<PlanHead *>(base + off); off += 256;
     w.items = reinterpret_cast<Item *>(base + off); off += pad(w.max_items * sizeof(Item));
     w.merges = reinterpret_cast<Merge *>(base + off); off += pad(items * sizeof(Merge));
     w.part_ml = reinterpret_cast<float2 *>(base + off); off += pad(parts * w.part_rows * 8);
     w.part_o = reinterpret_cast<float *>(base + off); off += pad(parts * w.part_rows * pv.d * 4);
-    w.score_parts = reinterpret_cast<float *>(base + off); off += pad((size_t)2 * kScoreCtas * kBlk * 4);
+    w.score_parts = reinterpret_cast<float *>(base + off); off += pv.window ? 0 : pad((size_t)2 * kScoreCtas * kBlk * 4);
     if (bytes) *bytes = off;
     return w;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool Win>
 cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    cudaError_t e = allow_dynamic_smem<paged_attn_tc_kernel<T, D>>(attn_smem<D>());
-    if (e == cudaSuccess) e = allow_dynamic_smem<paged_score_tc_kernel<D>>(score_smem<D>());
+    cudaError_t e = allow_dynamic_smem<paged_attn_tc_kernel<T, D, Win>>(attn_smem<D>());
+    if (!Win && e == cudaSuccess) e = allow_dynamic_smem<paged_score_tc_kernel<D>>(score_smem<D>());
     if (e != cudaSuccess) return e;
     CUtensorMap mq, mk, mv;
-    const int box = a.pv.ps;
+    const int box = Win ? a.pv.grain : a.pv.ps;
     if (!make_query_map(&mq, dtype, a.q, a.pv, a.sq) || !make_pool_map(&mk, dtype, a.pv.k, a.pv, box) ||
         !make_pool_map(&mv, dtype, a.pv.v, a.pv, box))
         return cudaErrorInvalidValue;
     const TcWs ws = carve(a.pv, a.ws, nullptr);
     if ((long long)ws.max_items * a.pv.H > 0x7fffffffll) return cudaErrorInvalidValue;
     if (!ws.direct) {
-        if ((e = launch_chained(paged_plan_kernel, 1, kPlanThreads, 0, s, a.pv, ws)) != cudaSuccess) return e;
+        if ((e = launch_chained(paged_plan_kernel<Win>, 1, kPlanThreads, 0, s, a.pv, ws)) != cudaSuccess) return e;
         count_launch();
     }
-    e = launch_chained(paged_attn_tc_kernel<T, D>, kSms, kAttnThreads, attn_smem<D>(), s, mq, mk, mv, a, ws);
+    e = launch_chained(paged_attn_tc_kernel<T, D, Win>, kSms, kAttnThreads, attn_smem<D>(), s, mq, mk, mv, a, ws);
     if (e != cudaSuccess) return e;
     count_launch();
     if (!ws.direct) {
         if ((e = launch_chained(paged_merge_kernel<T, D>, 4 * kSms, kMergeThreads, 0, s, a, ws)) != cudaSuccess) return e;
         count_launch();
     }
-    if (!a.scores) return cudaSuccess;
+    if (Win || !a.scores) return cudaSuccess;
     e = launch_chained(paged_score_tc_kernel<D>, kScoreCtas, kScoreThreads, score_smem<D>(), s, mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
     if (e != cudaSuccess) return e;
     count_launch();
@@ -1311,6 +1360,14 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
     if ((e = launch_chained(paged_score_join_kernel, kScoreCtas - 1, kBlk, 0, s, a, ws)) != cudaSuccess) return e;
     count_launch();
     return cudaSuccess;
+}
+
+template <bool Win>
+cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
+{
+    const bool wide = a.pv.d == 128;
+    if (dtype == A2SF_BF16) return wide ? launch<__nv_bfloat16, 128, Win>(dtype, a, s) : launch<__nv_bfloat16, 64, Win>(dtype, a, s);
+    return wide ? launch<__half, 128, Win>(dtype, a, s) : launch<__half, 64, Win>(dtype, a, s);
 }
 
 }  // namespace
@@ -1324,9 +1381,7 @@ size_t attend_tc_ws_bytes(const PagedView &pv)
 
 cudaError_t launch_attend_tc(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    const bool wide = a.pv.d == 128;
-    if (dtype == A2SF_BF16) return wide ? launch<__nv_bfloat16, 128>(dtype, a, s) : launch<__nv_bfloat16, 64>(dtype, a, s);
-    return wide ? launch<__half, 128>(dtype, a, s) : launch<__half, 64>(dtype, a, s);
+    return a.pv.window ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
 }
 
 }  // namespace a2sf

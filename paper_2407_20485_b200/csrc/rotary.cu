@@ -12,6 +12,10 @@
 // cosines -- about 30 instructions each, more than the memory time of a single head would hide --
 // are computed once per token and not once per head, and no table of them is read.  kHeads heads are
 // in flight at a time.  In append the same walk takes the keys into their pages, and the values.
+//
+// With several axes (kAxes) pair k turns by the position on its own axis, positions[axis[k]][b][t]; all else is the same.
+#include <type_traits>
+
 #include "paged.cuh"
 
 namespace a2sf {
@@ -34,15 +38,20 @@ template <typename P> __device__ __forceinline__ void store_pack(void *dst, cons
     else                           *reinterpret_cast<P *>(dst) = v;
 }
 
-struct PlanArg {
+template <bool kAxes> struct PlanArg {
     unsigned long long turn[A2SF_ROTARY_MAX_PAIRS];
 };
+template <> struct PlanArg<true> {
+    unsigned long long turn[A2SF_ROTARY_MAX_PAIRS];
+    uint8_t axis[A2SF_ROTARY_MAX_PAIRS];
+};
+template <bool kAxes> using PlanOf = std::conditional_t<kAxes, a2sf_rotary_axes_plan, a2sf_rotary_plan>;
 
 // One thread item of a row: W elements at `a`, and in the split layout W more at `b`.
 // Items 0 .. rot_items-1 rotate, the following ones copy W elements each.
-template <typename T, int W, bool Interleaved, bool Append>
+template <typename T, int W, bool Interleaved, bool Append, bool kAxes>
 __global__ void __launch_bounds__(kRotThreads, 4)
-rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ RotaryArgs r,
+rotary_kernel(const __grid_constant__ PlanArg<kAxes> plan, const __grid_constant__ RotaryArgs r,
               const __grid_constant__ PagedView pv, int r_dim, float magnitude, int rot_items, int items,
               int heads_per_block, int splits)
 {
@@ -68,7 +77,7 @@ rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ Rota
         base = r.start ? r.start[b] : 0;
     }
     if (t >= len) return;
-    const int pos = (!Append && r.positions) ? r.positions[(size_t)b * r.n + t] : base + t;
+    const int pos = (!Append && !kAxes && r.positions) ? r.positions[(size_t)b * r.n + t] : base + t;
 
     const bool rotates = item < rot_items;
     const int a_off = rotates ? item * W : r_dim + (item - rot_items) * W;
@@ -80,7 +89,9 @@ rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ Rota
         for (int e = 0; e < NP; ++e) {
             const int k = Interleaved ? item * NP + e : item * W + e;
             if (!A2SF_IN_RANGE(k, A2SF_ROTARY_MAX_PAIRS, kDbgRotary)) return;
-            const unsigned long long turn = plan.turn[k] * (unsigned long long)(long long)pos;
+            int at = pos;
+            if constexpr (kAxes) at = r.positions[((size_t)plan.axis[k] * r.B + b) * r.n + t];
+            const unsigned long long turn = plan.turn[k] * (unsigned long long)(long long)at;
             // the nearest quarter turn is in the top two bits of `near`; an eighth of a turn is left either way (half turns: [-1/4, 1/4])
             const unsigned top = (unsigned)(turn >> 32), near = top + 0x20000000u;
             float s0, c0;
@@ -151,8 +162,8 @@ rotary_kernel(const __grid_constant__ PlanArg plan, const __grid_constant__ Rota
     }
 }
 
-template <typename T, int W, bool Interleaved, bool Append>
-cudaError_t launch_w(const a2sf_rotary_plan *plan, const RotaryArgs &r, const PagedView &pv, cudaStream_t s)
+template <typename T, int W, bool Interleaved, bool Append, bool kAxes>
+cudaError_t launch_w(const PlanOf<kAxes> *plan, const RotaryArgs &r, const PagedView &pv, cudaStream_t s)
 {
     const int r_dim = plan ? plan->rotary_dim : 0;
     // in place, elements beyond the rotated ones are already where they belong -- unless keys and
@@ -160,8 +171,11 @@ cudaError_t launch_w(const a2sf_rotary_plan *plan, const RotaryArgs &r, const Pa
     const bool copies = Append || r.x != r.y;
     const int rot_items = Interleaved ? r_dim / W : r_dim / 2 / W;
     const int items = rot_items + (copies ? (r.d - r_dim) / W : 0);
-    PlanArg pa;
-    for (int k = 0; k < A2SF_ROTARY_MAX_PAIRS; ++k) pa.turn[k] = plan ? plan->turn[k] : 0;
+    PlanArg<kAxes> pa;
+    for (int k = 0; k < A2SF_ROTARY_MAX_PAIRS; ++k) {
+        pa.turn[k] = plan ? plan->turn[k] : 0;
+        if constexpr (kAxes) pa.axis[k] = plan->axis[k];
+    }
     const long long threads = (long long)r.B * r.n * items;
     const long long gx = (threads + kRotThreads - 1) / kRotThreads;
     if (gx > 0x7fffffffll) return cudaErrorInvalidValue;
@@ -175,43 +189,53 @@ cudaError_t launch_w(const a2sf_rotary_plan *plan, const RotaryArgs &r, const Pa
     const int hpb = (int)(((total + gy - 1) / gy + kHeads - 1) / kHeads) * kHeads;
     const int splits = (total + hpb - 1) / hpb;
     if (gx * splits > 0x7fffffffll) return cudaErrorInvalidValue;
-    const cudaError_t e = launch_chained(rotary_kernel<T, W, Interleaved, Append>, (unsigned)(gx * splits), kRotThreads, 0, s, pa, r, pv, r_dim,
+    const cudaError_t e = launch_chained(rotary_kernel<T, W, Interleaved, Append, kAxes>, (unsigned)(gx * splits), kRotThreads, 0, s, pa, r, pv, r_dim,
                                          plan ? plan->magnitude : 1.f, rot_items, items, hpb, splits);
     if (e == cudaSuccess) count_launch();
     return e;
 }
 
-template <typename T, bool Append>
-cudaError_t launch_t(const a2sf_rotary_plan *plan, const RotaryArgs &r, const PagedView &pv, cudaStream_t s)
+template <typename T, bool Append, bool kAxes>
+cudaError_t launch_t(const PlanOf<kAxes> *plan, const RotaryArgs &r, const PagedView &pv, cudaStream_t s)
 {
     // the widest access that divides the rotated part: the whole 16 bytes for the usual sizes
     const bool il = plan && plan->interleaved;
     const int part = plan ? (il ? plan->rotary_dim : plan->rotary_dim / 2) : r.d;
     constexpr int VEC = Elem<T>::kVec;
     if (il) {
-        if (part % VEC == 0) return launch_w<T, VEC, true, Append>(plan, r, pv, s);
-        if (part % 4 == 0) return launch_w<T, 4, true, Append>(plan, r, pv, s);
-        return launch_w<T, 2, true, Append>(plan, r, pv, s);
+        if (part % VEC == 0) return launch_w<T, VEC, true, Append, kAxes>(plan, r, pv, s);
+        if (part % 4 == 0) return launch_w<T, 4, true, Append, kAxes>(plan, r, pv, s);
+        return launch_w<T, 2, true, Append, kAxes>(plan, r, pv, s);
     }
-    if (part % VEC == 0) return launch_w<T, VEC, false, Append>(plan, r, pv, s);
-    if (part % 4 == 0) return launch_w<T, 4, false, Append>(plan, r, pv, s);
-    if (part % 2 == 0) return launch_w<T, 2, false, Append>(plan, r, pv, s);
-    return launch_w<T, 1, false, Append>(plan, r, pv, s);
+    if (part % VEC == 0) return launch_w<T, VEC, false, Append, kAxes>(plan, r, pv, s);
+    if (part % 4 == 0) return launch_w<T, 4, false, Append, kAxes>(plan, r, pv, s);
+    if (part % 2 == 0) return launch_w<T, 2, false, Append, kAxes>(plan, r, pv, s);
+    return launch_w<T, 1, false, Append, kAxes>(plan, r, pv, s);
 }
 
-}  // namespace
-
-cudaError_t launch_rotary(int dtype, const a2sf_rotary_plan *plan, const RotaryArgs &r, const PagedView *pages,
-                          cudaStream_t s)
+template <bool kAxes>
+cudaError_t launch(int dtype, const PlanOf<kAxes> *plan, const RotaryArgs &r, const PagedView *pages, cudaStream_t s)
 {
     PagedView none = {};
     const PagedView &pv = pages ? *pages : none;
     switch (dtype) {
-    case A2SF_F32: return pages ? launch_t<float, true>(plan, r, pv, s) : launch_t<float, false>(plan, r, pv, s);
+    case A2SF_F32: return pages ? launch_t<float, true, kAxes>(plan, r, pv, s) : launch_t<float, false, kAxes>(plan, r, pv, s);
     case A2SF_BF16:
-        return pages ? launch_t<__nv_bfloat16, true>(plan, r, pv, s) : launch_t<__nv_bfloat16, false>(plan, r, pv, s);
-    default: return pages ? launch_t<__half, true>(plan, r, pv, s) : launch_t<__half, false>(plan, r, pv, s);
+        return pages ? launch_t<__nv_bfloat16, true, kAxes>(plan, r, pv, s) : launch_t<__nv_bfloat16, false, kAxes>(plan, r, pv, s);
+    default: return pages ? launch_t<__half, true, kAxes>(plan, r, pv, s) : launch_t<__half, false, kAxes>(plan, r, pv, s);
     }
+}
+
+}  // namespace
+
+cudaError_t launch_rotary(int dtype, const a2sf_rotary_plan *plan, const RotaryArgs &r, const PagedView *pages, cudaStream_t s)
+{
+    return launch<false>(dtype, plan, r, pages, s);
+}
+
+cudaError_t launch_rotary_axes(int dtype, const a2sf_rotary_axes_plan *plan, const RotaryArgs &r, const PagedView *pages, cudaStream_t s)
+{
+    return launch<true>(dtype, plan, r, pages, s);
 }
 
 int *paged_status_word()

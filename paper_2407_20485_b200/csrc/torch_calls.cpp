@@ -7,6 +7,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/utils/pybind.h>
 
+#include <map>
 #include <optional>
 #include <sstream>
 #include <unordered_map>
@@ -24,6 +25,11 @@ struct {
     decltype(&a2sf_paged_attend) attend;
     decltype(&a2sf_paged_attend_workspace_bytes) attend_bytes;
     decltype(&a2sf_paged_evict) evict;
+    decltype(&a2sf_rotary_axes) rotary_axes;
+    decltype(&a2sf_paged_append_axes) append_axes;
+    decltype(&a2sf_paged_attend_window) attend_window;
+    decltype(&a2sf_paged_attend_window_workspace_bytes) window_bytes;
+    decltype(&a2sf_paged_slide) slide;
     decltype(&a2sf_paged_evict_workspace_bytes) evict_bytes;
 } fn;
 
@@ -110,6 +116,24 @@ std::pair<int, Tensor> rotary(int64_t plan, const Tensor &x, const OptTensor &ou
     return {rc, out};
 }
 
+std::pair<int, Tensor> rotary_axes(int64_t plan, const Tensor &x, const Tensor &positions, const OptTensor &out_opt, const OptTensor &lens, bool transpose,
+                                   int64_t stream)
+{
+    if (x.dim() != 4) throw pybind11::value_error("x: expected a [B,H,n,d] tensor");
+    const int device = x.get_device();
+    const auto shape = x.sizes();
+    const Rows xr(x, shape, x.scalar_type(), device, "x");
+    Place at(device, stream, "a2sf_rotary_axes");
+    const Tensor out = out_opt ? *out_opt : like(x);
+    const Rows yr(out, shape, x.scalar_type(), device, "out");
+    const auto *p = reinterpret_cast<const a2sf_rotary_axes_plan *>(plan);
+    const int64_t B = shape[0], n = shape[2];
+    const int32_t *pos = array<int32_t>(positions, {p->axes, B, n}, device, "positions"), *ln = array<int32_t>(lens, {B}, device, "lens");
+    const int rc = fn.rotary_axes(p, dtype_code(x.scalar_type()), (int32_t)B, (int32_t)shape[1], (int32_t)n, (int32_t)shape[3], xr.p, xr.b, xr.h, xr.t, yr.p,
+                                  yr.b, yr.h, yr.t, pos, ln, transpose ? A2SF_ROTARY_TRANSPOSE : 0, at.stream);
+    return {rc, out};
+}
+
 class Calls {
 public:
     Calls(int64_t cache, int device) : p_(*reinterpret_cast<const a2sf_paged *>(cache)), device_(device)
@@ -119,19 +143,25 @@ public:
 
     std::pair<int, OptTensor> append(const Tensor &k, const Tensor &v, const OptTensor &lens, const OptTensor &q, OptTensor q_out, int64_t plan, int64_t stream)
     {
-        const int64_t c = chunk(k, "k"), kv[4] = {p_.B, p_.H, c, p_.d}, qs[4] = {p_.B, (int64_t)p_.H * p_.group, c, p_.d};
-        const Rows kr(k, kv, type_, device_, "k"), vr(v, kv, type_, device_, "v");
-        if (!kr.same_strides(vr)) throw pybind11::value_error("k and v need the same strides");
+        const Chunk x(*this, k, v, q);
         Place at(device_, stream, "a2sf_paged_append");
-        Rows qr, yr;
-        if (q) {
-            qr = Rows(*q, qs, type_, device_, "q");
-            if (!q_out) q_out = like(*q);
-            yr = Rows(*q_out, qs, type_, device_, "q_out");
-        }
+        const Rows yr = x.output(*this, q, q_out);
         const int32_t *ln = array<int32_t>(lens, {p_.B}, device_, "lens");
-        const int rc = fn.append(&p_, reinterpret_cast<const a2sf_rotary_plan *>(plan), (int32_t)c, ln, kr.p, vr.p, kr.b, kr.h, kr.t, qr.p, qr.b, qr.h, qr.t,
-                                 yr.p, yr.b, yr.h, yr.t, at.stream);
+        const int rc = fn.append(&p_, reinterpret_cast<const a2sf_rotary_plan *>(plan), (int32_t)x.c, ln, x.k.p, x.v.p, x.k.b, x.k.h, x.k.t, x.q.p, x.q.b, x.q.h,
+                                 x.q.t, yr.p, yr.b, yr.h, yr.t, at.stream);
+        return {rc, q ? q_out : OptTensor()};
+    }
+
+    std::pair<int, OptTensor> append_axes(const Tensor &k, const Tensor &v, const Tensor &positions, int64_t plan, const OptTensor &lens, const OptTensor &q,
+                                          OptTensor q_out, int64_t stream)
+    {
+        const Chunk x(*this, k, v, q);
+        Place at(device_, stream, "a2sf_paged_append_axes");
+        const Rows yr = x.output(*this, q, q_out);
+        const auto *p = reinterpret_cast<const a2sf_rotary_axes_plan *>(plan);
+        const int32_t *pos = array<int32_t>(positions, {p->axes, p_.B, x.c}, device_, "positions"), *ln = array<int32_t>(lens, {p_.B}, device_, "lens");
+        const int rc = fn.append_axes(&p_, p, pos, (int32_t)x.c, ln, x.k.p, x.v.p, x.k.b, x.k.h, x.k.t, x.q.p, x.q.b, x.q.h, x.q.t, yr.p, yr.b, yr.h, yr.t,
+                                      at.stream);
         return {rc, q ? q_out : OptTensor()};
     }
 
@@ -152,11 +182,42 @@ public:
         return {rc, out, lse};
     }
 
+    std::tuple<int, Tensor, Tensor> attend_window(const Tensor &q, int64_t window, int64_t sinks, const OptTensor &lens, const OptTensor &out_opt,
+                                                  const OptTensor &lse_opt, const OptTensor &workspace, int64_t stream)
+    {
+        const int64_t c = chunk(q, "q"), qs[4] = {p_.B, (int64_t)p_.H * p_.group, c, p_.d};
+        numbers("window and sinks", {window, sinks});
+        const Rows qr(q, qs, type_, device_, "q");
+        Place at(device_, stream, "a2sf_paged_attend_window");
+        const Tensor out = out_opt ? *out_opt : like(q);
+        const Tensor lse = lse_opt ? *lse_opt : at::empty({qs[0], qs[1], c}, q.options().dtype(at::kFloat));
+        const Rows yr(out, qs, type_, device_, "out");
+        float *z = array<float>(lse, {qs[0], qs[1], c}, device_, "lse");
+        const int32_t *ln = array<int32_t>(lens, {p_.B}, device_, "lens");
+        auto &sizes = window_bytes_[{window, sinks}];
+        if (window_bytes_.size() > 256) { window_bytes_.clear(); return attend_window(q, window, sinks, lens, out, lse, workspace, stream); }
+        const Tensor ws = space(workspace, sizes, c, [&](const a2sf_paged *p, int32_t n) { return fn.window_bytes(p, n, (int32_t)window, (int32_t)sinks); });
+        const int rc = fn.attend_window(&p_, (int32_t)c, ln, (int32_t)window, (int32_t)sinks, qr.p, qr.b, qr.h, qr.t, yr.p, yr.b, yr.h, yr.t, z, ws.data_ptr(),
+                                        (size_t)ws.numel(), at.stream);
+        return {rc, out, lse};
+    }
+
+    int slide(int64_t window, int64_t sinks, int64_t c, const OptTensor &lens, const Tensor &table_out, const OptTensor &freed, const OptTensor &freed_count,
+              const Tensor &past_out, const Tensor &start_out, int64_t stream)
+    {
+        numbers("window, sinks and c", {window, sinks, c});
+        const int32_t *ln = array<int32_t>(lens, {p_.B}, device_, "lens");
+        int32_t *to = array<int32_t>(table_out, {p_.B, p_.max_pages}, device_, "table_out"), *fr = array<int32_t>(freed, {p_.B, p_.max_pages}, device_, "freed"),
+                *fc = array<int32_t>(freed_count, {p_.B}, device_, "freed_count"), *po = array<int32_t>(past_out, {p_.B}, device_, "past_out"),
+                *so = array<int32_t>(start_out, {p_.B}, device_, "start_out");
+        Place at(device_, stream, "a2sf_paged_slide");
+        return fn.slide(&p_, (int32_t)c, ln, (int32_t)window, (int32_t)sinks, to, fr, fc, po, so, at.stream);
+    }
+
     int evict(int64_t budget, int64_t recent, int64_t c, const OptTensor &lens, const OptTensor &dst, const Tensor &past_out, const Tensor &start_out,
               const OptTensor &workspace, int64_t stream)
     {
-        for (const int64_t x : {budget, recent, c})
-            if (x != (int32_t)x) throw pybind11::value_error("budget, recent and c are 32-bit numbers");
+        numbers("budget, recent and c", {budget, recent, c});
         if (dst && dst->dim() != 2) throw pybind11::value_error("dst_table: expected [B, pages]");
         const int64_t pages = dst ? dst->size(1) : 0;
         const int32_t *ln = array<int32_t>(lens, {p_.B}, device_, "lens"), *dt = array<int32_t>(dst, {p_.B, pages}, device_, "dst_table");
@@ -167,6 +228,31 @@ public:
     }
 
 private:
+    // keys, values and (or not) queries of an append
+    struct Chunk {
+        int64_t c;
+        Rows k, v, q;
+        Chunk(const Calls &at, const Tensor &kt, const Tensor &vt, const OptTensor &qt) : c(at.chunk(kt, "k"))
+        {
+            const int64_t kv[4] = {at.p_.B, at.p_.H, c, at.p_.d};
+            k = Rows(kt, kv, at.type_, at.device_, "k");
+            v = Rows(vt, kv, at.type_, at.device_, "v");
+            if (!k.same_strides(v)) throw pybind11::value_error("k and v need the same strides");
+            if (qt) q = Rows(*qt, {at.p_.B, (int64_t)at.p_.H * at.p_.group, c, at.p_.d}, at.type_, at.device_, "q");
+        }
+        Rows output(const Calls &at, const OptTensor &qt, OptTensor &out) const      // a new one where there is none
+        {
+            if (!qt) return Rows();
+            if (!out) out = like(*qt);
+            return Rows(*out, {at.p_.B, (int64_t)at.p_.H * at.p_.group, c, at.p_.d}, at.type_, at.device_, "q_out");
+        }
+    };
+
+    static void numbers(const char *what, std::initializer_list<int64_t> values)
+    {
+        for (const int64_t x : values)
+            if (x != (int32_t)x) throw pybind11::value_error(std::string(what) + " are 32-bit numbers");
+    }
     int64_t chunk(const Tensor &x, const char *name) const
     {
         if (x.dim() != 4) throw pybind11::value_error(std::string(name) + ": expected a [B,H,c,d] tensor");
@@ -193,6 +279,7 @@ private:
     int device_;
     at::ScalarType type_;
     std::unordered_map<int64_t, int64_t> attend_bytes_, evict_bytes_;
+    std::map<std::pair<int64_t, int64_t>, std::unordered_map<int64_t, int64_t>> window_bytes_;      // by window and sinks
 };
 
 }  // namespace
@@ -205,12 +292,21 @@ PYBIND11_MODULE(_torch_calls, m)
         fn.attend = reinterpret_cast<decltype(fn.attend)>(at.at("a2sf_paged_attend"));
         fn.attend_bytes = reinterpret_cast<decltype(fn.attend_bytes)>(at.at("a2sf_paged_attend_workspace_bytes"));
         fn.evict = reinterpret_cast<decltype(fn.evict)>(at.at("a2sf_paged_evict"));
+        fn.rotary_axes = reinterpret_cast<decltype(fn.rotary_axes)>(at.at("a2sf_rotary_axes"));
+        fn.append_axes = reinterpret_cast<decltype(fn.append_axes)>(at.at("a2sf_paged_append_axes"));
+        fn.attend_window = reinterpret_cast<decltype(fn.attend_window)>(at.at("a2sf_paged_attend_window"));
+        fn.window_bytes = reinterpret_cast<decltype(fn.window_bytes)>(at.at("a2sf_paged_attend_window_workspace_bytes"));
+        fn.slide = reinterpret_cast<decltype(fn.slide)>(at.at("a2sf_paged_slide"));
         fn.evict_bytes = reinterpret_cast<decltype(fn.evict_bytes)>(at.at("a2sf_paged_evict_workspace_bytes"));
     });
     m.def("rotary", &rotary);
+    m.def("rotary_axes", &rotary_axes);
     pybind11::class_<Calls>(m, "Calls")
         .def(pybind11::init<int64_t, int>())
         .def("append", &Calls::append)
+        .def("append_axes", &Calls::append_axes)
         .def("attend", &Calls::attend)
+        .def("attend_window", &Calls::attend_window)
+        .def("slide", &Calls::slide)
         .def("evict", &Calls::evict);
 }
