@@ -93,7 +93,6 @@ PagedView make_view(const a2sf_paged *p, int c, const int32_t *lens)
     v.ps_shift = p->page_size == 16 ? 4 : p->page_size == 32 ? 5 : p->page_size == 64 ? 6 : 7;
     v.max_pages = p->max_pages; v.num_pages = p->num_pages; v.c = c;
     v.sl2 = (p->scale > 0.f ? p->scale : 1.f / std::sqrt((float)p->d)) * kLog2e;
-    v.window = v.sinks = v.sink_end = v.grain = 0;
     return v;
 }
 
@@ -136,26 +135,27 @@ EncodeTiledFn encode_fn()
 // 2,000, 9e8: 42 and 70.  One tile of 64 rows: 640 heads, 64 behind 100, 1e9: 71 and 52; 64 x 64 behind 4,000, 2e9: 83 and 96.
 enum Path { kFew, kTc, kMma };
 // Windowed, a row tile of tcgen05 (256 rows) sees the near capacity of its tokens and that is what counts.
-Path path_of(const PagedView &v, int dtype)
+Path path_of(const PagedView &v, bool windowed, int dtype)
 {
     const int64_t rows = (int64_t)v.c * v.G;
     if (rows <= kFewRows) return kFew;
     if (dtype == A2SF_F32) return kMma;
     const int tokens = 256 / v.G < v.c ? 256 / v.G : v.c;
-    const double work = (double)v.B * v.H * rows * near_capacity(v, tokens) * v.d;
+    const double work = (double)v.B * v.H * rows * near_capacity(v, windowed, tokens) * v.d;
     return work < (rows <= 64 ? 1.2e9 : 3e8) ? kMma : kTc;
 }
 
-size_t attend_ws_bytes(const PagedView &v, int dtype)
+size_t attend_ws_bytes(const PagedView &v, bool windowed, int dtype)
 {
-    const Path path = path_of(v, dtype);
-    const size_t bytes = align_up(path == kFew ? attend_few_ws_bytes(dtype, v) : path == kTc ? attend_tc_ws_bytes(v) : attend_mma_ws_bytes(dtype, v));
+    const Path path = path_of(v, windowed, dtype);
+    const size_t bytes = align_up(path == kFew ? attend_few_ws_bytes(dtype, v, windowed) : path == kTc ? attend_tc_ws_bytes(v, windowed)
+                                                                                                       : attend_mma_ws_bytes(dtype, v, windowed));
     return bytes ? bytes : 256;                               // 0 says that arguments are invalid
 }
 
 cudaError_t launch_attend(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    const Path path = path_of(a.pv, dtype);
+    const Path path = path_of(a.pv, a.windowed, dtype);
     return path == kFew ? launch_attend_few(dtype, a, s) : path == kTc ? launch_attend_tc(dtype, a, s) : launch_attend_mma(dtype, a, s);
 }
 
@@ -406,7 +406,7 @@ int a2sf_paged_append(const a2sf_paged *cache, const a2sf_rotary_plan *rotary, i
 size_t a2sf_paged_attend_workspace_bytes(const a2sf_paged *cache, int32_t c)
 {
     if (check_paged(cache, c) != A2SF_OK) return 0;
-    return attend_ws_bytes(make_view(cache, c, nullptr), cache->dtype);
+    return attend_ws_bytes(make_view(cache, c, nullptr), false, cache->dtype);
 }
 
 int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, float alpha, const void *q,
@@ -434,6 +434,7 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
     a.so = Strides{out_stride_b, out_stride_h, out_stride_t};
     a.alpha = alpha; a.nl2a = neg_log2(alpha);
     a.scores = !(flags & A2SF_ATTEND_NO_SCORES);
+    a.windowed = false;
     a.ws = workspace;
     return launch_attend(cache->dtype, a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
 }
@@ -441,7 +442,7 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
 size_t a2sf_paged_attend_window_workspace_bytes(const a2sf_paged *cache, int32_t c, int32_t window, int32_t sinks)
 {
     if (check_paged(cache, c) != A2SF_OK || window < 1 || sinks < 0) return 0;
-    return attend_ws_bytes(make_window_view(cache, c, nullptr, window, sinks), cache->dtype);
+    return attend_ws_bytes(make_window_view(cache, c, nullptr, window, sinks), true, cache->dtype);
 }
 
 int a2sf_paged_attend_window(const a2sf_paged *cache, int32_t c, const int32_t *lens, int32_t window, int32_t sinks, const void *q,
@@ -462,13 +463,14 @@ int a2sf_paged_attend_window(const a2sf_paged *cache, int32_t c, const int32_t *
     if (q == out) return A2SF_ERR_INVALID_ARG;
     AttendArgs a;
     a.pv = make_window_view(cache, c, lens, window, sinks);
-    if (workspace_bytes < attend_ws_bytes(a.pv, cache->dtype)) return A2SF_ERR_WORKSPACE;
+    if (workspace_bytes < attend_ws_bytes(a.pv, true, cache->dtype)) return A2SF_ERR_WORKSPACE;
     if (!(a.pv.status = paged_status_word())) return A2SF_ERR_CUDA;
     a.q = q; a.out = out; a.lse = lse;
     a.sq = Strides{q_stride_b, q_stride_h, q_stride_t};
     a.so = Strides{out_stride_b, out_stride_h, out_stride_t};
     a.alpha = 1.f; a.nl2a = 0.f;
     a.scores = false;
+    a.windowed = true;
     a.ws = workspace;
     return launch_attend(cache->dtype, a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? A2SF_OK : A2SF_ERR_CUDA;
 }

@@ -920,9 +920,9 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
 }
 
 size_t pad(size_t x) { return (x + 255) / 256 * 256; }
-int padded_slots(const PagedView &pv) { return (near_capacity(pv, pv.c) + 127) / 128 * 128; }       // of either tile
+int padded_slots(const PagedView &pv, bool windowed) { return (near_capacity(pv, windowed, pv.c) + 127) / 128 * 128; }       // of either tile
 
-FewWs carve(int dtype, const PagedView &pv, void *ws, size_t *bytes)
+FewWs carve(int dtype, const PagedView &pv, bool windowed, void *ws, size_t *bytes)
 {
     const size_t U = (size_t)pv.B * pv.H, NP = rows_padded(pv.c * pv.G);
     // the size must not depend on a device: room for any SM count up to 256
@@ -930,9 +930,9 @@ FewWs carve(int dtype, const PagedView &pv, void *ws, size_t *bytes)
     FewWs w;
     size_t off = 0;
     char *base = static_cast<char *>(ws);
-    w.slots = padded_slots(pv);
+    w.slots = padded_slots(pv, windowed);
     w.segs = (int)segs;
-    w.logits = reinterpret_cast<float *>(base + off); off += pv.window ? 0 : pad(U * w.slots * NP * 4);
+    w.logits = reinterpret_cast<float *>(base + off); off += windowed ? 0 : pad(U * w.slots * NP * 4);
     w.ml = reinterpret_cast<float2 *>(base + off); off += pad(segs * NP * 8);
     w.o = reinterpret_cast<float *>(base + off); off += pad(segs * NP * pv.d * 4);
     w.prefix = reinterpret_cast<int32_t *>(base + off); off += pad(((size_t)pv.B + 1) * 4);
@@ -944,7 +944,7 @@ FewWs carve(int dtype, const PagedView &pv, void *ws, size_t *bytes)
 template <typename T, int D, int NC, bool Win> size_t whole_smem(const PagedView &pv)
 {
     using R = Ring<T, D>;
-    const int slots = (near_capacity(pv, pv.c) + R::kTile - 1) / R::kTile * R::kTile;
+    const int slots = (near_capacity(pv, Win, pv.c) + R::kTile - 1) / R::kTile * R::kTile;
     const size_t smem = R::kBytes + BodyOf<T, D, NC, Win>::kScratch + whole_bytes(warps_of<T>, D, rows_padded(pv.c * pv.G), Win ? 0 : slots);
     const int most = pv.B * pv.H >= kSms ? kWholeTilesMany : kWholeTiles;
     return slots <= most * R::kTile && smem + sizeof(WholeShared) <= 227 * 1024 ? smem : 0;
@@ -964,12 +964,12 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     if (const size_t whole = whole_smem<T, D, NC, Win>(a.pv)) {
         if ((e = allow_dynamic_smem<paged_few_whole_kernel<T, D, NC, Win>>(whole)) != cudaSuccess) return e;
         const long long resident = device_sm_count() * (2 * (whole + sizeof(WholeShared) + 1024) <= 228 * 1024 ? 2 : 1), units = (long long)a.pv.B * a.pv.H;
-        const int slots = (near_capacity(a.pv, a.pv.c) + R::kTile - 1) / R::kTile * R::kTile;
+        const int slots = (near_capacity(a.pv, Win, a.pv.c) + R::kTile - 1) / R::kTile * R::kTile;
         e = launch_chained(paged_few_whole_kernel<T, D, NC, Win>, (unsigned)(units < resident ? units : resident), 32 * (warps_of<T> + 1), whole, s, mk, mv, a, NP, slots);
         if (e == cudaSuccess) count_launch();
         return e;
     }
-    const FewWs ws = carve(dtype, a.pv, a.ws, nullptr);
+    const FewWs ws = carve(dtype, a.pv, Win, a.ws, nullptr);
     const int ctas = device_sm_count() * (2 * (smem + sizeof(FewShared) + 1024) <= 228 * 1024 ? 2 : 1);   // what is resident
     if (ctas < 1 || ctas > 512) return cudaErrorInvalidValue;
     if ((e = launch_chained(paged_few_kernel<T, D, NC, Win>, ctas, 32 * (warps_of<T> + 1), smem, s, mk, mv, a, ws, NP)) != cudaSuccess) return e;
@@ -1026,16 +1026,16 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
 
 }  // namespace
 
-size_t attend_few_ws_bytes(int dtype, const PagedView &pv)
+size_t attend_few_ws_bytes(int dtype, const PagedView &pv, bool windowed)
 {
     size_t bytes = 0;
-    carve(dtype, pv, nullptr, &bytes);
+    carve(dtype, pv, windowed, nullptr, &bytes);
     return bytes;
 }
 
 cudaError_t launch_attend_few(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    return a.pv.window ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
+    return a.windowed ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
 }
 
 }  // namespace a2sf

@@ -642,10 +642,10 @@ struct Shape {
     int pieces;
     bool large_score;
 };
-Shape shape_of(int dtype, const PagedView &pv)
+Shape shape_of(int dtype, const PagedView &pv, bool windowed)
 {
     Shape s;
-    const long long units = (long long)pv.B * pv.H, rows = (long long)pv.c * pv.G, cap = near_capacity(pv, std::min(pv.c, 64));      // of a row tile
+    const long long units = (long long)pv.B * pv.H, rows = (long long)pv.c * pv.G, cap = near_capacity(pv, windowed, std::min(pv.c, 64));      // of a row tile
     const long long most = std::max(1ll, (cap + kTile - 1) / kTile / (dtype == A2SF_F32 ? 2 : 4)), tiles = units * ((rows + 63) / 64);
     s.large = tiles * most >= 4 * kSms;
     s.row_tiles = s.large ? (rows + 63) / 64 : (rows + 15) / 16;
@@ -655,15 +655,15 @@ Shape shape_of(int dtype, const PagedView &pv)
     return s;
 }
 
-MmaWs carve(int dtype, const PagedView &pv, void *mem, size_t *bytes)
+MmaWs carve(int dtype, const PagedView &pv, bool windowed, void *mem, size_t *bytes)
 {
     MmaWs w;
     const size_t rows = (size_t)pv.B * pv.H * pv.G * pv.c;
-    w.pieces = shape_of(dtype, pv).pieces;
+    w.pieces = shape_of(dtype, pv, windowed).pieces;
     char *base = static_cast<char *>(mem);
     size_t off = 0;
     const size_t parts = w.pieces > 1 ? rows * w.pieces : 0;
-    w.lse2 = pv.window ? nullptr : reinterpret_cast<float *>(base + off); off += pv.window ? 0 : pad(rows * 4);     // for the scores
+    w.lse2 = windowed ? nullptr : reinterpret_cast<float *>(base + off); off += windowed ? 0 : pad(rows * 4);     // for the scores
     w.ml = reinterpret_cast<float2 *>(base + off); off += pad(parts * 8);
     w.o = reinterpret_cast<float *>(base + off); off += pad(parts * pv.d * 4);
     if (bytes) *bytes = off;
@@ -696,8 +696,8 @@ cudaError_t launch_score(const AttendArgs &a, const MmaWs &ws, long long slot_ti
 template <typename T, int D, bool Win>
 cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    const Shape sh = shape_of(dtype, a.pv);
-    const MmaWs ws = carve(dtype, a.pv, a.ws, nullptr);
+    const Shape sh = shape_of(dtype, a.pv, Win);
+    const MmaWs ws = carve(dtype, a.pv, Win, a.ws, nullptr);
     cudaError_t e = sh.large ? launch_attn<T, D, 4, Win>(a, ws, sh.row_tiles, s) : launch_attn<T, D, 1, Win>(a, ws, sh.row_tiles, s);
     if (e != cudaSuccess) return e;
     if (ws.pieces > 1) {
@@ -723,16 +723,16 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
 
 }  // namespace
 
-size_t attend_mma_ws_bytes(int dtype, const PagedView &pv)
+size_t attend_mma_ws_bytes(int dtype, const PagedView &pv, bool windowed)
 {
     size_t bytes = 0;
-    carve(dtype, pv, nullptr, &bytes);
+    carve(dtype, pv, windowed, nullptr, &bytes);
     return bytes;
 }
 
 cudaError_t launch_attend_mma(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    return a.pv.window ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
+    return a.windowed ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
 }
 
 }  // namespace a2sf

@@ -1298,7 +1298,7 @@ paged_score_join_kernel(const __grid_constant__ AttendArgs a, const __grid_const
 
 size_t pad(size_t x) { return (x + 255) / 256 * 256; }
 
-TcWs carve(const PagedView &pv, void *mem, size_t *bytes)
+TcWs carve(const PagedView &pv, bool windowed, void *mem, size_t *bytes)
 {
     TcWs w;
     const int tile_tokens = kBlk / pv.G;
@@ -1307,23 +1307,23 @@ TcWs carve(const PagedView &pv, void *mem, size_t *bytes)
     w.pairs = (pv.c + w.pair_tokens - 1) / w.pair_tokens;
     w.part_rows = pv.c <= tile_tokens ? kBlk : 2 * kBlk;
     const size_t U = (size_t)pv.B * pv.H, items = (size_t)pv.B * w.pairs;
-    const size_t cap_tiles = ((size_t)near_capacity(pv, w.pair_tokens) + kBlk - 1) / kBlk;
+    const size_t cap_tiles = ((size_t)near_capacity(pv, windowed, w.pair_tokens) + kBlk - 1) / kBlk;
     w.max_items = (int)(items + kMaxParts);
     // windowed, items are of one length: a plan is for cutting them
-    w.direct = (cap_tiles <= kDirectTiles || (pv.window && items * pv.H >= kSplitBelow)) && items * pv.H < 0x7fffffff;
+    w.direct = (cap_tiles <= kDirectTiles || (windowed && items * pv.H >= kSplitBelow)) && items * pv.H < 0x7fffffff;
     w.whole_scores = (pv.c + tile_tokens - 1) / tile_tokens <= kWholeRows;
     size_t parts = w.direct ? 0 : items * pv.H * ((cap_tiles + kMinPiece - 1) / kMinPiece);
     if (parts > kMaxParts) parts = kMaxParts;
     w.parts = (int)parts;
     char *base = static_cast<char *>(mem);
     size_t off = 0;
-    w.lse2 = pv.window ? nullptr : reinterpret_cast<float *>(base + off); off += pv.window ? 0 : pad(U * pv.c * pv.G * 4);      // for the scores
+    w.lse2 = windowed ? nullptr : reinterpret_cast<float *>(base + off); off += windowed ? 0 : pad(U * pv.c * pv.G * 4);      // for the scores
     w.head = reinterpret_cast<PlanHead *>(base + off); off += 256;
     w.items = reinterpret_cast<Item *>(base + off); off += pad(w.max_items * sizeof(Item));
     w.merges = reinterpret_cast<Merge *>(base + off); off += pad(items * sizeof(Merge));
     w.part_ml = reinterpret_cast<float2 *>(base + off); off += pad(parts * w.part_rows * 8);
     w.part_o = reinterpret_cast<float *>(base + off); off += pad(parts * w.part_rows * pv.d * 4);
-    w.score_parts = reinterpret_cast<float *>(base + off); off += pv.window ? 0 : pad((size_t)2 * kScoreCtas * kBlk * 4);
+    w.score_parts = reinterpret_cast<float *>(base + off); off += windowed ? 0 : pad((size_t)2 * kScoreCtas * kBlk * 4);
     if (bytes) *bytes = off;
     return w;
 }
@@ -1339,7 +1339,7 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
     if (!make_query_map(&mq, dtype, a.q, a.pv, a.sq) || !make_pool_map(&mk, dtype, a.pv.k, a.pv, box) ||
         !make_pool_map(&mv, dtype, a.pv.v, a.pv, box))
         return cudaErrorInvalidValue;
-    const TcWs ws = carve(a.pv, a.ws, nullptr);
+    const TcWs ws = carve(a.pv, Win, a.ws, nullptr);
     if ((long long)ws.max_items * a.pv.H > 0x7fffffffll) return cudaErrorInvalidValue;
     if (!ws.direct) {
         if ((e = launch_chained(paged_plan_kernel<Win>, 1, kPlanThreads, 0, s, a.pv, ws)) != cudaSuccess) return e;
@@ -1372,16 +1372,16 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
 
 }  // namespace
 
-size_t attend_tc_ws_bytes(const PagedView &pv)
+size_t attend_tc_ws_bytes(const PagedView &pv, bool windowed)
 {
     size_t bytes = 0;
-    carve(pv, nullptr, &bytes);
+    carve(pv, windowed, nullptr, &bytes);
     return bytes;
 }
 
 cudaError_t launch_attend_tc(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    return a.pv.window ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
+    return a.windowed ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
 }
 
 }  // namespace a2sf
