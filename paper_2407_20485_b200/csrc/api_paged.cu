@@ -148,15 +148,16 @@ Path path_of(const PagedView &v, bool windowed, int dtype)
 size_t attend_ws_bytes(const PagedView &v, bool windowed, int dtype)
 {
     const Path path = path_of(v, windowed, dtype);
-    const size_t bytes = align_up(path == kFew ? attend_few_ws_bytes(dtype, v, windowed) : path == kTc ? attend_tc_ws_bytes(v, windowed)
-                                                                                                       : attend_mma_ws_bytes(dtype, v, windowed));
+    const size_t bytes = align_up(path == kFew ? attend_few_ws_bytes(dtype, v, windowed) : path == kMma ? attend_mma_ws_bytes(dtype, v, windowed)
+                                  : windowed ? window_tc_ws_bytes(v) : attend_tc_ws_bytes(v));
     return bytes ? bytes : 256;                               // 0 says that arguments are invalid
 }
 
 cudaError_t launch_attend(int dtype, const AttendArgs &a, cudaStream_t s)
 {
     const Path path = path_of(a.pv, a.windowed, dtype);
-    return path == kFew ? launch_attend_few(dtype, a, s) : path == kTc ? launch_attend_tc(dtype, a, s) : launch_attend_mma(dtype, a, s);
+    return path == kFew ? launch_attend_few(dtype, a, s) : path == kMma ? launch_attend_mma(dtype, a, s)
+           : a.windowed ? launch_window_tc(dtype, a, s) : launch_attend_tc(dtype, a, s);
 }
 
 }  // namespace

@@ -117,7 +117,7 @@ enum DebugKernelId {
     kDbgGroupSum, kDbgPrefillSimt1, kDbgPrefillSimt2, kDbgAttnTc, kDbgScoreTc, kDbgVToHalf,
     kDbgIdealStats, kDbgSimilarityRow,
     kDbgPagedRow, kDbgPagedFew, kDbgPagedTc, kDbgPagedMma, kDbgPagedEvict, kDbgRotary,
-    kDbgPagedSlide
+    kDbgPagedSlide, kDbgWindowTc
 };
 #ifdef A2SF_DEBUG
 // one record per translation unit (no relocatable device code): {violations, kernel << 32 | line,

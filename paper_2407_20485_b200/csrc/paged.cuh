@@ -265,8 +265,10 @@ cudaError_t launch_attend_few(int dtype, const AttendArgs &a, cudaStream_t s);
 
 // many rows, 16-bit storage: tcgen05
 bool make_query_map(CUtensorMap *map, int dtype, const void *q, const PagedView &pv, const Strides &st);
-size_t attend_tc_ws_bytes(const PagedView &pv, bool windowed);
+size_t attend_tc_ws_bytes(const PagedView &pv);
 cudaError_t launch_attend_tc(int dtype, const AttendArgs &a, cudaStream_t s);
+size_t window_tc_ws_bytes(const PagedView &pv);               // windowed
+cudaError_t launch_window_tc(int dtype, const AttendArgs &a, cudaStream_t s);
 
 // 32-bit storage, and small calls of 16-bit storage
 size_t attend_mma_ws_bytes(int dtype, const PagedView &pv, bool windowed);

@@ -21,10 +21,6 @@
 //           830 tokens).  The (key tile, row tile) pairs of the call are one list, cut into equal shares; a
 //           key tile that a cut goes through is summed in parts, which the join kernel adds in order.
 //
-// Windowed (Win): an item walks over the near slots of its pair's rows (see Near): the sinks, and from the window of its first row
-// on; attn and merge alone.  All items of a call then are about as long as the window, so a plan is made only where they are to
-// be cut.  A row may see nothing of its item's first tiles; its reference is unset, +inf, until it does.
-//
 // What binds: one exponential per logit in attn and one in score, 16 a clock and SM, and 128 x 128 x d x 4
 // operations of a tile at 8192 a clock, 1024 clocks each for d = 128.  They overlap in part: the special-function unit runs at
 // 45 % of its rate in attn and at 53 % in score, the tensor pipe at 41 % and 21 %, and neither is full (a chunk of 2048 tokens
@@ -35,8 +31,7 @@
 // the most part, at 1.7e-3 of the outputs' norm (bf16) and at 2.0e-4 where one term has 2.2e-4 (fp16).
 #include <type_traits>
 
-#include "paged.cuh"
-#include "tc_sm100.cuh"
+#include "paged_tc.cuh"
 
 namespace a2sf {
 
@@ -44,9 +39,8 @@ A2SF_DEBUG_TRANSLATION_UNIT(paged_attn_tc)
 
 namespace {
 
-using namespace tc;
+using namespace paged_tc;
 
-constexpr int kBlk = 128;                    // rows per tile = TMEM lanes; key slots per tile
 constexpr int kSms = 148;
 constexpr int kSplitBelow = 4 * kSms;        // items of a call from which none is cut
 constexpr int kPieces = 4 * kSms;            // pieces that cutting makes at most, next to one per item
@@ -67,7 +61,7 @@ constexpr int kScoreCtas = 2 * kSms;
 struct Item {                                // of one head; all heads have the same
     int b, pair, t0, t1;                     // key tiles t0 .. t1-1
     int part;                                // -1: whole; else index of its partial result
-    int past, len, skip;                     // of its sequence, in near slots of the pair, and what they leave out
+    int past, len, pad;                      // of its sequence
 };
 struct Merge {
     int b, pair, n, part;                    // partial results part .. part + n - 1
@@ -94,19 +88,9 @@ __device__ __forceinline__ int pair_key_tiles(const SeqState &st, int pair, int 
     return (st.past + min((pair + 1) * pair_tokens, st.len) + kBlk - 1) / kBlk;
 }
 
-// past of the pair's rows in near slots
-template <bool Win> __device__ __forceinline__ SeqState pair_state(const PagedView &pv, SeqState st, int pair, int pair_tokens, int &skip)
-{
-    const Near near = near_slots<Win>(pv, st.past, pair * pair_tokens);
-    st.past = near.past;
-    skip = near.skip;
-    return st;
-}
-
 // The item list.  Cutting items into pieces of p tiles makes sum(ceil(T / p)) of them; CTAs take them in
 // rounds, so a call takes about  max(ceil(pieces / SMs) * (mean length + kItemCost), longest + kItemCost):
 // lengths between a quarter and one and a half of an SM's even share are tried, and no cut at all.
-template <bool Win>
 __global__ void __launch_bounds__(kPlanThreads)
 paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ TcWs ws)
 {
@@ -123,8 +107,7 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
     __syncthreads();
     auto measure = [&](int x) -> int {
         const int b = x / ws.pairs, p = x - b * ws.pairs;
-        int skip;
-        const SeqState st = pair_state<Win>(pv, seqs[b], p, ws.pair_tokens, skip);
+        const SeqState st = seqs[b];
         return p * ws.pair_tokens < st.len ? pair_key_tiles(st, p, ws.pair_tokens) : 0;
     };
     auto item_tiles = [&](int x) -> int { return x < kPlanCache ? tiles[x] : measure(x); };
@@ -202,8 +185,7 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
         const int t = item_tiles(x);
         if (!t) continue;
         const int n = (t - 1) / piece + 1, b = x / ws.pairs, p = x - b * ws.pairs;
-        int skip;
-        const SeqState st = pair_state<Win>(pv, seqs[b], p, ws.pair_tokens, skip);
+        const SeqState st = seqs[b];
         int at = atomicAdd(&level[level_of((t + n - 1) / n)], n);
         int part = -1;
         if (n > 1) {
@@ -213,119 +195,10 @@ paged_plan_kernel(const __grid_constant__ PagedView pv, const __grid_constant__ 
         }
         for (int s = 0; s < n; ++s, ++at)
             if (A2SF_IN_RANGE(at, ws.max_items, kDbgPagedTc) && at < ws.max_items)
-                ws.items[at] = Item{b, p, (int)((long long)t * s / n), (int)((long long)t * (s + 1) / n), n > 1 ? part + s : -1, st.past, st.len, skip};
+                ws.items[at] = Item{b, p, (int)((long long)t * s / n), (int)((long long)t * (s + 1) / n), n > 1 ? part + s : -1, st.past, st.len, 0};
     }
     __syncthreads();
     if (tid == 0) ws.head->merges = n_merges;
-}
-
-__device__ __forceinline__ float ex2_approx(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// Two fp32 operations per instruction (packed arithmetic on register pairs).
-__device__ __forceinline__ uint64_t pack_f32x2(uint32_t lo, uint32_t hi)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack_f32x2(uint64_t v, float &lo, float &hi)
-{
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
-template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b)
-{
-    const __half2 v = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-
-// Four lanes hold four 16-byte pieces of a row each; afterwards lane i holds piece i of all four rows, so that a
-// store instruction covers 64 consecutive bytes of 8 rows and not 16 bytes of 32.
-__device__ __forceinline__ void transpose4(uint4 (&p)[4])
-{
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int step = 1; step <= 2; step <<= 1) {
-        const bool up = lane & step;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            if (x & step) continue;
-            const int y = x | step;                         // keep x (lower lane) or y (upper lane), exchange the other
-            uint4 send = up ? p[x] : p[y], got;
-            got.x = __shfl_xor_sync(0xffffffffu, send.x, step);
-            got.y = __shfl_xor_sync(0xffffffffu, send.y, step);
-            got.z = __shfl_xor_sync(0xffffffffu, send.z, step);
-            got.w = __shfl_xor_sync(0xffffffffu, send.w, step);
-            if (up) p[x] = got;
-            else    p[y] = got;
-        }
-    }
-}
-
-template <int D> struct Tile {
-    static constexpr int kHalves = D / 64;                  // 64-element swizzled columns
-    static constexpr int kHalfBytes = kBlk * 128;
-    static constexpr int kBytes = kHalves * kHalfBytes;
-};
-
-__device__ __forceinline__ uint64_t kmajor_desc(uint32_t smem_addr) { return make_sdesc_sw128(smem_addr, 16, 1024); }
-
-// S = A B^T over D elements: step k starts (k / 4) halves + (k % 4) * 32 bytes into the tiles
-template <int D>
-__device__ __forceinline__ void issue_qk(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc)
-{
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-        const uint64_t off = (uint64_t)(((k >> 2) * Tile<D>::kHalfBytes + (k & 3) * 32) >> 4);
-        umma_ss(d_tmem, a_desc + off, b_desc + off, idesc, k > 0);
-    }
-}
-
-// Boxes of key tile t that hold tokens, and one lane's share of the copy (lane i: box i).
-struct PageTile {
-    int box, boxes;
-};
-template <bool Win = false> __device__ __forceinline__ PageTile page_tile(const PagedView &pv, int t, int used)
-{
-    PageTile p;
-    p.box = box_rows<Win>(pv, kBlk);
-    p.boxes = min(kBlk / p.box, (used - t * kBlk + p.box - 1) / p.box);
-    return p;
-}
-template <int D>
-__device__ __forceinline__ void copy_page_tile(uint8_t *dst, const CUtensorMap *map, uint64_t *bar, const PageTile &p, int row)
-{
-    const int lane = threadIdx.x & 31;
-    if (lane < p.boxes)
-#pragma unroll
-        for (int x = 0; x < Tile<D>::kHalves; ++x) tma_load_2d(dst + x * Tile<D>::kHalfBytes + lane * p.box * 128, map, bar, x * 64, row);
-}
-template <int D>
-__device__ __forceinline__ void copy_query_tile(uint8_t *dst, const CUtensorMap *map, uint64_t *bar, int head, int token, int b)
-{
-#pragma unroll
-    for (int x = 0; x < Tile<D>::kHalves; ++x) tma_load_4d(dst + x * Tile<D>::kHalfBytes, map, bar, x * 64, head, token, b);
 }
 
 // ============================================================================================
@@ -352,7 +225,7 @@ struct AttnShared {
 template <int D> constexpr size_t attn_smem() { return (size_t)Tile<D>::kBytes * (2 + kKStages + kVStages) + sizeof(AttnShared); }
 static_assert(attn_smem<128>() <= 227 * 1024, "attention shared memory");
 
-template <typename T, int D, bool Win>
+template <typename T, int D>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendArgs a, const __grid_constant__ TcWs ws)
@@ -412,7 +285,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     auto dealt = [&](int round) { return round * (int)gridDim.x + (round & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x); };
     // what an item means to every role
     struct Job {
-        int b, h, i0, tokens, t0, nt, ntA, ntB, past, used, part, skip;
+        int b, h, i0, tokens, t0, nt, ntA, ntB, past, used, part;
     };
     auto job = [&](int unit) -> Job {
         Job j;
@@ -424,7 +297,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             it.b = rest / pv.H;
             j.h = rest - it.b * pv.H;
             it.pair = ws.pairs - 1 - back;
-            const SeqState st = pair_state<Win>(pv, seq_state(pv, it.b), it.pair, ws.pair_tokens, it.skip);
+            const SeqState st = seq_state(pv, it.b);
             it.past = st.past; it.len = st.len; it.part = -1;
             it.t0 = 0;
             it.t1 = it.pair * ws.pair_tokens < st.len ? pair_key_tiles(st, it.pair, ws.pair_tokens) : 0;
@@ -436,7 +309,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             j.h = rest / n_items;
         }
         j.b = it.b;
-        j.past = it.past; j.used = it.past + it.len; j.skip = it.skip;
+        j.past = it.past; j.used = it.past + it.len;
         j.i0 = it.pair * ws.pair_tokens;
         j.tokens = min(ws.pair_tokens, it.len - j.i0);
         j.t0 = it.t0;
@@ -471,13 +344,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             ++n;
             for (int t = 0; t < j.nt; ++t, ++kt) {
                 const int tile = j.t0 + t, ks = kt % kKStages, vs = kt % kVStages;
-                const PageTile p = page_tile<Win>(pv, tile, j.used);
+                const PageTile p = page_tile(pv, tile, j.used);
                 const int slot = tile * kBlk + lane * p.box;
                 int row = 0;
-                if (lane < p.boxes) {
-                    const int real = real_slot<Win>(pv, Near{0, j.skip, 0}, slot);
-                    row = (int)pool_row(pv, page_for_read(pv, table, real), j.h, real);
-                }
+                if (lane < p.boxes) row = (int)pool_row(pv, page_for_read(pv, table, slot), j.h, slot);
                 const uint32_t bytes = (uint32_t)(p.boxes * p.box * 128 * Tile<D>::kHalves);
                 ok = 1;
                 if (lane == 0) {
@@ -555,19 +425,6 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     fence_async_smem();
                     __syncwarp();
                 }
-                if constexpr (Win) {
-                    // nor what lies between the sinks and the window of the pair's first row
-                    const int tile0 = (j.t0 + t) * kBlk, from = max(pv.sinks - tile0, 0), to = min(max(j.past + j.i0 + 1 - pv.window, 0) - tile0, kBlk);
-                    if (from < to) {
-                        uint8_t *V = Vs + vs * kTileBytes;
-                        for (int x = lane; x < Tile<D>::kHalves * (to - from) * 8; x += 32) {
-                            const int piece = x & 7, row = from + (x >> 3) % (to - from), half = (x >> 3) / (to - from);
-                            *reinterpret_cast<uint4 *>(V + half * Tile<D>::kHalfBytes + row * 128 + piece * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_async_smem();
-                        __syncwarp();
-                    }
-                }
 #pragma unroll
                 for (int X = 0; X < 2; ++X) {
                     if (t >= ntX[X]) continue;
@@ -617,19 +474,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 tmem_ld32(sp + 32, v[1]);
                 tmem_wait_ld();
                 const int tile0 = (j.t0 + t) * kBlk;
-                if constexpr (Win) {
-                    // the window of the stream's last row begins behind the tile's first slot, or some row ends before its last
-                    const int first_top = j.past + first_token + 1, last_top = min(first_top + tile_tokens - 1, j.used);
-                    if (tile0 + kBlk > first_top || tile0 < last_top - pv.window) {
-                        const int top = min(first_top + r_tok, j.used) - tile0 - half * 64;
-                        const int low = top - pv.window, sinks = min(top, pv.sinks - tile0 - half * 64);
-#pragma unroll
-                        for (int c = 0; c < 2; ++c)
-#pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                if (c * 32 + x >= sinks && (c * 32 + x >= top || c * 32 + x < low)) v[c][x] = 0xff800000u;
-                    }
-                } else if (tile0 + kBlk > j.past + first_token + 1) {
+                if (tile0 + kBlk > j.past + first_token + 1) {
                     // some row of the tile does not see all of it: a masked logit becomes -inf
                     const int vis = min(j.past + first_token + r_tok + 1, j.used) - tile0 - half * 64;
 #pragma unroll
@@ -664,9 +509,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 bool exact = (t == 0);
                 if (!exact) {
                     rowsum = write_p(-m_x);
-                    bool bad = !(rowsum <= kOptimisticLimit);                // also NaN
-                    // rows behind the chunk hold anything: they must not decide when the others' references move
-                    if constexpr (Win) bad = (bad || m_x == INFINITY) && X * tile_tokens + r_tok < j.tokens;
+                    const bool bad = !(rowsum <= kOptimisticLimit);          // also NaN
                     sh->xch[X][half][r] = bad ? 1.f : 0.f;
                     named_barrier(1 + quarter, 64);                // this quarter's two warps
                     const bool pair_bad = bad || sh->xch[X][half ^ 1][r] != 0.f;
@@ -685,13 +528,11 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (t == 0) {
                         // a piece of the keys may hold none that this row sees (then none of the following
                         // tiles does either): any finite reference gives the zeros that are wanted
-                        m_x = smax == -INFINITY ? (Win ? INFINITY : 0.f) : __fmaf_ru(smax, pv.sl2, -kBelow<T>);
+                        m_x = smax == -INFINITY ? 0.f : __fmaf_ru(smax, pv.sl2, -kBelow<T>);
                         l_x = 0.f;
                     } else {
-                        const bool unset = Win && m_x == INFINITY;
                         const float xmax = fmaf(smax, pv.sl2, -m_x);
-                        const bool grow = !unset && xmax > kRescaleThreshold;
-                        if (unset && smax != -INFINITY) m_x = __fmaf_ru(smax, pv.sl2, -kBelow<T>);       // what it has summed are zeros
+                        const bool grow = xmax > kRescaleThreshold;
                         if (grow) {
                             const float before = m_x;
                             m_x = __fmaf_ru(smax, pv.sl2, -kBelow<T>);
@@ -801,7 +642,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (half == 0 && live && done) {
                     if (j.part < 0) {
                         const float z = m_x + log2f(lsum);
-                        if (!Win) ws.lse2[((size_t)j.b * pv.H + j.h) * pv.c * G + (size_t)i * G + g] = z;
+                        ws.lse2[((size_t)j.b * pv.H + j.h) * pv.c * G + (size_t)i * G + g] = z;
                         if (a.lse) a.lse[(((size_t)j.b * pv.H + j.h) * G + g) * pv.c + i] = z * 0.6931471805599453f;
                     } else {
                         ws.part_ml[(size_t)j.part * ws.part_rows + X * kBlk + r] = make_float2(lsum > 0.f ? m_x : -INFINITY, lsum);
@@ -884,7 +725,7 @@ paged_merge_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__
         if (warp == 0 && i >= 0) {
             const int g = (pr % kBlk) % G;
             const float z = mx + log2f(l);
-            if (ws.lse2) ws.lse2[((size_t)mg.b * pv.H + h) * pv.c * G + (size_t)i * G + g] = z;
+            ws.lse2[((size_t)mg.b * pv.H + h) * pv.c * G + (size_t)i * G + g] = z;
             if (a.lse) a.lse[(((size_t)mg.b * pv.H + h) * G + g) * pv.c + i] = z * 0.6931471805599453f;
         }
         __syncthreads();
@@ -1298,7 +1139,7 @@ paged_score_join_kernel(const __grid_constant__ AttendArgs a, const __grid_const
 
 size_t pad(size_t x) { return (x + 255) / 256 * 256; }
 
-TcWs carve(const PagedView &pv, bool windowed, void *mem, size_t *bytes)
+TcWs carve(const PagedView &pv, void *mem, size_t *bytes)
 {
     TcWs w;
     const int tile_tokens = kBlk / pv.G;
@@ -1307,52 +1148,51 @@ TcWs carve(const PagedView &pv, bool windowed, void *mem, size_t *bytes)
     w.pairs = (pv.c + w.pair_tokens - 1) / w.pair_tokens;
     w.part_rows = pv.c <= tile_tokens ? kBlk : 2 * kBlk;
     const size_t U = (size_t)pv.B * pv.H, items = (size_t)pv.B * w.pairs;
-    const size_t cap_tiles = ((size_t)near_capacity(pv, windowed, w.pair_tokens) + kBlk - 1) / kBlk;
+    const size_t cap_tiles = (((size_t)pv.max_pages << pv.ps_shift) + kBlk - 1) / kBlk;
     w.max_items = (int)(items + kMaxParts);
-    // windowed, items are of one length: a plan is for cutting them
-    w.direct = (cap_tiles <= kDirectTiles || (windowed && items * pv.H >= kSplitBelow)) && items * pv.H < 0x7fffffff;
+    w.direct = cap_tiles <= kDirectTiles && items * pv.H < 0x7fffffff;
     w.whole_scores = (pv.c + tile_tokens - 1) / tile_tokens <= kWholeRows;
     size_t parts = w.direct ? 0 : items * pv.H * ((cap_tiles + kMinPiece - 1) / kMinPiece);
     if (parts > kMaxParts) parts = kMaxParts;
     w.parts = (int)parts;
     char *base = static_cast<char *>(mem);
     size_t off = 0;
-    w.lse2 = windowed ? nullptr : reinterpret_cast<float *>(base + off); off += windowed ? 0 : pad(U * pv.c * pv.G * 4);      // for the scores
+    w.lse2 = reinterpret_cast<float *>(base + off); off += pad(U * pv.c * pv.G * 4);
     w.head = reinterpret_cast<PlanHead *>(base + off); off += 256;
     w.items = reinterpret_cast<Item *>(base + off); off += pad(w.max_items * sizeof(Item));
     w.merges = reinterpret_cast<Merge *>(base + off); off += pad(items * sizeof(Merge));
     w.part_ml = reinterpret_cast<float2 *>(base + off); off += pad(parts * w.part_rows * 8);
     w.part_o = reinterpret_cast<float *>(base + off); off += pad(parts * w.part_rows * pv.d * 4);
-    w.score_parts = reinterpret_cast<float *>(base + off); off += windowed ? 0 : pad((size_t)2 * kScoreCtas * kBlk * 4);
+    w.score_parts = reinterpret_cast<float *>(base + off); off += pad((size_t)2 * kScoreCtas * kBlk * 4);
     if (bytes) *bytes = off;
     return w;
 }
 
-template <typename T, int D, bool Win>
+template <typename T, int D>
 cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    cudaError_t e = allow_dynamic_smem<paged_attn_tc_kernel<T, D, Win>>(attn_smem<D>());
-    if (!Win && e == cudaSuccess) e = allow_dynamic_smem<paged_score_tc_kernel<D>>(score_smem<D>());
+    cudaError_t e = allow_dynamic_smem<paged_attn_tc_kernel<T, D>>(attn_smem<D>());
+    if (e == cudaSuccess) e = allow_dynamic_smem<paged_score_tc_kernel<D>>(score_smem<D>());
     if (e != cudaSuccess) return e;
     CUtensorMap mq, mk, mv;
-    const int box = Win ? a.pv.grain : a.pv.ps;
+    const int box = a.pv.ps;
     if (!make_query_map(&mq, dtype, a.q, a.pv, a.sq) || !make_pool_map(&mk, dtype, a.pv.k, a.pv, box) ||
         !make_pool_map(&mv, dtype, a.pv.v, a.pv, box))
         return cudaErrorInvalidValue;
-    const TcWs ws = carve(a.pv, Win, a.ws, nullptr);
+    const TcWs ws = carve(a.pv, a.ws, nullptr);
     if ((long long)ws.max_items * a.pv.H > 0x7fffffffll) return cudaErrorInvalidValue;
     if (!ws.direct) {
-        if ((e = launch_chained(paged_plan_kernel<Win>, 1, kPlanThreads, 0, s, a.pv, ws)) != cudaSuccess) return e;
+        if ((e = launch_chained(paged_plan_kernel, 1, kPlanThreads, 0, s, a.pv, ws)) != cudaSuccess) return e;
         count_launch();
     }
-    e = launch_chained(paged_attn_tc_kernel<T, D, Win>, kSms, kAttnThreads, attn_smem<D>(), s, mq, mk, mv, a, ws);
+    e = launch_chained(paged_attn_tc_kernel<T, D>, kSms, kAttnThreads, attn_smem<D>(), s, mq, mk, mv, a, ws);
     if (e != cudaSuccess) return e;
     count_launch();
     if (!ws.direct) {
         if ((e = launch_chained(paged_merge_kernel<T, D>, 4 * kSms, kMergeThreads, 0, s, a, ws)) != cudaSuccess) return e;
         count_launch();
     }
-    if (Win || !a.scores) return cudaSuccess;
+    if (!a.scores) return cudaSuccess;
     e = launch_chained(paged_score_tc_kernel<D>, kScoreCtas, kScoreThreads, score_smem<D>(), s, mq, mk, a, ws, dtype == A2SF_BF16 ? 1 : 0);
     if (e != cudaSuccess) return e;
     count_launch();
@@ -1362,26 +1202,20 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
     return cudaSuccess;
 }
 
-template <bool Win>
-cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
-{
-    const bool wide = a.pv.d == 128;
-    if (dtype == A2SF_BF16) return wide ? launch<__nv_bfloat16, 128, Win>(dtype, a, s) : launch<__nv_bfloat16, 64, Win>(dtype, a, s);
-    return wide ? launch<__half, 128, Win>(dtype, a, s) : launch<__half, 64, Win>(dtype, a, s);
-}
-
 }  // namespace
 
-size_t attend_tc_ws_bytes(const PagedView &pv, bool windowed)
+size_t attend_tc_ws_bytes(const PagedView &pv)
 {
     size_t bytes = 0;
-    carve(pv, windowed, nullptr, &bytes);
+    carve(pv, nullptr, &bytes);
     return bytes;
 }
 
 cudaError_t launch_attend_tc(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    return a.windowed ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
+    const bool wide = a.pv.d == 128;
+    if (dtype == A2SF_BF16) return wide ? launch<__nv_bfloat16, 128>(dtype, a, s) : launch<__nv_bfloat16, 64>(dtype, a, s);
+    return wide ? launch<__half, 128>(dtype, a, s) : launch<__half, 64>(dtype, a, s);
 }
 
 }  // namespace a2sf
