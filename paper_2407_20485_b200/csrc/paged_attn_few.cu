@@ -18,7 +18,8 @@
 //   whole   instead of both where no sequence can have more than a few tiles: a CTA takes whole units, keeps
 //           logits and partial results in shared memory and ends each unit itself.
 // Windowed (Win): the same over the near slots of a sequence (see Near), which is all that it sees; no logits are kept, and the
-// finish kernel joins outputs alone.
+// finish kernel joins outputs alone.  Few units take a form of their own:
+//   cluster a cluster of CTAs per unit, joined through their shared memory.
 // P goes into P V as two terms of the storage type (off by the square of half a step; one term would be off by half a
 // step of every product, which shows where products cancel), as in the steps of the slot cache.  The memory time hides it: one
 // token over 32 x 40 caches of up to 4096 slots 241 us with one term, 242 with two; four tokens, G = 4, over 2 x 8 x 32,700
@@ -756,6 +757,199 @@ drained:
     }
 }
 
+// ---- windowed, few units: a cluster per unit ---------------------------------------------------------
+// What a unit sees is bounded, so where there are no more units than CTAs fit at once, the CTAs of a cluster share the tiles of one
+// unit evenly, and it is joined through their shared memory: no partial results in the workspace, no second kernel (us, split list
+// with finish kernel and clusters, bf16: 32 heads x 205 slots 7.1 and 6.0; 32 x 1,024: 10.8 and 8.2; 256 x 4,096: 88 and 82; 64 x
+// 4,224 of fp16, 16 rows: 34 and 28).  Where clusters leave half of the device idle the list is faster once a CTA has more than a
+// few tiles (8 x 4,096: 12.6 and 13.3; 8 x 8,192: 14 and 21; 8 x 8,192 of 32 bits, 16 rows: 57 and 106).
+constexpr int kRanks = 8;                    // CTAs of a cluster at most
+constexpr int kRankTiles = 8;                // tiles of a CTA at most, in half-empty devices
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// address of p's place in the shared memory of CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t remote(const void *p, int rank)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float2 remote2(uint32_t at)
+{
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 remote4(uint32_t at)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+template <typename T, int D, int NC>
+__global__ void __launch_bounds__(32 * (warps_of<T> + 1))
+paged_few_cluster_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                         const __grid_constant__ AttendArgs a, int NP, int ranks)
+{
+    using R = Ring<T, D>;
+    using Body = typename BodyOf<T, D, NC, true>::type;
+    constexpr int kTile = R::kTile, kWarps = warps_of<T>, kSlots = kTile / kWarps, kConsumers = 32 * kWarps;
+    // behind the last tile the warps' results, and the CTA's, stand in the ring's place
+    static_assert((size_t)R::kStages * 2 * R::kTileBytes >= (size_t)kFewRows * ((kWarps + 1) * (D * 4 + 8)), "results fit");
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ uint64_t full[R::kStages], empty[R::kStages];
+    __shared__ int abort_word;
+    const PagedView &pv = a.pv;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int u = blockIdx.x / ranks, rank = blockIdx.x - u * ranks;
+    volatile int *abort_flag = &abort_word;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < R::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], kWarps); }
+        abort_word = 0;
+        fence_mbar_init();
+        prefetch_tmap(&map_k);
+        prefetch_tmap(&map_v);
+    }
+    dependency_wait();
+    __syncthreads();
+    dependents_may_start();
+    Where x = {};
+    x.b = u / pv.H;
+    x.h = u - x.b * pv.H;
+    Near near;
+    const SeqState st = near_state<true>(pv, x.b, near);
+    const int used = st.len > 0 ? st.past + st.len : 0, tiles = (used + kTile - 1) / kTile;
+    const int t0 = tiles * rank / ranks, t1 = tiles * (rank + 1) / ranks;
+    float *o = reinterpret_cast<float *>(ring), *joined = o + (size_t)kWarps * NP * D;
+    float2 *ml = reinterpret_cast<float2 *>(joined + NP * D), *joined_ml = ml + kWarps * NP;
+
+    if (warp == 0) {
+        const int box = box_rows<true>(pv, kTile), boxes = kTile / box;
+        const int32_t *table = pv.table + (size_t)x.b * pv.max_pages;
+        const uint64_t policy = policy_evict_first();
+        int it = 0, ok = 1;
+        for (int t = t0; t < t1; ++t, ++it) {
+            const int s = it % R::kStages;
+            const int slot = t * kTile + lane * box;
+            const int nbox = min(boxes, (used - t * kTile + box - 1) / box);
+            int row = 0;
+            if (lane < nbox) {
+                const int real = real_slot<true>(pv, near, slot);
+                row = (int)pool_row(pv, page_for_read(pv, table, real), x.h, real);
+            }
+            if (lane == 0) {
+                if (it >= R::kStages) ok = mbar_wait(&empty[s], ((it / R::kStages) & 1) ^ 1, abort_flag) ? 1 : 0;
+                if (ok) mbar_arrive_expect_tx(&full[s], (uint32_t)(nbox * box * R::kRowBytes * 2));
+            }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            if (!ok) break;
+            if (lane < nbox) {
+                uint8_t *dst = ring + (size_t)s * 2 * R::kTileBytes + lane * box * 128;
+#pragma unroll
+                for (int ch = 0; ch < R::kChunks; ++ch) {
+                    tma_load_2d(dst + ch * (kTile * 128), &map_k, &full[s], ch * (128 / (int)sizeof(T)), row, policy);
+                    tma_load_2d(dst + R::kTileBytes + ch * (kTile * 128), &map_v, &full[s], ch * (128 / (int)sizeof(T)), row, policy);
+                }
+            }
+            __syncwarp();
+        }
+        if (lane == 0 && *abort_flag) {
+            int dummy = 0;                                   // copies still in flight get a bounded chance to land
+            for (int k = max(0, it - R::kStages); k < it; ++k)
+                mbar_wait(&full[k % R::kStages], (k / R::kStages) & 1, &dummy);
+            *pv.status = A2SF_ERR_TIMEOUT;
+        }
+    } else if (used > 0) {
+        const int cw = warp - 1, ct = threadIdx.x - 32;
+        float *scratch = reinterpret_cast<float *>(ring + (size_t)R::kStages * 2 * R::kTileBytes);
+        Body body;
+        body.begin(a, x, st, near, scratch);
+        for (int t = t0, it = 0; t < t1; ++t, ++it) {
+            const int s = it % R::kStages;
+            if (!*abort_flag && !mbar_wait(&full[s], (it / R::kStages) & 1, abort_flag)) *pv.status = A2SF_ERR_TIMEOUT;
+            const int j0 = t * kTile + cw * kSlots;
+            uint8_t *K = ring + (size_t)s * 2 * R::kTileBytes;
+            if (j0 < used) body.tile(a, K, K + R::kTileBytes, cw * kSlots, j0, used, nullptr, NP, scratch);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty[s]);
+        }
+        named_barrier(1, kConsumers);                        // the ring has been read
+        body.end(ml + cw * NP, o + (size_t)cw * NP * D, NP);
+        named_barrier(1, kConsumers);
+        for (int e = ct; e < NP * (D / 4); e += kConsumers) {
+            const int r = e / (D / 4), d4 = e - r * (D / 4);
+            float mx = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) mx = fmaxf(mx, ml[w * NP + r].x);
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float2 y = ml[w * NP + r];
+                if (!(y.y > 0.f)) continue;                  // a warp that saw nothing wrote no output
+                const float f = ex2(y.x - mx);
+                const float4 v = reinterpret_cast<const float4 *>(o + (size_t)(w * NP + r) * D)[d4];
+                l = fmaf(f, y.y, l);
+                sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y);
+                sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+            }
+            reinterpret_cast<float4 *>(joined + r * D)[d4] = sum;
+            if (d4 == 0) joined_ml[r] = make_float2(mx, l);
+        }
+    }
+    __syncwarp();
+    cluster_sync();
+    if (warp != 0) {
+        const int rows = st.len * pv.G;                      // 0 where the sequence takes no part
+        for (int e = rank * kConsumers + (int)threadIdx.x - 32; e < rows * (D / 4); e += ranks * kConsumers) {
+            const int r = e / (D / 4), d4 = e - r * (D / 4);
+            float2 y[kRanks];
+            float mx = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int k = 0; k < kRanks; ++k) {
+                y[k] = k < ranks ? remote2(remote(joined_ml + r, k)) : make_float2(-INFINITY, 0.f);
+                mx = fmaxf(mx, y[k].x);
+            }
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kRanks; ++k) {
+                if (k >= ranks) continue;
+                const float4 v = remote4(remote(joined + r * D + d4 * 4, k));
+                const float f = y[k].y > 0.f ? ex2(y[k].x - mx) : 0.f;
+                l = fmaf(f, y[k].y, l);
+                sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y);
+                sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+            }
+            const int i = r / pv.G, g = r - i * pv.G;
+            const float inv = 1.f / l;
+            T *dst = static_cast<T *>(a.out) + x.b * a.so.b + (int64_t)(x.h * pv.G + g) * a.so.h + (int64_t)i * a.so.t + d4 * 4;
+            dst[0] = Elem<T>::from_float(sum.x * inv);
+            dst[1] = Elem<T>::from_float(sum.y * inv);
+            dst[2] = Elem<T>::from_float(sum.z * inv);
+            dst[3] = Elem<T>::from_float(sum.w * inv);
+            if (d4 == 0 && a.lse) a.lse[((size_t)u * pv.G + g) * pv.c + i] = (mx + log2f(l)) * 0.6931471805599453f;
+        }
+    }
+    __syncwarp();
+    cluster_sync();                                          // no CTA ends while its results are read
+}
+
+// CTAs of a cluster, or 0 where the other forms serve: as many as fit at once, each with a tile at least.
+template <typename T, int D> int cluster_ranks(const PagedView &pv, int slots)
+{
+    const long long units = (long long)pv.B * pv.H;
+    const int tiles = (near_capacity(pv, true, pv.c) + Ring<T, D>::kTile - 1) / Ring<T, D>::kTile;
+    if (units > slots) return 0;
+    int ranks = 1;
+    while (ranks < kRanks && 2 * units * ranks <= slots && 2 * ranks <= tiles) ranks *= 2;
+    return 2 * units * ranks < slots && (tiles + ranks - 1) / ranks > kRankTiles ? 0 : ranks;
+}
+
 // The finish kernel: `blocks` blocks per unit.  Block y joins the output rows y, y + blocks, .. and brings the
 // scores of slots y * chunk .. up to date.  All of it is latency: dependent loads around a few bytes.  So the page
 // numbers and old scores of the first slots are read while the main kernel still drains, the logits and the
@@ -961,6 +1155,15 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     const int row = Win ? a.pv.grain : a.pv.ps, box = row < R::kTile ? row : R::kTile;
     if (!make_pool_map(&mk, dtype, a.pv.k, a.pv, box) || !make_pool_map(&mv, dtype, a.pv.v, a.pv, box)) return cudaErrorInvalidValue;
     const int NP = rows_padded(a.pv.c * a.pv.G);
+    if constexpr (Win) {
+        const int slots = device_sm_count() * (2 * (smem + 2 * 1024) <= 228 * 1024 ? 2 : 1);
+        if (const int ranks = cluster_ranks<T, D>(a.pv, slots)) {
+            if ((e = allow_dynamic_smem<paged_few_cluster_kernel<T, D, NC>>(smem)) != cudaSuccess) return e;
+            e = launch_clusters(paged_few_cluster_kernel<T, D, NC>, (unsigned)(a.pv.B * a.pv.H * ranks), ranks, 32 * (warps_of<T> + 1), smem, s, mk, mv, a, NP, ranks);
+            if (e == cudaSuccess) count_launch();
+            return e;
+        }
+    }
     if (const size_t whole = whole_smem<T, D, NC, Win>(a.pv)) {
         if ((e = allow_dynamic_smem<paged_few_whole_kernel<T, D, NC, Win>>(whole)) != cudaSuccess) return e;
         const long long resident = device_sm_count() * (2 * (whole + sizeof(WholeShared) + 1024) <= 228 * 1024 ? 2 : 1), units = (long long)a.pv.B * a.pv.H;
