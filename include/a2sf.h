@@ -532,7 +532,9 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
  * stays (a2sf_paged_slide).  Page-table entries whose page holds no slot that a row of the call sees are not read, and slots of
  * other pages that no row sees may hold anything.  out has strides of its own and must not overlap q; rows i >= len[b] of out
  * and lse are left as they were.  workspace: as for a2sf_paged_attend, from a2sf_paged_attend_window_workspace_bytes (0 = invalid
- * arguments); its size follows min(sinks + window + c, the capacity of the page table). */
+ * arguments); its size follows min(sinks + window + c, the capacity of the page table), and a call whose size is
+ * A2SF_NO_WORKSPACE_BYTES neither reads nor writes it. */
+#define A2SF_NO_WORKSPACE_BYTES 256
 size_t a2sf_paged_attend_window_workspace_bytes(const a2sf_paged *cache, int32_t c, int32_t window, int32_t sinks);
 int a2sf_paged_attend_window(const a2sf_paged *cache, int32_t c, const int32_t *lens, int32_t window, int32_t sinks,
                              const void *q, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_t,

@@ -48,6 +48,10 @@ class a2sf_rotary_axes_plan(ctypes.Structure):
                 ("check", ctypes.c_int32), ("axes", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("turn", ctypes.c_uint64 * 64), ("axis", ctypes.c_uint8 * 64)]
 
+    def __init__(self, *args):
+        super().__init__(*args)
+        self.at = ctypes.addressof(self)        # what the calls pass on
+
 
 class a2sf_paged(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("group", ctypes.c_int32), ("d", ctypes.c_int32),
@@ -530,9 +534,10 @@ def a2sf_rotary_axes_plan_init(pairs, plans, cycle: bool = False) -> a2sf_rotary
 
 
 def _axes_plan(plan) -> int:
-    if not isinstance(plan, a2sf_rotary_axes_plan):
-        raise ValueError(f"expected a plan of a2sf_rotary_axes_plan_init, got {type(plan).__name__}")
-    return _addressof(plan)
+    try:
+        return plan.at
+    except AttributeError:
+        raise ValueError(f"expected a plan of a2sf_rotary_axes_plan_init, got {type(plan).__name__}") from None
 
 
 def a2sf_rotary_axes(plan: a2sf_rotary_axes_plan, x, positions, out=None, lens=None, transpose=False, stream=None):

@@ -150,7 +150,7 @@ size_t attend_ws_bytes(const PagedView &v, bool windowed, int dtype)
     const Path path = path_of(v, windowed, dtype);
     const size_t bytes = align_up(path == kFew ? attend_few_ws_bytes(dtype, v, windowed) : path == kMma ? attend_mma_ws_bytes(dtype, v, windowed)
                                   : windowed ? window_tc_ws_bytes(v) : attend_tc_ws_bytes(v));
-    return bytes ? bytes : 256;                               // 0 says that arguments are invalid
+    return bytes ? bytes : A2SF_NO_WORKSPACE_BYTES;            // 0 says that arguments are invalid
 }
 
 cudaError_t launch_attend(int dtype, const AttendArgs &a, cudaStream_t s)

@@ -939,9 +939,12 @@ paged_few_cluster_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
     cluster_sync();                                          // no CTA ends while its results are read
 }
 
-// CTAs of a cluster, or 0 where the other forms serve: as many as fit at once, each with a tile at least.
-template <typename T, int D> int cluster_ranks(const PagedView &pv, int slots)
+// CTAs of a cluster, or 0 where the other forms serve: as many as fit at once, each with a tile at least.  What fits is counted for
+// the whole chip, since the size of the workspace, which clusters do without, must not depend on a device.
+template <typename T, int D, int NC> int cluster_ranks(const PagedView &pv)
 {
+    constexpr size_t smem = Ring<T, D>::kBytes + BodyOf<T, D, NC, true>::kScratch;
+    constexpr int slots = kSms * (2 * (smem + 2 * 1024) <= 228 * 1024 ? 2 : 1);
     const long long units = (long long)pv.B * pv.H;
     const int tiles = (near_capacity(pv, true, pv.c) + Ring<T, D>::kTile - 1) / Ring<T, D>::kTile;
     if (units > slots) return 0;
@@ -1156,8 +1159,7 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     if (!make_pool_map(&mk, dtype, a.pv.k, a.pv, box) || !make_pool_map(&mv, dtype, a.pv.v, a.pv, box)) return cudaErrorInvalidValue;
     const int NP = rows_padded(a.pv.c * a.pv.G);
     if constexpr (Win) {
-        const int slots = device_sm_count() * (2 * (smem + 2 * 1024) <= 228 * 1024 ? 2 : 1);
-        if (const int ranks = cluster_ranks<T, D>(a.pv, slots)) {
+        if (const int ranks = cluster_ranks<T, D, NC>(a.pv)) {
             if ((e = allow_dynamic_smem<paged_few_cluster_kernel<T, D, NC>>(smem)) != cudaSuccess) return e;
             e = launch_clusters(paged_few_cluster_kernel<T, D, NC>, (unsigned)(a.pv.B * a.pv.H * ranks), ranks, 32 * (warps_of<T> + 1), smem, s, mk, mv, a, NP, ranks);
             if (e == cudaSuccess) count_launch();
@@ -1199,38 +1201,45 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     return e;
 }
 
-template <typename T, int D, bool Win>
-cudaError_t launch_d(int dtype, const AttendArgs &a, cudaStream_t s)
+// The kernels' types, head size and rows for a call, as a value that a generic function takes apart.
+template <typename T, int D, int NC> struct Form {};
+
+template <typename T, int D, typename F> auto with_rows(int rows, F f)
 {
-    const int rows = a.pv.c * a.pv.G;
     if constexpr (sizeof(T) == 4) {
         switch (rows_padded(rows)) {
-        case 1: return launch_nc<T, D, 1, Win>(dtype, a, s);
-        case 2: return launch_nc<T, D, 2, Win>(dtype, a, s);
-        case 4: return launch_nc<T, D, 4, Win>(dtype, a, s);
-        case 8: return launch_nc<T, D, 8, Win>(dtype, a, s);
-        default: return launch_nc<T, D, 16, Win>(dtype, a, s);
+        case 1: return f(Form<T, D, 1>());
+        case 2: return f(Form<T, D, 2>());
+        case 4: return f(Form<T, D, 4>());
+        case 8: return f(Form<T, D, 8>());
+        default: return f(Form<T, D, 16>());
         }
     } else {
-        return rows <= 4 ? launch_nc<T, D, 4, Win>(dtype, a, s) : rows <= 8 ? launch_nc<T, D, 8, Win>(dtype, a, s) : launch_nc<T, D, 16, Win>(dtype, a, s);
+        return rows <= 4 ? f(Form<T, D, 4>()) : rows <= 8 ? f(Form<T, D, 8>()) : f(Form<T, D, 16>());
+    }
+}
+template <typename F> auto with_form(int dtype, const PagedView &pv, F f)
+{
+    const int rows = pv.c * pv.G;
+    const bool wide = pv.d == 128;
+    switch (dtype) {
+    case A2SF_F32: return wide ? with_rows<float, 128>(rows, f) : with_rows<float, 64>(rows, f);
+    case A2SF_BF16: return wide ? with_rows<__nv_bfloat16, 128>(rows, f) : with_rows<__nv_bfloat16, 64>(rows, f);
+    default: return wide ? with_rows<__half, 128>(rows, f) : with_rows<__half, 64>(rows, f);
     }
 }
 
-template <bool Win>
-cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
+template <bool Win, typename T, int D, int NC> cudaError_t launch(Form<T, D, NC>, int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    const bool wide = a.pv.d == 128;
-    switch (dtype) {
-    case A2SF_F32: return wide ? launch_d<float, 128, Win>(dtype, a, s) : launch_d<float, 64, Win>(dtype, a, s);
-    case A2SF_BF16: return wide ? launch_d<__nv_bfloat16, 128, Win>(dtype, a, s) : launch_d<__nv_bfloat16, 64, Win>(dtype, a, s);
-    default: return wide ? launch_d<__half, 128, Win>(dtype, a, s) : launch_d<__half, 64, Win>(dtype, a, s);
-    }
+    return launch_nc<T, D, NC, Win>(dtype, a, s);
 }
+template <typename T, int D, int NC> int ranks_of(Form<T, D, NC>, const PagedView &pv) { return cluster_ranks<T, D, NC>(pv); }
 
 }  // namespace
 
 size_t attend_few_ws_bytes(int dtype, const PagedView &pv, bool windowed)
 {
+    if (windowed && with_form(dtype, pv, [&](auto form) { return ranks_of(form, pv); }) > 0) return 0;
     size_t bytes = 0;
     carve(dtype, pv, windowed, nullptr, &bytes);
     return bytes;
@@ -1238,7 +1247,7 @@ size_t attend_few_ws_bytes(int dtype, const PagedView &pv, bool windowed)
 
 cudaError_t launch_attend_few(int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    return a.windowed ? launch<true>(dtype, a, s) : launch<false>(dtype, a, s);
+    return with_form(dtype, a.pv, [&](auto form) { return a.windowed ? launch<true>(form, dtype, a, s) : launch<false>(form, dtype, a, s); });
 }
 
 }  // namespace a2sf

@@ -194,9 +194,7 @@ public:
         const Rows yr(out, qs, type_, device_, "out");
         float *z = array<float>(lse, {qs[0], qs[1], c}, device_, "lse");
         const int32_t *ln = array<int32_t>(lens, {p_.B}, device_, "lens");
-        auto &sizes = window_bytes_[{window, sinks}];
-        if (window_bytes_.size() > 256) { window_bytes_.clear(); return attend_window(q, window, sinks, lens, out, lse, workspace, stream); }
-        const Tensor ws = space(workspace, sizes, c, [&](const a2sf_paged *p, int32_t n) { return fn.window_bytes(p, n, (int32_t)window, (int32_t)sinks); });
+        const Tensor ws = window_space(workspace, c, window, sinks);
         const int rc = fn.attend_window(&p_, (int32_t)c, ln, (int32_t)window, (int32_t)sinks, qr.p, qr.b, qr.h, qr.t, yr.p, yr.b, yr.h, yr.t, z, ws.data_ptr(),
                                         (size_t)ws.numel(), at.stream);
         return {rc, out, lse};
@@ -274,10 +272,22 @@ private:
         }
         return at::empty({it->second}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, (c10::DeviceIndex)device_));
     }
+    // ... of a windowed call: what no kernel touches may be the same memory for all calls
+    Tensor window_space(const OptTensor &given, int64_t c, int64_t window, int64_t sinks)
+    {
+        if (window_bytes_.size() > 256) window_bytes_.clear();
+        auto &sizes = window_bytes_[{window, sinks}];
+        const auto it = sizes.find(c);
+        if (!given && none_.defined() && it != sizes.end() && it->second == A2SF_NO_WORKSPACE_BYTES) return none_;
+        const Tensor ws = space(given, sizes, c, [&](const a2sf_paged *p, int32_t n) { return fn.window_bytes(p, n, (int32_t)window, (int32_t)sinks); });
+        if (!given && ws.numel() == A2SF_NO_WORKSPACE_BYTES) none_ = ws;
+        return ws;
+    }
 
     a2sf_paged p_;
     int device_;
     at::ScalarType type_;
+    Tensor none_;                                            // a workspace for calls that need none
     std::unordered_map<int64_t, int64_t> attend_bytes_, evict_bytes_;
     std::map<std::pair<int64_t, int64_t>, std::unordered_map<int64_t, int64_t>> window_bytes_;      // by window and sinks
 };
