@@ -11,10 +11,9 @@
 //   may have left fp16's range: then the half is done again against the row's maximum and the accumulator rescaled.  Until
 //   a row has seen a slot its reference is unset, +inf.  Blocks of 32 rows x 32 slots that no row of theirs sees cost no exponential.
 //
-//   All items of a call are about as long as the window.  The tiles of all (sequence, head, pair) items are one list, of which
-//   every CTA takes an equal part, and a part that begins or ends inside an item leaves partial results that the merge kernel
-//   joins; or, where that costs more than the last round of items leaves idle, whole items.  The list is not written down: a CTA sums
-//   the tiles of all pairs itself and finds its own place.
+//   All items of a call are about as long as the window, so they are dealt in turn.  Where there are few, their tiles are one list, of
+//   which every CTA takes an equal part, and a part that begins or ends inside an item leaves partial results that the merge kernel
+//   joins.  The list is not written down: a CTA sums the lengths itself and finds its own place.
 //
 // What binds: one exponential per logit, 16 a clock and SM, and 128 x 128 x d x 4 operations of a tile at 8192 a clock: 2048 clocks
 // each for a pair of tiles, d = 128.
@@ -41,9 +40,10 @@ constexpr float kRescaleThreshold = 8.0f;    // log2 units above the reference; 
 // 2^-24, so with 8 these are 2^-22 and 2^-32 of the maximum, and 64 logits that all equal it have half of the limit.
 template <typename T> constexpr float kBelow = std::is_same<T, __half>::value ? 8.f : 0.f;
 
-// Division of the work, in tiles: what an item costs beside its own (set-up, epilogue), what the merge kernel costs, and how near
+// Division of the list, in tiles: what an item costs beside its own (set-up, epilogue), what the merge kernel costs, and how near
 // an end of an item a cut goes to that end instead.
-constexpr int kItemCost = 1, kMergeCost = 4, kSnap = 2;
+constexpr int kItemCost = 2, kMergeCost = 4, kSnap = 2;
+constexpr int kItemSlots = kItemCost * kBlk + kBlk / 2;      // with what rounding to whole tiles adds
 constexpr int kCutBelow = 6 * kSms;          // items of a call (by its capacity) from which none is cut: the last round is short
 
 struct Desc {                                // of the item that CTA k cuts and began: its pieces, 0 where there is none
@@ -65,72 +65,77 @@ __device__ __forceinline__ int pair_tiles(const PagedView &pv, const SeqState &s
     return (near.past + min((pair + 1) * pair_tokens, st.len) + kBlk - 1) / kBlk;
 }
 
-// An item's length in the list.
-__device__ __forceinline__ int pair_cost(const PagedView &pv, const SeqState &st, int pair, int pair_tokens)
-{
-    return kItemCost + pair_tiles(pv, st, pair, pair_tokens);
-}
+// The list's lengths are estimates in slots, so that sums over a sequence's pairs are closed forms.  A pair whose window is full has
+// C near slots, but for its place in a grain; the E pairs before have all slots up to their own last.
+struct Lengths {
+    long long past, full;        // full: C
+    int pair_tokens, pairs, early, tail;                     // tail: tokens that the last pair lacks
+
+    __device__ Lengths(const PagedView &pv, const SeqState &st, int pt) : past(st.past), full((long long)pt + pv.window - 1 + pv.sink_end + pv.grain / 2), pair_tokens(pt)
+    {
+        pairs = pair_count(st, pt);
+        const long long e = (full - 1 - past) / pt;
+        early = full - 1 < past ? 0 : (int)min(e, (long long)pairs);
+        tail = pairs * pt - st.len;
+    }
+    // of the first p pairs of one head
+    __device__ long long sum(int p) const
+    {
+        const long long e = min(p, early);
+        return e * past + pair_tokens * (e * (e + 1) / 2) + (p - e) * full + (long long)p * kItemSlots - (p == pairs ? tail : 0);
+    }
+};
 
 // prefix[0 .. B] of the lengths of one head, and the number of its items, by the whole block
-__device__ __forceinline__ void count_tiles(long long *prefix, int *items, const PagedView &pv, int pair_tokens)
+__device__ __forceinline__ void sum_lengths(long long *prefix, int *items, const PagedView &pv, int pair_tokens)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    if (threadIdx.x == 0) *items = 0;
-    __syncthreads();
-    for (int b0 = warp * 32; b0 < pv.B; b0 += warps * 32) {
-        const int b = b0 + lane;
-        SeqState st = {0, 0};
-        if (b < pv.B) st = seq_state(pv, b);
-        const int pairs = pair_count(st, pair_tokens), most = __reduce_max_sync(0xffffffffu, pairs);
-        int sum = 0;
-        if (most <= 16) {                                    // a lane counts its own sequence's, or all lanes one sequence's
-            for (int p = 0; p < pairs; ++p) sum += pair_cost(pv, st, p, pair_tokens);
-        } else {
-            for (int s = 0; s < 32; ++s) {
-                const int n = __shfl_sync(0xffffffffu, pairs, s);
-                SeqState other;
-                other.past = __shfl_sync(0xffffffffu, st.past, s);
-                other.len = __shfl_sync(0xffffffffu, st.len, s);
-                int part = 0;
-                for (int p = lane; p < n; p += 32) part += pair_cost(pv, other, p, pair_tokens);
-                if (n) part = __reduce_add_sync(0xffffffffu, part);
-                if (lane == s) sum = part;
-            }
-        }
-        if (b < pv.B) prefix[b + 1] = sum;
-        const int all = __reduce_add_sync(0xffffffffu, pairs);
-        if (lane == 0) atomicAdd(items, all);
+    for (int b = threadIdx.x; b < pv.B; b += blockDim.x) {
+        const SeqState st = seq_state(pv, b);
+        const Lengths x(pv, st, pair_tokens);
+        prefix[b + 1] = st.len > 0 ? x.sum(x.pairs) : 0;
     }
     __syncthreads();
-    if (warp == 0) {
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
         long long run = 0;
+        int count = 0;
         for (int b0 = 0; b0 < pv.B; b0 += 32) {
-            long long incl = b0 + lane < pv.B ? prefix[b0 + lane + 1] : 0;
+            const int b = b0 + lane;
+            long long incl = b < pv.B ? prefix[b + 1] : 0;
+            if (b < pv.B) count += pair_count(seq_state(pv, b), pair_tokens);
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const long long x = __shfl_up_sync(0xffffffffu, incl, o);
                 if (lane >= o) incl += x;
             }
-            if (b0 + lane < pv.B) prefix[b0 + lane + 1] = run + incl;
+            if (b < pv.B) prefix[b + 1] = run + incl;
             run += __shfl_sync(0xffffffffu, incl, 31);
         }
-        if (lane == 0) prefix[0] = 0;
+        count = __reduce_add_sync(0xffffffffu, count);
+        if (lane == 0) {
+            prefix[0] = 0;
+            *items = count;
+        }
     }
     __syncthreads();
 }
 
-// Where a CTA's part begins: tile t of an item (t = its tiles: the next item), and the place in the list.
+// Where a CTA's part begins: tile t of an item (t = its tiles: the next item).
 struct Place {
     int b, h, pair, t;
-    long long w;
+    long long w, item;           // place in the list, and the item's
 };
 
-// The cut before part k of the list, by one warp: inside an item, or where it begins or ends, whichever is nearer.
-__device__ __forceinline__ Place cut_before(const long long *prefix, const PagedView &pv, int pair_tokens, int k, int parts, bool inside)
+// Tile of the item that a cut `in` slots behind its place goes through.
+__device__ __forceinline__ int tile_at(long long in) { return (int)((in - kItemSlots) >> 7); }
+static_assert(kBlk == 128, "tile_at");
+
+// The cut before part k of the list.
+__device__ __forceinline__ Place cut_before(const long long *prefix, const PagedView &pv, int pair_tokens, int k)
 {
-    const int lane = threadIdx.x & 31;
-    const long long total = pv.H * prefix[pv.B], w = total * k / parts;
-    if (w >= total) return Place{pv.B, 0, 0, 0, total};
+    const unsigned long long total = pv.H * prefix[pv.B];
+    const long long w = (long long)(total * k / (unsigned)kSms);
+    if (w >= (long long)total) return Place{pv.B, 0, 0, 0, w, w};
     int lo = 0, hi = pv.B - 1;                               // last b with H * prefix[b] <= w
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -138,37 +143,27 @@ __device__ __forceinline__ Place cut_before(const long long *prefix, const Paged
         else hi = mid - 1;
     }
     const SeqState st = seq_state(pv, lo);
-    const long long rest = w - pv.H * prefix[lo];
-    const int each = (int)(prefix[lo + 1] - prefix[lo]), pairs = pair_count(st, pair_tokens);
-    Place x = {lo, (int)(rest / each), 0, 0, w};
-    int at = (int)(rest - (long long)x.h * each);            // among the head's items
-    for (int p0 = 0; p0 < pairs; p0 += 32) {
-        const int own = p0 + lane < pairs ? pair_cost(pv, st, p0 + lane, pair_tokens) : 0;
-        int incl = own;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += y;
-        }
-        const unsigned beyond = __ballot_sync(0xffffffffu, incl > at);
-        if (!beyond) {
-            at -= __shfl_sync(0xffffffffu, incl, 31);
-            continue;
-        }
-        const int f = __ffs(beyond) - 1, cost = __shfl_sync(0xffffffffu, own, f);
-        const int in = at - (__shfl_sync(0xffffffffu, incl, f) - cost);      // of the item
-        x.pair = p0 + f;
-        if (inside ? in <= kItemCost + kSnap : 2 * in < cost) {
-            x.w -= in;
-        } else if (!inside || cost - in <= kSnap) {
-            x.w += cost - in;
-            x.t = cost - kItemCost;
-        } else {
-            x.t = in - kItemCost;
-        }
-        break;
+    const Lengths x(pv, st, pair_tokens);
+    const long long rest = w - pv.H * prefix[lo], each = prefix[lo + 1] - prefix[lo];
+    int h = (int)__fdividef((float)rest, (float)each);       // nearly
+    while (h * each > rest) --h;
+    while ((h + 1) * each <= rest) ++h;
+    const long long at = rest - h * each;                    // among the head's items
+    int p = 0, last = x.pairs - 1;                           // last pair with sum(p) <= at
+    while (p < last) {
+        const int mid = (p + last + 1) >> 1;
+        if (x.sum(mid) <= at) p = mid;
+        else last = mid - 1;
     }
-    return x;
+    const long long in = at - x.sum(p), length = x.sum(p + 1) - x.sum(p);
+    const int tiles = pair_tiles(pv, st, p, pair_tokens), t = tile_at(in);
+    Place y = {lo, h, p, 0, w - in, w - in};
+    if (t > kSnap) {
+        const bool end = tiles - t <= kSnap;
+        y.t = end ? tiles : t;
+        y.w = end ? w - in + length : w;
+    }
+    return y;
 }
 
 struct Job {
@@ -177,28 +172,30 @@ struct Job {
     int from[2], to[2];                      // ... of each stream: it sees nothing before and behind
 };
 
-// Walks over a CTA's part of the list.
+// Walks over a CTA's items: its part of the list, or one of every gridDim, in rounds of alternating direction.
 struct Walk {
     const PagedView &pv;
-    const Place &end;
+    Place end;
     int pair_tokens, tile_tokens, b, h, pair, t, pairs;
     SeqState st;
-    bool more;
+    bool more, inside, back;     // back: the next round runs backwards
 
-    __device__ Walk(const PagedView &v, int pt, const Place &at, const Place &e) : pv(v), end(e), pair_tokens(pt), tile_tokens(kBlk / v.G), b(at.b), h(at.h), pair(at.pair), t(at.t), more(at.w < e.w)
+    // whole items, dealt in turn
+    __device__ Walk(const PagedView &v, int pt) : pv(v), end{}, pair_tokens(pt), tile_tokens(kBlk / v.G), b(-1), h(0), pair(0), t(0), inside(false), back(true)
+    {
+        sequence();
+        skip(blockIdx.x);
+    }
+    // a part of the list
+    __device__ Walk(const PagedView &v, int pt, const Place &at, const Place &e) : pv(v), end(e), pair_tokens(pt), tile_tokens(kBlk / v.G), b(at.b), h(at.h), pair(at.pair), t(at.t), more(at.w < e.w), inside(true), back(false)
     {
         st = b < pv.B ? seq_state(pv, b) : SeqState{0, 0};
         pairs = pair_count(st, pair_tokens);
-        if (more && t >= pair_tiles(pv, st, pair, pair_tokens)) advance();
+        if (more && t >= pair_tiles(pv, st, pair, pair_tokens)) skip(1);
     }
-    __device__ void advance()
+    // the next sequence that has a part in the call, 32 at a time
+    __device__ void sequence()
     {
-        t = 0;
-        if (++pair < pairs) return;
-        pair = 0;
-        if (++h < pv.H) return;
-        h = 0;
-        // the next sequence that has a part in the call, 32 at a time
         const int lane = threadIdx.x & 31;
         for (int b0 = b + 1; b0 < pv.B; b0 += 32) {
             SeqState s = {0, 0};
@@ -210,9 +207,23 @@ struct Walk {
             st.past = __shfl_sync(0xffffffffu, s.past, f);
             st.len = __shfl_sync(0xffffffffu, s.len, f);
             pairs = pair_count(st, pair_tokens);
+            more = true;
             return;
         }
         more = false;
+    }
+    // so many items on
+    __device__ void skip(int items)
+    {
+        t = 0;
+        unsigned at = (unsigned)h * pairs + pair + items;    // the launch sees to it that a call's items are a 31-bit number
+        while (more && at >= (unsigned)pv.H * pairs) {
+            at -= (unsigned)pv.H * pairs;
+            sequence();
+        }
+        if (!more) return;
+        h = (int)(at / (unsigned)pairs);
+        pair = (int)at - h * pairs;
     }
     __device__ bool next(Job &j)
     {
@@ -224,7 +235,7 @@ struct Walk {
         const int tokens = min(pair_tokens, st.len - j.i0);
         j.tiles = (j.past + j.i0 + tokens + kBlk - 1) / kBlk;
         j.t0 = t;
-        const bool last = b == end.b && h == end.h && pair == end.pair;
+        const bool last = inside && b == end.b && h == end.h && pair == end.pair;
         j.t1 = last ? min(j.tiles, end.t) : j.tiles;
         if (j.t1 <= t) {
             more = false;
@@ -238,7 +249,8 @@ struct Walk {
         j.from[1] = max(j.t0, begin1);
         j.to[1] = tokens > tile_tokens ? j.t1 : 0;
         if (last) more = false;
-        else      advance();
+        else      skip(inside ? 1 : back ? 2 * (int)(gridDim.x - blockIdx.x) - 1 : 2 * (int)blockIdx.x + 1);
+        back = !back;
         return true;
     }
 };
@@ -259,7 +271,7 @@ struct Shared {
     uint64_t s_full[2][2], p_full[2][2], o_done[2][2];      // per stream and half: logits, probabilities, products with values
     uint64_t job_full[kJobs], job_empty[kJobs];
     uint32_t tmem_base;
-    int abort_flag, items;
+    int abort_flag, items, inside;
     Place cut[2];
     JobInfo jobs[kJobs];
 };
@@ -340,6 +352,7 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             }
         }
         sh->abort_flag = smem_u32(smem) & 1023u ? 1 : 0;    // the swizzled tiles need this alignment
+        sh->inside = 0;
         fence_mbar_init();
         prefetch_tmap(&map_q); prefetch_tmap(&map_k); prefetch_tmap(&map_v);
     }
@@ -348,35 +361,29 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         tmem_relinquish();
     }
     dependency_wait();
-    {
+    if (ws.cut) {
         // the CTA's part of the list
         long long *prefix = reinterpret_cast<long long *>(smem);
-        count_tiles(prefix, &sh->items, pv, ws.pair_tokens);
-        const long long total = pv.H * prefix[pv.B], n = (long long)pv.H * sh->items;
-        const int grid = gridDim.x;
-        const float mean = n ? (float)total / (float)n : 0.f, share = (float)total / grid;
-        const bool inside = ws.cut && total >= 8 * grid && share + kItemCost + kMergeCost < fminf((float)((n + grid - 1) / grid) * mean, share + mean);
-        if (warp < 2) {
-            const Place at = cut_before(prefix, pv, ws.pair_tokens, blockIdx.x + warp, grid, inside);
-            if (lane == 0) sh->cut[warp] = at;
-        }
-        __syncthreads();
-        if (ws.cut && threadIdx.x == 0) {
+        sum_lengths(prefix, &sh->items, pv, ws.pair_tokens);
+        const long long total = pv.H * prefix[pv.B];
+        const float n = (float)pv.H * (float)sh->items, mean = n > 0.f ? (float)total / n : 0.f, share = (float)total / kSms;
+        const bool inside = share >= 8.f * kBlk && share + (kItemCost + kMergeCost) * kBlk < fminf(ceilf(n / kSms) * mean, share + mean);
+        if (inside && lane == 0 && warp < 2) sh->cut[warp] = cut_before(prefix, pv, ws.pair_tokens, blockIdx.x + warp);
+        __syncthreads();                                     // the sums have been read
+        if (threadIdx.x == 0) {
             // The item that this part ends inside, if it began here: it goes on in the following parts whose own cuts lie inside it.
             Desc d = {0, 0, 0, 0};
             const Place end = sh->cut[1];
-            if (inside && end.b < pv.B && end.t > 0) {
-                const SeqState st = seq_state(pv, end.b);
-                const int tiles = pair_tiles(pv, st, end.pair, ws.pair_tokens);
-                if (end.t < tiles && end.w - end.t - kItemCost >= sh->cut[0].w) {
+            if (inside && end.b < pv.B && end.t > 0 && end.item >= sh->cut[0].w) {
+                const int tiles = pair_tiles(pv, seq_state(pv, end.b), end.pair, ws.pair_tokens);
+                if (end.t < tiles) {
                     d = Desc{end.b, end.h, end.pair, 2};
-                    const long long item_end = end.w - end.t + tiles;
-                    for (int k = blockIdx.x + 2; k < grid && item_end - total * k / grid > kSnap; ++k) ++d.pieces;
+                    for (int k = blockIdx.x + 2; k < kSms && tiles - tile_at((long long)((unsigned long long)total * k / (unsigned)kSms) - end.item) > kSnap; ++k) ++d.pieces;
                 }
             }
             ws.desc[blockIdx.x] = d;
+            sh->inside = inside;
         }
-        __syncthreads();                                     // the sums have been read
     }
     // rows that no query copy fills (G does not divide 128) are zero, so that their logits stay finite
     for (int x = threadIdx.x; x < 2 * Tile<D>::kHalves * (kBlk - tile_rows) * 8; x += kThreads) {
@@ -399,7 +406,7 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 
     if (warp == 0) {
         // ---- TMA producer: lane i copies box i -----------------------------------------------------
-        Walk walk(pv, ws.pair_tokens, sh->cut[0], sh->cut[1]);
+        Walk walk = sh->inside ? Walk(pv, ws.pair_tokens, sh->cut[0], sh->cut[1]) : Walk(pv, ws.pair_tokens);
         Job j;
         int kt = 0, n[2] = {0, 0}, jobs = 0, ok = 1;        // tiles so far, items of each stream, items
         // tells the others; behind the last job that there is none
@@ -569,6 +576,8 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const int X = (warp - kFirstSoftmaxWarp) >> 2;
         const int quarter = warp & 3;                      // TMEM lanes this warp may touch
         const int r = quarter * 32 + lane;                 // row in the tile = TMEM lane
+        const unsigned per = 65536u / G + 1;               // x / G = x * per >> 16 for a row x
+        auto token_of = [&](int x) { return (int)(x * per >> 16); };
         const uint32_t sp0 = tmem_base + X * 2 * kBlk + ((uint32_t)(quarter * 32) << 16), to = sp0 + kBlk;
         int cnt = 0;                                        // tiles of this stream so far
         for (int jobs = 0;; ++jobs) {
@@ -578,7 +587,7 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             if (j.t1 < 0) break;
             const int from = j.from[X], end = j.to[X], part = j.part;
             const int tok0 = X * tile_tokens;               // the stream's first token in the pair
-            const bool live = r < tile_rows && j.top + tok0 + r / G <= j.used;
+            const bool live = r < tile_rows && j.top + tok0 + token_of(r) <= j.used;
             if (from >= end) {
                 // a piece of the keys that holds nothing this stream sees: an empty partial result
                 if (part >= 0) ws.part_ml[(size_t)part * 2 * kBlk + X * kBlk + r] = make_float2(-INFINITY, 0.f);
@@ -587,7 +596,7 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 continue;
             }
             // near slots that the row sees: top - window .. top - 1 and the sinks; rows behind the chunk see what its last one does
-            const int top = min(j.top + tok0 + r / G, j.used);
+            const int top = min(j.top + tok0 + token_of(r), j.used);
             const int top_first = __shfl_sync(0xffffffffu, top, 0), top_last = __shfl_sync(0xffffffffu, top, 31);
             float m = INFINITY, l = 0.f;
             bool set = false;                               // every row of the warp has a reference
@@ -669,7 +678,8 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 // This lane stores piece lane & 3 of rows r0 .. r0 + 3
                 T *orow[4];
                 const int r0 = r & ~3;
-                int tk = tok0 + r0 / G, gk = r0 % G;
+                int tk = token_of(r0), gk = r0 - tk * G;
+                tk += tok0;
                 T *base = static_cast<T *>(a.out) + (int64_t)j.b * a.so.b + (lane & 3) * 8;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
@@ -695,7 +705,7 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     for (int k = 0; k < 4; ++k)
                         if (orow[k]) *reinterpret_cast<uint4 *>(orow[k] + c * 32) = w[k];
                 }
-                if (a.lse && live && done) a.lse[(((size_t)j.b * pv.H + j.h) * G + r % G) * pv.c + j.i0 + tok0 + r / G] = (m + log2f(l)) * 0.6931471805599453f;
+                if (a.lse && live && done) a.lse[(((size_t)j.b * pv.H + j.h) * G + r - token_of(r) * G) * pv.c + j.i0 + tok0 + token_of(r)] = (m + log2f(l)) * 0.6931471805599453f;
             } else if (A2SF_IN_RANGE(part, 2 * kSms, kDbgWindowTc)) {
                 float4 *po = reinterpret_cast<float4 *>(ws.part_o) + (size_t)part * (D / 4) * (2 * kBlk) + X * kBlk + r;
 #pragma unroll 1
@@ -817,6 +827,7 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
         !make_pool_map(&mv, dtype, a.pv.v, a.pv, a.pv.grain))
         return cudaErrorInvalidValue;
     const WinWs ws = carve(a.pv, a.ws, nullptr);
+    if ((long long)a.pv.B * a.pv.H * ((a.pv.c + ws.pair_tokens - 1) / ws.pair_tokens) > 0x7fffffff - 2 * kSms) return cudaErrorInvalidValue;
     if ((e = launch_chained(paged_window_tc_kernel<T, D>, kSms, kThreads, smem_bytes<D>(), s, mq, mk, mv, a, ws)) != cudaSuccess) return e;
     count_launch();
     if (!ws.cut) return cudaSuccess;
