@@ -134,7 +134,9 @@ EncodeTiledFn encode_fn()
 // 5e7: 14.9 and 12.4; 36 heads, 302 tokens, 2e8: 21.2 and 18.5; 8 heads, 928 tokens, 5e8: 32.1 and 31.7; 32 heads, 100 behind
 // 2,000, 9e8: 42 and 70.  One tile of 64 rows: 640 heads, 64 behind 100, 1e9: 71 and 52; 64 x 64 behind 4,000, 2e9: 83 and 96.
 enum Path { kFew, kTc, kMma };
-// Windowed, a row tile of tcgen05 (256 rows) sees the near capacity of its tokens and that is what counts.
+// Windowed, a row tile of tcgen05 (256 rows) sees the near capacity of its tokens and that is what counts; long items are cut, and one
+// row tile serves earlier (us, tcgen05 and mma.sync, bf16, d 128, kv heads x rows, window): 32 x 32, 1,024, 1.4e8: 28 and 16; 64 x
+// 40, 1,000, 3.5e8: 31 and 32; 32 x 64, 4,096, 1.1e9: 34 and 68; 32 x 100, 256, 1.6e8: 16 and 16; 48 x 244, 128, 3.7e8: 15 and 19.
 Path path_of(const PagedView &v, bool windowed, int dtype)
 {
     const int64_t rows = (int64_t)v.c * v.G;
@@ -142,7 +144,7 @@ Path path_of(const PagedView &v, bool windowed, int dtype)
     if (dtype == A2SF_F32) return kMma;
     const int tokens = 256 / v.G < v.c ? 256 / v.G : v.c;
     const double work = (double)v.B * v.H * rows * near_capacity(v, windowed, tokens) * v.d;
-    return work < (rows <= 64 ? 1.2e9 : 3e8) ? kMma : kTc;
+    return work < (rows > 64 ? 3e8 : windowed ? 4e8 : 1.2e9) ? kMma : kTc;
 }
 
 size_t attend_ws_bytes(const PagedView &v, bool windowed, int dtype)

@@ -40,9 +40,10 @@ constexpr float kRescaleThreshold = 8.0f;    // log2 units above the reference; 
 // 2^-24, so with 8 these are 2^-22 and 2^-32 of the maximum, and 64 logits that all equal it have half of the limit.
 template <typename T> constexpr float kBelow = std::is_same<T, __half>::value ? 8.f : 0.f;
 
-// Division of the list, in tiles: what an item costs beside its own (set-up, epilogue), what the merge kernel costs, and how near
-// an end of an item a cut goes to that end instead.
+// Division of the list, in tiles: what an item costs beside its own (set-up, epilogue), what the merge kernel costs, how near an
+// end of an item a cut goes to that end instead, and what a part has at least.
 constexpr int kItemCost = 2, kMergeCost = 4, kSnap = 2;
+constexpr int kMinPart = 6;                   // of the list
 constexpr int kItemSlots = kItemCost * kBlk + kBlk / 2;      // with what rounding to whole tiles adds
 constexpr int kCutBelow = 6 * kSms;          // items of a call (by its capacity) from which none is cut: the last round is short
 
@@ -131,11 +132,10 @@ __device__ __forceinline__ int tile_at(long long in) { return (int)((in - kItemS
 static_assert(kBlk == 128, "tile_at");
 
 // The cut before part k of the list.
-__device__ __forceinline__ Place cut_before(const long long *prefix, const PagedView &pv, int pair_tokens, int k)
+__device__ __forceinline__ Place cut_before(const long long *prefix, const PagedView &pv, int pair_tokens, int k, int parts)
 {
-    const unsigned long long total = pv.H * prefix[pv.B];
-    const long long w = (long long)(total * k / (unsigned)kSms);
-    if (w >= (long long)total) return Place{pv.B, 0, 0, 0, w, w};
+    const long long total = pv.H * prefix[pv.B], w = total * k / parts;
+    if (k >= parts) return Place{pv.B, 0, 0, 0, total, total};
     int lo = 0, hi = pv.B - 1;                               // last b with H * prefix[b] <= w
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -366,9 +366,10 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         long long *prefix = reinterpret_cast<long long *>(smem);
         sum_lengths(prefix, &sh->items, pv, ws.pair_tokens);
         const long long total = pv.H * prefix[pv.B];
-        const float n = (float)pv.H * (float)sh->items, mean = n > 0.f ? (float)total / n : 0.f, share = (float)total / kSms;
-        const bool inside = share >= 8.f * kBlk && share + (kItemCost + kMergeCost) * kBlk < fminf(ceilf(n / kSms) * mean, share + mean);
-        if (inside && lane == 0 && warp < 2) sh->cut[warp] = cut_before(prefix, pv, ws.pair_tokens, blockIdx.x + warp);
+        const int parts = (int)max(1ll, min((long long)kSms, total / (kMinPart * kBlk)));
+        const float n = (float)pv.H * (float)sh->items, mean = n > 0.f ? (float)total / n : 0.f;
+        const bool inside = (float)total / parts + (kItemCost + kMergeCost) * kBlk < fminf(ceilf(n / kSms) * mean, (float)total / kSms + mean);
+        if (inside && lane == 0 && warp < 2) sh->cut[warp] = cut_before(prefix, pv, ws.pair_tokens, blockIdx.x + warp, parts);
         __syncthreads();                                     // the sums have been read
         if (threadIdx.x == 0) {
             // The item that this part ends inside, if it began here: it goes on in the following parts whose own cuts lie inside it.
@@ -378,7 +379,7 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const int tiles = pair_tiles(pv, seq_state(pv, end.b), end.pair, ws.pair_tokens);
                 if (end.t < tiles) {
                     d = Desc{end.b, end.h, end.pair, 2};
-                    for (int k = blockIdx.x + 2; k < kSms && tiles - tile_at((long long)((unsigned long long)total * k / (unsigned)kSms) - end.item) > kSnap; ++k) ++d.pieces;
+                    for (int k = blockIdx.x + 2; k < parts && tiles - tile_at(total * k / parts - end.item) > kSnap; ++k) ++d.pieces;
                 }
             }
             ws.desc[blockIdx.x] = d;
