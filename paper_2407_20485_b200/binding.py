@@ -48,9 +48,7 @@ class a2sf_rotary_axes_plan(ctypes.Structure):
                 ("check", ctypes.c_int32), ("axes", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("turn", ctypes.c_uint64 * 64), ("axis", ctypes.c_uint8 * 64)]
 
-    def __init__(self, *args):
-        super().__init__(*args)
-        self.at = ctypes.addressof(self)        # what the calls pass on
+    at = property(ctypes.addressof)             # what the calls pass on
 
 
 class a2sf_paged(ctypes.Structure):

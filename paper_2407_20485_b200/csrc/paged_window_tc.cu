@@ -404,6 +404,12 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         if (*abort_flag) return false;
         return mbar_wait(bar, parity, abort_flag);
     };
+    // For jobs: the next one is made known, and an old one's place free, only when the one before is done, which may be long.
+    auto wait_job = [&](uint64_t *bar, uint32_t parity) -> bool {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*abort_flag) return false;
+        return mbar_wait(bar, parity, abort_flag, 64 * kWaitCycles);
+    };
 
     if (warp == 0) {
         // ---- TMA producer: lane i copies box i -----------------------------------------------------
@@ -414,7 +420,7 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         auto publish = [&](bool any) {
             if (lane == 0) {
                 const int slot = jobs % kJobs;
-                ok = jobs < kJobs || wait(&sh->job_empty[slot], ((jobs / kJobs) & 1) ^ 1) ? 1 : 0;
+                ok = jobs < kJobs || wait_job(&sh->job_empty[slot], ((jobs / kJobs) & 1) ^ 1) ? 1 : 0;
                 if (ok) {
                     JobInfo &x = sh->jobs[slot];
                     x.t1 = -1;
@@ -504,7 +510,7 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         int kt = 0, n = 0, cnt = 0;                         // tiles of all, items and tiles of this stream
         for (int jobs = 0;; ++jobs) {
             const int slot = jobs % kJobs;
-            if (__any_sync(0xffffffffu, !wait(&sh->job_full[slot], (jobs / kJobs) & 1))) break;
+            if (__any_sync(0xffffffffu, !wait_job(&sh->job_full[slot], (jobs / kJobs) & 1))) break;
             const JobInfo &j = sh->jobs[slot];
             const int t0 = j.t0, t1 = j.t1, from = j.from[X], to = j.to[X], used = j.used, dead = j.dead;
             if (t1 < 0) break;
@@ -583,7 +589,7 @@ paged_window_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         int cnt = 0;                                        // tiles of this stream so far
         for (int jobs = 0;; ++jobs) {
             const int slot = jobs % kJobs;
-            if (__any_sync(0xffffffffu, !wait(&sh->job_full[slot], (jobs / kJobs) & 1))) break;
+            if (__any_sync(0xffffffffu, !wait_job(&sh->job_full[slot], (jobs / kJobs) & 1))) break;
             const JobInfo &j = sh->jobs[slot];
             if (j.t1 < 0) break;
             const int from = j.from[X], end = j.to[X], part = j.part;

@@ -140,6 +140,15 @@ WIN = [
     (1, 1, 7, 128, BF, 16, [2500], 41, None, 1000, 7, "bhnd", 0.0),
     (2, 3, 1, 128, HF, 128, [640, 1], 513, [513, 512], 128, 0, "bhnd", 0.0),
 ]
+MANY = [                                                                       # few rows of more units than fit at once, and long windows of few units
+    (40, 8, 1, 128, BF, 16, [300 + 7 * (b % 9) for b in range(40)], 1, [b % 5 and 1 for b in range(40)], 100, 5, "bhnd", 0.0),
+    (40, 8, 2, 64, HF, 64, [90 + 100 * (b % 8) for b in range(40)], 3, [3, 2, 0, 1] * 10, 700, 33, "bnhd", 0.0),
+    (20, 8, 1, 128, FP, 32, [600 - 29 * b for b in range(20)], 1, None, 250, 20, "bhnd", 0.0),
+    (20, 9, 4, 64, FP, 16, [b * 20 for b in range(20)], 2, [2, 1, 0, 2, 2] * 4, 90, 0, "bnhd", 0.0),
+    (100, 3, 4, 128, BF, 16, [20 * (b % 30) for b in range(100)], 4, [4, 0, 3, 1] * 25, 64, 16, "bhnd", 0.0),
+    (1, 2, 3, 128, HF, 16, [9000], 5, None, 7000, 31, "bhnd", 0.0),
+    (1, 3, 2, 64, FP, 32, [5000], 4, None, 4000, 1, "bnhd", 0.0),
+]
 LARGE = [                                                                      # tcgen05: direct, and with pieces and merge
     (4, 12, 2, 128, BF, 16, [0, 700, 3, 1500], 400, [400, 399, 0, 130], 150, 4, "bnhd", 0.0),
     (4, 12, 2, 64, HF, 128, [0, 700, 3, 1500], 400, [400, 1, 77, 256], 1, 0, "bhnd", 0.0),
@@ -149,14 +158,17 @@ LARGE = [                                                                      #
     (1, 5, 3, 128, HF, 16, [2000], 700, None, 129, 33, "bnhd", 0.0),
     (2, 6, 8, 128, BF, 64, [0, 50], 500, [500, 450], 100000, 0, "bhnd", 0.0),
     (6, 20, 1, 128, BF, 64, [0, 10, 2000, 0, 5, 1], 600, [600, 0, 600, 33, 599, 256], 500, 16, "bhnd", 0.0),
+    (1, 4, 4, 128, HF, 64, [5000], 64, None, 4096, 4, "bhnd", 0.0),             # items longer than a part
+    (2, 3, 8, 64, BF, 16, [9000, 20], 40, [40, 33], 8000, 0, "bnhd", 0.0),
+    (60, 8, 1, 128, BF, 32, [b % 7 * 50 for b in range(60)], 130, [130 - 2 * b for b in range(60)], 40, 2, "bhnd", 0.0),      # rounds of whole items
 ]
 
 
 def ident(c):
-    return "-".join(str(x).replace("torch.", "").replace(" ", "") for x in c)
+    return "-".join(str(x).replace("torch.", "").replace(" ", "")[:40] for x in c)
 
 
-@pytest.mark.parametrize("case", WIN + LARGE, ids=ident)
+@pytest.mark.parametrize("case", WIN + MANY + LARGE, ids=ident)
 def test_window(a2sf, case):
     cache, qc, L, out, lse = check_window(a2sf, case)
     # the same call again, without lse given: the same bits

@@ -160,6 +160,15 @@ def test_the_plan_gives_every_pair_its_axis_and_frequency(a2sf, pairs, cycle, ea
     assert pu.inv_freq(8)[0] == 1.0
 
 
+def test_a_copied_plan_is_a_plan_of_its_own(a2sf):
+    import copy
+
+    plan = _plan(a2sf)
+    other = copy.copy(plan)
+    assert other.at == ctypes.addressof(other) != plan.at and bytes(other) == bytes(plan)
+    assert _append(a2sf, _paged(a2sf, d=64), other) == INVALID           # read as a plan: rotary_dim > d
+
+
 def test_bad_rotations_with_several_axes(a2sf):
     plan = _plan(a2sf, (8, 12, 12))
 
