@@ -16,7 +16,12 @@
 //   joins.  The list is not written down: a CTA sums the lengths itself and finds its own place.
 //
 // What binds: one exponential per logit, 16 a clock and SM, and 128 x 128 x d x 4 operations of a tile at 8192 a clock: 2048 clocks
-// each for a pair of tiles, d = 128.
+// each for a pair of tiles, d = 128, which takes 3,500 to 3,900: of 1,730 for half a tile of one stream 1,120 are its exponentials,
+// which the other stream's slow down, 200 the wait for logits, the rest latencies between (S as one product of 128 columns, after all of
+// P: 5,200).  The tensor pipe is active for 49 % of the time, the special-function unit for 47 % (2048 tokens, window 4096).  Long runs
+// are held by the board's power: 156 us in the first 20 ms, 168 us at 1000 W and 1.6 GHz.  A CTA's first item waits 5,000 to 7,000
+// clocks for its first logits, and an epilogue takes 5,000, most of it the first pass through its instructions, so code is kept short:
+// short items are bound by these (8 ragged prompts, window 512: 49 us, of which a CTA's 10 to 15 tiles take 20 to 27).
 // P as one term of the storage type, as without a window: every product is off by at most half a step.
 #include <type_traits>
 
@@ -40,9 +45,11 @@ constexpr float kRescaleThreshold = 8.0f;    // log2 units above the reference; 
 // 2^-24, so with 8 these are 2^-22 and 2^-32 of the maximum, and 64 logits that all equal it have half of the limit.
 template <typename T> constexpr float kBelow = std::is_same<T, __half>::value ? 8.f : 0.f;
 
-// Division of the list, in tiles: what an item costs beside its own (set-up, epilogue), what the merge kernel costs, how near an
-// end of an item a cut goes to that end instead, and what a part has at least.
-constexpr int kItemCost = 2, kMergeCost = 4, kSnap = 2;
+// Division of the list, in tiles: what an item costs beside its own (set-up, epilogue), what cutting must gain, how near an end of an
+// item a cut goes to that end instead, and what a part has at least.  The merge kernel takes the time of 3 to 4 tiles, but SMs that
+// idle in the last round leave power to the others (us, cut and whole, in long runs under the power cap: 256 items of 35 tiles 178 and
+// 168; 192 of 34: 119 and 150; 160 of 18: 67 and 85).
+constexpr int kItemCost = 2, kMergeCost = 10, kSnap = 2;
 constexpr int kMinPart = 6;                   // of the list
 constexpr int kItemSlots = kItemCost * kBlk + kBlk / 2;      // with what rounding to whole tiles adds
 constexpr int kCutBelow = 6 * kSms;          // items of a call (by its capacity) from which none is cut: the last round is short
