@@ -9,7 +9,7 @@
 //   of its own: while one stream waits for products the other's exponentials run.  P goes to the products in halves of 64 keys.
 //   A row's reference (what is subtracted before the exponential) stays where it is unless a row sum shows that a probability
 //   may have left fp16's range: then the half is done again against the row's maximum and the accumulator rescaled.  Until
-//   a row has seen a slot its reference is unset, +inf.  Blocks of 32 rows x 32 slots that no row of theirs sees cost no exponential.
+//   a row has seen a slot its reference is unset, +inf.  A half of which no row of a warp sees anything costs it no exponential.
 //
 //   All items of a call are about as long as the window, so they are dealt in turn.  Where there are few, their tiles are one list, of
 //   which every CTA takes an equal part, and a part that begins or ends inside an item leaves partial results that the merge kernel
