@@ -137,10 +137,13 @@ enum Path { kFew, kTc, kMma };
 // Windowed, a row tile of tcgen05 (256 rows) sees the near capacity of its tokens and that is what counts; long items are cut, and one
 // row tile serves earlier (us, tcgen05 and mma.sync, bf16, d 128, kv heads x rows, window): 32 x 32, 1,024, 1.4e8: 28 and 16; 64 x
 // 40, 1,000, 3.5e8: 31 and 32; 32 x 64, 4,096, 1.1e9: 34 and 68; 32 x 100, 256, 1.6e8: 16 and 16; 48 x 244, 128, 3.7e8: 15 and 19.
+// In 32 bits the few-row kernels, on the CUDA cores, take more than the bytes' time from 8 rows on, and mma.sync can cut a window's keys
+// (few rows and mma.sync: 99 heads x 13 rows, 556: 62 and 26; 8 x 16, 8,192: 57 and 38; 8 x 16, 300: 15.5 and 9.5; 32 x 8, 1,024: 18
+// and 18; 256 x 8, 300: 37 and 73).
 Path path_of(const PagedView &v, bool windowed, int dtype)
 {
     const int64_t rows = (int64_t)v.c * v.G;
-    if (rows <= kFewRows) return kFew;
+    if (rows <= (windowed && dtype == A2SF_F32 ? kFewRows / 2 : kFewRows)) return kFew;
     if (dtype == A2SF_F32) return kMma;
     const int tokens = 256 / v.G < v.c ? 256 / v.G : v.c;
     const double work = (double)v.B * v.H * rows * near_capacity(v, windowed, tokens) * v.d;
