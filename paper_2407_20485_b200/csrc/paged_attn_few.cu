@@ -1231,7 +1231,8 @@ template <typename F> auto with_form(int dtype, const PagedView &pv, F f)
 
 template <bool Win, typename T, int D, int NC> cudaError_t launch(Form<T, D, NC>, int dtype, const AttendArgs &a, cudaStream_t s)
 {
-    return launch_nc<T, D, NC, Win>(dtype, a, s);
+    if constexpr (Win && sizeof(T) == 4 && NC == kFewRows) return cudaErrorInvalidValue;      // mma.sync has these
+    else return launch_nc<T, D, NC, Win>(dtype, a, s);
 }
 template <typename T, int D, int NC> int ranks_of(Form<T, D, NC>, const PagedView &pv) { return cluster_ranks<T, D, NC>(pv); }
 

@@ -459,6 +459,12 @@ def test_the_largest_batch_with_mostly_empty_sequences(a2sf):
     check_window(a2sf, (B, 1, 1, 64, HF, 16, past, 20, lens, 20, 3, "bhnd", 0.0))
 
 
+@pytest.mark.parametrize("B,H,c,dtype,lens", [(300, 2, 140, BF, [140, 0, 17, 139, 1]), (1024, 1, 300, HF, [0] * 60 + [300, 0, 129, 1])])
+def test_many_sequences_in_large_chunks(a2sf, B, H, c, dtype, lens):
+    """The list of items over hundreds of sequences, most of them short or empty."""
+    check_window(a2sf, (B, H, 1, 64, dtype, 16, [b % 13 for b in range(B)], c, [lens[b % len(lens)] for b in range(B)], 50, 3, "bhnd", 0.0))
+
+
 @pytest.mark.parametrize("dtype,H,c", [(FP, 2, 3), (BF, 2, 1), (HF, 12, 300), (BF, 2, 40), (BF, 2, 4)])
 @pytest.mark.parametrize("bad", [-1, -2 ** 31, 2 ** 31 - 1, "pages", "past", "negative", "length"])
 def test_bad_pages_and_lengths_are_reported_and_not_followed(a2sf, dtype, H, c, bad):
