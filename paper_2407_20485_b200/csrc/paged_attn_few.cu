@@ -707,7 +707,7 @@ drained:
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float2 y = ml[w * NP + ct];
-                l += y.y > 0.f ? ex2(y.x - mx) * y.y : 0.f;
+                l += y.y != 0.f ? ex2(y.x - mx) * y.y : 0.f;     // 0: saw nothing; a NaN stays one, also beside no maximum
             }
             const float z = mx + log2f(l);
             const int i = ct / pv.G, g = ct - i * pv.G;
@@ -891,7 +891,7 @@ paged_few_cluster_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float2 y = ml[w * NP + r];
-                if (!(y.y > 0.f)) continue;                  // a warp that saw nothing wrote no output
+                if (y.y == 0.f) continue;                    // a warp that saw nothing wrote no output; a NaN stays one
                 const float f = ex2(y.x - mx);
                 const float4 v = reinterpret_cast<const float4 *>(o + (size_t)(w * NP + r) * D)[d4];
                 l = fmaf(f, y.y, l);
@@ -920,7 +920,7 @@ paged_few_cluster_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
             for (int k = 0; k < kRanks; ++k) {
                 if (k >= ranks) continue;
                 const float4 v = remote4(remote(joined + r * D + d4 * 4, k));
-                const float f = y[k].y > 0.f ? ex2(y[k].x - mx) : 0.f;
+                const float f = y[k].y != 0.f ? ex2(y[k].x - mx) : 0.f;
                 l = fmaf(f, y[k].y, l);
                 sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y);
                 sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
@@ -1063,7 +1063,7 @@ paged_few_finish_kernel(const __grid_constant__ AttendArgs a, const __grid_const
         for (int o = LR / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         for (int p = l0; p < parts; p += LR) {
             const float2 x = row[p * part_step];
-            l += x.y > 0.f ? ex2(x.x - mx) * x.y : 0.f;
+            l += x.y != 0.f ? ex2(x.x - mx) * x.y : 0.f;     // as in the whole-unit kernel
         }
 #pragma unroll
         for (int o = LR / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
