@@ -532,10 +532,10 @@ def a2sf_rotary_axes_plan_init(pairs, plans, cycle: bool = False) -> a2sf_rotary
 
 
 def _axes_plan(plan) -> int:
-    try:
-        return plan.at
-    except AttributeError:
-        raise ValueError(f"expected a plan of a2sf_rotary_axes_plan_init, got {type(plan).__name__}") from None
+    """Its address, which the calls read before the library checks the plan."""
+    if not isinstance(plan, a2sf_rotary_axes_plan):
+        raise ValueError(f"expected a plan of a2sf_rotary_axes_plan_init, got {type(plan).__name__}")
+    return plan.at
 
 
 def a2sf_rotary_axes(plan: a2sf_rotary_axes_plan, x, positions, out=None, lens=None, transpose=False, stream=None):
