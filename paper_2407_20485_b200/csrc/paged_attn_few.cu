@@ -875,7 +875,7 @@ paged_few_cluster_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
             if (!*abort_flag && !mbar_wait(&full[s], (it / R::kStages) & 1, abort_flag)) *pv.status = A2SF_ERR_TIMEOUT;
             const int j0 = t * kTile + cw * kSlots;
             uint8_t *K = ring + (size_t)s * 2 * R::kTileBytes;
-            if (j0 < used) body.tile(a, K, K + R::kTileBytes, cw * kSlots, j0, used, nullptr, NP, scratch);
+            if (j0 < used && A2SF_IN_RANGE(j0, pv.max_pages << pv.ps_shift, kDbgPagedFew)) body.tile(a, K, K + R::kTileBytes, cw * kSlots, j0, used, nullptr, NP, scratch);
             __syncwarp();
             if (lane == 0) mbar_arrive(&empty[s]);
         }
@@ -908,6 +908,7 @@ paged_few_cluster_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
         const int rows = st.len * pv.G;                      // 0 where the sequence takes no part
         for (int e = rank * kConsumers + (int)threadIdx.x - 32; e < rows * (D / 4); e += ranks * kConsumers) {
             const int r = e / (D / 4), d4 = e - r * (D / 4);
+            if (!A2SF_IN_RANGE(r, NP, kDbgPagedFew) || !A2SF_IN_RANGE(r / pv.G, pv.c, kDbgPagedFew) || !A2SF_IN_RANGE(x.b, pv.B, kDbgPagedFew)) continue;
             float2 y[kRanks];
             float mx = -INFINITY, l = 0.f;
 #pragma unroll

@@ -30,7 +30,7 @@ def attend(a2sf, cache, q, window, sinks, lens=None, out=None, lse=None):
     """One call -> out, lse and its form."""
     c, fp32 = q.shape[2], cache.dtype == torch.float32
     size = cache.attend_window_workspace_bytes(c, window, sinks)
-    ws = a2sf.torch.zeros((size,), dtype=torch.uint8, device="cuda")
+    ws = a2sf.torch.empty((size,), dtype=torch.uint8, device="cuda").zero_()      # the binding's torch: in the debug sweep it puts guard words around
     before = a2sf.a2sf_kernel_launch_count()
     out, lse = cache.a2sf_paged_attend_window(q, window, sinks, lens=lens, out=out, lse=lse, workspace=ws)
     launches = a2sf.a2sf_kernel_launch_count() - before
