@@ -8,7 +8,7 @@ from pathlib import Path
 import pytest
 
 ROOT = Path(__file__).resolve().parent.parent
-FORM_TESTS = ["tests/test_window_nan_gpu.py", "tests/test_window_precision_gpu.py"]
+FORM_TESTS = ["tests/test_window_nan_gpu.py", "tests/test_window_precision_gpu.py", "tests/test_window_chunk_kernel_gpu.py"]
 
 
 def test_every_kernel_of_few_rows_checks_its_own_indexes():
