@@ -96,18 +96,13 @@ PagedView make_view(const a2sf_paged *p, int c, const int32_t *lens)
     return v;
 }
 
-// Slots that lie together in the list of what a windowed call sees, and in one box of a copy (us with 16, 32, 64, 128: one token over
-// 32 x 40 windows of 2048 201, 204, 206, 205; four tokens 35.2, 35.4, 36.5, 36.6; prompts, window 512, 60.3, 60.4, 59.8, 59.7).
-constexpr int kGrain = 16;
-
 PagedView make_window_view(const a2sf_paged *p, int c, const int32_t *lens, int window, int sinks)
 {
     PagedView v = make_view(p, c, lens);
     const int cap = p->max_pages * p->page_size;              // nothing is beyond it
-    v.grain = kGrain < p->page_size ? kGrain : p->page_size;
     v.window = window < cap ? window : cap;
     v.sinks = sinks < cap ? sinks : cap;
-    v.sink_end = (v.sinks + v.grain - 1) / v.grain * v.grain;
+    v.sink_end = (v.sinks + kGrain - 1) / kGrain * kGrain;
     return v;
 }
 

@@ -1156,7 +1156,7 @@ cudaError_t launch_nc(int dtype, const AttendArgs &a, cudaStream_t s)
     cudaError_t e = allow_dynamic_smem<paged_few_kernel<T, D, NC, Win>>(smem);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv;
-    const int row = Win ? a.pv.grain : a.pv.ps, box = row < R::kTile ? row : R::kTile;
+    const int row = Win ? kGrain : a.pv.ps, box = row < R::kTile ? row : R::kTile;
     if (!make_pool_map(&mk, dtype, a.pv.k, a.pv, box) || !make_pool_map(&mv, dtype, a.pv.v, a.pv, box)) return cudaErrorInvalidValue;
     const int NP = rows_padded(a.pv.c * a.pv.G);
     if constexpr (Win) {

@@ -79,7 +79,7 @@ struct Lengths {
     long long past, full;        // full: C
     int pair_tokens, pairs, early, tail;                     // tail: tokens that the last pair lacks
 
-    __device__ Lengths(const PagedView &pv, const SeqState &st, int pt) : past(st.past), full((long long)pt + pv.window - 1 + pv.sink_end + pv.grain / 2), pair_tokens(pt)
+    __device__ Lengths(const PagedView &pv, const SeqState &st, int pt) : past(st.past), full((long long)pt + pv.window - 1 + pv.sink_end + kGrain / 2), pair_tokens(pt)
     {
         pairs = pair_count(st, pt);
         const long long e = (full - 1 - past) / pt;
@@ -837,8 +837,8 @@ cudaError_t launch(int dtype, const AttendArgs &a, cudaStream_t s)
     cudaError_t e = allow_dynamic_smem<paged_window_tc_kernel<T, D>>(smem_bytes<D>());
     if (e != cudaSuccess) return e;
     CUtensorMap mq, mk, mv;
-    if (!make_query_map(&mq, dtype, a.q, a.pv, a.sq) || !make_pool_map(&mk, dtype, a.pv.k, a.pv, a.pv.grain) ||
-        !make_pool_map(&mv, dtype, a.pv.v, a.pv, a.pv.grain))
+    if (!make_query_map(&mq, dtype, a.q, a.pv, a.sq) || !make_pool_map(&mk, dtype, a.pv.k, a.pv, kGrain) ||
+        !make_pool_map(&mv, dtype, a.pv.v, a.pv, kGrain))
         return cudaErrorInvalidValue;
     const WinWs ws = carve(a.pv, a.ws, nullptr);
     if ((long long)a.pv.B * a.pv.H * ((a.pv.c + ws.pair_tokens - 1) / ws.pair_tokens) > 0x7fffffff - 2 * kSms) return cudaErrorInvalidValue;
