@@ -760,11 +760,15 @@ drained:
 // ---- windowed, few units: a cluster per unit ---------------------------------------------------------
 // What a unit sees is bounded, so where there are no more units than CTAs fit at once, the CTAs of a cluster share the tiles of one
 // unit evenly, and it is joined through their shared memory: no partial results in the workspace, no second kernel (us, split list
-// with finish kernel and clusters, bf16: 32 heads x 205 slots 7.1 and 6.0; 32 x 1,024: 10.8 and 8.2; 256 x 4,096: 88 and 82; 64 x
-// 4,224 of fp16, 16 rows: 34 and 28).  Where clusters leave half of the device idle the list is faster once a CTA has more than a
-// few tiles (8 x 4,096: 12.6 and 13.3; 8 x 8,192: 14 and 21; 8 x 8,192 of 32 bits, 16 rows: 57 and 106).
+// with finish kernel and clusters, bf16: 32 heads x 205 slots 7.1 and 6.0; 32 x 1,024: 10.8 and 8.2; 32 x 4,096: 18.0 and 15.8; 64 x
+// 4,224 of fp16, 16 rows: 34 and 29).  The list divides what is there, a cluster has its unit's tiles whatever the others have.  So the list
+// serves calls whose clusters would leave a quarter of the device idle (38 x 4,096: 19.5 and 20.7; 32 bits, 38 x 4,096: 36 and 52; 75 x
+// 4,096: 62 and 98) and long parts of a unit, which one of two sequences in a batch of short ones would make all wait for (32 x 8 units,
+// two sequences at 4,096 and the others below 100, parts of 64 tiles: 18.5 and 62, where 256 full units take 89 and 81; 8 x 8
+// units, one sequence at 4,096, parts of 16: 13.3 and 19.6).
 constexpr int kRanks = 8;                    // CTAs of a cluster at most
-constexpr int kRankTiles = 8;                // tiles of a CTA at most, in half-empty devices
+constexpr int kRankTiles = 8;                // tiles of a CTA at most, whatever stays idle
+constexpr int kMostRankTiles = 20;           // ... with a full device
 
 __device__ __forceinline__ void cluster_sync()
 {
@@ -941,7 +945,12 @@ paged_few_cluster_kernel(const __grid_constant__ CUtensorMap map_k, const __grid
 }
 
 // CTAs of a cluster, or 0 where the other forms serve: as many as fit at once, each with a tile at least.  What fits is counted for
-// the whole chip, since the size of the workspace, which clusters do without, must not depend on a device.
+// the whole chip, since the size of the workspace, which clusters do without, must not depend on a device.  A cluster stays inside one of the
+// chip's parts, which leave some SMs over: of one and of two CTAs an SM 74 and 148 clusters of 2 fit, 33 and 71 of 4, 15 and 33 of 8
+// (one more than fit, 32 bits, 16 x 4,096 slots: 34 us where 14 units take 18).
+constexpr int clusters_fit(int slots, int ranks) { return (ranks > 2 ? slots - 5 * (ranks - 1) : slots) / ranks; }
+static_assert(clusters_fit(kSms, 4) == 33 && clusters_fit(2 * kSms, 4) == 70 && clusters_fit(kSms, 8) == 14 && clusters_fit(2 * kSms, 8) == 32, "at most what fits");
+
 template <typename T, int D, int NC> int cluster_ranks(const PagedView &pv)
 {
     constexpr size_t smem = Ring<T, D>::kBytes + BodyOf<T, D, NC, true>::kScratch;
@@ -950,8 +959,9 @@ template <typename T, int D, int NC> int cluster_ranks(const PagedView &pv)
     const int tiles = (near_capacity(pv, true, pv.c) + Ring<T, D>::kTile - 1) / Ring<T, D>::kTile;
     if (units > slots) return 0;
     int ranks = 1;
-    while (ranks < kRanks && 2 * units * ranks <= slots && 2 * ranks <= tiles) ranks *= 2;
-    return 2 * units * ranks < slots && (tiles + ranks - 1) / ranks > kRankTiles ? 0 : ranks;
+    while (ranks < kRanks && units <= clusters_fit(slots, 2 * ranks) && 2 * ranks <= tiles) ranks *= 2;
+    const int most = 4 * units * ranks < 3 * slots ? kRankTiles : kMostRankTiles;
+    return (tiles + ranks - 1) / ranks > most ? 0 : ranks;
 }
 
 // The finish kernel: `blocks` blocks per unit.  Block y joins the output rows y, y + blocks, .. and brings the
