@@ -531,9 +531,17 @@ int a2sf_paged_attend(const a2sf_paged *cache, int32_t c, const int32_t *lens, f
  * Scores are neither read nor written: what a token outside the window gets is zero from then on, so that age alone decides what
  * stays (a2sf_paged_slide).  Page-table entries whose page holds no slot that a row of the call sees are not read, and slots of
  * other pages that no row sees may hold anything.  out has strides of its own and must not overlap q; rows i >= len[b] of out
- * and lse are left as they were.  workspace: as for a2sf_paged_attend, from a2sf_paged_attend_window_workspace_bytes (0 = invalid
- * arguments); its size follows min(sinks + window + c, the capacity of the page table), and a call whose size is
- * A2SF_NO_WORKSPACE_BYTES neither reads nor writes it. */
+ * and lse are left as they were.
+ * Logits, sums and outputs are held in 32 bits.  In the products with values a probability of 32-bit storage keeps 22 bits at least;
+ * of 16-bit storage it is two terms of that type, but one term in calls of some 3e8 multiply-adds of Q K^T and more, which are the tensor cores':
+ * there a row of out may be off by half a step of sum P |V| beside its own rounding.  a2sf_paged_attend does the same.
+ * workspace: as for a2sf_paged_attend, from a2sf_paged_attend_window_workspace_bytes (0 = invalid arguments).  It holds partial
+ * results of rows whose keys are cut into pieces; the capacity of the page table beyond sinks + window + c slots does not add to it.
+ *   c * group <= 16 (8 in 32-bit storage): none where few heads and sequences have short windows, else what B * H
+ *     + 512 pieces take, 4 to 8 times the rows' (4 d + 8) bytes each (rows rounded up to a power of two).
+ *   more rows: none, or what the pieces take, up to 20 MB; 20 MB (d 64) or 39 MB for large chunks of 16-bit storage with fewer than 888
+ *     pairs of row tiles, whether or not the lengths on the device lead to cuts.
+ * A call whose size is A2SF_NO_WORKSPACE_BYTES neither reads nor writes it. */
 #define A2SF_NO_WORKSPACE_BYTES 256
 size_t a2sf_paged_attend_window_workspace_bytes(const a2sf_paged *cache, int32_t c, int32_t window, int32_t sinks);
 int a2sf_paged_attend_window(const a2sf_paged *cache, int32_t c, const int32_t *lens, int32_t window, int32_t sinks,

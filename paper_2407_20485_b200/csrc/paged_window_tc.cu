@@ -18,11 +18,15 @@
 // What binds: one exponential per logit, 16 a clock and SM, and 128 x 128 x d x 4 operations of a tile at 8192 a clock: 2048 clocks
 // each for a pair of tiles, d = 128, which takes 3,500 to 3,900: of 1,730 for half a tile of one stream 1,120 are its exponentials,
 // which the other stream's slow down, 200 the wait for logits, the rest latencies between (S as one product of 128 columns, after all of
-// P: 5,200).  The tensor pipe is active for 49 % of the time, the special-function unit for 47 % (2048 tokens, window 4096).  Long runs
+// P: 5,200).  The tensor pipe is active for 50 % of the time, the special-function unit for 49 % (2048 tokens, window 4096).  Long runs
 // are held by the board's power: 156 us in the first 20 ms, 168 us at 1000 W and 1.6 GHz.  A CTA's first item waits 5,000 to 7,000
 // clocks for its first logits, and an epilogue takes 5,000, most of it the first pass through its instructions, so code is kept short:
-// short items are bound by these (8 ragged prompts, window 512: 49 us, of which a CTA's 10 to 15 tiles take 20 to 27).
-// P as one term of the storage type, as without a window: every product is off by at most half a step.
+// short items are bound by these (8 prompts of 2048 and 125 to 265 tokens, window 512: 49 us, of which a CTA's 10 to 15 tiles take
+// 20 to 27).
+// P as one term of the storage type, as in the tcgen05 form without a window: a product is off by half a step at most, which adds to
+// what rounding the output costs (error against 64 bits, of the output's norm: 2048 tokens, window 4096, bf16 1.69e-3 where rounding alone is
+// 1.65e-3; 8 prompts, window 512, fp16 2.20e-4 and 2.04e-4).  A second term behind the first in tensor memory, as the forms for
+// fewer rows have it, brings the error down to the rounding's and takes 167 -> 214 us and 51 -> 59.
 #include <type_traits>
 
 #include "paged_tc.cuh"
